@@ -1,0 +1,224 @@
+"""Binding of include/fiona_adapter.h: low-rank adapters of many requests beside
+a shared projection, and dropout whose mask is never stored (argument
+marshalling only; the arithmetic and the mask are defined in the header).
+
+Tensors are torch tensors on the context's device, rows with any stride and
+contiguous columns; adapter weights and their gradients are contiguous.  As
+everywhere in this package, `stream` is a torch stream, a handle, or None for
+the legacy default stream.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Any, Optional, Sequence
+
+import numpy as np
+
+from . import fiona as F
+
+FIONA_F32, FIONA_F16, FIONA_BF16 = 0, 1, 2
+MAX_RANK = 128
+
+EXPORTED = ("fiona_adapter_batch_create", "fiona_adapter_batch_destroy", "fiona_adapter_work_bytes",
+            "fiona_adapter_forward", "fiona_adapter_backward", "fiona_dropout")
+
+
+class _Layer(ctypes.Structure):
+    _fields_ = [("d_in", ctypes.c_uint32), ("d_out", ctypes.c_uint32), ("dtype", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p)]
+
+
+class _DropoutSpec(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("p", ctypes.c_double)]
+
+
+_lib: Optional[ctypes.CDLL] = None
+
+
+def lib() -> ctypes.CDLL:
+    global _lib
+    if _lib is None:
+        L = F.lib()
+        p, u32, u64, i32 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int
+        L.fiona_adapter_batch_create.argtypes = [p, u32, p, p, u32, p, p, u32, ctypes.POINTER(p)]
+        L.fiona_adapter_batch_destroy.argtypes = [p]
+        L.fiona_adapter_batch_destroy.restype = None
+        L.fiona_adapter_work_bytes.argtypes = [p, u32, u32, u32, ctypes.POINTER(u64)]
+        L.fiona_adapter_forward.argtypes = [p, p, p, p, u64, p, u64, p, u64, p, p, p, u64]
+        L.fiona_adapter_backward.argtypes = [p, p, p, p, u64, p, p, u64, p, u64, p, u64, p, p, p, p, u64]
+        L.fiona_dropout.argtypes = [p, p, u32, u64, u64, p, u64, p, u64, p, u64, p]
+        for name in EXPORTED:
+            if name != "fiona_adapter_batch_destroy":
+                getattr(L, name).restype = i32
+        _lib = L
+    return _lib
+
+
+_dtypes: Optional[dict] = None
+
+
+def _dtype(t: Any) -> int:
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.float32: FIONA_F32, torch.float16: FIONA_F16, torch.bfloat16: FIONA_BF16}
+    d = _dtypes.get(t)
+    if d is None:
+        raise ValueError("element type %s: float32, float16 or bfloat16 expected" % t)
+    return d
+
+
+def _expect(t: Any, shape: tuple, dtype: Any, device: int, name: str) -> None:
+    if tuple(t.shape) != shape or t.dtype != dtype:
+        raise ValueError("%s: %s of %s expected, got %s of %s" % (name, shape, dtype, tuple(t.shape), t.dtype))
+    if t.device.type != "cuda" or t.device.index != device:
+        raise ValueError("%s is on %s, the context on cuda:%d" % (name, t.device, device))
+
+
+def _matrix(t: Any, shape: tuple, dtype: Any, device: int, name: str) -> int:
+    """The row stride of a matrix with contiguous columns."""
+    _expect(t, shape, dtype, device, name)
+    row, col = t.stride()
+    if col != 1 and shape[1] > 1:
+        raise ValueError("%s: columns must be contiguous" % name)
+    return row if shape[0] > 1 else shape[1]
+
+
+def _whole(t: Any, shape: tuple, dtype: Any, device: int, name: str) -> int:
+    _expect(t, shape, dtype, device, name)
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
+
+
+class Dropout:
+    """A dropout: probability, and the place of its mask in the generator's
+    stream.  `advance` moves on past a matrix of the given size."""
+
+    def __init__(self, p: float, seed: int, offset: int = 0):
+        self.p, self.seed, self.offset = float(p), int(seed), int(offset)
+        m = (1 << 64) - 1
+        self._spec = _DropoutSpec(self.seed & m, self.offset & m, self.p)
+
+    def advance(self, rows: int, cols: int) -> "Dropout":
+        return Dropout(self.p, self.seed, self.offset + rows * ((cols + 3) // 4))
+
+
+def _spec(d: Optional[Dropout]):
+    return None if d is None else ctypes.byref(d._spec)
+
+
+class Batch:
+    """fiona_adapter_batch: request r owns the rows starts[r] to starts[r + 1] and
+    uses adapter adapters[r] (-1: none); adapter a has rank ranks[a] and scale
+    scales[a] (None: 1).  One batch serves every layer of a model."""
+
+    def __init__(self, ctx: F.Context, starts: Sequence[int], adapters: Sequence[int], ranks: Sequence[int],
+                 r_max: int, scales: Optional[Sequence[float]] = None):
+        s = np.ascontiguousarray(np.asarray(starts, dtype=np.uint64))
+        a = np.ascontiguousarray(np.asarray(adapters, dtype=np.int32))
+        r = np.ascontiguousarray(np.asarray(ranks, dtype=np.uint32))
+        if s.ndim != 1 or a.ndim != 1 or r.ndim != 1 or s.shape[0] != a.shape[0] + 1:
+            raise ValueError("starts must have one entry more than adapters")
+        c = None
+        if scales is not None:
+            c = np.ascontiguousarray(np.asarray(scales, dtype=np.float32))
+            if c.shape != r.shape:
+                raise ValueError("one scale per adapter expected")
+        h = ctypes.c_void_p()
+        F._check(lib().fiona_adapter_batch_create(ctx.handle, a.shape[0], s.ctypes.data, a.ctypes.data, r.shape[0],
+                                                  r.ctypes.data, None if c is None else c.ctypes.data, int(r_max),
+                                                  ctypes.byref(h)), "fiona_adapter_batch_create")
+        self.ctx, self.handle = ctx, h
+        self.n_tokens, self.n_adapters, self.r_max = int(s[-1]), int(r.shape[0]), int(r_max)
+
+    def work_bytes(self, d_in: int, d_out: int, dtype: Any) -> int:
+        n = ctypes.c_uint64()
+        F._check(lib().fiona_adapter_work_bytes(self.handle, int(d_in), int(d_out), _dtype(dtype), ctypes.byref(n)),
+                 "fiona_adapter_work_bytes")
+        return n.value
+
+    def workspace(self, d_in: int, d_out: int, dtype: Any):
+        """A workspace for forward and backward calls on layers of these sizes;
+        calls that may overlap in time need one each."""
+        import torch
+        return torch.empty(max(self.work_bytes(d_in, d_out, dtype), 16), dtype=torch.uint8,
+                           device="cuda:%d" % self.ctx.device)
+
+    def _layer(self, x, A, B):
+        if x.dim() != 2 or B.dim() != 3:
+            raise ValueError("x [tokens][d_in] and B [adapters][d_out][r_max] expected")
+        d_in, d_out, dev = int(x.shape[1]), int(B.shape[1]), self.ctx.device
+        return d_in, d_out, _Layer(d_in, d_out, _dtype(x.dtype), 0,
+                                   _whole(A, (self.n_adapters, self.r_max, d_in), x.dtype, dev, "A"),
+                                   _whole(B, (self.n_adapters, d_out, self.r_max), x.dtype, dev, "B"))
+
+    def forward(self, x, A, B, out, base=None, h=None, dropout: Optional[Dropout] = None, work=None,
+                stream=None) -> None:
+        """fiona_adapter_forward: out = base + s_a (D(x) A_a^T) B_a^T by rows;
+        h [tokens][r_max] fp32, where given, gets D(x) A_a^T."""
+        import torch
+        d_in, d_out, layer = self._layer(x, A, B)
+        T, dt, dev = self.n_tokens, x.dtype, self.ctx.device
+        ldx = _matrix(x, (T, d_in), dt, dev, "x")
+        ld_out = _matrix(out, (T, d_out), dt, dev, "out")
+        ld_base = 0 if base is None else _matrix(base, (T, d_out), dt, dev, "base")
+        ph = None if h is None else _whole(h, (T, self.r_max), torch.float32, dev, "h")
+        if work is None:
+            raise ValueError("forward needs a workspace (Batch.workspace)")
+        F._check(lib().fiona_adapter_forward(self.handle, F.stream_handle(stream), ctypes.byref(layer), x.data_ptr(),
+                                             ldx, F.addr(base), ld_base, out.data_ptr(), ld_out, ph, _spec(dropout),
+                                             work.data_ptr(), work.numel() * work.element_size()),
+                 "fiona_adapter_forward")
+
+    def backward(self, x, h, dy, A, B, dx, dA, dB, dx_base=None, dropout: Optional[Dropout] = None, work=None,
+                 stream=None) -> None:
+        """fiona_adapter_backward: dx, dA and dB (overwritten) from the x, h and
+        dropout of the forward pass and the gradient dy of its out."""
+        import torch
+        d_in, d_out, layer = self._layer(x, A, B)
+        T, dt, dev = self.n_tokens, x.dtype, self.ctx.device
+        ldx = _matrix(x, (T, d_in), dt, dev, "x")
+        ld_dy = _matrix(dy, (T, d_out), dt, dev, "dy")
+        ld_dx = _matrix(dx, (T, d_in), dt, dev, "dx")
+        ld_base = 0 if dx_base is None else _matrix(dx_base, (T, d_in), dt, dev, "dx_base")
+        ph = _whole(h, (T, self.r_max), torch.float32, dev, "h")
+        pA = _whole(dA, tuple(A.shape), dt, dev, "dA")
+        pB = _whole(dB, tuple(B.shape), dt, dev, "dB")
+        if work is None:
+            raise ValueError("backward needs a workspace (Batch.workspace)")
+        F._check(lib().fiona_adapter_backward(self.handle, F.stream_handle(stream), ctypes.byref(layer), x.data_ptr(),
+                                              ldx, ph, dy.data_ptr(), ld_dy, F.addr(dx_base), ld_base, dx.data_ptr(),
+                                              ld_dx, pA, pB, _spec(dropout), work.data_ptr(),
+                                              work.numel() * work.element_size()), "fiona_adapter_backward")
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            lib().fiona_adapter_batch_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def dropout(ctx: F.Context, x, out, drop: Dropout, residual=None, stream=None) -> None:
+    """fiona_dropout: out = residual + D(x) on matrices [rows][cols] (out may be
+    x or residual)."""
+    if x.dim() != 2:
+        raise ValueError("x [rows][cols] expected")
+    shape = tuple(x.shape)
+    ldx = _matrix(x, shape, x.dtype, ctx.device, "x")
+    ld_out = _matrix(out, shape, x.dtype, ctx.device, "out")
+    ld_res = 0 if residual is None else _matrix(residual, shape, x.dtype, ctx.device, "residual")
+    F._check(lib().fiona_dropout(ctx.handle, F.stream_handle(stream), _dtype(x.dtype), shape[0], shape[1],
+                                 x.data_ptr(), ldx, F.addr(residual), ld_res, out.data_ptr(), ld_out, _spec(drop)),
+             "fiona_dropout")
+
+
+def dropout_backward(ctx: F.Context, dy, dx, drop: Dropout, stream=None) -> None:
+    """The gradient of x through `dropout`: the same mask and factor on dy (the
+    residual's gradient is dy itself)."""
+    dropout(ctx, dy, dx, drop, stream=stream)

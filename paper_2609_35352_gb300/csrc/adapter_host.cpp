@@ -1,0 +1,348 @@
+// adapter_host.cpp -- C entry points of fiona_adapter.h: batches, checks of
+// arguments and the choice of kernels (host side).
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "adapter.h"
+#include "device_guard.h"
+
+namespace {
+
+constexpr uint64_t kMaxTokens = 1ull << 26;
+constexpr uint32_t kMaxWidth = 1u << 20;
+constexpr uint32_t kMaxAdapters = 1u << 20;
+
+int cuda_fail(cudaError_t e, const char *what)
+{
+    return e == cudaErrorMemoryAllocation ? set_error(FIONA_ERR_NOMEM, "%s: device allocation", what)
+                                          : set_error(FIONA_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+uint64_t element(uint32_t dtype) { return dtype == FIONA_F32 ? 4 : 2; }
+
+uint64_t align_up(uint64_t n) { return (n + 255) & ~255ull; }
+
+// A strided matrix of one call.
+struct View {
+    const void *p;
+    uint64_t rows, cols, ld, size;  // ld in elements, size of one
+    const char *name;
+    uint64_t bytes() const { return rows && cols ? ((rows - 1) * ld + cols) * size : 0; }
+};
+
+// Whether two matrices share a byte, or cannot be told not to.  Two column
+// ranges of one buffer (the same stride) may interleave.
+bool overlap(const View &a, const View &b)
+{
+    const uint64_t p = (uint64_t)(uintptr_t)a.p, q = (uint64_t)(uintptr_t)b.p;
+    if (!a.bytes() || !b.bytes() || p + a.bytes() <= q || q + b.bytes() <= p) return false;
+    const uint64_t row = a.ld * a.size;
+    if (row != b.ld * b.size || a.cols * a.size > row || b.cols * b.size > row) return true;
+    const uint64_t off = q >= p ? (q - p) % row : (row - (p - q) % row) % row;
+    return off < a.cols * a.size || off + b.cols * b.size > row;
+}
+
+int check_input(const View &v, uint64_t align, const char *who)
+{
+    if (!v.p) return set_error(FIONA_ERR_ARG, "%s: null %s", who, v.name);
+    if ((uintptr_t)v.p % align) return set_error(FIONA_ERR_ARG, "%s: %s is not %llu-byte aligned", who, v.name, (unsigned long long)align);
+    if (v.ld >= (1ull << 40) || v.rows * std::max(v.ld, v.cols) >= (1ull << 60) || v.rows >= (1ull << 40))
+        return set_error(FIONA_ERR_ARG, "%s: rows or row stride of %s out of range", who, v.name);
+    return FIONA_OK;
+}
+
+int check_output(const View &v, uint64_t align, const char *who)
+{
+    const int rc = check_input(v, align, who);
+    if (rc) return rc;
+    if (v.rows > 1 && v.ld < v.cols)
+        return set_error(FIONA_ERR_ARG, "%s: row stride of %s (%llu) below its width (%llu)", who, v.name,
+                         (unsigned long long)v.ld, (unsigned long long)v.cols);
+    return FIONA_OK;
+}
+
+// `in_place`: which of the others `out` may be, or -1
+int check_apart(const View &out, const View *others, int n, int in_place, const char *who)
+{
+    for (int i = 0; i < n; ++i) {
+        if (!others[i].p || (i == in_place && others[i].p == out.p && (others[i].ld == out.ld || out.rows == 1))) continue;
+        if (overlap(out, others[i])) return set_error(FIONA_ERR_ARG, "%s: %s overlaps %s", who, out.name, others[i].name);
+    }
+    return FIONA_OK;
+}
+
+int make_mask(const fiona_dropout_spec *d, uint64_t cols, dropout::Mask &m, const char *who)
+{
+    m = dropout::Mask();
+    m.groups = (cols + 3) / 4;
+    if (!d) return FIONA_OK;
+    if (!(d->p >= 0.0 && d->p <= 1.0)) return set_error(FIONA_ERR_ARG, "%s: dropout probability outside [0, 1]", who);
+    m.level = (uint32_t)std::nearbyint(d->p * 65536.0);
+    m.factor = m.level < 65536 ? (float)(65536.0 / (65536.0 - m.level)) : 0.f;
+    m.base = dropout::mix64(d->seed + (dropout::kStream + 1) * dropout::kGolden) + (d->offset + 1) * dropout::kGolden;
+    return FIONA_OK;
+}
+
+int check_layer(const fiona_adapter_batch *b, const fiona_adapter_layer *l, const char *who)
+{
+    if (!b || !l) return set_error(FIONA_ERR_ARG, "%s: null batch or layer", who);
+    if (l->d_in < 1 || l->d_in > kMaxWidth || l->d_out < 1 || l->d_out > kMaxWidth)
+        return set_error(FIONA_ERR_ARG, "%s: width outside [1, %u]", who, kMaxWidth);
+    if (l->dtype > FIONA_BF16 || l->reserved) return set_error(FIONA_ERR_ARG, "%s: unknown element type or reserved field set", who);
+    if (b->n_adapters && (!l->A || !l->B)) return set_error(FIONA_ERR_ARG, "%s: null adapter weights", who);
+    if (((uintptr_t)l->A | (uintptr_t)l->B) & 15) return set_error(FIONA_ERR_ARG, "%s: adapter weights are not 16-byte aligned", who);
+    return FIONA_OK;
+}
+
+// the workspace of a call: what it holds, and where
+struct Work {
+    uint64_t dh = 0, bytes = 0;
+    explicit Work(const fiona_adapter_batch *b) { bytes = dh + align_up((uint64_t)b->n_tokens * b->r_max * 4); }
+};
+
+int check_work(const Work &w, const void *work, uint64_t bytes, const char *who)
+{
+    if (w.bytes && (!work || ((uintptr_t)work & 15))) return set_error(FIONA_ERR_ARG, "%s: null or misaligned workspace", who);
+    if (bytes < w.bytes)
+        return set_error(FIONA_ERR_ARG, "%s: workspace of %llu bytes, %llu needed", who, (unsigned long long)bytes,
+                         (unsigned long long)w.bytes);
+    return FIONA_OK;
+}
+
+AdapterArgs common_args(const fiona_adapter_batch *b, const fiona_adapter_layer *l)
+{
+    AdapterArgs a{};
+    a.n_tokens = b->n_tokens;
+    a.n_adapters = b->n_adapters;
+    a.r_max = b->r_max;
+    a.d_in = l->d_in;
+    a.d_out = l->d_out;
+    a.owner = b->d_owner;
+    a.order = b->d_order;
+    a.order_begin = b->d_order_begin;
+    a.ranks = b->d_ranks;
+    a.scales = b->d_scales;
+    a.A = l->A;
+    a.B = l->B;
+    return a;
+}
+
+}  // namespace
+
+extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_requests, const uint64_t *starts,
+                                          const int32_t *adapter, uint32_t n_adapters, const uint32_t *ranks,
+                                          const float *scales, uint32_t r_max, fiona_adapter_batch **out) try
+{
+    const char *who = "adapter_batch_create";
+    if (!ctx || !out || !starts || (n_requests && !adapter) || (n_adapters && !ranks))
+        return set_error(FIONA_ERR_ARG, "%s: null argument", who);
+    if (r_max < 1 || r_max > FIONA_ADAPTER_MAX_RANK)
+        return set_error(FIONA_ERR_ARG, "%s: r_max=%u outside [1, %d]", who, r_max, FIONA_ADAPTER_MAX_RANK);
+    if (n_adapters > kMaxAdapters || n_requests > kMaxTokens)
+        return set_error(FIONA_ERR_ARG, "%s: too many adapters or requests", who);
+    if (starts[0] != 0) return set_error(FIONA_ERR_PLAN, "%s: starts[0] must be 0", who);
+    for (uint32_t r = 0; r < n_requests; ++r) {
+        if (starts[r + 1] < starts[r]) return set_error(FIONA_ERR_PLAN, "%s: request %u ends before it starts", who, r);
+        if (starts[r + 1] > kMaxTokens) return set_error(FIONA_ERR_PLAN, "%s: request %u ends above 2^26 rows", who, r);
+        if (adapter[r] < -1 || (adapter[r] >= 0 && (uint32_t)adapter[r] >= n_adapters))
+            return set_error(FIONA_ERR_PLAN, "%s: request %u uses adapter %d of %u", who, r, adapter[r], n_adapters);
+    }
+    for (uint32_t a = 0; a < n_adapters; ++a)
+        if (ranks[a] > r_max) return set_error(FIONA_ERR_PLAN, "%s: adapter %u has rank %u, r_max is %u", who, a, ranks[a], r_max);
+
+    struct Hold {  // (an exception below frees what there is)
+        fiona_adapter_batch *b;
+        ~Hold() { fiona_adapter_batch_destroy(b); }
+    } hold{new fiona_adapter_batch};
+    fiona_adapter_batch *b = hold.b;
+    b->ctx = ctx;
+    b->n_tokens = (uint32_t)starts[n_requests];
+    b->n_adapters = n_adapters;
+    b->r_max = r_max;
+    b->ranks.assign(ranks, ranks + n_adapters);
+
+    const uint32_t T = b->n_tokens;
+    std::vector<uint32_t> owner(T), begin(n_adapters + 1, 0), order;
+    for (uint32_t r = 0; r < n_requests; ++r)
+        for (uint64_t t = starts[r]; t < starts[r + 1]; ++t) {
+            owner[t] = adapter[r] < 0 ? kNoAdapter : (uint32_t)adapter[r];
+            if (adapter[r] >= 0) ++begin[adapter[r] + 1];
+        }
+    for (uint32_t a = 0; a < n_adapters; ++a) begin[a + 1] += begin[a];
+    order.resize(begin[n_adapters]);
+    std::vector<uint32_t> next(begin.begin(), begin.end() - 1);
+    for (uint32_t t = 0; t < T; ++t)
+        if (owner[t] != kNoAdapter) order[next[owner[t]]++] = t;
+
+    if (ctx->device != FIONA_DEVICE_NONE) {
+        DeviceGuard g(ctx->device);
+        if (!g.ok) return set_error(FIONA_ERR_CUDA, "%s: cannot select device %d", who, ctx->device);
+        std::vector<float> s(n_adapters, 1.f);
+        if (scales) s.assign(scales, scales + n_adapters);
+        std::vector<uint8_t> image;
+        auto put = [&](const void *p, size_t bytes) {
+            const size_t at = image.size();
+            image.resize(at + align_up(std::max<size_t>(bytes, 1)));
+            if (bytes) memcpy(image.data() + at, p, bytes);
+            return at;
+        };
+        const size_t o_owner = put(owner.data(), owner.size() * 4), o_order = put(order.data(), order.size() * 4);
+        const size_t o_begin = put(begin.data(), begin.size() * 4), o_ranks = put(ranks, n_adapters * 4ull);
+        const size_t o_scales = put(s.data(), n_adapters * 4ull);
+        cudaError_t e = cudaMalloc(&b->blob, image.size());
+        if (e == cudaSuccess) e = cudaMemcpy(b->blob, image.data(), image.size(), cudaMemcpyHostToDevice);
+        if (e != cudaSuccess) return cuda_fail(e, who);
+        const uint8_t *d = static_cast<const uint8_t *>(b->blob);
+        b->d_owner = reinterpret_cast<const uint32_t *>(d + o_owner);
+        b->d_order = reinterpret_cast<const uint32_t *>(d + o_order);
+        b->d_order_begin = reinterpret_cast<const uint32_t *>(d + o_begin);
+        b->d_ranks = reinterpret_cast<const uint32_t *>(d + o_ranks);
+        b->d_scales = reinterpret_cast<const float *>(d + o_scales);
+    }
+    *out = b;
+    hold.b = nullptr;
+    return FIONA_OK;
+} catch (const std::bad_alloc &) {
+    return set_error(FIONA_ERR_NOMEM, "adapter_batch_create: host allocation");
+}
+
+extern "C" void fiona_adapter_batch_destroy(fiona_adapter_batch *b)
+{
+    if (!b) return;
+    if (b->blob) {
+        DeviceGuard g(b->ctx->device);
+        cudaFree(b->blob);
+    }
+    delete b;
+}
+
+extern "C" int fiona_adapter_work_bytes(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t dtype,
+                                        uint64_t *bytes)
+{
+    const char *who = "adapter_work_bytes";
+    if (!b || !bytes) return set_error(FIONA_ERR_ARG, "%s: null argument", who);
+    if (d_in < 1 || d_in > kMaxWidth || d_out < 1 || d_out > kMaxWidth || dtype > FIONA_BF16)
+        return set_error(FIONA_ERR_ARG, "%s: width outside [1, %u] or unknown element type", who, kMaxWidth);
+    *bytes = Work(b).bytes;
+    return FIONA_OK;
+}
+
+extern "C" int fiona_adapter_forward(const fiona_adapter_batch *b, void *stream, const fiona_adapter_layer *l,
+                                     const void *x, uint64_t ldx, const void *base, uint64_t ld_base, void *out,
+                                     uint64_t ld_out, float *h, const fiona_dropout_spec *drop, void *work,
+                                     uint64_t work_bytes)
+{
+    const char *who = "adapter_forward";
+    int rc = check_layer(b, l, who);
+    if (rc) return rc;
+    AdapterArgs a = common_args(b, l);
+    if ((rc = make_mask(drop, l->d_in, a.mask, who))) return rc;
+    const uint64_t T = b->n_tokens, e = element(l->dtype);
+    if (T == 0) return FIONA_OK;
+    const Work w(b);
+    const View vx{x, T, l->d_in, ldx, e, "x"}, vbase{base, T, l->d_out, ld_base, e, "base"};
+    const View vout{out, T, l->d_out, ld_out, e, "out"}, vh{h, T, b->r_max, b->r_max, 4, "h"};
+    const View vwork{work, 1, work_bytes, work_bytes, 1, "the workspace"};
+    const View vA{l->A, b->n_adapters, (uint64_t)b->r_max * l->d_in, (uint64_t)b->r_max * l->d_in, e, "A"};
+    const View vB{l->B, b->n_adapters, (uint64_t)b->r_max * l->d_out, (uint64_t)b->r_max * l->d_out, e, "B"};
+    if ((rc = check_input(vx, e, who)) || (base && (rc = check_input(vbase, e, who))) || (rc = check_output(vout, e, who)) ||
+        (h && (rc = check_output(vh, 16, who))) || (rc = check_work(w, work, work_bytes, who)))
+        return rc;
+    const View inputs[] = {vx, vbase, vA, vB, vh, vwork};
+    if ((rc = check_apart(vout, inputs, 6, 1, who)) || (h && (rc = check_apart(vh, inputs, 4, -1, who))) ||
+        (rc = check_apart(vwork, inputs, 5, -1, who)))
+        return rc;
+    if (b->ctx->device == FIONA_DEVICE_NONE) return set_error(FIONA_ERR_NODEVICE, "%s: validation-only context", who);
+    DeviceGuard g(b->ctx->device);
+    if (!g.ok) return set_error(FIONA_ERR_CUDA, "%s: cannot select device %d", who, b->ctx->device);
+    a.x = x;
+    a.ldx = ldx;
+    a.base = base;
+    a.ld_base = ld_base;
+    a.out = out;
+    a.ld_out = ld_out;
+    a.h = h;
+    a.dh = reinterpret_cast<float *>(static_cast<uint8_t *>(work) + w.dh);
+    return launch_adapter_simple_forward(b, stream, l->dtype, a);
+}
+
+extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream, const fiona_adapter_layer *l,
+                                      const void *x, uint64_t ldx, const float *h, const void *dy, uint64_t ld_dy,
+                                      const void *dx_base, uint64_t ld_dx_base, void *dx, uint64_t ld_dx, void *dA,
+                                      void *dB, const fiona_dropout_spec *drop, void *work, uint64_t work_bytes)
+{
+    const char *who = "adapter_backward";
+    int rc = check_layer(b, l, who);
+    if (rc) return rc;
+    AdapterArgs a = common_args(b, l);
+    if ((rc = make_mask(drop, l->d_in, a.mask, who))) return rc;
+    const uint64_t T = b->n_tokens, e = element(l->dtype), r = b->r_max;
+    const Work w(b);
+    const View vx{x, T, l->d_in, ldx, e, "x"}, vh{h, T, r, r, 4, "h"}, vdy{dy, T, l->d_out, ld_dy, e, "dy"};
+    const View vbase{dx_base, T, l->d_in, ld_dx_base, e, "dx_base"}, vdx{dx, T, l->d_in, ld_dx, e, "dx"};
+    const View vwork{work, 1, work_bytes, work_bytes, 1, "the workspace"};
+    const View vA{l->A, b->n_adapters, r * l->d_in, r * l->d_in, e, "A"}, vB{l->B, b->n_adapters, r * l->d_out, r * l->d_out, e, "B"};
+    const View vdA{dA, b->n_adapters, r * l->d_in, r * l->d_in, e, "dA"}, vdB{dB, b->n_adapters, r * l->d_out, r * l->d_out, e, "dB"};
+    if (T && ((rc = check_input(vx, e, who)) || (rc = check_input(vh, 16, who)) || (rc = check_input(vdy, e, who)) ||
+              (dx_base && (rc = check_input(vbase, e, who))) || (rc = check_output(vdx, e, who)) ||
+              (rc = check_work(w, work, work_bytes, who))))
+        return rc;
+    if (b->n_adapters && ((rc = check_output(vdA, 16, who)) || (rc = check_output(vdB, 16, who)))) return rc;
+    const View inputs[] = {vx, vh, vdy, vbase, vA, vB, vwork, vdA, vdB};
+    if ((rc = check_apart(vdx, inputs, 9, 3, who)) || (rc = check_apart(vdA, inputs, 7, -1, who)) ||
+        (rc = check_apart(vdB, inputs, 8, -1, who)) || (rc = check_apart(vwork, inputs, 6, -1, who)))
+        return rc;
+    if (b->ctx->device == FIONA_DEVICE_NONE) return set_error(FIONA_ERR_NODEVICE, "%s: validation-only context", who);
+    if (!T && !b->n_adapters) return FIONA_OK;
+    DeviceGuard g(b->ctx->device);
+    if (!g.ok) return set_error(FIONA_ERR_CUDA, "%s: cannot select device %d", who, b->ctx->device);
+    a.x = x;
+    a.ldx = ldx;
+    a.h_in = h;
+    a.dy = dy;
+    a.ld_dy = ld_dy;
+    a.base = dx_base;
+    a.ld_base = ld_dx_base;
+    a.out = dx;
+    a.ld_out = ld_dx;
+    a.dA = dA;
+    a.dB = dB;
+    a.dh = reinterpret_cast<float *>(static_cast<uint8_t *>(work) + w.dh);
+    return launch_adapter_simple_backward(b, stream, l->dtype, a);
+}
+
+extern "C" int fiona_dropout(const fiona_ctx *ctx, void *stream, uint32_t dtype, uint64_t rows, uint64_t cols,
+                             const void *x, uint64_t ldx, const void *residual, uint64_t ld_residual, void *out,
+                             uint64_t ld_out, const fiona_dropout_spec *drop)
+{
+    const char *who = "dropout";
+    if (!ctx || !drop) return set_error(FIONA_ERR_ARG, "%s: null argument", who);
+    if (dtype > FIONA_BF16) return set_error(FIONA_ERR_ARG, "%s: unknown element type", who);
+    if (cols < 1 || cols >= (1ull << 31) || rows >= (1ull << 40))
+        return set_error(FIONA_ERR_ARG, "%s: size out of range", who);
+    DropoutArgs a{};
+    int rc = make_mask(drop, cols, a.mask, who);
+    if (rc || rows == 0) return rc;
+    const uint64_t e = element(dtype);
+    const View vx{x, rows, cols, ldx, e, "x"}, vres{residual, rows, cols, ld_residual, e, "residual"};
+    const View vout{out, rows, cols, ld_out, e, "out"};
+    if ((rc = check_input(vx, e, who)) || (residual && (rc = check_input(vres, e, who))) || (rc = check_output(vout, e, who)) ||
+        (rc = check_apart(vout, &vx, 1, 0, who)) || (rc = check_apart(vout, &vres, 1, 0, who)))
+        return rc;
+    if (ctx->device == FIONA_DEVICE_NONE) return set_error(FIONA_ERR_NODEVICE, "%s: validation-only context", who);
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return set_error(FIONA_ERR_CUDA, "%s: cannot select device %d", who, ctx->device);
+    a.rows = rows;
+    a.cols = cols;
+    a.x = x;
+    a.ldx = ldx;
+    a.res = residual;
+    a.ld_res = ld_residual;
+    a.out = out;
+    a.ld_out = ld_out;
+    return launch_dropout(ctx, stream, dtype, a);
+}

@@ -11,6 +11,7 @@
 #include <map>
 #include <new>
 
+#include "device_guard.h"
 #include "fiona_internal.h"
 #include "gemm.h"
 #include "tiled.h"
@@ -74,23 +75,6 @@ extern "C" const char *fiona_status_str(int status)
     default: return "unknown status";
     }
 }
-
-// Sets the context's device for the duration of a call and restores the
-// caller's device afterwards.
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        if (prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard()
-    {
-        int cur = -1;
-        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-    }
-};
 
 // ---------------------------------------------------------------------------
 // moduli
