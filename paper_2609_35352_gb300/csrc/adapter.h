@@ -11,6 +11,21 @@
 
 constexpr uint32_t kNoAdapter = 0xFFFFFFFFu;
 
+// Up to 128 rows of one adapter, one after another.
+struct AdapterTile {
+    uint32_t row0, rows, adapter;
+};
+// Tiles [begin, end) of one adapter (tiles stand by adapter).
+struct AdapterChunk {
+    uint32_t adapter, begin, end;
+};
+// The tiles cut into chunks of at most `size`.
+struct AdapterChunks {
+    uint32_t size = 0, count = 0;
+    const AdapterChunk *d_chunks = nullptr;
+    const uint32_t *d_begin = nullptr;  // [n_adapters + 1] into d_chunks
+};
+
 struct fiona_adapter_batch {
     const fiona_ctx *ctx = nullptr;
     uint32_t n_tokens = 0, n_adapters = 0, r_max = 0;
@@ -22,6 +37,11 @@ struct fiona_adapter_batch {
     const uint32_t *d_order_begin = nullptr;  // [n_adapters + 1] into d_order
     const uint32_t *d_ranks = nullptr;        // [n_adapters]
     const float *d_scales = nullptr;          // [n_adapters]
+    const AdapterTile *d_tiles = nullptr;     // rows of adapters with a rank, by adapter
+    uint32_t n_tiles = 0;
+    std::vector<AdapterChunks> chunks;        // rising sizes, from 1 to the most tiles an adapter has
+    const AdapterTile *d_bare = nullptr;      // runs of rows without an adapter, or with one of rank 0 (any length)
+    uint32_t n_bare = 0, max_bare = 0;
 };
 
 // One call, as the kernels see it.  Rows are elements apart by their ld.
@@ -42,6 +62,14 @@ struct AdapterArgs {
 // adapter_simple.cu
 int launch_adapter_simple_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a);
 int launch_adapter_simple_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a);
+
+// adapter_tiles.cu: 16-bit types on the tensor cores.  Whether buffers of this
+// shape and alignment go there (rows is false where a pointer or stride is not a
+// multiple of 16 bytes); its workspace; the passes.
+bool adapter_tiles_apply(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t dtype);
+uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
+int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
+int launch_adapter_tiles_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
 
 // dropout.cu
 struct DropoutArgs {

@@ -7,7 +7,7 @@
 #include <cstring>
 #include <new>
 
-#include "adapter.h"
+#include "adapter_tiles.h"
 #include "device_guard.h"
 
 namespace {
@@ -98,18 +98,23 @@ int check_layer(const fiona_adapter_batch *b, const fiona_adapter_layer *l, cons
     return FIONA_OK;
 }
 
-// the workspace of a call: what it holds, and where
-struct Work {
-    uint64_t dh = 0, bytes = 0;
-    explicit Work(const fiona_adapter_batch *b) { bytes = dh + align_up((uint64_t)b->n_tokens * b->r_max * 4); }
-};
-
-int check_work(const Work &w, const void *work, uint64_t bytes, const char *who)
+// bytes of a call's workspace, whichever kernels its buffers' alignment sends it to
+uint64_t work_needed(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t dtype)
 {
-    if (w.bytes && (!work || ((uintptr_t)work & 15))) return set_error(FIONA_ERR_ARG, "%s: null or misaligned workspace", who);
-    if (bytes < w.bytes)
+    uint64_t n = align_up((uint64_t)b->n_tokens * b->r_max * 4);
+    if (adapter_tiles_apply(b, d_in, d_out, dtype)) n = std::max(n, adapter_tiles_work(b, d_in, d_out));
+    return n;
+}
+
+// rows that TMA can address
+bool tma_rows(const View &v) { return !v.p || (((uintptr_t)v.p | (v.ld * v.size)) % 16 == 0 && v.ld >= v.cols); }
+
+int check_work(uint64_t needed, const void *work, uint64_t bytes, const char *who)
+{
+    if (needed && (!work || ((uintptr_t)work & 15))) return set_error(FIONA_ERR_ARG, "%s: null or misaligned workspace", who);
+    if (bytes < needed)
         return set_error(FIONA_ERR_ARG, "%s: workspace of %llu bytes, %llu needed", who, (unsigned long long)bytes,
-                         (unsigned long long)w.bytes);
+                         (unsigned long long)needed);
     return FIONA_OK;
 }
 
@@ -178,6 +183,29 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
     for (uint32_t t = 0; t < T; ++t)
         if (owner[t] != kNoAdapter) order[next[owner[t]]++] = t;
 
+    // token tiles, by adapter; runs of rows that no adapter changes
+    std::vector<std::vector<AdapterTile>> by(n_adapters);
+    std::vector<AdapterTile> tiles, bare;
+    for (uint32_t t = 0; t < T;) {
+        const uint32_t ad = owner[t], first = t;
+        while (t < T && owner[t] == ad) ++t;
+        if (ad == kNoAdapter || ranks[ad] == 0) {
+            bare.push_back({first, t - first, kNoAdapter});
+            b->max_bare = std::max(b->max_bare, t - first);
+        } else {
+            for (uint32_t r = first; r < t; r += kTileRows) by[ad].push_back({r, std::min(kTileRows, t - r), ad});
+        }
+    }
+    std::vector<uint32_t> tile_begin(n_adapters + 1, 0);
+    uint32_t most = 1;
+    for (uint32_t a = 0; a < n_adapters; ++a) {
+        tiles.insert(tiles.end(), by[a].begin(), by[a].end());
+        tile_begin[a + 1] = (uint32_t)tiles.size();
+        most = std::max(most, (uint32_t)by[a].size());
+    }
+    b->n_tiles = (uint32_t)tiles.size();
+    b->n_bare = (uint32_t)bare.size();
+
     if (ctx->device != FIONA_DEVICE_NONE) {
         DeviceGuard g(ctx->device);
         if (!g.ok) return set_error(FIONA_ERR_CUDA, "%s: cannot select device %d", who, ctx->device);
@@ -193,6 +221,22 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         const size_t o_owner = put(owner.data(), owner.size() * 4), o_order = put(order.data(), order.size() * 4);
         const size_t o_begin = put(begin.data(), begin.size() * 4), o_ranks = put(ranks, n_adapters * 4ull);
         const size_t o_scales = put(s.data(), n_adapters * 4ull);
+        const size_t o_tiles = put(tiles.data(), tiles.size() * sizeof(AdapterTile));
+        const size_t o_bare = put(bare.data(), bare.size() * sizeof(AdapterTile));
+        std::vector<std::pair<size_t, size_t>> o_chunks;
+        for (uint32_t size = 1;; size += std::max(1u, size / 4)) {
+            std::vector<AdapterChunk> chunks;
+            std::vector<uint32_t> first(1, 0);
+            for (uint32_t a = 0; a < n_adapters; ++a) {
+                for (uint32_t t = tile_begin[a]; t < tile_begin[a + 1]; t += size)
+                    chunks.push_back({a, t, std::min(t + size, tile_begin[a + 1])});
+                first.push_back((uint32_t)chunks.size());
+            }
+            b->chunks.push_back({size, (uint32_t)chunks.size(), nullptr, nullptr});
+            const size_t at = put(chunks.data(), chunks.size() * sizeof(AdapterChunk));
+            o_chunks.emplace_back(at, put(first.data(), first.size() * 4));
+            if (size >= most) break;
+        }
         cudaError_t e = cudaMalloc(&b->blob, image.size());
         if (e == cudaSuccess) e = cudaMemcpy(b->blob, image.data(), image.size(), cudaMemcpyHostToDevice);
         if (e != cudaSuccess) return cuda_fail(e, who);
@@ -202,6 +246,12 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         b->d_order_begin = reinterpret_cast<const uint32_t *>(d + o_begin);
         b->d_ranks = reinterpret_cast<const uint32_t *>(d + o_ranks);
         b->d_scales = reinterpret_cast<const float *>(d + o_scales);
+        b->d_tiles = reinterpret_cast<const AdapterTile *>(d + o_tiles);
+        b->d_bare = reinterpret_cast<const AdapterTile *>(d + o_bare);
+        for (size_t i = 0; i < o_chunks.size(); ++i) {
+            b->chunks[i].d_chunks = reinterpret_cast<const AdapterChunk *>(d + o_chunks[i].first);
+            b->chunks[i].d_begin = reinterpret_cast<const uint32_t *>(d + o_chunks[i].second);
+        }
     }
     *out = b;
     hold.b = nullptr;
@@ -227,7 +277,7 @@ extern "C" int fiona_adapter_work_bytes(const fiona_adapter_batch *b, uint32_t d
     if (!b || !bytes) return set_error(FIONA_ERR_ARG, "%s: null argument", who);
     if (d_in < 1 || d_in > kMaxWidth || d_out < 1 || d_out > kMaxWidth || dtype > FIONA_BF16)
         return set_error(FIONA_ERR_ARG, "%s: width outside [1, %u] or unknown element type", who, kMaxWidth);
-    *bytes = Work(b).bytes;
+    *bytes = work_needed(b, d_in, d_out, dtype);
     return FIONA_OK;
 }
 
@@ -243,14 +293,15 @@ extern "C" int fiona_adapter_forward(const fiona_adapter_batch *b, void *stream,
     if ((rc = make_mask(drop, l->d_in, a.mask, who))) return rc;
     const uint64_t T = b->n_tokens, e = element(l->dtype);
     if (T == 0) return FIONA_OK;
-    const Work w(b);
+    const uint64_t needed = work_needed(b, l->d_in, l->d_out, l->dtype);
+    if (T == 1) ldx = (l->d_in + 7) & ~7ull, ld_base = ld_out = (l->d_out + 7) & ~7ull;  // (one row has no stride)
     const View vx{x, T, l->d_in, ldx, e, "x"}, vbase{base, T, l->d_out, ld_base, e, "base"};
     const View vout{out, T, l->d_out, ld_out, e, "out"}, vh{h, T, b->r_max, b->r_max, 4, "h"};
     const View vwork{work, 1, work_bytes, work_bytes, 1, "the workspace"};
     const View vA{l->A, b->n_adapters, (uint64_t)b->r_max * l->d_in, (uint64_t)b->r_max * l->d_in, e, "A"};
     const View vB{l->B, b->n_adapters, (uint64_t)b->r_max * l->d_out, (uint64_t)b->r_max * l->d_out, e, "B"};
     if ((rc = check_input(vx, e, who)) || (base && (rc = check_input(vbase, e, who))) || (rc = check_output(vout, e, who)) ||
-        (h && (rc = check_output(vh, 16, who))) || (rc = check_work(w, work, work_bytes, who)))
+        (h && (rc = check_output(vh, 16, who))) || (rc = check_work(needed, work, work_bytes, who)))
         return rc;
     const View inputs[] = {vx, vbase, vA, vB, vh, vwork};
     if ((rc = check_apart(vout, inputs, 6, 1, who)) || (h && (rc = check_apart(vh, inputs, 4, -1, who))) ||
@@ -266,7 +317,9 @@ extern "C" int fiona_adapter_forward(const fiona_adapter_batch *b, void *stream,
     a.out = out;
     a.ld_out = ld_out;
     a.h = h;
-    a.dh = reinterpret_cast<float *>(static_cast<uint8_t *>(work) + w.dh);
+    a.dh = static_cast<float *>(work);
+    if (adapter_tiles_apply(b, l->d_in, l->d_out, l->dtype) && tma_rows(vx) && tma_rows(vbase) && tma_rows(vout))
+        return launch_adapter_tiles_forward(b, stream, l->dtype, a, work);
     return launch_adapter_simple_forward(b, stream, l->dtype, a);
 }
 
@@ -281,7 +334,7 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
     AdapterArgs a = common_args(b, l);
     if ((rc = make_mask(drop, l->d_in, a.mask, who))) return rc;
     const uint64_t T = b->n_tokens, e = element(l->dtype), r = b->r_max;
-    const Work w(b);
+    const uint64_t needed = work_needed(b, l->d_in, l->d_out, l->dtype);
     const View vx{x, T, l->d_in, ldx, e, "x"}, vh{h, T, r, r, 4, "h"}, vdy{dy, T, l->d_out, ld_dy, e, "dy"};
     const View vbase{dx_base, T, l->d_in, ld_dx_base, e, "dx_base"}, vdx{dx, T, l->d_in, ld_dx, e, "dx"};
     const View vwork{work, 1, work_bytes, work_bytes, 1, "the workspace"};
@@ -289,7 +342,7 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
     const View vdA{dA, b->n_adapters, r * l->d_in, r * l->d_in, e, "dA"}, vdB{dB, b->n_adapters, r * l->d_out, r * l->d_out, e, "dB"};
     if (T && ((rc = check_input(vx, e, who)) || (rc = check_input(vh, 16, who)) || (rc = check_input(vdy, e, who)) ||
               (dx_base && (rc = check_input(vbase, e, who))) || (rc = check_output(vdx, e, who)) ||
-              (rc = check_work(w, work, work_bytes, who))))
+              (rc = check_work(needed, work, work_bytes, who))))
         return rc;
     if (b->n_adapters && ((rc = check_output(vdA, 16, who)) || (rc = check_output(vdB, 16, who)))) return rc;
     const View inputs[] = {vx, vh, vdy, vbase, vA, vB, vwork, vdA, vdB};
@@ -311,7 +364,7 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
     a.ld_out = ld_dx;
     a.dA = dA;
     a.dB = dB;
-    a.dh = reinterpret_cast<float *>(static_cast<uint8_t *>(work) + w.dh);
+    a.dh = static_cast<float *>(work);
     return launch_adapter_simple_backward(b, stream, l->dtype, a);
 }
 
