@@ -205,6 +205,19 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
     }
     b->n_tiles = (uint32_t)tiles.size();
     b->n_bare = (uint32_t)bare.size();
+    // the tiles in chunks of several sizes, and where each adapter's begin
+    std::vector<std::pair<std::vector<AdapterChunk>, std::vector<uint32_t>>> chunks;
+    for (uint32_t size = 1;; size += std::max(1u, size / 4)) {
+        chunks.emplace_back();
+        std::vector<AdapterChunk> &c = chunks.back().first;
+        for (uint32_t a = 0; a < n_adapters; ++a) {
+            chunks.back().second.push_back((uint32_t)c.size());
+            for (uint32_t t = tile_begin[a]; t < tile_begin[a + 1]; t += size) c.push_back({a, t, std::min(t + size, tile_begin[a + 1])});
+        }
+        chunks.back().second.push_back((uint32_t)c.size());
+        b->chunks.push_back({size, (uint32_t)c.size(), nullptr, nullptr});
+        if (size >= most) break;
+    }
 
     if (ctx->device != FIONA_DEVICE_NONE) {
         DeviceGuard g(ctx->device);
@@ -224,19 +237,8 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         const size_t o_tiles = put(tiles.data(), tiles.size() * sizeof(AdapterTile));
         const size_t o_bare = put(bare.data(), bare.size() * sizeof(AdapterTile));
         std::vector<std::pair<size_t, size_t>> o_chunks;
-        for (uint32_t size = 1;; size += std::max(1u, size / 4)) {
-            std::vector<AdapterChunk> chunks;
-            std::vector<uint32_t> first(1, 0);
-            for (uint32_t a = 0; a < n_adapters; ++a) {
-                for (uint32_t t = tile_begin[a]; t < tile_begin[a + 1]; t += size)
-                    chunks.push_back({a, t, std::min(t + size, tile_begin[a + 1])});
-                first.push_back((uint32_t)chunks.size());
-            }
-            b->chunks.push_back({size, (uint32_t)chunks.size(), nullptr, nullptr});
-            const size_t at = put(chunks.data(), chunks.size() * sizeof(AdapterChunk));
-            o_chunks.emplace_back(at, put(first.data(), first.size() * 4));
-            if (size >= most) break;
-        }
+        for (const auto &c : chunks)
+            o_chunks.emplace_back(put(c.first.data(), c.first.size() * sizeof(AdapterChunk)), put(c.second.data(), c.second.size() * 4));
         cudaError_t e = cudaMalloc(&b->blob, image.size());
         if (e == cudaSuccess) e = cudaMemcpy(b->blob, image.data(), image.size(), cudaMemcpyHostToDevice);
         if (e != cudaSuccess) return cuda_fail(e, who);
@@ -335,6 +337,7 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
     if ((rc = make_mask(drop, l->d_in, a.mask, who))) return rc;
     const uint64_t T = b->n_tokens, e = element(l->dtype), r = b->r_max;
     const uint64_t needed = work_needed(b, l->d_in, l->d_out, l->dtype);
+    if (T == 1) ldx = ld_dx_base = ld_dx = (l->d_in + 7) & ~7ull, ld_dy = (l->d_out + 7) & ~7ull;  // (one row has no stride)
     const View vx{x, T, l->d_in, ldx, e, "x"}, vh{h, T, r, r, 4, "h"}, vdy{dy, T, l->d_out, ld_dy, e, "dy"};
     const View vbase{dx_base, T, l->d_in, ld_dx_base, e, "dx_base"}, vdx{dx, T, l->d_in, ld_dx, e, "dx"};
     const View vwork{work, 1, work_bytes, work_bytes, 1, "the workspace"};
@@ -365,6 +368,8 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
     a.dA = dA;
     a.dB = dB;
     a.dh = static_cast<float *>(work);
+    if (adapter_tiles_apply(b, l->d_in, l->d_out, l->dtype) && tma_rows(vx) && tma_rows(vdy) && tma_rows(vbase) && tma_rows(vdx))
+        return launch_adapter_tiles_backward(b, stream, l->dtype, a, work);
     return launch_adapter_simple_backward(b, stream, l->dtype, a);
 }
 

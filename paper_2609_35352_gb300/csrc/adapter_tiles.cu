@@ -502,6 +502,522 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
     if (me.warp == 1) tcs::tmem_dealloc(tmem, 128);
 }
 
+// ---------------------------------------------------------------------------
+// the gradients: a chunk of one adapter's token tiles over a range of columns
+// ---------------------------------------------------------------------------
+constexpr uint32_t kGradThreads = 448;  // TMA, MMA, eight workers, four that clean tiles
+constexpr uint32_t kGradWorkers = 256;
+constexpr uint32_t kBlockCols = 128;
+constexpr uint32_t kMostWarps = kGradWorkers / 32;
+
+__host__ __device__ constexpr uint32_t shrink_grad_stage(uint32_t blocks) { return 2 * kBoxBytes + blocks * kBoxBytes; }
+__host__ __device__ constexpr uint32_t expand_grad_stage(uint32_t r16) { return 2 * kBoxBytes + 2 * r16 * 128 + kTileRows * 16; }
+
+// a chunk's walk: stage i is block i % width of the chunk's tile i / width
+struct GradJob {
+    AdapterChunk c;
+    uint32_t slab, b0, width, n;  // first block of 128 columns, blocks, stages in all
+    uint32_t rank, n16;
+    __device__ explicit GradJob(const TileArgs &g)
+    {
+        c = g.chunks[blockIdx.x / g.cut.slabs];
+        slab = blockIdx.x % g.cut.slabs;
+        b0 = slab * g.cut.width;
+        width = min(g.boxes - b0, g.cut.width);
+        n = width * (c.end - c.begin);
+        rank = g.a.ranks[c.adapter];
+        n16 = (rank + 15) & ~15u;
+    }
+    __device__ bool ragged(const TileArgs &g) const
+    {
+        bool r = false;
+        for (uint32_t k = c.begin; k < c.end; ++k) r |= g.tiles[k].rows < kTileRows;
+        return r;
+    }
+};
+
+// shrink_grad: per tile the partial dh = dy B of this range of columns, and over
+// the tiles dB += dy^T h.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_constant__ CUtensorMap tdy,
+                                                              const __grid_constant__ CUtensorMap tB, const TileArgs g)
+{
+    extern __shared__ uint8_t sm[];
+    __shared__ __align__(8) uint64_t bars[3 * kMaxStages + 9];
+    __shared__ uint32_t s_tmem, s_most;
+    __shared__ int s_abort;
+    const Roles me;
+    const uint32_t S = g.stages, H = g.buffers, operand = aligned_smem(sm), op_bytes = operand_bytes(g.blocks);
+    const uint32_t base = operand + H * op_bytes, stage = shrink_grad_stage(g.blocks), bar0 = async::smem_addr(bars);
+    const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
+    const uint32_t ready = bar0 + 3 * kBar * kMaxStages, used = ready + 2 * kBar;  // h, by buffer
+    const uint32_t done = used + 2 * kBar, free_ = done + 2 * kBar, all = free_ + 2 * kBar;  // partial dh, by buffer; everything
+    const GradJob job(g);
+    const bool fix = job.ragged(g);
+    const tiles::Waits w{&s_abort, g.err, g.wait_ns};
+
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        s_most = 0;
+        for (uint32_t s = 0; s < S; ++s) {
+            async::mbar_init(full + kBar * s, 1);
+            async::mbar_init(fixed + kBar * s, 4);
+            async::mbar_init(empty + kBar * s, 1);
+        }
+        for (uint32_t k = 0; k < 2; ++k) {
+            async::mbar_init(ready + kBar * k, kGradWorkers / 32);
+            async::mbar_init(used + kBar * k, 1);
+            async::mbar_init(done + kBar * k, 1);
+            async::mbar_init(free_ + kBar * k, kGradWorkers / 32);
+        }
+        async::mbar_init(all, 1);
+        async::mbar_init_fence();
+        tiles::prefetch_map(&tdy);
+        tiles::prefetch_map(&tB);
+    }
+    if (me.warp == 1) tcs::tmem_alloc(async::smem_addr(&s_tmem), g.tmem_cols);
+    tcs::fence_before();
+    __syncthreads();
+    tcs::fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+    const uint32_t n_tiles = job.c.end - job.c.begin;
+
+    if (me.warp == 0) {
+        uint32_t issued = 0;
+        for (uint32_t i = 0; i < job.n; ++i) {
+            const uint32_t s = i % S, buf = base + s * stage, col0 = (job.b0 + i % job.width) * kBlockCols;
+            const uint32_t row0 = g.tiles[job.c.begin + i / job.width].row0;
+            if (i >= S) w.pass(empty + kBar * s, (i / S - 1) & 1);
+            __syncwarp();
+            if (!__all_sync(0xffffffffu, w.going())) break;
+            if (tiles::elect_one()) {
+                async::mbar_arrive_expect_tx(full + kBar * s, stage);
+                tiles::tma_load_2d(buf, &tdy, col0, row0, full + kBar * s);
+                tiles::tma_load_2d(buf + kBoxBytes, &tdy, col0 + 64, row0, full + kBar * s);
+                for (uint32_t k = 0; k < g.blocks; ++k)
+                    async::tma_load_3d(buf + (2 + k) * kBoxBytes, &tB, k * 64, col0, job.c.adapter, full + kBar * s);
+            }
+            __syncwarp();
+            issued = i + 1;
+        }
+        for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) tiles::drain(full + kBar * (i % S), (i / S) & 1);
+    } else if (me.warp == 1) {
+        const uint32_t id_dh = tiles::idesc(is_bf16<T>(), false, true, job.n16);
+        const uint32_t id_db = tiles::idesc(is_bf16<T>(), true, true, job.n16);
+        uint32_t i = 0;
+        for (uint32_t t = 0; t < n_tiles; ++t) {
+            const uint32_t h = operand + (t % H) * op_bytes, d = t & 1;
+            w.pass(ready + kBar * (t % H), (t / H) & 1);
+            if (t >= 2) w.pass(free_ + kBar * d, (t / 2 - 1) & 1);
+            for (uint32_t j = 0; j < job.width; ++j, ++i) {
+                const uint32_t s = i % S, buf = base + s * stage;
+                w.pass(full + kBar * s, (i / S) & 1);
+                if (fix) w.pass(fixed + kBar * s, (i / S) & 1);
+                tcs::fence_after();
+                __syncwarp();
+                if (tiles::elect_one()) {
+                    const uint64_t b = tiles::desc(buf + 2 * kBoxBytes, kBoxBytes), m = tiles::desc(buf, kBoxBytes);
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k)
+                        tiles::mma(tmem + d * g.r16, tiles::desc(buf + k / 4 * kBoxBytes, 16) + k % 4 * tiles::kStepK,
+                                   b + k * tiles::kStepMN, id_dh, j > 0 || k > 0);
+                    for (uint32_t p = 0; p < 2; ++p) {
+                        const uint64_t hd = tiles::desc(h + p * g.blocks * kBoxBytes, kBoxBytes);
+#pragma unroll
+                        for (uint32_t k = 0; k < 8; ++k)
+                            tiles::mma(tmem + (2 + j) * g.r16, m + k * tiles::kStepMN, hd + k * tiles::kStepMN, id_db,
+                                       t > 0 || p > 0 || k > 0);
+                    }
+                    tcs::commit(empty + kBar * s);
+                    if (j + 1 == job.width) {
+                        tcs::commit(done + kBar * d);
+                        tcs::commit(used + kBar * (t % H));
+                        if (t + 1 == n_tiles) tcs::commit(all);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        tiles::drain(all, 0);
+    } else if (me.warp < 10) {
+        const uint32_t worker = threadIdx.x - 64, quarter = me.warp & 3, half = (me.warp - 2) / 4;
+        const uint32_t groups = job.n16 / 4, row = quarter * 32 + me.lane;
+        auto hidden = [&](const AdapterTile &t, uint32_t r, uint32_t j) {
+            if (r >= t.rows || j >= g.a.r_max) return make_float4(0.f, 0.f, 0.f, 0.f);
+            return below(*reinterpret_cast<const float4 *>(g.a.h_in + (size_t)(t.row0 + r) * g.a.r_max + j), j, job.rank, 1.f);
+        };
+        float most = 0.f;
+        if (!is_bf16<T>()) {
+            for (uint32_t t = job.c.begin; t < job.c.end; ++t) {
+                const AdapterTile tile = g.tiles[t];
+                for (uint32_t k = worker; k < tile.rows * groups; k += kGradWorkers) {
+                    const float4 v = hidden(tile, k / groups, k % groups * 4);
+                    most = fmaxf(most, fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
+                }
+            }
+            most = group_max(most, &s_most, 1, kGradWorkers);
+        }
+        const float up = range_scale<T>(most);
+        auto prepare = [&](uint32_t t) {
+            const AdapterTile tile = g.tiles[job.c.begin + t];
+            if (t >= H) w.pass(used + kBar * (t % H), (t / H - 1) & 1);
+            __syncwarp();
+            for (uint32_t k = worker; k < kTileRows * groups; k += kGradWorkers) {
+                const uint32_t r = k / groups, j = k % groups * 4;
+                const float4 v = hidden(tile, r, j);
+                put_parts<T>(operand + (t % H) * op_bytes, g.blocks, r, j, make_float4(v.x * up, v.y * up, v.z * up, v.w * up));
+            }
+            async::fence_proxy_async();
+            arrive_warp(ready + kBar * (t % H), me.lane);
+        };
+        prepare(0);
+        for (uint32_t t = 0; t < n_tiles; ++t) {
+            if (t + 1 < n_tiles) prepare(t + 1);
+            const uint32_t d = t & 1, tile_no = job.c.begin + t;
+            const AdapterTile tile = g.tiles[tile_no];
+            w.pass(done + kBar * d, (t / 2) & 1);
+            tcs::fence_after();
+            __syncwarp();
+            float *p = g.part_out + ((size_t)job.slab * g.a.n_tokens + tile.row0 + row) * g.r16;
+            float big = 0.f;
+            for (uint32_t c = half * 16; c < job.n16; c += 32) {
+                float v[16];
+                tiles::ld16(tmem + ((quarter * 32) << 16) + d * g.r16 + c, v);
+                tcs::wait_ld();
+                if (row < tile.rows) {
+#pragma unroll
+                    for (uint32_t k = 0; k < 16; k += 4)
+                        *reinterpret_cast<float4 *>(p + c + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+                    if (!is_bf16<T>())
+#pragma unroll
+                        for (uint32_t k = 0; k < 16; ++k)
+                            if (c + k < job.rank) big = fmaxf(big, finite_abs(v[k]));
+                }
+            }
+            tcs::fence_before();
+            arrive_warp(free_ + kBar * d, me.lane);
+            if (!is_bf16<T>()) {
+                for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+                if (me.lane == 0) g.most_out[((size_t)job.slab * g.n_tiles + tile_no) * kMostWarps + me.warp - 2] = big;
+            }
+        }
+        w.pass(all, 0);
+        tcs::fence_after();
+        __syncwarp();
+        const float scale = g.a.scales[job.c.adapter] * (1.f / up);
+        for (uint32_t j = 0; j < job.width; ++j) {
+            const uint32_t col = (job.b0 + j) * kBlockCols + row;
+            float *p = g.grad + ((size_t)(blockIdx.x / g.cut.slabs) * g.cols + col) * g.r16;
+            for (uint32_t c = half * 16; c < job.n16; c += 32) {
+                float v[16];
+                tiles::ld16(tmem + ((quarter * 32) << 16) + (2 + j) * g.r16 + c, v);
+                tcs::wait_ld();
+                if (col < g.cols)
+#pragma unroll
+                    for (uint32_t k = 0; k < 16; k += 4)
+                        *reinterpret_cast<float4 *>(p + c + k) =
+                            make_float4(v[k] * scale, v[k + 1] * scale, v[k + 2] * scale, v[k + 3] * scale);
+            }
+        }
+        tcs::fence_before();
+    } else if (fix) {
+        // rows past a tile's end are another request's
+        const dropout::Mask none;
+        for (uint32_t i = 0; i < job.n; ++i) {
+            const uint32_t s = i % S, buf = base + s * stage, rows = g.tiles[job.c.begin + i / job.width].rows;
+            w.pass(full + kBar * s, (i / S) & 1);
+            __syncwarp();
+            if (rows < kTileRows)
+                for (uint32_t k = 0; k < 2; ++k)
+                    clean_box(buf + k * kBoxBytes, none, 0, rows, 0, threadIdx.x - 320, 128, nullptr);
+            async::fence_proxy_async();
+            arrive_warp(fixed + kBar * s, me.lane);
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    tcs::fence_after();
+    if (me.warp == 1) tcs::tmem_dealloc(tmem, g.tmem_cols);
+}
+
+// expand_grad: per tile dx = dx_base + D'(dh A) of this range of columns, and over
+// the tiles dA += D(x)^T dh.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_constant__ CUtensorMap tx,
+                                                              const __grid_constant__ CUtensorMap tA,
+                                                              const __grid_constant__ CUtensorMap tdx, const TileArgs g)
+{
+    extern __shared__ uint8_t sm[];
+    __shared__ __align__(8) uint64_t bars[3 * kMaxStages + 9];
+    __shared__ uint32_t s_tmem, s_most;
+    __shared__ int s_abort;
+    const Roles me;
+    const uint32_t S = g.stages, H = g.buffers, operand = aligned_smem(sm), op_bytes = operand_bytes(g.blocks);
+    const uint32_t base = operand + H * op_bytes, stage = expand_grad_stage(g.r16), bar0 = async::smem_addr(bars);
+    const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
+    const uint32_t ready = bar0 + 3 * kBar * kMaxStages, used = ready + 2 * kBar;  // dh, by buffer
+    const uint32_t done = used + 2 * kBar, free_ = done + 2 * kBar, all = free_ + 2 * kBar;  // dx, by buffer; everything
+    const GradJob job(g);
+    const bool mask = g.a.mask.level != 0, clean_A = job.rank != job.n16 && job.rank < g.a.r_max;
+    const bool fix = mask || clean_A || job.ragged(g);
+    const tiles::Waits w{&s_abort, g.err, g.wait_ns};
+    const uint32_t a_box = g.r16 * 128, bits_at = 2 * kBoxBytes + 2 * a_box;
+
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        s_most = 0;
+        for (uint32_t s = 0; s < S; ++s) {
+            async::mbar_init(full + kBar * s, 1);
+            async::mbar_init(fixed + kBar * s, 4);
+            async::mbar_init(empty + kBar * s, 1);
+        }
+        for (uint32_t k = 0; k < 2; ++k) {
+            async::mbar_init(ready + kBar * k, kGradWorkers / 32);
+            async::mbar_init(used + kBar * k, 1);
+            async::mbar_init(done + kBar * k, 1);
+            async::mbar_init(free_ + kBar * k, kGradWorkers / 32);
+        }
+        async::mbar_init(all, 1);
+        async::mbar_init_fence();
+        tiles::prefetch_map(&tx);
+        tiles::prefetch_map(&tA);
+        tiles::prefetch_map(&tdx);
+    }
+    if (me.warp == 1) tcs::tmem_alloc(async::smem_addr(&s_tmem), g.tmem_cols);
+    tcs::fence_before();
+    __syncthreads();
+    tcs::fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+    const uint32_t n_tiles = job.c.end - job.c.begin;
+
+    if (me.warp == 0) {
+        uint32_t issued = 0;
+        for (uint32_t i = 0; i < job.n; ++i) {
+            const uint32_t s = i % S, buf = base + s * stage, col0 = (job.b0 + i % job.width) * kBlockCols;
+            const uint32_t row0 = g.tiles[job.c.begin + i / job.width].row0;
+            if (i >= S) w.pass(empty + kBar * s, (i / S - 1) & 1);
+            __syncwarp();
+            if (!__all_sync(0xffffffffu, w.going())) break;
+            if (tiles::elect_one()) {
+                async::mbar_arrive_expect_tx(full + kBar * s, bits_at);
+                for (uint32_t k = 0; k < 2; ++k) {
+                    tiles::tma_load_2d(buf + k * kBoxBytes, &tx, col0 + k * 64, row0, full + kBar * s);
+                    async::tma_load_3d(buf + 2 * kBoxBytes + k * a_box, &tA, col0 + k * 64, 0, job.c.adapter, full + kBar * s);
+                }
+            }
+            __syncwarp();
+            issued = i + 1;
+        }
+        for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) tiles::drain(full + kBar * (i % S), (i / S) & 1);
+    } else if (me.warp == 1) {
+        const uint32_t id_dx = tiles::idesc(is_bf16<T>(), false, true, kBlockCols);
+        const uint32_t id_da = tiles::idesc(is_bf16<T>(), true, true, job.n16);
+        const uint32_t acc = tmem + 2 * kBlockCols;
+        uint32_t i = 0;
+        for (uint32_t t = 0; t < n_tiles; ++t) {
+            const uint32_t dh = operand + (t % H) * op_bytes;
+            w.pass(ready + kBar * (t % H), (t / H) & 1);
+            for (uint32_t j = 0; j < job.width; ++j, ++i) {
+                const uint32_t s = i % S, buf = base + s * stage, d = i & 1;
+                if (i >= 2) w.pass(free_ + kBar * d, (i / 2 - 1) & 1);
+                w.pass(full + kBar * s, (i / S) & 1);
+                if (fix) w.pass(fixed + kBar * s, (i / S) & 1);
+                tcs::fence_after();
+                __syncwarp();
+                if (tiles::elect_one()) {
+                    const uint64_t A = tiles::desc(buf + 2 * kBoxBytes, a_box), m = tiles::desc(buf, kBoxBytes);
+                    for (uint32_t p = 0; p < 2; ++p)
+                        for (uint32_t k = 0; k < job.n16 / 16; ++k)
+                            tiles::mma(tmem + d * kBlockCols,
+                                       tiles::desc(dh + (p * g.blocks + k / 4) * kBoxBytes, 16) + k % 4 * tiles::kStepK,
+                                       A + k * tiles::kStepMN, id_dx, p > 0 || k > 0);
+                    for (uint32_t p = 0; p < 2; ++p) {
+                        const uint64_t hd = tiles::desc(dh + p * g.blocks * kBoxBytes, kBoxBytes);
+#pragma unroll
+                        for (uint32_t k = 0; k < 8; ++k)
+                            tiles::mma(acc + j * g.r16, m + k * tiles::kStepMN, hd + k * tiles::kStepMN, id_da,
+                                       t > 0 || p > 0 || k > 0);
+                    }
+                    tcs::commit(done + kBar * d);
+                    if (j + 1 == job.width) {
+                        tcs::commit(used + kBar * (t % H));
+                        if (t + 1 == n_tiles) tcs::commit(all);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        tiles::drain(all, 0);
+    } else if (me.warp < 10) {
+        const uint32_t worker = threadIdx.x - 64, quarter = me.warp & 3, half = (me.warp - 2) / 4;
+        const uint32_t groups = job.n16 / 4, row = quarter * 32 + me.lane;
+        const float s_a = g.a.scales[job.c.adapter];
+        float most = 0.f;
+        if (!is_bf16<T>()) {
+            // (a bound: the ranges' largest partial sums, added up)
+            for (uint32_t t = job.c.begin + worker; t < job.c.end; t += kGradWorkers) {
+                float sum = 0.f;
+                for (uint32_t k = 0; k < g.slabs_in; ++k) {
+                    float m = 0.f;
+                    for (uint32_t q = 0; q < kMostWarps; ++q) m = fmaxf(m, g.most_in[((size_t)k * g.n_tiles + t) * kMostWarps + q]);
+                    sum += m;
+                }
+                most = fmaxf(most, finite_abs(sum * s_a));
+            }
+            most = group_max(most, &s_most, 1, kGradWorkers);
+        }
+        const float up = range_scale<T>(most), scale = g.a.mask.factor * (1.f / up);
+        auto prepare = [&](uint32_t t) {
+            const AdapterTile tile = g.tiles[job.c.begin + t];
+            if (t >= H) w.pass(used + kBar * (t % H), (t / H - 1) & 1);
+            __syncwarp();
+            for (uint32_t k = worker; k < kTileRows * groups; k += kGradWorkers) {
+                const uint32_t r = k / groups, j = k % groups * 4;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (r < tile.rows) v = below(sum_parts(g, tile.row0 + r, j), j, job.rank, s_a);
+                put_parts<T>(operand + (t % H) * op_bytes, g.blocks, r, j, make_float4(v.x * up, v.y * up, v.z * up, v.w * up));
+            }
+            async::fence_proxy_async();
+            arrive_warp(ready + kBar * (t % H), me.lane);
+        };
+        prepare(0);
+        uint32_t i = 0;
+        for (uint32_t t = 0; t < n_tiles; ++t) {
+            if (H > 1 && t + 1 < n_tiles) prepare(t + 1);
+            const AdapterTile tile = g.tiles[job.c.begin + t];
+            for (uint32_t j = 0; j < job.width; ++j, ++i) {
+                const uint32_t s = i % S, buf = base + s * stage, d = i & 1, col0 = (job.b0 + j) * kBlockCols;
+                if (mask) w.pass(fixed + kBar * s, (i / S) & 1);
+                w.pass(done + kBar * d, (i / 2) & 1);
+                tcs::fence_after();
+                __syncwarp();
+                float v[4][16];
+#pragma unroll
+                for (uint32_t c = 0; c < 4; ++c)
+                    tiles::ld16(tmem + ((quarter * 32) << 16) + d * kBlockCols + half * 64 + c * 16, v[c]);
+                tcs::wait_ld();
+                tcs::fence_before();
+                arrive_warp(free_ + kBar * d, me.lane);
+                uint2 bits = make_uint2(~0u, ~0u);
+                if (mask && row < tile.rows)
+                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(bits.x), "=r"(bits.y) : "r"(buf + bits_at + half * 1024 + row * 8) : "memory");
+                const T *b = g.a.base && row < tile.rows ? (const T *)g.a.base + (uint64_t)(tile.row0 + row) * g.a.ld_base : nullptr;
+#pragma unroll
+                for (uint32_t c = 0; c < 8; ++c) {
+                    const uint32_t col = col0 + half * 64 + c * 8, keep = (c < 4 ? bits.x >> (8 * c) : bits.y >> (8 * (c - 4))) & 255;
+                    uint4 o = make_uint4(0, 0, 0, 0);
+                    if (b && col < g.cols) o = *reinterpret_cast<const uint4 *>(b + col);
+                    uint32_t *u = reinterpret_cast<uint32_t *>(&o);
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) {
+                        const float2 f = unpack<T>(u[k]);
+                        const float *a = &v[c / 2][(c % 2) * 8 + 2 * k];
+                        u[k] = pack<T>(keep >> (2 * k) & 1 ? fmaf(scale, a[0], f.x) : f.x,
+                                       keep >> (2 * k) & 2 ? fmaf(scale, a[1], f.y) : f.y);
+                    }
+                    st_shared16(buf + half * kBoxBytes + chunk_at(row, c), o);
+                }
+                if (tile.rows == kTileRows) {
+                    async::fence_proxy_async();
+                    async::named_barrier(1, kGradWorkers);
+                    if (me.warp == 2) {
+                        if (me.lane == 0) {
+                            tiles::tma_store_2d(&tdx, col0, tile.row0, buf);
+                            if (col0 + 64 < g.cols) tiles::tma_store_2d(&tdx, col0 + 64, tile.row0, buf + kBoxBytes);
+                            tiles::store_commit();
+                            tiles::store_wait_read();
+                        }
+                        arrive_warp(empty + kBar * s, me.lane);
+                    }
+                } else {
+                    async::named_barrier(1, kGradWorkers);
+                    for (uint32_t k = worker; k < tile.rows * 16; k += kGradWorkers) {
+                        const uint32_t r = k / 16, c = k % 16, col = col0 + c * 8;
+                        if (col < g.cols)  // (columns come in eights)
+                            *reinterpret_cast<uint4 *>((T *)g.a.out + (uint64_t)(tile.row0 + r) * g.a.ld_out + col) =
+                                ld_shared16(buf + c / 8 * kBoxBytes + chunk_at(r, c % 8));
+                    }
+                    async::fence_proxy_async();
+                    async::named_barrier(1, kGradWorkers);
+                    if (me.warp == 2) arrive_warp(empty + kBar * s, me.lane);
+                }
+            }
+            if (H == 1 && t + 1 < n_tiles) prepare(t + 1);
+        }
+        w.pass(all, 0);
+        tcs::fence_after();
+        __syncwarp();
+        for (uint32_t j = 0; j < job.width; ++j) {
+            const uint32_t col = (job.b0 + j) * kBlockCols + row;
+            float *p = g.grad + (size_t)(blockIdx.x / g.cut.slabs) * g.r16 * g.cols + col;
+            for (uint32_t c = half * 16; c < job.n16; c += 32) {
+                float v[16];
+                tiles::ld16(tmem + ((quarter * 32) << 16) + 2 * kBlockCols + j * g.r16 + c, v);
+                tcs::wait_ld();
+                if (col < g.cols)
+#pragma unroll
+                    for (uint32_t k = 0; k < 16; ++k) p[(size_t)(c + k) * g.cols] = v[k] * scale;
+            }
+        }
+        tcs::fence_before();
+    } else if (fix) {
+        for (uint32_t i = 0; i < job.n; ++i) {
+            const uint32_t s = i % S, buf = base + s * stage, col0 = (job.b0 + i % job.width) * kBlockCols;
+            const AdapterTile tile = g.tiles[job.c.begin + i / job.width];
+            w.pass(full + kBar * s, (i / S) & 1);
+            __syncwarp();
+            const uint32_t thread = threadIdx.x - 320;
+            if (mask || tile.rows < kTileRows)
+                for (uint32_t k = 0; k < 2; ++k)
+                    clean_box(buf + k * kBoxBytes, g.a.mask, tile.row0, tile.rows, col0 + k * 64, thread, 128,
+                              sm + (buf + bits_at + k * 1024 - async::smem_addr(sm)));
+            if (clean_A)  // A's rows from the rank to the next multiple of 16 are not A's
+                for (uint32_t k = thread; k < (job.n16 - job.rank) * 16; k += 128)
+                    st_shared16(buf + 2 * kBoxBytes + k % 16 / 8 * a_box + chunk_at(job.rank + k / 16, k % 8), make_uint4(0, 0, 0, 0));
+            async::fence_proxy_async();
+            arrive_warp(fixed + kBar * s, me.lane);
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    tcs::fence_after();
+    if (me.warp == 1) tcs::tmem_dealloc(tmem, g.tmem_cols);
+}
+
+// dA and dB of every adapter: its chunks' sums added up in order, zero where
+// there are none and outside the rank.
+struct GradSum {
+    const float *part;       // [chunks][part_rows][part_inner]
+    const uint32_t *begin;   // [n_adapters + 1]
+    void *out;               // [n_adapters][rows][inner]
+    uint32_t rows, inner, part_rows, part_inner;
+    uint32_t rank_rows;      // the rank bounds rows (dA) or columns (dB)
+};
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_grad_sum(const GradSum A, const GradSum B, const uint32_t *ranks, uint32_t blocks_A,
+                                                  uint32_t first)
+{
+    const GradSum &g = blockIdx.x < blocks_A ? A : B;
+    const uint32_t ad = first + blockIdx.y, rank = ranks[ad], per_row = g.inner / 8;
+    const uint64_t k = (uint64_t)(blockIdx.x < blocks_A ? blockIdx.x : blockIdx.x - blocks_A) * 256 + threadIdx.x;
+    if (k >= (uint64_t)g.rows * per_row) return;
+    const uint32_t row = (uint32_t)(k / per_row), col = (uint32_t)(k % per_row) * 8;
+    float v[8] = {};
+    if (row < (g.rank_rows ? rank : g.rows) && col < (g.rank_rows ? g.inner : rank))
+        for (uint32_t c = g.begin[ad]; c < g.begin[ad + 1]; ++c) {
+            const float4 *p = reinterpret_cast<const float4 *>(g.part + ((size_t)c * g.part_rows + row) * g.part_inner + col);
+            const float4 x = p[0], y = p[1];
+            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+        }
+    if (!g.rank_rows)
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (col + i >= rank) v[i] = 0.f;
+    *reinterpret_cast<uint4 *>((T *)g.out + ((size_t)ad * g.rows + row) * g.inner + col) =
+        make_uint4(pack<T>(v[0], v[1]), pack<T>(v[2], v[3]), pack<T>(v[4], v[5]), pack<T>(v[6], v[7]));
+}
+
 // rows without an adapter: out = base (or zero), h = 0
 template <typename T>
 __global__ void __launch_bounds__(256) k_bare(const AdapterArgs a, const AdapterTile *runs, uint32_t cols)
@@ -560,6 +1076,8 @@ int tensor_map(CUtensorMap *tm, uint32_t dtype, const void *p, uint64_t cols, ui
     return FIONA_OK;
 }
 
+uint64_t align_up(uint64_t n) { return (n + 255) & ~255ull; }
+
 // `boxes` of a row's columns in ranges, so that `units` of them make about
 // `want` CTAs
 Cut cut_columns(uint32_t boxes, uint32_t units, uint32_t want)
@@ -580,7 +1098,7 @@ struct ForwardShape {
     }
     uint64_t part_bytes(const fiona_adapter_batch *b) const
     {
-        return (((uint64_t)shrink.slabs * b->n_tokens * r.r16 * 4) + 255) & ~255ull;
+        return align_up((uint64_t)shrink.slabs * b->n_tokens * r.r16 * 4);
     }
 };
 
@@ -656,6 +1174,115 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
                   operand_bytes(g.blocks) + (size_t)g.stages * expand_stage(g.blocks) + 1024, s, eargs, "adapter expand");
 }
 
+// How one of the gradients' passes is cut: blocks of 128 columns a CTA, tiles a
+// chunk.  More columns a CTA: fewer partial dh; more tiles: fewer partial dB or dA;
+// both: fewer CTAs.  By a model of the pass in microseconds of one CTA an SM: 0.75
+// for a tile's block of 128 columns, half as much again for its operand; and the
+// partial sums at 5 TB/s.
+struct GradCut {
+    Cut cut{};
+    const AdapterChunks *chunks = nullptr;
+    uint32_t tmem_cols = 0;
+    GradCut(const fiona_adapter_batch *b, uint32_t cols, const RankShape &r, bool shrink)
+    {
+        const uint32_t n = ceil_div(cols, kBlockCols), sms = (uint32_t)std::max(b->ctx->sm_count, 1);
+        const uint32_t fixed = shrink ? 2 * r.r16 : 2 * kBlockCols;
+        const uint32_t most = std::min({n, 4u, (512 - std::max(fixed, 2 * kBlockCols)) / r.r16});
+        double best = 0;
+        for (uint32_t width = most; width >= 1; --width)
+            for (const AdapterChunks &c : b->chunks) {
+                const uint32_t slabs = ceil_div(n, width);
+                const double waves = ceil_div(c.count * slabs, sms);
+                const double us = waves * (2.0 + c.size * (0.75 * width + 0.4) + 0.01 * width * r.r16) +
+                                  8.0 * c.count * (double)cols * r.r16 / 5e6 + (shrink ? 8.0 : 0.0) * slabs * b->n_tokens * (double)r.r16 / 5e6;
+                if (!chunks || us < best) {
+                    best = us;
+                    chunks = &c;
+                    cut = Cut{width, slabs};
+                }
+            }
+        tmem_cols = 32;
+        while (tmem_cols < fixed + cut.width * r.r16) tmem_cols *= 2;
+    }
+};
+
+struct BackwardShape {
+    RankShape r;
+    GradCut shrink, expand;
+    uint64_t part, grad_A, grad_B, most, bytes;  // offsets in the workspace
+    BackwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
+        : r(b->r_max), shrink(b, d_out, r, true), expand(b, d_in, r, false)
+    {
+        part = 0;
+        grad_A = part + align_up((uint64_t)shrink.cut.slabs * b->n_tokens * r.r16 * 4);
+        grad_B = grad_A + align_up((uint64_t)expand.chunks->count * d_in * r.r16 * 4);
+        most = grad_B + align_up((uint64_t)shrink.chunks->count * d_out * r.r16 * 4);
+        bytes = most + align_up((uint64_t)shrink.cut.slabs * b->n_tiles * kMostWarps * 4);
+    }
+};
+
+template <typename T>
+int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const AdapterArgs &a, void *work)
+{
+    int rc = FIONA_OK;
+    if (b->n_bare && (rc = bare<T>(b, a, a.d_in, s))) return rc;
+    const BackwardShape f(b, a.d_in, a.d_out);
+    uint8_t *ws = static_cast<uint8_t *>(work);
+    if (b->n_tiles) {
+        TileArgs g{};
+        g.a = a;
+        g.tiles = b->d_tiles;
+        g.n_tiles = b->n_tiles;
+        g.r16 = f.r.r16;
+        g.blocks = f.r.blocks;
+        g.buffers = f.r.blocks == 1 ? 2 : 1;
+        g.err = b->ctx->d_kerr;
+        g.wait_ns = kWaitNs;
+        CUtensorMap tx, tA, tdy, tB, tdx;
+        if ((rc = tensor_map(&tx, dtype, a.x, a.d_in, a.n_tokens, 0, a.ldx, kTileRows)) ||
+            (rc = tensor_map(&tA, dtype, a.A, a.d_in, a.r_max, a.n_adapters, a.d_in, f.r.r16)) ||
+            (rc = tensor_map(&tdy, dtype, a.dy, a.d_out, a.n_tokens, 0, a.ld_dy, kTileRows)) ||
+            (rc = tensor_map(&tB, dtype, a.B, a.r_max, a.d_out, a.n_adapters, a.r_max, kBlockCols)) ||
+            (rc = tensor_map(&tdx, dtype, a.out, a.d_in, a.n_tokens, 0, a.ld_out, kTileRows)))
+            return rc;
+        const uint32_t op = g.buffers * operand_bytes(g.blocks);
+        g.chunks = f.shrink.chunks->d_chunks;
+        g.cols = a.d_out;
+        g.boxes = ceil_div(a.d_out, kBlockCols);
+        g.cut = f.shrink.cut;
+        g.tmem_cols = f.shrink.tmem_cols;
+        g.part_out = reinterpret_cast<float *>(ws + f.part);
+        g.most_out = reinterpret_cast<float *>(ws + f.most);
+        g.grad = reinterpret_cast<float *>(ws + f.grad_B);
+        g.stages = std::min(kMaxStages, (kSmemOne - op) / shrink_grad_stage(g.blocks));
+        void *sargs[] = {&tdy, &tB, &g};
+        rc = launch(k_shrink_grad<T>, f.shrink.chunks->count * g.cut.slabs, kGradThreads,
+                    op + (size_t)g.stages * shrink_grad_stage(g.blocks) + 1024, s, sargs, "adapter shrink_grad");
+        if (rc) return rc;
+        g.part_in = g.part_out;
+        g.most_in = g.most_out;
+        g.slabs_in = g.cut.slabs;
+        g.chunks = f.expand.chunks->d_chunks;
+        g.cols = a.d_in;
+        g.boxes = ceil_div(a.d_in, kBlockCols);
+        g.cut = f.expand.cut;
+        g.tmem_cols = f.expand.tmem_cols;
+        g.grad = reinterpret_cast<float *>(ws + f.grad_A);
+        g.stages = std::min(kMaxStages, (kSmemOne - op) / expand_grad_stage(g.r16));
+        void *eargs[] = {&tx, &tA, &tdx, &g};
+        rc = launch(k_expand_grad<T>, f.expand.chunks->count * g.cut.slabs, kGradThreads,
+                    op + (size_t)g.stages * expand_grad_stage(g.r16) + 1024, s, eargs, "adapter expand_grad");
+        if (rc) return rc;
+    }
+    const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_max, a.d_in, f.r.r16, a.d_in, 1};
+    const GradSum B{reinterpret_cast<const float *>(ws + f.grad_B), f.shrink.chunks->d_begin, a.dB, a.d_out, a.r_max, a.d_out, f.r.r16, 0};
+    const uint32_t blocks_A = ceil_div(a.r_max * (a.d_in / 8), 256), blocks_B = ceil_div(a.d_out * (a.r_max / 8), 256);
+    for (uint32_t i = 0; i < a.n_adapters; i += 65535)
+        k_grad_sum<T><<<dim3(blocks_A + blocks_B, std::min(a.n_adapters - i, 65535u)), 256, 0, s>>>(A, B, a.ranks, blocks_A, i);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? FIONA_OK : set_error(FIONA_ERR_CUDA, "adapter gradient launch: %s", cudaGetErrorString(e));
+}
+
 }  // namespace
 
 bool adapter_tiles_apply(const fiona_adapter_batch *b, uint32_t d_in, uint32_t, uint32_t dtype)
@@ -665,11 +1292,17 @@ bool adapter_tiles_apply(const fiona_adapter_batch *b, uint32_t d_in, uint32_t, 
 
 uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
 {
-    return ForwardShape(b, d_in, d_out).part_bytes(b);
+    return std::max(ForwardShape(b, d_in, d_out).part_bytes(b), BackwardShape(b, d_in, d_out).bytes);
 }
 
 int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work)
 {
     return dtype == FIONA_BF16 ? forward<__nv_bfloat16>(b, (cudaStream_t)stream, dtype, a, work)
                                : forward<__half>(b, (cudaStream_t)stream, dtype, a, work);
+}
+
+int launch_adapter_tiles_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work)
+{
+    return dtype == FIONA_BF16 ? backward<__nv_bfloat16>(b, (cudaStream_t)stream, dtype, a, work)
+                               : backward<__half>(b, (cudaStream_t)stream, dtype, a, work);
 }

@@ -35,9 +35,9 @@ struct TileArgs {
     uint32_t slabs_in;
     float *part_out;       // the same, of the pass that makes them
     float *grad;           // [chunks][...] partial dB or dA
-    float *most_out;       // fp16, backward: [slabs][tiles] largest |dh| of a tile and slab
+    float *most_out;       // fp16, backward: [slabs][tiles][8] largest |partial dh| of a tile, by warp
     const float *most_in;
-    uint32_t n_tiles, stages;
+    uint32_t n_tiles, stages, buffers, tmem_cols;
     int *err;
     uint64_t wait_ns;
 };
