@@ -19,6 +19,11 @@ struct AdapterTile {
 struct AdapterChunk {
     uint32_t adapter, begin, end;
 };
+// Up to four rows of one adapter, wherever they stand.
+constexpr uint32_t kAdapterRows = 4;
+struct AdapterRows {
+    uint32_t adapter, count, row[kAdapterRows];
+};
 // The tiles cut into chunks of at most `size`.
 struct AdapterChunks {
     uint32_t size = 0, count = 0;
@@ -40,8 +45,14 @@ struct fiona_adapter_batch {
     const AdapterTile *d_tiles = nullptr;     // rows of adapters with a rank, by adapter
     uint32_t n_tiles = 0;
     std::vector<AdapterChunks> chunks;        // rising sizes, from 1 to the most tiles an adapter has
-    const AdapterTile *d_bare = nullptr;      // runs of rows without an adapter, or with one of rank 0 (any length)
-    uint32_t n_bare = 0, max_bare = 0;
+    const uint32_t *d_tile_begin = nullptr;   // [n_adapters + 1] into d_tiles
+    // the same rows, those in short runs apart (adapter_rows.cu)
+    const AdapterTile *d_long = nullptr;
+    uint32_t n_long = 0;
+    const AdapterRows *d_rows = nullptr;
+    uint32_t n_rows = 0, most_rows = 0;       // groups; the most rows of one
+    const AdapterTile *d_bare = nullptr;      // rows without an adapter, or with one of rank 0
+    uint32_t n_bare = 0;
 };
 
 // One call, as the kernels see it.  Rows are elements apart by their ld.
@@ -63,12 +74,17 @@ struct AdapterArgs {
 int launch_adapter_simple_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a);
 int launch_adapter_simple_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a);
 
+// adapter_rows.cu: the forward pass on the short runs of rows, any type and alignment
+bool adapter_rows_apply(const fiona_adapter_batch *b, uint32_t d_in);
+int launch_adapter_rows(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a);
+
 // adapter_tiles.cu: 16-bit types on the tensor cores.  Whether buffers of this
 // shape and alignment go there (rows is false where a pointer or stride is not a
 // multiple of 16 bytes); its workspace; the passes.
 bool adapter_tiles_apply(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t dtype);
 uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
-int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
+int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,
+                                 bool only_long);
 int launch_adapter_tiles_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
 
 // dropout.cu

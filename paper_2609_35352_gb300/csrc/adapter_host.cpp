@@ -15,6 +15,8 @@ namespace {
 constexpr uint64_t kMaxTokens = 1ull << 26;
 constexpr uint32_t kMaxWidth = 1u << 20;
 constexpr uint32_t kMaxAdapters = 1u << 20;
+constexpr uint32_t kShortRun = 16;  // rows; below: groups of rows
+constexpr uint32_t kBareRows = 4;   // rows without an adapter that a CTA copies
 
 int cuda_fail(cudaError_t e, const char *what)
 {
@@ -190,8 +192,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         const uint32_t ad = owner[t], first = t;
         while (t < T && owner[t] == ad) ++t;
         if (ad == kNoAdapter || ranks[ad] == 0) {
-            bare.push_back({first, t - first, kNoAdapter});
-            b->max_bare = std::max(b->max_bare, t - first);
+            for (uint32_t r = first; r < t; r += kBareRows) bare.push_back({r, std::min(kBareRows, t - r), kNoAdapter});
         } else {
             for (uint32_t r = first; r < t; r += kTileRows) by[ad].push_back({r, std::min(kTileRows, t - r), ad});
         }
@@ -205,6 +206,31 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
     }
     b->n_tiles = (uint32_t)tiles.size();
     b->n_bare = (uint32_t)bare.size();
+    // runs shorter than kShortRun in groups of an adapter's rows
+    std::vector<AdapterTile> longer;
+    std::vector<AdapterRows> rows;
+    for (uint32_t a = 0; a < n_adapters; ++a) {
+        AdapterRows group{a, 0, {}};
+        for (size_t k = 0; k < by[a].size(); ++k) {
+            const AdapterTile &t = by[a][k];
+            const bool starts = k == 0 || by[a][k - 1].row0 + by[a][k - 1].rows != t.row0;
+            if (t.rows >= kShortRun || !starts) {
+                longer.push_back(t);
+                continue;
+            }
+            for (uint32_t r = t.row0; r < t.row0 + t.rows; ++r) {
+                group.row[group.count++] = r;
+                b->most_rows = std::max(b->most_rows, group.count);
+                if (group.count == kAdapterRows) {
+                    rows.push_back(group);
+                    group.count = 0;
+                }
+            }
+        }
+        if (group.count) rows.push_back(group);
+    }
+    b->n_long = (uint32_t)longer.size();
+    b->n_rows = (uint32_t)rows.size();
     // the tiles in chunks of several sizes, and where each adapter's begin
     std::vector<std::pair<std::vector<AdapterChunk>, std::vector<uint32_t>>> chunks;
     for (uint32_t size = 1;; size += std::max(1u, size / 4)) {
@@ -235,6 +261,9 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         const size_t o_begin = put(begin.data(), begin.size() * 4), o_ranks = put(ranks, n_adapters * 4ull);
         const size_t o_scales = put(s.data(), n_adapters * 4ull);
         const size_t o_tiles = put(tiles.data(), tiles.size() * sizeof(AdapterTile));
+        const size_t o_tile_begin = put(tile_begin.data(), tile_begin.size() * 4);
+        const size_t o_long = put(longer.data(), longer.size() * sizeof(AdapterTile));
+        const size_t o_rows = put(rows.data(), rows.size() * sizeof(AdapterRows));
         const size_t o_bare = put(bare.data(), bare.size() * sizeof(AdapterTile));
         std::vector<std::pair<size_t, size_t>> o_chunks;
         for (const auto &c : chunks)
@@ -249,6 +278,9 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         b->d_ranks = reinterpret_cast<const uint32_t *>(d + o_ranks);
         b->d_scales = reinterpret_cast<const float *>(d + o_scales);
         b->d_tiles = reinterpret_cast<const AdapterTile *>(d + o_tiles);
+        b->d_tile_begin = reinterpret_cast<const uint32_t *>(d + o_tile_begin);
+        b->d_long = reinterpret_cast<const AdapterTile *>(d + o_long);
+        b->d_rows = reinterpret_cast<const AdapterRows *>(d + o_rows);
         b->d_bare = reinterpret_cast<const AdapterTile *>(d + o_bare);
         for (size_t i = 0; i < o_chunks.size(); ++i) {
             b->chunks[i].d_chunks = reinterpret_cast<const AdapterChunk *>(d + o_chunks[i].first);
@@ -320,8 +352,11 @@ extern "C" int fiona_adapter_forward(const fiona_adapter_batch *b, void *stream,
     a.ld_out = ld_out;
     a.h = h;
     a.dh = static_cast<float *>(work);
-    if (adapter_tiles_apply(b, l->d_in, l->d_out, l->dtype) && tma_rows(vx) && tma_rows(vbase) && tma_rows(vout))
-        return launch_adapter_tiles_forward(b, stream, l->dtype, a, work);
+    const bool short_apart = b->n_rows && adapter_rows_apply(b, l->d_in);
+    const bool on_tiles = adapter_tiles_apply(b, l->d_in, l->d_out, l->dtype) && tma_rows(vx) && tma_rows(vbase) && tma_rows(vout);
+    if (short_apart && (on_tiles || (!b->n_long && !b->n_bare)) && (rc = launch_adapter_rows(b, stream, l->dtype, a))) return rc;
+    if (short_apart && !b->n_long && !b->n_bare) return FIONA_OK;
+    if (on_tiles) return launch_adapter_tiles_forward(b, stream, l->dtype, a, work, short_apart);
     return launch_adapter_simple_forward(b, stream, l->dtype, a);
 }
 

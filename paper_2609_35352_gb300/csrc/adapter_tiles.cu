@@ -78,24 +78,11 @@ __device__ __forceinline__ float range_scale(float most)
 
 __device__ __forceinline__ float finite_abs(float v) { return isfinite(v) ? fabsf(v) : 0.f; }
 
-// the 8 mask bits of columns 8 c .. 8 c + 7 of row t (bit set: kept)
-__device__ __forceinline__ uint32_t keep8(const dropout::Mask &m, uint64_t t, uint32_t c)
+// The two fields of `v` as a pair's mask: 0xFFFF where a field is below the level
+// (dropped), by the sign of the difference.
+__device__ __forceinline__ uint32_t dropped(uint32_t v, uint32_t level)
 {
-    const uint64_t v0 = m.draw(t, 2 * c), v1 = m.draw(t, 2 * c + 1);
-    uint32_t bits = 0;
-#pragma unroll
-    for (uint32_t k = 0; k < 4; ++k) {
-        bits |= (dropout::Mask::field(v0, k) >= m.level ? 1u : 0u) << k;
-        bits |= (dropout::Mask::field(v1, k) >= m.level ? 1u : 0u) << (4 + k);
-    }
-    return bits;
-}
-
-// 16-bit pairs of a 16-byte chunk, dropped ones cleared
-__device__ __forceinline__ uint4 masked(uint4 v, uint32_t bits)
-{
-    auto pair = [&](uint32_t u, uint32_t b) { return u & ((b & 1 ? 0xFFFFu : 0u) | (b & 2 ? 0xFFFF0000u : 0u)); };
-    return make_uint4(pair(v.x, bits), pair(v.y, bits >> 2), pair(v.z, bits >> 4), pair(v.w, bits >> 6));
+    return __byte_perm((v & 0xFFFFu) - level, (v >> 16) - level, 0xFFBB);
 }
 
 __device__ __forceinline__ uint4 ld_shared16(uint32_t addr)
@@ -128,16 +115,21 @@ __device__ __forceinline__ float4 below(float4 v, uint32_t j, uint32_t rank, flo
                        j + 3 < rank ? v.w * by : 0.f);
 }
 
-// four ranks of a row into the operand's two parts (boxes of 64 ranks)
+// four ranks of a row into the operand's two parts
 template <typename T>
-__device__ __forceinline__ void put_parts(uint32_t operand, uint32_t blocks, uint32_t row, uint32_t j, float4 v)
+__device__ __forceinline__ void put_parts(uint32_t operand, uint32_t lo, uint32_t row, uint32_t j, float4 v)
 {
     uint32_t h0, h1, l0, l1;
     split2<T>(v.x, v.y, h0, l0);
     split2<T>(v.z, v.w, h1, l1);
-    const uint32_t at = operand + (j / 64) * kBoxBytes + chunk_at(row, (j % 64) / 8) + (j % 8) * 2;
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(h0), "r"(h1) : "memory");
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + blocks * kBoxBytes), "r"(l0), "r"(l1) : "memory");
+    auto at = [&](uint32_t e) { return operand + (e / 64) * kBoxBytes + chunk_at(row, (e % 64) / 8) + (e % 8) * 2; };
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at(j)), "r"(h0), "r"(h1) : "memory");
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at(lo + j)), "r"(l0), "r"(l1) : "memory");
+}
+// the operand from element e on, K-major
+__device__ __forceinline__ uint64_t operand_k(uint32_t operand, uint32_t e)
+{
+    return tiles::desc(operand + e / 64 * kBoxBytes, 16) + e % 64 / 16 * tiles::kStepK;
 }
 
 // the largest of `v` over the threads of a named barrier's group, in `slot`
@@ -165,31 +157,75 @@ __device__ __forceinline__ void arrive_warp(uint32_t bar, uint32_t lane)
 }
 
 // Drop masked elements and rows at or past `rows` of a box of 128 rows, by
-// `threads` threads; with `bits` (shared, 8 bytes a row) the mask is kept.
+// `threads` threads (a multiple of 16; eight a row); with `bits` (shared, 8 bytes a
+// row) a set bit says dropped.
+template <uint32_t THREADS, bool BITS>
 __device__ __forceinline__ void clean_box(uint32_t box, const dropout::Mask &m, uint32_t row0, uint32_t rows,
-                                          uint32_t col0, uint32_t thread, uint32_t threads, uint8_t *bits)
+                                          uint32_t col0, uint32_t thread, uint32_t bits)
 {
-    for (uint32_t k = thread; k < kTileRows * 8; k += threads) {
-        const uint32_t row = k / 8, c = k % 8, at = box + chunk_at(row, c);
-        if (row >= rows) {
-            st_shared16(at, make_uint4(0, 0, 0, 0));
-        } else if (m.level) {
-            const uint32_t b = keep8(m, row0 + row, col0 / 8 + c);
-            if (b != 255) st_shared16(at, masked(ld_shared16(at), b));
-            if (bits) bits[k] = (uint8_t)b;
+    constexpr uint32_t kRows = THREADS / 8;  // a multiple of 8 or 4, 2: a thread's chunk keeps its swizzle every 8 rows
+    const uint32_t c = thread % 8;
+    uint32_t row = thread / 8;
+    if (m.level) {
+        uint64_t z = m.base + ((uint64_t)(row0 + row) * m.groups + col0 / 4 + 2 * c) * dropout::kGolden;
+        const uint64_t step = (uint64_t)kRows * m.groups * dropout::kGolden;
+#pragma unroll 2
+        for (; row < rows; row += kRows, z += step) {
+            const uint64_t v0 = dropout::mix64(z), v1 = dropout::mix64(z + dropout::kGolden);
+            const uint32_t at = box + chunk_at(row, c);
+            const uint32_t d0 = dropped((uint32_t)v0, m.level), d1 = dropped((uint32_t)(v0 >> 32), m.level);
+            const uint32_t d2 = dropped((uint32_t)v1, m.level), d3 = dropped((uint32_t)(v1 >> 32), m.level);
+            uint4 u = ld_shared16(at);
+            u.x &= ~d0, u.y &= ~d1, u.z &= ~d2, u.w &= ~d3;
+            st_shared16(at, u);
+            if (BITS) {
+                const uint32_t b = (d0 & 0x00020001u) | (d1 & 0x00080004u) | (d2 & 0x00200010u) | (d3 & 0x00800040u);
+                asm volatile("st.shared.b8 [%0], %1;" ::"r"(bits + row * 8 + c), "r"(b | b >> 16) : "memory");
+            }
+        }
+    } else if (row < rows) {
+        row += (rows - row + kRows - 1) / kRows * kRows;
+    }
+    for (; row < kTileRows; row += kRows) st_shared16(box + chunk_at(row, c), make_uint4(0, 0, 0, 0));
+}
+
+// rows without an adapter: out = base (or zero), h = 0; by a CTA of `threads`
+template <typename T>
+__device__ void bare_rows(const AdapterArgs &a, const AdapterTile t, uint32_t cols, uint32_t threads)
+{
+    constexpr uint32_t kVec = 16 / sizeof(T);
+    if (a.base != a.out) {
+        const bool wide = (((uintptr_t)a.base | (uintptr_t)a.out) & 15) == 0 && (a.ld_base | a.ld_out) % kVec == 0;
+        const uint32_t n = wide ? cols / kVec : 0, rest = cols - n * kVec;
+        for (uint32_t k = threadIdx.x; k < t.rows * n; k += threads) {
+            const uint64_t row = t.row0 + k / n, i = k % n;
+            reinterpret_cast<uint4 *>((T *)a.out + row * a.ld_out)[i] =
+                a.base ? reinterpret_cast<const uint4 *>((const T *)a.base + row * a.ld_base)[i] : make_uint4(0, 0, 0, 0);
+        }
+        for (uint32_t k = threadIdx.x; k < t.rows * rest; k += threads) {
+            const uint64_t row = t.row0 + k / rest, i = n * kVec + k % rest;
+            ((T *)a.out)[row * a.ld_out + i] = a.base ? ((const T *)a.base)[row * a.ld_base + i] : narrow<T>(0.f);
         }
     }
+    if (a.h)
+        for (uint32_t k = threadIdx.x; k < t.rows * a.r_max; k += threads) a.h[(uint64_t)t.row0 * a.r_max + k] = 0.f;
 }
 
 // ---------------------------------------------------------------------------
 // shrink: partial h of a token tile over a range of columns
 // ---------------------------------------------------------------------------
-constexpr uint32_t kShrinkThreads = 192;
+constexpr uint32_t kShrinkThreads = 320;  // TMA, MMA, eight that mask and store
 constexpr uint32_t kMaxStages = 8;
 
-__host__ __device__ constexpr uint32_t shrink_stage(uint32_t r16) { return kBoxBytes + r16 * 128; }
+// (BACK: partial dh = dy B, for ranks above 64: shrink_grad's accumulators of dB
+// leave it a range of 256 columns then, whose partial dh is as large as its dy)
+template <bool BACK>
+__host__ __device__ constexpr uint32_t shrink_stage(uint32_t r16, uint32_t blocks)
+{
+    return kBoxBytes + (BACK ? blocks * 64 * 128 : r16 * 128);
+}
 
-template <typename T>
+template <typename T, bool BACK>
 __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant__ CUtensorMap tx,
                                                            const __grid_constant__ CUtensorMap tA, const TileArgs g)
 {
@@ -201,18 +237,19 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
     const uint32_t base = aligned_smem(sm), bar0 = async::smem_addr(bars), S = g.stages;
     const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
     const uint32_t done = bar0 + 3 * kBar * kMaxStages;
-    const uint32_t stage = shrink_stage(g.r16), cols = max(32u, g.r16 <= 32 ? 32u : g.r16 <= 64 ? 64u : 128u);
+    const uint32_t stage = shrink_stage<BACK>(g.r16, g.blocks), cols = max(32u, g.r16 <= 32 ? 32u : g.r16 <= 64 ? 64u : 128u);
     const AdapterTile t = g.tiles[blockIdx.x / g.cut.slabs];
     const uint32_t slab = blockIdx.x % g.cut.slabs;
     const uint32_t b0 = slab * g.cut.width, n = min(g.boxes - b0, g.cut.width);
-    const bool fix = g.a.mask.level != 0;
+    const bool fix = !BACK && g.a.mask.level != 0;
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
 
+    tiles::next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (uint32_t s = 0; s < S; ++s) {
             async::mbar_init(full + kBar * s, 1);
-            async::mbar_init(fixed + kBar * s, 4);
+            async::mbar_init(fixed + kBar * s, 8);
             async::mbar_init(empty + kBar * s, 1);
         }
         async::mbar_init(done, 1);
@@ -237,14 +274,18 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
             if (tiles::elect_one()) {
                 async::mbar_arrive_expect_tx(full + kBar * s, stage);
                 tiles::tma_load_2d(buf, &tx, (b0 + i) * 64, t.row0, full + kBar * s);
-                async::tma_load_3d(buf + kBoxBytes, &tA, (b0 + i) * 64, 0, t.adapter, full + kBar * s);
+                if (!BACK)
+                    async::tma_load_3d(buf + kBoxBytes, &tA, (b0 + i) * 64, 0, t.adapter, full + kBar * s);
+                else
+                    for (uint32_t k = 0; k < g.blocks; ++k)
+                        async::tma_load_3d(buf + kBoxBytes + k * 64 * 128, &tA, k * 64, (b0 + i) * 64, t.adapter, full + kBar * s);
             }
             __syncwarp();
             issued = i + 1;
         }
         for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) tiles::drain(full + kBar * (i % S), (i / S) & 1);
     } else if (me.warp == 1) {
-        const uint32_t id = tiles::idesc(is_bf16<T>(), false, false, n16);
+        const uint32_t id = tiles::idesc(is_bf16<T>(), false, BACK, n16);
         for (uint32_t i = 0; i < n; ++i) {
             const uint32_t s = i % S, buf = base + s * stage;
             w.pass(full + kBar * s, (i / S) & 1);
@@ -252,10 +293,11 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
             tcs::fence_after();
             __syncwarp();
             if (tiles::elect_one()) {
-                const uint64_t da = tiles::desc(buf, 16), db = tiles::desc(buf + kBoxBytes, 16);
+                const uint64_t da = tiles::desc(buf, 16), db = tiles::desc(buf + kBoxBytes, BACK ? 64 * 128 : 16);
 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k)
-                    tiles::mma(tmem, da + k * tiles::kStepK, db + k * tiles::kStepK, id, i > 0 || k > 0);
+                    tiles::mma(tmem, da + k * tiles::kStepK, db + k * (BACK ? tiles::kStepMN : tiles::kStepK), id,
+                               i > 0 || k > 0);
                 tcs::commit(empty + kBar * s);
                 if (i + 1 == n) tcs::commit(done);
             }
@@ -263,21 +305,22 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
         }
         tiles::drain(done, 0);
     } else {
-        const uint32_t quarter = me.warp & 3, row = quarter * 32 + me.lane;
+        const uint32_t quarter = me.warp & 3, half = (me.warp - 2) / 4, row = quarter * 32 + me.lane;
         if (fix)
             for (uint32_t i = 0; i < n; ++i) {
                 const uint32_t s = i % S;
                 w.pass(full + kBar * s, (i / S) & 1);
                 __syncwarp();
-                clean_box(base + s * stage, g.a.mask, t.row0, t.rows, (b0 + i) * 64, threadIdx.x - 64, 128, nullptr);
+                clean_box<256, false>(base + s * stage, g.a.mask, t.row0, t.rows, (b0 + i) * 64, threadIdx.x - 64, 0);
                 async::fence_proxy_async();
                 arrive_warp(fixed + kBar * s, me.lane);
             }
         w.pass(done, 0);
         tcs::fence_after();
         __syncwarp();
+        tiles::previous_done();
         float *p = g.part_out + ((size_t)slab * g.a.n_tokens + t.row0 + row) * g.r16;
-        for (uint32_t c = 0; c < n16; c += 16) {
+        for (uint32_t c = half * 16; c < n16; c += 32) {
             float v[16];
             tiles::ld16(tmem + ((quarter * 32) << 16) + c, v);
             tcs::wait_ld();
@@ -301,7 +344,6 @@ constexpr uint32_t kExpandThreads = 384;  // TMA, MMA, eight epilogue warps, two
 constexpr uint32_t kExpandWorkers = 256;
 
 __host__ __device__ constexpr uint32_t expand_stage(uint32_t blocks) { return kBoxBytes + blocks * 64 * 128; }
-__host__ __device__ constexpr uint32_t operand_bytes(uint32_t blocks) { return 2 * blocks * kBoxBytes; }
 
 template <typename T>
 __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant__ CUtensorMap tbase,
@@ -313,18 +355,26 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
     __shared__ uint32_t s_tmem, s_most;
     __shared__ int s_abort;
     const Roles me;
-    const uint32_t S = g.stages, operand = aligned_smem(sm), base = operand + operand_bytes(g.blocks);
+    const uint32_t S = g.stages, operand = aligned_smem(sm), base = operand + g.op_boxes * kBoxBytes;
     const uint32_t bar0 = async::smem_addr(bars);
     const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
     const uint32_t done = bar0 + 3 * kBar * kMaxStages, free_ = done + 2 * kBar, ready = free_ + 2 * kBar;
     const uint32_t stage = expand_stage(g.blocks);
-    const AdapterTile t = g.tiles[blockIdx.x / g.cut.slabs];
-    const uint32_t slab = blockIdx.x % g.cut.slabs;
+    if (blockIdx.x < g.n_bare) {
+        tiles::next_may_start();
+        tiles::previous_done();
+        bare_rows<T>(g.a, g.bare[blockIdx.x], g.cols, kExpandThreads);
+        return;
+    }
+    const uint32_t unit = blockIdx.x - g.n_bare;
+    const AdapterTile t = g.tiles[unit / g.cut.slabs];
+    const uint32_t slab = unit % g.cut.slabs;
     const uint32_t b0 = slab * g.cut.width, n = min(g.boxes - b0, g.cut.width);
     const uint32_t rank = g.a.ranks[t.adapter], n16 = (rank + 15) & ~15u;
     const bool fix = rank != n16 && rank < g.a.r_max;
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
 
+    tiles::next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         s_most = 0;
@@ -380,10 +430,9 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
             if (tiles::elect_one()) {
                 for (uint32_t p = 0; p < 2; ++p)
                     for (uint32_t k = 0; k < n16; k += 16) {
-                        const uint64_t da = tiles::desc(operand + (p * g.blocks + k / 64) * kBoxBytes, 16);
                         const uint64_t db = tiles::desc(buf + kBoxBytes + (k / 64) * 64 * 128, 16);
-                        const uint32_t step = (k % 64) / 16 * tiles::kStepK;
-                        tiles::mma(tmem + d * 64, da + step, db + step, id, p > 0 || k > 0);
+                        tiles::mma(tmem + d * 64, operand_k(operand, p * g.lo + k), db + (k % 64) / 16 * tiles::kStepK, id,
+                                   p > 0 || k > 0);
                     }
                 tcs::commit(done + kBar * d);
             }
@@ -394,6 +443,7 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
     } else if (me.warp < 10) {
         const uint32_t worker = threadIdx.x - 64, quarter = me.warp & 3, half = (me.warp - 2) / 4;
         // h: the sum of its parts, in two 16-bit parts (and whole, where wanted)
+        tiles::previous_done();
         const uint32_t groups = n16 / 4;
         float most = 0.f;
         if (!is_bf16<T>()) {
@@ -411,7 +461,7 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
             if (row < t.rows) v = below(sum_parts(g, t.row0 + row, j), j, rank, g.a.mask.factor);
             if (g.a.h && slab == 0 && row < t.rows && j < g.a.r_max)
                 *reinterpret_cast<float4 *>(g.a.h + (size_t)(t.row0 + row) * g.a.r_max + j) = v;
-            put_parts<T>(operand, g.blocks, row, j, make_float4(v.x * up, v.y * up, v.z * up, v.w * up));
+            put_parts<T>(operand, g.lo, row, j, make_float4(v.x * up, v.y * up, v.z * up, v.w * up));
         }
         if (g.a.h && slab == 0)  // zero at and above the last block of ranks
             for (uint32_t k = worker; k < t.rows * ((g.a.r_max - min(n16, g.a.r_max)) / 4); k += kExpandWorkers) {
@@ -505,23 +555,25 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
 // ---------------------------------------------------------------------------
 // the gradients: a chunk of one adapter's token tiles over a range of columns
 // ---------------------------------------------------------------------------
-constexpr uint32_t kGradThreads = 448;  // TMA, MMA, eight workers, four that clean tiles
+constexpr uint32_t kGradThreads = 480;  // TMA, MMA, eight workers, the operand's TMA, four that clean tiles
+constexpr uint32_t kExpandGradThreads = 608;  // the same, eight that clean and mask
 constexpr uint32_t kGradWorkers = 256;
 constexpr uint32_t kBlockCols = 128;
-constexpr uint32_t kMostWarps = kGradWorkers / 32;
 
+// (`blocks` of B, none without dh)
 __host__ __device__ constexpr uint32_t shrink_grad_stage(uint32_t blocks) { return 2 * kBoxBytes + blocks * kBoxBytes; }
 __host__ __device__ constexpr uint32_t expand_grad_stage(uint32_t r16) { return 2 * kBoxBytes + 2 * r16 * 128 + kTileRows * 16; }
 
 // a chunk's walk: stage i is block i % width of the chunk's tile i / width
 struct GradJob {
     AdapterChunk c;
-    uint32_t slab, b0, width, n;  // first block of 128 columns, blocks, stages in all
+    uint32_t chunk, slab, b0, width, n;  // first block of 128 columns, blocks, stages in all
     uint32_t rank, n16;
     __device__ explicit GradJob(const TileArgs &g)
     {
-        c = g.chunks[blockIdx.x / g.cut.slabs];
-        slab = blockIdx.x % g.cut.slabs;
+        chunk = (blockIdx.x - g.n_bare) / g.cut.slabs;
+        c = g.chunks[chunk];
+        slab = (blockIdx.x - g.n_bare) % g.cut.slabs;
         b0 = slab * g.cut.width;
         width = min(g.boxes - b0, g.cut.width);
         n = width * (c.end - c.begin);
@@ -536,6 +588,42 @@ struct GradJob {
     }
 };
 
+// The operand of each tile from its image, by one warp.
+__device__ __forceinline__ void load_operands(const TileArgs &g, const GradJob &job, uint32_t operand, uint32_t ready,
+                                              uint32_t used, const tiles::Waits &w)
+{
+    const uint32_t n = job.c.end - job.c.begin, H = g.buffers, bytes = g.op_boxes * kBoxBytes;
+    uint32_t issued = 0;
+    tiles::previous_done();
+    for (uint32_t t = 0; t < n; ++t) {
+        if (t >= H) w.pass(used + kBar * (t % H), (t / H - 1) & 1);
+        __syncwarp();
+        if (!__all_sync(0xffffffffu, w.going())) break;
+        if (tiles::elect_one()) {
+            async::mbar_arrive_expect_tx(ready + kBar * (t % H), bytes);
+            async::bulk_g2s(operand + (t % H) * bytes, g.image + (size_t)(job.c.begin + t) * bytes, bytes, ready + kBar * (t % H));
+        }
+        __syncwarp();
+        issued = t + 1;
+    }
+    for (uint32_t t = issued > H ? issued - H : 0; t < issued; ++t) tiles::drain(ready + kBar * (t % H), (t / H) & 1);
+}
+
+// sixteen accumulators of a weight gradient (complete on return)
+__device__ __forceinline__ void ld_both(uint32_t taddr, const TileArgs &g, float (&v)[16])
+{
+    tiles::ld16(taddr, v);
+    if (g.both) {
+        float u[16];
+        tiles::ld16(taddr + g.lo, u);
+        tcs::wait_ld();
+#pragma unroll
+        for (uint32_t k = 0; k < 16; ++k) v[k] += u[k];
+    } else {
+        tcs::wait_ld();
+    }
+}
+
 // shrink_grad: per tile the partial dh = dy B of this range of columns, and over
 // the tiles dB += dy^T h.
 template <typename T>
@@ -544,11 +632,11 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
 {
     extern __shared__ uint8_t sm[];
     __shared__ __align__(8) uint64_t bars[3 * kMaxStages + 9];
-    __shared__ uint32_t s_tmem, s_most;
+    __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const Roles me;
-    const uint32_t S = g.stages, H = g.buffers, operand = aligned_smem(sm), op_bytes = operand_bytes(g.blocks);
-    const uint32_t base = operand + H * op_bytes, stage = shrink_grad_stage(g.blocks), bar0 = async::smem_addr(bars);
+    const uint32_t S = g.stages, H = g.buffers, operand = aligned_smem(sm), op_bytes = g.op_boxes * kBoxBytes;
+    const uint32_t base = operand + H * op_bytes, stage = shrink_grad_stage(g.with_dh ? g.blocks : 0), bar0 = async::smem_addr(bars);
     const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
     const uint32_t ready = bar0 + 3 * kBar * kMaxStages, used = ready + 2 * kBar;  // h, by buffer
     const uint32_t done = used + 2 * kBar, free_ = done + 2 * kBar, all = free_ + 2 * kBar;  // partial dh, by buffer; everything
@@ -556,16 +644,16 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
     const bool fix = job.ragged(g);
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
 
+    tiles::next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
-        s_most = 0;
         for (uint32_t s = 0; s < S; ++s) {
             async::mbar_init(full + kBar * s, 1);
             async::mbar_init(fixed + kBar * s, 4);
             async::mbar_init(empty + kBar * s, 1);
         }
         for (uint32_t k = 0; k < 2; ++k) {
-            async::mbar_init(ready + kBar * k, kGradWorkers / 32);
+            async::mbar_init(ready + kBar * k, 1);
             async::mbar_init(used + kBar * k, 1);
             async::mbar_init(done + kBar * k, 1);
             async::mbar_init(free_ + kBar * k, kGradWorkers / 32);
@@ -594,7 +682,7 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
                 async::mbar_arrive_expect_tx(full + kBar * s, stage);
                 tiles::tma_load_2d(buf, &tdy, col0, row0, full + kBar * s);
                 tiles::tma_load_2d(buf + kBoxBytes, &tdy, col0 + 64, row0, full + kBar * s);
-                for (uint32_t k = 0; k < g.blocks; ++k)
+                for (uint32_t k = 0; k < (g.with_dh ? g.blocks : 0); ++k)
                     async::tma_load_3d(buf + (2 + k) * kBoxBytes, &tB, k * 64, col0, job.c.adapter, full + kBar * s);
             }
             __syncwarp();
@@ -603,12 +691,13 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
         for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) tiles::drain(full + kBar * (i % S), (i / S) & 1);
     } else if (me.warp == 1) {
         const uint32_t id_dh = tiles::idesc(is_bf16<T>(), false, true, job.n16);
-        const uint32_t id_db = tiles::idesc(is_bf16<T>(), true, true, job.n16);
+        const uint32_t id_db = tiles::idesc(is_bf16<T>(), true, true, g.both ? g.both : job.n16);
+        const uint32_t acc = tmem + (g.with_dh ? 2 * g.r16 : 0), wide = g.both ? g.both : g.r16;
         uint32_t i = 0;
         for (uint32_t t = 0; t < n_tiles; ++t) {
             const uint32_t h = operand + (t % H) * op_bytes, d = t & 1;
             w.pass(ready + kBar * (t % H), (t / H) & 1);
-            if (t >= 2) w.pass(free_ + kBar * d, (t / 2 - 1) & 1);
+            if (g.with_dh && t >= 2) w.pass(free_ + kBar * d, (t / 2 - 1) & 1);
             for (uint32_t j = 0; j < job.width; ++j, ++i) {
                 const uint32_t s = i % S, buf = base + s * stage;
                 w.pass(full + kBar * s, (i / S) & 1);
@@ -617,15 +706,16 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
                 __syncwarp();
                 if (tiles::elect_one()) {
                     const uint64_t b = tiles::desc(buf + 2 * kBoxBytes, kBoxBytes), m = tiles::desc(buf, kBoxBytes);
+                    if (g.with_dh)
 #pragma unroll
-                    for (uint32_t k = 0; k < 8; ++k)
-                        tiles::mma(tmem + d * g.r16, tiles::desc(buf + k / 4 * kBoxBytes, 16) + k % 4 * tiles::kStepK,
-                                   b + k * tiles::kStepMN, id_dh, j > 0 || k > 0);
-                    for (uint32_t p = 0; p < 2; ++p) {
+                        for (uint32_t k = 0; k < 8; ++k)
+                            tiles::mma(tmem + d * g.r16, tiles::desc(buf + k / 4 * kBoxBytes, 16) + k % 4 * tiles::kStepK,
+                                       b + k * tiles::kStepMN, id_dh, j > 0 || k > 0);
+                    for (uint32_t p = 0; p < (g.both ? 1 : 2); ++p) {
                         const uint64_t hd = tiles::desc(h + p * g.blocks * kBoxBytes, kBoxBytes);
 #pragma unroll
                         for (uint32_t k = 0; k < 8; ++k)
-                            tiles::mma(tmem + (2 + j) * g.r16, m + k * tiles::kStepMN, hd + k * tiles::kStepMN, id_db,
+                            tiles::mma(acc + j * wide, m + k * tiles::kStepMN, hd + k * tiles::kStepMN, id_db,
                                        t > 0 || p > 0 || k > 0);
                     }
                     tcs::commit(empty + kBar * s);
@@ -640,78 +730,39 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
         }
         tiles::drain(all, 0);
     } else if (me.warp < 10) {
-        const uint32_t worker = threadIdx.x - 64, quarter = me.warp & 3, half = (me.warp - 2) / 4;
-        const uint32_t groups = job.n16 / 4, row = quarter * 32 + me.lane;
-        auto hidden = [&](const AdapterTile &t, uint32_t r, uint32_t j) {
-            if (r >= t.rows || j >= g.a.r_max) return make_float4(0.f, 0.f, 0.f, 0.f);
-            return below(*reinterpret_cast<const float4 *>(g.a.h_in + (size_t)(t.row0 + r) * g.a.r_max + j), j, job.rank, 1.f);
-        };
-        float most = 0.f;
-        if (!is_bf16<T>()) {
-            for (uint32_t t = job.c.begin; t < job.c.end; ++t) {
-                const AdapterTile tile = g.tiles[t];
-                for (uint32_t k = worker; k < tile.rows * groups; k += kGradWorkers) {
-                    const float4 v = hidden(tile, k / groups, k % groups * 4);
-                    most = fmaxf(most, fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
-                }
-            }
-            most = group_max(most, &s_most, 1, kGradWorkers);
-        }
-        const float up = range_scale<T>(most);
-        auto prepare = [&](uint32_t t) {
+        const uint32_t quarter = me.warp & 3, half = (me.warp - 2) / 4;
+        const uint32_t row = quarter * 32 + me.lane;
+        tiles::previous_done();
+        for (uint32_t t = 0; t < (g.with_dh ? n_tiles : 0); ++t) {
+            const uint32_t d = t & 1;
             const AdapterTile tile = g.tiles[job.c.begin + t];
-            if (t >= H) w.pass(used + kBar * (t % H), (t / H - 1) & 1);
-            __syncwarp();
-            for (uint32_t k = worker; k < kTileRows * groups; k += kGradWorkers) {
-                const uint32_t r = k / groups, j = k % groups * 4;
-                const float4 v = hidden(tile, r, j);
-                put_parts<T>(operand + (t % H) * op_bytes, g.blocks, r, j, make_float4(v.x * up, v.y * up, v.z * up, v.w * up));
-            }
-            async::fence_proxy_async();
-            arrive_warp(ready + kBar * (t % H), me.lane);
-        };
-        prepare(0);
-        for (uint32_t t = 0; t < n_tiles; ++t) {
-            if (t + 1 < n_tiles) prepare(t + 1);
-            const uint32_t d = t & 1, tile_no = job.c.begin + t;
-            const AdapterTile tile = g.tiles[tile_no];
             w.pass(done + kBar * d, (t / 2) & 1);
             tcs::fence_after();
             __syncwarp();
             float *p = g.part_out + ((size_t)job.slab * g.a.n_tokens + tile.row0 + row) * g.r16;
-            float big = 0.f;
             for (uint32_t c = half * 16; c < job.n16; c += 32) {
                 float v[16];
                 tiles::ld16(tmem + ((quarter * 32) << 16) + d * g.r16 + c, v);
                 tcs::wait_ld();
-                if (row < tile.rows) {
+                if (row < tile.rows)
 #pragma unroll
                     for (uint32_t k = 0; k < 16; k += 4)
                         *reinterpret_cast<float4 *>(p + c + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
-                    if (!is_bf16<T>())
-#pragma unroll
-                        for (uint32_t k = 0; k < 16; ++k)
-                            if (c + k < job.rank) big = fmaxf(big, finite_abs(v[k]));
-                }
             }
             tcs::fence_before();
             arrive_warp(free_ + kBar * d, me.lane);
-            if (!is_bf16<T>()) {
-                for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-                if (me.lane == 0) g.most_out[((size_t)job.slab * g.n_tiles + tile_no) * kMostWarps + me.warp - 2] = big;
-            }
         }
         w.pass(all, 0);
         tcs::fence_after();
         __syncwarp();
-        const float scale = g.a.scales[job.c.adapter] * (1.f / up);
+        const float scale = g.a.scales[job.c.adapter] * (1.f / g.ups[job.c.begin]);
+        const uint32_t acc = tmem + (g.with_dh ? 2 * g.r16 : 0), wide = g.both ? g.both : g.r16;
         for (uint32_t j = 0; j < job.width; ++j) {
             const uint32_t col = (job.b0 + j) * kBlockCols + row;
-            float *p = g.grad + ((size_t)(blockIdx.x / g.cut.slabs) * g.cols + col) * g.r16;
+            float *p = g.grad + ((size_t)job.chunk * g.cols + col) * g.r16;
             for (uint32_t c = half * 16; c < job.n16; c += 32) {
                 float v[16];
-                tiles::ld16(tmem + ((quarter * 32) << 16) + (2 + j) * g.r16 + c, v);
-                tcs::wait_ld();
+                ld_both(acc + ((quarter * 32) << 16) + j * wide + c, g, v);
                 if (col < g.cols)
 #pragma unroll
                     for (uint32_t k = 0; k < 16; k += 4)
@@ -720,6 +771,8 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
             }
         }
         tcs::fence_before();
+    } else if (me.warp == 10) {
+        load_operands(g, job, operand, ready, used, w);
     } else if (fix) {
         // rows past a tile's end are another request's
         const dropout::Mask none;
@@ -729,7 +782,7 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
             __syncwarp();
             if (rows < kTileRows)
                 for (uint32_t k = 0; k < 2; ++k)
-                    clean_box(buf + k * kBoxBytes, none, 0, rows, 0, threadIdx.x - 320, 128, nullptr);
+                    clean_box<128, false>(buf + k * kBoxBytes, none, 0, rows, 0, threadIdx.x - 352, 0);
             async::fence_proxy_async();
             arrive_warp(fixed + kBar * s, me.lane);
         }
@@ -743,16 +796,22 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
 // expand_grad: per tile dx = dx_base + D'(dh A) of this range of columns, and over
 // the tiles dA += D(x)^T dh.
 template <typename T>
-__global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_constant__ CUtensorMap tx,
+__global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid_constant__ CUtensorMap tx,
                                                               const __grid_constant__ CUtensorMap tA,
                                                               const __grid_constant__ CUtensorMap tdx, const TileArgs g)
 {
     extern __shared__ uint8_t sm[];
     __shared__ __align__(8) uint64_t bars[3 * kMaxStages + 9];
-    __shared__ uint32_t s_tmem, s_most;
+    __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const Roles me;
-    const uint32_t S = g.stages, H = g.buffers, operand = aligned_smem(sm), op_bytes = operand_bytes(g.blocks);
+    if (blockIdx.x < g.n_bare) {
+        tiles::next_may_start();
+        tiles::previous_done();
+        bare_rows<T>(g.a, g.bare[blockIdx.x], g.cols, kExpandGradThreads);
+        return;
+    }
+    const uint32_t S = g.stages, H = g.buffers, operand = aligned_smem(sm), op_bytes = g.op_boxes * kBoxBytes;
     const uint32_t base = operand + H * op_bytes, stage = expand_grad_stage(g.r16), bar0 = async::smem_addr(bars);
     const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
     const uint32_t ready = bar0 + 3 * kBar * kMaxStages, used = ready + 2 * kBar;  // dh, by buffer
@@ -763,16 +822,16 @@ __global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_const
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
     const uint32_t a_box = g.r16 * 128, bits_at = 2 * kBoxBytes + 2 * a_box;
 
+    tiles::next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
-        s_most = 0;
         for (uint32_t s = 0; s < S; ++s) {
             async::mbar_init(full + kBar * s, 1);
-            async::mbar_init(fixed + kBar * s, 4);
+            async::mbar_init(fixed + kBar * s, 8);
             async::mbar_init(empty + kBar * s, 1);
         }
         for (uint32_t k = 0; k < 2; ++k) {
-            async::mbar_init(ready + kBar * k, kGradWorkers / 32);
+            async::mbar_init(ready + kBar * k, 1);
             async::mbar_init(used + kBar * k, 1);
             async::mbar_init(done + kBar * k, 1);
             async::mbar_init(free_ + kBar * k, kGradWorkers / 32);
@@ -811,8 +870,8 @@ __global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_const
         for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) tiles::drain(full + kBar * (i % S), (i / S) & 1);
     } else if (me.warp == 1) {
         const uint32_t id_dx = tiles::idesc(is_bf16<T>(), false, true, kBlockCols);
-        const uint32_t id_da = tiles::idesc(is_bf16<T>(), true, true, job.n16);
-        const uint32_t acc = tmem + 2 * kBlockCols;
+        const uint32_t id_da = tiles::idesc(is_bf16<T>(), true, true, g.both ? g.both : job.n16);
+        const uint32_t acc = tmem + 2 * kBlockCols, wide = g.both ? g.both : g.r16;
         uint32_t i = 0;
         for (uint32_t t = 0; t < n_tiles; ++t) {
             const uint32_t dh = operand + (t % H) * op_bytes;
@@ -828,14 +887,13 @@ __global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_const
                     const uint64_t A = tiles::desc(buf + 2 * kBoxBytes, a_box), m = tiles::desc(buf, kBoxBytes);
                     for (uint32_t p = 0; p < 2; ++p)
                         for (uint32_t k = 0; k < job.n16 / 16; ++k)
-                            tiles::mma(tmem + d * kBlockCols,
-                                       tiles::desc(dh + (p * g.blocks + k / 4) * kBoxBytes, 16) + k % 4 * tiles::kStepK,
-                                       A + k * tiles::kStepMN, id_dx, p > 0 || k > 0);
-                    for (uint32_t p = 0; p < 2; ++p) {
+                            tiles::mma(tmem + d * kBlockCols, operand_k(dh, p * g.lo + 16 * k), A + k * tiles::kStepMN, id_dx,
+                                       p > 0 || k > 0);
+                    for (uint32_t p = 0; p < (g.both ? 1 : 2); ++p) {
                         const uint64_t hd = tiles::desc(dh + p * g.blocks * kBoxBytes, kBoxBytes);
 #pragma unroll
                         for (uint32_t k = 0; k < 8; ++k)
-                            tiles::mma(acc + j * g.r16, m + k * tiles::kStepMN, hd + k * tiles::kStepMN, id_da,
+                            tiles::mma(acc + j * wide, m + k * tiles::kStepMN, hd + k * tiles::kStepMN, id_da,
                                        t > 0 || p > 0 || k > 0);
                     }
                     tcs::commit(done + kBar * d);
@@ -850,40 +908,11 @@ __global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_const
         tiles::drain(all, 0);
     } else if (me.warp < 10) {
         const uint32_t worker = threadIdx.x - 64, quarter = me.warp & 3, half = (me.warp - 2) / 4;
-        const uint32_t groups = job.n16 / 4, row = quarter * 32 + me.lane;
-        const float s_a = g.a.scales[job.c.adapter];
-        float most = 0.f;
-        if (!is_bf16<T>()) {
-            // (a bound: the ranges' largest partial sums, added up)
-            for (uint32_t t = job.c.begin + worker; t < job.c.end; t += kGradWorkers) {
-                float sum = 0.f;
-                for (uint32_t k = 0; k < g.slabs_in; ++k) {
-                    float m = 0.f;
-                    for (uint32_t q = 0; q < kMostWarps; ++q) m = fmaxf(m, g.most_in[((size_t)k * g.n_tiles + t) * kMostWarps + q]);
-                    sum += m;
-                }
-                most = fmaxf(most, finite_abs(sum * s_a));
-            }
-            most = group_max(most, &s_most, 1, kGradWorkers);
-        }
-        const float up = range_scale<T>(most), scale = g.a.mask.factor * (1.f / up);
-        auto prepare = [&](uint32_t t) {
-            const AdapterTile tile = g.tiles[job.c.begin + t];
-            if (t >= H) w.pass(used + kBar * (t % H), (t / H - 1) & 1);
-            __syncwarp();
-            for (uint32_t k = worker; k < kTileRows * groups; k += kGradWorkers) {
-                const uint32_t r = k / groups, j = k % groups * 4;
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (r < tile.rows) v = below(sum_parts(g, tile.row0 + r, j), j, job.rank, s_a);
-                put_parts<T>(operand + (t % H) * op_bytes, g.blocks, r, j, make_float4(v.x * up, v.y * up, v.z * up, v.w * up));
-            }
-            async::fence_proxy_async();
-            arrive_warp(ready + kBar * (t % H), me.lane);
-        };
-        prepare(0);
+        const uint32_t row = quarter * 32 + me.lane;
+        tiles::previous_done();
+        const float scale = g.a.mask.factor * (1.f / g.ups[job.c.begin]);
         uint32_t i = 0;
         for (uint32_t t = 0; t < n_tiles; ++t) {
-            if (H > 1 && t + 1 < n_tiles) prepare(t + 1);
             const AdapterTile tile = g.tiles[job.c.begin + t];
             for (uint32_t j = 0; j < job.width; ++j, ++i) {
                 const uint32_t s = i % S, buf = base + s * stage, d = i & 1, col0 = (job.b0 + j) * kBlockCols;
@@ -898,13 +927,13 @@ __global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_const
                 tcs::wait_ld();
                 tcs::fence_before();
                 arrive_warp(free_ + kBar * d, me.lane);
-                uint2 bits = make_uint2(~0u, ~0u);
+                uint2 bits = make_uint2(0u, 0u);
                 if (mask && row < tile.rows)
                     asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(bits.x), "=r"(bits.y) : "r"(buf + bits_at + half * 1024 + row * 8) : "memory");
                 const T *b = g.a.base && row < tile.rows ? (const T *)g.a.base + (uint64_t)(tile.row0 + row) * g.a.ld_base : nullptr;
 #pragma unroll
                 for (uint32_t c = 0; c < 8; ++c) {
-                    const uint32_t col = col0 + half * 64 + c * 8, keep = (c < 4 ? bits.x >> (8 * c) : bits.y >> (8 * (c - 4))) & 255;
+                    const uint32_t col = col0 + half * 64 + c * 8, drop = (c < 4 ? bits.x >> (8 * c) : bits.y >> (8 * (c - 4))) & 255;
                     uint4 o = make_uint4(0, 0, 0, 0);
                     if (b && col < g.cols) o = *reinterpret_cast<const uint4 *>(b + col);
                     uint32_t *u = reinterpret_cast<uint32_t *>(&o);
@@ -912,8 +941,8 @@ __global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_const
                     for (uint32_t k = 0; k < 4; ++k) {
                         const float2 f = unpack<T>(u[k]);
                         const float *a = &v[c / 2][(c % 2) * 8 + 2 * k];
-                        u[k] = pack<T>(keep >> (2 * k) & 1 ? fmaf(scale, a[0], f.x) : f.x,
-                                       keep >> (2 * k) & 2 ? fmaf(scale, a[1], f.y) : f.y);
+                        u[k] = pack<T>(drop >> (2 * k) & 1 ? f.x : fmaf(scale, a[0], f.x),
+                                       drop >> (2 * k) & 2 ? f.y : fmaf(scale, a[1], f.y));
                     }
                     st_shared16(buf + half * kBoxBytes + chunk_at(row, c), o);
                 }
@@ -942,37 +971,37 @@ __global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_const
                     if (me.warp == 2) arrive_warp(empty + kBar * s, me.lane);
                 }
             }
-            if (H == 1 && t + 1 < n_tiles) prepare(t + 1);
         }
         w.pass(all, 0);
         tcs::fence_after();
         __syncwarp();
         for (uint32_t j = 0; j < job.width; ++j) {
             const uint32_t col = (job.b0 + j) * kBlockCols + row;
-            float *p = g.grad + (size_t)(blockIdx.x / g.cut.slabs) * g.r16 * g.cols + col;
+            float *p = g.grad + (size_t)job.chunk * g.r16 * g.cols + col;
             for (uint32_t c = half * 16; c < job.n16; c += 32) {
                 float v[16];
-                tiles::ld16(tmem + ((quarter * 32) << 16) + 2 * kBlockCols + j * g.r16 + c, v);
-                tcs::wait_ld();
+                ld_both(tmem + ((quarter * 32) << 16) + 2 * kBlockCols + j * (g.both ? g.both : g.r16) + c, g, v);
                 if (col < g.cols)
 #pragma unroll
                     for (uint32_t k = 0; k < 16; ++k) p[(size_t)(c + k) * g.cols] = v[k] * scale;
             }
         }
         tcs::fence_before();
+    } else if (me.warp == 10) {
+        load_operands(g, job, operand, ready, used, w);
     } else if (fix) {
         for (uint32_t i = 0; i < job.n; ++i) {
             const uint32_t s = i % S, buf = base + s * stage, col0 = (job.b0 + i % job.width) * kBlockCols;
             const AdapterTile tile = g.tiles[job.c.begin + i / job.width];
             w.pass(full + kBar * s, (i / S) & 1);
             __syncwarp();
-            const uint32_t thread = threadIdx.x - 320;
+            const uint32_t thread = threadIdx.x - 352;
             if (mask || tile.rows < kTileRows)
                 for (uint32_t k = 0; k < 2; ++k)
-                    clean_box(buf + k * kBoxBytes, g.a.mask, tile.row0, tile.rows, col0 + k * 64, thread, 128,
-                              sm + (buf + bits_at + k * 1024 - async::smem_addr(sm)));
+                    clean_box<256, true>(buf + k * kBoxBytes, g.a.mask, tile.row0, tile.rows, col0 + k * 64, thread,
+                                         buf + bits_at + k * 1024);
             if (clean_A)  // A's rows from the rank to the next multiple of 16 are not A's
-                for (uint32_t k = thread; k < (job.n16 - job.rank) * 16; k += 128)
+                for (uint32_t k = thread; k < (job.n16 - job.rank) * 16; k += 256)
                     st_shared16(buf + 2 * kBoxBytes + k % 16 / 8 * a_box + chunk_at(job.rank + k / 16, k % 8), make_uint4(0, 0, 0, 0));
             async::fence_proxy_async();
             arrive_warp(fixed + kBar * s, me.lane);
@@ -982,6 +1011,63 @@ __global__ void __launch_bounds__(kGradThreads) k_expand_grad(const __grid_const
     __syncthreads();
     tcs::fence_after();
     if (me.warp == 1) tcs::tmem_dealloc(tmem, g.tmem_cols);
+}
+
+// The images of h or dh (DH: the sum of its parts, times s_a): a block 32 rows of
+// a tile, zero past the tile and from the rank on.  fp16 goes by a power of two that is
+// one for all of an adapter's tiles (they share accumulators), from the largest
+// value of each quarter tile (MOST: this kernel's first pass).
+template <typename T, bool DH, bool MOST>
+__global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image, float *ups, float *most, const uint32_t *tile_begin)
+{
+    __shared__ uint32_t s_most;
+    const uint32_t tile = blockIdx.x / 4, r0 = blockIdx.x % 4 * 32;
+    const AdapterTile t = g.tiles[tile];
+    const uint32_t rank = g.a.ranks[t.adapter], groups = g.r16 / 4;
+    const float s_a = DH ? g.a.scales[t.adapter] : 1.f;
+    if (threadIdx.x == 0) s_most = 0;
+    tiles::next_may_start();
+    tiles::previous_done();
+    __syncthreads();
+    auto value = [&](uint32_t k) {
+        const uint32_t r = r0 + k / groups, j = k % groups * 4;
+        if (r >= t.rows || j >= rank) return make_float4(0.f, 0.f, 0.f, 0.f);
+        return below(DH ? sum_parts(g, t.row0 + r, j)
+                        : *reinterpret_cast<const float4 *>(g.a.h_in + (size_t)(t.row0 + r) * g.a.r_max + j),
+                     j, rank, s_a);
+    };
+    float up = 1.f;
+    if (!is_bf16<T>()) {
+        float big = 0.f;
+        if (MOST) {
+            for (uint32_t k = threadIdx.x; k < 32 * groups; k += 256) {
+                const float4 v = value(k);
+                big = fmaxf(big, fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
+            }
+        } else {
+            for (uint32_t k = 4 * tile_begin[t.adapter] + threadIdx.x; k < 4 * tile_begin[t.adapter + 1]; k += 256) big = fmaxf(big, most[k]);
+        }
+        for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+        if ((threadIdx.x & 31) == 0) atomicMax(&s_most, __float_as_uint(big));
+        __syncthreads();
+        if (MOST) {
+            if (threadIdx.x == 0) most[blockIdx.x] = __uint_as_float(s_most);
+            return;
+        }
+        up = range_scale<T>(__uint_as_float(s_most));
+    }
+    if (threadIdx.x == 0 && r0 == 0) ups[tile] = up;
+    uint8_t *to = image + (size_t)tile * g.op_boxes * kBoxBytes;
+    for (uint32_t k = threadIdx.x; k < 32 * groups; k += 256) {
+        const uint32_t row = r0 + k / groups, j = k % groups * 4;
+        const float4 v = value(k);
+        uint2 hi, lo;
+        split2<T>(v.x * up, v.y * up, hi.x, lo.x);
+        split2<T>(v.z * up, v.w * up, hi.y, lo.y);
+        auto at = [&](uint32_t e) { return to + (e / 64) * kBoxBytes + chunk_at(row, (e % 64) / 8) + (e % 8) * 2; };
+        *reinterpret_cast<uint2 *>(at(j)) = hi;
+        *reinterpret_cast<uint2 *>(at(g.lo + j)) = lo;
+    }
 }
 
 // dA and dB of every adapter: its chunks' sums added up in order, zero where
@@ -999,45 +1085,24 @@ __global__ void __launch_bounds__(256) k_grad_sum(const GradSum A, const GradSum
                                                   uint32_t first)
 {
     const GradSum &g = blockIdx.x < blocks_A ? A : B;
-    const uint32_t ad = first + blockIdx.y, rank = ranks[ad], per_row = g.inner / 8;
+    const uint32_t ad = first + blockIdx.y, rank = ranks[ad], per_row = g.inner / 4;
     const uint64_t k = (uint64_t)(blockIdx.x < blocks_A ? blockIdx.x : blockIdx.x - blocks_A) * 256 + threadIdx.x;
     if (k >= (uint64_t)g.rows * per_row) return;
-    const uint32_t row = (uint32_t)(k / per_row), col = (uint32_t)(k % per_row) * 8;
-    float v[8] = {};
-    if (row < (g.rank_rows ? rank : g.rows) && col < (g.rank_rows ? g.inner : rank))
-        for (uint32_t c = g.begin[ad]; c < g.begin[ad + 1]; ++c) {
-            const float4 *p = reinterpret_cast<const float4 *>(g.part + ((size_t)c * g.part_rows + row) * g.part_inner + col);
-            const float4 x = p[0], y = p[1];
-            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+    const uint32_t row = (uint32_t)(k / per_row), col = (uint32_t)(k % per_row) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    tiles::previous_done();
+    if (row < (g.rank_rows ? rank : g.rows) && col < (g.rank_rows ? g.inner : rank)) {
+        const uint32_t end = g.begin[ad + 1];
+        const size_t step = (size_t)g.part_rows * g.part_inner;
+        const float *p = g.part + ((size_t)g.begin[ad] * g.part_rows + row) * g.part_inner + col;
+#pragma unroll 8
+        for (uint32_t c = g.begin[ad]; c < end; ++c, p += step) {
+            const float4 x = *reinterpret_cast<const float4 *>(p);
+            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
         }
-    if (!g.rank_rows)
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-            if (col + i >= rank) v[i] = 0.f;
-    *reinterpret_cast<uint4 *>((T *)g.out + ((size_t)ad * g.rows + row) * g.inner + col) =
-        make_uint4(pack<T>(v[0], v[1]), pack<T>(v[2], v[3]), pack<T>(v[4], v[5]), pack<T>(v[6], v[7]));
-}
-
-// rows without an adapter: out = base (or zero), h = 0
-template <typename T>
-__global__ void __launch_bounds__(256) k_bare(const AdapterArgs a, const AdapterTile *runs, uint32_t cols)
-{
-    const AdapterTile t = runs[blockIdx.y];
-    const bool copy = a.base != a.out;
-    for (uint32_t r = blockIdx.x; r < t.rows; r += gridDim.x) {
-        const uint64_t row = t.row0 + r;
-        const T *b = a.base ? (const T *)a.base + row * a.ld_base : nullptr;
-        T *o = (T *)a.out + row * a.ld_out;
-        if (copy) {
-            const bool wide = (((uintptr_t)o | (uintptr_t)b) & 15) == 0;
-            const uint32_t n = wide ? cols / (16 / sizeof(T)) : 0;
-            for (uint32_t i = threadIdx.x; i < n; i += 256)
-                reinterpret_cast<uint4 *>(o)[i] = b ? reinterpret_cast<const uint4 *>(b)[i] : make_uint4(0, 0, 0, 0);
-            for (uint32_t i = n * (16 / sizeof(T)) + threadIdx.x; i < cols; i += 256) o[i] = b ? b[i] : narrow<T>(0.f);
-        }
-        if (a.h)
-            for (uint32_t i = threadIdx.x; i < a.r_max; i += 256) a.h[row * a.r_max + i] = 0.f;
     }
+    if (!g.rank_rows) v = below(v, col, rank, 1.f);
+    *reinterpret_cast<uint2 *>((T *)g.out + ((size_t)ad * g.rows + row) * g.inner + col) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
 }
 
 // ---------------------------------------------------------------------------
@@ -1090,11 +1155,11 @@ Cut cut_columns(uint32_t boxes, uint32_t units, uint32_t want)
 struct ForwardShape {
     RankShape r;
     Cut shrink, expand;
-    ForwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) : r(b->r_max)
+    ForwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t n_tiles) : r(b->r_max)
     {
         const uint32_t resident = 2 * (uint32_t)std::max(b->ctx->sm_count, 1);
-        shrink = cut_columns(ceil_div(d_in, 64), b->n_tiles, resident);
-        expand = cut_columns(ceil_div(d_out, 64), b->n_tiles, resident);
+        shrink = cut_columns(ceil_div(d_in, 64), n_tiles, resident);
+        expand = cut_columns(ceil_div(d_out, 64), n_tiles, resident);
     }
     uint64_t part_bytes(const fiona_adapter_batch *b) const
     {
@@ -1102,11 +1167,23 @@ struct ForwardShape {
     }
 };
 
+// `after`: the kernel waits for the one before it by itself
 template <typename K>
-int launch(K kernel, uint32_t grid, uint32_t threads, size_t smem, cudaStream_t s, void **args, const char *what)
+int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t s, bool after, void **args, const char *what)
 {
-    if (const int rc = allow_shared_memory((const void *)kernel, smem, what)) return rc;
-    const cudaError_t e = cudaLaunchKernel((const void *)kernel, dim3(grid), dim3(threads), args, smem, s);
+    if (smem > 48 * 1024)
+        if (const int rc = allow_shared_memory((const void *)kernel, smem, what)) return rc;
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid;
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = s;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &attr;
+    c.numAttrs = after ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelExC(&c, (const void *)kernel, args);
     if (e != cudaSuccess) return set_error(FIONA_ERR_CUDA, "%s launch: %s", what, cudaGetErrorString(e));
     return FIONA_OK;
 }
@@ -1124,27 +1201,21 @@ uint32_t stages_for(uint32_t fixed, uint32_t stage, uint32_t least)
 }
 
 template <typename T>
-int bare(const fiona_adapter_batch *b, const AdapterArgs &a, uint32_t cols, cudaStream_t s)
-{
-    for (uint32_t i = 0; i < b->n_bare; i += 65535)
-        k_bare<T><<<dim3(std::min(b->max_bare, 512u), std::min(b->n_bare - i, 65535u)), 256, 0, s>>>(a, b->d_bare + i, cols);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? FIONA_OK : set_error(FIONA_ERR_CUDA, "adapter rows launch: %s", cudaGetErrorString(e));
-}
-
-template <typename T>
-int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const AdapterArgs &a, void *work)
+int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const AdapterArgs &a, void *work, bool only_long)
 {
     int rc = FIONA_OK;
-    if (b->n_bare && (rc = bare<T>(b, a, a.d_out, s))) return rc;
-    if (!b->n_tiles) return FIONA_OK;
-    const ForwardShape f(b, a.d_in, a.d_out);
+    const uint32_t n_tiles = only_long ? b->n_long : b->n_tiles;
+    if (!n_tiles && !b->n_bare) return FIONA_OK;
+    const ForwardShape f(b, a.d_in, a.d_out, n_tiles);
     TileArgs g{};
     g.a = a;
-    g.tiles = b->d_tiles;
-    g.n_tiles = b->n_tiles;
+    g.tiles = only_long ? b->d_long : b->d_tiles;
+    g.n_tiles = n_tiles;
     g.r16 = f.r.r16;
     g.blocks = f.r.blocks;
+    g.lo = f.r.lo;
+    g.op_boxes = f.r.boxes;
+    g.both = f.r.both;
     g.err = b->ctx->d_kerr;
     g.wait_ns = kWaitNs;
     g.part_out = static_cast<float *>(work);
@@ -1160,18 +1231,22 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     g.cut = f.shrink;
     g.cols = a.d_in;
     g.boxes = ceil_div(a.d_in, 64);
-    g.stages = stages_for(0, shrink_stage(g.r16), 3);
+    const uint32_t stage = shrink_stage<false>(g.r16, g.blocks);
+    g.stages = stages_for(0, stage, 3);
     void *sargs[] = {&tx, &tA, &g};
-    rc = launch(k_shrink<T>, b->n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * shrink_stage(g.r16) + 1024, s,
-                sargs, "adapter shrink");
-    if (rc) return rc;
+    if (n_tiles && (rc = launch(k_shrink<T, false>, n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024,
+                                   s, false, sargs, "adapter shrink")))
+        return rc;
+    g.bare = b->d_bare;
+    g.n_bare = b->n_bare;
     g.cut = f.expand;
     g.cols = a.d_out;
     g.boxes = ceil_div(a.d_out, 64);
-    g.stages = stages_for(operand_bytes(g.blocks), expand_stage(g.blocks), 3);
+    g.stages = stages_for(g.op_boxes * kBoxBytes, expand_stage(g.blocks), 3);
     void *eargs[] = {&tbase, &tB, &tout, &g};
-    return launch(k_expand<T>, b->n_tiles * g.cut.slabs, kExpandThreads,
-                  operand_bytes(g.blocks) + (size_t)g.stages * expand_stage(g.blocks) + 1024, s, eargs, "adapter expand");
+    return launch(k_expand<T>, n_tiles * g.cut.slabs + b->n_bare, kExpandThreads,
+                  g.op_boxes * kBoxBytes + (size_t)g.stages * expand_stage(g.blocks) + 1024, s, n_tiles != 0, eargs,
+                  "adapter expand");
 }
 
 // How one of the gradients' passes is cut: blocks of 128 columns a CTA, tiles a
@@ -1183,18 +1258,19 @@ struct GradCut {
     Cut cut{};
     const AdapterChunks *chunks = nullptr;
     uint32_t tmem_cols = 0;
-    GradCut(const fiona_adapter_batch *b, uint32_t cols, const RankShape &r, bool shrink)
+    GradCut(const fiona_adapter_batch *b, uint32_t cols, const RankShape &r, uint32_t fixed)
     {
         const uint32_t n = ceil_div(cols, kBlockCols), sms = (uint32_t)std::max(b->ctx->sm_count, 1);
-        const uint32_t fixed = shrink ? 2 * r.r16 : 2 * kBlockCols;
-        const uint32_t most = std::min({n, 4u, (512 - std::max(fixed, 2 * kBlockCols)) / r.r16});
+        const uint32_t wide = r.both ? r.both : r.r16;
+        const uint32_t most = std::min({n, 4u, (512 - fixed) / wide});
+        const bool parts = fixed == 2 * r.r16;
         double best = 0;
         for (uint32_t width = most; width >= 1; --width)
             for (const AdapterChunks &c : b->chunks) {
                 const uint32_t slabs = ceil_div(n, width);
                 const double waves = ceil_div(c.count * slabs, sms);
                 const double us = waves * (2.0 + c.size * (0.75 * width + 0.4) + 0.01 * width * r.r16) +
-                                  8.0 * c.count * (double)cols * r.r16 / 5e6 + (shrink ? 8.0 : 0.0) * slabs * b->n_tokens * (double)r.r16 / 5e6;
+                                  8.0 * c.count * (double)cols * r.r16 / 5e6 + (parts ? 8.0 : 0.0) * slabs * b->n_tokens * (double)r.r16 / 5e6;
                 if (!chunks || us < best) {
                     best = us;
                     chunks = &c;
@@ -1202,22 +1278,28 @@ struct GradCut {
                 }
             }
         tmem_cols = 32;
-        while (tmem_cols < fixed + cut.width * r.r16) tmem_cols *= 2;
+        while (tmem_cols < fixed + cut.width * wide) tmem_cols *= 2;
     }
 };
 
 struct BackwardShape {
     RankShape r;
+    bool apart;  // dh by a pass of its own
+    Cut dh_cut{};
     GradCut shrink, expand;
-    uint64_t part, grad_A, grad_B, most, bytes;  // offsets in the workspace
+    uint64_t part, image, dh_image, grad_A, grad_B, most, ups, bytes;  // offsets in the workspace
     BackwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
-        : r(b->r_max), shrink(b, d_out, r, true), expand(b, d_in, r, false)
+        : r(b->r_max), apart(r.r16 > 64), shrink(b, d_out, r, apart ? 0 : 2 * r.r16), expand(b, d_in, r, 2 * kBlockCols)
     {
+        dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1)) : shrink.cut;
         part = 0;
-        grad_A = part + align_up((uint64_t)shrink.cut.slabs * b->n_tokens * r.r16 * 4);
+        image = part + align_up((uint64_t)dh_cut.slabs * b->n_tokens * r.r16 * 4);
+        dh_image = image + (uint64_t)b->n_tiles * r.boxes * kBoxBytes;
+        grad_A = dh_image + (uint64_t)b->n_tiles * r.boxes * kBoxBytes;
         grad_B = grad_A + align_up((uint64_t)expand.chunks->count * d_in * r.r16 * 4);
         most = grad_B + align_up((uint64_t)shrink.chunks->count * d_out * r.r16 * 4);
-        bytes = most + align_up((uint64_t)shrink.cut.slabs * b->n_tiles * kMostWarps * 4);
+        ups = most + align_up((uint64_t)b->n_tiles * 4 * 4);
+        bytes = ups + align_up((uint64_t)b->n_tiles * 2 * 4);
     }
 };
 
@@ -1225,62 +1307,99 @@ template <typename T>
 int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const AdapterArgs &a, void *work)
 {
     int rc = FIONA_OK;
-    if (b->n_bare && (rc = bare<T>(b, a, a.d_in, s))) return rc;
     const BackwardShape f(b, a.d_in, a.d_out);
     uint8_t *ws = static_cast<uint8_t *>(work);
-    if (b->n_tiles) {
+    if (b->n_tiles || b->n_bare) {
         TileArgs g{};
         g.a = a;
         g.tiles = b->d_tiles;
         g.n_tiles = b->n_tiles;
         g.r16 = f.r.r16;
         g.blocks = f.r.blocks;
-        g.buffers = f.r.blocks == 1 ? 2 : 1;
+    g.lo = f.r.lo;
+    g.op_boxes = f.r.boxes;
+    g.both = f.r.both;
         g.err = b->ctx->d_kerr;
         g.wait_ns = kWaitNs;
         CUtensorMap tx, tA, tdy, tB, tdx;
         if ((rc = tensor_map(&tx, dtype, a.x, a.d_in, a.n_tokens, 0, a.ldx, kTileRows)) ||
             (rc = tensor_map(&tA, dtype, a.A, a.d_in, a.r_max, a.n_adapters, a.d_in, f.r.r16)) ||
             (rc = tensor_map(&tdy, dtype, a.dy, a.d_out, a.n_tokens, 0, a.ld_dy, kTileRows)) ||
-            (rc = tensor_map(&tB, dtype, a.B, a.r_max, a.d_out, a.n_adapters, a.r_max, kBlockCols)) ||
+            (rc = tensor_map(&tB, dtype, a.B, a.r_max, a.d_out, a.n_adapters, a.r_max, f.apart ? 64 : kBlockCols)) ||
             (rc = tensor_map(&tdx, dtype, a.out, a.d_in, a.n_tokens, 0, a.ld_out, kTileRows)))
             return rc;
-        const uint32_t op = g.buffers * operand_bytes(g.blocks);
+        const uint32_t op = g.op_boxes * kBoxBytes;
+        g.part_out = reinterpret_cast<float *>(ws + f.part);
+        // h as an operand
+        uint8_t *image = ws + f.image;
+        float *ups = reinterpret_cast<float *>(ws + f.ups), *most = reinterpret_cast<float *>(ws + f.most);
+        void *iargs[] = {&g, &image, &ups, &most, (void *)&b->d_tile_begin};
+        const dim3 quarters(4 * b->n_tiles);
+        const bool any = b->n_tiles != 0;
+        if (any && !is_bf16<T>() && (rc = launch(k_image<T, false, true>, quarters, 256, 0, s, false, iargs, "adapter image"))) return rc;
+        if (any && (rc = launch(k_image<T, false, false>, quarters, 256, 0, s, !is_bf16<T>(), iargs, "adapter image"))) return rc;
+        if (any && f.apart) {
+            const uint32_t stage = shrink_stage<true>(g.r16, g.blocks);
+            g.cols = a.d_out;
+            g.boxes = ceil_div(a.d_out, 64);
+            g.cut = f.dh_cut;
+            g.stages = stages_for(0, stage, 3);
+            void *args[] = {&tdy, &tB, &g};
+            rc = launch(k_shrink<T, true>, b->n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024, s, true,
+                        args, "adapter dh");
+            if (rc) return rc;
+        }
+        g.with_dh = !f.apart;
         g.chunks = f.shrink.chunks->d_chunks;
         g.cols = a.d_out;
         g.boxes = ceil_div(a.d_out, kBlockCols);
         g.cut = f.shrink.cut;
         g.tmem_cols = f.shrink.tmem_cols;
-        g.part_out = reinterpret_cast<float *>(ws + f.part);
-        g.most_out = reinterpret_cast<float *>(ws + f.most);
         g.grad = reinterpret_cast<float *>(ws + f.grad_B);
-        g.stages = std::min(kMaxStages, (kSmemOne - op) / shrink_grad_stage(g.blocks));
+        const uint32_t sstage = shrink_grad_stage(g.with_dh ? g.blocks : 0);
+        g.buffers = 2;
+        g.stages = std::min(kMaxStages, (kSmemOne - 2 * op) / sstage);
         void *sargs[] = {&tdy, &tB, &g};
-        rc = launch(k_shrink_grad<T>, f.shrink.chunks->count * g.cut.slabs, kGradThreads,
-                    op + (size_t)g.stages * shrink_grad_stage(g.blocks) + 1024, s, sargs, "adapter shrink_grad");
-        if (rc) return rc;
+        g.image = image;
+        g.ups = ups;
+        if (any && (rc = launch(k_shrink_grad<T>, f.shrink.chunks->count * g.cut.slabs, kGradThreads,
+                                2 * op + (size_t)g.stages * sstage + 1024, s, true, sargs, "adapter shrink_grad")))
+            return rc;
+        // dh as an operand (its image in a place of its own: the next kernel starts
+        // while this one reads)
+        image = ws + f.dh_image;
+        ups += b->n_tiles;
         g.part_in = g.part_out;
-        g.most_in = g.most_out;
-        g.slabs_in = g.cut.slabs;
+        g.slabs_in = f.dh_cut.slabs;
+        if (any && !is_bf16<T>() && (rc = launch(k_image<T, true, true>, quarters, 256, 0, s, true, iargs, "adapter image"))) return rc;
+        if (any && (rc = launch(k_image<T, true, false>, quarters, 256, 0, s, true, iargs, "adapter image"))) return rc;
+        g.image = image;
+        g.ups = ups;
+        g.bare = b->d_bare;
+        g.n_bare = b->n_bare;
+        g.n_chunks = f.expand.chunks->count;
         g.chunks = f.expand.chunks->d_chunks;
         g.cols = a.d_in;
         g.boxes = ceil_div(a.d_in, kBlockCols);
         g.cut = f.expand.cut;
         g.tmem_cols = f.expand.tmem_cols;
         g.grad = reinterpret_cast<float *>(ws + f.grad_A);
-        g.stages = std::min(kMaxStages, (kSmemOne - op) / expand_grad_stage(g.r16));
+        g.buffers = g.blocks == 1 ? 2 : 1;
+        g.stages = std::min(kMaxStages, (kSmemOne - g.buffers * op) / expand_grad_stage(g.r16));
         void *eargs[] = {&tx, &tA, &tdx, &g};
-        rc = launch(k_expand_grad<T>, f.expand.chunks->count * g.cut.slabs, kGradThreads,
-                    op + (size_t)g.stages * expand_grad_stage(g.r16) + 1024, s, eargs, "adapter expand_grad");
+        rc = launch(k_expand_grad<T>, g.n_chunks * g.cut.slabs + b->n_bare, kExpandGradThreads,
+                    g.buffers * op + (size_t)g.stages * expand_grad_stage(g.r16) + 1024, s, any, eargs, "adapter expand_grad");
         if (rc) return rc;
     }
     const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_max, a.d_in, f.r.r16, a.d_in, 1};
     const GradSum B{reinterpret_cast<const float *>(ws + f.grad_B), f.shrink.chunks->d_begin, a.dB, a.d_out, a.r_max, a.d_out, f.r.r16, 0};
-    const uint32_t blocks_A = ceil_div(a.r_max * (a.d_in / 8), 256), blocks_B = ceil_div(a.d_out * (a.r_max / 8), 256);
-    for (uint32_t i = 0; i < a.n_adapters; i += 65535)
-        k_grad_sum<T><<<dim3(blocks_A + blocks_B, std::min(a.n_adapters - i, 65535u)), 256, 0, s>>>(A, B, a.ranks, blocks_A, i);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? FIONA_OK : set_error(FIONA_ERR_CUDA, "adapter gradient launch: %s", cudaGetErrorString(e));
+    const uint32_t blocks_A = ceil_div(a.r_max * (a.d_in / 4), 256), blocks_B = ceil_div(a.d_out * (a.r_max / 4), 256);
+    for (uint32_t i = 0; i < a.n_adapters && rc == FIONA_OK; i += 65535) {
+        void *args[] = {(void *)&A, (void *)&B, (void *)&a.ranks, (void *)&blocks_A, &i};
+        rc = launch(k_grad_sum<T>, dim3(blocks_A + blocks_B, std::min(a.n_adapters - i, 65535u)), 256, 0, s, b->n_tiles || b->n_bare,
+                    args, "adapter gradients");
+    }
+    return rc;
 }
 
 }  // namespace
@@ -1292,13 +1411,14 @@ bool adapter_tiles_apply(const fiona_adapter_batch *b, uint32_t d_in, uint32_t, 
 
 uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
 {
-    return std::max(ForwardShape(b, d_in, d_out).part_bytes(b), BackwardShape(b, d_in, d_out).bytes);
+    return std::max({ForwardShape(b, d_in, d_out, b->n_tiles).part_bytes(b), ForwardShape(b, d_in, d_out, b->n_long).part_bytes(b), BackwardShape(b, d_in, d_out).bytes});
 }
 
-int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work)
+int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,
+                                 bool only_long)
 {
-    return dtype == FIONA_BF16 ? forward<__nv_bfloat16>(b, (cudaStream_t)stream, dtype, a, work)
-                               : forward<__half>(b, (cudaStream_t)stream, dtype, a, work);
+    return dtype == FIONA_BF16 ? forward<__nv_bfloat16>(b, (cudaStream_t)stream, dtype, a, work, only_long)
+                               : forward<__half>(b, (cudaStream_t)stream, dtype, a, work, only_long);
 }
 
 int launch_adapter_tiles_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work)
