@@ -13,6 +13,7 @@ import ctypes
 from typing import Any, Optional, Sequence
 
 import numpy as np
+import torch
 
 from . import fiona as F
 
@@ -54,41 +55,49 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-_dtypes: Optional[dict] = None
+_dtypes = {torch.float32: FIONA_F32, torch.float16: FIONA_F16, torch.bfloat16: FIONA_BF16}
 
 
 def _dtype(t: Any) -> int:
-    global _dtypes
-    if _dtypes is None:
-        import torch
-        _dtypes = {torch.float32: FIONA_F32, torch.float16: FIONA_F16, torch.bfloat16: FIONA_BF16}
     d = _dtypes.get(t)
     if d is None:
         raise ValueError("element type %s: float32, float16 or bfloat16 expected" % t)
     return d
 
 
-def _expect(t: Any, shape: tuple, dtype: Any, device: int, name: str) -> None:
-    if tuple(t.shape) != shape or t.dtype != dtype:
+def _refuse(t: Any, shape: tuple, dtype: Any, device: Any, name: str) -> None:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError("%s: %s of %s expected, got %s of %s" % (name, shape, dtype, tuple(t.shape), t.dtype))
-    if t.device.type != "cuda" or t.device.index != device:
-        raise ValueError("%s is on %s, the context on cuda:%d" % (name, t.device, device))
+    if t.device != device:
+        raise ValueError("%s is on %s, the context on %s" % (name, t.device, device))
+    raise ValueError("%s: columns must be contiguous" % name)
 
 
-def _matrix(t: Any, shape: tuple, dtype: Any, device: int, name: str) -> int:
+def _matrix(t: Any, shape: tuple, dtype: Any, device: Any, name: str) -> int:
     """The row stride of a matrix with contiguous columns."""
-    _expect(t, shape, dtype, device, name)
-    row, col = t.stride()
-    if col != 1 and shape[1] > 1:
-        raise ValueError("%s: columns must be contiguous" % name)
-    return row if shape[0] > 1 else shape[1]
+    if t.shape == shape and t.dtype == dtype and t.device == device:
+        row, col = t.stride()
+        if col == 1 or shape[1] == 1:
+            return row if shape[0] > 1 else shape[1]
+    _refuse(t, shape, dtype, device, name)
 
 
-def _whole(t: Any, shape: tuple, dtype: Any, device: int, name: str) -> int:
-    _expect(t, shape, dtype, device, name)
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
-    return t.data_ptr()
+def _whole(t: Any, shape: tuple, dtype: Any, device: Any, name: str) -> int:
+    """The address of a contiguous tensor."""
+    if t.shape == shape and t.dtype == dtype and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(t, shape, dtype, device, name)
+
+
+_devices: dict = {}
+
+
+def _device(ctx: F.Context) -> Any:
+    """The context's device (None: validation only)."""
+    d = _devices.get(ctx.device)
+    if d is None and ctx.device >= 0:
+        d = _devices[ctx.device] = torch.device("cuda", ctx.device)
+    return d
 
 
 class Dropout:
@@ -131,6 +140,7 @@ class Batch:
                                                   ctypes.byref(h)), "fiona_adapter_batch_create")
         self.ctx, self.handle = ctx, h
         self.n_tokens, self.n_adapters, self.r_max = int(s[-1]), int(r.shape[0]), int(r_max)
+        self._dev = _device(ctx)
 
     def work_bytes(self, d_in: int, d_out: int, dtype: Any) -> int:
         n = ctypes.c_uint64()
@@ -141,14 +151,13 @@ class Batch:
     def workspace(self, d_in: int, d_out: int, dtype: Any):
         """A workspace for forward and backward calls on layers of these sizes;
         calls that may overlap in time need one each."""
-        import torch
         return torch.empty(max(self.work_bytes(d_in, d_out, dtype), 16), dtype=torch.uint8,
                            device="cuda:%d" % self.ctx.device)
 
     def _layer(self, x, A, B):
         if x.dim() != 2 or B.dim() != 3:
             raise ValueError("x [tokens][d_in] and B [adapters][d_out][r_max] expected")
-        d_in, d_out, dev = int(x.shape[1]), int(B.shape[1]), self.ctx.device
+        d_in, d_out, dev = x.shape[1], B.shape[1], self._dev
         return d_in, d_out, _Layer(d_in, d_out, _dtype(x.dtype), 0,
                                    _whole(A, (self.n_adapters, self.r_max, d_in), x.dtype, dev, "A"),
                                    _whole(B, (self.n_adapters, d_out, self.r_max), x.dtype, dev, "B"))
@@ -157,9 +166,8 @@ class Batch:
                 stream=None) -> None:
         """fiona_adapter_forward: out = base + s_a (D(x) A_a^T) B_a^T by rows;
         h [tokens][r_max] fp32, where given, gets D(x) A_a^T."""
-        import torch
         d_in, d_out, layer = self._layer(x, A, B)
-        T, dt, dev = self.n_tokens, x.dtype, self.ctx.device
+        T, dt, dev = self.n_tokens, x.dtype, self._dev
         ldx = _matrix(x, (T, d_in), dt, dev, "x")
         ld_out = _matrix(out, (T, d_out), dt, dev, "out")
         ld_base = 0 if base is None else _matrix(base, (T, d_out), dt, dev, "base")
@@ -175,9 +183,8 @@ class Batch:
                  stream=None) -> None:
         """fiona_adapter_backward: dx, dA and dB (overwritten) from the x, h and
         dropout of the forward pass and the gradient dy of its out."""
-        import torch
         d_in, d_out, layer = self._layer(x, A, B)
-        T, dt, dev = self.n_tokens, x.dtype, self.ctx.device
+        T, dt, dev = self.n_tokens, x.dtype, self._dev
         ldx = _matrix(x, (T, d_in), dt, dev, "x")
         ld_dy = _matrix(dy, (T, d_out), dt, dev, "dy")
         ld_dx = _matrix(dx, (T, d_in), dt, dev, "dx")
@@ -209,11 +216,11 @@ def dropout(ctx: F.Context, x, out, drop: Dropout, residual=None, stream=None) -
     x or residual)."""
     if x.dim() != 2:
         raise ValueError("x [rows][cols] expected")
-    shape = tuple(x.shape)
-    ldx = _matrix(x, shape, x.dtype, ctx.device, "x")
-    ld_out = _matrix(out, shape, x.dtype, ctx.device, "out")
-    ld_res = 0 if residual is None else _matrix(residual, shape, x.dtype, ctx.device, "residual")
-    F._check(lib().fiona_dropout(ctx.handle, F.stream_handle(stream), _dtype(x.dtype), shape[0], shape[1],
+    shape, dt, dev = x.shape, x.dtype, _device(ctx)
+    ldx = _matrix(x, shape, dt, dev, "x")
+    ld_out = _matrix(out, shape, dt, dev, "out")
+    ld_res = 0 if residual is None else _matrix(residual, shape, dt, dev, "residual")
+    F._check(lib().fiona_dropout(ctx.handle, F.stream_handle(stream), _dtype(dt), shape[0], shape[1],
                                  x.data_ptr(), ldx, F.addr(residual), ld_res, out.data_ptr(), ld_out, _spec(drop)),
              "fiona_dropout")
 

@@ -81,6 +81,7 @@ int launch_adapter_rows(const fiona_adapter_batch *b, void *stream, uint32_t dty
 // adapter_tiles.cu: 16-bit types on the tensor cores.  Whether buffers of this
 // shape and alignment go there (rows is false where a pointer or stride is not a
 // multiple of 16 bytes); its workspace; the passes.
+int adapter_tiles_configure();  // on the current device
 bool adapter_tiles_apply(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t dtype);
 uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
 int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,

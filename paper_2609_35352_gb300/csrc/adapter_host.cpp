@@ -248,6 +248,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
     if (ctx->device != FIONA_DEVICE_NONE) {
         DeviceGuard g(ctx->device);
         if (!g.ok) return set_error(FIONA_ERR_CUDA, "%s: cannot select device %d", who, ctx->device);
+        if (const int rc = adapter_tiles_configure()) return rc;
         std::vector<float> s(n_adapters, 1.f);
         if (scales) s.assign(scales, scales + n_adapters);
         std::vector<uint8_t> image;

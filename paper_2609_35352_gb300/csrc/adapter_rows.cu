@@ -27,19 +27,22 @@ using real::widen;
 
 constexpr uint32_t kThreads = 256, kWarps = kThreads / 32;
 constexpr uint32_t kCluster = 8;
-constexpr uint32_t kUnroll = 4;  // ranks a warp has under way
+// loads a lane has under way, for groups of G rows (with more, registers would
+// cost the second and third CTA of an SM)
+constexpr uint32_t under_way(uint32_t G) { return G <= 2 ? 8 : 4; }
 
 template <typename T>
 struct Vec {
     static constexpr uint32_t n = 16 / sizeof(T);
-    __device__ static void load(const T *p, float (&v)[n])
+    __device__ static void widen_all(const uint4 &u, float (&v)[n])
     {
-        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p));
         const T *x = reinterpret_cast<const T *>(&u);
 #pragma unroll
         for (uint32_t i = 0; i < n; ++i) v[i] = widen(x[i]);
     }
 };
+
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 struct RowsArgs {
     AdapterArgs a;
@@ -47,10 +50,62 @@ struct RowsArgs {
     uint32_t slice_in, slice_out;  // columns a CTA, multiples of 8
 };
 
-template <typename T, bool VA, bool VB, uint32_t G>
-__device__ void rows_body(const RowsArgs &g, const AdapterRows &rows, float *s_x, float *s_part, float *s_h)
+// This CTA's partial h of the ranks of one warp (every kWarps-th), UJ of them and
+// kUnroll / UJ vectors along the columns at a time.
+template <typename T, uint32_t G, uint32_t UJ>
+__device__ __forceinline__ void partial_h(const T *A, uint32_t d_in, uint32_t n_in, uint32_t rank, uint32_t slice,
+                                          const float *s_x, float *s_part, uint32_t warp, uint32_t lane)
 {
-    constexpr uint32_t V = Vec<T>::n;
+    constexpr uint32_t V = Vec<T>::n, UI = under_way(G) / UJ;
+    for (uint32_t j0 = warp; j0 < rank; j0 += kWarps * UJ) {
+        float acc[UJ][G] = {};
+        for (uint32_t i0 = lane * V; i0 < n_in; i0 += 32 * V * UI) {
+            uint4 w[UI][UJ];
+#pragma unroll
+            for (uint32_t q = 0; q < UI; ++q)
+#pragma unroll
+                for (uint32_t u = 0; u < UJ; ++u) {
+                    const uint32_t i = i0 + q * 32 * V, j = j0 + u * kWarps;
+                    w[q][u] = make_uint4(0, 0, 0, 0);
+                    if (i < n_in && j < rank) w[q][u] = __ldg(reinterpret_cast<const uint4 *>(A + (size_t)j * d_in + i));
+                }
+#pragma unroll
+            for (uint32_t q = 0; q < UI; ++q) {
+                const uint32_t i = i0 + q * 32 * V;
+                if (i >= n_in) break;
+                float x[G][V];
+#pragma unroll
+                for (uint32_t r = 0; r < G; ++r)
+#pragma unroll
+                    for (uint32_t k = 0; k < V; k += 4)
+                        *reinterpret_cast<float4 *>(&x[r][k]) = *reinterpret_cast<const float4 *>(s_x + r * slice + i + k);
+#pragma unroll
+                for (uint32_t u = 0; u < UJ; ++u) {
+                    float f[V];
+                    Vec<T>::widen_all(w[q][u], f);
+#pragma unroll
+                    for (uint32_t k = 0; k < V; ++k)
+#pragma unroll
+                        for (uint32_t r = 0; r < G; ++r) acc[u][r] = fmaf(f[k], x[r][k], acc[u][r]);
+                }
+            }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < UJ; ++u)
+#pragma unroll
+            for (uint32_t r = 0; r < G; ++r) {
+                float s = acc[u][r];
+                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                if (lane == 0 && j0 + u * kWarps < rank) s_part[r * FIONA_ADAPTER_MAX_RANK + j0 + u * kWarps] = s;
+            }
+    }
+}
+
+// VEC: rows of A and B are whole vectors of 16 bytes
+template <typename T, bool VEC, uint32_t G>
+__device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &rows, float *s_x, float *s_part, float *s_h)
+{
+    constexpr uint32_t V = VEC ? Vec<T>::n : 1, kUnroll = under_way(G);
     cg::cluster_group cluster = cg::this_cluster();
     const AdapterArgs &a = g.a;
     const uint32_t cta = cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -60,11 +115,14 @@ __device__ void rows_body(const RowsArgs &g, const AdapterRows &rows, float *s_x
     const T *A = (const T *)a.A + (size_t)rows.adapter * a.r_max * a.d_in + i0;
     const T *B = (const T *)a.B + ((size_t)rows.adapter * a.d_out + o0) * a.r_max;
 
-    {  // this CTA's B towards L2
-        const char *p = reinterpret_cast<const char *>(B);
-        const size_t bytes = (size_t)n_out * a.r_max * sizeof(T);
-        for (size_t k = (size_t)tid * 128; k < bytes; k += kThreads * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + k));
-    }
+    // this CTA's A and B towards L2 (not B where less than half of a row is wanted:
+    // lines come whole)
+    const uint32_t lines = (n_in * (uint32_t)sizeof(T) + 127) / 128;
+    for (uint32_t k = tid; k < rank * lines; k += kThreads)
+        prefetch_l2(reinterpret_cast<const char *>(A + (size_t)(k / lines) * a.d_in) + k % lines * 128);
+    if (2 * rank > a.r_max)
+        for (size_t k = (size_t)tid * 128; k < (size_t)n_out * a.r_max * sizeof(T); k += kThreads * 128)
+            prefetch_l2(reinterpret_cast<const char *>(B) + k);
 #pragma unroll
     for (uint32_t r = 0; r < G; ++r) {
         const uint64_t t = rows.row[r];
@@ -76,58 +134,37 @@ __device__ void rows_body(const RowsArgs &g, const AdapterRows &rows, float *s_x
     }
     __syncthreads();
 
-    for (uint32_t j0 = warp; j0 < rank; j0 += kWarps * kUnroll) {
-        float acc[kUnroll][G] = {};
-        if (VA) {
-            for (uint32_t i = lane * V; i < n_in; i += 32 * V) {
-                float w[kUnroll][V];
+    if (VEC) {
+        if (rank <= 2 * kWarps)
+            partial_h<T, G, 2>(A, a.d_in, n_in, rank, g.slice_in, s_x, s_part, warp, lane);
+        else
+            partial_h<T, G, kUnroll>(A, a.d_in, n_in, rank, g.slice_in, s_x, s_part, warp, lane);
+    } else {
+        for (uint32_t j = warp; j < rank; j += kWarps) {
+            float acc[G] = {};
+#pragma unroll 8
+            for (uint32_t i = lane; i < n_in; i += 32) {
+                const float w = widen(A[(size_t)j * a.d_in + i]);
 #pragma unroll
-                for (uint32_t u = 0; u < kUnroll; ++u) {
-                    const uint32_t j = j0 + u * kWarps;
-                    if (j < rank) {
-                        Vec<T>::load(A + (size_t)j * a.d_in + i, w[u]);
-                    } else {
-#pragma unroll
-                        for (uint32_t k = 0; k < V; ++k) w[u][k] = 0.f;
-                    }
-                }
-#pragma unroll
-                for (uint32_t r = 0; r < G; ++r)
-#pragma unroll
-                    for (uint32_t k = 0; k < V; k += 4) {
-                        const float4 x = *reinterpret_cast<const float4 *>(s_x + r * g.slice_in + i + k);
-#pragma unroll
-                        for (uint32_t u = 0; u < kUnroll; ++u)
-                            acc[u][r] = fmaf(w[u][k + 3], x.w, fmaf(w[u][k + 2], x.z, fmaf(w[u][k + 1], x.y, fmaf(w[u][k], x.x, acc[u][r]))));
-                    }
+                for (uint32_t r = 0; r < G; ++r) acc[r] = fmaf(w, s_x[r * g.slice_in + i], acc[r]);
             }
-        } else {
-#pragma unroll 2
-            for (uint32_t i = lane; i < n_in; i += 32)
-#pragma unroll
-                for (uint32_t u = 0; u < kUnroll; ++u) {
-                    const uint32_t j = j0 + u * kWarps;
-                    const float w = j < rank ? widen(A[(size_t)j * a.d_in + i]) : 0.f;
-#pragma unroll
-                    for (uint32_t r = 0; r < G; ++r) acc[u][r] = fmaf(w, s_x[r * g.slice_in + i], acc[u][r]);
-                }
-        }
-#pragma unroll
-        for (uint32_t u = 0; u < kUnroll; ++u)
 #pragma unroll
             for (uint32_t r = 0; r < G; ++r) {
-                float s = acc[u][r];
-                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (lane == 0 && j0 + u * kWarps < rank) s_part[r * FIONA_ADAPTER_MAX_RANK + j0 + u * kWarps] = s;
+                for (int o = 16; o; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
+                if (lane == 0) s_part[r * FIONA_ADAPTER_MAX_RANK + j] = acc[r];
             }
+        }
     }
     cluster.sync();
     for (uint32_t k = tid; k < G * a.r_max; k += kThreads) {
         const uint32_t r = k / a.r_max, j = k % a.r_max;
         float s = 0.f;
         if (j < rank) {
+            float v[kCluster];
 #pragma unroll
-            for (uint32_t c = 0; c < kCluster; ++c) s += cluster.map_shared_rank(s_part, c)[r * FIONA_ADAPTER_MAX_RANK + j];
+            for (uint32_t c = 0; c < kCluster; ++c) v[c] = cluster.map_shared_rank(s_part, c)[r * FIONA_ADAPTER_MAX_RANK + j];
+#pragma unroll
+            for (uint32_t c = 0; c < kCluster; ++c) s += v[c];
             s *= a.mask.factor;
         }
         s_h[r * FIONA_ADAPTER_MAX_RANK + j] = s;
@@ -136,71 +173,102 @@ __device__ void rows_body(const RowsArgs &g, const AdapterRows &rows, float *s_x
     cluster.barrier_arrive();  // (the others' last read of this CTA's shared memory: awaited at the end)
     __syncthreads();
 
-    // 2^shift lanes a column, each every 2^shift-th vector (or element) of its ranks
+    // 2^shift lanes a column, a vector of ranks each; kUnroll columns at a time, the
+    // lanes' results to as many lanes
     const float scale = a.scales[rows.adapter];
-    const uint32_t pieces = VB ? (rank + V - 1) / V : rank;
     uint32_t shift = 0;
-    while (shift < 4 && (1u << shift) < pieces) ++shift;
-    const uint32_t lanes = 1u << shift, sub = lane & (lanes - 1), step = kThreads >> shift;
-    for (uint32_t c0 = 0; c0 < n_out; c0 += step) {
-        const uint32_t c = c0 + (tid >> shift);
-        float acc[G] = {};
-        if (c < n_out) {
-            const T *b = B + (size_t)c * a.r_max;
-            if (VB) {
-                for (uint32_t j = sub * V; j < rank; j += lanes * V) {
-                    float w[V];
-                    Vec<T>::load(b + j, w);
+    while (shift < 5 && (V << shift) < rank) ++shift;
+    const uint32_t lanes = 1u << shift, sub = lane & (lanes - 1), step = (kThreads >> shift) * kUnroll;
+    for (uint32_t c0 = (tid >> shift) * kUnroll; c0 - (tid >> shift) * kUnroll < n_out; c0 += step) {
+        float acc[kUnroll][G] = {}, base[kUnroll][G] = {};
+        if (a.base)
 #pragma unroll
-                    for (uint32_t k = 0; k < V; ++k)
-                        if (j + k < rank)
+            for (uint32_t u = 0; u < kUnroll; ++u)
+                if (u % lanes == sub && c0 + u < n_out)
 #pragma unroll
-                            for (uint32_t r = 0; r < G; ++r) acc[r] = fmaf(w[k], s_h[r * FIONA_ADAPTER_MAX_RANK + j + k], acc[r]);
+                    for (uint32_t r = 0; r < G; ++r)
+                        base[u][r] = widen(((const T *)a.base)[(uint64_t)rows.row[r] * a.ld_base + o0 + c0 + u]);
+        for (uint32_t j = sub * V; j < rank; j += lanes * V) {
+            uint4 w[kUnroll];
+            T e[kUnroll];
+#pragma unroll
+            for (uint32_t u = 0; u < kUnroll; ++u) {
+                const T *b = B + (size_t)(c0 + u) * a.r_max + j;
+                w[u] = make_uint4(0, 0, 0, 0);
+                e[u] = narrow<T>(0.f);
+                if (c0 + u < n_out) {
+                    if (VEC)
+                        w[u] = __ldg(reinterpret_cast<const uint4 *>(b));
+                    else
+                        e[u] = *b;
                 }
-            } else {
-                for (uint32_t j = sub; j < rank; j += lanes)
+            }
+            float h[G][V];
 #pragma unroll
-                    for (uint32_t r = 0; r < G; ++r) acc[r] = fmaf(widen(b[j]), s_h[r * FIONA_ADAPTER_MAX_RANK + j], acc[r]);
+            for (uint32_t r = 0; r < G; ++r)
+#pragma unroll
+                for (uint32_t k = 0; k < V; ++k) h[r][k] = s_h[r * FIONA_ADAPTER_MAX_RANK + j + k];
+#pragma unroll
+            for (uint32_t u = 0; u < kUnroll; ++u) {
+                float f[Vec<T>::n];
+                if (VEC)
+                    Vec<T>::widen_all(w[u], f);
+                else
+                    f[0] = widen(e[u]);
+#pragma unroll
+                for (uint32_t k = 0; k < V; ++k)
+                    if (j + k < rank)
+#pragma unroll
+                        for (uint32_t r = 0; r < G; ++r) acc[u][r] = fmaf(f[k], h[r][k], acc[u][r]);
             }
         }
         for (uint32_t o = lanes / 2; o; o >>= 1)
 #pragma unroll
-            for (uint32_t r = 0; r < G; ++r) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
-        if (c < n_out && sub == 0)
+            for (uint32_t u = 0; u < kUnroll; ++u)
 #pragma unroll
-            for (uint32_t r = 0; r < G; ++r) {
-                const uint64_t t = rows.row[r], col = o0 + c;
-                const float base = a.base ? widen(((const T *)a.base)[t * a.ld_base + col]) : 0.f;
-                ((T *)a.out)[t * a.ld_out + col] = narrow<T>(fmaf(scale, acc[r], base));
-            }
+                for (uint32_t r = 0; r < G; ++r) acc[u][r] += __shfl_xor_sync(0xffffffffu, acc[u][r], o);
+#pragma unroll
+        for (uint32_t u = 0; u < kUnroll; ++u)
+            if (u % lanes == sub && c0 + u < n_out)
+#pragma unroll
+                for (uint32_t r = 0; r < G; ++r)
+                    ((T *)a.out)[(uint64_t)rows.row[r] * a.ld_out + o0 + c0 + u] = narrow<T>(fmaf(scale, acc[u][r], base[u][r]));
     }
     cluster.barrier_wait();
 }
 
-template <typename T, bool VA, bool VB>
-__global__ void __launch_bounds__(kThreads) k_rows(const RowsArgs g)
+// MOST: the largest group of the batch
+template <typename T, bool VEC, uint32_t MOST>
+__global__ void __launch_bounds__(kThreads, MOST <= 2 ? 3 : 2) k_rows(const RowsArgs g)
 {
     extern __shared__ __align__(16) float s_x[];  // [rows][slice_in]
     __shared__ float s_part[kAdapterRows * FIONA_ADAPTER_MAX_RANK], s_h[kAdapterRows * FIONA_ADAPTER_MAX_RANK];
     const AdapterRows rows = g.groups[blockIdx.x / kCluster];
-    switch (rows.count) {
-        case 1: rows_body<T, VA, VB, 1>(g, rows, s_x, s_part, s_h); break;
-        case 2: rows_body<T, VA, VB, 2>(g, rows, s_x, s_part, s_h); break;
-        case 3: rows_body<T, VA, VB, 3>(g, rows, s_x, s_part, s_h); break;
-        default: rows_body<T, VA, VB, 4>(g, rows, s_x, s_part, s_h); break;
-    }
+    if (rows.count == 1)
+        rows_body<T, VEC, 1>(g, rows, s_x, s_part, s_h);
+    else if (MOST > 1 && rows.count == 2)
+        rows_body<T, VEC, (MOST > 1 ? 2 : 1)>(g, rows, s_x, s_part, s_h);
+    else if (MOST > 2 && rows.count == 3)
+        rows_body<T, VEC, (MOST > 2 ? 3 : 1)>(g, rows, s_x, s_part, s_h);
+    else if (MOST > 2)
+        rows_body<T, VEC, (MOST > 2 ? 4 : 1)>(g, rows, s_x, s_part, s_h);
 }
 
 // columns of `d` a CTA of the cluster takes
 uint32_t slice(uint32_t d) { return ((d + kCluster - 1) / kCluster + 7) & ~7u; }
 
+template <typename T, bool VEC>
+auto pick(uint32_t most)
+{
+    return most <= 1 ? k_rows<T, VEC, 1> : most == 2 ? k_rows<T, VEC, 2> : k_rows<T, VEC, 4>;
+}
+
 template <typename T>
 int run(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a)
 {
     const RowsArgs g{a, b->d_rows, slice(a.d_in), slice(a.d_out)};
-    const bool va = a.d_in % Vec<T>::n == 0, vb = a.r_max % Vec<T>::n == 0;
-    void (*kernel)(RowsArgs) = va ? (vb ? k_rows<T, true, true> : k_rows<T, true, false>)
-                                  : (vb ? k_rows<T, false, true> : k_rows<T, false, false>);
+    void (*kernel)(RowsArgs) = a.d_in % Vec<T>::n == 0 && a.r_max % Vec<T>::n == 0 ? pick<T, true>(b->most_rows)
+                                                                                   : pick<T, false>(b->most_rows);
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(b->n_rows * kCluster);
     c.blockDim = dim3(kThreads);

@@ -1171,8 +1171,6 @@ struct ForwardShape {
 template <typename K>
 int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t s, bool after, void **args, const char *what)
 {
-    if (smem > 48 * 1024)
-        if (const int rc = allow_shared_memory((const void *)kernel, smem, what)) return rc;
     cudaLaunchConfig_t c{};
     c.gridDim = grid;
     c.blockDim = dim3(threads);
@@ -1407,6 +1405,18 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
 bool adapter_tiles_apply(const fiona_adapter_batch *b, uint32_t d_in, uint32_t, uint32_t dtype)
 {
     return dtype != FIONA_F32 && d_in % 8 == 0 && b->r_max % 8 == 0;
+}
+
+int adapter_tiles_configure()
+{
+    const void *kernels[] = {(const void *)k_shrink<__half, false>, (const void *)k_shrink<__half, true>,
+                             (const void *)k_expand<__half>, (const void *)k_shrink_grad<__half>,
+                             (const void *)k_expand_grad<__half>, (const void *)k_shrink<__nv_bfloat16, false>,
+                             (const void *)k_shrink<__nv_bfloat16, true>, (const void *)k_expand<__nv_bfloat16>,
+                             (const void *)k_shrink_grad<__nv_bfloat16>, (const void *)k_expand_grad<__nv_bfloat16>};
+    for (const void *k : kernels)
+        if (const int rc = allow_shared_memory(k, kSmemOne + 1024, "adapter kernel attribute")) return rc;
+    return FIONA_OK;
 }
 
 uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
