@@ -34,12 +34,8 @@ struct AdapterChunks {
 struct fiona_adapter_batch {
     const fiona_ctx *ctx = nullptr;
     uint32_t n_tokens = 0, n_adapters = 0, r_max = 0;
-    std::vector<uint32_t> ranks;
     // device arrays, in `blob`
     void *blob = nullptr;
-    const uint32_t *d_owner = nullptr;        // [n_tokens] adapter or kNoAdapter
-    const uint32_t *d_order = nullptr;        // rows with an adapter, by adapter, rising within one
-    const uint32_t *d_order_begin = nullptr;  // [n_adapters + 1] into d_order
     const uint32_t *d_ranks = nullptr;        // [n_adapters]
     const float *d_scales = nullptr;          // [n_adapters]
     const AdapterTile *d_tiles = nullptr;     // rows of adapters with a rank, by adapter
@@ -58,7 +54,7 @@ struct fiona_adapter_batch {
 // One call, as the kernels see it.  Rows are elements apart by their ld.
 struct AdapterArgs {
     uint32_t n_tokens, n_adapters, r_max, d_in, d_out;
-    const uint32_t *owner, *order, *order_begin, *ranks;
+    const uint32_t *ranks;
     const float *scales;
     const void *A, *B;
     const void *x, *base, *dy;  // base: of out, or of dx
@@ -66,13 +62,15 @@ struct AdapterArgs {
     uint64_t ldx, ld_base, ld_dy, ld_out;
     const float *h_in;
     float *h;   // forward: null where it is not wanted
-    float *dh;  // [n_tokens][r_max] in the workspace; forward: h where the caller wants none
     dropout::Mask mask;
 };
 
-// adapter_simple.cu
-int launch_adapter_simple_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a);
-int launch_adapter_simple_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a);
+// adapter_any.cu: any type and alignment, on the FMA units; its workspace; the
+// passes (only_long: without the short runs)
+uint64_t adapter_any_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
+int launch_adapter_any_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,
+                               bool only_long);
+int launch_adapter_any_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
 
 // adapter_rows.cu: the forward pass on the short runs of rows, any type and alignment
 bool adapter_rows_apply(const fiona_adapter_batch *b, uint32_t d_in);

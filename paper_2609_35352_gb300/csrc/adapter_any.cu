@@ -1,0 +1,496 @@
+// adapter_any.cu -- the adapters' products on the FMA units: fp32, whose sums the
+// tensor cores would not keep, and 16-bit rows that TMA cannot address (a width,
+// stride or start that is no multiple of 16 bytes).
+//
+// The four passes of adapter_tiles.cu on half tiles of 64 rows, in fp32 throughout:
+// shrink (h or dh over a range of columns), expand (out or dx, 64 columns) and the
+// weight gradients (64 columns over a chunk of an adapter's tiles).  A block keeps
+// its tile's sums in registers, 4 x 4 (4 x 8 above rank 64) a thread, and reads
+// both factors from shared memory as they were widened: 16 multiplications for two
+// 16-byte reads.  Where few ranks leave threads over, they split the sum's axis
+// and are added up at the end.  Loads are element by element along the rows, the
+// next slice's under the multiplications.
+//
+// Bound by the FMA units above rank 16 or so; below, by launches and HBM.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "adapter_parts.cuh"
+
+namespace {
+
+using namespace parts;
+
+constexpr uint32_t kThreads = 256, kWarps = kThreads / 32;
+constexpr uint32_t kRows = 64;   // of a half tile
+constexpr uint32_t kCols = 64;   // of an output tile, and of a weight gradient's
+constexpr uint32_t kSlice = 32;  // of the sum's axis
+constexpr uint32_t kPad = 4;
+
+// A block's 64 x (NRG * RPT) sums: thread (16 groups of 4, NRG groups of RPT ranks,
+// KS shares of each slice).
+template <uint32_t NRG, uint32_t RPT>
+struct Sums {
+    static constexpr uint32_t kRanks = NRG * RPT, kShares = kThreads / (16 * NRG), kSteps = kSlice / kShares;
+    float acc[4][RPT];
+    uint32_t x4, r0, share;
+    __device__ Sums() : x4(threadIdx.x % 16 * 4), r0(threadIdx.x / 16 % NRG * RPT), share(threadIdx.x / (16 * NRG))
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < RPT; ++j) acc[i][j] = 0.f;
+    }
+    __device__ __forceinline__ void slice(const float (&X)[kSlice][64 + kPad], const float (&S)[kSlice][kRanks + kPad])
+    {
+#pragma unroll 4
+        for (uint32_t k = share * kSteps; k < (share + 1) * kSteps; ++k) {
+            const float4 x = *reinterpret_cast<const float4 *>(&X[k][x4]);
+            float s[RPT];
+#pragma unroll
+            for (uint32_t j = 0; j < RPT; j += 4) *reinterpret_cast<float4 *>(&s[j]) = *reinterpret_cast<const float4 *>(&S[k][r0 + j]);
+#pragma unroll
+            for (uint32_t j = 0; j < RPT; ++j) {
+                acc[0][j] = fmaf(x.x, s[j], acc[0][j]);
+                acc[1][j] = fmaf(x.y, s[j], acc[1][j]);
+                acc[2][j] = fmaf(x.z, s[j], acc[2][j]);
+                acc[3][j] = fmaf(x.w, s[j], acc[3][j]);
+            }
+        }
+    }
+    // the shares added up in order, in `sum` (64 x kRanks, at least kShares of it, shared)
+    __device__ __forceinline__ void join(float *sum)
+    {
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < RPT; ++j) sum[(share * 64 + x4 + i) * (kRanks + 1) + r0 + j] = acc[i][j];
+        __syncthreads();
+        if (kShares > 1) {
+            for (uint32_t e = threadIdx.x; e < 64 * kRanks; e += kThreads) {
+                float *p = sum + e / kRanks * (kRanks + 1) + e % kRanks, v = 0.f;
+#pragma unroll
+                for (uint32_t s = 0; s < kShares; ++s) v += p[s * 64 * (kRanks + 1)];
+                *p = v;
+            }
+            __syncthreads();
+        }
+    }
+};
+
+// shared memory: two slices' factors, or the shares' sums
+template <uint32_t NRG, uint32_t RPT>
+union Shared {
+    static constexpr uint32_t kRanks = NRG * RPT, kShares = kThreads / (16 * NRG);
+    struct {
+        float X[kSlice][64 + kPad];
+        float S[kSlice][kRanks + kPad];
+    } f;
+    float sum[kShares * 64 * (kRanks + 1)];
+};
+
+template <typename T>
+__device__ __forceinline__ float element(const T *p, bool valid) { return valid ? widen(*p) : 0.f; }
+
+// partial h = D(x) A^T, or dh = dy B (BACK), of half a tile over g.cut.width columns
+template <typename T, bool BACK, uint32_t NRG, uint32_t RPT>
+__global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
+{
+    using Sh = Shared<NRG, RPT>;
+    __shared__ __align__(16) Sh sm;
+    constexpr uint32_t kRanks = Sh::kRanks;
+    next_may_start();
+    const AdapterTile t = g.tiles[blockIdx.x / (2 * g.cut.slabs)];
+    const uint32_t half = blockIdx.x / g.cut.slabs % 2, slab = blockIdx.x % g.cut.slabs;
+    if (half * kRows >= t.rows) return;
+    const uint32_t rows = min(kRows, t.rows - half * kRows), row0 = t.row0 + half * kRows;
+    const uint32_t k0 = slab * g.cut.width, k1 = min(g.cols, k0 + g.cut.width);
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = g.a.ranks[t.adapter];
+    const T *x = BACK ? (const T *)g.a.dy : (const T *)g.a.x;
+    const uint64_t ld = BACK ? g.a.ld_dy : g.a.ldx;
+    const T *W = BACK ? (const T *)g.a.B + (size_t)t.adapter * g.a.d_out * g.a.r_max : (const T *)g.a.A + (size_t)t.adapter * g.a.r_max * g.a.d_in;
+    constexpr uint32_t kX = kRows / kWarps, kW = BACK ? kSlice / kWarps * ((kRanks + 31) / 32) : (kRanks + kWarps - 1) / kWarps;
+    float fx[kX], fw[kW];
+    auto fetch = [&](uint32_t k) {
+        const uint32_t col = k + lane;
+#pragma unroll
+        for (uint32_t q = 0; q < kX; ++q) {
+            const uint32_t r = warp + q * kWarps;
+            fx[q] = element(x + (uint64_t)(row0 + r) * ld + col, r < rows && col < k1);
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kW; ++q) {
+            if (!BACK) {
+                const uint32_t j = warp + q * kWarps;
+                fw[q] = element(W + (size_t)j * g.a.d_in + col, j < rank && col < k1);
+            } else {
+                const uint32_t i = k + warp + q % (kSlice / kWarps) * kWarps, j = lane + q / (kSlice / kWarps) * 32;
+                fw[q] = element(W + (size_t)i * g.a.r_max + j, j < rank && i < k1);
+            }
+        }
+    };
+    Sums<NRG, RPT> s;
+    fetch(k0);
+    for (uint32_t k = k0; k < k1; k += kSlice) {
+        __syncthreads();
+#pragma unroll
+        for (uint32_t q = 0; q < kX; ++q) {
+            const uint32_t r = warp + q * kWarps;
+            const bool drop = !BACK && g.a.mask.level && k + lane < k1 && !g.a.mask.keep(row0 + r, k + lane);
+            sm.f.X[lane][r] = drop ? 0.f : fx[q];
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kW; ++q) {
+            if (!BACK) {
+                if (warp + q * kWarps < kRanks) sm.f.S[lane][warp + q * kWarps] = fw[q];
+            } else {
+                const uint32_t j = lane + q / (kSlice / kWarps) * 32;
+                if (j < kRanks) sm.f.S[warp + q % (kSlice / kWarps) * kWarps][j] = fw[q];
+            }
+        }
+        __syncthreads();
+        if (k + kSlice < k1) fetch(k + kSlice);
+        s.slice(sm.f.X, sm.f.S);
+    }
+    s.join(sm.sum);
+    for (uint32_t e = threadIdx.x; e < rows * g.r16; e += kThreads) {
+        const uint32_t r = e / g.r16, j = e % g.r16;
+        if (j < rank) g.part_out[((size_t)slab * g.a.n_tokens + row0 + r) * g.r16 + j] = sm.sum[r * (kRanks + 1) + j];
+    }
+}
+
+// out = base + s h B^T, or dx = dx_base + D'(dh A) (BACK), of half a tile and 64
+// columns: a thread 4 rows and the columns 16 apart
+template <typename T, bool BACK>
+__global__ void __launch_bounds__(kThreads) k_any_expand(const TileArgs g)
+{
+    __shared__ __align__(16) float H[kSlice][kRows + kPad], S[kSlice][kCols + 1];
+    next_may_start();
+    if (blockIdx.x < g.n_bare) {
+        previous_done();
+        bare_rows<T>(g.a, g.bare[blockIdx.x], g.cols, kThreads);
+        return;
+    }
+    const uint32_t unit = blockIdx.x - g.n_bare, col0 = unit % g.cut.slabs * kCols, half = unit / g.cut.slabs % 2;
+    const AdapterTile t = g.tiles[unit / (2 * g.cut.slabs)];
+    if (half * kRows >= t.rows) {
+        previous_done();
+        return;
+    }
+    const uint32_t rows = min(kRows, t.rows - half * kRows), row0 = t.row0 + half * kRows;
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = g.a.ranks[t.adapter];
+    const uint32_t c = threadIdx.x % 16, r4 = threadIdx.x / 16 * 4;
+    const T *W = BACK ? (const T *)g.a.A + (size_t)t.adapter * g.a.r_max * g.a.d_in : (const T *)g.a.B + (size_t)t.adapter * g.a.d_out * g.a.r_max;
+    float base[4][4];
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
+            const uint32_t col = col0 + c + 16 * q;
+            base[i][q] = g.a.base ? element((const T *)g.a.base + (uint64_t)(row0 + r4 + i) * g.a.ld_base + col, r4 + i < rows && col < g.cols) : 0.f;
+        }
+    float acc[4][4] = {};
+    previous_done();
+    const float by = BACK ? g.a.scales[t.adapter] : g.a.mask.factor;
+    for (uint32_t j0 = 0; j0 < g.a.r_max; j0 += kSlice) {
+        if (j0 >= rank && !(g.a.h && col0 == 0)) break;
+        __syncthreads();
+        for (uint32_t e = threadIdx.x; e < kRows * (kSlice / 4); e += kThreads) {
+            const uint32_t r = e / (kSlice / 4), j = j0 + e % (kSlice / 4) * 4;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r < rows && j < rank) v = below(sum_parts(g, row0 + r, j), j, rank, by);
+            const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                H[j - j0 + i][r] = f[i];
+                if (!BACK && g.a.h && col0 == 0 && r < rows && j + i < g.a.r_max) g.a.h[(size_t)(row0 + r) * g.a.r_max + j + i] = f[i];
+            }
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kSlice * kCols / kThreads; ++q) {
+            if (BACK) {
+                const uint32_t j = warp + q / 2 * kWarps, i = lane + q % 2 * 32;
+                S[j][i] = element(W + (size_t)(j0 + j) * g.a.d_in + col0 + i, j0 + j < rank && col0 + i < g.cols);
+            } else {
+                const uint32_t i = warp + q * kWarps;
+                S[lane][i] = element(W + (size_t)(col0 + i) * g.a.r_max + j0 + lane, j0 + lane < rank && col0 + i < g.cols);
+            }
+        }
+        __syncthreads();
+        const uint32_t n = min(kSlice, rank > j0 ? rank - j0 : 0);
+#pragma unroll 4
+        for (uint32_t j = 0; j < n; ++j) {
+            const float4 h = *reinterpret_cast<const float4 *>(&H[j][r4]);
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                const float w = S[j][c + 16 * q];
+                acc[0][q] = fmaf(h.x, w, acc[0][q]);
+                acc[1][q] = fmaf(h.y, w, acc[1][q]);
+                acc[2][q] = fmaf(h.z, w, acc[2][q]);
+                acc[3][q] = fmaf(h.w, w, acc[3][q]);
+            }
+        }
+    }
+    const float scale = BACK ? g.a.mask.factor : g.a.scales[t.adapter];
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
+            const uint32_t row = row0 + r4 + i, col = col0 + c + 16 * q;
+            if (r4 + i >= rows || col >= g.cols) continue;
+            const bool drop = BACK && g.a.mask.level && !g.a.mask.keep(row, col);
+            ((T *)g.a.out)[(uint64_t)row * g.a.ld_out + col] = narrow<T>(drop ? base[i][q] : fmaf(scale, acc[i][q], base[i][q]));
+        }
+}
+
+// dB += dy^T h, or dA += D(x)^T dh (INNER), of 64 columns over a chunk of tiles.
+// The blocks of dA come first.
+template <typename T, bool INNER, uint32_t NRG, uint32_t RPT>
+__device__ __forceinline__ void weight_grad(const TileArgs &g, uint32_t block, Shared<NRG, RPT> &sm)
+{
+    constexpr uint32_t kRanks = NRG * RPT;
+    const uint32_t cols = INNER ? g.a.d_in : g.a.d_out, slabs = (cols + kCols - 1) / kCols;
+    const uint32_t chunk = block / slabs, col0 = block % slabs * kCols;
+    const AdapterChunk ch = g.chunks[chunk];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = g.a.ranks[ch.adapter];
+    const T *x = INNER ? (const T *)g.a.x : (const T *)g.a.dy;
+    const uint64_t ld = INNER ? g.a.ldx : g.a.ld_dy;
+    const float s_a = g.a.scales[ch.adapter];
+    constexpr uint32_t kX = kSlice * kCols / kThreads, kS = kSlice / kWarps * ((kRanks + 31) / 32);
+    float fx[kX], fs[kS];
+    auto fetch = [&](const AdapterTile &t, uint32_t r0) {
+#pragma unroll
+        for (uint32_t q = 0; q < kX; ++q) {
+            const uint32_t r = r0 + warp + q / 2 * kWarps, col = col0 + lane + q % 2 * 32;
+            fx[q] = element(x + (uint64_t)(t.row0 + r) * ld + col, r < t.rows && col < cols);
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kS; ++q) {
+            const uint32_t r = r0 + warp + q % (kSlice / kWarps) * kWarps, j = lane + q / (kSlice / kWarps) * 32;
+            float v = 0.f;
+            if (r < t.rows && j < rank) {
+                if (INNER) {
+                    const float *p = g.part_in + (size_t)(t.row0 + r) * g.r16 + j;
+                    for (uint32_t k = 0; k < g.slabs_in; ++k) v += p[k * (size_t)g.a.n_tokens * g.r16];
+                    v *= s_a;
+                } else {
+                    v = g.a.h_in[(size_t)(t.row0 + r) * g.a.r_max + j];
+                }
+            }
+            fs[q] = v;
+        }
+    };
+    Sums<NRG, RPT> s;
+    uint32_t tile = ch.begin, r0 = 0;
+    AdapterTile t = g.tiles[tile];
+    fetch(t, 0);
+    while (tile < ch.end) {
+        __syncthreads();
+#pragma unroll
+        for (uint32_t q = 0; q < kX; ++q) {
+            const uint32_t r = warp + q / 2 * kWarps, c = lane + q % 2 * 32;
+            const bool drop = INNER && g.a.mask.level && r0 + r < t.rows && col0 + c < cols && !g.a.mask.keep(t.row0 + r0 + r, col0 + c);
+            sm.f.X[r][c] = drop ? 0.f : fx[q];
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kS; ++q) {
+            const uint32_t j = lane + q / (kSlice / kWarps) * 32;
+            if (j < kRanks) sm.f.S[warp + q % (kSlice / kWarps) * kWarps][j] = fs[q];
+        }
+        __syncthreads();
+        r0 += kSlice;
+        if (r0 >= t.rows) {
+            r0 = 0;
+            if (++tile < ch.end) t = g.tiles[tile];
+        }
+        if (tile < ch.end) fetch(t, r0);
+        s.slice(sm.f.X, sm.f.S);
+    }
+    s.join(sm.sum);
+    const float scale = INNER ? g.a.mask.factor : s_a;
+    for (uint32_t e = threadIdx.x; e < 64 * rank; e += kThreads) {
+        const uint32_t c = INNER ? e % 64 : e / rank, j = INNER ? e / 64 : e % rank;
+        if (col0 + c >= cols) continue;
+        const float v = sm.sum[c * (kRanks + 1) + j] * scale;
+        if (INNER)
+            g.grad[((size_t)chunk * g.r16 + j) * cols + col0 + c] = v;
+        else
+            g.grad_b[((size_t)chunk * cols + col0 + c) * g.r16 + j] = v;
+    }
+}
+
+template <typename T, uint32_t NRG, uint32_t RPT>
+__global__ void __launch_bounds__(kThreads) k_any_grad(const TileArgs g, uint32_t blocks_A)
+{
+    __shared__ __align__(16) Shared<NRG, RPT> sm;
+    next_may_start();
+    previous_done();
+    if (blockIdx.x < blocks_A)
+        weight_grad<T, true, NRG, RPT>(g, blockIdx.x, sm);
+    else
+        weight_grad<T, false, NRG, RPT>(g, blockIdx.x - blocks_A, sm);
+}
+
+// dA and dB of an adapter: its chunks' sums in order
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_any_grad_sum(const GradSum A, const GradSum B, const uint32_t *ranks, uint32_t blocks_A,
+                                                           uint32_t first)
+{
+    const GradSum &g = blockIdx.x < blocks_A ? A : B;
+    const uint32_t ad = first + blockIdx.y, rank = ranks[ad];
+    const uint64_t k = (uint64_t)(blockIdx.x < blocks_A ? blockIdx.x : blockIdx.x - blocks_A) * kThreads + threadIdx.x;
+    previous_done();
+    if (k >= (uint64_t)g.rows * g.inner) return;
+    const uint32_t row = (uint32_t)(k / g.inner), col = (uint32_t)(k % g.inner);
+    float v = 0.f;
+    if ((g.rank_rows ? row : col) < rank) {
+        const size_t step = (size_t)g.part_rows * g.part_inner;
+        const float *p = g.part + ((size_t)g.begin[ad] * g.part_rows + row) * g.part_inner + col;
+        const uint32_t n = g.begin[ad + 1] - g.begin[ad];
+#pragma unroll 8
+        for (uint32_t c = 0; c < n; ++c) v += p[c * step];
+    }
+    ((T *)g.out)[(size_t)ad * g.rows * g.inner + k] = narrow<T>(v);
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+template <typename T, bool BACK>
+auto pick_shrink(uint32_t r)
+{
+    return r <= 8 ? k_any_shrink<T, BACK, 2, 4> : r <= 16 ? k_any_shrink<T, BACK, 4, 4> : r <= 32 ? k_any_shrink<T, BACK, 8, 4>
+         : r <= 64 ? k_any_shrink<T, BACK, 16, 4> : k_any_shrink<T, BACK, 16, 8>;
+}
+template <typename T>
+auto pick_grad(uint32_t r)
+{
+    return r <= 8 ? k_any_grad<T, 2, 4> : r <= 16 ? k_any_grad<T, 4, 4> : r <= 32 ? k_any_grad<T, 8, 4>
+         : r <= 64 ? k_any_grad<T, 16, 4> : k_any_grad<T, 16, 8>;
+}
+
+// Column ranges of a shrink: enough blocks for four an SM, and no fewer than eight
+// slices each.
+Cut shrink_cut(const fiona_adapter_batch *b, uint32_t cols, uint32_t n_tiles)
+{
+    const uint32_t want = 4 * (uint32_t)std::max(b->ctx->sm_count, 1), slices = ceil_div(cols, kSlice);
+    uint32_t slabs = std::min(want / std::max(2 * n_tiles, 1u), ceil_div(slices, 8));
+    slabs = std::max(1u, std::min(slabs, 16u));
+    const uint32_t width = ceil_div(slices, slabs) * kSlice;
+    return Cut{width, ceil_div(cols, width)};
+}
+
+// the largest chunks that still make four blocks an SM
+const AdapterChunks &grad_chunks(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
+{
+    const uint32_t want = 4 * (uint32_t)std::max(b->ctx->sm_count, 1), slabs = ceil_div(d_in, kCols) + ceil_div(d_out, kCols);
+    size_t i = b->chunks.size() - 1;
+    while (i > 0 && (uint64_t)b->chunks[i].count * slabs < want) --i;
+    return b->chunks[i];
+}
+
+struct AnyShape {
+    uint32_t r16;
+    uint64_t part = 0, grad_A = 0, grad_B = 0, bytes = 0;
+    AnyShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) : r16((b->r_max + 15) & ~15u)
+    {
+        const uint32_t slabs = std::max({shrink_cut(b, d_in, b->n_tiles).slabs, shrink_cut(b, d_out, b->n_tiles).slabs,
+                                         shrink_cut(b, d_in, b->n_long).slabs});
+        const uint32_t chunks = grad_chunks(b, d_in, d_out).count;
+        grad_A = part + align_up((uint64_t)slabs * b->n_tokens * r16 * 4);
+        grad_B = grad_A + align_up((uint64_t)chunks * d_in * r16 * 4);
+        bytes = grad_B + align_up((uint64_t)chunks * d_out * r16 * 4);
+    }
+};
+
+template <typename T>
+int forward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a, void *work, bool only_long)
+{
+    TileArgs g{};
+    g.a = a;
+    g.tiles = only_long ? b->d_long : b->d_tiles;
+    g.n_tiles = only_long ? b->n_long : b->n_tiles;
+    g.r16 = AnyShape(b, a.d_in, a.d_out).r16;
+    g.part_out = static_cast<float *>(work);
+    g.part_in = g.part_out;
+    g.cols = a.d_in;
+    g.cut = shrink_cut(b, a.d_in, g.n_tiles);
+    g.slabs_in = g.cut.slabs;
+    void *args[] = {&g};
+    int rc = FIONA_OK;
+    if (g.n_tiles && (rc = launch(pick_shrink<T, false>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, false, args, "adapter shrink")))
+        return rc;
+    g.cols = a.d_out;
+    g.cut = Cut{kCols, ceil_div(a.d_out, kCols)};
+    g.bare = b->d_bare;
+    g.n_bare = b->n_bare;
+    if (!g.n_tiles && !g.n_bare) return FIONA_OK;
+    return launch(k_any_expand<T, false>, g.n_bare + 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, g.n_tiles != 0, args, "adapter expand");
+}
+
+template <typename T>
+int backward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a, void *work)
+{
+    const AnyShape f(b, a.d_in, a.d_out);
+    const AdapterChunks &chunks = grad_chunks(b, a.d_in, a.d_out);
+    uint8_t *ws = static_cast<uint8_t *>(work);
+    TileArgs g{};
+    g.a = a;
+    g.tiles = b->d_tiles;
+    g.n_tiles = b->n_tiles;
+    g.r16 = f.r16;
+    g.part_out = reinterpret_cast<float *>(ws + f.part);
+    g.part_in = g.part_out;
+    g.cols = a.d_out;
+    g.cut = shrink_cut(b, a.d_out, g.n_tiles);
+    g.slabs_in = g.cut.slabs;
+    void *args[] = {&g};
+    int rc = FIONA_OK;
+    const bool any = b->n_tiles != 0;
+    if (any && (rc = launch(pick_shrink<T, true>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, false, args, "adapter dh"))) return rc;
+    g.cols = a.d_in;
+    g.cut = Cut{kCols, ceil_div(a.d_in, kCols)};
+    g.bare = b->d_bare;
+    g.n_bare = b->n_bare;
+    if ((any || g.n_bare) && (rc = launch(k_any_expand<T, true>, g.n_bare + 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, any, args, "adapter dx")))
+        return rc;
+    g.chunks = chunks.d_chunks;
+    g.grad = reinterpret_cast<float *>(ws + f.grad_A);
+    g.grad_b = reinterpret_cast<float *>(ws + f.grad_B);
+    uint32_t blocks_A = chunks.count * ceil_div(a.d_in, kCols), blocks_B = chunks.count * ceil_div(a.d_out, kCols);
+    void *gargs[] = {&g, &blocks_A};
+    if (any && (rc = launch(pick_grad<T>(a.r_max), blocks_A + blocks_B, kThreads, 0, s, true, gargs, "adapter weight gradients"))) return rc;
+    const GradSum A{g.grad, chunks.d_begin, a.dA, a.r_max, a.d_in, f.r16, a.d_in, 1};
+    const GradSum B{g.grad_b, chunks.d_begin, a.dB, a.d_out, a.r_max, a.d_out, f.r16, 0};
+    const uint32_t sum_A = (uint32_t)(((uint64_t)a.r_max * a.d_in + kThreads - 1) / kThreads);
+    const uint32_t sum_B = (uint32_t)(((uint64_t)a.r_max * a.d_out + kThreads - 1) / kThreads);
+    for (uint32_t i = 0; i < a.n_adapters && rc == FIONA_OK; i += 65535) {
+        void *sargs[] = {(void *)&A, (void *)&B, (void *)&a.ranks, (void *)&sum_A, &i};
+        rc = launch(k_any_grad_sum<T>, dim3(sum_A + sum_B, std::min(a.n_adapters - i, 65535u)), kThreads, 0, s, any || g.n_bare, sargs,
+                    "adapter gradients");
+    }
+    return rc;
+}
+
+}  // namespace
+
+uint64_t adapter_any_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) { return AnyShape(b, d_in, d_out).bytes; }
+
+int launch_adapter_any_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,
+                               bool only_long)
+{
+    cudaStream_t s = (cudaStream_t)stream;
+    return dtype == FIONA_F32   ? forward<float>(b, s, a, work, only_long)
+           : dtype == FIONA_F16 ? forward<__half>(b, s, a, work, only_long)
+                                : forward<__nv_bfloat16>(b, s, a, work, only_long);
+}
+
+int launch_adapter_any_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work)
+{
+    cudaStream_t s = (cudaStream_t)stream;
+    return dtype == FIONA_F32   ? backward<float>(b, s, a, work)
+           : dtype == FIONA_F16 ? backward<__half>(b, s, a, work)
+                                : backward<__nv_bfloat16>(b, s, a, work);
+}

@@ -103,7 +103,7 @@ int check_layer(const fiona_adapter_batch *b, const fiona_adapter_layer *l, cons
 // bytes of a call's workspace, whichever kernels its buffers' alignment sends it to
 uint64_t work_needed(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t dtype)
 {
-    uint64_t n = align_up((uint64_t)b->n_tokens * b->r_max * 4);
+    uint64_t n = adapter_any_work(b, d_in, d_out);
     if (adapter_tiles_apply(b, d_in, d_out, dtype)) n = std::max(n, adapter_tiles_work(b, d_in, d_out));
     return n;
 }
@@ -128,9 +128,6 @@ AdapterArgs common_args(const fiona_adapter_batch *b, const fiona_adapter_layer 
     a.r_max = b->r_max;
     a.d_in = l->d_in;
     a.d_out = l->d_out;
-    a.owner = b->d_owner;
-    a.order = b->d_order;
-    a.order_begin = b->d_order_begin;
     a.ranks = b->d_ranks;
     a.scales = b->d_scales;
     a.A = l->A;
@@ -170,20 +167,11 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
     b->n_tokens = (uint32_t)starts[n_requests];
     b->n_adapters = n_adapters;
     b->r_max = r_max;
-    b->ranks.assign(ranks, ranks + n_adapters);
 
     const uint32_t T = b->n_tokens;
-    std::vector<uint32_t> owner(T), begin(n_adapters + 1, 0), order;
+    std::vector<uint32_t> owner(T);
     for (uint32_t r = 0; r < n_requests; ++r)
-        for (uint64_t t = starts[r]; t < starts[r + 1]; ++t) {
-            owner[t] = adapter[r] < 0 ? kNoAdapter : (uint32_t)adapter[r];
-            if (adapter[r] >= 0) ++begin[adapter[r] + 1];
-        }
-    for (uint32_t a = 0; a < n_adapters; ++a) begin[a + 1] += begin[a];
-    order.resize(begin[n_adapters]);
-    std::vector<uint32_t> next(begin.begin(), begin.end() - 1);
-    for (uint32_t t = 0; t < T; ++t)
-        if (owner[t] != kNoAdapter) order[next[owner[t]]++] = t;
+        std::fill(owner.begin() + starts[r], owner.begin() + starts[r + 1], adapter[r] < 0 ? kNoAdapter : (uint32_t)adapter[r]);
 
     // token tiles, by adapter; runs of rows that no adapter changes
     std::vector<std::vector<AdapterTile>> by(n_adapters);
@@ -258,8 +246,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
             if (bytes) memcpy(image.data() + at, p, bytes);
             return at;
         };
-        const size_t o_owner = put(owner.data(), owner.size() * 4), o_order = put(order.data(), order.size() * 4);
-        const size_t o_begin = put(begin.data(), begin.size() * 4), o_ranks = put(ranks, n_adapters * 4ull);
+        const size_t o_ranks = put(ranks, n_adapters * 4ull);
         const size_t o_scales = put(s.data(), n_adapters * 4ull);
         const size_t o_tiles = put(tiles.data(), tiles.size() * sizeof(AdapterTile));
         const size_t o_tile_begin = put(tile_begin.data(), tile_begin.size() * 4);
@@ -273,9 +260,6 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         if (e == cudaSuccess) e = cudaMemcpy(b->blob, image.data(), image.size(), cudaMemcpyHostToDevice);
         if (e != cudaSuccess) return cuda_fail(e, who);
         const uint8_t *d = static_cast<const uint8_t *>(b->blob);
-        b->d_owner = reinterpret_cast<const uint32_t *>(d + o_owner);
-        b->d_order = reinterpret_cast<const uint32_t *>(d + o_order);
-        b->d_order_begin = reinterpret_cast<const uint32_t *>(d + o_begin);
         b->d_ranks = reinterpret_cast<const uint32_t *>(d + o_ranks);
         b->d_scales = reinterpret_cast<const float *>(d + o_scales);
         b->d_tiles = reinterpret_cast<const AdapterTile *>(d + o_tiles);
@@ -291,7 +275,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
     *out = b;
     hold.b = nullptr;
     return FIONA_OK;
-} catch (const std::bad_alloc &) {
+} catch (const std::exception &) {  // (allocation)
     return set_error(FIONA_ERR_NOMEM, "adapter_batch_create: host allocation");
 }
 
@@ -352,13 +336,11 @@ extern "C" int fiona_adapter_forward(const fiona_adapter_batch *b, void *stream,
     a.out = out;
     a.ld_out = ld_out;
     a.h = h;
-    a.dh = static_cast<float *>(work);
     const bool short_apart = b->n_rows && adapter_rows_apply(b, l->d_in);
     const bool on_tiles = adapter_tiles_apply(b, l->d_in, l->d_out, l->dtype) && tma_rows(vx) && tma_rows(vbase) && tma_rows(vout);
-    if (short_apart && (on_tiles || (!b->n_long && !b->n_bare)) && (rc = launch_adapter_rows(b, stream, l->dtype, a))) return rc;
-    if (short_apart && !b->n_long && !b->n_bare) return FIONA_OK;
+    if (short_apart && (rc = launch_adapter_rows(b, stream, l->dtype, a))) return rc;
     if (on_tiles) return launch_adapter_tiles_forward(b, stream, l->dtype, a, work, short_apart);
-    return launch_adapter_simple_forward(b, stream, l->dtype, a);
+    return launch_adapter_any_forward(b, stream, l->dtype, a, work, short_apart);
 }
 
 extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream, const fiona_adapter_layer *l,
@@ -403,10 +385,9 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
     a.ld_out = ld_dx;
     a.dA = dA;
     a.dB = dB;
-    a.dh = static_cast<float *>(work);
     if (adapter_tiles_apply(b, l->d_in, l->d_out, l->dtype) && tma_rows(vx) && tma_rows(vdy) && tma_rows(vbase) && tma_rows(vdx))
         return launch_adapter_tiles_backward(b, stream, l->dtype, a, work);
-    return launch_adapter_simple_backward(b, stream, l->dtype, a);
+    return launch_adapter_any_backward(b, stream, l->dtype, a, work);
 }
 
 extern "C" int fiona_dropout(const fiona_ctx *ctx, void *stream, uint32_t dtype, uint64_t rows, uint64_t cols,

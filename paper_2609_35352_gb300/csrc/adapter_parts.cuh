@@ -1,0 +1,93 @@
+// adapter_parts.cuh -- what the adapters' kernels share: partial sums in the
+// workspace, rows without an adapter, launches.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "adapter_tiles.h"
+#include "real.cuh"
+
+namespace parts {
+
+using real::narrow;
+using real::widen;
+
+// Launches that follow one another in a call overlap: a kernel lets the next start
+// at once (`next_may_start`), and the next waits for it, as a whole, before it
+// touches what it wrote (`previous_done`).
+__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void previous_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Sum over column ranges of the partial h or dh of four ranks of a row.
+__device__ __forceinline__ float4 sum_parts(const TileArgs &g, uint32_t row, uint32_t j)
+{
+    const size_t step = (size_t)g.a.n_tokens * g.r16;
+    const float *p = g.part_in + (size_t)row * g.r16 + j;
+    float4 s = *reinterpret_cast<const float4 *>(p);
+    for (uint32_t k = 1; k < g.slabs_in; ++k) {
+        const float4 v = *reinterpret_cast<const float4 *>(p + k * step);
+        s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    return s;
+}
+
+__device__ __forceinline__ float4 below(float4 v, uint32_t j, uint32_t rank, float by)
+{
+    return make_float4(j < rank ? v.x * by : 0.f, j + 1 < rank ? v.y * by : 0.f, j + 2 < rank ? v.z * by : 0.f,
+                       j + 3 < rank ? v.w * by : 0.f);
+}
+
+// rows without an adapter: out = base (or zero), h = 0; by a CTA of `threads`
+template <typename T>
+__device__ void bare_rows(const AdapterArgs &a, const AdapterTile t, uint32_t cols, uint32_t threads)
+{
+    constexpr uint32_t kVec = 16 / sizeof(T);
+    if (a.base != a.out) {
+        const bool wide = (((uintptr_t)a.base | (uintptr_t)a.out) & 15) == 0 && (a.ld_base | a.ld_out) % kVec == 0;
+        const uint32_t n = wide ? cols / kVec : 0, rest = cols - n * kVec;
+        for (uint32_t k = threadIdx.x; k < t.rows * n; k += threads) {
+            const uint64_t row = t.row0 + k / n, i = k % n;
+            reinterpret_cast<uint4 *>((T *)a.out + row * a.ld_out)[i] =
+                a.base ? reinterpret_cast<const uint4 *>((const T *)a.base + row * a.ld_base)[i] : make_uint4(0, 0, 0, 0);
+        }
+        for (uint32_t k = threadIdx.x; k < t.rows * rest; k += threads) {
+            const uint64_t row = t.row0 + k / rest, i = n * kVec + k % rest;
+            ((T *)a.out)[row * a.ld_out + i] = a.base ? ((const T *)a.base)[row * a.ld_base + i] : narrow<T>(0.f);
+        }
+    }
+    if (a.h)
+        for (uint32_t k = threadIdx.x; k < t.rows * a.r_max; k += threads) a.h[(uint64_t)t.row0 * a.r_max + k] = 0.f;
+}
+
+// dA and dB of every adapter: its chunks' sums added up in order, zero where
+// there are none and outside the rank.
+struct GradSum {
+    const float *part;       // [chunks][part_rows][part_inner]
+    const uint32_t *begin;   // [n_adapters + 1]
+    void *out;               // [n_adapters][rows][inner]
+    uint32_t rows, inner, part_rows, part_inner;
+    uint32_t rank_rows;      // the rank bounds rows (dA) or columns (dB)
+};
+
+// `after`: the kernel waits for the one before it by itself
+template <typename K>
+inline int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t s, bool after, void **args, const char *what)
+{
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid;
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = s;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &attr;
+    c.numAttrs = after ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelExC(&c, (const void *)kernel, args);
+    if (e != cudaSuccess) return set_error(FIONA_ERR_CUDA, "%s launch: %s", what, cudaGetErrorString(e));
+    return FIONA_OK;
+}
+
+inline uint64_t align_up(uint64_t n) { return (n + 255) & ~255ull; }
+
+}  // namespace parts

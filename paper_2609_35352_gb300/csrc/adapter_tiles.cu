@@ -30,14 +30,14 @@
 #include <mutex>
 #include <type_traits>
 
+#include "adapter_parts.cuh"
 #include "adapter_tiles.h"
 #include "real.cuh"
 #include "tc_tiles.cuh"
 
 namespace {
 
-using real::narrow;
-using real::widen;
+using namespace parts;
 using tiles::chunk_at;
 
 constexpr uint32_t kBar = 8;
@@ -94,25 +94,6 @@ __device__ __forceinline__ uint4 ld_shared16(uint32_t addr)
 __device__ __forceinline__ void st_shared16(uint32_t addr, uint4 v)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-
-// Sum over column ranges of the partial h or dh of four ranks of a row.
-__device__ __forceinline__ float4 sum_parts(const TileArgs &g, uint32_t row, uint32_t j)
-{
-    const size_t step = (size_t)g.a.n_tokens * g.r16;
-    const float *p = g.part_in + (size_t)row * g.r16 + j;
-    float4 s = *reinterpret_cast<const float4 *>(p);
-    for (uint32_t k = 1; k < g.slabs_in; ++k) {
-        const float4 v = *reinterpret_cast<const float4 *>(p + k * step);
-        s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-    }
-    return s;
-}
-
-__device__ __forceinline__ float4 below(float4 v, uint32_t j, uint32_t rank, float by)
-{
-    return make_float4(j < rank ? v.x * by : 0.f, j + 1 < rank ? v.y * by : 0.f, j + 2 < rank ? v.z * by : 0.f,
-                       j + 3 < rank ? v.w * by : 0.f);
 }
 
 // four ranks of a row into the operand's two parts
@@ -189,28 +170,6 @@ __device__ __forceinline__ void clean_box(uint32_t box, const dropout::Mask &m, 
     for (; row < kTileRows; row += kRows) st_shared16(box + chunk_at(row, c), make_uint4(0, 0, 0, 0));
 }
 
-// rows without an adapter: out = base (or zero), h = 0; by a CTA of `threads`
-template <typename T>
-__device__ void bare_rows(const AdapterArgs &a, const AdapterTile t, uint32_t cols, uint32_t threads)
-{
-    constexpr uint32_t kVec = 16 / sizeof(T);
-    if (a.base != a.out) {
-        const bool wide = (((uintptr_t)a.base | (uintptr_t)a.out) & 15) == 0 && (a.ld_base | a.ld_out) % kVec == 0;
-        const uint32_t n = wide ? cols / kVec : 0, rest = cols - n * kVec;
-        for (uint32_t k = threadIdx.x; k < t.rows * n; k += threads) {
-            const uint64_t row = t.row0 + k / n, i = k % n;
-            reinterpret_cast<uint4 *>((T *)a.out + row * a.ld_out)[i] =
-                a.base ? reinterpret_cast<const uint4 *>((const T *)a.base + row * a.ld_base)[i] : make_uint4(0, 0, 0, 0);
-        }
-        for (uint32_t k = threadIdx.x; k < t.rows * rest; k += threads) {
-            const uint64_t row = t.row0 + k / rest, i = n * kVec + k % rest;
-            ((T *)a.out)[row * a.ld_out + i] = a.base ? ((const T *)a.base)[row * a.ld_base + i] : narrow<T>(0.f);
-        }
-    }
-    if (a.h)
-        for (uint32_t k = threadIdx.x; k < t.rows * a.r_max; k += threads) a.h[(uint64_t)t.row0 * a.r_max + k] = 0.f;
-}
-
 // ---------------------------------------------------------------------------
 // shrink: partial h of a token tile over a range of columns
 // ---------------------------------------------------------------------------
@@ -237,14 +196,18 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
     const uint32_t base = aligned_smem(sm), bar0 = async::smem_addr(bars), S = g.stages;
     const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
     const uint32_t done = bar0 + 3 * kBar * kMaxStages;
-    const uint32_t stage = shrink_stage<BACK>(g.r16, g.blocks), cols = max(32u, g.r16 <= 32 ? 32u : g.r16 <= 64 ? 64u : 128u);
+    const uint32_t stage = shrink_stage<BACK>(g.r16, g.blocks);
+    // The accumulator cuts every addition to fp32 toward zero: boxes go to several
+    // in turn, for chains a few times shorter (one chain of 128 additions erred by
+    // 2.1e-6 of h, two fp32 dot products by 1.1e-6)
+    const uint32_t accs = g.r16 <= 64 ? 4 : 2, cols = g.r16 <= 16 ? 64 : g.r16 <= 32 ? 128 : 256;
     const AdapterTile t = g.tiles[blockIdx.x / g.cut.slabs];
     const uint32_t slab = blockIdx.x % g.cut.slabs;
     const uint32_t b0 = slab * g.cut.width, n = min(g.boxes - b0, g.cut.width);
     const bool fix = !BACK && g.a.mask.level != 0;
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
 
-    tiles::next_may_start();
+    parts::next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (uint32_t s = 0; s < S; ++s) {
@@ -296,8 +259,8 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
                 const uint64_t da = tiles::desc(buf, 16), db = tiles::desc(buf + kBoxBytes, BACK ? 64 * 128 : 16);
 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k)
-                    tiles::mma(tmem, da + k * tiles::kStepK, db + k * (BACK ? tiles::kStepMN : tiles::kStepK), id,
-                               i > 0 || k > 0);
+                    tiles::mma(tmem + i % accs * g.r16, da + k * tiles::kStepK,
+                               db + k * (BACK ? tiles::kStepMN : tiles::kStepK), id, i >= accs || k > 0);
                 tcs::commit(empty + kBar * s);
                 if (i + 1 == n) tcs::commit(done);
             }
@@ -318,12 +281,19 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
         w.pass(done, 0);
         tcs::fence_after();
         __syncwarp();
-        tiles::previous_done();
+        parts::previous_done();
         float *p = g.part_out + ((size_t)slab * g.a.n_tokens + t.row0 + row) * g.r16;
         for (uint32_t c = half * 16; c < n16; c += 32) {
             float v[16];
             tiles::ld16(tmem + ((quarter * 32) << 16) + c, v);
             tcs::wait_ld();
+            for (uint32_t q = 1; q < min(accs, n); ++q) {
+                float u[16];
+                tiles::ld16(tmem + ((quarter * 32) << 16) + q * g.r16 + c, u);
+                tcs::wait_ld();
+#pragma unroll
+                for (uint32_t k = 0; k < 16; ++k) v[k] += u[k];
+            }
             if (row < t.rows)
 #pragma unroll
                 for (uint32_t k = 0; k < 16; k += 4)
@@ -361,8 +331,8 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
     const uint32_t done = bar0 + 3 * kBar * kMaxStages, free_ = done + 2 * kBar, ready = free_ + 2 * kBar;
     const uint32_t stage = expand_stage(g.blocks);
     if (blockIdx.x < g.n_bare) {
-        tiles::next_may_start();
-        tiles::previous_done();
+        parts::next_may_start();
+        parts::previous_done();
         bare_rows<T>(g.a, g.bare[blockIdx.x], g.cols, kExpandThreads);
         return;
     }
@@ -374,7 +344,7 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
     const bool fix = rank != n16 && rank < g.a.r_max;
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
 
-    tiles::next_may_start();
+    parts::next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         s_most = 0;
@@ -443,7 +413,7 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
     } else if (me.warp < 10) {
         const uint32_t worker = threadIdx.x - 64, quarter = me.warp & 3, half = (me.warp - 2) / 4;
         // h: the sum of its parts, in two 16-bit parts (and whole, where wanted)
-        tiles::previous_done();
+        parts::previous_done();
         const uint32_t groups = n16 / 4;
         float most = 0.f;
         if (!is_bf16<T>()) {
@@ -594,7 +564,7 @@ __device__ __forceinline__ void load_operands(const TileArgs &g, const GradJob &
 {
     const uint32_t n = job.c.end - job.c.begin, H = g.buffers, bytes = g.op_boxes * kBoxBytes;
     uint32_t issued = 0;
-    tiles::previous_done();
+    parts::previous_done();
     for (uint32_t t = 0; t < n; ++t) {
         if (t >= H) w.pass(used + kBar * (t % H), (t / H - 1) & 1);
         __syncwarp();
@@ -644,7 +614,7 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
     const bool fix = job.ragged(g);
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
 
-    tiles::next_may_start();
+    parts::next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (uint32_t s = 0; s < S; ++s) {
@@ -732,7 +702,7 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
     } else if (me.warp < 10) {
         const uint32_t quarter = me.warp & 3, half = (me.warp - 2) / 4;
         const uint32_t row = quarter * 32 + me.lane;
-        tiles::previous_done();
+        parts::previous_done();
         for (uint32_t t = 0; t < (g.with_dh ? n_tiles : 0); ++t) {
             const uint32_t d = t & 1;
             const AdapterTile tile = g.tiles[job.c.begin + t];
@@ -806,8 +776,8 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
     __shared__ int s_abort;
     const Roles me;
     if (blockIdx.x < g.n_bare) {
-        tiles::next_may_start();
-        tiles::previous_done();
+        parts::next_may_start();
+        parts::previous_done();
         bare_rows<T>(g.a, g.bare[blockIdx.x], g.cols, kExpandGradThreads);
         return;
     }
@@ -822,7 +792,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
     const uint32_t a_box = g.r16 * 128, bits_at = 2 * kBoxBytes + 2 * a_box;
 
-    tiles::next_may_start();
+    parts::next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (uint32_t s = 0; s < S; ++s) {
@@ -909,7 +879,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
     } else if (me.warp < 10) {
         const uint32_t worker = threadIdx.x - 64, quarter = me.warp & 3, half = (me.warp - 2) / 4;
         const uint32_t row = quarter * 32 + me.lane;
-        tiles::previous_done();
+        parts::previous_done();
         const float scale = g.a.mask.factor * (1.f / g.ups[job.c.begin]);
         uint32_t i = 0;
         for (uint32_t t = 0; t < n_tiles; ++t) {
@@ -1026,8 +996,8 @@ __global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image,
     const uint32_t rank = g.a.ranks[t.adapter], groups = g.r16 / 4;
     const float s_a = DH ? g.a.scales[t.adapter] : 1.f;
     if (threadIdx.x == 0) s_most = 0;
-    tiles::next_may_start();
-    tiles::previous_done();
+    parts::next_may_start();
+    parts::previous_done();
     __syncthreads();
     auto value = [&](uint32_t k) {
         const uint32_t r = r0 + k / groups, j = k % groups * 4;
@@ -1070,16 +1040,6 @@ __global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image,
     }
 }
 
-// dA and dB of every adapter: its chunks' sums added up in order, zero where
-// there are none and outside the rank.
-struct GradSum {
-    const float *part;       // [chunks][part_rows][part_inner]
-    const uint32_t *begin;   // [n_adapters + 1]
-    void *out;               // [n_adapters][rows][inner]
-    uint32_t rows, inner, part_rows, part_inner;
-    uint32_t rank_rows;      // the rank bounds rows (dA) or columns (dB)
-};
-
 template <typename T>
 __global__ void __launch_bounds__(256) k_grad_sum(const GradSum A, const GradSum B, const uint32_t *ranks, uint32_t blocks_A,
                                                   uint32_t first)
@@ -1090,7 +1050,7 @@ __global__ void __launch_bounds__(256) k_grad_sum(const GradSum A, const GradSum
     if (k >= (uint64_t)g.rows * per_row) return;
     const uint32_t row = (uint32_t)(k / per_row), col = (uint32_t)(k % per_row) * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    tiles::previous_done();
+    parts::previous_done();
     if (row < (g.rank_rows ? rank : g.rows) && col < (g.rank_rows ? g.inner : rank)) {
         const uint32_t end = g.begin[ad + 1];
         const size_t step = (size_t)g.part_rows * g.part_inner;
@@ -1141,8 +1101,6 @@ int tensor_map(CUtensorMap *tm, uint32_t dtype, const void *p, uint64_t cols, ui
     return FIONA_OK;
 }
 
-uint64_t align_up(uint64_t n) { return (n + 255) & ~255ull; }
-
 // `boxes` of a row's columns in ranges, so that `units` of them make about
 // `want` CTAs
 Cut cut_columns(uint32_t boxes, uint32_t units, uint32_t want)
@@ -1166,25 +1124,6 @@ struct ForwardShape {
         return align_up((uint64_t)shrink.slabs * b->n_tokens * r.r16 * 4);
     }
 };
-
-// `after`: the kernel waits for the one before it by itself
-template <typename K>
-int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t s, bool after, void **args, const char *what)
-{
-    cudaLaunchConfig_t c{};
-    c.gridDim = grid;
-    c.blockDim = dim3(threads);
-    c.dynamicSmemBytes = smem;
-    c.stream = s;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = &attr;
-    c.numAttrs = after ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelExC(&c, (const void *)kernel, args);
-    if (e != cudaSuccess) return set_error(FIONA_ERR_CUDA, "%s launch: %s", what, cudaGetErrorString(e));
-    return FIONA_OK;
-}
 
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr uint32_t kSmemTwo = 110 * 1024;   // dynamic shared memory of a CTA, two of them an SM

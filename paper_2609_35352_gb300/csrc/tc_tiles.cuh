@@ -82,12 +82,6 @@ __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.com
 // until the stores committed have read their shared memory
 __device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 
-// Launches that follow one another in a call overlap: a kernel lets the next start
-// at once (`next_may_start`), and the next waits for it, as a whole, before it
-// touches what it wrote (`previous_done`).
-__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void previous_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *tm)
 {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
