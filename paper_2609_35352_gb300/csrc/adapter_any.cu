@@ -8,8 +8,8 @@
 // its tile's sums in registers, 4 x 4 (4 x 8 above rank 64) a thread, and reads
 // both factors from shared memory as they were widened: 16 multiplications for two
 // 16-byte reads.  Where few ranks leave threads over, they split the sum's axis
-// and are added up at the end.  Loads are element by element along the rows, the
-// next slice's under the multiplications.
+// and are added up at the end.  Loads are element by element along the rows, two
+// slices ahead of the multiplications.
 //
 // Bound by the FMA units above rank 16 or so; below, by launches and HBM.
 #include <cuda_runtime.h>
@@ -112,8 +112,8 @@ __global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
     const uint64_t ld = BACK ? g.a.ld_dy : g.a.ldx;
     const T *W = BACK ? (const T *)g.a.B + (size_t)t.adapter * g.a.d_out * g.a.r_max : (const T *)g.a.A + (size_t)t.adapter * g.a.r_max * g.a.d_in;
     constexpr uint32_t kX = kRows / kWarps, kW = BACK ? kSlice / kWarps * ((kRanks + 31) / 32) : (kRanks + kWarps - 1) / kWarps;
-    float fx[kX], fw[kW];
-    auto fetch = [&](uint32_t k) {
+    float fx0[kX], fw0[kW], fx1[kX], fw1[kW];
+    auto fetch = [&](uint32_t k, float (&fx)[kX], float (&fw)[kW]) {
         const uint32_t col = k + lane;
 #pragma unroll
         for (uint32_t q = 0; q < kX; ++q) {
@@ -132,8 +132,7 @@ __global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
         }
     };
     Sums<NRG, RPT> s;
-    fetch(k0);
-    for (uint32_t k = k0; k < k1; k += kSlice) {
+    auto step = [&](uint32_t k, float (&fx)[kX], float (&fw)[kW]) {
         __syncthreads();
 #pragma unroll
         for (uint32_t q = 0; q < kX; ++q) {
@@ -151,8 +150,14 @@ __global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
             }
         }
         __syncthreads();
-        if (k + kSlice < k1) fetch(k + kSlice);
+        if (k + 2 * kSlice < k1) fetch(k + 2 * kSlice, fx, fw);
         s.slice(sm.f.X, sm.f.S);
+    };
+    fetch(k0, fx0, fw0);
+    if (k0 + kSlice < k1) fetch(k0 + kSlice, fx1, fw1);
+    for (uint32_t k = k0; k < k1; k += 2 * kSlice) {
+        step(k, fx0, fw0);
+        if (k + kSlice < k1) step(k + kSlice, fx1, fw1);
     }
     s.join(sm.sum);
     for (uint32_t e = threadIdx.x; e < rows * g.r16; e += kThreads) {
@@ -162,7 +167,8 @@ __global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
 }
 
 // out = base + s h B^T, or dx = dx_base + D'(dh A) (BACK), of half a tile and 64
-// columns: a thread 4 rows and the columns 16 apart
+// columns: a thread 4 rows and the columns 16 apart.  The block of the first columns
+// leaves h or dh whole
 template <typename T, bool BACK>
 __global__ void __launch_bounds__(kThreads) k_any_expand(const TileArgs g)
 {
@@ -191,7 +197,20 @@ __global__ void __launch_bounds__(kThreads) k_any_expand(const TileArgs g)
             const uint32_t col = col0 + c + 16 * q;
             base[i][q] = g.a.base ? element((const T *)g.a.base + (uint64_t)(row0 + r4 + i) * g.a.ld_base + col, r4 + i < rows && col < g.cols) : 0.f;
         }
-    float acc[4][4] = {};
+    float acc[4][4] = {}, fw[kSlice * kCols / kThreads];
+    auto fetch = [&](uint32_t j0) {
+#pragma unroll
+        for (uint32_t q = 0; q < kSlice * kCols / kThreads; ++q) {
+            if (BACK) {
+                const uint32_t j = j0 + warp + q / 2 * kWarps, i = col0 + lane + q % 2 * 32;
+                fw[q] = element(W + (size_t)j * g.a.d_in + i, j < rank && i < g.cols);
+            } else {
+                const uint32_t j = j0 + lane, i = col0 + warp + q * kWarps;
+                fw[q] = element(W + (size_t)i * g.a.r_max + j, j < rank && i < g.cols);
+            }
+        }
+    };
+    fetch(0);
     previous_done();
     const float by = BACK ? g.a.scales[t.adapter] : g.a.mask.factor;
     for (uint32_t j0 = 0; j0 < g.a.r_max; j0 += kSlice) {
@@ -206,18 +225,17 @@ __global__ void __launch_bounds__(kThreads) k_any_expand(const TileArgs g)
             for (uint32_t i = 0; i < 4; ++i) {
                 H[j - j0 + i][r] = f[i];
                 if (!BACK && g.a.h && col0 == 0 && r < rows && j + i < g.a.r_max) g.a.h[(size_t)(row0 + r) * g.a.r_max + j + i] = f[i];
+                if (BACK && col0 == 0 && r < rows && j + i < rank) g.dh[(size_t)(row0 + r) * g.r16 + j + i] = f[i];
             }
         }
 #pragma unroll
         for (uint32_t q = 0; q < kSlice * kCols / kThreads; ++q) {
-            if (BACK) {
-                const uint32_t j = warp + q / 2 * kWarps, i = lane + q % 2 * 32;
-                S[j][i] = element(W + (size_t)(j0 + j) * g.a.d_in + col0 + i, j0 + j < rank && col0 + i < g.cols);
-            } else {
-                const uint32_t i = warp + q * kWarps;
-                S[lane][i] = element(W + (size_t)(col0 + i) * g.a.r_max + j0 + lane, j0 + lane < rank && col0 + i < g.cols);
-            }
+            if (BACK)
+                S[warp + q / 2 * kWarps][lane + q % 2 * 32] = fw[q];
+            else
+                S[lane][warp + q * kWarps] = fw[q];
         }
+        if (j0 + kSlice < rank) fetch(j0 + kSlice);
         __syncthreads();
         const uint32_t n = min(kSlice, rank > j0 ? rank - j0 : 0);
 #pragma unroll 4
@@ -257,10 +275,25 @@ __device__ __forceinline__ void weight_grad(const TileArgs &g, uint32_t block, S
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = g.a.ranks[ch.adapter];
     const T *x = INNER ? (const T *)g.a.x : (const T *)g.a.dy;
     const uint64_t ld = INNER ? g.a.ldx : g.a.ld_dy;
-    const float s_a = g.a.scales[ch.adapter];
     constexpr uint32_t kX = kSlice * kCols / kThreads, kS = kSlice / kWarps * ((kRanks + 31) / 32);
-    float fx[kX], fs[kS];
-    auto fetch = [&](const AdapterTile &t, uint32_t r0) {
+    // slice i of the chunk: 32 rows of a tile
+    struct Place {
+        AdapterTile t;
+        uint32_t tile, r0;
+    };
+    auto next = [&](Place p) {
+        p.r0 += kSlice;
+        if (p.r0 >= p.t.rows) {
+            p.r0 = 0;
+            if (++p.tile < ch.end) p.t = g.tiles[p.tile];
+        }
+        return p;
+    };
+    float fx0[kX], fs0[kS], fx1[kX], fs1[kS];
+    auto fetch = [&](const Place &p, float (&fx)[kX], float (&fs)[kS]) {
+        if (p.tile >= ch.end) return;
+        const AdapterTile &t = p.t;
+        const uint32_t r0 = p.r0;
 #pragma unroll
         for (uint32_t q = 0; q < kX; ++q) {
             const uint32_t r = r0 + warp + q / 2 * kWarps, col = col0 + lane + q % 2 * 32;
@@ -272,9 +305,7 @@ __device__ __forceinline__ void weight_grad(const TileArgs &g, uint32_t block, S
             float v = 0.f;
             if (r < t.rows && j < rank) {
                 if (INNER) {
-                    const float *p = g.part_in + (size_t)(t.row0 + r) * g.r16 + j;
-                    for (uint32_t k = 0; k < g.slabs_in; ++k) v += p[k * (size_t)g.a.n_tokens * g.r16];
-                    v *= s_a;
+                    v = g.dh[(size_t)(t.row0 + r) * g.r16 + j];
                 } else {
                     v = g.a.h_in[(size_t)(t.row0 + r) * g.a.r_max + j];
                 }
@@ -283,15 +314,13 @@ __device__ __forceinline__ void weight_grad(const TileArgs &g, uint32_t block, S
         }
     };
     Sums<NRG, RPT> s;
-    uint32_t tile = ch.begin, r0 = 0;
-    AdapterTile t = g.tiles[tile];
-    fetch(t, 0);
-    while (tile < ch.end) {
+    auto step = [&](const Place &p, const Place &ahead, float (&fx)[kX], float (&fs)[kS]) {
         __syncthreads();
 #pragma unroll
         for (uint32_t q = 0; q < kX; ++q) {
             const uint32_t r = warp + q / 2 * kWarps, c = lane + q % 2 * 32;
-            const bool drop = INNER && g.a.mask.level && r0 + r < t.rows && col0 + c < cols && !g.a.mask.keep(t.row0 + r0 + r, col0 + c);
+            const bool drop = INNER && g.a.mask.level && p.r0 + r < p.t.rows && col0 + c < cols &&
+                              !g.a.mask.keep(p.t.row0 + p.r0 + r, col0 + c);
             sm.f.X[r][c] = drop ? 0.f : fx[q];
         }
 #pragma unroll
@@ -300,16 +329,23 @@ __device__ __forceinline__ void weight_grad(const TileArgs &g, uint32_t block, S
             if (j < kRanks) sm.f.S[warp + q % (kSlice / kWarps) * kWarps][j] = fs[q];
         }
         __syncthreads();
-        r0 += kSlice;
-        if (r0 >= t.rows) {
-            r0 = 0;
-            if (++tile < ch.end) t = g.tiles[tile];
-        }
-        if (tile < ch.end) fetch(t, r0);
+        fetch(ahead, fx, fs);
         s.slice(sm.f.X, sm.f.S);
+    };
+    Place p{g.tiles[ch.begin], ch.begin, 0}, q = next(p);
+    fetch(p, fx0, fs0);
+    fetch(q, fx1, fs1);
+    while (p.tile < ch.end) {
+        Place a = next(q);
+        step(p, a, fx0, fs0);
+        if (q.tile >= ch.end) break;
+        p = a;
+        a = next(a);
+        step(q, a, fx1, fs1);
+        q = a;
     }
     s.join(sm.sum);
-    const float scale = INNER ? g.a.mask.factor : s_a;
+    const float scale = INNER ? g.a.mask.factor : g.a.scales[ch.adapter];
     for (uint32_t e = threadIdx.x; e < 64 * rank; e += kThreads) {
         const uint32_t c = INNER ? e % 64 : e / rank, j = INNER ? e / 64 : e % rank;
         if (col0 + c >= cols) continue;
@@ -371,12 +407,12 @@ auto pick_grad(uint32_t r)
          : r <= 64 ? k_any_grad<T, 16, 4> : k_any_grad<T, 16, 8>;
 }
 
-// Column ranges of a shrink: enough blocks for four an SM, and no fewer than eight
-// slices each.
+// Column ranges of a shrink: enough blocks for four an SM, and no fewer than four
+// slices each (two are under way at once).
 Cut shrink_cut(const fiona_adapter_batch *b, uint32_t cols, uint32_t n_tiles)
 {
     const uint32_t want = 4 * (uint32_t)std::max(b->ctx->sm_count, 1), slices = ceil_div(cols, kSlice);
-    uint32_t slabs = std::min(want / std::max(2 * n_tiles, 1u), ceil_div(slices, 8));
+    uint32_t slabs = std::min(want / std::max(2 * n_tiles, 1u), ceil_div(slices, 4));
     slabs = std::max(1u, std::min(slabs, 16u));
     const uint32_t width = ceil_div(slices, slabs) * kSlice;
     return Cut{width, ceil_div(cols, width)};
@@ -393,13 +429,14 @@ const AdapterChunks &grad_chunks(const fiona_adapter_batch *b, uint32_t d_in, ui
 
 struct AnyShape {
     uint32_t r16;
-    uint64_t part = 0, grad_A = 0, grad_B = 0, bytes = 0;
+    uint64_t part = 0, dh = 0, grad_A = 0, grad_B = 0, bytes = 0;
     AnyShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) : r16((b->r_max + 15) & ~15u)
     {
         const uint32_t slabs = std::max({shrink_cut(b, d_in, b->n_tiles).slabs, shrink_cut(b, d_out, b->n_tiles).slabs,
                                          shrink_cut(b, d_in, b->n_long).slabs});
         const uint32_t chunks = grad_chunks(b, d_in, d_out).count;
-        grad_A = part + align_up((uint64_t)slabs * b->n_tokens * r16 * 4);
+        dh = part + align_up((uint64_t)slabs * b->n_tokens * r16 * 4);
+        grad_A = dh + align_up((uint64_t)b->n_tokens * r16 * 4);
         grad_B = grad_A + align_up((uint64_t)chunks * d_in * r16 * 4);
         bytes = grad_B + align_up((uint64_t)chunks * d_out * r16 * 4);
     }
@@ -443,6 +480,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a,
     g.r16 = f.r16;
     g.part_out = reinterpret_cast<float *>(ws + f.part);
     g.part_in = g.part_out;
+    g.dh = reinterpret_cast<float *>(ws + f.dh);
     g.cols = a.d_out;
     g.cut = shrink_cut(b, a.d_out, g.n_tiles);
     g.slabs_in = g.cut.slabs;

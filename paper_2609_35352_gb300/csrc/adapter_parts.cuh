@@ -24,6 +24,7 @@ __device__ __forceinline__ float4 sum_parts(const TileArgs &g, uint32_t row, uin
     const size_t step = (size_t)g.a.n_tokens * g.r16;
     const float *p = g.part_in + (size_t)row * g.r16 + j;
     float4 s = *reinterpret_cast<const float4 *>(p);
+#pragma unroll 4
     for (uint32_t k = 1; k < g.slabs_in; ++k) {
         const float4 v = *reinterpret_cast<const float4 *>(p + k * step);
         s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;

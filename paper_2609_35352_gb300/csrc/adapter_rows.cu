@@ -8,17 +8,18 @@
 // lanes a column of B, so that loads run along B's rows).  One launch, no workspace.
 //
 // Bound by reading A and B once (rows of one adapter share a read), and for a few
-// requests by the latency of that chain: B's eighth is on its way into L2 while A's
-// is read.  Partial sums are added in the order of the CTAs.
-#include <cooperative_groups.h>
+// requests by the latency of that chain.  Partial sums are added in the order of the
+// CTAs.  Measured on GB300, 256 requests of 200 adapters, 2048 -> 8192, ranks 16 to
+// 64 in rows of 64: 52 us, 248 MB from HBM, as the unused ranks come with the others
+// in lines of 128 bytes (36 us at the copy bandwidth).  Every output stored by the
+// lane that held its sum made it 58 us, a cluster of four 63.
 #include <cuda_runtime.h>
 
 #include <algorithm>
 
 #include "adapter.h"
 #include "real.cuh"
-
-namespace cg = cooperative_groups;
+#include "tc_tiles.cuh"
 
 namespace {
 
@@ -44,10 +45,45 @@ struct Vec {
 
 __device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
+// The cluster's barrier in two halves, for execution order alone.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_cta()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// the address of this CTA's shared `addr` in CTA `cta` of the cluster
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t cta)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
+    return r;
+}
+// 16 bytes to another CTA's shared memory, counted on its barrier
+__device__ __forceinline__ void push16(uint32_t dst, uint32_t bar, float4 v)
+{
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(dst),
+                 "r"(__float_as_uint(v.x)), "r"(__float_as_uint(v.y)), "r"(__float_as_uint(v.z)), "r"(__float_as_uint(v.w)), "r"(bar)
+                 : "memory");
+}
+
 struct RowsArgs {
     AdapterArgs a;
     const AdapterRows *groups;
     uint32_t slice_in, slice_out;  // columns a CTA, multiples of 8
+    int *err;
+    uint64_t wait_ns;
+};
+
+// shared memory of a CTA, but for its rows of x
+struct RowsShared {
+    float part[kAdapterRows][FIONA_ADAPTER_MAX_RANK];           // this CTA's partial h
+    float from[kCluster][kAdapterRows][FIONA_ADAPTER_MAX_RANK]; // everyone's
+    float h[kAdapterRows][FIONA_ADAPTER_MAX_RANK];
+    uint64_t bar;
+    int abort;
 };
 
 // This CTA's partial h of the ranks of one warp (every kWarps-th), UJ of them and
@@ -101,98 +137,103 @@ __device__ __forceinline__ void partial_h(const T *A, uint32_t d_in, uint32_t n_
     }
 }
 
-// VEC: rows of A and B are whole vectors of 16 bytes
-template <typename T, bool VEC, uint32_t G>
-__device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &rows, float *s_x, float *s_part, float *s_h)
+// N values of T next to one another, in one access where they are aligned
+template <typename T, uint32_t N>
+__device__ __forceinline__ void load_run(const T *p, bool wide, uint32_t valid, float (&v)[N])
 {
-    constexpr uint32_t V = VEC ? Vec<T>::n : 1, kUnroll = under_way(G);
-    cg::cluster_group cluster = cg::this_cluster();
-    const AdapterArgs &a = g.a;
-    const uint32_t cta = cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t rank = a.ranks[rows.adapter];
-    const uint32_t i0 = min(cta * g.slice_in, a.d_in), n_in = min(g.slice_in, a.d_in - i0);
-    const uint32_t o0 = min(cta * g.slice_out, a.d_out), n_out = min(g.slice_out, a.d_out - o0);
-    const T *A = (const T *)a.A + (size_t)rows.adapter * a.r_max * a.d_in + i0;
-    const T *B = (const T *)a.B + ((size_t)rows.adapter * a.d_out + o0) * a.r_max;
-
-    // this CTA's A and B towards L2 (not B where less than half of a row is wanted:
-    // lines come whole)
-    const uint32_t lines = (n_in * (uint32_t)sizeof(T) + 127) / 128;
-    for (uint32_t k = tid; k < rank * lines; k += kThreads)
-        prefetch_l2(reinterpret_cast<const char *>(A + (size_t)(k / lines) * a.d_in) + k % lines * 128);
-    if (2 * rank > a.r_max)
-        for (size_t k = (size_t)tid * 128; k < (size_t)n_out * a.r_max * sizeof(T); k += kThreads * 128)
-            prefetch_l2(reinterpret_cast<const char *>(B) + k);
+    constexpr uint32_t kBytes = N * sizeof(T);
+    __align__(16) T e[N];
+    if (wide && valid >= N) {
+        if constexpr (kBytes % 16 == 0) {
 #pragma unroll
-    for (uint32_t r = 0; r < G; ++r) {
-        const uint64_t t = rows.row[r];
-        const T *x = (const T *)a.x + t * a.ldx + i0;
-        for (uint32_t i = tid; i < n_in; i += kThreads) {
-            const bool drop = a.mask.level && !a.mask.keep(t, i0 + i);
-            s_x[r * g.slice_in + i] = drop ? 0.f : widen(x[i]);
+            for (uint32_t i = 0; i < kBytes / 16; ++i) reinterpret_cast<uint4 *>(e)[i] = reinterpret_cast<const uint4 *>(p)[i];
+        } else if constexpr (kBytes == 8) {
+            *reinterpret_cast<uint2 *>(e) = *reinterpret_cast<const uint2 *>(p);
+        } else if constexpr (kBytes == 4) {
+            *reinterpret_cast<uint32_t *>(e) = *reinterpret_cast<const uint32_t *>(p);
+        } else {
+            e[0] = p[0];
         }
-    }
-    __syncthreads();
-
-    if (VEC) {
-        if (rank <= 2 * kWarps)
-            partial_h<T, G, 2>(A, a.d_in, n_in, rank, g.slice_in, s_x, s_part, warp, lane);
-        else
-            partial_h<T, G, kUnroll>(A, a.d_in, n_in, rank, g.slice_in, s_x, s_part, warp, lane);
     } else {
-        for (uint32_t j = warp; j < rank; j += kWarps) {
-            float acc[G] = {};
-#pragma unroll 8
-            for (uint32_t i = lane; i < n_in; i += 32) {
-                const float w = widen(A[(size_t)j * a.d_in + i]);
 #pragma unroll
-                for (uint32_t r = 0; r < G; ++r) acc[r] = fmaf(w, s_x[r * g.slice_in + i], acc[r]);
-            }
-#pragma unroll
-            for (uint32_t r = 0; r < G; ++r) {
-                for (int o = 16; o; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
-                if (lane == 0) s_part[r * FIONA_ADAPTER_MAX_RANK + j] = acc[r];
-            }
-        }
+        for (uint32_t i = 0; i < N; ++i) e[i] = i < valid ? p[i] : narrow<T>(0.f);
     }
-    cluster.sync();
-    for (uint32_t k = tid; k < G * a.r_max; k += kThreads) {
-        const uint32_t r = k / a.r_max, j = k % a.r_max;
-        float s = 0.f;
-        if (j < rank) {
-            float v[kCluster];
 #pragma unroll
-            for (uint32_t c = 0; c < kCluster; ++c) v[c] = cluster.map_shared_rank(s_part, c)[r * FIONA_ADAPTER_MAX_RANK + j];
+    for (uint32_t i = 0; i < N; ++i) v[i] = widen(e[i]);
+}
+template <typename T, uint32_t N>
+__device__ __forceinline__ void store_run(T *p, bool wide, uint32_t valid, const float (&v)[N])
+{
+    constexpr uint32_t kBytes = N * sizeof(T);
+    __align__(16) T e[N];
 #pragma unroll
-            for (uint32_t c = 0; c < kCluster; ++c) s += v[c];
-            s *= a.mask.factor;
+    for (uint32_t i = 0; i < N; ++i) e[i] = narrow<T>(v[i]);
+    if (wide && valid >= N) {
+        if constexpr (kBytes % 16 == 0) {
+#pragma unroll
+            for (uint32_t i = 0; i < kBytes / 16; ++i) reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(e)[i];
+        } else if constexpr (kBytes == 8) {
+            *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(e);
+        } else if constexpr (kBytes == 4) {
+            *reinterpret_cast<uint32_t *>(p) = *reinterpret_cast<const uint32_t *>(e);
+        } else {
+            p[0] = e[0];
         }
-        s_h[r * FIONA_ADAPTER_MAX_RANK + j] = s;
-        if (a.h && cta == 0) a.h[(size_t)rows.row[r] * a.r_max + j] = s;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i)
+            if (i < valid) p[i] = e[i];
     }
-    cluster.barrier_arrive();  // (the others' last read of this CTA's shared memory: awaited at the end)
-    __syncthreads();
+}
 
-    // 2^shift lanes a column, a vector of ranks each; kUnroll columns at a time, the
-    // lanes' results to as many lanes
+// The sums over L lanes of U values each, scattered: lane s of the L keeps the sums
+// of the U / L values from s U / L on (of one value, where L is larger).
+template <uint32_t U, uint32_t L>
+__device__ __forceinline__ void sum_scatter(float (&v)[U], uint32_t lane)
+{
+    uint32_t n = U;
+#pragma unroll
+    for (uint32_t o = L / 2; o; o /= 2) {
+        if (n > 1) {
+            n /= 2;
+            const bool upper = lane & o;
+#pragma unroll
+            for (uint32_t i = 0; i < U / 2; ++i)
+                if (i < n) {
+                    const float give = upper ? v[i] : v[i + n], keep = upper ? v[i + n] : v[i];
+                    v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                }
+        } else {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+        }
+    }
+}
+
+// This CTA's outputs: L lanes a column of B, a vector of ranks each (or element by
+// element), as many columns at a time as loads are to be under way.
+template <typename T, bool VEC, uint32_t G, uint32_t L>
+__device__ __forceinline__ void outputs(const RowsArgs &g, const AdapterRows &rows, const T *B, uint32_t rank, uint32_t o0,
+                                        uint32_t n_out, const RowsShared &sh)
+{
+    constexpr uint32_t V = VEC ? Vec<T>::n : 1, U = under_way(G), kMine = U > L ? U / L : 1, kStep = kThreads / L * U;
+    const AdapterArgs &a = g.a;
+    const uint32_t lane = threadIdx.x & 31, sub = lane % L;
+    const uint32_t mine = U > L ? sub * kMine : sub / (L / U);  // first of the columns this lane ends up with
+    const bool writes = U > L || sub % (L > U ? L / U : 1) == 0;
+    const bool wide = ((uintptr_t)a.out | (uintptr_t)a.base | (a.ld_out | (a.base ? a.ld_base : 0)) * sizeof(T)) % 16 == 0;
     const float scale = a.scales[rows.adapter];
-    uint32_t shift = 0;
-    while (shift < 5 && (V << shift) < rank) ++shift;
-    const uint32_t lanes = 1u << shift, sub = lane & (lanes - 1), step = (kThreads >> shift) * kUnroll;
-    for (uint32_t c0 = (tid >> shift) * kUnroll; c0 - (tid >> shift) * kUnroll < n_out; c0 += step) {
-        float acc[kUnroll][G] = {}, base[kUnroll][G] = {};
+    for (uint32_t at = 0; at < n_out; at += kStep) {
+        const uint32_t c0 = at + threadIdx.x / L * U, col = c0 + mine, valid = col < n_out && writes ? n_out - col : 0;
+        float acc[G][U] = {}, base[G][kMine] = {};
         if (a.base)
 #pragma unroll
-            for (uint32_t u = 0; u < kUnroll; ++u)
-                if (u % lanes == sub && c0 + u < n_out)
+            for (uint32_t r = 0; r < G; ++r)
+                load_run<T, kMine>((const T *)a.base + (uint64_t)rows.row[r] * a.ld_base + o0 + col, wide, valid, base[r]);
+        for (uint32_t j = sub * V; j < rank; j += L * V) {
+            uint4 w[U];
+            T e[U];
 #pragma unroll
-                    for (uint32_t r = 0; r < G; ++r)
-                        base[u][r] = widen(((const T *)a.base)[(uint64_t)rows.row[r] * a.ld_base + o0 + c0 + u]);
-        for (uint32_t j = sub * V; j < rank; j += lanes * V) {
-            uint4 w[kUnroll];
-            T e[kUnroll];
-#pragma unroll
-            for (uint32_t u = 0; u < kUnroll; ++u) {
+            for (uint32_t u = 0; u < U; ++u) {
                 const T *b = B + (size_t)(c0 + u) * a.r_max + j;
                 w[u] = make_uint4(0, 0, 0, 0);
                 e[u] = narrow<T>(0.f);
@@ -207,9 +248,9 @@ __device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &
 #pragma unroll
             for (uint32_t r = 0; r < G; ++r)
 #pragma unroll
-                for (uint32_t k = 0; k < V; ++k) h[r][k] = s_h[r * FIONA_ADAPTER_MAX_RANK + j + k];
+                for (uint32_t k = 0; k < V; ++k) h[r][k] = sh.h[r][j + k];
 #pragma unroll
-            for (uint32_t u = 0; u < kUnroll; ++u) {
+            for (uint32_t u = 0; u < U; ++u) {
                 float f[Vec<T>::n];
                 if (VEC)
                     Vec<T>::widen_all(w[u], f);
@@ -219,39 +260,124 @@ __device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &
                 for (uint32_t k = 0; k < V; ++k)
                     if (j + k < rank)
 #pragma unroll
-                        for (uint32_t r = 0; r < G; ++r) acc[u][r] = fmaf(f[k], h[r][k], acc[u][r]);
+                        for (uint32_t r = 0; r < G; ++r) acc[r][u] = fmaf(f[k], h[r][k], acc[r][u]);
             }
         }
-        for (uint32_t o = lanes / 2; o; o >>= 1)
 #pragma unroll
-            for (uint32_t u = 0; u < kUnroll; ++u)
+        for (uint32_t r = 0; r < G; ++r) {
+            __syncwarp();
+            sum_scatter<U, L>(acc[r], lane);
+            float y[kMine];
 #pragma unroll
-                for (uint32_t r = 0; r < G; ++r) acc[u][r] += __shfl_xor_sync(0xffffffffu, acc[u][r], o);
-#pragma unroll
-        for (uint32_t u = 0; u < kUnroll; ++u)
-            if (u % lanes == sub && c0 + u < n_out)
-#pragma unroll
-                for (uint32_t r = 0; r < G; ++r)
-                    ((T *)a.out)[(uint64_t)rows.row[r] * a.ld_out + o0 + c0 + u] = narrow<T>(fmaf(scale, acc[u][r], base[u][r]));
+            for (uint32_t i = 0; i < kMine; ++i) y[i] = fmaf(scale, acc[r][i], base[r][i]);
+            store_run<T, kMine>((T *)a.out + (uint64_t)rows.row[r] * a.ld_out + o0 + col, wide, valid, y);
+        }
     }
-    cluster.barrier_wait();
+}
+
+// VEC: rows of A and B are whole vectors of 16 bytes
+template <typename T, bool VEC, uint32_t G>
+__device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &rows, float *s_x, RowsShared &sh)
+{
+    constexpr uint32_t V = VEC ? Vec<T>::n : 1, kUnroll = under_way(G);  // (V: ranks a lane)
+    const AdapterArgs &a = g.a;
+    const uint32_t cta = cluster_cta(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t rank = a.ranks[rows.adapter], rank4 = (rank + 3) / 4;
+    const uint32_t bar = async::smem_addr(&sh.bar);
+    if (tid == 0) {
+        sh.abort = 0;
+        async::mbar_init(bar, 1);
+        async::mbar_init_fence();
+        async::mbar_arrive_expect_tx(bar, kCluster * G * rank4 * 16);
+    }
+    __syncthreads();
+    cluster_arrive();  // (awaited before the first push to another CTA)
+    const uint32_t i0 = min(cta * g.slice_in, a.d_in), n_in = min(g.slice_in, a.d_in - i0);
+    const uint32_t o0 = min(cta * g.slice_out, a.d_out), n_out = min(g.slice_out, a.d_out - o0);
+    const T *A = (const T *)a.A + (size_t)rows.adapter * a.r_max * a.d_in + i0;
+    const T *B = (const T *)a.B + ((size_t)rows.adapter * a.d_out + o0) * a.r_max;
+
+    // this CTA's A on its way while x comes
+    const uint32_t lines = (n_in * (uint32_t)sizeof(T) + 127) / 128;
+    for (uint32_t k = tid; k < rank * lines; k += kThreads)
+        prefetch_l2(reinterpret_cast<const char *>(A + (size_t)(k / lines) * a.d_in) + k % lines * 128);
+#pragma unroll
+    for (uint32_t r = 0; r < G; ++r) {
+        const uint64_t t = rows.row[r];
+        const T *x = (const T *)a.x + t * a.ldx + i0;
+        for (uint32_t i = tid; i < n_in; i += kThreads) {
+            const bool drop = a.mask.level && !a.mask.keep(t, i0 + i);
+            s_x[r * g.slice_in + i] = drop ? 0.f : widen(x[i]);
+        }
+    }
+    __syncthreads();
+
+    if (VEC) {
+        if (rank <= 2 * kWarps)
+            partial_h<T, G, 2>(A, a.d_in, n_in, rank, g.slice_in, s_x, &sh.part[0][0], warp, lane);
+        else
+            partial_h<T, G, kUnroll>(A, a.d_in, n_in, rank, g.slice_in, s_x, &sh.part[0][0], warp, lane);
+    } else {
+        for (uint32_t j = warp; j < rank; j += kWarps) {
+            float acc[G] = {};
+#pragma unroll 8
+            for (uint32_t i = lane; i < n_in; i += 32) {
+                const float w = widen(A[(size_t)j * a.d_in + i]);
+#pragma unroll
+                for (uint32_t r = 0; r < G; ++r) acc[r] = fmaf(w, s_x[r * g.slice_in + i], acc[r]);
+            }
+#pragma unroll
+            for (uint32_t r = 0; r < G; ++r) {
+                for (int o = 16; o; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
+                if (lane == 0) sh.part[r][j] = acc[r];
+            }
+        }
+    }
+    __syncthreads();
+    cluster_wait();
+    for (uint32_t k = tid; k < kCluster * G * rank4; k += kThreads) {
+        const uint32_t to = k % kCluster, r = k / kCluster % G, j = k / kCluster / G * 4;
+        push16(in_cta(async::smem_addr(&sh.from[cta][r][j]), to), in_cta(bar, to), *reinterpret_cast<const float4 *>(&sh.part[r][j]));
+    }
+    tiles::Waits{&sh.abort, g.err, g.wait_ns}.pass(bar, 0);
+    for (uint32_t k = tid; k < G * a.r_max; k += kThreads) {
+        const uint32_t r = k / a.r_max, j = k % a.r_max;
+        float s = 0.f;
+        if (j < rank) {
+#pragma unroll
+            for (uint32_t c = 0; c < kCluster; ++c) s += sh.from[c][r][j];
+            s *= a.mask.factor;
+        }
+        sh.h[r][j] = s;
+        if (a.h && cta == 0) a.h[(size_t)rows.row[r] * a.r_max + j] = s;
+    }
+    __syncthreads();
+
+    switch (rank > V ? 32 - __clz((int)((rank + V - 1) / V - 1)) : 0) {  // log2 of the lanes a column
+        case 0: outputs<T, VEC, G, 1>(g, rows, B, rank, o0, n_out, sh); break;
+        case 1: outputs<T, VEC, G, 2>(g, rows, B, rank, o0, n_out, sh); break;
+        case 2: outputs<T, VEC, G, 4>(g, rows, B, rank, o0, n_out, sh); break;
+        case 3: outputs<T, VEC, G, 8>(g, rows, B, rank, o0, n_out, sh); break;
+        case 4: outputs<T, VEC, G, 16>(g, rows, B, rank, o0, n_out, sh); break;
+        default: outputs<T, VEC, G, 32>(g, rows, B, rank, o0, n_out, sh); break;
+    }
 }
 
 // MOST: the largest group of the batch
 template <typename T, bool VEC, uint32_t MOST>
-__global__ void __launch_bounds__(kThreads, MOST <= 2 ? 3 : 2) k_rows(const RowsArgs g)
+__global__ void __launch_bounds__(kThreads, MOST <= 2 ? 4 : 2) k_rows(const RowsArgs g)
 {
     extern __shared__ __align__(16) float s_x[];  // [rows][slice_in]
-    __shared__ float s_part[kAdapterRows * FIONA_ADAPTER_MAX_RANK], s_h[kAdapterRows * FIONA_ADAPTER_MAX_RANK];
+    __shared__ __align__(16) RowsShared sh;
     const AdapterRows rows = g.groups[blockIdx.x / kCluster];
     if (rows.count == 1)
-        rows_body<T, VEC, 1>(g, rows, s_x, s_part, s_h);
+        rows_body<T, VEC, 1>(g, rows, s_x, sh);
     else if (MOST > 1 && rows.count == 2)
-        rows_body<T, VEC, (MOST > 1 ? 2 : 1)>(g, rows, s_x, s_part, s_h);
+        rows_body<T, VEC, (MOST > 1 ? 2 : 1)>(g, rows, s_x, sh);
     else if (MOST > 2 && rows.count == 3)
-        rows_body<T, VEC, (MOST > 2 ? 3 : 1)>(g, rows, s_x, s_part, s_h);
+        rows_body<T, VEC, (MOST > 2 ? 3 : 1)>(g, rows, s_x, sh);
     else if (MOST > 2)
-        rows_body<T, VEC, (MOST > 2 ? 4 : 1)>(g, rows, s_x, s_part, s_h);
+        rows_body<T, VEC, (MOST > 2 ? 4 : 1)>(g, rows, s_x, sh);
 }
 
 // columns of `d` a CTA of the cluster takes
@@ -266,7 +392,7 @@ auto pick(uint32_t most)
 template <typename T>
 int run(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a)
 {
-    const RowsArgs g{a, b->d_rows, slice(a.d_in), slice(a.d_out)};
+    const RowsArgs g{a, b->d_rows, slice(a.d_in), slice(a.d_out), b->ctx->d_kerr, 2000000000ull};
     void (*kernel)(RowsArgs) = a.d_in % Vec<T>::n == 0 && a.r_max % Vec<T>::n == 0 ? pick<T, true>(b->most_rows)
                                                                                    : pick<T, false>(b->most_rows);
     cudaLaunchConfig_t c{};
@@ -287,7 +413,7 @@ int run(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a)
 
 bool adapter_rows_apply(const fiona_adapter_batch *b, uint32_t d_in)
 {
-    return (size_t)b->most_rows * slice(d_in) * 4 <= 32 * 1024;
+    return (size_t)b->most_rows * slice(d_in) * 4 <= 24 * 1024;  // (beside 21 KB)
 }
 
 int launch_adapter_rows(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a)

@@ -983,15 +983,19 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
     if (me.warp == 1) tcs::tmem_dealloc(tmem, g.tmem_cols);
 }
 
-// The images of h or dh (DH: the sum of its parts, times s_a): a block 32 rows of
-// a tile, zero past the tile and from the rank on.  fp16 goes by a power of two that is
+// The images of h or dh (DH: the sum of its parts, times s_a): a block as many
+// rows of a tile as make 256 pieces of four ranks, zero past the tile and from the rank
+// on.  fp16 goes by a power of two that is
 // one for all of an adapter's tiles (they share accumulators), from the largest
-// value of each quarter tile (MOST: this kernel's first pass).
+// value of each block (MOST: this kernel's first pass).
+__host__ __device__ constexpr uint32_t image_blocks(uint32_t r16) { return r16 <= 16 ? 2 : r16 <= 32 ? 4 : r16 <= 64 ? 8 : 16; }
+
 template <typename T, bool DH, bool MOST>
 __global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image, float *ups, float *most, const uint32_t *tile_begin)
 {
     __shared__ uint32_t s_most;
-    const uint32_t tile = blockIdx.x / 4, r0 = blockIdx.x % 4 * 32;
+    const uint32_t per_tile = image_blocks(g.r16), n_rows = kTileRows / per_tile;
+    const uint32_t tile = blockIdx.x / per_tile, r0 = blockIdx.x % per_tile * n_rows;
     const AdapterTile t = g.tiles[tile];
     const uint32_t rank = g.a.ranks[t.adapter], groups = g.r16 / 4;
     const float s_a = DH ? g.a.scales[t.adapter] : 1.f;
@@ -1010,12 +1014,12 @@ __global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image,
     if (!is_bf16<T>()) {
         float big = 0.f;
         if (MOST) {
-            for (uint32_t k = threadIdx.x; k < 32 * groups; k += 256) {
+            for (uint32_t k = threadIdx.x; k < n_rows * groups; k += 256) {
                 const float4 v = value(k);
                 big = fmaxf(big, fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
             }
         } else {
-            for (uint32_t k = 4 * tile_begin[t.adapter] + threadIdx.x; k < 4 * tile_begin[t.adapter + 1]; k += 256) big = fmaxf(big, most[k]);
+            for (uint32_t k = per_tile * tile_begin[t.adapter] + threadIdx.x; k < per_tile * tile_begin[t.adapter + 1]; k += 256) big = fmaxf(big, most[k]);
         }
         for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
         if ((threadIdx.x & 31) == 0) atomicMax(&s_most, __float_as_uint(big));
@@ -1028,7 +1032,7 @@ __global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image,
     }
     if (threadIdx.x == 0 && r0 == 0) ups[tile] = up;
     uint8_t *to = image + (size_t)tile * g.op_boxes * kBoxBytes;
-    for (uint32_t k = threadIdx.x; k < 32 * groups; k += 256) {
+    for (uint32_t k = threadIdx.x; k < n_rows * groups; k += 256) {
         const uint32_t row = r0 + k / groups, j = k % groups * 4;
         const float4 v = value(k);
         uint2 hi, lo;
@@ -1235,7 +1239,7 @@ struct BackwardShape {
         grad_A = dh_image + (uint64_t)b->n_tiles * r.boxes * kBoxBytes;
         grad_B = grad_A + align_up((uint64_t)expand.chunks->count * d_in * r.r16 * 4);
         most = grad_B + align_up((uint64_t)shrink.chunks->count * d_out * r.r16 * 4);
-        ups = most + align_up((uint64_t)b->n_tiles * 4 * 4);
+        ups = most + align_up((uint64_t)b->n_tiles * image_blocks(r.r16) * 4);
         bytes = ups + align_up((uint64_t)b->n_tiles * 2 * 4);
     }
 };
@@ -1271,10 +1275,10 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         uint8_t *image = ws + f.image;
         float *ups = reinterpret_cast<float *>(ws + f.ups), *most = reinterpret_cast<float *>(ws + f.most);
         void *iargs[] = {&g, &image, &ups, &most, (void *)&b->d_tile_begin};
-        const dim3 quarters(4 * b->n_tiles);
+        const dim3 iblocks(image_blocks(g.r16) * b->n_tiles);
         const bool any = b->n_tiles != 0;
-        if (any && !is_bf16<T>() && (rc = launch(k_image<T, false, true>, quarters, 256, 0, s, false, iargs, "adapter image"))) return rc;
-        if (any && (rc = launch(k_image<T, false, false>, quarters, 256, 0, s, !is_bf16<T>(), iargs, "adapter image"))) return rc;
+        if (any && !is_bf16<T>() && (rc = launch(k_image<T, false, true>, iblocks, 256, 0, s, false, iargs, "adapter image"))) return rc;
+        if (any && (rc = launch(k_image<T, false, false>, iblocks, 256, 0, s, !is_bf16<T>(), iargs, "adapter image"))) return rc;
         if (any && f.apart) {
             const uint32_t stage = shrink_stage<true>(g.r16, g.blocks);
             g.cols = a.d_out;
@@ -1308,8 +1312,8 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         ups += b->n_tiles;
         g.part_in = g.part_out;
         g.slabs_in = f.dh_cut.slabs;
-        if (any && !is_bf16<T>() && (rc = launch(k_image<T, true, true>, quarters, 256, 0, s, true, iargs, "adapter image"))) return rc;
-        if (any && (rc = launch(k_image<T, true, false>, quarters, 256, 0, s, true, iargs, "adapter image"))) return rc;
+        if (any && !is_bf16<T>() && (rc = launch(k_image<T, true, true>, iblocks, 256, 0, s, true, iargs, "adapter image"))) return rc;
+        if (any && (rc = launch(k_image<T, true, false>, iblocks, 256, 0, s, true, iargs, "adapter image"))) return rc;
         g.image = image;
         g.ups = ups;
         g.bare = b->d_bare;

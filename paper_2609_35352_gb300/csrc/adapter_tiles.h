@@ -51,7 +51,7 @@ struct TileArgs {
     float *part_out;       // partial h or dh of this pass
     uint32_t with_dh;      // shrink_grad: whether it makes the partial dh
     float *grad;           // [chunks][...] partial dB or dA
-    float *grad_b;         // (the passes of adapter_any.cu: dB, beside dA)
+    float *grad_b, *dh;    // (adapter_any.cu: dB beside dA; dh whole, [n_tokens][r16])
     uint32_t n_tiles, n_chunks, stages, buffers, tmem_cols;
     int *err;
     uint64_t wait_ns;
