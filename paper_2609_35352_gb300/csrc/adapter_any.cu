@@ -101,6 +101,7 @@ __global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
     using Sh = Shared<NRG, RPT>;
     __shared__ __align__(16) Sh sm;
     constexpr uint32_t kRanks = Sh::kRanks;
+    previous_done();
     next_may_start();
     const AdapterTile t = g.tiles[blockIdx.x / (2 * g.cut.slabs)];
     const uint32_t half = blockIdx.x / g.cut.slabs % 2, slab = blockIdx.x % g.cut.slabs;
@@ -377,6 +378,7 @@ __global__ void __launch_bounds__(kThreads) k_any_grad_sum(const GradSum A, cons
     const GradSum &g = blockIdx.x < blocks_A ? A : B;
     const uint32_t ad = first + blockIdx.y, rank = ranks[ad];
     const uint64_t k = (uint64_t)(blockIdx.x < blocks_A ? blockIdx.x : blockIdx.x - blocks_A) * kThreads + threadIdx.x;
+    next_may_start();
     previous_done();
     if (k >= (uint64_t)g.rows * g.inner) return;
     const uint32_t row = (uint32_t)(k / g.inner), col = (uint32_t)(k % g.inner);
@@ -457,14 +459,14 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a, 
     g.slabs_in = g.cut.slabs;
     void *args[] = {&g};
     int rc = FIONA_OK;
-    if (g.n_tiles && (rc = launch(pick_shrink<T, false>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, false, args, "adapter shrink")))
+    if (g.n_tiles && (rc = launch(pick_shrink<T, false>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter shrink")))
         return rc;
     g.cols = a.d_out;
     g.cut = Cut{kCols, ceil_div(a.d_out, kCols)};
     g.bare = b->d_bare;
     g.n_bare = b->n_bare;
     if (!g.n_tiles && !g.n_bare) return FIONA_OK;
-    return launch(k_any_expand<T, false>, g.n_bare + 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, g.n_tiles != 0, args, "adapter expand");
+    return launch(k_any_expand<T, false>, g.n_bare + 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter expand");
 }
 
 template <typename T>
@@ -487,26 +489,26 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a,
     void *args[] = {&g};
     int rc = FIONA_OK;
     const bool any = b->n_tiles != 0;
-    if (any && (rc = launch(pick_shrink<T, true>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, false, args, "adapter dh"))) return rc;
+    if (any && (rc = launch(pick_shrink<T, true>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter dh"))) return rc;
     g.cols = a.d_in;
     g.cut = Cut{kCols, ceil_div(a.d_in, kCols)};
     g.bare = b->d_bare;
     g.n_bare = b->n_bare;
-    if ((any || g.n_bare) && (rc = launch(k_any_expand<T, true>, g.n_bare + 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, any, args, "adapter dx")))
+    if ((any || g.n_bare) && (rc = launch(k_any_expand<T, true>, g.n_bare + 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter dx")))
         return rc;
     g.chunks = chunks.d_chunks;
     g.grad = reinterpret_cast<float *>(ws + f.grad_A);
     g.grad_b = reinterpret_cast<float *>(ws + f.grad_B);
     uint32_t blocks_A = chunks.count * ceil_div(a.d_in, kCols), blocks_B = chunks.count * ceil_div(a.d_out, kCols);
     void *gargs[] = {&g, &blocks_A};
-    if (any && (rc = launch(pick_grad<T>(a.r_max), blocks_A + blocks_B, kThreads, 0, s, true, gargs, "adapter weight gradients"))) return rc;
+    if (any && (rc = launch(pick_grad<T>(a.r_max), blocks_A + blocks_B, kThreads, 0, s, gargs, "adapter weight gradients"))) return rc;
     const GradSum A{g.grad, chunks.d_begin, a.dA, a.r_max, a.d_in, f.r16, a.d_in, 1};
     const GradSum B{g.grad_b, chunks.d_begin, a.dB, a.d_out, a.r_max, a.d_out, f.r16, 0};
     const uint32_t sum_A = (uint32_t)(((uint64_t)a.r_max * a.d_in + kThreads - 1) / kThreads);
     const uint32_t sum_B = (uint32_t)(((uint64_t)a.r_max * a.d_out + kThreads - 1) / kThreads);
     for (uint32_t i = 0; i < a.n_adapters && rc == FIONA_OK; i += 65535) {
         void *sargs[] = {(void *)&A, (void *)&B, (void *)&a.ranks, (void *)&sum_A, &i};
-        rc = launch(k_any_grad_sum<T>, dim3(sum_A + sum_B, std::min(a.n_adapters - i, 65535u)), kThreads, 0, s, any || g.n_bare, sargs,
+        rc = launch(k_any_grad_sum<T>, dim3(sum_A + sum_B, std::min(a.n_adapters - i, 65535u)), kThreads, 0, s, sargs,
                     "adapter gradients");
     }
     return rc;

@@ -12,9 +12,12 @@ namespace parts {
 using real::narrow;
 using real::widen;
 
-// Launches that follow one another in a call overlap: a kernel lets the next start
-// at once (`next_may_start`), and the next waits for it, as a whole, before it
-// touches what it wrote (`previous_done`).
+// Launches overlap: a kernel lets the next start at once (`next_may_start`), and the
+// next waits for it, as a whole (`previous_done`), before it touches anything that a
+// kernel before it writes.  The first kernel of a call waits for what came before
+// the call, before it reads anything, and only then lets the next start: so the later
+// ones may read the call's inputs without waiting.  Every kernel waits before it
+// ends, so that the last one's end is the end of all.
 __device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void previous_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -70,9 +73,9 @@ struct GradSum {
     uint32_t rank_rows;      // the rank bounds rows (dA) or columns (dB)
 };
 
-// `after`: the kernel waits for the one before it by itself
+// a kernel that waits for the one before it by itself
 template <typename K>
-inline int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t s, bool after, void **args, const char *what)
+inline int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t s, void **args, const char *what)
 {
     cudaLaunchConfig_t c{};
     c.gridDim = grid;
@@ -83,7 +86,7 @@ inline int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     c.attrs = &attr;
-    c.numAttrs = after ? 1 : 0;
+    c.numAttrs = 1;
     const cudaError_t e = cudaLaunchKernelExC(&c, (const void *)kernel, args);
     if (e != cudaSuccess) return set_error(FIONA_ERR_CUDA, "%s launch: %s", what, cudaGetErrorString(e));
     return FIONA_OK;

@@ -17,7 +17,7 @@
 
 #include <algorithm>
 
-#include "adapter.h"
+#include "adapter_parts.cuh"
 #include "real.cuh"
 #include "tc_tiles.cuh"
 
@@ -297,6 +297,8 @@ __device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &
     const T *A = (const T *)a.A + (size_t)rows.adapter * a.r_max * a.d_in + i0;
     const T *B = (const T *)a.B + ((size_t)rows.adapter * a.d_out + o0) * a.r_max;
 
+    parts::previous_done();
+    parts::next_may_start();
     // this CTA's A on its way while x comes
     const uint32_t lines = (n_in * (uint32_t)sizeof(T) + 127) / 128;
     for (uint32_t k = tid; k < rank * lines; k += kThreads)
@@ -400,11 +402,13 @@ int run(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a)
     c.blockDim = dim3(kThreads);
     c.dynamicSmemBytes = (size_t)b->most_rows * g.slice_in * 4;
     c.stream = s;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim = {kCluster, 1, 1};
-    c.attrs = &attr;
-    c.numAttrs = 1;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {kCluster, 1, 1};
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = attr;
+    c.numAttrs = 2;
     const cudaError_t e = cudaLaunchKernelEx(&c, kernel, g);
     return e == cudaSuccess ? FIONA_OK : set_error(FIONA_ERR_CUDA, "adapter rows launch: %s", cudaGetErrorString(e));
 }

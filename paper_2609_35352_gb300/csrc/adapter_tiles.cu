@@ -26,6 +26,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <mutex>
 #include <type_traits>
@@ -137,12 +138,15 @@ __device__ __forceinline__ void arrive_warp(uint32_t bar, uint32_t lane)
     if (lane == 0) async::mbar_arrive(bar);
 }
 
+// the place of the flags of a row's chunk of 8 elements
+__device__ __forceinline__ uint32_t flags_at(uint32_t row, uint32_t chunk) { return row * 64 + ((chunk ^ (row & 7)) << 3); }
+
 // Drop masked elements and rows at or past `rows` of a box of 128 rows, by
-// `threads` threads (a multiple of 16; eight a row); with `bits` (shared, 8 bytes a
-// row) a set bit says dropped.
-template <uint32_t THREADS, bool BITS>
+// `threads` threads (eight a row); with FLAGS a byte an element (shared, 64 a row,
+// flags_at) says dropped (0xFF) or kept (0).
+template <uint32_t THREADS, bool FLAGS>
 __device__ __forceinline__ void clean_box(uint32_t box, const dropout::Mask &m, uint32_t row0, uint32_t rows,
-                                          uint32_t col0, uint32_t thread, uint32_t bits)
+                                          uint32_t col0, uint32_t thread, uint32_t flags)
 {
     constexpr uint32_t kRows = THREADS / 8;  // a multiple of 8 or 4, 2: a thread's chunk keeps its swizzle every 8 rows
     const uint32_t c = thread % 8;
@@ -159,10 +163,10 @@ __device__ __forceinline__ void clean_box(uint32_t box, const dropout::Mask &m, 
             uint4 u = ld_shared16(at);
             u.x &= ~d0, u.y &= ~d1, u.z &= ~d2, u.w &= ~d3;
             st_shared16(at, u);
-            if (BITS) {
-                const uint32_t b = (d0 & 0x00020001u) | (d1 & 0x00080004u) | (d2 & 0x00200010u) | (d3 & 0x00800040u);
-                asm volatile("st.shared.b8 [%0], %1;" ::"r"(bits + row * 8 + c), "r"(b | b >> 16) : "memory");
-            }
+            if (FLAGS)
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(flags + flags_at(row, c)), "r"(__byte_perm(d0, d1, 0x6420)),
+                             "r"(__byte_perm(d2, d3, 0x6420))
+                             : "memory");
         }
     } else if (row < rows) {
         row += (rows - row + kRows - 1) / kRows * kRows;
@@ -207,7 +211,7 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
     const bool fix = !BACK && g.a.mask.level != 0;
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
 
-    parts::next_may_start();
+    if (BACK) parts::next_may_start();
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (uint32_t s = 0; s < S; ++s) {
@@ -226,6 +230,10 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
     tcs::fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
     const uint32_t rank = g.a.ranks[t.adapter], n16 = (rank + 15) & ~15u;
+    if (!BACK) {  // (the first of a forward pass)
+        parts::previous_done();
+        parts::next_may_start();
+    }
 
     if (me.warp == 0) {
         uint32_t issued = 0;
@@ -310,10 +318,43 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
 // ---------------------------------------------------------------------------
 // expand: out = base + s h B^T of a token tile over a range of columns
 // ---------------------------------------------------------------------------
-constexpr uint32_t kExpandThreads = 384;  // TMA, MMA, eight epilogue warps, two that clear B past the rank
+constexpr uint32_t kExpandThreads = 416;  // TMA, MMA, eight epilogue warps, two that clear B past the rank, stores
 constexpr uint32_t kExpandWorkers = 256;
 
 __host__ __device__ constexpr uint32_t expand_stage(uint32_t blocks) { return kBoxBytes + blocks * 64 * 128; }
+
+// A tile of `boxes` boxes out of shared memory, by one warp: by TMA where it has all
+// of its rows, else row by row (the rows behind are another request's); then its
+// stage is free.
+template <typename T>
+__device__ __forceinline__ void store_tile(const TileArgs &g, const CUtensorMap &map, const AdapterTile &t, uint32_t buf,
+                                           uint32_t col0, uint32_t boxes, uint32_t empty, uint32_t lane)
+{
+    if (t.rows == kTileRows) {
+        if (lane == 0) {
+            for (uint32_t k = 0; k < boxes; ++k)
+                if (col0 + k * 64 < g.cols) tiles::tma_store_2d(&map, col0 + k * 64, t.row0, buf + k * kBoxBytes);
+            tiles::store_commit();
+            tiles::store_wait_read();
+        }
+    } else {
+        const uint32_t per = 8 * boxes;
+        for (uint32_t k = lane; k < t.rows * per; k += 32) {
+            const uint32_t r = k / per, c = k % per, col = col0 + c * 8;
+            const uint4 v = ld_shared16(buf + c / 8 * kBoxBytes + chunk_at(r, c % 8));
+            T *o = (T *)g.a.out + (uint64_t)(t.row0 + r) * g.a.ld_out + col;
+            if (col + 8 <= g.cols) {
+                *reinterpret_cast<uint4 *>(o) = v;
+            } else {
+                const T *x = reinterpret_cast<const T *>(&v);
+                for (uint32_t q = 0; q < 8; ++q)
+                    if (col + q < g.cols) o[q] = x[q];
+            }
+        }
+        async::fence_proxy_async();
+    }
+    arrive_warp(empty, lane);
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant__ CUtensorMap tbase,
@@ -321,14 +362,14 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
                                                            const __grid_constant__ CUtensorMap tout, const TileArgs g)
 {
     extern __shared__ uint8_t sm[];
-    __shared__ __align__(8) uint64_t bars[3 * kMaxStages + 5];
+    __shared__ __align__(8) uint64_t bars[4 * kMaxStages + 5];
     __shared__ uint32_t s_tmem, s_most;
     __shared__ int s_abort;
     const Roles me;
     const uint32_t S = g.stages, operand = aligned_smem(sm), base = operand + g.op_boxes * kBoxBytes;
     const uint32_t bar0 = async::smem_addr(bars);
     const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
-    const uint32_t done = bar0 + 3 * kBar * kMaxStages, free_ = done + 2 * kBar, ready = free_ + 2 * kBar;
+    const uint32_t written = bar0 + 3 * kBar * kMaxStages, done = bar0 + 4 * kBar * kMaxStages, free_ = done + 2 * kBar, ready = free_ + 2 * kBar;
     const uint32_t stage = expand_stage(g.blocks);
     if (blockIdx.x < g.n_bare) {
         parts::next_may_start();
@@ -352,6 +393,7 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
             async::mbar_init(full + kBar * s, 1);
             async::mbar_init(fixed + kBar * s, 2);
             async::mbar_init(empty + kBar * s, 1);
+            async::mbar_init(written + kBar * s, kExpandWorkers / 32);
         }
         for (uint32_t k = 0; k < 2; ++k) {
             async::mbar_init(done + kBar * k, 1);
@@ -444,7 +486,7 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
 
         const uint32_t row = quarter * 32 + me.lane;
         for (uint32_t i = 0; i < n; ++i) {
-            const uint32_t s = i % S, buf = base + s * stage, d = i & 1, col0 = (b0 + i) * 64;
+            const uint32_t s = i % S, buf = base + s * stage, d = i & 1;
             w.pass(full + kBar * s, (i / S) & 1);
             w.pass(done + kBar * d, (i / 2) & 1);
             tcs::fence_after();
@@ -470,35 +512,15 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
                 }
                 st_shared16(at, b);
             }
-            if (t.rows == kTileRows) {
-                async::fence_proxy_async();
-                async::named_barrier(1, kExpandWorkers);
-                if (me.warp == 2) {
-                    if (me.lane == 0) {
-                        tiles::tma_store_2d(&tout, col0, t.row0, buf);
-                        tiles::store_commit();
-                        tiles::store_wait_read();
-                    }
-                    arrive_warp(empty + kBar * s, me.lane);
-                }
-            } else {
-                async::named_barrier(1, kExpandWorkers);
-                for (uint32_t k = worker; k < t.rows * 8; k += kExpandWorkers) {
-                    const uint32_t r = k / 8, col = col0 + k % 8 * 8;
-                    const uint4 v4 = ld_shared16(buf + chunk_at(r, k % 8));
-                    T *o = (T *)g.a.out + (uint64_t)(t.row0 + r) * g.a.ld_out + col;
-                    if (col + 8 <= g.cols) {
-                        *reinterpret_cast<uint4 *>(o) = v4;
-                    } else {
-                        const T *x = reinterpret_cast<const T *>(&v4);
-                        for (uint32_t q = 0; q < 8; ++q)
-                            if (col + q < g.cols) o[q] = x[q];
-                    }
-                }
-                async::fence_proxy_async();
-                async::named_barrier(1, kExpandWorkers);
-                if (me.warp == 2) arrive_warp(empty + kBar * s, me.lane);
-            }
+            async::fence_proxy_async();
+            arrive_warp(written + kBar * s, me.lane);
+        }
+    } else if (me.warp == 12) {
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t s = i % S;
+            w.pass(written + kBar * s, (i / S) & 1);
+            __syncwarp();
+            store_tile<T>(g, tout, t, base + s * stage, (b0 + i) * 64, 1, empty + kBar * s, me.lane);
         }
     } else if (fix) {
         // B's columns from the rank to the next multiple of 16 are not B's
@@ -526,13 +548,17 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
 // the gradients: a chunk of one adapter's token tiles over a range of columns
 // ---------------------------------------------------------------------------
 constexpr uint32_t kGradThreads = 480;  // TMA, MMA, eight workers, the operand's TMA, four that clean tiles
-constexpr uint32_t kExpandGradThreads = 608;  // the same, eight that clean and mask
+constexpr uint32_t kExpandGradThreads = 640;  // the same, stores, eight that clean and mask
 constexpr uint32_t kGradWorkers = 256;
 constexpr uint32_t kBlockCols = 128;
 
 // (`blocks` of B, none without dh)
 __host__ __device__ constexpr uint32_t shrink_grad_stage(uint32_t blocks) { return 2 * kBoxBytes + blocks * kBoxBytes; }
-__host__ __device__ constexpr uint32_t expand_grad_stage(uint32_t r16) { return 2 * kBoxBytes + 2 * r16 * 128 + kTileRows * 16; }
+// (and a mask's flags)
+__host__ __device__ constexpr uint32_t expand_grad_stage(uint32_t r16, bool mask)
+{
+    return 2 * kBoxBytes + 2 * r16 * 128 + (mask ? kTileRows * kBlockCols : 0);
+}
 
 // a chunk's walk: stage i is block i % width of the chunk's tile i / width
 struct GradJob {
@@ -771,7 +797,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
                                                               const __grid_constant__ CUtensorMap tdx, const TileArgs g)
 {
     extern __shared__ uint8_t sm[];
-    __shared__ __align__(8) uint64_t bars[3 * kMaxStages + 9];
+    __shared__ __align__(8) uint64_t bars[4 * kMaxStages + 9];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const Roles me;
@@ -782,15 +808,15 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
         return;
     }
     const uint32_t S = g.stages, H = g.buffers, operand = aligned_smem(sm), op_bytes = g.op_boxes * kBoxBytes;
-    const uint32_t base = operand + H * op_bytes, stage = expand_grad_stage(g.r16), bar0 = async::smem_addr(bars);
+    const uint32_t base = operand + H * op_bytes, stage = expand_grad_stage(g.r16, g.a.mask.level != 0), bar0 = async::smem_addr(bars);
     const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
-    const uint32_t ready = bar0 + 3 * kBar * kMaxStages, used = ready + 2 * kBar;  // dh, by buffer
+    const uint32_t written = bar0 + 3 * kBar * kMaxStages, ready = bar0 + 4 * kBar * kMaxStages, used = ready + 2 * kBar;  // dh, by buffer
     const uint32_t done = used + 2 * kBar, free_ = done + 2 * kBar, all = free_ + 2 * kBar;  // dx, by buffer; everything
     const GradJob job(g);
     const bool mask = g.a.mask.level != 0, clean_A = job.rank != job.n16 && job.rank < g.a.r_max;
     const bool fix = mask || clean_A || job.ragged(g);
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
-    const uint32_t a_box = g.r16 * 128, bits_at = 2 * kBoxBytes + 2 * a_box;
+    const uint32_t a_box = g.r16 * 128, flags = 2 * kBoxBytes + 2 * a_box;
 
     parts::next_may_start();
     if (threadIdx.x == 0) {
@@ -799,6 +825,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
             async::mbar_init(full + kBar * s, 1);
             async::mbar_init(fixed + kBar * s, 8);
             async::mbar_init(empty + kBar * s, 1);
+            async::mbar_init(written + kBar * s, kGradWorkers / 32);
         }
         for (uint32_t k = 0; k < 2; ++k) {
             async::mbar_init(ready + kBar * k, 1);
@@ -828,7 +855,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
             __syncwarp();
             if (!__all_sync(0xffffffffu, w.going())) break;
             if (tiles::elect_one()) {
-                async::mbar_arrive_expect_tx(full + kBar * s, bits_at);
+                async::mbar_arrive_expect_tx(full + kBar * s, flags);
                 for (uint32_t k = 0; k < 2; ++k) {
                     tiles::tma_load_2d(buf + k * kBoxBytes, &tx, col0 + k * 64, row0, full + kBar * s);
                     async::tma_load_3d(buf + 2 * kBoxBytes + k * a_box, &tA, col0 + k * 64, 0, job.c.adapter, full + kBar * s);
@@ -877,7 +904,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
         }
         tiles::drain(all, 0);
     } else if (me.warp < 10) {
-        const uint32_t worker = threadIdx.x - 64, quarter = me.warp & 3, half = (me.warp - 2) / 4;
+        const uint32_t quarter = me.warp & 3, half = (me.warp - 2) / 4;
         const uint32_t row = quarter * 32 + me.lane;
         parts::previous_done();
         const float scale = g.a.mask.factor * (1.f / g.ups[job.c.begin]);
@@ -897,49 +924,33 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
                 tcs::wait_ld();
                 tcs::fence_before();
                 arrive_warp(free_ + kBar * d, me.lane);
-                uint2 bits = make_uint2(0u, 0u);
-                if (mask && row < tile.rows)
-                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(bits.x), "=r"(bits.y) : "r"(buf + bits_at + half * 1024 + row * 8) : "memory");
                 const T *b = g.a.base && row < tile.rows ? (const T *)g.a.base + (uint64_t)(tile.row0 + row) * g.a.ld_base : nullptr;
 #pragma unroll
                 for (uint32_t c = 0; c < 8; ++c) {
-                    const uint32_t col = col0 + half * 64 + c * 8, drop = (c < 4 ? bits.x >> (8 * c) : bits.y >> (8 * (c - 4))) & 255;
-                    uint4 o = make_uint4(0, 0, 0, 0);
-                    if (b && col < g.cols) o = *reinterpret_cast<const uint4 *>(b + col);
-                    uint32_t *u = reinterpret_cast<uint32_t *>(&o);
+                    const float *a = &v[c / 2][(c % 2) * 8];
+                    uint4 o = make_uint4(pack<T>(scale * a[0], scale * a[1]), pack<T>(scale * a[2], scale * a[3]),
+                                         pack<T>(scale * a[4], scale * a[5]), pack<T>(scale * a[6], scale * a[7]));
+                    uint2 f = make_uint2(0u, 0u);
+                    if (mask)
+                        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(f.x), "=r"(f.y) : "r"(buf + flags + half * 8192 + flags_at(row, c)) : "memory");
+                    const uint32_t col = col0 + half * 64 + c * 8;
+                    if (b && col < g.cols) {
+                        o = *reinterpret_cast<const uint4 *>(b + col);
+                        uint32_t *u = reinterpret_cast<uint32_t *>(&o);
 #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) {
-                        const float2 f = unpack<T>(u[k]);
-                        const float *a = &v[c / 2][(c % 2) * 8 + 2 * k];
-                        u[k] = pack<T>(drop >> (2 * k) & 1 ? f.x : fmaf(scale, a[0], f.x),
-                                       drop >> (2 * k) & 2 ? f.y : fmaf(scale, a[1], f.y));
+                        for (uint32_t k = 0; k < 4; ++k) {
+                            const float2 x = unpack<T>(u[k]);
+                            const uint32_t d = (k < 2 ? f.x : f.y) >> (16 * (k % 2));
+                            u[k] = pack<T>(d & 0xFF ? x.x : fmaf(scale, a[2 * k], x.x), d & 0xFF00 ? x.y : fmaf(scale, a[2 * k + 1], x.y));
+                        }
+                    } else {
+                        o.x &= ~__byte_perm(f.x, 0, 0x1100), o.y &= ~__byte_perm(f.x, 0, 0x3322);
+                        o.z &= ~__byte_perm(f.y, 0, 0x1100), o.w &= ~__byte_perm(f.y, 0, 0x3322);
                     }
                     st_shared16(buf + half * kBoxBytes + chunk_at(row, c), o);
                 }
-                if (tile.rows == kTileRows) {
-                    async::fence_proxy_async();
-                    async::named_barrier(1, kGradWorkers);
-                    if (me.warp == 2) {
-                        if (me.lane == 0) {
-                            tiles::tma_store_2d(&tdx, col0, tile.row0, buf);
-                            if (col0 + 64 < g.cols) tiles::tma_store_2d(&tdx, col0 + 64, tile.row0, buf + kBoxBytes);
-                            tiles::store_commit();
-                            tiles::store_wait_read();
-                        }
-                        arrive_warp(empty + kBar * s, me.lane);
-                    }
-                } else {
-                    async::named_barrier(1, kGradWorkers);
-                    for (uint32_t k = worker; k < tile.rows * 16; k += kGradWorkers) {
-                        const uint32_t r = k / 16, c = k % 16, col = col0 + c * 8;
-                        if (col < g.cols)  // (columns come in eights)
-                            *reinterpret_cast<uint4 *>((T *)g.a.out + (uint64_t)(tile.row0 + r) * g.a.ld_out + col) =
-                                ld_shared16(buf + c / 8 * kBoxBytes + chunk_at(r, c % 8));
-                    }
-                    async::fence_proxy_async();
-                    async::named_barrier(1, kGradWorkers);
-                    if (me.warp == 2) arrive_warp(empty + kBar * s, me.lane);
-                }
+                async::fence_proxy_async();
+                arrive_warp(written + kBar * s, me.lane);
             }
         }
         w.pass(all, 0);
@@ -959,17 +970,25 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
         tcs::fence_before();
     } else if (me.warp == 10) {
         load_operands(g, job, operand, ready, used, w);
+    } else if (me.warp == 11) {
+        for (uint32_t i = 0; i < job.n; ++i) {
+            const uint32_t s = i % S;
+            w.pass(written + kBar * s, (i / S) & 1);
+            __syncwarp();
+            store_tile<T>(g, tdx, g.tiles[job.c.begin + i / job.width], base + s * stage, (job.b0 + i % job.width) * kBlockCols, 2,
+                          empty + kBar * s, me.lane);
+        }
     } else if (fix) {
         for (uint32_t i = 0; i < job.n; ++i) {
             const uint32_t s = i % S, buf = base + s * stage, col0 = (job.b0 + i % job.width) * kBlockCols;
             const AdapterTile tile = g.tiles[job.c.begin + i / job.width];
             w.pass(full + kBar * s, (i / S) & 1);
             __syncwarp();
-            const uint32_t thread = threadIdx.x - 352;
+            const uint32_t thread = threadIdx.x - 384;
             if (mask || tile.rows < kTileRows)
                 for (uint32_t k = 0; k < 2; ++k)
                     clean_box<256, true>(buf + k * kBoxBytes, g.a.mask, tile.row0, tile.rows, col0 + k * 64, thread,
-                                         buf + bits_at + k * 1024);
+                                         buf + flags + k * 8192);
             if (clean_A)  // A's rows from the rank to the next multiple of 16 are not A's
                 for (uint32_t k = thread; k < (job.n16 - job.rank) * 16; k += 256)
                     st_shared16(buf + 2 * kBoxBytes + k % 16 / 8 * a_box + chunk_at(job.rank + k / 16, k % 8), make_uint4(0, 0, 0, 0));
@@ -1000,8 +1019,8 @@ __global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image,
     const uint32_t rank = g.a.ranks[t.adapter], groups = g.r16 / 4;
     const float s_a = DH ? g.a.scales[t.adapter] : 1.f;
     if (threadIdx.x == 0) s_most = 0;
-    parts::next_may_start();
     parts::previous_done();
+    parts::next_may_start();
     __syncthreads();
     auto value = [&](uint32_t k) {
         const uint32_t r = r0 + k / groups, j = k % groups * 4;
@@ -1051,10 +1070,11 @@ __global__ void __launch_bounds__(256) k_grad_sum(const GradSum A, const GradSum
     const GradSum &g = blockIdx.x < blocks_A ? A : B;
     const uint32_t ad = first + blockIdx.y, rank = ranks[ad], per_row = g.inner / 4;
     const uint64_t k = (uint64_t)(blockIdx.x < blocks_A ? blockIdx.x : blockIdx.x - blocks_A) * 256 + threadIdx.x;
+    parts::next_may_start();
+    parts::previous_done();
     if (k >= (uint64_t)g.rows * per_row) return;
     const uint32_t row = (uint32_t)(k / per_row), col = (uint32_t)(k % per_row) * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    parts::previous_done();
     if (row < (g.rank_rows ? rank : g.rows) && col < (g.rank_rows ? g.inner : rank)) {
         const uint32_t end = g.begin[ad + 1];
         const size_t step = (size_t)g.part_rows * g.part_inner;
@@ -1105,11 +1125,15 @@ int tensor_map(CUtensorMap *tm, uint32_t dtype, const void *p, uint64_t cols, ui
     return FIONA_OK;
 }
 
-// `boxes` of a row's columns in ranges, so that `units` of them make about
-// `want` CTAs
-Cut cut_columns(uint32_t boxes, uint32_t units, uint32_t want)
+// `boxes` of a row's columns in ranges, so that `units` of them make at most `want`
+// CTAs; where the ranges' partial sums are read by every CTA of the pass that follows
+// (r16 ranks, 0: they are not), no more than balances the two: a box takes a CTA
+// some 0.35 us and a range's partial sums of 128 rows some 0.008 us a rank (measured on
+// 256 rows: 64 ranges of one box took 35 us, 9 ranges 14).
+Cut cut_columns(uint32_t boxes, uint32_t units, uint32_t want, uint32_t r16)
 {
-    const uint32_t slabs = std::max(1u, std::min(boxes, want / std::max(units, 1u)));
+    uint32_t slabs = std::max(1u, std::min(boxes, want / std::max(units, 1u)));
+    if (r16) slabs = std::min(slabs, (uint32_t)std::ceil(std::sqrt(boxes * 0.35 / (0.008 * r16))));
     const uint32_t width = ceil_div(boxes, slabs);
     return Cut{width, ceil_div(boxes, width)};
 }
@@ -1120,8 +1144,8 @@ struct ForwardShape {
     ForwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t n_tiles) : r(b->r_max)
     {
         const uint32_t resident = 2 * (uint32_t)std::max(b->ctx->sm_count, 1);
-        shrink = cut_columns(ceil_div(d_in, 64), n_tiles, resident);
-        expand = cut_columns(ceil_div(d_out, 64), n_tiles, resident);
+        shrink = cut_columns(ceil_div(d_in, 64), n_tiles, resident, r.r16);
+        expand = cut_columns(ceil_div(d_out, 64), n_tiles, resident, 0);
     }
     uint64_t part_bytes(const fiona_adapter_batch *b) const
     {
@@ -1176,7 +1200,7 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     g.stages = stages_for(0, stage, 3);
     void *sargs[] = {&tx, &tA, &g};
     if (n_tiles && (rc = launch(k_shrink<T, false>, n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024,
-                                   s, false, sargs, "adapter shrink")))
+                                   s, sargs, "adapter shrink")))
         return rc;
     g.bare = b->d_bare;
     g.n_bare = b->n_bare;
@@ -1186,7 +1210,7 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     g.stages = stages_for(g.op_boxes * kBoxBytes, expand_stage(g.blocks), 3);
     void *eargs[] = {&tbase, &tB, &tout, &g};
     return launch(k_expand<T>, n_tiles * g.cut.slabs + b->n_bare, kExpandThreads,
-                  g.op_boxes * kBoxBytes + (size_t)g.stages * expand_stage(g.blocks) + 1024, s, n_tiles != 0, eargs,
+                  g.op_boxes * kBoxBytes + (size_t)g.stages * expand_stage(g.blocks) + 1024, s, eargs,
                   "adapter expand");
 }
 
@@ -1232,7 +1256,7 @@ struct BackwardShape {
     BackwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
         : r(b->r_max), apart(r.r16 > 64), shrink(b, d_out, r, apart ? 0 : 2 * r.r16), expand(b, d_in, r, 2 * kBlockCols)
     {
-        dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1)) : shrink.cut;
+        dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1), r.r16) : shrink.cut;
         part = 0;
         image = part + align_up((uint64_t)dh_cut.slabs * b->n_tokens * r.r16 * 4);
         dh_image = image + (uint64_t)b->n_tiles * r.boxes * kBoxBytes;
@@ -1277,8 +1301,8 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         void *iargs[] = {&g, &image, &ups, &most, (void *)&b->d_tile_begin};
         const dim3 iblocks(image_blocks(g.r16) * b->n_tiles);
         const bool any = b->n_tiles != 0;
-        if (any && !is_bf16<T>() && (rc = launch(k_image<T, false, true>, iblocks, 256, 0, s, false, iargs, "adapter image"))) return rc;
-        if (any && (rc = launch(k_image<T, false, false>, iblocks, 256, 0, s, !is_bf16<T>(), iargs, "adapter image"))) return rc;
+        if (any && !is_bf16<T>() && (rc = launch(k_image<T, false, true>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
+        if (any && (rc = launch(k_image<T, false, false>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
         if (any && f.apart) {
             const uint32_t stage = shrink_stage<true>(g.r16, g.blocks);
             g.cols = a.d_out;
@@ -1286,8 +1310,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
             g.cut = f.dh_cut;
             g.stages = stages_for(0, stage, 3);
             void *args[] = {&tdy, &tB, &g};
-            rc = launch(k_shrink<T, true>, b->n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024, s, true,
-                        args, "adapter dh");
+            rc = launch(k_shrink<T, true>, b->n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024, s, args, "adapter dh");
             if (rc) return rc;
         }
         g.with_dh = !f.apart;
@@ -1304,7 +1327,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.image = image;
         g.ups = ups;
         if (any && (rc = launch(k_shrink_grad<T>, f.shrink.chunks->count * g.cut.slabs, kGradThreads,
-                                2 * op + (size_t)g.stages * sstage + 1024, s, true, sargs, "adapter shrink_grad")))
+                                2 * op + (size_t)g.stages * sstage + 1024, s, sargs, "adapter shrink_grad")))
             return rc;
         // dh as an operand (its image in a place of its own: the next kernel starts
         // while this one reads)
@@ -1312,8 +1335,8 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         ups += b->n_tiles;
         g.part_in = g.part_out;
         g.slabs_in = f.dh_cut.slabs;
-        if (any && !is_bf16<T>() && (rc = launch(k_image<T, true, true>, iblocks, 256, 0, s, true, iargs, "adapter image"))) return rc;
-        if (any && (rc = launch(k_image<T, true, false>, iblocks, 256, 0, s, true, iargs, "adapter image"))) return rc;
+        if (any && !is_bf16<T>() && (rc = launch(k_image<T, true, true>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
+        if (any && (rc = launch(k_image<T, true, false>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
         g.image = image;
         g.ups = ups;
         g.bare = b->d_bare;
@@ -1326,10 +1349,11 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.tmem_cols = f.expand.tmem_cols;
         g.grad = reinterpret_cast<float *>(ws + f.grad_A);
         g.buffers = g.blocks == 1 ? 2 : 1;
-        g.stages = std::min(kMaxStages, (kSmemOne - g.buffers * op) / expand_grad_stage(g.r16));
+        const uint32_t estage = expand_grad_stage(g.r16, a.mask.level != 0);
+        g.stages = std::min(kMaxStages, (kSmemOne - g.buffers * op) / estage);
         void *eargs[] = {&tx, &tA, &tdx, &g};
         rc = launch(k_expand_grad<T>, g.n_chunks * g.cut.slabs + b->n_bare, kExpandGradThreads,
-                    g.buffers * op + (size_t)g.stages * expand_grad_stage(g.r16) + 1024, s, any, eargs, "adapter expand_grad");
+                    g.buffers * op + (size_t)g.stages * estage + 1024, s, eargs, "adapter expand_grad");
         if (rc) return rc;
     }
     const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_max, a.d_in, f.r.r16, a.d_in, 1};
@@ -1337,8 +1361,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
     const uint32_t blocks_A = ceil_div(a.r_max * (a.d_in / 4), 256), blocks_B = ceil_div(a.d_out * (a.r_max / 4), 256);
     for (uint32_t i = 0; i < a.n_adapters && rc == FIONA_OK; i += 65535) {
         void *args[] = {(void *)&A, (void *)&B, (void *)&a.ranks, (void *)&blocks_A, &i};
-        rc = launch(k_grad_sum<T>, dim3(blocks_A + blocks_B, std::min(a.n_adapters - i, 65535u)), 256, 0, s, b->n_tiles || b->n_bare,
-                    args, "adapter gradients");
+        rc = launch(k_grad_sum<T>, dim3(blocks_A + blocks_B, std::min(a.n_adapters - i, 65535u)), 256, 0, s, args, "adapter gradients");
     }
     return rc;
 }

@@ -304,3 +304,32 @@ def test_gradients_are_differences(ctx):
         want = float((grad.double() * step.double()).sum())
         # the step itself rounds once (keep + step), every sum as in `allowed`
         assert abs((loss[0] - loss[1]) / 2 - want) <= size * 2 * (96 + 72 + 300 + 16) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("starts,ids", [([0, 700, 900], [0, 1]), (list(range(41)), [i % 2 for i in range(40)])])
+def test_order_on_a_stream(ctx, dtype, starts, ids):
+    """A call follows what was queued before it, and what is queued after follows
+    the call: inputs that a slow kernel writes just before, and overwrites just after."""
+    pr = Problem(ctx, dtype, starts, ids, [16, 8], 16, 1024, 768, seed=3, p=0.1)
+    pr.forward()
+    pr.backward()
+    torch.cuda.synchronize()
+    first = [t.clone() for t in (pr.out, pr.h, pr.dx, pr.dA, pr.dB)]
+    inputs = [pr.x, pr.base, pr.dy, pr.dx_base, pr.A, pr.B]
+    good = [t.clone() for t in inputs]
+    slow = torch.randn(4096, 4096, device="cuda")
+    for _ in range(3):
+        for t in inputs + [pr.out, pr.h, pr.dx, pr.dA, pr.dB]:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        torch.mm(slow, slow)
+        for t, g in zip(inputs, good):
+            t.copy_(g)
+        pr.forward()
+        pr.backward()
+        for t in inputs:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for a, b in zip(first, (pr.out, pr.h, pr.dx, pr.dA, pr.dB)):
+            assert torch.equal(a, b)
