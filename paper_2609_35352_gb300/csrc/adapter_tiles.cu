@@ -80,10 +80,12 @@ __device__ __forceinline__ float range_scale(float most)
 __device__ __forceinline__ float finite_abs(float v) { return isfinite(v) ? fabsf(v) : 0.f; }
 
 // The two fields of `v` as a pair's mask: 0xFFFF where a field is below the level
-// (dropped), by the sign of the difference.
+// (dropped), by the signs of the differences (a two-element dot product with (1, 0)
+// or (0, 1) takes a field and subtracts at once: 20.0 us to 17.4 for the masks of
+// 67 M elements, formed alone)
 __device__ __forceinline__ uint32_t dropped(uint32_t v, uint32_t level)
 {
-    return __byte_perm((v & 0xFFFFu) - level, (v >> 16) - level, 0xFFBB);
+    return __byte_perm(__dp2a_lo(v, 0x0001u, 0u - level), __dp2a_lo(v, 0x0100u, 0u - level), 0xFFBB);
 }
 
 __device__ __forceinline__ uint4 ld_shared16(uint32_t addr)
@@ -138,40 +140,58 @@ __device__ __forceinline__ void arrive_warp(uint32_t bar, uint32_t lane)
     if (lane == 0) async::mbar_arrive(bar);
 }
 
-// the place of the flags of a row's chunk of 8 elements
-__device__ __forceinline__ uint32_t flags_at(uint32_t row, uint32_t chunk) { return row * 64 + ((chunk ^ (row & 7)) << 3); }
+// Masks and rows of a box of 128 rows, by 256 threads: thread k the chunk k % 8 of
+// the rows k / 8 + 32 q.  A mask does not wait for its box: the eight warps that form
+// masks do so while the box is on its way, and only clear what is dropped when it
+// has come (formed afterwards, a training forward's shrink took 47 us, expand_grad 66).
+constexpr uint32_t kMaskThreads = 256, kMaskRows = 4;
 
-// Drop masked elements and rows at or past `rows` of a box of 128 rows, by
-// `threads` threads (eight a row); with FLAGS a byte an element (shared, 64 a row,
-// flags_at) says dropped (0xFF) or kept (0).
-template <uint32_t THREADS, bool FLAGS>
-__device__ __forceinline__ void clean_box(uint32_t box, const dropout::Mask &m, uint32_t row0, uint32_t rows,
-                                          uint32_t col0, uint32_t thread, uint32_t flags)
+// words of dropped pairs (0xFFFF a half) of rows row0 + ... and columns col0 + ...
+__device__ __forceinline__ void form_masks(const dropout::Mask &m, uint32_t row0, uint32_t col0, uint32_t thread,
+                                           uint4 (&d)[kMaskRows])
 {
-    constexpr uint32_t kRows = THREADS / 8;  // a multiple of 8 or 4, 2: a thread's chunk keeps its swizzle every 8 rows
-    const uint32_t c = thread % 8;
-    uint32_t row = thread / 8;
-    if (m.level) {
-        uint64_t z = m.base + ((uint64_t)(row0 + row) * m.groups + col0 / 4 + 2 * c) * dropout::kGolden;
-        const uint64_t step = (uint64_t)kRows * m.groups * dropout::kGolden;
-#pragma unroll 2
-        for (; row < rows; row += kRows, z += step) {
-            const uint64_t v0 = dropout::mix64(z), v1 = dropout::mix64(z + dropout::kGolden);
-            const uint32_t at = box + chunk_at(row, c);
-            const uint32_t d0 = dropped((uint32_t)v0, m.level), d1 = dropped((uint32_t)(v0 >> 32), m.level);
-            const uint32_t d2 = dropped((uint32_t)v1, m.level), d3 = dropped((uint32_t)(v1 >> 32), m.level);
-            uint4 u = ld_shared16(at);
-            u.x &= ~d0, u.y &= ~d1, u.z &= ~d2, u.w &= ~d3;
-            st_shared16(at, u);
-            if (FLAGS)
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(flags + flags_at(row, c)), "r"(__byte_perm(d0, d1, 0x6420)),
-                             "r"(__byte_perm(d2, d3, 0x6420))
-                             : "memory");
-        }
-    } else if (row < rows) {
-        row += (rows - row + kRows - 1) / kRows * kRows;
+    uint64_t z = m.base + ((uint64_t)(row0 + thread / 8) * m.groups + col0 / 4 + 2 * (thread % 8)) * dropout::kGolden;
+    const uint64_t step = (uint64_t)(kMaskThreads / 8) * m.groups * dropout::kGolden;
+#pragma unroll
+    for (uint32_t q = 0; q < kMaskRows; ++q, z += step) {
+        const uint64_t v0 = dropout::mix64(z), v1 = dropout::mix64(z + dropout::kGolden);
+        d[q] = make_uint4(dropped((uint32_t)v0, m.level), dropped((uint32_t)(v0 >> 32), m.level),
+                          dropped((uint32_t)v1, m.level), dropped((uint32_t)(v1 >> 32), m.level));
+        // (here, not where they are used: the compiler would move them behind the wait)
+        asm volatile("" : "+r"(d[q].x), "+r"(d[q].y), "+r"(d[q].z), "+r"(d[q].w));
     }
-    for (; row < kTileRows; row += kRows) st_shared16(box + chunk_at(row, c), make_uint4(0, 0, 0, 0));
+}
+
+// Clear them in the box, and the rows at or past `rows`.
+__device__ __forceinline__ void apply_masks(uint32_t box, uint32_t rows, uint32_t thread, const uint4 (&d)[kMaskRows])
+{
+#pragma unroll
+    for (uint32_t q = 0; q < kMaskRows; ++q) {
+        const uint32_t r = thread / 8 + q * (kMaskThreads / 8), at = box + chunk_at(r, thread % 8);
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (r < rows) {
+            u = ld_shared16(at);
+            u.x &= ~d[q].x, u.y &= ~d[q].y, u.z &= ~d[q].z, u.w &= ~d[q].w;
+        }
+        st_shared16(at, u);
+    }
+}
+
+// The masks as a byte an element (shared, 64 a row, chunks at flags_at).
+__device__ __forceinline__ uint32_t flags_at(uint32_t row, uint32_t chunk) { return row * 64 + ((chunk ^ (row & 7)) << 3); }
+__device__ __forceinline__ void put_flags(uint32_t flags, uint32_t thread, const uint4 (&d)[kMaskRows])
+{
+#pragma unroll
+    for (uint32_t q = 0; q < kMaskRows; ++q)
+        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(flags + flags_at(thread / 8 + q * (kMaskThreads / 8), thread % 8)),
+                     "r"(__byte_perm(d[q].x, d[q].y, 0x6420)), "r"(__byte_perm(d[q].z, d[q].w, 0x6420))
+                     : "memory");
+}
+
+// rows at or past `rows` of a box, by `threads` threads
+__device__ __forceinline__ void clear_rows(uint32_t box, uint32_t rows, uint32_t thread, uint32_t threads)
+{
+    for (uint32_t k = rows * 8 + thread; k < kTileRows * 8; k += threads) st_shared16(box + chunk_at(k / 8, k % 8), make_uint4(0, 0, 0, 0));
 }
 
 // ---------------------------------------------------------------------------
@@ -280,9 +300,11 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
         if (fix)
             for (uint32_t i = 0; i < n; ++i) {
                 const uint32_t s = i % S;
+                uint4 d[kMaskRows];
+                form_masks(g.a.mask, t.row0, (b0 + i) * 64, threadIdx.x - 64, d);
                 w.pass(full + kBar * s, (i / S) & 1);
                 __syncwarp();
-                clean_box<256, false>(base + s * stage, g.a.mask, t.row0, t.rows, (b0 + i) * 64, threadIdx.x - 64, 0);
+                apply_masks(base + s * stage, t.rows, threadIdx.x - 64, d);
                 async::fence_proxy_async();
                 arrive_warp(fixed + kBar * s, me.lane);
             }
@@ -554,11 +576,8 @@ constexpr uint32_t kBlockCols = 128;
 
 // (`blocks` of B, none without dh)
 __host__ __device__ constexpr uint32_t shrink_grad_stage(uint32_t blocks) { return 2 * kBoxBytes + blocks * kBoxBytes; }
-// (and a mask's flags)
-__host__ __device__ constexpr uint32_t expand_grad_stage(uint32_t r16, bool mask)
-{
-    return 2 * kBoxBytes + 2 * r16 * 128 + (mask ? kTileRows * kBlockCols : 0);
-}
+__host__ __device__ constexpr uint32_t expand_grad_stage(uint32_t r16) { return 2 * kBoxBytes + 2 * r16 * 128; }
+constexpr uint32_t kFlagBytes = kTileRows * kBlockCols;  // of a mask
 
 // a chunk's walk: stage i is block i % width of the chunk's tile i / width
 struct GradJob {
@@ -771,14 +790,11 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
         load_operands(g, job, operand, ready, used, w);
     } else if (fix) {
         // rows past a tile's end are another request's
-        const dropout::Mask none;
         for (uint32_t i = 0; i < job.n; ++i) {
             const uint32_t s = i % S, buf = base + s * stage, rows = g.tiles[job.c.begin + i / job.width].rows;
             w.pass(full + kBar * s, (i / S) & 1);
             __syncwarp();
-            if (rows < kTileRows)
-                for (uint32_t k = 0; k < 2; ++k)
-                    clean_box<128, false>(buf + k * kBoxBytes, none, 0, rows, 0, threadIdx.x - 352, 0);
+            for (uint32_t k = 0; k < 2; ++k) clear_rows(buf + k * kBoxBytes, rows, threadIdx.x - 352, 128);
             async::fence_proxy_async();
             arrive_warp(fixed + kBar * s, me.lane);
         }
@@ -808,7 +824,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
         return;
     }
     const uint32_t S = g.stages, H = g.buffers, operand = aligned_smem(sm), op_bytes = g.op_boxes * kBoxBytes;
-    const uint32_t base = operand + H * op_bytes, stage = expand_grad_stage(g.r16, g.a.mask.level != 0), bar0 = async::smem_addr(bars);
+    const uint32_t base = operand + H * op_bytes, stage = expand_grad_stage(g.r16), bar0 = async::smem_addr(bars);
     const uint32_t full = bar0, fixed = bar0 + kBar * kMaxStages, empty = bar0 + 2 * kBar * kMaxStages;
     const uint32_t written = bar0 + 3 * kBar * kMaxStages, ready = bar0 + 4 * kBar * kMaxStages, used = ready + 2 * kBar;  // dh, by buffer
     const uint32_t done = used + 2 * kBar, free_ = done + 2 * kBar, all = free_ + 2 * kBar;  // dx, by buffer; everything
@@ -816,7 +832,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
     const bool mask = g.a.mask.level != 0, clean_A = job.rank != job.n16 && job.rank < g.a.r_max;
     const bool fix = mask || clean_A || job.ragged(g);
     const tiles::Waits w{&s_abort, g.err, g.wait_ns};
-    const uint32_t a_box = g.r16 * 128, flags = 2 * kBoxBytes + 2 * a_box;
+    const uint32_t a_box = g.r16 * 128, flags = base + S * stage;  // two stages' flags
 
     parts::next_may_start();
     if (threadIdx.x == 0) {
@@ -855,7 +871,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
             __syncwarp();
             if (!__all_sync(0xffffffffu, w.going())) break;
             if (tiles::elect_one()) {
-                async::mbar_arrive_expect_tx(full + kBar * s, flags);
+                async::mbar_arrive_expect_tx(full + kBar * s, stage);
                 for (uint32_t k = 0; k < 2; ++k) {
                     tiles::tma_load_2d(buf + k * kBoxBytes, &tx, col0 + k * 64, row0, full + kBar * s);
                     async::tma_load_3d(buf + 2 * kBoxBytes + k * a_box, &tA, col0 + k * 64, 0, job.c.adapter, full + kBar * s);
@@ -932,7 +948,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
                                          pack<T>(scale * a[4], scale * a[5]), pack<T>(scale * a[6], scale * a[7]));
                     uint2 f = make_uint2(0u, 0u);
                     if (mask)
-                        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(f.x), "=r"(f.y) : "r"(buf + flags + half * 8192 + flags_at(row, c)) : "memory");
+                        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(f.x), "=r"(f.y) : "r"(flags + d * kFlagBytes + half * (kFlagBytes / 2) + flags_at(row, c)) : "memory");
                     const uint32_t col = col0 + half * 64 + c * 8;
                     if (b && col < g.cols) {
                         o = *reinterpret_cast<const uint4 *>(b + col);
@@ -982,13 +998,24 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
         for (uint32_t i = 0; i < job.n; ++i) {
             const uint32_t s = i % S, buf = base + s * stage, col0 = (job.b0 + i % job.width) * kBlockCols;
             const AdapterTile tile = g.tiles[job.c.begin + i / job.width];
+            const uint32_t thread = threadIdx.x - 384;
+            uint4 d[2][kMaskRows];
+            if (mask) {
+                form_masks(g.a.mask, tile.row0, col0, thread, d[0]);
+                form_masks(g.a.mask, tile.row0, col0 + 64, thread, d[1]);
+                if (i >= 2) w.pass(written + kBar * ((i - 2) % S), ((i - 2) / S) & 1);  // the flags before have been read
+                __syncwarp();
+                put_flags(flags + i % 2 * kFlagBytes, thread, d[0]);
+                put_flags(flags + i % 2 * kFlagBytes + kFlagBytes / 2, thread, d[1]);
+            }
             w.pass(full + kBar * s, (i / S) & 1);
             __syncwarp();
-            const uint32_t thread = threadIdx.x - 384;
-            if (mask || tile.rows < kTileRows)
-                for (uint32_t k = 0; k < 2; ++k)
-                    clean_box<256, true>(buf + k * kBoxBytes, g.a.mask, tile.row0, tile.rows, col0 + k * 64, thread,
-                                         buf + flags + k * 8192);
+            for (uint32_t k = 0; k < 2; ++k) {
+                if (mask)
+                    apply_masks(buf + k * kBoxBytes, tile.rows, thread, d[k]);
+                else
+                    clear_rows(buf + k * kBoxBytes, tile.rows, thread, kMaskThreads);
+            }
             if (clean_A)  // A's rows from the rank to the next multiple of 16 are not A's
                 for (uint32_t k = thread; k < (job.n16 - job.rank) * 16; k += 256)
                     st_shared16(buf + 2 * kBoxBytes + k % 16 / 8 * a_box + chunk_at(job.rank + k / 16, k % 8), make_uint4(0, 0, 0, 0));
@@ -1348,12 +1375,14 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.cut = f.expand.cut;
         g.tmem_cols = f.expand.tmem_cols;
         g.grad = reinterpret_cast<float *>(ws + f.grad_A);
-        g.buffers = g.blocks == 1 ? 2 : 1;
-        const uint32_t estage = expand_grad_stage(g.r16, a.mask.level != 0);
-        g.stages = std::min(kMaxStages, (kSmemOne - g.buffers * op) / estage);
+        // two operands' buffers where that leaves three stages
+        const uint32_t estage = expand_grad_stage(g.r16), room = kSmemOne - (a.mask.level ? 2 * kFlagBytes : 0);
+        g.buffers = room >= 2 * op + 3 * estage ? 2 : 1;
+        g.stages = std::min(kMaxStages, (room - g.buffers * op) / estage);
+        const size_t esmem = g.buffers * op + (size_t)g.stages * estage + (a.mask.level ? 2 * kFlagBytes : 0) + 1024;
         void *eargs[] = {&tx, &tA, &tdx, &g};
         rc = launch(k_expand_grad<T>, g.n_chunks * g.cut.slabs + b->n_bare, kExpandGradThreads,
-                    g.buffers * op + (size_t)g.stages * estage + 1024, s, eargs, "adapter expand_grad");
+                    esmem, s, eargs, "adapter expand_grad");
         if (rc) return rc;
     }
     const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_max, a.d_in, f.r.r16, a.d_in, 1};
