@@ -220,7 +220,12 @@ __global__ void __launch_bounds__(kThreads) k_any_expand(const TileArgs g)
         for (uint32_t e = threadIdx.x; e < kRows * (kSlice / 4); e += kThreads) {
             const uint32_t r = e / (kSlice / 4), j = j0 + e % (kSlice / 4) * 4;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r < rows && j < rank) v = below(sum_parts(g, row0 + r, j), j, rank, by);
+            if (r < rows && j < rank) {
+                const int64_t at[1] = {(int64_t)((uint64_t)(row0 + r) * g.r16 + j)};
+                float4 s[1];
+                sum_parts(g, at, s);
+                v = below(s[0], j, rank, by);
+            }
             const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i) {

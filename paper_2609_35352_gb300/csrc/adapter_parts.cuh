@@ -21,18 +21,31 @@ using real::widen;
 __device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void previous_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Sum over column ranges of the partial h or dh of four ranks of a row.
-__device__ __forceinline__ float4 sum_parts(const TileArgs &g, uint32_t row, uint32_t j)
+// Sums over column ranges of the partial h or dh: N pieces of four ranks at once,
+// piece i at element at[i] of a range (none where that is negative), all of
+// their loads of four ranges under way.
+template <uint32_t N>
+__device__ __forceinline__ void sum_parts(const TileArgs &g, const int64_t (&at)[N], float4 (&s)[N])
 {
     const size_t step = (size_t)g.a.n_tokens * g.r16;
-    const float *p = g.part_in + (size_t)row * g.r16 + j;
-    float4 s = *reinterpret_cast<const float4 *>(p);
-#pragma unroll 4
-    for (uint32_t k = 1; k < g.slabs_in; ++k) {
-        const float4 v = *reinterpret_cast<const float4 *>(p + k * step);
-        s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) s[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float *p = g.part_in;
+    for (uint32_t k = 0; k < g.slabs_in; k += 4, p += 4 * step) {
+        float4 v[4][N];
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q)
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) {
+                v[q][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k + q < g.slabs_in && at[i] >= 0) v[q][i] = *reinterpret_cast<const float4 *>(p + q * step + at[i]);
+            }
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q)
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i)
+                s[i].x += v[q][i].x, s[i].y += v[q][i].y, s[i].z += v[q][i].z, s[i].w += v[q][i].w;
     }
-    return s;
 }
 
 __device__ __forceinline__ float4 below(float4 v, uint32_t j, uint32_t rank, float by)

@@ -345,11 +345,11 @@ constexpr uint32_t kExpandWorkers = 256;
 
 __host__ __device__ constexpr uint32_t expand_stage(uint32_t blocks) { return kBoxBytes + blocks * 64 * 128; }
 
-// A tile of `boxes` boxes out of shared memory, by one warp: by TMA where it has all
-// of its rows, else row by row (the rows behind are another request's); then its
-// stage is free.
+// A tile of `boxes` boxes out of shared memory, by one warp: by TMA, whole or (the
+// rows behind a request's last are another's) in eights of rows and the last few by
+// the lanes; then its stage is free.  `map`: boxes of 128 rows, `map8`: of 8.
 template <typename T>
-__device__ __forceinline__ void store_tile(const TileArgs &g, const CUtensorMap &map, const AdapterTile &t, uint32_t buf,
+__device__ __forceinline__ void store_tile(const TileArgs &g, const CUtensorMap &map, const CUtensorMap &map8, const AdapterTile &t, uint32_t buf,
                                            uint32_t col0, uint32_t boxes, uint32_t empty, uint32_t lane)
 {
     if (t.rows == kTileRows) {
@@ -360,8 +360,16 @@ __device__ __forceinline__ void store_tile(const TileArgs &g, const CUtensorMap 
             tiles::store_wait_read();
         }
     } else {
-        const uint32_t per = 8 * boxes;
-        for (uint32_t k = lane; k < t.rows * per; k += 32) {
+        const uint32_t whole = t.rows & ~7u, per = 8 * boxes;
+        if (lane == 0 && whole) {
+            for (uint32_t k = 0; k < boxes; ++k)
+                if (col0 + k * 64 < g.cols)
+                    for (uint32_t r = 0; r < whole; r += 8)
+                        tiles::tma_store_2d(&map8, col0 + k * 64, t.row0 + r, buf + k * kBoxBytes + r * 128);
+            tiles::store_commit();
+        }
+        __syncwarp();
+        for (uint32_t k = whole * per + lane; k < t.rows * per; k += 32) {
             const uint32_t r = k / per, c = k % per, col = col0 + c * 8;
             const uint4 v = ld_shared16(buf + c / 8 * kBoxBytes + chunk_at(r, c % 8));
             T *o = (T *)g.a.out + (uint64_t)(t.row0 + r) * g.a.ld_out + col;
@@ -374,14 +382,16 @@ __device__ __forceinline__ void store_tile(const TileArgs &g, const CUtensorMap 
             }
         }
         async::fence_proxy_async();
+        if (lane == 0 && whole) tiles::store_wait_read();
     }
     arrive_warp(empty, lane);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant__ CUtensorMap tbase,
+__global__ void __launch_bounds__(kExpandThreads, 2) k_expand(const __grid_constant__ CUtensorMap tbase,
                                                            const __grid_constant__ CUtensorMap tB,
-                                                           const __grid_constant__ CUtensorMap tout, const TileArgs g)
+                                                           const __grid_constant__ CUtensorMap tout,
+                                                           const __grid_constant__ CUtensorMap tout8, const TileArgs g)
 {
     extern __shared__ uint8_t sm[];
     __shared__ __align__(8) uint64_t bars[4 * kMaxStages + 5];
@@ -478,25 +488,38 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
         const uint32_t worker = threadIdx.x - 64, quarter = me.warp & 3, half = (me.warp - 2) / 4;
         // h: the sum of its parts, in two 16-bit parts (and whole, where wanted)
         parts::previous_done();
-        const uint32_t groups = n16 / 4;
+        const uint32_t groups = n16 / 4, pieces = kTileRows * groups;
+        constexpr uint32_t kAtOnce = 2;
+        auto hidden = [&](uint32_t k0, auto use) {
+            int64_t at[kAtOnce];
+            float4 v[kAtOnce];
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+                const uint32_t k = k0 + i * kExpandWorkers, row = k / groups, j = k % groups * 4;
+                at[i] = k < pieces && row < t.rows && j < rank ? (int64_t)((uint64_t)(t.row0 + row) * g.r16 + j) : -1;
+            }
+            sum_parts(g, at, v);
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+                const uint32_t k = k0 + i * kExpandWorkers, row = k / groups, j = k % groups * 4;
+                if (k < pieces) use(row, j, below(v[i], j, rank, g.a.mask.factor));
+            }
+        };
         float most = 0.f;
         if (!is_bf16<T>()) {
-            for (uint32_t k = worker; k < t.rows * groups; k += kExpandWorkers) {
-                const uint32_t j = k % groups * 4;
-                const float4 v = below(sum_parts(g, t.row0 + k / groups, j), j, rank, g.a.mask.factor);
-                most = fmaxf(most, fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
-            }
+            for (uint32_t k = worker; k < pieces; k += kAtOnce * kExpandWorkers)
+                hidden(k, [&](uint32_t, uint32_t, float4 v) {
+                    most = fmaxf(most, fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
+                });
             most = group_max(most, &s_most, 1, kExpandWorkers);
         }
         const float up = range_scale<T>(most), scale = g.a.scales[t.adapter] * (1.f / up);
-        for (uint32_t k = worker; k < kTileRows * groups; k += kExpandWorkers) {
-            const uint32_t row = k / groups, j = k % groups * 4;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (row < t.rows) v = below(sum_parts(g, t.row0 + row, j), j, rank, g.a.mask.factor);
-            if (g.a.h && slab == 0 && row < t.rows && j < g.a.r_max)
-                *reinterpret_cast<float4 *>(g.a.h + (size_t)(t.row0 + row) * g.a.r_max + j) = v;
-            put_parts<T>(operand, g.lo, row, j, make_float4(v.x * up, v.y * up, v.z * up, v.w * up));
-        }
+        for (uint32_t k = worker; k < pieces; k += kAtOnce * kExpandWorkers)
+            hidden(k, [&](uint32_t row, uint32_t j, float4 v) {
+                if (g.a.h && slab == 0 && row < t.rows && j < g.a.r_max)
+                    *reinterpret_cast<float4 *>(g.a.h + (size_t)(t.row0 + row) * g.a.r_max + j) = v;
+                put_parts<T>(operand, g.lo, row, j, make_float4(v.x * up, v.y * up, v.z * up, v.w * up));
+            });
         if (g.a.h && slab == 0)  // zero at and above the last block of ranks
             for (uint32_t k = worker; k < t.rows * ((g.a.r_max - min(n16, g.a.r_max)) / 4); k += kExpandWorkers) {
                 const uint32_t m = (g.a.r_max - min(n16, g.a.r_max)) / 4;
@@ -542,7 +565,7 @@ __global__ void __launch_bounds__(kExpandThreads) k_expand(const __grid_constant
             const uint32_t s = i % S;
             w.pass(written + kBar * s, (i / S) & 1);
             __syncwarp();
-            store_tile<T>(g, tout, t, base + s * stage, (b0 + i) * 64, 1, empty + kBar * s, me.lane);
+            store_tile<T>(g, tout, tout8, t, base + s * stage, (b0 + i) * 64, 1, empty + kBar * s, me.lane);
         }
     } else if (fix) {
         // B's columns from the rank to the next multiple of 16 are not B's
@@ -810,7 +833,8 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
 template <typename T>
 __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid_constant__ CUtensorMap tx,
                                                               const __grid_constant__ CUtensorMap tA,
-                                                              const __grid_constant__ CUtensorMap tdx, const TileArgs g)
+                                                              const __grid_constant__ CUtensorMap tdx,
+                                                                    const __grid_constant__ CUtensorMap tdx8, const TileArgs g)
 {
     extern __shared__ uint8_t sm[];
     __shared__ __align__(8) uint64_t bars[4 * kMaxStages + 9];
@@ -991,7 +1015,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
             const uint32_t s = i % S;
             w.pass(written + kBar * s, (i / S) & 1);
             __syncwarp();
-            store_tile<T>(g, tdx, g.tiles[job.c.begin + i / job.width], base + s * stage, (job.b0 + i % job.width) * kBlockCols, 2,
+            store_tile<T>(g, tdx, tdx8, g.tiles[job.c.begin + i / job.width], base + s * stage, (job.b0 + i % job.width) * kBlockCols, 2,
                           empty + kBar * s, me.lane);
         }
     } else if (fix) {
@@ -1051,10 +1075,15 @@ __global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image,
     __syncthreads();
     auto value = [&](uint32_t k) {
         const uint32_t r = r0 + k / groups, j = k % groups * 4;
-        if (r >= t.rows || j >= rank) return make_float4(0.f, 0.f, 0.f, 0.f);
-        return below(DH ? sum_parts(g, t.row0 + r, j)
-                        : *reinterpret_cast<const float4 *>(g.a.h_in + (size_t)(t.row0 + r) * g.a.r_max + j),
-                     j, rank, s_a);
+        float4 v[1] = {make_float4(0.f, 0.f, 0.f, 0.f)};
+        if (r >= t.rows || j >= rank) return v[0];
+        if (DH) {
+            const int64_t at[1] = {(int64_t)((uint64_t)(t.row0 + r) * g.r16 + j)};
+            sum_parts(g, at, v);
+        } else {
+            v[0] = *reinterpret_cast<const float4 *>(g.a.h_in + (size_t)(t.row0 + r) * g.a.r_max + j);
+        }
+        return below(v[0], j, rank, s_a);
     };
     float up = 1.f;
     if (!is_bf16<T>()) {
@@ -1213,12 +1242,13 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     g.part_out = static_cast<float *>(work);
     g.part_in = g.part_out;
     g.slabs_in = f.shrink.slabs;
-    CUtensorMap tx, tA, tbase, tB, tout;
+    CUtensorMap tx, tA, tbase, tB, tout, tout8;
     if ((rc = tensor_map(&tx, dtype, a.x, a.d_in, a.n_tokens, 0, a.ldx, kTileRows)) ||
         (rc = tensor_map(&tA, dtype, a.A, a.d_in, a.r_max, a.n_adapters, a.d_in, f.r.r16)) ||
         (rc = tensor_map(&tbase, dtype, a.base, a.d_out, a.n_tokens, 0, a.ld_base, kTileRows)) ||
         (rc = tensor_map(&tB, dtype, a.B, a.r_max, a.d_out, a.n_adapters, a.r_max, 64)) ||
-        (rc = tensor_map(&tout, dtype, a.out, a.d_out, a.n_tokens, 0, a.ld_out, kTileRows)))
+        (rc = tensor_map(&tout, dtype, a.out, a.d_out, a.n_tokens, 0, a.ld_out, kTileRows)) ||
+        (rc = tensor_map(&tout8, dtype, a.out, a.d_out, a.n_tokens, 0, a.ld_out, 8)))
         return rc;
     g.cut = f.shrink;
     g.cols = a.d_in;
@@ -1235,7 +1265,7 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     g.cols = a.d_out;
     g.boxes = ceil_div(a.d_out, 64);
     g.stages = stages_for(g.op_boxes * kBoxBytes, expand_stage(g.blocks), 3);
-    void *eargs[] = {&tbase, &tB, &tout, &g};
+    void *eargs[] = {&tbase, &tB, &tout, &tout8, &g};
     return launch(k_expand<T>, n_tiles * g.cut.slabs + b->n_bare, kExpandThreads,
                   g.op_boxes * kBoxBytes + (size_t)g.stages * expand_stage(g.blocks) + 1024, s, eargs,
                   "adapter expand");
@@ -1243,9 +1273,10 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
 
 // How one of the gradients' passes is cut: blocks of 128 columns a CTA, tiles a
 // chunk.  More columns a CTA: fewer partial dh; more tiles: fewer partial dB or dA;
-// both: fewer CTAs.  By a model of the pass in microseconds of one CTA an SM: 0.75
-// for a tile's block of 128 columns, half as much again for its operand; and the
-// partial sums at 5 TB/s.
+// both: fewer CTAs.  By a model of the pass in microseconds of one CTA an SM, fitted
+// to measured passes: 3 to begin and end, 1.1 for a tile's block of 128 columns (more
+// with the few stages that high ranks leave), 0.4 for its operand; and the partial
+// sums at 5 TB/s.
 struct GradCut {
     Cut cut{};
     const AdapterChunks *chunks = nullptr;
@@ -1261,7 +1292,8 @@ struct GradCut {
             for (const AdapterChunks &c : b->chunks) {
                 const uint32_t slabs = ceil_div(n, width);
                 const double waves = ceil_div(c.count * slabs, sms);
-                const double us = waves * (2.0 + c.size * (0.75 * width + 0.4) + 0.01 * width * r.r16) +
+                const double block = r.r16 <= 32 ? 1.1 : r.r16 <= 64 ? 1.6 : 2.4;
+                const double us = waves * (3.0 + c.size * (block * width + 0.4) + 0.01 * width * r.r16) +
                                   8.0 * c.count * (double)cols * r.r16 / 5e6 + (parts ? 8.0 : 0.0) * slabs * b->n_tokens * (double)r.r16 / 5e6;
                 if (!chunks || us < best) {
                     best = us;
@@ -1283,7 +1315,7 @@ struct BackwardShape {
     BackwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
         : r(b->r_max), apart(r.r16 > 64), shrink(b, d_out, r, apart ? 0 : 2 * r.r16), expand(b, d_in, r, 2 * kBlockCols)
     {
-        dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1), r.r16) : shrink.cut;
+        dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1), 0) : shrink.cut;
         part = 0;
         image = part + align_up((uint64_t)dh_cut.slabs * b->n_tokens * r.r16 * 4);
         dh_image = image + (uint64_t)b->n_tiles * r.boxes * kBoxBytes;
@@ -1313,12 +1345,13 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
     g.both = f.r.both;
         g.err = b->ctx->d_kerr;
         g.wait_ns = kWaitNs;
-        CUtensorMap tx, tA, tdy, tB, tdx;
+        CUtensorMap tx, tA, tdy, tB, tdx, tdx8;
         if ((rc = tensor_map(&tx, dtype, a.x, a.d_in, a.n_tokens, 0, a.ldx, kTileRows)) ||
             (rc = tensor_map(&tA, dtype, a.A, a.d_in, a.r_max, a.n_adapters, a.d_in, f.r.r16)) ||
             (rc = tensor_map(&tdy, dtype, a.dy, a.d_out, a.n_tokens, 0, a.ld_dy, kTileRows)) ||
             (rc = tensor_map(&tB, dtype, a.B, a.r_max, a.d_out, a.n_adapters, a.r_max, f.apart ? 64 : kBlockCols)) ||
-            (rc = tensor_map(&tdx, dtype, a.out, a.d_in, a.n_tokens, 0, a.ld_out, kTileRows)))
+            (rc = tensor_map(&tdx, dtype, a.out, a.d_in, a.n_tokens, 0, a.ld_out, kTileRows)) ||
+            (rc = tensor_map(&tdx8, dtype, a.out, a.d_in, a.n_tokens, 0, a.ld_out, 8)))
             return rc;
         const uint32_t op = g.op_boxes * kBoxBytes;
         g.part_out = reinterpret_cast<float *>(ws + f.part);
@@ -1380,7 +1413,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.buffers = room >= 2 * op + 3 * estage ? 2 : 1;
         g.stages = std::min(kMaxStages, (room - g.buffers * op) / estage);
         const size_t esmem = g.buffers * op + (size_t)g.stages * estage + (a.mask.level ? 2 * kFlagBytes : 0) + 1024;
-        void *eargs[] = {&tx, &tA, &tdx, &g};
+        void *eargs[] = {&tx, &tA, &tdx, &tdx8, &g};
         rc = launch(k_expand_grad<T>, g.n_chunks * g.cut.slabs + b->n_bare, kExpandGradThreads,
                     esmem, s, eargs, "adapter expand_grad");
         if (rc) return rc;
