@@ -10,6 +10,7 @@ the legacy default stream.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Any, Optional, Sequence
 
 import numpy as np
@@ -24,13 +25,10 @@ EXPORTED = ("fiona_adapter_batch_create", "fiona_adapter_batch_destroy", "fiona_
             "fiona_adapter_forward", "fiona_adapter_backward", "fiona_dropout")
 
 
-class _Layer(ctypes.Structure):
-    _fields_ = [("d_in", ctypes.c_uint32), ("d_out", ctypes.c_uint32), ("dtype", ctypes.c_uint32),
-                ("reserved", ctypes.c_uint32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p)]
-
-
-class _DropoutSpec(ctypes.Structure):
-    _fields_ = [("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("p", ctypes.c_double)]
+# fiona_adapter_layer and fiona_dropout_spec as bytes (a call on one token is its
+# marshalling for the most part: packing takes a quarter of a ctypes structure's time)
+_layer = struct.Struct("=IIIIQQ").pack
+_dropout_spec = struct.Struct("=QQd").pack
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -107,14 +105,14 @@ class Dropout:
     def __init__(self, p: float, seed: int, offset: int = 0):
         self.p, self.seed, self.offset = float(p), int(seed), int(offset)
         m = (1 << 64) - 1
-        self._spec = _DropoutSpec(self.seed & m, self.offset & m, self.p)
+        self._spec = _dropout_spec(self.seed & m, self.offset & m, self.p)
 
     def advance(self, rows: int, cols: int) -> "Dropout":
         return Dropout(self.p, self.seed, self.offset + rows * ((cols + 3) // 4))
 
 
-def _spec(d: Optional[Dropout]):
-    return None if d is None else ctypes.byref(d._spec)
+def _handle(stream: Any) -> int:
+    return 0 if stream is None else stream if type(stream) is int else stream.cuda_stream
 
 
 class Batch:
@@ -158,9 +156,10 @@ class Batch:
         if x.dim() != 2 or B.dim() != 3:
             raise ValueError("x [tokens][d_in] and B [adapters][d_out][r_max] expected")
         d_in, d_out, dev = x.shape[1], B.shape[1], self._dev
-        return d_in, d_out, _Layer(d_in, d_out, _dtype(x.dtype), 0,
-                                   _whole(A, (self.n_adapters, self.r_max, d_in), x.dtype, dev, "A"),
-                                   _whole(B, (self.n_adapters, d_out, self.r_max), x.dtype, dev, "B"))
+        dt = x.dtype
+        return d_in, d_out, _layer(d_in, d_out, _dtype(dt), 0,
+                                   _whole(A, (self.n_adapters, self.r_max, d_in), dt, dev, "A"),
+                                   _whole(B, (self.n_adapters, d_out, self.r_max), dt, dev, "B"))
 
     def forward(self, x, A, B, out, base=None, h=None, dropout: Optional[Dropout] = None, work=None,
                 stream=None) -> None:
@@ -170,14 +169,15 @@ class Batch:
         T, dt, dev = self.n_tokens, x.dtype, self._dev
         ldx = _matrix(x, (T, d_in), dt, dev, "x")
         ld_out = _matrix(out, (T, d_out), dt, dev, "out")
-        ld_base = 0 if base is None else _matrix(base, (T, d_out), dt, dev, "base")
+        ld_base, p_base = (0, None) if base is None else (_matrix(base, (T, d_out), dt, dev, "base"), base.data_ptr())
         ph = None if h is None else _whole(h, (T, self.r_max), torch.float32, dev, "h")
         if work is None:
             raise ValueError("forward needs a workspace (Batch.workspace)")
-        F._check(lib().fiona_adapter_forward(self.handle, F.stream_handle(stream), ctypes.byref(layer), x.data_ptr(),
-                                             ldx, F.addr(base), ld_base, out.data_ptr(), ld_out, ph, _spec(dropout),
-                                             work.data_ptr(), work.numel() * work.element_size()),
-                 "fiona_adapter_forward")
+        rc = lib().fiona_adapter_forward(self.handle, _handle(stream), layer, x.data_ptr(), ldx, p_base, ld_base,
+                                         out.data_ptr(), ld_out, ph, None if dropout is None else dropout._spec,
+                                         work.data_ptr(), work.nbytes)
+        if rc:
+            F._check(rc, "fiona_adapter_forward")
 
     def backward(self, x, h, dy, A, B, dx, dA, dB, dx_base=None, dropout: Optional[Dropout] = None, work=None,
                  stream=None) -> None:
@@ -188,16 +188,17 @@ class Batch:
         ldx = _matrix(x, (T, d_in), dt, dev, "x")
         ld_dy = _matrix(dy, (T, d_out), dt, dev, "dy")
         ld_dx = _matrix(dx, (T, d_in), dt, dev, "dx")
-        ld_base = 0 if dx_base is None else _matrix(dx_base, (T, d_in), dt, dev, "dx_base")
+        ld_base, p_base = (0, None) if dx_base is None else (_matrix(dx_base, (T, d_in), dt, dev, "dx_base"), dx_base.data_ptr())
         ph = _whole(h, (T, self.r_max), torch.float32, dev, "h")
-        pA = _whole(dA, tuple(A.shape), dt, dev, "dA")
-        pB = _whole(dB, tuple(B.shape), dt, dev, "dB")
+        pA = _whole(dA, A.shape, dt, dev, "dA")
+        pB = _whole(dB, B.shape, dt, dev, "dB")
         if work is None:
             raise ValueError("backward needs a workspace (Batch.workspace)")
-        F._check(lib().fiona_adapter_backward(self.handle, F.stream_handle(stream), ctypes.byref(layer), x.data_ptr(),
-                                              ldx, ph, dy.data_ptr(), ld_dy, F.addr(dx_base), ld_base, dx.data_ptr(),
-                                              ld_dx, pA, pB, _spec(dropout), work.data_ptr(),
-                                              work.numel() * work.element_size()), "fiona_adapter_backward")
+        rc = lib().fiona_adapter_backward(self.handle, _handle(stream), layer, x.data_ptr(), ldx, ph, dy.data_ptr(),
+                                          ld_dy, p_base, ld_base, dx.data_ptr(), ld_dx, pA, pB,
+                                          None if dropout is None else dropout._spec, work.data_ptr(), work.nbytes)
+        if rc:
+            F._check(rc, "fiona_adapter_backward")
 
     def close(self) -> None:
         if getattr(self, "handle", None):
@@ -220,9 +221,10 @@ def dropout(ctx: F.Context, x, out, drop: Dropout, residual=None, stream=None) -
     ldx = _matrix(x, shape, dt, dev, "x")
     ld_out = _matrix(out, shape, dt, dev, "out")
     ld_res = 0 if residual is None else _matrix(residual, shape, dt, dev, "residual")
-    F._check(lib().fiona_dropout(ctx.handle, F.stream_handle(stream), _dtype(dt), shape[0], shape[1],
-                                 x.data_ptr(), ldx, F.addr(residual), ld_res, out.data_ptr(), ld_out, _spec(drop)),
-             "fiona_dropout")
+    rc = lib().fiona_dropout(ctx.handle, _handle(stream), _dtype(dt), shape[0], shape[1], x.data_ptr(), ldx,
+                             None if residual is None else residual.data_ptr(), ld_res, out.data_ptr(), ld_out, drop._spec)
+    if rc:
+        F._check(rc, "fiona_dropout")
 
 
 def dropout_backward(ctx: F.Context, dy, dx, drop: Dropout, stream=None) -> None:

@@ -47,6 +47,8 @@ struct fiona_adapter_batch {
     uint32_t n_long = 0;
     const AdapterRows *d_rows = nullptr;
     uint32_t n_rows = 0, most_rows = 0;       // groups; the most rows of one
+    const uint32_t *d_idle = nullptr;         // adapters without tiles
+    uint32_t n_idle = 0;
     const AdapterTile *d_bare = nullptr;      // rows without an adapter, or with one of rank 0
     uint32_t n_bare = 0;
 };

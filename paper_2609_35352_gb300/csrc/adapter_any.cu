@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
 // columns: a thread 4 rows and the columns 16 apart.  The block of the first columns
 // leaves h or dh whole
 template <typename T, bool BACK>
-__global__ void __launch_bounds__(kThreads) k_any_expand(const TileArgs g)
+__global__ void __launch_bounds__(kThreads, 4) k_any_expand(const TileArgs g)
 {
     __shared__ __align__(16) float H[kSlice][kRows + kPad], S[kSlice][kCols + 1];
     next_may_start();
@@ -352,24 +352,33 @@ __device__ __forceinline__ void weight_grad(const TileArgs &g, uint32_t block, S
     }
     s.join(sm.sum);
     const float scale = INNER ? g.a.mask.factor : g.a.scales[ch.adapter];
-    for (uint32_t e = threadIdx.x; e < 64 * rank; e += kThreads) {
-        const uint32_t c = INNER ? e % 64 : e / rank, j = INNER ? e / 64 : e % rank;
+    const uint32_t ranks = g.direct ? g.a.r_max : rank;
+    for (uint32_t e = threadIdx.x; e < 64 * ranks; e += kThreads) {
+        const uint32_t c = INNER ? e % 64 : e / ranks, j = INNER ? e / 64 : e % ranks;
         if (col0 + c >= cols) continue;
-        const float v = sm.sum[c * (kRanks + 1) + j] * scale;
-        if (INNER)
+        const float v = j < rank ? sm.sum[c * (kRanks + 1) + j] * scale : 0.f;
+        if (g.direct) {
+            if (INNER)
+                ((T *)g.a.dA)[((size_t)ch.adapter * g.a.r_max + j) * cols + col0 + c] = narrow<T>(v);
+            else
+                ((T *)g.a.dB)[((size_t)ch.adapter * cols + col0 + c) * g.a.r_max + j] = narrow<T>(v);
+        } else if (INNER) {
             g.grad[((size_t)chunk * g.r16 + j) * cols + col0 + c] = v;
-        else
+        } else {
             g.grad_b[((size_t)chunk * cols + col0 + c) * g.r16 + j] = v;
+        }
     }
 }
 
 template <typename T, uint32_t NRG, uint32_t RPT>
-__global__ void __launch_bounds__(kThreads) k_any_grad(const TileArgs g, uint32_t blocks_A)
+__global__ void __launch_bounds__(kThreads) k_any_grad(const TileArgs g, uint32_t blocks_A, uint32_t blocks)
 {
     __shared__ __align__(16) Shared<NRG, RPT> sm;
     next_may_start();
     previous_done();
-    if (blockIdx.x < blocks_A)
+    if (blockIdx.x >= blocks)
+        idle_grads<T>(g.a, g.idle[blockIdx.x - blocks], kThreads);
+    else if (blockIdx.x < blocks_A)
         weight_grad<T, true, NRG, RPT>(g, blockIdx.x, sm);
     else
         weight_grad<T, false, NRG, RPT>(g, blockIdx.x - blocks_A, sm);
@@ -504,9 +513,13 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a,
     g.chunks = chunks.d_chunks;
     g.grad = reinterpret_cast<float *>(ws + f.grad_A);
     g.grad_b = reinterpret_cast<float *>(ws + f.grad_B);
-    uint32_t blocks_A = chunks.count * ceil_div(a.d_in, kCols), blocks_B = chunks.count * ceil_div(a.d_out, kCols);
-    void *gargs[] = {&g, &blocks_A};
-    if (any && (rc = launch(pick_grad<T>(a.r_max), blocks_A + blocks_B, kThreads, 0, s, gargs, "adapter weight gradients"))) return rc;
+    g.direct = any && chunks.count + b->n_idle == b->n_adapters;
+    g.idle = b->d_idle;
+    g.n_idle = g.direct ? b->n_idle : 0;
+    uint32_t blocks_A = chunks.count * ceil_div(a.d_in, kCols), blocks = blocks_A + chunks.count * ceil_div(a.d_out, kCols);
+    void *gargs[] = {&g, &blocks_A, &blocks};
+    if (any && (rc = launch(pick_grad<T>(a.r_max), blocks + g.n_idle, kThreads, 0, s, gargs, "adapter weight gradients"))) return rc;
+    if (g.direct) return rc;
     const GradSum A{g.grad, chunks.d_begin, a.dA, a.r_max, a.d_in, f.r16, a.d_in, 1};
     const GradSum B{g.grad_b, chunks.d_begin, a.dB, a.d_out, a.r_max, a.d_out, f.r16, 0};
     const uint32_t sum_A = (uint32_t)(((uint64_t)a.r_max * a.d_in + kThreads - 1) / kThreads);

@@ -193,6 +193,10 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         most = std::max(most, (uint32_t)by[a].size());
     }
     b->n_tiles = (uint32_t)tiles.size();
+    std::vector<uint32_t> idle;
+    for (uint32_t a = 0; a < n_adapters; ++a)
+        if (by[a].empty()) idle.push_back(a);
+    b->n_idle = (uint32_t)idle.size();
     b->n_bare = (uint32_t)bare.size();
     // runs shorter than kShortRun in groups of an adapter's rows
     std::vector<AdapterTile> longer;
@@ -252,6 +256,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         const size_t o_tile_begin = put(tile_begin.data(), tile_begin.size() * 4);
         const size_t o_long = put(longer.data(), longer.size() * sizeof(AdapterTile));
         const size_t o_rows = put(rows.data(), rows.size() * sizeof(AdapterRows));
+        const size_t o_idle = put(idle.data(), idle.size() * 4);
         const size_t o_bare = put(bare.data(), bare.size() * sizeof(AdapterTile));
         std::vector<std::pair<size_t, size_t>> o_chunks;
         for (const auto &c : chunks)
@@ -266,6 +271,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         b->d_tile_begin = reinterpret_cast<const uint32_t *>(d + o_tile_begin);
         b->d_long = reinterpret_cast<const AdapterTile *>(d + o_long);
         b->d_rows = reinterpret_cast<const AdapterRows *>(d + o_rows);
+        b->d_idle = reinterpret_cast<const uint32_t *>(d + o_idle);
         b->d_bare = reinterpret_cast<const AdapterTile *>(d + o_bare);
         for (size_t i = 0; i < o_chunks.size(); ++i) {
             b->chunks[i].d_chunks = reinterpret_cast<const AdapterChunk *>(d + o_chunks[i].first);

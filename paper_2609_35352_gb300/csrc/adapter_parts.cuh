@@ -76,6 +76,15 @@ __device__ void bare_rows(const AdapterArgs &a, const AdapterTile t, uint32_t co
         for (uint32_t k = threadIdx.x; k < t.rows * a.r_max; k += threads) a.h[(uint64_t)t.row0 * a.r_max + k] = 0.f;
 }
 
+// the gradients of an adapter without rows, by a CTA of `threads`
+template <typename T>
+__device__ void idle_grads(const AdapterArgs &a, uint32_t ad, uint32_t threads)
+{
+    const size_t nA = (size_t)a.r_max * a.d_in, nB = (size_t)a.r_max * a.d_out;
+    for (size_t i = threadIdx.x; i < nA; i += threads) ((T *)a.dA)[ad * nA + i] = narrow<T>(0.f);
+    for (size_t i = threadIdx.x; i < nB; i += threads) ((T *)a.dB)[ad * nB + i] = narrow<T>(0.f);
+}
+
 // dA and dB of every adapter: its chunks' sums added up in order, zero where
 // there are none and outside the rank.
 struct GradSum {

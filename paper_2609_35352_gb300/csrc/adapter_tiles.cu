@@ -798,14 +798,26 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
         for (uint32_t j = 0; j < job.width; ++j) {
             const uint32_t col = (job.b0 + j) * kBlockCols + row;
             float *p = g.grad + ((size_t)job.chunk * g.cols + col) * g.r16;
-            for (uint32_t c = half * 16; c < job.n16; c += 32) {
+            T *o = (T *)g.a.dB + ((size_t)job.c.adapter * g.cols + col) * g.a.r_max;
+            for (uint32_t c = half * 16; c < (g.direct ? g.r16 : job.n16); c += 32) {
                 float v[16];
-                ld_both(acc + ((quarter * 32) << 16) + j * wide + c, g, v);
-                if (col < g.cols)
+                if (c < job.n16) {
+                    ld_both(acc + ((quarter * 32) << 16) + j * wide + c, g, v);
+                } else {
 #pragma unroll
-                    for (uint32_t k = 0; k < 16; k += 4)
-                        *reinterpret_cast<float4 *>(p + c + k) =
-                            make_float4(v[k] * scale, v[k + 1] * scale, v[k + 2] * scale, v[k + 3] * scale);
+                    for (uint32_t k = 0; k < 16; ++k) v[k] = 0.f;
+                }
+                if (col >= g.cols) continue;
+#pragma unroll
+                for (uint32_t k = 0; k < 16; k += 4) {
+                    const float4 x = make_float4(v[k] * scale, v[k + 1] * scale, v[k + 2] * scale, v[k + 3] * scale);
+                    if (!g.direct) {
+                        *reinterpret_cast<float4 *>(p + c + k) = x;
+                    } else if (c + k < g.a.r_max) {  // (ranks come in eights)
+                        const float4 y = below(x, c + k, job.rank, 1.f);
+                        *reinterpret_cast<uint2 *>(o + c + k) = make_uint2(pack<T>(y.x, y.y), pack<T>(y.z, y.w));
+                    }
+                }
             }
         }
         tcs::fence_before();
@@ -845,6 +857,12 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
         parts::next_may_start();
         parts::previous_done();
         bare_rows<T>(g.a, g.bare[blockIdx.x], g.cols, kExpandGradThreads);
+        return;
+    }
+    if (blockIdx.x >= g.n_bare + g.n_chunks * g.cut.slabs) {
+        parts::next_may_start();
+        parts::previous_done();
+        idle_grads<T>(g.a, g.idle[blockIdx.x - g.n_bare - g.n_chunks * g.cut.slabs], kExpandGradThreads);
         return;
     }
     const uint32_t S = g.stages, H = g.buffers, operand = aligned_smem(sm), op_bytes = g.op_boxes * kBoxBytes;
@@ -999,12 +1017,23 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
         for (uint32_t j = 0; j < job.width; ++j) {
             const uint32_t col = (job.b0 + j) * kBlockCols + row;
             float *p = g.grad + (size_t)job.chunk * g.r16 * g.cols + col;
-            for (uint32_t c = half * 16; c < job.n16; c += 32) {
+            T *o = (T *)g.a.dA + (size_t)job.c.adapter * g.a.r_max * g.cols + col;
+            for (uint32_t c = half * 16; c < (g.direct ? g.r16 : job.n16); c += 32) {
                 float v[16];
-                ld_both(tmem + ((quarter * 32) << 16) + 2 * kBlockCols + j * (g.both ? g.both : g.r16) + c, g, v);
-                if (col < g.cols)
+                if (c < job.n16) {
+                    ld_both(tmem + ((quarter * 32) << 16) + 2 * kBlockCols + j * (g.both ? g.both : g.r16) + c, g, v);
+                } else {
 #pragma unroll
-                    for (uint32_t k = 0; k < 16; ++k) p[(size_t)(c + k) * g.cols] = v[k] * scale;
+                    for (uint32_t k = 0; k < 16; ++k) v[k] = 0.f;
+                }
+                if (col >= g.cols) continue;
+#pragma unroll
+                for (uint32_t k = 0; k < 16; ++k) {
+                    if (!g.direct)
+                        p[(size_t)(c + k) * g.cols] = v[k] * scale;
+                    else if (c + k < g.a.r_max)
+                        o[(size_t)(c + k) * g.cols] = narrow<T>(c + k < job.rank ? v[k] * scale : 0.f);
+                }
             }
         }
         tcs::fence_before();
@@ -1275,8 +1304,8 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
 // chunk.  More columns a CTA: fewer partial dh; more tiles: fewer partial dB or dA;
 // both: fewer CTAs.  By a model of the pass in microseconds of one CTA an SM, fitted
 // to measured passes: 3 to begin and end, 1.1 for a tile's block of 128 columns (more
-// with the few stages that high ranks leave), 0.4 for its operand; and the partial
-// sums at 5 TB/s.
+// with the few stages that high ranks leave), 0.4 for its operand; the partial sums
+// at 5 TB/s, and 2.5 for adding the chunks' up, where an adapter has several.
 struct GradCut {
     Cut cut{};
     const AdapterChunks *chunks = nullptr;
@@ -1287,6 +1316,7 @@ struct GradCut {
         const uint32_t wide = r.both ? r.both : r.r16;
         const uint32_t most = std::min({n, 4u, (512 - fixed) / wide});
         const bool parts = fixed == 2 * r.r16;
+        const uint32_t active = b->n_adapters - b->n_idle;
         double best = 0;
         for (uint32_t width = most; width >= 1; --width)
             for (const AdapterChunks &c : b->chunks) {
@@ -1294,7 +1324,7 @@ struct GradCut {
                 const double waves = ceil_div(c.count * slabs, sms);
                 const double block = r.r16 <= 32 ? 1.1 : r.r16 <= 64 ? 1.6 : 2.4;
                 const double us = waves * (3.0 + c.size * (block * width + 0.4) + 0.01 * width * r.r16) +
-                                  8.0 * c.count * (double)cols * r.r16 / 5e6 + (parts ? 8.0 : 0.0) * slabs * b->n_tokens * (double)r.r16 / 5e6;
+                                  (c.count > active ? 2.5 + 8.0 * c.count * (double)cols * r.r16 / 5e6 : 0.0) + (parts ? 8.0 : 0.0) * slabs * b->n_tokens * (double)r.r16 / 5e6;
                 if (!chunks || us < best) {
                     best = us;
                     chunks = &c;
@@ -1309,6 +1339,7 @@ struct GradCut {
 struct BackwardShape {
     RankShape r;
     bool apart;  // dh by a pass of its own
+    bool direct = false;  // one chunk an adapter in both passes
     Cut dh_cut{};
     GradCut shrink, expand;
     uint64_t part, image, dh_image, grad_A, grad_B, most, ups, bytes;  // offsets in the workspace
@@ -1316,6 +1347,7 @@ struct BackwardShape {
         : r(b->r_max), apart(r.r16 > 64), shrink(b, d_out, r, apart ? 0 : 2 * r.r16), expand(b, d_in, r, 2 * kBlockCols)
     {
         dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1), 0) : shrink.cut;
+        direct = shrink.chunks->count + b->n_idle == b->n_adapters && expand.chunks->count + b->n_idle == b->n_adapters;
         part = 0;
         image = part + align_up((uint64_t)dh_cut.slabs * b->n_tokens * r.r16 * 4);
         dh_image = image + (uint64_t)b->n_tiles * r.boxes * kBoxBytes;
@@ -1374,6 +1406,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
             if (rc) return rc;
         }
         g.with_dh = !f.apart;
+        g.direct = f.direct;
         g.chunks = f.shrink.chunks->d_chunks;
         g.cols = a.d_out;
         g.boxes = ceil_div(a.d_out, kBlockCols);
@@ -1402,6 +1435,8 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.bare = b->d_bare;
         g.n_bare = b->n_bare;
         g.n_chunks = f.expand.chunks->count;
+        g.idle = b->d_idle;
+        g.n_idle = f.direct ? b->n_idle : 0;
         g.chunks = f.expand.chunks->d_chunks;
         g.cols = a.d_in;
         g.boxes = ceil_div(a.d_in, kBlockCols);
@@ -1414,9 +1449,9 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.stages = std::min(kMaxStages, (room - g.buffers * op) / estage);
         const size_t esmem = g.buffers * op + (size_t)g.stages * estage + (a.mask.level ? 2 * kFlagBytes : 0) + 1024;
         void *eargs[] = {&tx, &tA, &tdx, &tdx8, &g};
-        rc = launch(k_expand_grad<T>, g.n_chunks * g.cut.slabs + b->n_bare, kExpandGradThreads,
+        rc = launch(k_expand_grad<T>, g.n_chunks * g.cut.slabs + b->n_bare + g.n_idle, kExpandGradThreads,
                     esmem, s, eargs, "adapter expand_grad");
-        if (rc) return rc;
+        if (rc || f.direct) return rc;
     }
     const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_max, a.d_in, f.r.r16, a.d_in, 1};
     const GradSum B{reinterpret_cast<const float *>(ws + f.grad_B), f.shrink.chunks->d_begin, a.dB, a.d_out, a.r_max, a.d_out, f.r.r16, 0};

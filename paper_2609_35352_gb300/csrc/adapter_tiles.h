@@ -52,6 +52,9 @@ struct TileArgs {
     uint32_t with_dh;      // shrink_grad: whether it makes the partial dh
     float *grad;           // [chunks][...] partial dB or dA
     float *grad_b, *dh;    // (adapter_any.cu: dB beside dA; dh whole, [n_tokens][r16])
+    uint32_t direct;       // every adapter has one chunk: dA and dB are written as they are
+    const uint32_t *idle;  // direct: adapters without tiles, whose gradients are zero
+    uint32_t n_idle;
     uint32_t n_tiles, n_chunks, stages, buffers, tmem_cols;
     int *err;
     uint64_t wait_ns;

@@ -24,6 +24,21 @@ def ctx():
     return F.Context(1024, W.ntt_primes(1024, 40, 1), device=F.FIONA_DEVICE_NONE)
 
 
+class Layer(ctypes.Structure):  # fiona_adapter_layer
+    _fields_ = [("d_in", ctypes.c_uint32), ("d_out", ctypes.c_uint32), ("dtype", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p)]
+
+
+class DropoutSpec(ctypes.Structure):  # fiona_dropout_spec
+    _fields_ = [("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("p", ctypes.c_double)]
+
+
+def test_packed_structures():
+    """The binding's packed arguments are the header's structures."""
+    assert AD._layer(3, 5, 2, 0, 1 << 40, 7) == bytes(Layer(3, 5, 2, 0, 1 << 40, 7))
+    assert AD.Dropout(0.25, -1, 1 << 63)._spec == bytes(DropoutSpec((1 << 64) - 1, 1 << 63, 0.25))
+
+
 def test_exports(ctx):
     text = open(os.path.join(ROOT, "include", "fiona_adapter.h")).read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
@@ -81,8 +96,8 @@ class Call:
         self.p = {k: (v.ctypes.data + 15) // 16 * 16 for k, v in self.keep.items()}
         self.ld = {"x": d_in, "base": d_out, "out": d_out, "dy": d_out, "dx_base": d_in, "dx": d_in}
         self.work_bytes = size
-        self.layer = AD._Layer(d_in, d_out, 2, 0, 0, 0)
-        self.spec = AD._DropoutSpec(1, 2, 0.5)
+        self.layer = Layer(d_in, d_out, 2, 0, 0, 0)
+        self.spec = DropoutSpec(1, 2, 0.5)
 
     def __call__(self):
         p, ld = self.p, self.ld
@@ -169,7 +184,7 @@ def test_dropout_refused(ctx):
     L = AD.lib()
     buf = np.zeros(4096, np.uint8)
     at = (buf.ctypes.data + 15) // 16 * 16
-    spec = AD._DropoutSpec(1, 2, 0.5)
+    spec = DropoutSpec(1, 2, 0.5)
 
     def call(dtype=2, rows=4, cols=8, x=at, ldx=8, res=None, ldr=0, out=at + 1024, ldo=8, s=spec, c=ctx.handle):
         return L.fiona_dropout(c, None, dtype, rows, cols, x, ldx, res, ldr, out, ldo, None if s is None else ctypes.byref(s))
@@ -179,7 +194,7 @@ def test_dropout_refused(ctx):
     assert call(rows=0) == F.FIONA_OK
     bad = [dict(dtype=3), dict(cols=0), dict(x=None), dict(out=None), dict(x=at + 1), dict(ldo=7), dict(out=at + 16),
            dict(res=at + 1024 + 16, ldr=8), dict(s=None), dict(c=None), dict(rows=1 << 40), dict(out=at, ldo=9),
-           dict(s=AD._DropoutSpec(1, 2, float("nan"))), dict(s=AD._DropoutSpec(1, 2, -1.0))]
+           dict(s=DropoutSpec(1, 2, float("nan"))), dict(s=DropoutSpec(1, 2, -1.0))]
     for b in bad:
         assert call(**b) == ARG, b
 
