@@ -42,11 +42,15 @@ struct fiona_adapter_batch {
     uint32_t n_tiles = 0;
     std::vector<AdapterChunks> chunks;        // rising sizes, from 1 to the most tiles an adapter has
     const uint32_t *d_tile_begin = nullptr;   // [n_adapters + 1] into d_tiles
-    // the same rows, those in short runs apart (adapter_rows.cu)
-    const AdapterTile *d_long = nullptr;
-    uint32_t n_long = 0;
+    // The same rows for the forward pass: tiles of runs of more than a tile first, then
+    // those of runs of kFewRows or more, then the rest; and the runs of a tile or less
+    // as groups of rows, those below kFewRows first.  A call takes one of three splits.
+    const AdapterTile *d_forward = nullptr;
     const AdapterRows *d_rows = nullptr;
-    uint32_t n_rows = 0, most_rows = 0;       // groups; the most rows of one
+    struct Split {
+        uint32_t tiles = 0, groups = 0, most = 0;  // of d_forward and d_rows; the most rows of a group
+    };
+    Split split[3];  // all tiles; the runs below kFewRows as groups; every run of a tile or less
     const uint32_t *d_idle = nullptr;         // adapters without tiles
     uint32_t n_idle = 0;
     const AdapterTile *d_bare = nullptr;      // rows without an adapter, or with one of rank 0
@@ -68,24 +72,28 @@ struct AdapterArgs {
 };
 
 // adapter_any.cu: any type and alignment, on the FMA units; its workspace; the
-// passes (only_long: without the short runs)
+// passes (forward: on the first n_tiles of d_forward, and their time by a model)
 uint64_t adapter_any_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
+double adapter_any_us(const fiona_adapter_batch *b, uint32_t n_tiles, uint32_t d_in, uint32_t d_out);
 int launch_adapter_any_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,
-                               bool only_long);
+                               uint32_t n_tiles);
 int launch_adapter_any_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
 
-// adapter_rows.cu: the forward pass on the short runs of rows, any type and alignment
-bool adapter_rows_apply(const fiona_adapter_batch *b, uint32_t d_in);
-int launch_adapter_rows(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a);
+// adapter_rows.cu: the forward pass on groups of rows, any type and alignment
+constexpr uint32_t kFewRows = 16;
+bool adapter_rows_apply(const fiona_adapter_batch::Split &s, uint32_t d_in);
+double adapter_rows_us(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &s, uint32_t d_in, uint32_t d_out);
+int launch_adapter_rows(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &s, void *stream, uint32_t dtype,
+                        const AdapterArgs &a);
 
-// adapter_tiles.cu: 16-bit types on the tensor cores.  Whether buffers of this
-// shape and alignment go there (rows is false where a pointer or stride is not a
-// multiple of 16 bytes); its workspace; the passes.
+// adapter_tiles.cu: 16-bit types on the tensor cores.  Whether layers of these
+// sizes go there (if TMA can address their rows); its workspace; the passes, as above.
 int adapter_tiles_configure();  // on the current device
 bool adapter_tiles_apply(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t dtype);
 uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
 int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,
-                                 bool only_long);
+                                 uint32_t n_tiles);
+double adapter_tiles_us(const fiona_adapter_batch *b, uint32_t n_tiles, uint32_t d_in, uint32_t d_out);
 int launch_adapter_tiles_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
 
 // dropout.cu

@@ -448,8 +448,8 @@ struct AnyShape {
     uint64_t part = 0, dh = 0, grad_A = 0, grad_B = 0, bytes = 0;
     AnyShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) : r16((b->r_max + 15) & ~15u)
     {
-        const uint32_t slabs = std::max({shrink_cut(b, d_in, b->n_tiles).slabs, shrink_cut(b, d_out, b->n_tiles).slabs,
-                                         shrink_cut(b, d_in, b->n_long).slabs});
+        uint32_t slabs = shrink_cut(b, d_out, b->n_tiles).slabs;
+        for (const auto &s : b->split) slabs = std::max(slabs, shrink_cut(b, d_in, s.tiles).slabs);
         const uint32_t chunks = grad_chunks(b, d_in, d_out).count;
         dh = part + align_up((uint64_t)slabs * b->n_tokens * r16 * 4);
         grad_A = dh + align_up((uint64_t)b->n_tokens * r16 * 4);
@@ -459,12 +459,12 @@ struct AnyShape {
 };
 
 template <typename T>
-int forward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a, void *work, bool only_long)
+int forward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a, void *work, uint32_t n_tiles)
 {
     TileArgs g{};
     g.a = a;
-    g.tiles = only_long ? b->d_long : b->d_tiles;
-    g.n_tiles = only_long ? b->n_long : b->n_tiles;
+    g.tiles = b->d_forward;
+    g.n_tiles = n_tiles;
     g.r16 = AnyShape(b, a.d_in, a.d_out).r16;
     g.part_out = static_cast<float *>(work);
     g.part_in = g.part_out;
@@ -536,13 +536,21 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a,
 
 uint64_t adapter_any_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) { return AnyShape(b, d_in, d_out).bytes; }
 
+// as adapter_tiles_us
+double adapter_any_us(const fiona_adapter_batch *b, uint32_t n_tiles, uint32_t d_in, uint32_t d_out)
+{
+    if (!n_tiles) return 0;
+    const double r = b->r_max, d = (double)d_in + d_out;
+    return 7.0 + 0.14 * r + d * (4e-4 + 1.4e-5 * r) + (n_tiles - 1) * (0.15 + d * (0.8e-4 + 3e-6 * r));
+}
+
 int launch_adapter_any_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,
-                               bool only_long)
+                               uint32_t n_tiles)
 {
     cudaStream_t s = (cudaStream_t)stream;
-    return dtype == FIONA_F32   ? forward<float>(b, s, a, work, only_long)
-           : dtype == FIONA_F16 ? forward<__half>(b, s, a, work, only_long)
-                                : forward<__nv_bfloat16>(b, s, a, work, only_long);
+    return dtype == FIONA_F32   ? forward<float>(b, s, a, work, n_tiles)
+           : dtype == FIONA_F16 ? forward<__half>(b, s, a, work, n_tiles)
+                                : forward<__nv_bfloat16>(b, s, a, work, n_tiles);
 }
 
 int launch_adapter_any_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work)

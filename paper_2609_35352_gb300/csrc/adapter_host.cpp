@@ -15,7 +15,6 @@ namespace {
 constexpr uint64_t kMaxTokens = 1ull << 26;
 constexpr uint32_t kMaxWidth = 1u << 20;
 constexpr uint32_t kMaxAdapters = 1u << 20;
-constexpr uint32_t kShortRun = 16;  // rows; below: groups of rows
 constexpr uint32_t kBareRows = 4;   // rows without an adapter that a CTA copies
 
 int cuda_fail(cudaError_t e, const char *what)
@@ -198,31 +197,44 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         if (by[a].empty()) idle.push_back(a);
     b->n_idle = (uint32_t)idle.size();
     b->n_bare = (uint32_t)bare.size();
-    // runs shorter than kShortRun in groups of an adapter's rows
-    std::vector<AdapterTile> longer;
-    std::vector<AdapterRows> rows;
+    // the forward pass's tiles and groups of rows (fiona_adapter_batch)
+    std::vector<AdapterTile> ordered[3];
+    std::vector<AdapterRows> groups[2];
+    uint32_t most_rows[2] = {};
     for (uint32_t a = 0; a < n_adapters; ++a) {
-        AdapterRows group{a, 0, {}};
+        AdapterRows open[2] = {{a, 0, {}}, {a, 0, {}}};
         for (size_t k = 0; k < by[a].size(); ++k) {
             const AdapterTile &t = by[a][k];
-            const bool starts = k == 0 || by[a][k - 1].row0 + by[a][k - 1].rows != t.row0;
-            if (t.rows >= kShortRun || !starts) {
-                longer.push_back(t);
-                continue;
-            }
+            const bool alone = (k == 0 || by[a][k - 1].row0 + by[a][k - 1].rows != t.row0) &&
+                               (k + 1 == by[a].size() || t.row0 + t.rows != by[a][k + 1].row0);
+            const int kind = !alone ? 0 : t.rows >= kFewRows ? 1 : 2;
+            ordered[kind].push_back(t);
+            if (kind == 0) continue;
+            const int g = kind == 2 ? 0 : 1;
             for (uint32_t r = t.row0; r < t.row0 + t.rows; ++r) {
-                group.row[group.count++] = r;
-                b->most_rows = std::max(b->most_rows, group.count);
-                if (group.count == kAdapterRows) {
-                    rows.push_back(group);
-                    group.count = 0;
+                open[g].row[open[g].count++] = r;
+                most_rows[g] = std::max(most_rows[g], open[g].count);
+                if (open[g].count == kAdapterRows) {
+                    groups[g].push_back(open[g]);
+                    open[g].count = 0;
                 }
             }
         }
-        if (group.count) rows.push_back(group);
+        for (int g = 0; g < 2; ++g)
+            if (open[g].count) groups[g].push_back(open[g]);
     }
-    b->n_long = (uint32_t)longer.size();
-    b->n_rows = (uint32_t)rows.size();
+    b->split[0].tiles = b->n_tiles;
+    b->split[1].tiles = (uint32_t)(ordered[0].size() + ordered[1].size());
+    b->split[2].tiles = (uint32_t)ordered[0].size();
+    b->split[1].groups = (uint32_t)groups[0].size();
+    b->split[2].groups = (uint32_t)(groups[0].size() + groups[1].size());
+    b->split[1].most = most_rows[0];
+    b->split[2].most = std::max(most_rows[0], most_rows[1]);
+    std::vector<AdapterTile> &in_order = ordered[0];
+    in_order.insert(in_order.end(), ordered[1].begin(), ordered[1].end());
+    in_order.insert(in_order.end(), ordered[2].begin(), ordered[2].end());
+    std::vector<AdapterRows> &rows = groups[0];
+    rows.insert(rows.end(), groups[1].begin(), groups[1].end());
     // the tiles in chunks of several sizes, and where each adapter's begin
     std::vector<std::pair<std::vector<AdapterChunk>, std::vector<uint32_t>>> chunks;
     for (uint32_t size = 1;; size += std::max(1u, size / 4)) {
@@ -254,7 +266,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         const size_t o_scales = put(s.data(), n_adapters * 4ull);
         const size_t o_tiles = put(tiles.data(), tiles.size() * sizeof(AdapterTile));
         const size_t o_tile_begin = put(tile_begin.data(), tile_begin.size() * 4);
-        const size_t o_long = put(longer.data(), longer.size() * sizeof(AdapterTile));
+        const size_t o_forward = put(in_order.data(), in_order.size() * sizeof(AdapterTile));
         const size_t o_rows = put(rows.data(), rows.size() * sizeof(AdapterRows));
         const size_t o_idle = put(idle.data(), idle.size() * 4);
         const size_t o_bare = put(bare.data(), bare.size() * sizeof(AdapterTile));
@@ -269,7 +281,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         b->d_scales = reinterpret_cast<const float *>(d + o_scales);
         b->d_tiles = reinterpret_cast<const AdapterTile *>(d + o_tiles);
         b->d_tile_begin = reinterpret_cast<const uint32_t *>(d + o_tile_begin);
-        b->d_long = reinterpret_cast<const AdapterTile *>(d + o_long);
+        b->d_forward = reinterpret_cast<const AdapterTile *>(d + o_forward);
         b->d_rows = reinterpret_cast<const AdapterRows *>(d + o_rows);
         b->d_idle = reinterpret_cast<const uint32_t *>(d + o_idle);
         b->d_bare = reinterpret_cast<const AdapterTile *>(d + o_bare);
@@ -342,11 +354,23 @@ extern "C" int fiona_adapter_forward(const fiona_adapter_batch *b, void *stream,
     a.out = out;
     a.ld_out = ld_out;
     a.h = h;
-    const bool short_apart = b->n_rows && adapter_rows_apply(b, l->d_in);
     const bool on_tiles = adapter_tiles_apply(b, l->d_in, l->d_out, l->dtype) && tma_rows(vx) && tma_rows(vbase) && tma_rows(vout);
-    if (short_apart && (rc = launch_adapter_rows(b, stream, l->dtype, a))) return rc;
-    if (on_tiles) return launch_adapter_tiles_forward(b, stream, l->dtype, a, work, short_apart);
-    return launch_adapter_any_forward(b, stream, l->dtype, a, work, short_apart);
+    // the split of the short runs that is quickest by the kernels' models
+    const fiona_adapter_batch::Split *split = nullptr;
+    double best = 0;
+    for (const auto &s : b->split) {
+        if (s.groups && !adapter_rows_apply(s, l->d_in)) continue;
+        const double us = adapter_rows_us(b, s, l->d_in, l->d_out) + (on_tiles ? adapter_tiles_us(b, s.tiles, l->d_in, l->d_out)
+                                                                               : adapter_any_us(b, s.tiles, l->d_in, l->d_out));
+        if (!split || us < best) {
+            best = us;
+            split = &s;
+        }
+    }
+    if (split->groups && (rc = launch_adapter_rows(b, *split, stream, l->dtype, a))) return rc;
+    if (!split->tiles && !b->n_bare) return FIONA_OK;
+    if (on_tiles) return launch_adapter_tiles_forward(b, stream, l->dtype, a, work, split->tiles);
+    return launch_adapter_any_forward(b, stream, l->dtype, a, work, split->tiles);
 }
 
 extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream, const fiona_adapter_layer *l,

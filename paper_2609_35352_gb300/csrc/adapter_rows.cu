@@ -16,6 +16,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "adapter_parts.cuh"
 #include "real.cuh"
@@ -392,15 +393,15 @@ auto pick(uint32_t most)
 }
 
 template <typename T>
-int run(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a)
+int run(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &split, cudaStream_t s, const AdapterArgs &a)
 {
     const RowsArgs g{a, b->d_rows, slice(a.d_in), slice(a.d_out), b->ctx->d_kerr, 2000000000ull};
-    void (*kernel)(RowsArgs) = a.d_in % Vec<T>::n == 0 && a.r_max % Vec<T>::n == 0 ? pick<T, true>(b->most_rows)
-                                                                                   : pick<T, false>(b->most_rows);
+    void (*kernel)(RowsArgs) = a.d_in % Vec<T>::n == 0 && a.r_max % Vec<T>::n == 0 ? pick<T, true>(split.most)
+                                                                                   : pick<T, false>(split.most);
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3(b->n_rows * kCluster);
+    c.gridDim = dim3(split.groups * kCluster);
     c.blockDim = dim3(kThreads);
-    c.dynamicSmemBytes = (size_t)b->most_rows * g.slice_in * 4;
+    c.dynamicSmemBytes = (size_t)split.most * g.slice_in * 4;
     c.stream = s;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -415,13 +416,26 @@ int run(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a)
 
 }  // namespace
 
-bool adapter_rows_apply(const fiona_adapter_batch *b, uint32_t d_in)
+bool adapter_rows_apply(const fiona_adapter_batch::Split &s, uint32_t d_in)
 {
-    return (size_t)b->most_rows * slice(d_in) * 4 <= 24 * 1024;  // (beside 21 KB)
+    return (size_t)s.most * slice(d_in) * 4 <= 24 * 1024;  // (beside 21 KB)
 }
 
-int launch_adapter_rows(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a)
+// Microseconds of a launch, as adapter_tiles_us: 4.2 and 18 for a million elements of
+// A and B, for each wave of clusters.
+double adapter_rows_us(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &s, uint32_t d_in, uint32_t d_out)
+{
+    if (!s.groups) return 0;
+    const uint32_t resident = (s.most <= 2 ? 4 : 2) * (uint32_t)std::max(b->ctx->sm_count, 1);
+    const double waves = std::ceil((double)s.groups * kCluster / resident);
+    return (waves > 1 ? 1.3 * waves : 1.0) * (4.2 + 18e-6 * b->r_max * ((double)d_in + d_out) * (s.most <= 2 ? 0.6 : 1.0));
+}
+
+int launch_adapter_rows(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &split, void *stream, uint32_t dtype,
+                        const AdapterArgs &a)
 {
     cudaStream_t s = (cudaStream_t)stream;
-    return dtype == FIONA_F32 ? run<float>(b, s, a) : dtype == FIONA_F16 ? run<__half>(b, s, a) : run<__nv_bfloat16>(b, s, a);
+    return dtype == FIONA_F32   ? run<float>(b, split, s, a)
+           : dtype == FIONA_F16 ? run<__half>(b, split, s, a)
+                                : run<__nv_bfloat16>(b, split, s, a);
 }

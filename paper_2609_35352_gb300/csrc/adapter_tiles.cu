@@ -1251,15 +1251,14 @@ uint32_t stages_for(uint32_t fixed, uint32_t stage, uint32_t least)
 }
 
 template <typename T>
-int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const AdapterArgs &a, void *work, bool only_long)
+int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const AdapterArgs &a, void *work, uint32_t n_tiles)
 {
     int rc = FIONA_OK;
-    const uint32_t n_tiles = only_long ? b->n_long : b->n_tiles;
     if (!n_tiles && !b->n_bare) return FIONA_OK;
     const ForwardShape f(b, a.d_in, a.d_out, n_tiles);
     TileArgs g{};
     g.a = a;
-    g.tiles = only_long ? b->d_long : b->d_tiles;
+    g.tiles = b->d_forward;
     g.n_tiles = n_tiles;
     g.r16 = f.r.r16;
     g.blocks = f.r.blocks;
@@ -1484,14 +1483,25 @@ int adapter_tiles_configure()
 
 uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
 {
-    return std::max({ForwardShape(b, d_in, d_out, b->n_tiles).part_bytes(b), ForwardShape(b, d_in, d_out, b->n_long).part_bytes(b), BackwardShape(b, d_in, d_out).bytes});
+    uint64_t n = BackwardShape(b, d_in, d_out).bytes;
+    for (const auto &s : b->split) n = std::max(n, ForwardShape(b, d_in, d_out, s.tiles).part_bytes(b));
+    return n;
+}
+
+// Microseconds of the two passes on few tiles, fitted to 16 to 512 rows, ranks 8 to
+// 128 and widths 768 to 8192 (to about 15%), with 1.5 for the second launch.
+double adapter_tiles_us(const fiona_adapter_batch *b, uint32_t n_tiles, uint32_t d_in, uint32_t d_out)
+{
+    if (!n_tiles) return 0;
+    const double r = b->r_max, d = (double)d_in + d_out;
+    return 5.9 + 0.045 * r + d * (2.5e-4 + 1.2e-6 * r) + (n_tiles - 1) * (0.08 + d * (2.2e-5 + 6.5e-7 * r));
 }
 
 int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,
-                                 bool only_long)
+                                 uint32_t n_tiles)
 {
-    return dtype == FIONA_BF16 ? forward<__nv_bfloat16>(b, (cudaStream_t)stream, dtype, a, work, only_long)
-                               : forward<__half>(b, (cudaStream_t)stream, dtype, a, work, only_long);
+    return dtype == FIONA_BF16 ? forward<__nv_bfloat16>(b, (cudaStream_t)stream, dtype, a, work, n_tiles)
+                               : forward<__half>(b, (cudaStream_t)stream, dtype, a, work, n_tiles);
 }
 
 int launch_adapter_tiles_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work)
