@@ -59,7 +59,9 @@ struct fiona_adapter_batch {
 
 // One call, as the kernels see it.  Rows are elements apart by their ld.
 struct AdapterArgs {
-    uint32_t n_tokens, n_adapters, r_max, d_in, d_out;
+    uint32_t n_tokens, n_adapters, d_in, d_out;
+    uint32_t r_rows, r_max;  // the layer's r_max; that of h's rows (the same, or padded: adapter_pad.cu)
+    uint64_t ldA, ldB;       // row strides of A and B
     const uint32_t *ranks;
     const float *scales;
     const void *A, *B;
@@ -95,6 +97,15 @@ int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uin
                                  uint32_t n_tiles);
 double adapter_tiles_us(const fiona_adapter_batch *b, uint32_t n_tiles, uint32_t d_in, uint32_t d_out);
 int launch_adapter_tiles_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
+
+// adapter_pad.cu: 16-bit layers whose sizes are no multiples of eight, by copies for
+// adapter_tiles.cu; whether it can, its workspace, its time by a model, the passes
+// (forward: on all tiles)
+bool adapter_pad_applies(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t dtype);
+uint64_t adapter_pad_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
+double adapter_pad_us(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
+int launch_adapter_pad_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
+int launch_adapter_pad_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
 
 // dropout.cu
 struct DropoutArgs {

@@ -167,13 +167,32 @@ __global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
     }
 }
 
-// out = base + s h B^T, or dx = dx_base + D'(dh A) (BACK), of half a tile and 64
-// columns: a thread 4 rows and the columns 16 apart.  The block of the first columns
-// leaves h or dh whole
-template <typename T, bool BACK>
-__global__ void __launch_bounds__(kThreads, 4) k_any_expand(const TileArgs g)
+// the partial h or dh of all ranges, in the place of the first's
+__global__ void __launch_bounds__(kThreads) k_any_whole(const TileArgs g)
 {
-    __shared__ __align__(16) float H[kSlice][kRows + kPad], S[kSlice][kCols + 1];
+    next_may_start();
+    previous_done();
+    const uint64_t k = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (k >= (uint64_t)g.a.n_tokens * g.r16 / 4) return;
+    const int64_t at[1] = {(int64_t)(4 * k)};
+    float4 s[1];
+    sum_parts(g, at, s);
+    *reinterpret_cast<float4 *>(g.part_out + 4 * k) = s[0];
+}
+
+// out = base + s h B^T, or dx = dx_base + D'(dh A) (BACK), of half a tile and 64
+// columns: a thread the sums of 4 x 4, and, by way of shared memory, the base and the
+// stores of 16 elements 4 rows apart, along the rows.  The block of the first
+// columns leaves h or dh whole.
+template <typename T, bool BACK>
+__global__ void __launch_bounds__(kThreads, 3) k_any_expand(const TileArgs g)
+{
+    __shared__ __align__(16) union {
+        struct {
+            float H[kSlice][kRows + kPad], S[kSlice][kCols + kPad];
+        } f;
+        float sum[kRows][kCols + kPad];
+    } sm;
     next_may_start();
     if (blockIdx.x < g.n_bare) {
         previous_done();
@@ -188,15 +207,16 @@ __global__ void __launch_bounds__(kThreads, 4) k_any_expand(const TileArgs g)
     }
     const uint32_t rows = min(kRows, t.rows - half * kRows), row0 = t.row0 + half * kRows;
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = g.a.ranks[t.adapter];
-    const uint32_t c = threadIdx.x % 16, r4 = threadIdx.x / 16 * 4;
+    const uint32_t c4 = threadIdx.x % 16 * 4, r4 = threadIdx.x / 16 * 4;
     const T *W = BACK ? (const T *)g.a.A + (size_t)t.adapter * g.a.r_max * g.a.d_in : (const T *)g.a.B + (size_t)t.adapter * g.a.d_out * g.a.r_max;
-    float base[4][4];
+    constexpr uint32_t kMine = kRows * kCols / kThreads, kStep = kThreads / kCols;  // elements a thread, rows apart
+    const uint32_t my_row = threadIdx.x / kCols, my_col = col0 + threadIdx.x % kCols;
+    T base[kMine];
+    if (g.a.base)
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i)
-#pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-            const uint32_t col = col0 + c + 16 * q;
-            base[i][q] = g.a.base ? element((const T *)g.a.base + (uint64_t)(row0 + r4 + i) * g.a.ld_base + col, r4 + i < rows && col < g.cols) : 0.f;
+        for (uint32_t i = 0; i < kMine; ++i) {
+            const uint32_t r = my_row + i * kStep;
+            base[i] = r < rows && my_col < g.cols ? ((const T *)g.a.base)[(uint64_t)(row0 + r) * g.a.ld_base + my_col] : narrow<T>(0.f);
         }
     float acc[4][4] = {}, fw[kSlice * kCols / kThreads];
     auto fetch = [&](uint32_t j0) {
@@ -229,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_any_expand(const TileArgs g)
             const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i) {
-                H[j - j0 + i][r] = f[i];
+                sm.f.H[j - j0 + i][r] = f[i];
                 if (!BACK && g.a.h && col0 == 0 && r < rows && j + i < g.a.r_max) g.a.h[(size_t)(row0 + r) * g.a.r_max + j + i] = f[i];
                 if (BACK && col0 == 0 && r < rows && j + i < rank) g.dh[(size_t)(row0 + r) * g.r16 + j + i] = f[i];
             }
@@ -237,36 +257,36 @@ __global__ void __launch_bounds__(kThreads, 4) k_any_expand(const TileArgs g)
 #pragma unroll
         for (uint32_t q = 0; q < kSlice * kCols / kThreads; ++q) {
             if (BACK)
-                S[warp + q / 2 * kWarps][lane + q % 2 * 32] = fw[q];
+                sm.f.S[warp + q / 2 * kWarps][lane + q % 2 * 32] = fw[q];
             else
-                S[lane][warp + q * kWarps] = fw[q];
+                sm.f.S[lane][warp + q * kWarps] = fw[q];
         }
         if (j0 + kSlice < rank) fetch(j0 + kSlice);
         __syncthreads();
         const uint32_t n = min(kSlice, rank > j0 ? rank - j0 : 0);
-#pragma unroll 4
+#pragma unroll 8
         for (uint32_t j = 0; j < n; ++j) {
-            const float4 h = *reinterpret_cast<const float4 *>(&H[j][r4]);
+            const float4 h = *reinterpret_cast<const float4 *>(&sm.f.H[j][r4]), w = *reinterpret_cast<const float4 *>(&sm.f.S[j][c4]);
+            const float a[4] = {h.x, h.y, h.z, h.w}, b[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (uint32_t q = 0; q < 4; ++q) {
-                const float w = S[j][c + 16 * q];
-                acc[0][q] = fmaf(h.x, w, acc[0][q]);
-                acc[1][q] = fmaf(h.y, w, acc[1][q]);
-                acc[2][q] = fmaf(h.z, w, acc[2][q]);
-                acc[3][q] = fmaf(h.w, w, acc[3][q]);
-            }
+            for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+                for (uint32_t q = 0; q < 4; ++q) acc[i][q] = fmaf(a[i], b[q], acc[i][q]);
         }
     }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(&sm.sum[r4 + i][c4]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    __syncthreads();
     const float scale = BACK ? g.a.mask.factor : g.a.scales[t.adapter];
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i)
-#pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-            const uint32_t row = row0 + r4 + i, col = col0 + c + 16 * q;
-            if (r4 + i >= rows || col >= g.cols) continue;
-            const bool drop = BACK && g.a.mask.level && !g.a.mask.keep(row, col);
-            ((T *)g.a.out)[(uint64_t)row * g.a.ld_out + col] = narrow<T>(drop ? base[i][q] : fmaf(scale, acc[i][q], base[i][q]));
-        }
+    for (uint32_t i = 0; i < kMine; ++i) {
+        const uint32_t r = my_row + i * kStep, row = row0 + r;
+        if (r >= rows || my_col >= g.cols) continue;
+        const bool drop = BACK && g.a.mask.level && !g.a.mask.keep(row, my_col);
+        const float x = g.a.base ? widen(base[i]) : 0.f;
+        ((T *)g.a.out)[(uint64_t)row * g.a.ld_out + my_col] = narrow<T>(drop ? x : fmaf(scale, sm.sum[r][threadIdx.x % kCols], x));
+    }
 }
 
 // dB += dy^T h, or dA += D(x)^T dh (INNER), of 64 columns over a chunk of tiles.
@@ -434,6 +454,20 @@ Cut shrink_cut(const fiona_adapter_batch *b, uint32_t cols, uint32_t n_tiles)
     return Cut{width, ceil_div(cols, width)};
 }
 
+// The ranges' partial sums, added up once where the blocks of the expand would
+// otherwise read more than 40 MB of them (some 5 us, what the launch takes with its
+// own reads): leaves g with one range.
+int whole_parts(TileArgs &g, uint32_t out_cols, cudaStream_t s)
+{
+    const uint64_t read = (uint64_t)g.slabs_in * 2 * g.n_tiles * ceil_div(out_cols, kCols) * kRows * g.r16 * 4;
+    if (g.slabs_in == 1 || read < 40000000) return FIONA_OK;
+    const uint64_t pieces = (uint64_t)g.a.n_tokens * g.r16 / 4;
+    void *args[] = {&g};
+    const int rc = launch(k_any_whole, dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), kThreads, 0, s, args, "adapter sums");
+    g.slabs_in = 1;
+    return rc;
+}
+
 // the largest chunks that still make four blocks an SM
 const AdapterChunks &grad_chunks(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
 {
@@ -475,12 +509,27 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a, 
     int rc = FIONA_OK;
     if (g.n_tiles && (rc = launch(pick_shrink<T, false>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter shrink")))
         return rc;
+    if (g.n_tiles && (rc = whole_parts(g, a.d_out, s))) return rc;
     g.cols = a.d_out;
     g.cut = Cut{kCols, ceil_div(a.d_out, kCols)};
     g.bare = b->d_bare;
     g.n_bare = b->n_bare;
     if (!g.n_tiles && !g.n_bare) return FIONA_OK;
     return launch(k_any_expand<T, false>, g.n_bare + 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter expand");
+}
+
+template <typename T>
+int grad_sum(const fiona_adapter_batch *b, cudaStream_t s, const GradSum &A, const GradSum &B)
+{
+    int rc = FIONA_OK;
+    const uint32_t sum_A = (uint32_t)(((uint64_t)A.rows * A.inner + kThreads - 1) / kThreads);
+    const uint32_t sum_B = (uint32_t)(((uint64_t)B.rows * B.inner + kThreads - 1) / kThreads);
+    for (uint32_t i = 0; i < b->n_adapters && rc == FIONA_OK; i += 65535) {
+        void *sargs[] = {(void *)&A, (void *)&B, (void *)&b->d_ranks, (void *)&sum_A, &i};
+        rc = launch(k_any_grad_sum<T>, dim3(sum_A + sum_B, std::min(b->n_adapters - i, 65535u)), kThreads, 0, s, sargs,
+                    "adapter gradients");
+    }
+    return rc;
 }
 
 template <typename T>
@@ -504,6 +553,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a,
     int rc = FIONA_OK;
     const bool any = b->n_tiles != 0;
     if (any && (rc = launch(pick_shrink<T, true>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter dh"))) return rc;
+    if (any && (rc = whole_parts(g, a.d_in, s))) return rc;
     g.cols = a.d_in;
     g.cut = Cut{kCols, ceil_div(a.d_in, kCols)};
     g.bare = b->d_bare;
@@ -522,21 +572,19 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a,
     if (g.direct) return rc;
     const GradSum A{g.grad, chunks.d_begin, a.dA, a.r_max, a.d_in, f.r16, a.d_in, 1};
     const GradSum B{g.grad_b, chunks.d_begin, a.dB, a.d_out, a.r_max, a.d_out, f.r16, 0};
-    const uint32_t sum_A = (uint32_t)(((uint64_t)a.r_max * a.d_in + kThreads - 1) / kThreads);
-    const uint32_t sum_B = (uint32_t)(((uint64_t)a.r_max * a.d_out + kThreads - 1) / kThreads);
-    for (uint32_t i = 0; i < a.n_adapters && rc == FIONA_OK; i += 65535) {
-        void *sargs[] = {(void *)&A, (void *)&B, (void *)&a.ranks, (void *)&sum_A, &i};
-        rc = launch(k_any_grad_sum<T>, dim3(sum_A + sum_B, std::min(a.n_adapters - i, 65535u)), kThreads, 0, s, sargs,
-                    "adapter gradients");
-    }
-    return rc;
+    return grad_sum<T>(b, s, A, B);
 }
 
 }  // namespace
 
+int parts::launch_any_grad_sum(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const GradSum &A, const GradSum &B)
+{
+    return dtype == FIONA_F32 ? grad_sum<float>(b, s, A, B) : dtype == FIONA_F16 ? grad_sum<__half>(b, s, A, B) : grad_sum<__nv_bfloat16>(b, s, A, B);
+}
+
 uint64_t adapter_any_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) { return AnyShape(b, d_in, d_out).bytes; }
 
-// as adapter_tiles_us
+// as adapter_tiles_us, on the FMA units
 double adapter_any_us(const fiona_adapter_batch *b, uint32_t n_tiles, uint32_t d_in, uint32_t d_out)
 {
     if (!n_tiles) return 0;

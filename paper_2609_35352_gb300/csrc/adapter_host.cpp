@@ -104,6 +104,7 @@ uint64_t work_needed(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out
 {
     uint64_t n = adapter_any_work(b, d_in, d_out);
     if (adapter_tiles_apply(b, d_in, d_out, dtype)) n = std::max(n, adapter_tiles_work(b, d_in, d_out));
+    if (adapter_pad_applies(b, d_in, d_out, dtype)) n = std::max(n, adapter_pad_work(b, d_in, d_out));
     return n;
 }
 
@@ -124,7 +125,9 @@ AdapterArgs common_args(const fiona_adapter_batch *b, const fiona_adapter_layer 
     AdapterArgs a{};
     a.n_tokens = b->n_tokens;
     a.n_adapters = b->n_adapters;
-    a.r_max = b->r_max;
+    a.r_rows = a.r_max = b->r_max;
+    a.ldA = l->d_in;
+    a.ldB = b->r_max;
     a.d_in = l->d_in;
     a.d_out = l->d_out;
     a.ranks = b->d_ranks;
@@ -367,6 +370,8 @@ extern "C" int fiona_adapter_forward(const fiona_adapter_batch *b, void *stream,
             split = &s;
         }
     }
+    if (!on_tiles && adapter_pad_applies(b, l->d_in, l->d_out, l->dtype) && adapter_pad_us(b, l->d_in, l->d_out) < best)
+        return launch_adapter_pad_forward(b, stream, l->dtype, a, work);
     if (split->groups && (rc = launch_adapter_rows(b, *split, stream, l->dtype, a))) return rc;
     if (!split->tiles && !b->n_bare) return FIONA_OK;
     if (on_tiles) return launch_adapter_tiles_forward(b, stream, l->dtype, a, work, split->tiles);
@@ -417,6 +422,10 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
     a.dB = dB;
     if (adapter_tiles_apply(b, l->d_in, l->d_out, l->dtype) && tma_rows(vx) && tma_rows(vdy) && tma_rows(vbase) && tma_rows(vdx))
         return launch_adapter_tiles_backward(b, stream, l->dtype, a, work);
+    // (both take some 2.3 times their forward passes)
+    if (adapter_pad_applies(b, l->d_in, l->d_out, l->dtype) &&
+        adapter_pad_us(b, l->d_in, l->d_out) < adapter_any_us(b, b->n_tiles, l->d_in, l->d_out))
+        return launch_adapter_pad_backward(b, stream, l->dtype, a, work);
     return launch_adapter_any_backward(b, stream, l->dtype, a, work);
 }
 

@@ -95,6 +95,9 @@ struct GradSum {
     uint32_t rank_rows;      // the rank bounds rows (dA) or columns (dB)
 };
 
+// adapter_any.cu: the sums element by element
+int launch_any_grad_sum(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const GradSum &A, const GradSum &B);
+
 // a kernel that waits for the one before it by itself
 template <typename K>
 inline int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t s, void **args, const char *what)

@@ -1272,9 +1272,9 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     g.slabs_in = f.shrink.slabs;
     CUtensorMap tx, tA, tbase, tB, tout, tout8;
     if ((rc = tensor_map(&tx, dtype, a.x, a.d_in, a.n_tokens, 0, a.ldx, kTileRows)) ||
-        (rc = tensor_map(&tA, dtype, a.A, a.d_in, a.r_max, a.n_adapters, a.d_in, f.r.r16)) ||
+        (rc = tensor_map(&tA, dtype, a.A, a.d_in, a.r_rows, a.n_adapters, a.ldA, f.r.r16)) ||
         (rc = tensor_map(&tbase, dtype, a.base, a.d_out, a.n_tokens, 0, a.ld_base, kTileRows)) ||
-        (rc = tensor_map(&tB, dtype, a.B, a.r_max, a.d_out, a.n_adapters, a.r_max, 64)) ||
+        (rc = tensor_map(&tB, dtype, a.B, a.r_rows, a.d_out, a.n_adapters, a.ldB, 64)) ||
         (rc = tensor_map(&tout, dtype, a.out, a.d_out, a.n_tokens, 0, a.ld_out, kTileRows)) ||
         (rc = tensor_map(&tout8, dtype, a.out, a.d_out, a.n_tokens, 0, a.ld_out, 8)))
         return rc;
@@ -1362,7 +1362,9 @@ template <typename T>
 int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const AdapterArgs &a, void *work)
 {
     int rc = FIONA_OK;
-    const BackwardShape f(b, a.d_in, a.d_out);
+    BackwardShape f(b, a.d_in, a.d_out);
+    const bool eights = a.d_in % 8 == 0 && a.r_rows % 8 == 0;
+    f.direct = f.direct && eights;  // (dA and dB are written by eights there, and by fours below)
     uint8_t *ws = static_cast<uint8_t *>(work);
     if (b->n_tiles || b->n_bare) {
         TileArgs g{};
@@ -1378,9 +1380,9 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.wait_ns = kWaitNs;
         CUtensorMap tx, tA, tdy, tB, tdx, tdx8;
         if ((rc = tensor_map(&tx, dtype, a.x, a.d_in, a.n_tokens, 0, a.ldx, kTileRows)) ||
-            (rc = tensor_map(&tA, dtype, a.A, a.d_in, a.r_max, a.n_adapters, a.d_in, f.r.r16)) ||
+            (rc = tensor_map(&tA, dtype, a.A, a.d_in, a.r_rows, a.n_adapters, a.ldA, f.r.r16)) ||
             (rc = tensor_map(&tdy, dtype, a.dy, a.d_out, a.n_tokens, 0, a.ld_dy, kTileRows)) ||
-            (rc = tensor_map(&tB, dtype, a.B, a.r_max, a.d_out, a.n_adapters, a.r_max, f.apart ? 64 : kBlockCols)) ||
+            (rc = tensor_map(&tB, dtype, a.B, a.r_rows, a.d_out, a.n_adapters, a.ldB, f.apart ? 64 : kBlockCols)) ||
             (rc = tensor_map(&tdx, dtype, a.out, a.d_in, a.n_tokens, 0, a.ld_out, kTileRows)) ||
             (rc = tensor_map(&tdx8, dtype, a.out, a.d_in, a.n_tokens, 0, a.ld_out, 8)))
             return rc;
@@ -1452,8 +1454,9 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
                     esmem, s, eargs, "adapter expand_grad");
         if (rc || f.direct) return rc;
     }
-    const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_max, a.d_in, f.r.r16, a.d_in, 1};
-    const GradSum B{reinterpret_cast<const float *>(ws + f.grad_B), f.shrink.chunks->d_begin, a.dB, a.d_out, a.r_max, a.d_out, f.r.r16, 0};
+    const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_rows, a.d_in, f.r.r16, a.d_in, 1};
+    const GradSum B{reinterpret_cast<const float *>(ws + f.grad_B), f.shrink.chunks->d_begin, a.dB, a.d_out, a.r_rows, a.d_out, f.r.r16, 0};
+    if (!eights) return launch_any_grad_sum(b, s, dtype, A, B);
     const uint32_t blocks_A = ceil_div(a.r_max * (a.d_in / 4), 256), blocks_B = ceil_div(a.d_out * (a.r_max / 4), 256);
     for (uint32_t i = 0; i < a.n_adapters && rc == FIONA_OK; i += 65535) {
         void *args[] = {(void *)&A, (void *)&B, (void *)&a.ranks, (void *)&blocks_A, &i};

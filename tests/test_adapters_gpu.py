@@ -333,3 +333,13 @@ def test_order_on_a_stream(ctx, dtype, starts, ids):
         torch.cuda.synchronize()
         for a, b in zip(first, (pr.out, pr.h, pr.dx, pr.dA, pr.dB)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d_in,d_out,r_max,pad", [(1001, 777, 43, 0), (1024, 777, 24, 0), (1001, 768, 33, 5), (640, 512, 100, 3)])
+def test_odd_sizes_of_long_batches(ctx, dtype, d_in, d_out, r_max, pad):
+    """Widths, ranks and strides that are no multiples of eight, with enough rows
+    that copies for the tensor cores pay."""
+    pr = Problem(ctx, dtype, [0, 1800, 1803, 1900, 4000], [0, 1, -1, 2], [r_max, r_max - 2, 7], r_max, d_in, d_out,
+                 seed=r_max, p=0.1, pad=pad)
+    pr.run_and_check()
