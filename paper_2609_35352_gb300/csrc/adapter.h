@@ -34,6 +34,8 @@ struct AdapterChunks {
 struct fiona_adapter_batch {
     const fiona_ctx *ctx = nullptr;
     uint32_t n_tokens = 0, n_adapters = 0, r_max = 0;
+    bool stall = false;  // FIONA_ADAPTER_TEST_STALL, read when the batch is made: its kernels' waits run out
+    uint64_t wait_ns = 2000000000ull;  // bound of every wait
     // device arrays, in `blob`
     void *blob = nullptr;
     const uint32_t *d_ranks = nullptr;        // [n_adapters]

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 #include <new>
 
@@ -169,6 +170,10 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
     b->n_tokens = (uint32_t)starts[n_requests];
     b->n_adapters = n_adapters;
     b->r_max = r_max;
+    if (const char *env = getenv("FIONA_ADAPTER_TEST_STALL"); env && env[0] == '1') {
+        b->stall = true;
+        b->wait_ns = 2000000ull;
+    }
 
     const uint32_t T = b->n_tokens;
     std::vector<uint32_t> owner(T);

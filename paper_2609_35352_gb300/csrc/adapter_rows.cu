@@ -76,6 +76,7 @@ struct RowsArgs {
     uint32_t slice_in, slice_out;  // columns a CTA, multiples of 8
     int *err;
     uint64_t wait_ns;
+    uint32_t stall;  // test only: the barrier expects an arrival too many
 };
 
 // shared memory of a CTA, but for its rows of x
@@ -287,7 +288,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &
     const uint32_t bar = async::smem_addr(&sh.bar);
     if (tid == 0) {
         sh.abort = 0;
-        async::mbar_init(bar, 1);
+        async::mbar_init(bar, 1 + g.stall);
         async::mbar_init_fence();
         async::mbar_arrive_expect_tx(bar, kCluster * G * rank4 * 16);
     }
@@ -395,7 +396,7 @@ auto pick(uint32_t most)
 template <typename T>
 int run(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &split, cudaStream_t s, const AdapterArgs &a)
 {
-    const RowsArgs g{a, b->d_rows, slice(a.d_in), slice(a.d_out), b->ctx->d_kerr, 2000000000ull};
+    const RowsArgs g{a, b->d_rows, slice(a.d_in), slice(a.d_out), b->ctx->d_kerr, b->wait_ns, b->stall};
     void (*kernel)(RowsArgs) = a.d_in % Vec<T>::n == 0 && a.r_max % Vec<T>::n == 0 ? pick<T, true>(split.most)
                                                                                    : pick<T, false>(split.most);
     cudaLaunchConfig_t c{};

@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (uint32_t s = 0; s < S; ++s) {
-            async::mbar_init(full + kBar * s, 1);
+            async::mbar_init(full + kBar * s, 1 + g.stall);
             async::mbar_init(fixed + kBar * s, 8);
             async::mbar_init(empty + kBar * s, 1);
         }
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kExpandThreads, 2) k_expand(const __grid_const
         s_abort = 0;
         s_most = 0;
         for (uint32_t s = 0; s < S; ++s) {
-            async::mbar_init(full + kBar * s, 1);
+            async::mbar_init(full + kBar * s, 1 + g.stall);
             async::mbar_init(fixed + kBar * s, 2);
             async::mbar_init(empty + kBar * s, 1);
             async::mbar_init(written + kBar * s, kExpandWorkers / 32);
@@ -686,7 +686,7 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (uint32_t s = 0; s < S; ++s) {
-            async::mbar_init(full + kBar * s, 1);
+            async::mbar_init(full + kBar * s, 1 + g.stall);
             async::mbar_init(fixed + kBar * s, 4);
             async::mbar_init(empty + kBar * s, 1);
         }
@@ -880,7 +880,7 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (uint32_t s = 0; s < S; ++s) {
-            async::mbar_init(full + kBar * s, 1);
+            async::mbar_init(full + kBar * s, 1 + g.stall);
             async::mbar_init(fixed + kBar * s, 8);
             async::mbar_init(empty + kBar * s, 1);
             async::mbar_init(written + kBar * s, kGradWorkers / 32);
@@ -1238,7 +1238,6 @@ struct ForwardShape {
     }
 };
 
-constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr uint32_t kSmemTwo = 110 * 1024;   // dynamic shared memory of a CTA, two of them an SM
 constexpr uint32_t kSmemOne = 224 * 1024;
 
@@ -1266,7 +1265,8 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     g.op_boxes = f.r.boxes;
     g.both = f.r.both;
     g.err = b->ctx->d_kerr;
-    g.wait_ns = kWaitNs;
+    g.wait_ns = b->wait_ns;
+    g.stall = b->stall;
     g.part_out = static_cast<float *>(work);
     g.part_in = g.part_out;
     g.slabs_in = f.shrink.slabs;
@@ -1377,7 +1377,8 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
     g.op_boxes = f.r.boxes;
     g.both = f.r.both;
         g.err = b->ctx->d_kerr;
-        g.wait_ns = kWaitNs;
+        g.wait_ns = b->wait_ns;
+        g.stall = b->stall;
         CUtensorMap tx, tA, tdy, tB, tdx, tdx8;
         if ((rc = tensor_map(&tx, dtype, a.x, a.d_in, a.n_tokens, 0, a.ldx, kTileRows)) ||
             (rc = tensor_map(&tA, dtype, a.A, a.d_in, a.r_rows, a.n_adapters, a.ldA, f.r.r16)) ||

@@ -56,6 +56,7 @@ struct TileArgs {
     const uint32_t *idle;  // direct: adapters without tiles, whose gradients are zero
     uint32_t n_idle;
     uint32_t n_tiles, n_chunks, stages, buffers, tmem_cols;
+    uint32_t stall;        // test only: a barrier that expects an arrival too many
     int *err;
     uint64_t wait_ns;
 };

@@ -343,3 +343,18 @@ def test_odd_sizes_of_long_batches(ctx, dtype, d_in, d_out, r_max, pad):
     pr = Problem(ctx, dtype, [0, 1800, 1803, 1900, 4000], [0, 1, -1, 2], [r_max, r_max - 2, 7], r_max, d_in, d_out,
                  seed=r_max, p=0.1, pad=pad)
     pr.run_and_check()
+
+
+@pytest.mark.parametrize("dtype,starts", [("bf16", [0, 300]), ("f16", [0, 130]), ("bf16", list(range(9))), ("f32", list(range(9)))])
+def test_waits_that_run_out_are_reported(ctx, dtype, starts, monkeypatch):
+    """Kernels whose barriers expect an arrival that never comes give up, end and
+    say so; the context goes on."""
+    ids = [0] * (len(starts) - 1)
+    monkeypatch.setenv("FIONA_ADAPTER_TEST_STALL", "1")
+    stalled = Problem(ctx, dtype, starts, ids, [32], 32, 512, 384, p=0.1)
+    monkeypatch.delenv("FIONA_ADAPTER_TEST_STALL")
+    for call in (stalled.forward,) if len(starts) > 2 else (stalled.forward, stalled.backward):
+        assert ctx.device_check() == F.FIONA_OK
+        call()
+        assert ctx.device_check() == F.FIONA_ERR_TIMEOUT
+    Problem(ctx, dtype, starts, ids, [32], 32, 512, 384, p=0.1).run_and_check()
