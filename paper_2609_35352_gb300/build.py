@@ -34,7 +34,8 @@ EXTRA = {"kernel_tiled.cu": ["-Xptxas", "-regUsageLevel=8"],
 LIBRARIES = {
     "libfiona.so": ["fiona_host.cpp", "lower_tiled.cpp", "lower_gemm.cpp", "plan_compile.cpp", "kernel_direct.cu",
                     "kernel_tiled.cu", "kernel_tiled_off.cu", "kernel_tiled_w12.cu", "kernel_ws.cu", "kernel_gemm.cu", "rescale.cu", "encode.cu",
-                    "adapter_host.cpp", "adapter_any.cu", "adapter_rows.cu", "adapter_tiles.cu", "adapter_pad.cu",
+                    "adapter_host.cpp", "adapter_any.cu", "adapter_rows.cpp", "adapter_rows_f32.cu", "adapter_rows_f16.cu",
+                    "adapter_rows_bf16.cu", "adapter_tiles.cu", "adapter_pad.cu",
                     "dropout.cu"],
     "libfiona_workload.so": ["workload_fill.cu", "mul_roof.cu"],
 }

@@ -83,7 +83,7 @@ int launch_adapter_any_forward(const fiona_adapter_batch *b, void *stream, uint3
                                uint32_t n_tiles);
 int launch_adapter_any_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
 
-// adapter_rows.cu: the forward pass on groups of rows, any type and alignment
+// adapter_rows.cpp, .cuh: the forward pass on groups of rows, any type and alignment
 constexpr uint32_t kFewRows = 16;
 bool adapter_rows_apply(const fiona_adapter_batch::Split &s, uint32_t d_in);
 double adapter_rows_us(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &s, uint32_t d_in, uint32_t d_out);
@@ -105,7 +105,7 @@ int launch_adapter_tiles_backward(const fiona_adapter_batch *b, void *stream, ui
 // (forward: on all tiles)
 bool adapter_pad_applies(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t dtype);
 uint64_t adapter_pad_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
-double adapter_pad_us(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out);
+double adapter_pad_us(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, bool backward);
 int launch_adapter_pad_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
 int launch_adapter_pad_backward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work);
 

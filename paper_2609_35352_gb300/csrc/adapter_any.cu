@@ -584,12 +584,12 @@ int parts::launch_any_grad_sum(const fiona_adapter_batch *b, cudaStream_t s, uin
 
 uint64_t adapter_any_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) { return AnyShape(b, d_in, d_out).bytes; }
 
-// as adapter_tiles_us, on the FMA units
+// as adapter_tiles_us, on the FMA units (whose time on a tile goes by its rows)
 double adapter_any_us(const fiona_adapter_batch *b, uint32_t n_tiles, uint32_t d_in, uint32_t d_out)
 {
     if (!n_tiles) return 0;
-    const double r = b->r_max, d = (double)d_in + d_out;
-    return 7.0 + 0.14 * r + d * (4e-4 + 1.4e-5 * r) + (n_tiles - 1) * (0.15 + d * (0.8e-4 + 3e-6 * r));
+    const double r = b->r_max, d = (double)d_in + d_out, rows = (double)b->n_tokens / std::max(b->n_tiles, 1u);
+    return 7.0 + 0.14 * r + d * (4e-4 + 1.4e-5 * r) + (n_tiles - 1) * (0.35 + 0.65 * rows / 32) * (0.15 + d * (0.8e-4 + 3e-6 * r));
 }
 
 int launch_adapter_any_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,

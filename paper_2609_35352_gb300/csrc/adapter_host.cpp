@@ -375,7 +375,7 @@ extern "C" int fiona_adapter_forward(const fiona_adapter_batch *b, void *stream,
             split = &s;
         }
     }
-    if (!on_tiles && adapter_pad_applies(b, l->d_in, l->d_out, l->dtype) && adapter_pad_us(b, l->d_in, l->d_out) < best)
+    if (!on_tiles && adapter_pad_applies(b, l->d_in, l->d_out, l->dtype) && adapter_pad_us(b, l->d_in, l->d_out, false) < best)
         return launch_adapter_pad_forward(b, stream, l->dtype, a, work);
     if (split->groups && (rc = launch_adapter_rows(b, *split, stream, l->dtype, a))) return rc;
     if (!split->tiles && !b->n_bare) return FIONA_OK;
@@ -427,9 +427,8 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
     a.dB = dB;
     if (adapter_tiles_apply(b, l->d_in, l->d_out, l->dtype) && tma_rows(vx) && tma_rows(vdy) && tma_rows(vbase) && tma_rows(vdx))
         return launch_adapter_tiles_backward(b, stream, l->dtype, a, work);
-    // (both take some 2.3 times their forward passes)
     if (adapter_pad_applies(b, l->d_in, l->d_out, l->dtype) &&
-        adapter_pad_us(b, l->d_in, l->d_out) < adapter_any_us(b, b->n_tiles, l->d_in, l->d_out))
+        adapter_pad_us(b, l->d_in, l->d_out, true) < 2.5 * adapter_any_us(b, b->n_tiles, l->d_in, l->d_out))
         return launch_adapter_pad_backward(b, stream, l->dtype, a, work);
     return launch_adapter_any_backward(b, stream, l->dtype, a, work);
 }

@@ -111,12 +111,14 @@ bool adapter_pad_applies(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d
 
 uint64_t adapter_pad_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) { return PadShape(b, d_in, d_out).bytes; }
 
-// Microseconds, as adapter_tiles_us: two launches more, and the copies at 2.5 TB/s.
-double adapter_pad_us(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
+// Microseconds, as adapter_tiles_us: two launches more (their time on the host, some 5
+// each, counts where the rest is short), and the copies' reads and writes at 3.5 TB/s
+// (a gradient takes 2.3 times its forward passes).
+double adapter_pad_us(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, bool backward)
 {
     const double T = b->n_tokens, weights = (double)b->n_adapters * b->r_max * ((double)d_in + d_out);
-    const double copied = 2.0 * ((d_in % 8 ? T * d_in : 0) + (d_out % 8 ? 2 * T * d_out : 0) + weights);
-    return adapter_tiles_us(b, b->n_tiles, d_in, d_out) + 5.0 + 2 * copied / 2.5e6;
+    const double copied = (d_in % 8 ? (backward ? 2 : 1) * T * d_in : 0) + (d_out % 8 ? (backward ? 1 : 2) * T * d_out : 0) + weights;
+    return (backward ? 2.3 : 1.0) * adapter_tiles_us(b, b->n_tiles, d_in, d_out) + (backward ? 14.0 : 10.0) + 4 * copied / 3.5e6;
 }
 
 int launch_adapter_pad_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work)

@@ -1,4 +1,5 @@
-// adapter_rows.cu -- the adapters' forward pass on a few rows each: a step of many
+// adapter_rows.cuh -- the adapters' forward pass on a few rows each (a type a
+// translation unit: adapter_rows_*.cu): a step of many
 // requests that bring one new token, or a handful.
 //
 // A cluster of eight CTAs takes up to four rows of one adapter, wherever they
@@ -13,12 +14,13 @@
 // 64 in rows of 64: 52 us, 248 MB from HBM, as the unused ranks come with the others
 // in lines of 128 bytes (36 us at the copy bandwidth).  Every output stored by the
 // lane that held its sum made it 58 us, a cluster of four 63.
+#pragma once
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 
 #include "adapter_parts.cuh"
+#include "adapter_rows.h"
 #include "real.cuh"
 #include "tc_tiles.cuh"
 
@@ -28,7 +30,6 @@ using real::narrow;
 using real::widen;
 
 constexpr uint32_t kThreads = 256, kWarps = kThreads / 32;
-constexpr uint32_t kCluster = 8;
 // loads a lane has under way, for groups of G rows (with more, registers would
 // cost the second and third CTA of an SM)
 constexpr uint32_t under_way(uint32_t G) { return G <= 2 ? 8 : 4; }
@@ -277,11 +278,11 @@ __device__ __forceinline__ void outputs(const RowsArgs &g, const AdapterRows &ro
     }
 }
 
-// VEC: rows of A and B are whole vectors of 16 bytes
-template <typename T, bool VEC, uint32_t G>
+// VA, VB: rows of A, of B are whole vectors of 16 bytes
+template <typename T, bool VA, bool VB, uint32_t G>
 __device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &rows, float *s_x, RowsShared &sh)
 {
-    constexpr uint32_t V = VEC ? Vec<T>::n : 1, kUnroll = under_way(G);  // (V: ranks a lane)
+    constexpr uint32_t V = VB ? Vec<T>::n : 1, kUnroll = under_way(G);  // (V: ranks a lane)
     const AdapterArgs &a = g.a;
     const uint32_t cta = cluster_cta(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = a.ranks[rows.adapter], rank4 = (rank + 3) / 4;
@@ -316,7 +317,7 @@ __device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &
     }
     __syncthreads();
 
-    if (VEC) {
+    if (VA) {
         if (rank <= 2 * kWarps)
             partial_h<T, G, 2>(A, a.d_in, n_in, rank, g.slice_in, s_x, &sh.part[0][0], warp, lane);
         else
@@ -358,47 +359,44 @@ __device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &
     __syncthreads();
 
     switch (rank > V ? 32 - __clz((int)((rank + V - 1) / V - 1)) : 0) {  // log2 of the lanes a column
-        case 0: outputs<T, VEC, G, 1>(g, rows, B, rank, o0, n_out, sh); break;
-        case 1: outputs<T, VEC, G, 2>(g, rows, B, rank, o0, n_out, sh); break;
-        case 2: outputs<T, VEC, G, 4>(g, rows, B, rank, o0, n_out, sh); break;
-        case 3: outputs<T, VEC, G, 8>(g, rows, B, rank, o0, n_out, sh); break;
-        case 4: outputs<T, VEC, G, 16>(g, rows, B, rank, o0, n_out, sh); break;
-        default: outputs<T, VEC, G, 32>(g, rows, B, rank, o0, n_out, sh); break;
+        case 0: outputs<T, VB, G, 1>(g, rows, B, rank, o0, n_out, sh); break;
+        case 1: outputs<T, VB, G, 2>(g, rows, B, rank, o0, n_out, sh); break;
+        case 2: outputs<T, VB, G, 4>(g, rows, B, rank, o0, n_out, sh); break;
+        case 3: outputs<T, VB, G, 8>(g, rows, B, rank, o0, n_out, sh); break;
+        case 4: outputs<T, VB, G, 16>(g, rows, B, rank, o0, n_out, sh); break;
+        default: outputs<T, VB, G, 32>(g, rows, B, rank, o0, n_out, sh); break;
     }
 }
 
 // MOST: the largest group of the batch
-template <typename T, bool VEC, uint32_t MOST>
+template <typename T, bool VA, bool VB, uint32_t MOST>
 __global__ void __launch_bounds__(kThreads, MOST <= 2 ? 4 : 2) k_rows(const RowsArgs g)
 {
     extern __shared__ __align__(16) float s_x[];  // [rows][slice_in]
     __shared__ __align__(16) RowsShared sh;
     const AdapterRows rows = g.groups[blockIdx.x / kCluster];
     if (rows.count == 1)
-        rows_body<T, VEC, 1>(g, rows, s_x, sh);
+        rows_body<T, VA, VB, 1>(g, rows, s_x, sh);
     else if (MOST > 1 && rows.count == 2)
-        rows_body<T, VEC, (MOST > 1 ? 2 : 1)>(g, rows, s_x, sh);
+        rows_body<T, VA, VB, (MOST > 1 ? 2 : 1)>(g, rows, s_x, sh);
     else if (MOST > 2 && rows.count == 3)
-        rows_body<T, VEC, (MOST > 2 ? 3 : 1)>(g, rows, s_x, sh);
+        rows_body<T, VA, VB, (MOST > 2 ? 3 : 1)>(g, rows, s_x, sh);
     else if (MOST > 2)
-        rows_body<T, VEC, (MOST > 2 ? 4 : 1)>(g, rows, s_x, sh);
+        rows_body<T, VA, VB, (MOST > 2 ? 4 : 1)>(g, rows, s_x, sh);
 }
 
-// columns of `d` a CTA of the cluster takes
-uint32_t slice(uint32_t d) { return ((d + kCluster - 1) / kCluster + 7) & ~7u; }
-
-template <typename T, bool VEC>
-auto pick(uint32_t most)
+template <typename T, bool VA>
+auto pick(bool vb, uint32_t most)
 {
-    return most <= 1 ? k_rows<T, VEC, 1> : most == 2 ? k_rows<T, VEC, 2> : k_rows<T, VEC, 4>;
+    return vb ? (most <= 2 ? k_rows<T, VA, true, 2> : k_rows<T, VA, true, 4>) : (most <= 2 ? k_rows<T, VA, false, 2> : k_rows<T, VA, false, 4>);
 }
 
 template <typename T>
 int run(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &split, cudaStream_t s, const AdapterArgs &a)
 {
-    const RowsArgs g{a, b->d_rows, slice(a.d_in), slice(a.d_out), b->ctx->d_kerr, b->wait_ns, b->stall};
-    void (*kernel)(RowsArgs) = a.d_in % Vec<T>::n == 0 && a.r_max % Vec<T>::n == 0 ? pick<T, true>(split.most)
-                                                                                   : pick<T, false>(split.most);
+    const RowsArgs g{a, b->d_rows, rows_slice(a.d_in), rows_slice(a.d_out), b->ctx->d_kerr, b->wait_ns, b->stall};
+    const bool vb = a.r_max % Vec<T>::n == 0;
+    void (*kernel)(RowsArgs) = a.d_in % Vec<T>::n == 0 ? pick<T, true>(vb, split.most) : pick<T, false>(vb, split.most);
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(split.groups * kCluster);
     c.blockDim = dim3(kThreads);
@@ -416,27 +414,3 @@ int run(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &split, c
 }
 
 }  // namespace
-
-bool adapter_rows_apply(const fiona_adapter_batch::Split &s, uint32_t d_in)
-{
-    return (size_t)s.most * slice(d_in) * 4 <= 24 * 1024;  // (beside 21 KB)
-}
-
-// Microseconds of a launch, as adapter_tiles_us: 4.2 and 18 for a million elements of
-// A and B, for each wave of clusters.
-double adapter_rows_us(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &s, uint32_t d_in, uint32_t d_out)
-{
-    if (!s.groups) return 0;
-    const uint32_t resident = (s.most <= 2 ? 4 : 2) * (uint32_t)std::max(b->ctx->sm_count, 1);
-    const double waves = std::ceil((double)s.groups * kCluster / resident);
-    return (waves > 1 ? 1.3 * waves : 1.0) * (4.2 + 18e-6 * b->r_max * ((double)d_in + d_out) * (s.most <= 2 ? 0.6 : 1.0));
-}
-
-int launch_adapter_rows(const fiona_adapter_batch *b, const fiona_adapter_batch::Split &split, void *stream, uint32_t dtype,
-                        const AdapterArgs &a)
-{
-    cudaStream_t s = (cudaStream_t)stream;
-    return dtype == FIONA_F32   ? run<float>(b, split, s, a)
-           : dtype == FIONA_F16 ? run<__half>(b, split, s, a)
-                                : run<__nv_bfloat16>(b, split, s, a);
-}

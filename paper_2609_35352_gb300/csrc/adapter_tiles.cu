@@ -42,6 +42,7 @@ using namespace parts;
 using tiles::chunk_at;
 
 constexpr uint32_t kBar = 8;
+constexpr uint32_t kMostWarps = 8;  // warps that store a tile's sums
 
 template <typename T>
 constexpr bool is_bf16() { return std::is_same<T, __nv_bfloat16>::value; }
@@ -194,6 +195,21 @@ __device__ __forceinline__ void clear_rows(uint32_t box, uint32_t rows, uint32_t
     for (uint32_t k = rows * 8 + thread; k < kTileRows * 8; k += threads) st_shared16(box + chunk_at(k / 8, k % 8), make_uint4(0, 0, 0, 0));
 }
 
+// the largest of sixteen sums, of ranks c on, and of a warp's (TileArgs::most)
+__device__ __forceinline__ float largest(const float (&v)[16], uint32_t c, uint32_t rank)
+{
+    float big = 0.f;
+#pragma unroll
+    for (uint32_t k = 0; k < 16; ++k)
+        if (c + k < rank) big = fmaxf(big, finite_abs(v[k]));
+    return big;
+}
+__device__ __forceinline__ void put_most(const TileArgs &g, uint32_t slab, uint32_t tile, float big, uint32_t warp, uint32_t lane)
+{
+    for (int o = 16; o; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+    if (lane == 0) g.most[((size_t)slab * g.n_tiles + tile) * kMostWarps + warp] = big;
+}
+
 // ---------------------------------------------------------------------------
 // shrink: partial h of a token tile over a range of columns
 // ---------------------------------------------------------------------------
@@ -313,6 +329,7 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
         __syncwarp();
         parts::previous_done();
         float *p = g.part_out + ((size_t)slab * g.a.n_tokens + t.row0 + row) * g.r16;
+        float big = 0.f;
         for (uint32_t c = half * 16; c < n16; c += 32) {
             float v[16];
             tiles::ld16(tmem + ((quarter * 32) << 16) + c, v);
@@ -328,7 +345,9 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
 #pragma unroll
                 for (uint32_t k = 0; k < 16; k += 4)
                     *reinterpret_cast<float4 *>(p + c + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+            if (BACK && !is_bf16<T>() && row < t.rows) big = fmaxf(big, largest(v, c, rank));
         }
+        if (BACK && !is_bf16<T>()) put_most(g, slab, blockIdx.x / g.cut.slabs, big, me.warp - 2, me.lane);
         tcs::fence_before();
     }
     __syncwarp();
@@ -778,6 +797,7 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
             tcs::fence_after();
             __syncwarp();
             float *p = g.part_out + ((size_t)job.slab * g.a.n_tokens + tile.row0 + row) * g.r16;
+            float big = 0.f;
             for (uint32_t c = half * 16; c < job.n16; c += 32) {
                 float v[16];
                 tiles::ld16(tmem + ((quarter * 32) << 16) + d * g.r16 + c, v);
@@ -786,9 +806,11 @@ __global__ void __launch_bounds__(kGradThreads) k_shrink_grad(const __grid_const
 #pragma unroll
                     for (uint32_t k = 0; k < 16; k += 4)
                         *reinterpret_cast<float4 *>(p + c + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+                if (!is_bf16<T>() && row < tile.rows) big = fmaxf(big, largest(v, c, job.rank));
             }
             tcs::fence_before();
             arrive_warp(free_ + kBar * d, me.lane);
+            if (!is_bf16<T>()) put_most(g, job.slab, job.c.begin + t, big, me.warp - 2, me.lane);
         }
         w.pass(all, 0);
         tcs::fence_after();
@@ -1082,17 +1104,56 @@ __global__ void __launch_bounds__(kExpandGradThreads) k_expand_grad(const __grid
     if (me.warp == 1) tcs::tmem_dealloc(tmem, g.tmem_cols);
 }
 
-// The images of h or dh (DH: the sum of its parts, times s_a): a block as many
-// rows of a tile as make 256 pieces of four ranks, zero past the tile and from the rank
-// on.  fp16 goes by a power of two that is
-// one for all of an adapter's tiles (they share accumulators), from the largest
-// value of each block (MOST: this kernel's first pass).
+// four elements of a weight gradient (GradSum): its chunks' sums, in order
+template <typename T>
+__device__ __forceinline__ void add_up(const GradSum &g, const uint32_t *ranks, uint32_t ad, uint64_t k)
+{
+    const uint32_t rank = ranks[ad], per_row = g.inner / 4;
+    if (k >= (uint64_t)g.rows * per_row) return;
+    const uint32_t row = (uint32_t)(k / per_row), col = (uint32_t)(k % per_row) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row < (g.rank_rows ? rank : g.rows) && col < (g.rank_rows ? g.inner : rank)) {
+        const uint32_t end = g.begin[ad + 1];
+        const size_t step = (size_t)g.part_rows * g.part_inner;
+        const float *p = g.part + ((size_t)g.begin[ad] * g.part_rows + row) * g.part_inner + col;
+#pragma unroll 8
+        for (uint32_t c = g.begin[ad]; c < end; ++c, p += step) {
+            const float4 x = *reinterpret_cast<const float4 *>(p);
+            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+        }
+    }
+    if (!g.rank_rows) v = below(v, col, rank, 1.f);
+    *reinterpret_cast<uint2 *>((T *)g.out + ((size_t)ad * g.rows + row) * g.inner + col) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_grad_sum(const GradSum A, const uint32_t *ranks, uint32_t first)
+{
+    parts::next_may_start();
+    parts::previous_done();
+    add_up<T>(A, ranks, first + blockIdx.y, (uint64_t)blockIdx.x * 256 + threadIdx.x);
+}
+
+// The images of h or dh (DH: the sum of its parts, times s_a): a block as many rows
+// of a tile as make 256 pieces of four ranks, zero past the tile and from the rank
+// on.  fp16 goes by a power of two that is one for all of an adapter's tiles (they share
+// accumulators): for h from the largest value of each block (MOST: a pass that only
+// finds them), for dh from the largest of its partial sums, times their number.
 __host__ __device__ constexpr uint32_t image_blocks(uint32_t r16) { return r16 <= 16 ? 2 : r16 <= 32 ? 4 : r16 <= 64 ? 8 : 16; }
 
+// (DH: the blocks behind the images' add up dB, whose chunks' sums are ready by then)
 template <typename T, bool DH, bool MOST>
-__global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image, float *ups, float *most, const uint32_t *tile_begin)
+__global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image, float *ups, float *most, const uint32_t *tile_begin,
+                                               uint32_t blocks, const GradSum B, uint32_t per_adapter)
 {
     __shared__ uint32_t s_most;
+    if (DH && blockIdx.x >= blocks) {
+        parts::previous_done();
+        parts::next_may_start();
+        const uint32_t k = blockIdx.x - blocks;
+        add_up<T>(B, g.a.ranks, k / per_adapter, (uint64_t)(k % per_adapter) * 256 + threadIdx.x);
+        return;
+    }
     const uint32_t per_tile = image_blocks(g.r16), n_rows = kTileRows / per_tile;
     const uint32_t tile = blockIdx.x / per_tile, r0 = blockIdx.x % per_tile * n_rows;
     const AdapterTile t = g.tiles[tile];
@@ -1122,6 +1183,14 @@ __global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image,
                 const float4 v = value(k);
                 big = fmaxf(big, fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
             }
+        } else if (DH) {
+            const uint32_t per_slab = (tile_begin[t.adapter + 1] - tile_begin[t.adapter]) * (kMostWarps / 4);
+            for (uint32_t k = threadIdx.x; k < g.slabs_in * per_slab; k += 256) {
+                const float4 v = reinterpret_cast<const float4 *>(
+                    g.most + ((size_t)(k / per_slab) * g.n_tiles + tile_begin[t.adapter]) * kMostWarps)[k % per_slab];
+                big = fmaxf(big, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
+            }
+            big = finite_abs(big * s_a * (float)g.slabs_in);
         } else {
             for (uint32_t k = per_tile * tile_begin[t.adapter] + threadIdx.x; k < per_tile * tile_begin[t.adapter + 1]; k += 256) big = fmaxf(big, most[k]);
         }
@@ -1146,32 +1215,6 @@ __global__ void __launch_bounds__(256) k_image(const TileArgs g, uint8_t *image,
         *reinterpret_cast<uint2 *>(at(j)) = hi;
         *reinterpret_cast<uint2 *>(at(g.lo + j)) = lo;
     }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(256) k_grad_sum(const GradSum A, const GradSum B, const uint32_t *ranks, uint32_t blocks_A,
-                                                  uint32_t first)
-{
-    const GradSum &g = blockIdx.x < blocks_A ? A : B;
-    const uint32_t ad = first + blockIdx.y, rank = ranks[ad], per_row = g.inner / 4;
-    const uint64_t k = (uint64_t)(blockIdx.x < blocks_A ? blockIdx.x : blockIdx.x - blocks_A) * 256 + threadIdx.x;
-    parts::next_may_start();
-    parts::previous_done();
-    if (k >= (uint64_t)g.rows * per_row) return;
-    const uint32_t row = (uint32_t)(k / per_row), col = (uint32_t)(k % per_row) * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row < (g.rank_rows ? rank : g.rows) && col < (g.rank_rows ? g.inner : rank)) {
-        const uint32_t end = g.begin[ad + 1];
-        const size_t step = (size_t)g.part_rows * g.part_inner;
-        const float *p = g.part + ((size_t)g.begin[ad] * g.part_rows + row) * g.part_inner + col;
-#pragma unroll 8
-        for (uint32_t c = g.begin[ad]; c < end; ++c, p += step) {
-            const float4 x = *reinterpret_cast<const float4 *>(p);
-            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-        }
-    }
-    if (!g.rank_rows) v = below(v, col, rank, 1.f);
-    *reinterpret_cast<uint2 *>((T *)g.out + ((size_t)ad * g.rows + row) * g.inner + col) = make_uint2(pack<T>(v.x, v.y), pack<T>(v.z, v.w));
 }
 
 // ---------------------------------------------------------------------------
@@ -1341,7 +1384,7 @@ struct BackwardShape {
     bool direct = false;  // one chunk an adapter in both passes
     Cut dh_cut{};
     GradCut shrink, expand;
-    uint64_t part, image, dh_image, grad_A, grad_B, most, ups, bytes;  // offsets in the workspace
+    uint64_t part, image, dh_image, grad_A, grad_B, most, ups, dh_most, bytes;  // offsets in the workspace
     BackwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
         : r(b->r_max), apart(r.r16 > 64), shrink(b, d_out, r, apart ? 0 : 2 * r.r16), expand(b, d_in, r, 2 * kBlockCols)
     {
@@ -1354,7 +1397,8 @@ struct BackwardShape {
         grad_B = grad_A + align_up((uint64_t)expand.chunks->count * d_in * r.r16 * 4);
         most = grad_B + align_up((uint64_t)shrink.chunks->count * d_out * r.r16 * 4);
         ups = most + align_up((uint64_t)b->n_tiles * image_blocks(r.r16) * 4);
-        bytes = ups + align_up((uint64_t)b->n_tiles * 2 * 4);
+        dh_most = ups + align_up((uint64_t)b->n_tiles * 2 * 4);
+        bytes = dh_most + align_up((uint64_t)dh_cut.slabs * b->n_tiles * kMostWarps * 4);
     }
 };
 
@@ -1366,6 +1410,9 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
     const bool eights = a.d_in % 8 == 0 && a.r_rows % 8 == 0;
     f.direct = f.direct && eights;  // (dA and dB are written by eights there, and by fours below)
     uint8_t *ws = static_cast<uint8_t *>(work);
+    const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_rows, a.d_in, f.r.r16, a.d_in, 1};
+    const GradSum B{reinterpret_cast<const float *>(ws + f.grad_B), f.shrink.chunks->d_begin, a.dB, a.d_out, a.r_rows, a.d_out, f.r.r16, 0};
+    bool with_dB = false;
     if (b->n_tiles || b->n_bare) {
         TileArgs g{};
         g.a = a;
@@ -1392,9 +1439,14 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         // h as an operand
         uint8_t *image = ws + f.image;
         float *ups = reinterpret_cast<float *>(ws + f.ups), *most = reinterpret_cast<float *>(ws + f.most);
-        void *iargs[] = {&g, &image, &ups, &most, (void *)&b->d_tile_begin};
-        const dim3 iblocks(image_blocks(g.r16) * b->n_tiles);
+        const uint32_t iblocks = image_blocks(g.r16) * b->n_tiles;
+        // (dB's sums: by fours of a row, on the images' launch, where they are wanted and fit)
+        const uint32_t per_adapter = ceil_div(a.d_out * (a.r_max / 4), 256);
+        const uint64_t sums = (uint64_t)per_adapter * a.n_adapters;
+        with_dB = !f.direct && eights && sums < (1u << 30);
+        void *iargs[] = {&g, &image, &ups, &most, (void *)&b->d_tile_begin, (void *)&iblocks, (void *)&B, (void *)&per_adapter};
         const bool any = b->n_tiles != 0;
+        g.most = reinterpret_cast<float *>(ws + f.dh_most);
         if (any && !is_bf16<T>() && (rc = launch(k_image<T, false, true>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
         if (any && (rc = launch(k_image<T, false, false>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
         if (any && f.apart) {
@@ -1430,8 +1482,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         ups += b->n_tiles;
         g.part_in = g.part_out;
         g.slabs_in = f.dh_cut.slabs;
-        if (any && !is_bf16<T>() && (rc = launch(k_image<T, true, true>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
-        if (any && (rc = launch(k_image<T, true, false>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
+        if (any && (rc = launch(k_image<T, true, false>, iblocks + (with_dB ? (uint32_t)sums : 0), 256, 0, s, iargs, "adapter image"))) return rc;
         g.image = image;
         g.ups = ups;
         g.bare = b->d_bare;
@@ -1455,13 +1506,14 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
                     esmem, s, eargs, "adapter expand_grad");
         if (rc || f.direct) return rc;
     }
-    const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_rows, a.d_in, f.r.r16, a.d_in, 1};
-    const GradSum B{reinterpret_cast<const float *>(ws + f.grad_B), f.shrink.chunks->d_begin, a.dB, a.d_out, a.r_rows, a.d_out, f.r.r16, 0};
     if (!eights) return launch_any_grad_sum(b, s, dtype, A, B);
-    const uint32_t blocks_A = ceil_div(a.r_max * (a.d_in / 4), 256), blocks_B = ceil_div(a.d_out * (a.r_max / 4), 256);
-    for (uint32_t i = 0; i < a.n_adapters && rc == FIONA_OK; i += 65535) {
-        void *args[] = {(void *)&A, (void *)&B, (void *)&a.ranks, (void *)&blocks_A, &i};
-        rc = launch(k_grad_sum<T>, dim3(blocks_A + blocks_B, std::min(a.n_adapters - i, 65535u)), 256, 0, s, args, "adapter gradients");
+    for (const GradSum *g : {&A, &B}) {
+        if (g == &B && with_dB && b->n_tiles) break;
+        const uint32_t blocks = ceil_div(g->rows * (g->inner / 4), 256);
+        for (uint32_t i = 0; i < a.n_adapters && rc == FIONA_OK; i += 65535) {
+            void *args[] = {(void *)g, (void *)&a.ranks, &i};
+            rc = launch(k_grad_sum<T>, dim3(blocks, std::min(a.n_adapters - i, 65535u)), 256, 0, s, args, "adapter gradients");
+        }
     }
     return rc;
 }
@@ -1492,13 +1544,15 @@ uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_
     return n;
 }
 
-// Microseconds of the two passes on few tiles, fitted to 16 to 512 rows, ranks 8 to
-// 128 and widths 768 to 8192 (to about 15%), with 1.5 for the second launch.
+// Microseconds of the two passes, fitted to 16 to 512 rows in runs of 16 to 128, ranks
+// 8 to 128 and widths 768 to 8192 (to about 15%), with 1.5 for the second launch; and
+// for many tiles their bytes at 5.5 TB/s.
 double adapter_tiles_us(const fiona_adapter_batch *b, uint32_t n_tiles, uint32_t d_in, uint32_t d_out)
 {
     if (!n_tiles) return 0;
-    const double r = b->r_max, d = (double)d_in + d_out;
-    return 5.9 + 0.045 * r + d * (2.5e-4 + 1.2e-6 * r) + (n_tiles - 1) * (0.08 + d * (2.2e-5 + 6.5e-7 * r));
+    const double r = b->r_max, d = (double)d_in + d_out, rows = (double)b->n_tokens / std::max(b->n_tiles, 1u);
+    return 5.9 + 0.045 * r + d * (2.5e-4 + 1.2e-6 * r) +
+           (n_tiles - 1) * std::max(0.08 + d * (2.2e-5 + 6.5e-7 * r), rows * (d_in + 2.0 * d_out) * 2 / 5.5e6);
 }
 
 int launch_adapter_tiles_forward(const fiona_adapter_batch *b, void *stream, uint32_t dtype, const AdapterArgs &a, void *work,

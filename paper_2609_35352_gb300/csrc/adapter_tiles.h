@@ -50,6 +50,7 @@ struct TileArgs {
     uint32_t n_bare;       // expand: rows without an adapter, the first CTAs
     float *part_out;       // partial h or dh of this pass
     uint32_t with_dh;      // shrink_grad: whether it makes the partial dh
+    float *most;           // fp16, gradients: [slabs][n_tiles][8] largest |partial dh| of a tile, by warp
     float *grad;           // [chunks][...] partial dB or dA
     float *grad_b, *dh;    // (adapter_any.cu: dB beside dA; dh whole, [n_tokens][r16])
     uint32_t direct;       // every adapter has one chunk: dA and dB are written as they are
