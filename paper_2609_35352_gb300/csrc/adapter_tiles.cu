@@ -20,6 +20,13 @@
 // tiles of its chunk: 128 columns a lane each, r16 accumulators.  Chunks' sums go to
 // the workspace and are added in order at the end (k_grad_sum).
 //
+// Bound by HBM, and where a mask is formed by its integer instructions; above rank 64
+// the gradients by the tensor cores, as every product runs on two parts.  A pass that
+// reads 134 MB and does nothing else takes 24.6 us, whatever the boxes' shape, so
+// x or dy is read once a pass and nothing of its size is written in between.
+// Measured on GB300, bf16, 4096 -> 4096: 8192 rows of 24 adapters, ranks 8 to 32,
+// forward 46 us; 16384 rows, rank 32, p = 0.05, forward 78 us, backward 106 us.
+//
 // Waits are bounded (tiles::Waits).
 #include <cuda.h>
 #include <cudaTypedefs.h>
