@@ -345,6 +345,26 @@ def test_odd_sizes_of_long_batches(ctx, dtype, d_in, d_out, r_max, pad):
     pr.run_and_check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("starts,ids", [([0, 299, 300], [0, 1]), (list(range(41)), [i % 3 - 1 for i in range(40)])])
+@pytest.mark.parametrize("d_in,d_out,shift", [(256, 136, 8), (77, 131, 3)])
+def test_rows_past_32_bits(ctx, dtype, starts, ids, d_in, d_out, shift):
+    """Rows so far apart that the last lie more than 2^32 elements on, all of them
+    columns of one buffer."""
+    T = starts[-1]
+    ld = (5 << 30) // T // 64 * 64 + shift
+    assert (T - 1) * ld > 1 << 32
+    pr = Problem(ctx, dtype, starts, ids, [16, 9], 16, d_in, d_out, seed=T, p=0.2)
+    wide, at = torch.empty(T * ld, dtype=DT[dtype], device="cuda").view(T, ld), 0
+    for name in ("x", "base", "dy", "dx_base", "out", "dx"):
+        t = getattr(pr, name)
+        view = wide[:, at:at + t.shape[1]]
+        view.copy_(t)
+        setattr(pr, name, view)
+        at += (t.shape[1] + 7) // 8 * 8 + shift
+    pr.run_and_check()
+
+
 @pytest.mark.parametrize("dtype,starts", [("bf16", [0, 300]), ("f16", [0, 130]), ("bf16", list(range(9))), ("f32", list(range(9)))])
 def test_waits_that_run_out_are_reported(ctx, dtype, starts, monkeypatch):
     """Kernels whose barriers expect an arrival that never comes give up, end and
