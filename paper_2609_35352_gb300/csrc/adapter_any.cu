@@ -30,6 +30,20 @@ constexpr uint32_t kCols = 64;   // of an output tile, and of a weight gradient'
 constexpr uint32_t kSlice = 32;  // of the sum's axis
 constexpr uint32_t kPad = 4;
 
+// V consecutive values (1, 2 or 4) to shared memory in one store: a lane a row, so
+// that values one by one would fall on 8 of the 32 banks (4096 fp32 rows, 2048 -> 2048,
+// rank 16, forward: 57 us so, for 50).
+template <uint32_t V>
+__device__ __forceinline__ void put(float *p, const float *v)
+{
+    if constexpr (V == 4)
+        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else if constexpr (V == 2)
+        *reinterpret_cast<float2 *>(p) = make_float2(v[0], v[1]);
+    else
+        *p = v[0];
+}
+
 // A block's 64 x (NRG * RPT) sums: thread (16 groups of 4, NRG groups of RPT ranks,
 // KS shares of each slice).
 template <uint32_t NRG, uint32_t RPT>
@@ -114,19 +128,23 @@ __global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
     const T *x = BACK ? (const T *)g.a.dy : (const T *)g.a.x;
     const uint64_t ld = BACK ? g.a.ld_dy : g.a.ldx;
     const T *W = BACK ? (const T *)g.a.B + (size_t)t.adapter * g.a.d_out * g.a.r_max : (const T *)g.a.A + (size_t)t.adapter * g.a.r_max * g.a.d_in;
-    constexpr uint32_t kX = kRows / kWarps, kW = BACK ? kSlice / kWarps * ((kRanks + 31) / 32) : (kRanks + kWarps - 1) / kWarps;
+    constexpr uint32_t kX = kRows / kWarps, kW = BACK ? kSlice / kWarps * ((kRanks + 31) / 32) : kRanks / kWarps;
+    // a warp's q-th row of x and rank of A: runs of up to four
+    constexpr uint32_t kRun = BACK || kW > 4 ? 4 : kW;
+    auto row_of = [&](uint32_t q) { return (warp + q / 4 * kWarps) * 4 + q % 4; };
+    auto rank_of = [&](uint32_t q) { return (warp + q / kRun * kWarps) * kRun + q % kRun; };
     float fx0[kX], fw0[kW], fx1[kX], fw1[kW];
     auto fetch = [&](uint32_t k, float (&fx)[kX], float (&fw)[kW]) {
         const uint32_t col = k + lane;
 #pragma unroll
         for (uint32_t q = 0; q < kX; ++q) {
-            const uint32_t r = warp + q * kWarps;
+            const uint32_t r = row_of(q);
             fx[q] = element(x + (uint64_t)(row0 + r) * ld + col, r < rows && col < k1);
         }
 #pragma unroll
         for (uint32_t q = 0; q < kW; ++q) {
             if (!BACK) {
-                const uint32_t j = warp + q * kWarps;
+                const uint32_t j = rank_of(q);
                 fw[q] = element(W + (size_t)j * g.a.d_in + col, j < rank && col < k1);
             } else {
                 const uint32_t i = k + warp + q % (kSlice / kWarps) * kWarps, j = lane + q / (kSlice / kWarps) * 32;
@@ -139,14 +157,14 @@ __global__ void __launch_bounds__(kThreads) k_any_shrink(const TileArgs g)
         __syncthreads();
 #pragma unroll
         for (uint32_t q = 0; q < kX; ++q) {
-            const uint32_t r = warp + q * kWarps;
-            const bool drop = !BACK && g.a.mask.level && k + lane < k1 && !g.a.mask.keep(row0 + r, k + lane);
-            sm.f.X[lane][r] = drop ? 0.f : fx[q];
+            const bool drop = !BACK && g.a.mask.level && k + lane < k1 && !g.a.mask.keep(row0 + row_of(q), k + lane);
+            if (drop) fx[q] = 0.f;
+            if (q % 4 == 3) put<4>(&sm.f.X[lane][row_of(q - 3)], &fx[q - 3]);
         }
 #pragma unroll
         for (uint32_t q = 0; q < kW; ++q) {
             if (!BACK) {
-                if (warp + q * kWarps < kRanks) sm.f.S[lane][warp + q * kWarps] = fw[q];
+                if (q % kRun == kRun - 1) put<kRun>(&sm.f.S[lane][rank_of(q + 1 - kRun)], &fw[q + 1 - kRun]);
             } else {
                 const uint32_t j = lane + q / (kSlice / kWarps) * 32;
                 if (j < kRanks) sm.f.S[warp + q % (kSlice / kWarps) * kWarps][j] = fw[q];
@@ -221,6 +239,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_any_expand(const TileArgs g)
             base[i] = r < rows && my_col < g.cols ? ((const T *)g.a.base)[(uint64_t)(row0 + r) * g.a.ld_base + my_col] : narrow<T>(0.f);
         }
     float acc[4][4] = {}, fw[kSlice * kCols / kThreads];
+    auto col_of = [&](uint32_t q) { return (warp + q / 4 * kWarps) * 4 + q % 4; };
     auto fetch = [&](uint32_t j0) {
 #pragma unroll
         for (uint32_t q = 0; q < kSlice * kCols / kThreads; ++q) {
@@ -228,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_any_expand(const TileArgs g)
                 const uint32_t j = j0 + warp + q / 2 * kWarps, i = col0 + lane + q % 2 * 32;
                 fw[q] = element(W + (size_t)j * g.a.d_in + i, j < rank && i < g.cols);
             } else {
-                const uint32_t j = j0 + lane, i = col0 + warp + q * kWarps;
+                const uint32_t j = j0 + lane, i = col0 + col_of(q);
                 fw[q] = element(W + (size_t)i * g.a.r_max + j, j < rank && i < g.cols);
             }
         }
@@ -260,8 +279,8 @@ __global__ void __launch_bounds__(kThreads, 3) k_any_expand(const TileArgs g)
         for (uint32_t q = 0; q < kSlice * kCols / kThreads; ++q) {
             if (BACK)
                 sm.f.S[warp + q / 2 * kWarps][lane + q % 2 * 32] = fw[q];
-            else
-                sm.f.S[lane][warp + q * kWarps] = fw[q];
+            else if (q % 4 == 3)
+                put<4>(&sm.f.S[lane][col_of(q - 3)], &fw[q - 3]);
         }
         if (j0 + kSlice < rank) fetch(j0 + kSlice);
         __syncthreads();
