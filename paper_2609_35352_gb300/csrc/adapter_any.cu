@@ -11,9 +11,9 @@
 // and are added up at the end.  Loads are element by element along the rows, two
 // slices ahead of the multiplications.
 //
-// Bound by the FMA units at high ranks (26 to 28 TFLOP/s at rank 128); at low ones by
+// Bound by the FMA units at high ranks (27 to 30 TFLOP/s at rank 128); at low ones by
 // the latency of a few slices and launches.  Measured on GB300, fp32: 2048 rows,
-// 1024 -> 1024, rank 16, forward 18 us; 768 -> 768, rank 8, backward 30 us.
+// 1024 -> 1024, rank 16, forward 17 us; 768 -> 768, rank 8, backward 29 us.
 #include <cuda_runtime.h>
 
 #include <algorithm>
