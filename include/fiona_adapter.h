@@ -39,7 +39,11 @@
  *
  * Arithmetic: sums in fp32.  16-bit products are exact and go to the tensor
  * cores; h and dh, where they are an operand of the second product, go there
- * as two 16-bit parts (about 16 bits), and an output is rounded once.  Results
+ * as two 16-bit parts (about 16 bits), and an output is rounded once.  The
+ * tensor cores' accumulator cuts an addition where fp32 would round it: chains
+ * of such additions are bounded, whatever the sizes, so that a sum loses at most
+ * some 2^-16 (dA and dB: 2^-15) of its terms' absolute values; the chains are
+ * added up in fp32.  Results
  * do not depend on the order in which blocks run: no atomics on values.
  *
  * Dropout D on a [rows][cols] matrix, for a probability p in [0, 1]: with

@@ -24,9 +24,9 @@ constexpr uint32_t kAdapterRows = 4;
 struct AdapterRows {
     uint32_t adapter, count, row[kAdapterRows];
 };
-// The tiles cut into chunks of at most `size`.
+// The tiles cut into chunks of at most `size`; the most tiles that one has.
 struct AdapterChunks {
-    uint32_t size = 0, count = 0;
+    uint32_t size = 0, longest = 0, count = 0;
     const AdapterChunk *d_chunks = nullptr;
     const uint32_t *d_begin = nullptr;  // [n_adapters + 1] into d_chunks
 };

@@ -253,7 +253,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
             for (uint32_t t = tile_begin[a]; t < tile_begin[a + 1]; t += size) c.push_back({a, t, std::min(t + size, tile_begin[a + 1])});
         }
         chunks.back().second.push_back((uint32_t)c.size());
-        b->chunks.push_back({size, (uint32_t)c.size(), nullptr, nullptr});
+        b->chunks.push_back({size, std::min(size, most), (uint32_t)c.size(), nullptr, nullptr});
         if (size >= most) break;
     }
 

@@ -223,6 +223,19 @@ __device__ __forceinline__ void put_most(const TileArgs &g, uint32_t slab, uint3
 constexpr uint32_t kShrinkThreads = 320;  // TMA, MMA, eight that mask and store
 constexpr uint32_t kMaxStages = 8;
 
+// Additions (of sixteen products each) that an accumulator takes before its sum goes to
+// one that rounds.  Each cuts some 1e-7 of a sum whose terms have one sign (measured in
+// longer chains: h of 2^20 columns 1.5e-3 off at rank 8, 16384 additions, 3.0e-3 at
+// rank 72, 32768; dA and dB of 2^25 rows 1.4e-3 off at rank 64, 13800).  So 128 of them
+// for h and dh, a loss of 1.3e-5 at most; and the tiles of a chunk for dA and dB, 32, a
+// loss of 3e-5, about a tenth of fp16's own rounding (a tile adds eight times, or
+// sixteen, half of them low parts).  With 16 tiles the gradient of 4096 rows,
+// 2048 -> 8192, rank 128 took 82.4 us for 78.0.
+constexpr uint32_t kShrinkChain = 128, kGradTiles = 32;
+
+// accumulators of a shrink, taken by its boxes in turn
+__host__ __device__ constexpr uint32_t shrink_accs(uint32_t r16) { return r16 <= 64 ? 4 : 2; }
+
 // (BACK: partial dh = dy B, for ranks above 64: shrink_grad's accumulators of dB
 // leave it a range of 256 columns then, whose partial dh is as large as its dy)
 template <bool BACK>
@@ -246,8 +259,9 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
     const uint32_t stage = shrink_stage<BACK>(g.r16, g.blocks);
     // The accumulator cuts every addition to fp32 toward zero: boxes go to several
     // in turn, for chains a few times shorter (one chain of 128 additions erred by
-    // 2.1e-6 of h, two fp32 dot products by 1.1e-6)
-    const uint32_t accs = g.r16 <= 64 ? 4 : 2, cols = g.r16 <= 16 ? 64 : g.r16 <= 32 ? 128 : 256;
+    // 2.1e-6 of h, two fp32 dot products by 1.1e-6), and a range is short enough
+    // (kShrinkChain)
+    const uint32_t accs = shrink_accs(g.r16), cols = g.r16 <= 16 ? 64 : g.r16 <= 32 ? 128 : 256;
     const AdapterTile t = g.tiles[blockIdx.x / g.cut.slabs];
     const uint32_t slab = blockIdx.x % g.cut.slabs;
     const uint32_t b0 = slab * g.cut.width, n = min(g.boxes - b0, g.cut.width);
@@ -1264,14 +1278,19 @@ int tensor_map(CUtensorMap *tm, uint32_t dtype, const void *p, uint64_t cols, ui
 // CTAs; where the ranges' partial sums are read by every CTA of the pass that follows
 // (r16 ranks, 0: they are not), no more than balances the two: a box takes a CTA
 // some 0.35 us and a range's partial sums of 128 rows some 0.008 us a rank (measured on
-// 256 rows: 64 ranges of one box took 35 us, 9 ranges 14).
-Cut cut_columns(uint32_t boxes, uint32_t units, uint32_t want, uint32_t r16)
+// 256 rows: 64 ranges of one box took 35 us, 9 ranges 14).  No range has more than `most`
+// boxes.
+Cut cut_columns(uint32_t boxes, uint32_t units, uint32_t want, uint32_t r16, uint32_t most)
 {
     uint32_t slabs = std::max(1u, std::min(boxes, want / std::max(units, 1u)));
     if (r16) slabs = std::min(slabs, (uint32_t)std::ceil(std::sqrt(boxes * 0.35 / (0.008 * r16))));
+    slabs = std::max(slabs, ceil_div(boxes, most));
     const uint32_t width = ceil_div(boxes, slabs);
     return Cut{width, ceil_div(boxes, width)};
 }
+
+// boxes of a range of a shrink: its accumulators take four additions a box, in turn
+uint32_t shrink_most(uint32_t r16) { return kShrinkChain / 4 * shrink_accs(r16); }
 
 struct ForwardShape {
     RankShape r;
@@ -1279,8 +1298,8 @@ struct ForwardShape {
     ForwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out, uint32_t n_tiles) : r(b->r_max)
     {
         const uint32_t resident = 2 * (uint32_t)std::max(b->ctx->sm_count, 1);
-        shrink = cut_columns(ceil_div(d_in, 64), n_tiles, resident, r.r16);
-        expand = cut_columns(ceil_div(d_out, 64), n_tiles, resident, 0);
+        shrink = cut_columns(ceil_div(d_in, 64), n_tiles, resident, r.r16, shrink_most(r.r16));
+        expand = cut_columns(ceil_div(d_out, 64), n_tiles, resident, 0, ceil_div(d_out, 64));
     }
     uint64_t part_bytes(const fiona_adapter_batch *b) const
     {
@@ -1369,6 +1388,7 @@ struct GradCut {
         double best = 0;
         for (uint32_t width = most; width >= 1; --width)
             for (const AdapterChunks &c : b->chunks) {
+                if (c.longest > kGradTiles) continue;
                 const uint32_t slabs = ceil_div(n, width);
                 const double waves = ceil_div(c.count * slabs, sms);
                 const double block = r.r16 <= 32 ? 1.1 : r.r16 <= 64 ? 1.6 : 2.4;
@@ -1395,7 +1415,7 @@ struct BackwardShape {
     BackwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
         : r(b->r_max), apart(r.r16 > 64), shrink(b, d_out, r, apart ? 0 : 2 * r.r16), expand(b, d_in, r, 2 * kBlockCols)
     {
-        dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1), 0) : shrink.cut;
+        dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1), 0, shrink_most(r.r16)) : shrink.cut;
         direct = shrink.chunks->count + b->n_idle == b->n_adapters && expand.chunks->count + b->n_idle == b->n_adapters;
         part = 0;
         image = part + align_up((uint64_t)dh_cut.slabs * b->n_tokens * r.r16 * 4);
