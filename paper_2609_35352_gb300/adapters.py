@@ -87,6 +87,13 @@ def _whole(t: Any, shape: tuple, dtype: Any, device: Any, name: str) -> int:
     _refuse(t, shape, dtype, device, name)
 
 
+def _workspace(t: Any, device: Any) -> int:
+    """The address of a workspace."""
+    if t is None or t.device != device or not t.is_contiguous():
+        raise ValueError("a contiguous workspace on the context's device expected (Batch.workspace)")
+    return t.data_ptr()
+
+
 _devices: dict = {}
 
 
@@ -171,11 +178,10 @@ class Batch:
         ld_out = _matrix(out, (T, d_out), dt, dev, "out")
         ld_base, p_base = (0, None) if base is None else (_matrix(base, (T, d_out), dt, dev, "base"), base.data_ptr())
         ph = None if h is None else _whole(h, (T, self.r_max), torch.float32, dev, "h")
-        if work is None:
-            raise ValueError("forward needs a workspace (Batch.workspace)")
+        p_work = _workspace(work, dev)
         rc = lib().fiona_adapter_forward(self.handle, _handle(stream), layer, x.data_ptr(), ldx, p_base, ld_base,
                                          out.data_ptr(), ld_out, ph, None if dropout is None else dropout._spec,
-                                         work.data_ptr(), work.nbytes)
+                                         p_work, work.nbytes)
         if rc:
             F._check(rc, "fiona_adapter_forward")
 
@@ -192,11 +198,10 @@ class Batch:
         ph = _whole(h, (T, self.r_max), torch.float32, dev, "h")
         pA = _whole(dA, A.shape, dt, dev, "dA")
         pB = _whole(dB, B.shape, dt, dev, "dB")
-        if work is None:
-            raise ValueError("backward needs a workspace (Batch.workspace)")
+        p_work = _workspace(work, dev)
         rc = lib().fiona_adapter_backward(self.handle, _handle(stream), layer, x.data_ptr(), ldx, ph, dy.data_ptr(),
                                           ld_dy, p_base, ld_base, dx.data_ptr(), ld_dx, pA, pB,
-                                          None if dropout is None else dropout._spec, work.data_ptr(), work.nbytes)
+                                          None if dropout is None else dropout._spec, p_work, work.nbytes)
         if rc:
             F._check(rc, "fiona_adapter_backward")
 
