@@ -122,6 +122,17 @@ def _handle(stream: Any) -> int:
     return 0 if stream is None else stream if type(stream) is int else stream.cuda_stream
 
 
+def _indices(values: Any, dtype: Any, name: str) -> np.ndarray:
+    """Whole numbers as a C array (numpy would wrap what does not fit, and cut fractions)."""
+    v, limits = np.asarray(values), np.iinfo(dtype)
+    if v.size == 0:
+        return np.zeros(v.shape, dtype)
+    top = limits.max if v.dtype.kind in "iu" else min(limits.max, 1 << 53)
+    if v.dtype.kind not in "iuf" or not (v.min() >= limits.min and v.max() <= top) or (v != np.floor(v)).any():
+        raise ValueError("%s: whole numbers from %d to %d expected" % (name, limits.min, limits.max))
+    return np.ascontiguousarray(v.astype(dtype))
+
+
 class Batch:
     """fiona_adapter_batch: request r owns the rows starts[r] to starts[r + 1] and
     uses adapter adapters[r] (-1: none); adapter a has rank ranks[a] and scale
@@ -129,9 +140,9 @@ class Batch:
 
     def __init__(self, ctx: F.Context, starts: Sequence[int], adapters: Sequence[int], ranks: Sequence[int],
                  r_max: int, scales: Optional[Sequence[float]] = None):
-        s = np.ascontiguousarray(np.asarray(starts, dtype=np.uint64))
-        a = np.ascontiguousarray(np.asarray(adapters, dtype=np.int32))
-        r = np.ascontiguousarray(np.asarray(ranks, dtype=np.uint32))
+        s, a, r = (_indices(v, t, n) for v, t, n in ((starts, np.uint64, "starts"), (adapters, np.int32, "adapters"),
+                                                     (ranks, np.uint32, "ranks")))
+        r_max = int(_indices([r_max], np.uint32, "r_max")[0])
         if s.ndim != 1 or a.ndim != 1 or r.ndim != 1 or s.shape[0] != a.shape[0] + 1:
             raise ValueError("starts must have one entry more than adapters")
         c = None
@@ -141,10 +152,10 @@ class Batch:
                 raise ValueError("one scale per adapter expected")
         h = ctypes.c_void_p()
         F._check(lib().fiona_adapter_batch_create(ctx.handle, a.shape[0], s.ctypes.data, a.ctypes.data, r.shape[0],
-                                                  r.ctypes.data, None if c is None else c.ctypes.data, int(r_max),
+                                                  r.ctypes.data, None if c is None else c.ctypes.data, r_max,
                                                   ctypes.byref(h)), "fiona_adapter_batch_create")
         self.ctx, self.handle = ctx, h
-        self.n_tokens, self.n_adapters, self.r_max = int(s[-1]), int(r.shape[0]), int(r_max)
+        self.n_tokens, self.n_adapters, self.r_max = int(s[-1]), int(r.shape[0]), r_max
         self._dev = _device(ctx)
 
     def work_bytes(self, d_in: int, d_out: int, dtype: Any) -> int:

@@ -56,3 +56,18 @@ def test_workspaces(batch, backward):
     batch._dev = torch.device("meta")
     with pytest.raises(ValueError):
         call(batch, backward, aligned(n, dtype=torch.uint8))
+
+
+def test_indices_are_taken_as_they_are(ctx):
+    """Whole numbers that the C arrays cannot hold are refused, not wrapped or cut."""
+    import numpy as np
+    good = dict(starts=[0, 3, 5], adapters=[0, -1], ranks=[4, 8], r_max=8)
+    AD.Batch(ctx, **good)
+    AD.Batch(ctx, **{k: np.array(v) if k != "r_max" else v for k, v in good.items()})
+    AD.Batch(ctx, np.array([0.0, 3.0, 5.0]), [0, -1], torch.tensor([4, 8]), 8)
+    AD.Batch(ctx, [0], [], [], 8)
+    for change in (dict(adapters=np.array([1 << 32, -1])), dict(adapters=[0.5, -1]), dict(ranks=np.array([(1 << 32) + 4, 8])),
+                   dict(ranks=np.array([4, -(1 << 32)])), dict(starts=np.array([0, 3.5, 5])), dict(starts=[0, float("nan"), 5]),
+                   dict(starts=[0, -1, 5]), dict(adapters=[1 << 40, -1]), dict(ranks=["a", 8]), dict(r_max=8.5)):
+        with pytest.raises(ValueError):
+            AD.Batch(ctx, **dict(good, **change))
