@@ -10,6 +10,7 @@
 
 #include "adapter_tiles.h"
 #include "device_guard.h"
+#include "upload.h"
 
 namespace {
 
@@ -282,7 +283,7 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
         for (const auto &c : chunks)
             o_chunks.emplace_back(put(c.first.data(), c.first.size() * sizeof(AdapterChunk)), put(c.second.data(), c.second.size() * 4));
         cudaError_t e = cudaMalloc(&b->blob, image.size());
-        if (e == cudaSuccess) e = cudaMemcpy(b->blob, image.data(), image.size(), cudaMemcpyHostToDevice);
+        if (e == cudaSuccess) e = upload(b->blob, image.data(), image.size());
         if (e != cudaSuccess) return cuda_fail(e, who);
         const uint8_t *d = static_cast<const uint8_t *>(b->blob);
         b->d_ranks = reinterpret_cast<const uint32_t *>(d + o_ranks);

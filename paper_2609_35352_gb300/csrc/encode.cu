@@ -40,6 +40,7 @@
 
 #include "fiona_internal.h"
 #include "ntt.cuh"
+#include "upload.h"
 
 using namespace fiona_ntt;
 
@@ -253,7 +254,7 @@ int build_encode_tables(const fiona_ctx *ctx)
     void *dev = nullptr;
     cudaError_t err = cudaMalloc(&dev, off.total);
     if (err != cudaSuccess) return set_error(FIONA_ERR_NOMEM, "encode tables: %s", cudaGetErrorString(err));
-    err = cudaMemcpy(dev, host.data(), off.total, cudaMemcpyHostToDevice);
+    err = upload(dev, host.data(), off.total);
     if (err != cudaSuccess) {
         cudaFree(dev);
         return set_error(FIONA_ERR_CUDA, "encode tables: %s", cudaGetErrorString(err));

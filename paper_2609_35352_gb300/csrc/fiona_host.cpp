@@ -15,6 +15,7 @@
 #include "fiona_internal.h"
 #include "gemm.h"
 #include "tiled.h"
+#include "upload.h"
 
 typedef unsigned __int128 u128;
 
@@ -189,8 +190,7 @@ extern "C" int fiona_ctx_create(uint32_t N, const uint64_t *moduli, uint32_t L, 
         if (e == cudaSuccess) e = cudaMalloc(&ctx->d_kerr, sizeof(int));
         if (e == cudaSuccess) e = cudaMemset(ctx->d_kerr, 0, sizeof(int));
         if (e == cudaSuccess)
-            e = cudaMemcpy(ctx->d_limbs, ctx->limbs.data(), sizeof(LimbConst) * L,
-                           cudaMemcpyHostToDevice);
+            e = upload(ctx->d_limbs, ctx->limbs.data(), sizeof(LimbConst) * L);
         if (e != cudaSuccess) {
             cudaFree(ctx->d_limbs);
             cudaFree(ctx->d_flag);
@@ -435,7 +435,7 @@ static int upload(fiona_plan *p, const std::vector<std::pair<const void *, size_
     cudaError_t e = cudaMalloc(&p->sched.blob, total);
     if (e != cudaSuccess) return set_error(FIONA_ERR_NOMEM, "schedule upload: %s", cudaGetErrorString(e));
     p->sched.bytes = total;
-    e = cudaMemcpy(p->sched.blob, host.data(), total, cudaMemcpyHostToDevice);
+    e = upload(p->sched.blob, host.data(), total);
     if (e != cudaSuccess) return cuda_fail(e, "schedule upload");
     return FIONA_OK;
 }

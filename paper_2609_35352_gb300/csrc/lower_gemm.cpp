@@ -8,6 +8,7 @@
 #include <set>
 
 #include "gemm.h"
+#include "upload.h"
 
 int gemm_configure(size_t smem);  // kernel_gemm.cu
 
@@ -134,7 +135,7 @@ int lower_gemm(fiona_plan *p)
     cudaError_t e = cudaMalloc(&g->sched.blob, blob.size());
     if (e != cudaSuccess) return set_error(FIONA_ERR_NOMEM, "matrix kernel schedule: %s", cudaGetErrorString(e));
     g->sched.bytes = blob.size();
-    e = cudaMemcpy(g->sched.blob, blob.data(), blob.size(), cudaMemcpyHostToDevice);
+    e = upload(g->sched.blob, blob.data(), blob.size());
     if (e != cudaSuccess) return set_error(FIONA_ERR_CUDA, "matrix kernel schedule: %s", cudaGetErrorString(e));
     const uint8_t *d = static_cast<const uint8_t *>(g->sched.blob);
     a.raw = reinterpret_cast<const GemmTerm *>(d + o_raw);

@@ -33,6 +33,7 @@
 #include <tuple>
 
 #include "tiled.h"
+#include "upload.h"
 
 namespace {
 
@@ -1207,7 +1208,7 @@ int upload_blob(TiledSchedule *ts, const std::vector<uint32_t> &words)
     cudaError_t e = cudaMalloc(&ts->sched.blob, bytes);
     if (e != cudaSuccess) return set_error(FIONA_ERR_NOMEM, "tiled schedule: %s", cudaGetErrorString(e));
     ts->sched.bytes = bytes;
-    e = cudaMemcpy(ts->sched.blob, words.data(), words.size() * 4, cudaMemcpyHostToDevice);
+    e = upload(ts->sched.blob, words.data(), words.size() * 4);
     if (e != cudaSuccess) return set_error(FIONA_ERR_CUDA, "tiled schedule: %s", cudaGetErrorString(e));
     return FIONA_OK;
 }

@@ -35,6 +35,7 @@
 
 #include "fiona_internal.h"
 #include "ntt.cuh"
+#include "upload.h"
 
 using namespace fiona_ntt;
 
@@ -324,7 +325,7 @@ int build_tables(const fiona_ctx *ctx)
         T.mu64 = ~(uint64_t)0 / q;
         T.ninv = twiddle(powm(N % q, q - 2, q), q);
     }
-    e = cudaMemcpy(dev, host.data(), bytes, cudaMemcpyHostToDevice);
+    e = upload(dev, host.data(), bytes);
     if (e != cudaSuccess) {
         cudaFree(dev);
         return set_error(FIONA_ERR_CUDA, "rescale tables: %s", cudaGetErrorString(e));
