@@ -367,6 +367,14 @@ __device__ __forceinline__ void rows_body(const RowsArgs &g, const AdapterRows &
         case 4: outputs<T, VB, G, 16>(g, rows, B, rank, o0, n_out, sh); break;
         default: outputs<T, VB, G, 32>(g, rows, B, rank, o0, n_out, sh); break;
     }
+    // A CTA that gave up may be one that others are still to push to: it stays until each
+    // of them has ended or given up too (the barrier does not wait for what has exited,
+    // so the others need not come to it).
+    if (*(volatile int *)&sh.abort) {  // (the same for all: the last wait is behind)
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    }
 }
 
 // MOST: the largest group of the batch
