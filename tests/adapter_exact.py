@@ -13,7 +13,8 @@ BITS = {"f32": 24, "f16": 11, "bf16": 8}
 def round_to(dtype, v):
     """v (float64) to the nearest value of the type, ties to even (as float64)."""
     if dtype == "f16":
-        return v.astype(np.float16).astype(np.float64)
+        with np.errstate(over="ignore"):  # (past its range: infinite, in the kernels too)
+            return v.astype(np.float16).astype(np.float64)
     f = v.astype(np.float32)
     if dtype == "f32":
         return f.astype(np.float64)
