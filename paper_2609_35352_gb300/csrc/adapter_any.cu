@@ -484,9 +484,27 @@ int whole_parts(TileArgs &g, uint32_t out_cols, cudaStream_t s)
     if (g.slabs_in == 1 || read < 40000000) return FIONA_OK;
     const uint64_t pieces = (uint64_t)g.a.n_tokens * g.r16 / 4;
     void *args[] = {&g};
-    const int rc = launch(k_any_whole, dim3((uint32_t)((pieces + kThreads - 1) / kThreads)), kThreads, 0, s, args, "adapter sums");
+    const int rc = launch(k_any_whole, (pieces + kThreads - 1) / kThreads, kThreads, 0, s, args, "adapter sums");
     g.slabs_in = 1;
     return rc;
+}
+
+// The expand of all tiles, in as many launches as grids hold their blocks (two for
+// every 64 columns of a tile, however few rows it has: one launch up to 7e10 elements).
+template <typename K>
+int expand_all(K kernel, TileArgs g, cudaStream_t s, const char *what)
+{
+    const uint32_t n_tiles = g.n_tiles;
+    const uint64_t per_tile = 2ull * g.cut.slabs, most = (kMostBlocks - g.n_bare) / per_tile;
+    for (uint32_t first = 0; first < n_tiles || g.n_bare;) {
+        const uint32_t n = (uint32_t)std::min<uint64_t>(n_tiles - first, most);
+        void *args[] = {&g};
+        if (const int rc = launch(kernel, g.n_bare + n * per_tile, kThreads, 0, s, args, what)) return rc;
+        first += n;
+        g.tiles += n;
+        g.n_bare = 0;
+    }
+    return FIONA_OK;
 }
 
 // the largest chunks that still make four blocks an SM
@@ -528,15 +546,14 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a, 
     g.slabs_in = g.cut.slabs;
     void *args[] = {&g};
     int rc = FIONA_OK;
-    if (g.n_tiles && (rc = launch(pick_shrink<T, false>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter shrink")))
+    if (g.n_tiles && (rc = launch(pick_shrink<T, false>(a.r_max), 2ull * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter shrink")))
         return rc;
     if (g.n_tiles && (rc = whole_parts(g, a.d_out, s))) return rc;
     g.cols = a.d_out;
     g.cut = Cut{kCols, ceil_div(a.d_out, kCols)};
     g.bare = b->d_bare;
     g.n_bare = b->n_bare;
-    if (!g.n_tiles && !g.n_bare) return FIONA_OK;
-    return launch(k_any_expand<T, false>, g.n_bare + 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter expand");
+    return expand_all(k_any_expand<T, false>, g, s, "adapter expand");
 }
 
 template <typename T>
@@ -573,23 +590,23 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a,
     void *args[] = {&g};
     int rc = FIONA_OK;
     const bool any = b->n_tiles != 0;
-    if (any && (rc = launch(pick_shrink<T, true>(a.r_max), 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter dh"))) return rc;
+    if (any && (rc = launch(pick_shrink<T, true>(a.r_max), 2ull * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter dh"))) return rc;
     if (any && (rc = whole_parts(g, a.d_in, s))) return rc;
     g.cols = a.d_in;
     g.cut = Cut{kCols, ceil_div(a.d_in, kCols)};
     g.bare = b->d_bare;
     g.n_bare = b->n_bare;
-    if ((any || g.n_bare) && (rc = launch(k_any_expand<T, true>, g.n_bare + 2 * g.n_tiles * g.cut.slabs, kThreads, 0, s, args, "adapter dx")))
-        return rc;
+    if ((rc = expand_all(k_any_expand<T, true>, g, s, "adapter dx"))) return rc;
     g.chunks = chunks.d_chunks;
     g.grad = reinterpret_cast<float *>(ws + f.grad_A);
     g.grad_b = reinterpret_cast<float *>(ws + f.grad_B);
     g.direct = any && chunks.count + b->n_idle == b->n_adapters;
     g.idle = b->d_idle;
     g.n_idle = g.direct ? b->n_idle : 0;
-    uint32_t blocks_A = chunks.count * ceil_div(a.d_in, kCols), blocks = blocks_A + chunks.count * ceil_div(a.d_out, kCols);
+    const uint64_t all = (uint64_t)chunks.count * (ceil_div(a.d_in, kCols) + ceil_div(a.d_out, kCols)) + g.n_idle;
+    uint32_t blocks_A = chunks.count * ceil_div(a.d_in, kCols), blocks = (uint32_t)all - g.n_idle;
     void *gargs[] = {&g, &blocks_A, &blocks};
-    if (any && (rc = launch(pick_grad<T>(a.r_max), blocks + g.n_idle, kThreads, 0, s, gargs, "adapter weight gradients"))) return rc;
+    if (any && (rc = launch(pick_grad<T>(a.r_max), all, kThreads, 0, s, gargs, "adapter weight gradients"))) return rc;
     if (g.direct) return rc;
     const GradSum A{g.grad, chunks.d_begin, a.dA, a.r_max, a.d_in, f.r16, a.d_in, 1};
     const GradSum B{g.grad_b, chunks.d_begin, a.dB, a.d_out, a.r_max, a.d_out, f.r16, 0};

@@ -81,9 +81,8 @@ struct Plan {
         if (!list.n) return FIONA_OK;
         const uint64_t units = list.c[list.n - 1].end, blocks = (units + kThreads / 32 - 1) / (kThreads / 32);
         if (blocks == 0) return FIONA_OK;
-        if (blocks >> 31) return set_error(FIONA_ERR_ARG, "adapter: a call of this size needs widths and ranks in multiples of 8");
         void *args[] = {&list};
-        return launch(k_copy, dim3((uint32_t)blocks), kThreads, 0, s, args, "adapter copy");
+        return launch(k_copy, blocks, kThreads, 0, s, args, "adapter copy");
     }
 };
 

@@ -98,6 +98,8 @@ struct GradSum {
 // adapter_any.cu: the sums element by element
 int launch_any_grad_sum(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const GradSum &A, const GradSum &B);
 
+constexpr uint64_t kMostBlocks = 0x7FFFFFFF;  // of a grid
+
 // a kernel that waits for the one before it by itself
 template <typename K>
 inline int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t s, void **args, const char *what)
@@ -115,6 +117,14 @@ inline int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream
     const cudaError_t e = cudaLaunchKernelExC(&c, (const void *)kernel, args);
     if (e != cudaSuccess) return set_error(FIONA_ERR_CUDA, "%s launch: %s", what, cudaGetErrorString(e));
     return FIONA_OK;
+}
+
+// the same for `blocks` in one dimension, which may be more than a grid holds
+template <typename K>
+inline int launch(K kernel, uint64_t blocks, uint32_t threads, size_t smem, cudaStream_t s, void **args, const char *what)
+{
+    if (blocks > kMostBlocks) return set_error(FIONA_ERR_ARG, "%s: %llu blocks", what, (unsigned long long)blocks);
+    return launch(kernel, dim3((uint32_t)blocks), threads, smem, s, args, what);
 }
 
 inline uint64_t align_up(uint64_t n) { return (n + 255) & ~255ull; }

@@ -1353,7 +1353,7 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     const uint32_t stage = shrink_stage<false>(g.r16, g.blocks);
     g.stages = stages_for(0, stage, 3);
     void *sargs[] = {&tx, &tA, &g};
-    if (n_tiles && (rc = launch(k_shrink<T, false>, n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024,
+    if (n_tiles && (rc = launch(k_shrink<T, false>, (uint64_t)n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024,
                                    s, sargs, "adapter shrink")))
         return rc;
     g.bare = b->d_bare;
@@ -1363,7 +1363,7 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     g.boxes = ceil_div(a.d_out, 64);
     g.stages = stages_for(g.op_boxes * kBoxBytes, expand_stage(g.blocks), 3);
     void *eargs[] = {&tbase, &tB, &tout, &tout8, &g};
-    return launch(k_expand<T>, n_tiles * g.cut.slabs + b->n_bare, kExpandThreads,
+    return launch(k_expand<T>, (uint64_t)n_tiles * g.cut.slabs + b->n_bare, kExpandThreads,
                   g.op_boxes * kBoxBytes + (size_t)g.stages * expand_stage(g.blocks) + 1024, s, eargs,
                   "adapter expand");
 }
@@ -1474,8 +1474,8 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         void *iargs[] = {&g, &image, &ups, &most, (void *)&b->d_tile_begin, (void *)&iblocks, (void *)&B, (void *)&per_adapter};
         const bool any = b->n_tiles != 0;
         g.most = reinterpret_cast<float *>(ws + f.dh_most);
-        if (any && !is_bf16<T>() && (rc = launch(k_image<T, false, true>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
-        if (any && (rc = launch(k_image<T, false, false>, iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
+        if (any && !is_bf16<T>() && (rc = launch(k_image<T, false, true>, (uint64_t)iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
+        if (any && (rc = launch(k_image<T, false, false>, (uint64_t)iblocks, 256, 0, s, iargs, "adapter image"))) return rc;
         if (any && f.apart) {
             const uint32_t stage = shrink_stage<true>(g.r16, g.blocks);
             g.cols = a.d_out;
@@ -1483,7 +1483,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
             g.cut = f.dh_cut;
             g.stages = stages_for(0, stage, 3);
             void *args[] = {&tdy, &tB, &g};
-            rc = launch(k_shrink<T, true>, b->n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024, s, args, "adapter dh");
+            rc = launch(k_shrink<T, true>, (uint64_t)b->n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024, s, args, "adapter dh");
             if (rc) return rc;
         }
         g.with_dh = !f.apart;
@@ -1500,7 +1500,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         void *sargs[] = {&tdy, &tB, &g};
         g.image = image;
         g.ups = ups;
-        if (any && (rc = launch(k_shrink_grad<T>, f.shrink.chunks->count * g.cut.slabs, kGradThreads,
+        if (any && (rc = launch(k_shrink_grad<T>, (uint64_t)f.shrink.chunks->count * g.cut.slabs, kGradThreads,
                                 2 * op + (size_t)g.stages * sstage + 1024, s, sargs, "adapter shrink_grad")))
             return rc;
         // dh as an operand (its image in a place of its own: the next kernel starts
@@ -1509,7 +1509,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         ups += b->n_tiles;
         g.part_in = g.part_out;
         g.slabs_in = f.dh_cut.slabs;
-        if (any && (rc = launch(k_image<T, true, false>, iblocks + (with_dB ? (uint32_t)sums : 0), 256, 0, s, iargs, "adapter image"))) return rc;
+        if (any && (rc = launch(k_image<T, true, false>, iblocks + (with_dB ? sums : 0), 256, 0, s, iargs, "adapter image"))) return rc;
         g.image = image;
         g.ups = ups;
         g.bare = b->d_bare;
@@ -1529,7 +1529,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.stages = std::min(kMaxStages, (room - g.buffers * op) / estage);
         const size_t esmem = g.buffers * op + (size_t)g.stages * estage + (a.mask.level ? 2 * kFlagBytes : 0) + 1024;
         void *eargs[] = {&tx, &tA, &tdx, &tdx8, &g};
-        rc = launch(k_expand_grad<T>, g.n_chunks * g.cut.slabs + b->n_bare + g.n_idle, kExpandGradThreads,
+        rc = launch(k_expand_grad<T>, (uint64_t)g.n_chunks * g.cut.slabs + b->n_bare + g.n_idle, kExpandGradThreads,
                     esmem, s, eargs, "adapter expand_grad");
         if (rc || f.direct) return rc;
     }

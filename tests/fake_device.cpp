@@ -1,17 +1,21 @@
 // fake_device.cpp -- the CUDA calls that the adapters' host code makes, on host
-// memory, for tests without a GPU.  A copy from pageable memory is what CUDA
+// memory, for tests without a GPU; linked with the library's own objects.  A copy from pageable memory is what CUDA
 // documents it to be: the source may be reused when the call returns, but the bytes
 // reach their destination only by the next synchronisation (of the legacy default
-// stream, or of the device).  Kernels are not there: launches do nothing.
+// stream, or of the device).  No kernel runs: a launch is checked
+// and written down.
 #include <cuda_runtime.h>
+#include <cuda.h>
 
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <map>
+#include <string>
 #include <vector>
 
-#include "adapter.h"
+#include "adapter_tiles.h"
 
 namespace {
 struct Pending {
@@ -20,6 +24,28 @@ struct Pending {
 };
 std::vector<Pending> g_pending;
 char g_error[512];
+
+struct Launch {
+    std::string name;
+    dim3 grid;
+    size_t smem;
+    TileArgs tiles;  // of the kernels that take one first (adapter_any.cu)
+};
+std::vector<Launch> g_launches;
+std::map<const void *, std::string> &names()
+{
+    static std::map<const void *, std::string> m;
+    return m;
+}
+
+cudaError_t record(const void *func, dim3 grid, size_t smem, void **args)
+{
+    if (grid.x == 0 || grid.x > 0x7FFFFFFFu || grid.y == 0 || grid.y > 65535 || grid.z != 1) return cudaErrorInvalidConfiguration;
+    Launch l{names()[func], grid, smem, {}};
+    if (l.name.find("k_any_") != std::string::npos && l.name.find("sum") == std::string::npos) memcpy(&l.tiles, args[0], sizeof l.tiles);
+    g_launches.push_back(l);
+    return cudaSuccess;
+}
 
 cudaError_t arrive()
 {
@@ -57,6 +83,53 @@ cudaError_t cudaGetDevice(int *d)
 }
 cudaError_t cudaSetDevice(int) { return cudaSuccess; }
 const char *cudaGetErrorString(cudaError_t) { return "fake"; }
+cudaError_t cudaGetLastError() { return cudaSuccess; }
+cudaError_t cudaLaunchKernelExC(const cudaLaunchConfig_t *c, const void *func, void **args)
+{
+    return record(func, c->gridDim, c->dynamicSmemBytes, args);
+}
+CUresult fake_encode(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                     const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill)
+{
+    return CUDA_SUCCESS;
+}
+cudaError_t cudaGetDriverEntryPointByVersion(const char *, void **f, unsigned int, unsigned long long, cudaDriverEntryPointQueryResult *q)
+{
+    *f = (void *)fake_encode;
+    *q = cudaDriverEntryPointSuccess;
+    return cudaSuccess;
+}
+
+// what a translation unit with kernels calls when it is loaded
+void **__cudaRegisterFatBinary(void *)
+{
+    static void *handle;
+    return &handle;
+}
+void __cudaRegisterFatBinaryEnd(void **) {}
+void __cudaUnregisterFatBinary(void **) {}
+void __cudaRegisterFunction(void **, const char *host, char *, const char *name, int, uint3 *, uint3 *, dim3 *, dim3 *, int *)
+{
+    names()[host] = name;
+}
+unsigned __cudaPushCallConfiguration(dim3, dim3, size_t, void *) { return 1; }
+cudaError_t __cudaPopCallConfiguration(dim3 *, dim3 *, size_t *, void *) { return cudaErrorUnknown; }
+cudaError_t __cudaGetKernel(cudaKernel_t *, const void *) { return cudaErrorUnknown; }
+cudaError_t __cudaLaunchKernel(cudaKernel_t, dim3, dim3, void **, size_t, cudaStream_t) { return cudaErrorUnknown; }
+
+// the launches since the last fake_forget
+void fake_forget() { g_launches.clear(); }
+int fake_launches() { return (int)g_launches.size(); }
+const char *fake_name(int i) { return g_launches[i].name.c_str(); }
+uint64_t fake_blocks(int i) { return (uint64_t)g_launches[i].grid.x * g_launches[i].grid.y; }
+uint64_t fake_shared(int i) { return g_launches[i].smem; }
+uint32_t fake_bare(int i) { return g_launches[i].tiles.n_bare; }
+// the first row of a launch's first tile (its column ranges in *slabs)
+uint32_t fake_first_row(int i, uint32_t *slabs)
+{
+    *slabs = g_launches[i].tiles.cut.slabs;
+    return g_launches[i].tiles.tiles[0].row0;
+}
 const char *fake_last_error() { return g_error; }
 
 // Whether a batch's tables are in device memory when its creation returns.
@@ -78,6 +151,7 @@ fiona_ctx *fake_context(int sm_count)
 void fake_context_destroy(fiona_ctx *c) { delete c; }
 }
 
+int allow_shared_memory(const void *, size_t, const char *) { return FIONA_OK; }
 int set_error(int code, const char *fmt, ...)
 {
     va_list ap;
@@ -86,23 +160,3 @@ int set_error(int code, const char *fmt, ...)
     va_end(ap);
     return code;
 }
-
-int adapter_tiles_configure() { return FIONA_OK; }
-uint64_t adapter_any_work(const fiona_adapter_batch *, uint32_t, uint32_t) { return 256; }
-uint64_t adapter_tiles_work(const fiona_adapter_batch *, uint32_t, uint32_t) { return 256; }
-uint64_t adapter_pad_work(const fiona_adapter_batch *, uint32_t, uint32_t) { return 256; }
-bool adapter_rows_apply(const fiona_adapter_batch::Split &, uint32_t) { return true; }
-bool adapter_tiles_apply(const fiona_adapter_batch *, uint32_t, uint32_t, uint32_t) { return true; }
-bool adapter_pad_applies(const fiona_adapter_batch *, uint32_t, uint32_t, uint32_t) { return false; }
-double adapter_any_us(const fiona_adapter_batch *, uint32_t, uint32_t, uint32_t) { return 1; }
-double adapter_tiles_us(const fiona_adapter_batch *, uint32_t, uint32_t, uint32_t) { return 1; }
-double adapter_pad_us(const fiona_adapter_batch *, uint32_t, uint32_t, bool) { return 1; }
-double adapter_rows_us(const fiona_adapter_batch *, const fiona_adapter_batch::Split &, uint32_t, uint32_t) { return 1; }
-int launch_adapter_any_forward(const fiona_adapter_batch *, void *, uint32_t, const AdapterArgs &, void *, uint32_t) { return FIONA_OK; }
-int launch_adapter_any_backward(const fiona_adapter_batch *, void *, uint32_t, const AdapterArgs &, void *) { return FIONA_OK; }
-int launch_adapter_tiles_forward(const fiona_adapter_batch *, void *, uint32_t, const AdapterArgs &, void *, uint32_t) { return FIONA_OK; }
-int launch_adapter_tiles_backward(const fiona_adapter_batch *, void *, uint32_t, const AdapterArgs &, void *) { return FIONA_OK; }
-int launch_adapter_pad_forward(const fiona_adapter_batch *, void *, uint32_t, const AdapterArgs &, void *) { return FIONA_OK; }
-int launch_adapter_pad_backward(const fiona_adapter_batch *, void *, uint32_t, const AdapterArgs &, void *) { return FIONA_OK; }
-int launch_adapter_rows(const fiona_adapter_batch *, const fiona_adapter_batch::Split &, void *, uint32_t, const AdapterArgs &) { return FIONA_OK; }
-int launch_dropout(const fiona_ctx *, void *, uint32_t, const DropoutArgs &) { return FIONA_OK; }

@@ -1,5 +1,5 @@
 """The adapters' host code on a fake device (fake_device.cpp: CUDA's calls on host
-memory, no kernels)."""
+memory; kernels' launches are written down, none runs)."""
 import ctypes
 import os
 import subprocess
@@ -14,11 +14,14 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 
 @pytest.fixture(scope="module")
 def fake(tmp_path_factory):
+    B.build()
     out = str(tmp_path_factory.mktemp("fake") / "libfake.so")
     cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(B.nvcc()))), "include")
     # (symbolic: a process with torch in it has the real calls loaded)
     cmd = ["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wl,-Bsymbolic", "-I" + B.INCLUDE, "-I" + B.CSRC, "-I" + cuda,
-           os.path.join(B.CSRC, "adapter_host.cpp"), os.path.join(HERE, "fake_device.cpp"), "-o", out]
+           os.path.join(HERE, "fake_device.cpp")]
+    objects = [f for f in B.LIBRARIES["libfiona.so"] if f.startswith(("adapter", "dropout"))]
+    cmd += [os.path.join(B.OUT, f + ".o") for f in objects] + ["-o", out]
     r = subprocess.run(cmd, capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     L = ctypes.CDLL(out)
@@ -26,6 +29,11 @@ def fake(tmp_path_factory):
     L.fake_context.restype, L.fake_last_error.restype = p, ctypes.c_char_p
     L.fake_context_destroy.argtypes, L.fake_tables_arrived.argtypes = [p], [p, p]
     L.fiona_adapter_batch_create.argtypes = [p, u32, p, p, u32, p, p, u32, ctypes.POINTER(p)]
+    for name, result in (("name", ctypes.c_char_p), ("blocks", u64), ("shared", u64), ("bare", u32), ("first_row", u32)):
+        getattr(L, "fake_" + name).restype = result
+    L.fiona_adapter_forward.argtypes = [p, p, p, p, u64, p, u64, p, u64, p, p, p, u64]
+    L.fiona_adapter_backward.argtypes = [p, p, p, p, u64, p, p, u64, p, u64, p, u64, p, p, p, p, u64]
+    L.fiona_adapter_work_bytes.argtypes = [p, u32, u32, u32, ctypes.POINTER(u64)]
     L.fiona_adapter_batch_destroy.argtypes, L.fiona_adapter_batch_destroy.restype = [p], None
     return L
 
@@ -52,4 +60,53 @@ def test_a_batch_is_on_the_device_when_its_creation_returns(fake, ctx):
     ranks = np.array([8, 3, 16], np.uint32)
     h = make_batch(fake, ctx, [0, 200, 210, 500], [2, 0, 1], ranks, 16)
     assert fake.fake_tables_arrived(h, ranks.ctypes.data) == 1
+    fake.fiona_adapter_batch_destroy(h)
+
+
+class Layer(ctypes.Structure):  # fiona_adapter_layer
+    _fields_ = [("d_in", ctypes.c_uint32), ("d_out", ctypes.c_uint32), ("dtype", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p)]
+
+
+F32, BF16 = 0, 2
+
+
+def call(fake, batch, d_in, d_out, dtype, backward=False):
+    """A call on addresses far apart (nothing reads them)."""
+    n = ctypes.c_uint64()
+    assert fake.fiona_adapter_work_bytes(batch, d_in, d_out, dtype, ctypes.byref(n)) == 0
+    at = lambda k: k << 48  # noqa: E731
+    layer = Layer(d_in, d_out, dtype, 0, at(1), at(2))
+    fake.fake_forget()
+    if backward:
+        return fake.fiona_adapter_backward(batch, None, ctypes.byref(layer), at(3), d_in, at(4), at(5), d_out, None, 0, at(6), d_in,
+                                           at(7), at(8), None, at(9), n.value)
+    return fake.fiona_adapter_forward(batch, None, ctypes.byref(layer), at(3), d_in, None, 0, at(5), d_out, None, None, at(9), n.value)
+
+
+def launches(fake, part):
+    return [i for i in range(fake.fake_launches()) if part in fake.fake_name(i).decode()]
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_grids_past_what_a_launch_holds(fake, ctx, backward):
+    """70000 runs of one row beside 2^20 columns: 2.3e9 blocks, in two launches.  Every
+    tile is in one of them, and the rows without an adapter are in the first."""
+    n, d = 70000, 1 << 20
+    ids = [-1] + [i % 2 for i in range(n)]
+    h = make_batch(fake, ctx, list(range(n + 2)), ids, [4, 4], 4)
+    rc = call(fake, h, d, d, F32, backward)
+    assert rc == 0, fake.fake_last_error()
+    found, tiles = launches(fake, "k_any_expand"), [r for a in (0, 1) for r, i in enumerate(ids) if i == a]
+    assert len(found) == 2
+    at = 0
+    for i in found:
+        slabs = ctypes.c_uint32()
+        assert fake.fake_first_row(i, ctypes.byref(slabs)) == tiles[at] and slabs.value == d // 64
+        assert fake.fake_bare(i) == (1 if at == 0 else 0)
+        at += (fake.fake_blocks(i) - fake.fake_bare(i)) // (2 * slabs.value)
+    assert at == len(tiles)
+    if backward:  # the weight gradients' chunks count from the first tile again
+        for i in launches(fake, "k_any_grad")[:1]:
+            assert fake.fake_first_row(i, ctypes.byref(ctypes.c_uint32())) == tiles[0]
     fake.fiona_adapter_batch_destroy(h)
