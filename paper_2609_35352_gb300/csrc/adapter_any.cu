@@ -518,16 +518,18 @@ const AdapterChunks &grad_chunks(const fiona_adapter_batch *b, uint32_t d_in, ui
 
 struct AnyShape {
     uint32_t r16;
+    bool direct;  // one chunk an adapter: its gradients are written as they are
     uint64_t part = 0, dh = 0, grad_A = 0, grad_B = 0, bytes = 0;
     AnyShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) : r16((b->r_max + 15) & ~15u)
     {
         uint32_t slabs = shrink_cut(b, d_out, b->n_tiles).slabs;
         for (const auto &s : b->split) slabs = std::max(slabs, shrink_cut(b, d_in, s.tiles).slabs);
         const uint32_t chunks = grad_chunks(b, d_in, d_out).count;
+        direct = b->n_tiles && chunks + b->n_idle == b->n_adapters;
         dh = part + align_up((uint64_t)slabs * b->n_tokens * r16 * 4);
         grad_A = dh + align_up((uint64_t)b->n_tokens * r16 * 4);
-        grad_B = grad_A + align_up((uint64_t)chunks * d_in * r16 * 4);
-        bytes = grad_B + align_up((uint64_t)chunks * d_out * r16 * 4);
+        grad_B = grad_A + (direct ? 0 : align_up((uint64_t)chunks * d_in * r16 * 4));
+        bytes = grad_B + (direct ? 0 : align_up((uint64_t)chunks * d_out * r16 * 4));
     }
 };
 
@@ -600,7 +602,7 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, const AdapterArgs &a,
     g.chunks = chunks.d_chunks;
     g.grad = reinterpret_cast<float *>(ws + f.grad_A);
     g.grad_b = reinterpret_cast<float *>(ws + f.grad_B);
-    g.direct = any && chunks.count + b->n_idle == b->n_adapters;
+    g.direct = f.direct;
     g.idle = b->d_idle;
     g.n_idle = g.direct ? b->n_idle : 0;
     const uint64_t all = (uint64_t)chunks.count * (ceil_div(a.d_in, kCols) + ceil_div(a.d_out, kCols)) + g.n_idle;

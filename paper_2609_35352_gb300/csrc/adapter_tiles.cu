@@ -1408,7 +1408,8 @@ struct GradCut {
 struct BackwardShape {
     RankShape r;
     bool apart;  // dh by a pass of its own
-    bool direct = false;  // one chunk an adapter in both passes
+    // one chunk an adapter in both passes: dA and dB are written as they are, by eights
+    bool eights, direct;
     Cut dh_cut{};
     GradCut shrink, expand;
     uint64_t part, image, dh_image, grad_A, grad_B, most, ups, dh_most, bytes;  // offsets in the workspace
@@ -1416,13 +1417,14 @@ struct BackwardShape {
         : r(b->r_max), apart(r.r16 > 64), shrink(b, d_out, r, apart ? 0 : 2 * r.r16), expand(b, d_in, r, 2 * kBlockCols)
     {
         dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1), 0, shrink_most(r.r16)) : shrink.cut;
-        direct = shrink.chunks->count + b->n_idle == b->n_adapters && expand.chunks->count + b->n_idle == b->n_adapters;
+        eights = d_in % 8 == 0 && b->r_max % 8 == 0;
+        direct = eights && shrink.chunks->count + b->n_idle == b->n_adapters && expand.chunks->count + b->n_idle == b->n_adapters;
         part = 0;
         image = part + align_up((uint64_t)dh_cut.slabs * b->n_tokens * r.r16 * 4);
         dh_image = image + (uint64_t)b->n_tiles * r.boxes * kBoxBytes;
         grad_A = dh_image + (uint64_t)b->n_tiles * r.boxes * kBoxBytes;
-        grad_B = grad_A + align_up((uint64_t)expand.chunks->count * d_in * r.r16 * 4);
-        most = grad_B + align_up((uint64_t)shrink.chunks->count * d_out * r.r16 * 4);
+        grad_B = grad_A + (direct ? 0 : align_up((uint64_t)expand.chunks->count * d_in * r.r16 * 4));
+        most = grad_B + (direct ? 0 : align_up((uint64_t)shrink.chunks->count * d_out * r.r16 * 4));
         ups = most + align_up((uint64_t)b->n_tiles * image_blocks(r.r16) * 4);
         dh_most = ups + align_up((uint64_t)b->n_tiles * 2 * 4);
         bytes = dh_most + align_up((uint64_t)dh_cut.slabs * b->n_tiles * kMostWarps * 4);
@@ -1433,9 +1435,8 @@ template <typename T>
 int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const AdapterArgs &a, void *work)
 {
     int rc = FIONA_OK;
-    BackwardShape f(b, a.d_in, a.d_out);
-    const bool eights = a.d_in % 8 == 0 && a.r_rows % 8 == 0;
-    f.direct = f.direct && eights;  // (dA and dB are written by eights there, and by fours below)
+    const BackwardShape f(b, a.d_in, a.d_out);
+    const bool eights = f.eights;  // (dA and dB are added up by fours below)
     uint8_t *ws = static_cast<uint8_t *>(work);
     const GradSum A{reinterpret_cast<const float *>(ws + f.grad_A), f.expand.chunks->d_begin, a.dA, a.r_rows, a.d_in, f.r.r16, a.d_in, 1};
     const GradSum B{reinterpret_cast<const float *>(ws + f.grad_B), f.shrink.chunks->d_begin, a.dB, a.d_out, a.r_rows, a.d_out, f.r.r16, 0};

@@ -110,3 +110,26 @@ def test_grids_past_what_a_launch_holds(fake, ctx, backward):
         for i in launches(fake, "k_any_grad")[:1]:
             assert fake.fake_first_row(i, ctypes.byref(ctypes.c_uint32())) == tiles[0]
     fake.fiona_adapter_batch_destroy(h)
+
+
+def work_bytes(fake, batch, d_in, d_out, dtype):
+    n = ctypes.c_uint64()
+    assert fake.fiona_adapter_work_bytes(batch, d_in, d_out, dtype, ctypes.byref(n)) == 0
+    return n.value
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_room_for_partial_gradients_that_are_not_made(fake, ctx, dtype):
+    """256 tokens of 200 adapters: each adapter's gradient comes from one chunk and is
+    written as it is.  Partial sums of dA and dB would take 524 MB."""
+    h = make_batch(fake, ctx, list(range(257)), [i % 200 for i in range(256)], [64] * 200, 64)
+    assert call(fake, h, 2048, 8192, dtype, backward=True) == 0
+    assert not launches(fake, "grad_sum")
+    assert work_bytes(fake, h, 2048, 8192, dtype) < 100e6
+    fake.fiona_adapter_batch_destroy(h)
+    # one adapter's long batch is cut into chunks, and their sums have their room
+    h = make_batch(fake, ctx, [0, 16384], [0], [64], 64)
+    assert call(fake, h, 2048, 8192, dtype, backward=True) == 0
+    assert launches(fake, "grad_sum") or launches(fake, "k_image")
+    assert work_bytes(fake, h, 2048, 8192, dtype) > 2 * 64 * (2048 + 8192) * 4
+    fake.fiona_adapter_batch_destroy(h)
