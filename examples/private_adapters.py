@@ -157,7 +157,7 @@ def main(steps=300, verbose=True):
 
     # serve one new token of each client
     token = torch.randn(CLIENTS, WIDTH, device="cuda")
-    single = AD.Batch(ctx, list(range(CLIENTS + 1)), list(range(CLIENTS)), ranks, r_max, [2.0] * CLIENTS)
+    single = AD.Batch(ctx, list(range(CLIENTS + 1)), list(range(CLIENTS)), ranks, r_max, [2.0] * CLIENTS, gradients=False)
     served, stream_out = torch.empty(CLIENTS, WIDTH, device="cuda"), torch.empty(CLIENTS, WIDTH, device="cuda")
     token_base = project(token)
     single.forward(token, A, B, served, base=token_base, work=single.workspace(WIDTH, WIDTH, token.dtype), stream=stream)

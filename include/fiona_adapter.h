@@ -102,10 +102,15 @@ typedef struct fiona_dropout_spec {
 int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_requests, const uint64_t *starts,
                                const int32_t *adapter, uint32_t n_adapters, const uint32_t *ranks,
                                const float *scales, uint32_t r_max, fiona_adapter_batch **out);
+/* For a batch that only serves: from now on fiona_adapter_work_bytes is what its
+ * forward calls need, without the gradient's images and partial sums, and backward
+ * calls on it are refused.  To be called before the batch's workspaces are made.
+ * Errors: FIONA_ERR_ARG. */
+int fiona_adapter_batch_forward_only(fiona_adapter_batch *batch);
 void fiona_adapter_batch_destroy(fiona_adapter_batch *batch); /* NULL is a no-op */
 
 /* Bytes of `work` that a forward or backward call on layers of these sizes
- * needs (the larger of the two).  Calls that may run at the same time need a
+ * needs (the larger of the two; of a batch for forward calls only: theirs).  Calls that may run at the same time need a
  * workspace each; nothing in it outlives a call. */
 int fiona_adapter_work_bytes(const fiona_adapter_batch *batch, uint32_t d_in, uint32_t d_out, uint32_t dtype,
                              uint64_t *bytes);
@@ -121,7 +126,8 @@ int fiona_adapter_forward(const fiona_adapter_batch *batch, void *cuda_stream, c
 
 /* The gradient, from the x, h and drop of the forward pass.  dx_base == NULL:
  * zero.  dA and dB are overwritten, for every adapter (zero where it has no
- * rows).  Errors as fiona_adapter_forward. */
+ * rows).  Errors as fiona_adapter_forward, and FIONA_ERR_ARG on a batch for
+ * forward calls only. */
 int fiona_adapter_backward(const fiona_adapter_batch *batch, void *cuda_stream, const fiona_adapter_layer *layer,
                            const void *x, uint64_t ldx, const float *h, const void *dy, uint64_t ld_dy,
                            const void *dx_base, uint64_t ld_dx_base, void *dx, uint64_t ld_dx, void *dA, void *dB,

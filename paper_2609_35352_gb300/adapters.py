@@ -21,7 +21,7 @@ from . import fiona as F
 FIONA_F32, FIONA_F16, FIONA_BF16 = 0, 1, 2
 MAX_RANK = 128
 
-EXPORTED = ("fiona_adapter_batch_create", "fiona_adapter_batch_destroy", "fiona_adapter_work_bytes",
+EXPORTED = ("fiona_adapter_batch_create", "fiona_adapter_batch_forward_only", "fiona_adapter_batch_destroy", "fiona_adapter_work_bytes",
             "fiona_adapter_forward", "fiona_adapter_backward", "fiona_dropout")
 
 
@@ -40,6 +40,7 @@ def lib() -> ctypes.CDLL:
         L = F.lib()
         p, u32, u64, i32 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int
         L.fiona_adapter_batch_create.argtypes = [p, u32, p, p, u32, p, p, u32, ctypes.POINTER(p)]
+        L.fiona_adapter_batch_forward_only.argtypes = [p]
         L.fiona_adapter_batch_destroy.argtypes = [p]
         L.fiona_adapter_batch_destroy.restype = None
         L.fiona_adapter_work_bytes.argtypes = [p, u32, u32, u32, ctypes.POINTER(u64)]
@@ -136,10 +137,11 @@ def _indices(values: Any, dtype: Any, name: str) -> np.ndarray:
 class Batch:
     """fiona_adapter_batch: request r owns the rows starts[r] to starts[r + 1] and
     uses adapter adapters[r] (-1: none); adapter a has rank ranks[a] and scale
-    scales[a] (None: 1).  One batch serves every layer of a model."""
+    scales[a] (None: 1).  One batch serves every layer of a model.  One without
+    `gradients` is for forward calls only, and its workspaces are smaller."""
 
     def __init__(self, ctx: F.Context, starts: Sequence[int], adapters: Sequence[int], ranks: Sequence[int],
-                 r_max: int, scales: Optional[Sequence[float]] = None):
+                 r_max: int, scales: Optional[Sequence[float]] = None, gradients: bool = True):
         s, a, r = (_indices(v, t, n) for v, t, n in ((starts, np.uint64, "starts"), (adapters, np.int32, "adapters"),
                                                      (ranks, np.uint32, "ranks")))
         r_max = int(_indices([r_max], np.uint32, "r_max")[0])
@@ -155,6 +157,8 @@ class Batch:
                                                   r.ctypes.data, None if c is None else c.ctypes.data, r_max,
                                                   ctypes.byref(h)), "fiona_adapter_batch_create")
         self.ctx, self.handle = ctx, h
+        if not gradients:
+            F._check(lib().fiona_adapter_batch_forward_only(h), "fiona_adapter_batch_forward_only")
         self.n_tokens, self.n_adapters, self.r_max = int(s[-1]), int(r.shape[0]), r_max
         self._dev = _device(ctx)
 
@@ -165,7 +169,7 @@ class Batch:
         return n.value
 
     def workspace(self, d_in: int, d_out: int, dtype: Any):
-        """A workspace for forward and backward calls on layers of these sizes;
+        """A workspace for calls on layers of these sizes;
         calls that may overlap in time need one each."""
         return torch.empty(max(self.work_bytes(d_in, d_out, dtype), 16), dtype=torch.uint8,
                            device="cuda:%d" % self.ctx.device)

@@ -34,6 +34,7 @@ struct AdapterChunks {
 struct fiona_adapter_batch {
     const fiona_ctx *ctx = nullptr;
     uint32_t n_tokens = 0, n_adapters = 0, r_max = 0;
+    bool forward_only = false;  // no gradient: less workspace
     bool stall = false;  // FIONA_ADAPTER_TEST_STALL, read when the batch is made: its kernels' waits run out
     uint64_t wait_ns = 2000000000ull;  // bound of every wait
     // device arrays, in `blob`

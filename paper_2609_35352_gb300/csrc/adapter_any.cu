@@ -522,11 +522,13 @@ struct AnyShape {
     uint64_t part = 0, dh = 0, grad_A = 0, grad_B = 0, bytes = 0;
     AnyShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out) : r16((b->r_max + 15) & ~15u)
     {
-        uint32_t slabs = shrink_cut(b, d_out, b->n_tiles).slabs;
+        uint32_t slabs = b->forward_only ? 0 : shrink_cut(b, d_out, b->n_tiles).slabs;
         for (const auto &s : b->split) slabs = std::max(slabs, shrink_cut(b, d_in, s.tiles).slabs);
         const uint32_t chunks = grad_chunks(b, d_in, d_out).count;
         direct = b->n_tiles && chunks + b->n_idle == b->n_adapters;
         dh = part + align_up((uint64_t)slabs * b->n_tokens * r16 * 4);
+        bytes = dh;
+        if (b->forward_only) return;
         grad_A = dh + align_up((uint64_t)b->n_tokens * r16 * 4);
         grad_B = grad_A + (direct ? 0 : align_up((uint64_t)chunks * d_in * r16 * 4));
         bytes = grad_B + (direct ? 0 : align_up((uint64_t)chunks * d_out * r16 * 4));

@@ -306,6 +306,13 @@ extern "C" int fiona_adapter_batch_create(const fiona_ctx *ctx, uint32_t n_reque
     return set_error(FIONA_ERR_NOMEM, "adapter_batch_create: host allocation");
 }
 
+extern "C" int fiona_adapter_batch_forward_only(fiona_adapter_batch *b)
+{
+    if (!b) return set_error(FIONA_ERR_ARG, "adapter_batch_forward_only: null batch");
+    b->forward_only = true;
+    return FIONA_OK;
+}
+
 extern "C" void fiona_adapter_batch_destroy(fiona_adapter_batch *b)
 {
     if (!b) return;
@@ -392,6 +399,7 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
     const char *who = "adapter_backward";
     int rc = check_layer(b, l, who);
     if (rc) return rc;
+    if (b->forward_only) return set_error(FIONA_ERR_ARG, "%s: the batch is for forward calls only", who);
     AdapterArgs a = common_args(b, l);
     if ((rc = make_mask(drop, l->d_in, a.mask, who))) return rc;
     const uint64_t T = b->n_tokens, e = element(l->dtype), r = b->r_max;

@@ -98,7 +98,7 @@ struct PadShape {
         B = A + align_up(n * b->r_max * di * 2);
         wide = B + align_up(n * d_out * r8 * 2);
         back = wide + align_up(T * dout * 2);
-        h = back + align_up(T * di * 2);
+        h = back + (b->forward_only ? 0 : align_up(T * di * 2));
         bytes = h + align_up(T * r8 * 4);
     }
 };

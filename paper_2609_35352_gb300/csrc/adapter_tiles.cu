@@ -1567,7 +1567,7 @@ int adapter_tiles_configure()
 
 uint64_t adapter_tiles_work(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
 {
-    uint64_t n = BackwardShape(b, d_in, d_out).bytes;
+    uint64_t n = b->forward_only ? 0 : BackwardShape(b, d_in, d_out).bytes;
     for (const auto &s : b->split) n = std::max(n, ForwardShape(b, d_in, d_out, s.tiles).part_bytes(b));
     return n;
 }

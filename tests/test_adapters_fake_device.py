@@ -34,6 +34,7 @@ def fake(tmp_path_factory):
     L.fiona_adapter_forward.argtypes = [p, p, p, p, u64, p, u64, p, u64, p, p, p, u64]
     L.fiona_adapter_backward.argtypes = [p, p, p, p, u64, p, p, u64, p, u64, p, u64, p, p, p, p, u64]
     L.fiona_adapter_work_bytes.argtypes = [p, u32, u32, u32, ctypes.POINTER(u64)]
+    L.fiona_adapter_batch_forward_only.argtypes = [p]
     L.fiona_adapter_batch_destroy.argtypes, L.fiona_adapter_batch_destroy.restype = [p], None
     return L
 
@@ -133,3 +134,20 @@ def test_no_room_for_partial_gradients_that_are_not_made(fake, ctx, dtype):
     assert launches(fake, "grad_sum") or launches(fake, "k_image")
     assert work_bytes(fake, h, 2048, 8192, dtype) > 2 * 64 * (2048 + 8192) * 4
     fake.fiona_adapter_batch_destroy(h)
+
+
+@pytest.mark.parametrize("dtype,d_in,d_out,most", [(F32, 4096, 4096, 70e6), (BF16, 4096, 4096, 70e6), (BF16, 4092, 4091, 300e6)])
+def test_workspace_of_a_batch_for_forward_calls_only(fake, ctx, dtype, d_in, d_out, most):
+    """8192 tokens of 2 adapters in turn, rank 128.  The gradient's images alone take
+    1.07 GB in 16 bits.  (Off eight, the copies of x and out have their room.)"""
+    h = make_batch(fake, ctx, list(range(8193)), [i % 2 for i in range(8192)], [128, 128], 128)
+    assert call(fake, h, d_in, d_out, dtype, backward=True) == 0
+    both = work_bytes(fake, h, d_in, d_out, dtype)
+    assert fake.fiona_adapter_batch_forward_only(h) == 0
+    n = work_bytes(fake, h, d_in, d_out, dtype)
+    assert n < most and (dtype == F32 or n < both / 4)
+    assert call(fake, h, d_in, d_out, dtype) == 0, fake.fake_last_error()
+    assert call(fake, h, d_in, d_out, dtype, backward=True) == -1
+    assert b"forward" in fake.fake_last_error()
+    fake.fiona_adapter_batch_destroy(h)
+    assert fake.fiona_adapter_batch_forward_only(None) == -1

@@ -6,6 +6,7 @@ torch = pytest.importorskip("torch")
 
 pytestmark = pytest.mark.gpu
 
+from paper_2609_35352_gb300 import adapters as AD  # noqa: E402
 from paper_2609_35352_gb300 import build as BUILD  # noqa: E402
 from paper_2609_35352_gb300 import fiona as F  # noqa: E402
 from paper_2609_35352_gb300 import workloads as W  # noqa: E402
@@ -40,3 +41,22 @@ def test_nothing_behind_the_workspace_changes(ctx, dtype, starts, ids, ranks, r_
     pr.work = whole[:n] if n else whole
     pr.run_and_check()
     assert bool((whole[n:] == 0xA5).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("starts,ids,r_max,d_in,d_out", [
+    (list(range(65)), [i % 48 for i in range(64)], 16, 1024, 512), ([0, 700, 701, 2000], [0, 1, 0], 24, 768, 640),
+    (list(range(41)), [i % 3 - 1 for i in range(40)], 8, 200000, 64), ([0, 3000, 3500], [0, -1], 128, 256, 512),
+    ([0, 1800, 1803, 1900, 3000], [0, 1, -1, 2], 43, 1001, 777), ([0, 9, 40], [0, 1], 5, 77, 131)])
+def test_forward_only(ctx, dtype, starts, ids, r_max, d_in, d_out):
+    pr = Problem(ctx, dtype, starts, ids, [r_max] * (max(ids) + 1), r_max, d_in, d_out, seed=d_out)
+    pr.batch = AD.Batch(ctx, starts, ids, pr.ranks, r_max, pr.scales, gradients=False)
+    n = pr.batch.work_bytes(d_in, d_out, DT[dtype])
+    whole = torch.full((n + GUARD,), 0xA5, dtype=torch.uint8, device="cuda")
+    pr.work = whole[:n] if n else whole
+    pr.forward()
+    torch.cuda.synchronize()
+    pr.check_forward()
+    assert bool((whole[n:] == 0xA5).all())
+    with pytest.raises(F.FionaError):
+        pr.backward()
