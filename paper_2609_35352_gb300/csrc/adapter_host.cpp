@@ -42,7 +42,8 @@ struct View {
 bool overlap(const View &a, const View &b)
 {
     const uint64_t p = (uint64_t)(uintptr_t)a.p, q = (uint64_t)(uintptr_t)b.p;
-    if (!a.bytes() || !b.bytes() || p + a.bytes() <= q || q + b.bytes() <= p) return false;
+    if (!a.bytes() || !b.bytes()) return false;
+    if (q >= p ? q - p >= a.bytes() : p - q >= b.bytes()) return false;
     const uint64_t row = a.ld * a.size;
     if (row != b.ld * b.size || a.cols * a.size > row || b.cols * b.size > row) return true;
     const uint64_t off = q >= p ? (q - p) % row : (row - (p - q) % row) % row;
@@ -53,7 +54,8 @@ int check_input(const View &v, uint64_t align, const char *who)
 {
     if (!v.p) return set_error(FIONA_ERR_ARG, "%s: null %s", who, v.name);
     if ((uintptr_t)v.p % align) return set_error(FIONA_ERR_ARG, "%s: %s is not %llu-byte aligned", who, v.name, (unsigned long long)align);
-    if (v.ld >= (1ull << 40) || v.rows * std::max(v.ld, v.cols) >= (1ull << 60) || v.rows >= (1ull << 40))
+    const uint64_t reach = std::max<uint64_t>(std::max(v.ld, v.cols), 1);
+    if (v.ld >= (1ull << 40) || v.rows >= (1ull << 40) || v.rows > (1ull << 60) / reach)  // (no product that could wrap)
         return set_error(FIONA_ERR_ARG, "%s: rows or row stride of %s out of range", who, v.name);
     return FIONA_OK;
 }
