@@ -1378,12 +1378,12 @@ struct GradCut {
     Cut cut{};
     const AdapterChunks *chunks = nullptr;
     uint32_t tmem_cols = 0;
-    GradCut(const fiona_adapter_batch *b, uint32_t cols, const RankShape &r, uint32_t fixed)
+    // `fixed`: columns of tensor memory beside the sums; `parts`: the pass writes partial dh
+    GradCut(const fiona_adapter_batch *b, uint32_t cols, const RankShape &r, uint32_t fixed, bool parts)
     {
         const uint32_t n = ceil_div(cols, kBlockCols), sms = (uint32_t)std::max(b->ctx->sm_count, 1);
         const uint32_t wide = r.both ? r.both : r.r16;
         const uint32_t most = std::min({n, 4u, (512 - fixed) / wide});
-        const bool parts = fixed == 2 * r.r16;
         const uint32_t active = b->n_adapters - b->n_idle;
         double best = 0;
         for (uint32_t width = most; width >= 1; --width)
@@ -1414,7 +1414,8 @@ struct BackwardShape {
     GradCut shrink, expand;
     uint64_t part, image, dh_image, grad_A, grad_B, most, ups, dh_most, bytes;  // offsets in the workspace
     BackwardShape(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out)
-        : r(b->r_max), apart(r.r16 > 64), shrink(b, d_out, r, apart ? 0 : 2 * r.r16), expand(b, d_in, r, 2 * kBlockCols)
+        : r(b->r_max), apart(r.r16 > 64), shrink(b, d_out, r, apart ? 0 : 2 * r.r16, !apart),
+          expand(b, d_in, r, 2 * kBlockCols, false)
     {
         dh_cut = apart ? cut_columns(ceil_div(d_out, 64), b->n_tiles, 2 * (uint32_t)std::max(b->ctx->sm_count, 1), 0, shrink_most(r.r16)) : shrink.cut;
         eights = d_in % 8 == 0 && b->r_max % 8 == 0;

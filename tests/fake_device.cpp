@@ -29,7 +29,7 @@ struct Launch {
     std::string name;
     dim3 grid;
     size_t smem;
-    TileArgs tiles;  // of the kernels that take one first (adapter_any.cu)
+    TileArgs tiles;  // of the kernels that take one
 };
 std::vector<Launch> g_launches;
 std::map<const void *, std::string> &names()
@@ -42,7 +42,9 @@ cudaError_t record(const void *func, dim3 grid, size_t smem, void **args)
 {
     if (grid.x == 0 || grid.x > 0x7FFFFFFFu || grid.y == 0 || grid.y > 65535 || grid.z != 1) return cudaErrorInvalidConfiguration;
     Launch l{names()[func], grid, smem, {}};
-    if (l.name.find("k_any_") != std::string::npos && l.name.find("sum") == std::string::npos) memcpy(&l.tiles, args[0], sizeof l.tiles);
+    const struct { const char *name; int at; } takes[] = {{"k_any_shrink", 0}, {"k_any_expand", 0}, {"k_any_grad", 0}, {"k_shrink_grad", 2}, {"k_expand_grad", 4}};
+    for (const auto &k : takes)
+        if (l.name.find(k.name) != std::string::npos && l.name.find("sum") == std::string::npos) memcpy(&l.tiles, args[k.at], sizeof l.tiles);
     g_launches.push_back(l);
     return cudaSuccess;
 }

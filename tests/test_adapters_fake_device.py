@@ -151,3 +151,19 @@ def test_workspace_of_a_batch_for_forward_calls_only(fake, ctx, dtype, d_in, d_o
     assert b"forward" in fake.fake_last_error()
     fake.fiona_adapter_batch_destroy(h)
     assert fake.fiona_adapter_batch_forward_only(None) == -1
+
+
+@pytest.mark.parametrize("r_max", [16, 64, 72, 112, 128])
+def test_cut_of_dx_goes_by_tiles(fake, ctx, r_max):
+    """The pass that makes dx and dA writes no partial dh: how it is cut goes by the
+    tiles, whether they hold 128 rows each or one."""
+    blocks = []
+    for rows in (128, 1):
+        h = make_batch(fake, ctx, [rows * i for i in range(33)], [i % 2 for i in range(32)], [r_max] * 2, r_max)
+        assert call(fake, h, 2048, 2048, BF16, backward=True) == 0
+        (i,) = launches(fake, "k_expand_grad")
+        slabs = ctypes.c_uint32()
+        fake.fake_first_row(i, ctypes.byref(slabs))
+        blocks.append((fake.fake_blocks(i), slabs.value))
+        fake.fiona_adapter_batch_destroy(h)
+    assert blocks[0] == blocks[1]
