@@ -233,8 +233,10 @@ constexpr uint32_t kMaxStages = 8;
 // 2048 -> 8192, rank 128 took 82.4 us for 78.0.
 constexpr uint32_t kShrinkChain = 128, kGradTiles = 32;
 
-// accumulators of a shrink, taken by its boxes in turn
+// accumulators of a shrink, taken by its boxes in turn, and columns of tensor memory
 __host__ __device__ constexpr uint32_t shrink_accs(uint32_t r16) { return r16 <= 64 ? 4 : 2; }
+__host__ __device__ constexpr uint32_t shrink_cols(uint32_t r16) { return r16 <= 16 ? 64 : r16 <= 32 ? 128 : 256; }
+constexpr uint32_t kExpandCols = 128;
 
 // (BACK: partial dh = dy B, for ranks above 64: shrink_grad's accumulators of dB
 // leave it a range of 256 columns then, whose partial dh is as large as its dy)
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(kShrinkThreads) k_shrink(const __grid_constant
     // in turn, for chains a few times shorter (one chain of 128 additions erred by
     // 2.1e-6 of h, two fp32 dot products by 1.1e-6), and a range is short enough
     // (kShrinkChain)
-    const uint32_t accs = shrink_accs(g.r16), cols = g.r16 <= 16 ? 64 : g.r16 <= 32 ? 128 : 256;
+    const uint32_t accs = shrink_accs(g.r16), cols = shrink_cols(g.r16);
     const AdapterTile t = g.tiles[blockIdx.x / g.cut.slabs];
     const uint32_t slab = blockIdx.x % g.cut.slabs;
     const uint32_t b0 = slab * g.cut.width, n = min(g.boxes - b0, g.cut.width);
@@ -477,7 +479,7 @@ __global__ void __launch_bounds__(kExpandThreads, 2) k_expand(const __grid_const
         tiles::prefetch_map(&tB);
         tiles::prefetch_map(&tout);
     }
-    if (me.warp == 1) tcs::tmem_alloc(async::smem_addr(&s_tmem), 128);
+    if (me.warp == 1) tcs::tmem_alloc(async::smem_addr(&s_tmem), kExpandCols);
     tcs::fence_before();
     __syncthreads();
     tcs::fence_after();
@@ -626,7 +628,7 @@ __global__ void __launch_bounds__(kExpandThreads, 2) k_expand(const __grid_const
     __syncwarp();
     __syncthreads();
     tcs::fence_after();
-    if (me.warp == 1) tcs::tmem_dealloc(tmem, 128);
+    if (me.warp == 1) tcs::tmem_dealloc(tmem, kExpandCols);
 }
 
 // ---------------------------------------------------------------------------
@@ -1310,6 +1312,21 @@ struct ForwardShape {
 constexpr uint32_t kSmemTwo = 110 * 1024;   // dynamic shared memory of a CTA, two of them an SM
 constexpr uint32_t kSmemOne = 224 * 1024;
 
+// Launches of kernels that take `cols` columns of tensor memory.  A CTA's wait for them
+// has no limit, and launches overlap: a later launch's CTA may hold its columns while it
+// waits for the end of an earlier launch, of which a CTA beside it may still be about to
+// ask for its own.  So no two CTAs on an SM may ever want more than its 512 columns.
+// Shared memory sees to that (228 KB an SM, some 1 KB a CTA reserved): of those with up to
+// 256 columns and a third of it at least two fit, those with more columns and two
+// thirds are alone.  (Tensor memory that other kernels of the library hold comes free by
+// itself: they wait for no launch.)
+template <typename K>
+int launch_tc(K kernel, uint64_t blocks, uint32_t threads, size_t smem, uint32_t cols, cudaStream_t s, void **args, const char *what)
+{
+    if (smem < (cols <= 256 ? 76u : 152u) * 1024) return set_error(FIONA_ERR_INTERNAL, "%s: %zu bytes of shared memory beside %u columns", what, smem, cols);
+    return launch(kernel, blocks, threads, smem, s, args, what);
+}
+
 // as many stages as fit beside `fixed` bytes, for two CTAs an SM where that
 // leaves `least`
 uint32_t stages_for(uint32_t fixed, uint32_t stage, uint32_t least)
@@ -1353,8 +1370,8 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     const uint32_t stage = shrink_stage<false>(g.r16, g.blocks);
     g.stages = stages_for(0, stage, 3);
     void *sargs[] = {&tx, &tA, &g};
-    if (n_tiles && (rc = launch(k_shrink<T, false>, (uint64_t)n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024,
-                                   s, sargs, "adapter shrink")))
+    if (n_tiles && (rc = launch_tc(k_shrink<T, false>, (uint64_t)n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024,
+                                   shrink_cols(g.r16), s, sargs, "adapter shrink")))
         return rc;
     g.bare = b->d_bare;
     g.n_bare = b->n_bare;
@@ -1363,9 +1380,9 @@ int forward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const 
     g.boxes = ceil_div(a.d_out, 64);
     g.stages = stages_for(g.op_boxes * kBoxBytes, expand_stage(g.blocks), 3);
     void *eargs[] = {&tbase, &tB, &tout, &tout8, &g};
-    return launch(k_expand<T>, (uint64_t)n_tiles * g.cut.slabs + b->n_bare, kExpandThreads,
-                  g.op_boxes * kBoxBytes + (size_t)g.stages * expand_stage(g.blocks) + 1024, s, eargs,
-                  "adapter expand");
+    return launch_tc(k_expand<T>, (uint64_t)n_tiles * g.cut.slabs + b->n_bare, kExpandThreads,
+                     g.op_boxes * kBoxBytes + (size_t)g.stages * expand_stage(g.blocks) + 1024, kExpandCols, s, eargs,
+                     "adapter expand");
 }
 
 // How one of the gradients' passes is cut: blocks of 128 columns a CTA, tiles a
@@ -1485,7 +1502,8 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
             g.cut = f.dh_cut;
             g.stages = stages_for(0, stage, 3);
             void *args[] = {&tdy, &tB, &g};
-            rc = launch(k_shrink<T, true>, (uint64_t)b->n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024, s, args, "adapter dh");
+            rc = launch_tc(k_shrink<T, true>, (uint64_t)b->n_tiles * g.cut.slabs, kShrinkThreads, (size_t)g.stages * stage + 1024,
+                           shrink_cols(g.r16), s, args, "adapter dh");
             if (rc) return rc;
         }
         g.with_dh = !f.apart;
@@ -1502,8 +1520,8 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         void *sargs[] = {&tdy, &tB, &g};
         g.image = image;
         g.ups = ups;
-        if (any && (rc = launch(k_shrink_grad<T>, (uint64_t)f.shrink.chunks->count * g.cut.slabs, kGradThreads,
-                                2 * op + (size_t)g.stages * sstage + 1024, s, sargs, "adapter shrink_grad")))
+        if (any && (rc = launch_tc(k_shrink_grad<T>, (uint64_t)f.shrink.chunks->count * g.cut.slabs, kGradThreads,
+                                   2 * op + (size_t)g.stages * sstage + 1024, g.tmem_cols, s, sargs, "adapter shrink_grad")))
             return rc;
         // dh as an operand (its image in a place of its own: the next kernel starts
         // while this one reads)
@@ -1531,8 +1549,8 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.stages = std::min(kMaxStages, (room - g.buffers * op) / estage);
         const size_t esmem = g.buffers * op + (size_t)g.stages * estage + (a.mask.level ? 2 * kFlagBytes : 0) + 1024;
         void *eargs[] = {&tx, &tA, &tdx, &tdx8, &g};
-        rc = launch(k_expand_grad<T>, (uint64_t)g.n_chunks * g.cut.slabs + b->n_bare + g.n_idle, kExpandGradThreads,
-                    esmem, s, eargs, "adapter expand_grad");
+        rc = launch_tc(k_expand_grad<T>, (uint64_t)g.n_chunks * g.cut.slabs + b->n_bare + g.n_idle, kExpandGradThreads,
+                       esmem, g.tmem_cols, s, eargs, "adapter expand_grad");
         if (rc || f.direct) return rc;
     }
     if (!eights) return launch_any_grad_sum(b, s, dtype, A, B);

@@ -69,20 +69,25 @@ class Layer(ctypes.Structure):  # fiona_adapter_layer
                 ("reserved", ctypes.c_uint32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p)]
 
 
+class DropoutSpec(ctypes.Structure):  # fiona_dropout_spec
+    _fields_ = [("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("p", ctypes.c_double)]
+
+
 F32, BF16 = 0, 2
 
 
-def call(fake, batch, d_in, d_out, dtype, backward=False):
+def call(fake, batch, d_in, d_out, dtype, backward=False, drop=None):
     """A call on addresses far apart (nothing reads them)."""
     n = ctypes.c_uint64()
     assert fake.fiona_adapter_work_bytes(batch, d_in, d_out, dtype, ctypes.byref(n)) == 0
     at = lambda k: k << 48  # noqa: E731
     layer = Layer(d_in, d_out, dtype, 0, at(1), at(2))
+    spec = None if drop is None else ctypes.byref(drop)
     fake.fake_forget()
     if backward:
         return fake.fiona_adapter_backward(batch, None, ctypes.byref(layer), at(3), d_in, at(4), at(5), d_out, None, 0, at(6), d_in,
-                                           at(7), at(8), None, at(9), n.value)
-    return fake.fiona_adapter_forward(batch, None, ctypes.byref(layer), at(3), d_in, None, 0, at(5), d_out, None, None, at(9), n.value)
+                                           at(7), at(8), spec, at(9), n.value)
+    return fake.fiona_adapter_forward(batch, None, ctypes.byref(layer), at(3), d_in, None, 0, at(5), d_out, None, spec, at(9), n.value)
 
 
 def launches(fake, part):
@@ -167,3 +172,20 @@ def test_cut_of_dx_goes_by_tiles(fake, ctx, r_max):
         blocks.append((fake.fake_blocks(i), slabs.value))
         fake.fiona_adapter_batch_destroy(h)
     assert blocks[0] == blocks[1]
+
+
+@pytest.mark.parametrize("r_max", range(8, 129, 8))
+@pytest.mark.parametrize("p", [None, 0.25])
+def test_tensor_memory_of_blocks_that_meet(fake, ctx, r_max, p):
+    """Two blocks that shared memory lets onto an SM never ask for more than its 512
+    columns, whichever kernels and ranks (a block would wait for ever).  The kernels that
+    take over 256 columns are the weight gradients'."""
+    h = make_batch(fake, ctx, [0, 700, 8000], [0, 1], [r_max] * 2, r_max)
+    drop = None if p is None else DropoutSpec(1, 2, p)
+    for backward in (False, True):
+        assert call(fake, h, 2048, 4096, BF16, backward, drop) == 0, fake.fake_last_error()
+        for i in launches(fake, "k_shrink") + launches(fake, "k_expand"):
+            cols = 512 if "grad" in fake.fake_name(i).decode() else 256
+            assert fake.fake_shared(i) >= (152 if cols > 256 else 76) * 1024
+            assert 3 * (fake.fake_shared(i) + 1024) > 228 * 1024
+    fake.fiona_adapter_batch_destroy(h)
