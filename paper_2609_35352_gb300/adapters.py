@@ -125,13 +125,14 @@ def _handle(stream: Any) -> int:
 
 def _indices(values: Any, dtype: Any, name: str) -> np.ndarray:
     """Whole numbers as a C array (numpy would wrap what does not fit, and cut fractions)."""
-    v, limits = np.asarray(values), np.iinfo(dtype)
-    if v.size == 0:
-        return np.zeros(v.shape, dtype)
-    top = limits.max if v.dtype.kind in "iu" else min(limits.max, 1 << 53)
-    if v.dtype.kind not in "iuf" or not (v.min() >= limits.min and v.max() <= top) or (v != np.floor(v)).any():
+    v = np.asarray(values)
+    if v.dtype == dtype or v.size == 0:
+        return np.ascontiguousarray(v, dtype)
+    limits, whole = np.iinfo(dtype), v.dtype.kind in "iu"
+    if not (whole or v.dtype.kind == "f") or not (v.min() >= limits.min and v.max() <= (limits.max if whole else min(limits.max, 1 << 53))) \
+            or not (whole or (v == np.floor(v)).all()):
         raise ValueError("%s: whole numbers from %d to %d expected" % (name, limits.min, limits.max))
-    return np.ascontiguousarray(v.astype(dtype))
+    return np.ascontiguousarray(v, dtype)
 
 
 class Batch:
@@ -144,7 +145,7 @@ class Batch:
                  r_max: int, scales: Optional[Sequence[float]] = None, gradients: bool = True):
         s, a, r = (_indices(v, t, n) for v, t, n in ((starts, np.uint64, "starts"), (adapters, np.int32, "adapters"),
                                                      (ranks, np.uint32, "ranks")))
-        r_max = int(_indices([r_max], np.uint32, "r_max")[0])
+        r_max = r_max if type(r_max) is int and 0 <= r_max < 1 << 32 else int(_indices([r_max], np.uint32, "r_max")[0])
         if s.ndim != 1 or a.ndim != 1 or r.ndim != 1 or s.shape[0] != a.shape[0] + 1:
             raise ValueError("starts must have one entry more than adapters")
         c = None

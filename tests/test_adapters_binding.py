@@ -68,6 +68,7 @@ def test_indices_are_taken_as_they_are(ctx):
     AD.Batch(ctx, [0], [], [], 8)
     for change in (dict(adapters=np.array([1 << 32, -1])), dict(adapters=[0.5, -1]), dict(ranks=np.array([(1 << 32) + 4, 8])),
                    dict(ranks=np.array([4, -(1 << 32)])), dict(starts=np.array([0, 3.5, 5])), dict(starts=[0, float("nan"), 5]),
-                   dict(starts=[0, -1, 5]), dict(adapters=[1 << 40, -1]), dict(ranks=["a", 8]), dict(r_max=8.5)):
+                   dict(starts=[0, -1, 5]), dict(adapters=[1 << 40, -1]), dict(ranks=np.array([2.0 ** 33, 8])), dict(adapters=[float(1 << 31), -1]),
+                   dict(starts=[0, 2.0 ** 64, 5]), dict(r_max=-1), dict(r_max=(1 << 32) + 8), dict(r_max=float("nan")), dict(ranks=["a", 8]), dict(r_max=8.5)):
         with pytest.raises(ValueError):
             AD.Batch(ctx, **dict(good, **change))
