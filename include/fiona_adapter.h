@@ -43,8 +43,10 @@
  * tensor cores' accumulator cuts an addition where fp32 would round it: chains
  * of such additions are bounded, whatever the sizes, so that a sum loses at most
  * some 2^-16 (dA and dB: 2^-15) of its terms' absolute values; the chains are
- * added up in fp32.  Results
- * do not depend on the order in which blocks run: no atomics on values.
+ * added up in fp32.  Where a used element of x, dy, A or B is infinite, a result
+ * may be NaN where the formula is infinite (the two parts' products with it
+ * differ in sign, or one part is zero).  Results do not depend on the order in
+ * which blocks run: no atomics on values.
  *
  * Dropout D on a [rows][cols] matrix, for a probability p in [0, 1]: with
  * level = p 65536 rounded to the nearest integer (ties to even), element (t, i)
@@ -94,8 +96,9 @@ typedef struct fiona_dropout_spec {
  * entries, starts[0] = 0, not decreasing, at most 2^26 rows; a request may be
  * empty) and uses adapter `adapter[r]` (-1: none).  ranks[a] <= r_max, which is
  * 1 .. 128; a rank of 0 is an adapter that adds nothing.  scales == NULL: 1.  One batch
- * serves every layer of a model, whatever its sizes.  The arrays are copied; the
- * device copy is synchronous.
+ * serves every layer of a model, whatever its sizes.  The arrays are copied, and
+ * the device's copies are there when the call returns.  The batch keeps a pointer
+ * to ctx: destroy it first.
  * Errors: FIONA_ERR_ARG, FIONA_ERR_PLAN (the arrays do not describe a batch),
  * FIONA_ERR_NOMEM, FIONA_ERR_CUDA.  On a validation-only context the arrays are
  * checked and evaluations return FIONA_ERR_NODEVICE. */

@@ -1,6 +1,5 @@
-// adapter_any.cu -- the adapters' products on the FMA units: fp32, whose sums the
-// tensor cores would not keep, and 16-bit rows that TMA cannot address (a width,
-// stride or start that is no multiple of 16 bytes).
+// adapter_any.cu -- the adapters' products on the FMA units: fp32, and 16-bit rows that
+// TMA cannot address (a width, stride or start that is no multiple of 16 bytes).
 //
 // The four passes of adapter_tiles.cu on half tiles of 64 rows, in fp32 throughout:
 // shrink (h or dh over a range of columns), expand (out or dx, 64 columns) and the

@@ -6,8 +6,8 @@
 // Bound by HBM and L2: a copy moves its buffer twice more.  That and two launches
 // are what a call on the FMA units (adapter_any.cu) has to cost more for this to be
 // taken (adapter_pad_us).  Measured on GB300: 6611 rows, 4992 -> 4428, rank 64, forward
-// 88 us (419 on the FMA units); 10571 rows, 4224 -> 3136, rank 43, backward 99 us (857);
-// 9386 rows, 1280 -> 4459, rank 32, backward with dropout 82 us (495).
+// 87 us a call (419 on the FMA units); 10571 rows, 4224 -> 3136, rank 43, backward 97 us
+// (857); 9386 rows, 1280 -> 4459, rank 32, backward with dropout 81 us (495).
 #include <cuda_runtime.h>
 
 #include <algorithm>

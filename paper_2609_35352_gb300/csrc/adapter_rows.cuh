@@ -12,7 +12,7 @@
 // requests by the latency of that chain.  Partial sums are added in the order of the
 // CTAs.  Measured on GB300, 256 requests of 200 adapters, 2048 -> 8192, ranks 16 to
 // 64 in rows of 64: 49 us, 246 MB from HBM, as the unused ranks come with the others
-// in lines of 128 bytes (36 us at the copy bandwidth); one request, 768 -> 768, 3.1 us
+// in lines of 128 bytes (36 us at the copy bandwidth); one request, 768 -> 768, 3.2 us
 // in a graph.  Every output stored by the lane that held its sum made the first 58 us
 // (52 in runs, at the time), a cluster of four 63.
 #pragma once

@@ -17,15 +17,16 @@
 // D's factor is applied to the fp32 sums, so that a masked 16-bit x stays exact.
 //
 // The gradients' dB and dA stay in tensor memory while a CTA walks the token
-// tiles of its chunk: 128 columns a lane each, r16 accumulators.  Chunks' sums go to
-// the workspace and are added in order at the end (k_grad_sum).
+// tiles of its chunk, at most kGradTiles: 128 columns a lane each, r16 accumulators.
+// Chunks' sums go to the workspace and are added in order at the end (k_grad_sum),
+// unless every adapter has one chunk: then they are the gradients, and written as such.
 //
 // Bound by HBM, and where a mask is formed by its integer instructions; above rank 64
 // the gradients by the tensor cores, as every product runs on two parts.  A pass that
 // reads 134 MB and does nothing else takes 24.6 us, whatever the boxes' shape, so
 // x or dy is read once a pass and nothing of its size is written in between.
 // Measured on GB300, bf16, 4096 -> 4096: 8192 rows of 24 adapters, ranks 8 to 32,
-// forward 46 us; 16384 rows, rank 32, p = 0.05, forward 78 us, backward 106 us.
+// forward 46 us; 16384 rows, rank 32, p = 0.05, forward 78 us, backward 107 us.
 //
 // Waits are bounded (tiles::Waits).
 #include <cuda.h>
@@ -1466,9 +1467,9 @@ int backward(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const
         g.n_tiles = b->n_tiles;
         g.r16 = f.r.r16;
         g.blocks = f.r.blocks;
-    g.lo = f.r.lo;
-    g.op_boxes = f.r.boxes;
-    g.both = f.r.both;
+        g.lo = f.r.lo;
+        g.op_boxes = f.r.boxes;
+        g.both = f.r.both;
         g.err = b->ctx->d_kerr;
         g.wait_ns = b->wait_ns;
         g.stall = b->stall;
