@@ -9,88 +9,18 @@
 #include <new>
 
 #include "adapter_tiles.h"
+#include "checks.h"
 #include "device_guard.h"
 #include "upload.h"
 
 namespace {
 
+using namespace checks;
+
 constexpr uint64_t kMaxTokens = 1ull << 26;
 constexpr uint32_t kMaxWidth = 1u << 20;
 constexpr uint32_t kMaxAdapters = 1u << 20;
 constexpr uint32_t kBareRows = 4;   // rows without an adapter that a CTA copies
-
-int cuda_fail(cudaError_t e, const char *what)
-{
-    return e == cudaErrorMemoryAllocation ? set_error(FIONA_ERR_NOMEM, "%s: device allocation", what)
-                                          : set_error(FIONA_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
-}
-
-uint64_t element(uint32_t dtype) { return dtype == FIONA_F32 ? 4 : 2; }
-
-uint64_t align_up(uint64_t n) { return (n + 255) & ~255ull; }
-
-// A strided matrix of one call.
-struct View {
-    const void *p;
-    uint64_t rows, cols, ld, size;  // ld in elements, size of one
-    const char *name;
-    uint64_t bytes() const { return rows && cols ? ((rows - 1) * ld + cols) * size : 0; }
-};
-
-// Whether two matrices share a byte, or cannot be told not to.  Two column
-// ranges of one buffer (the same stride) may interleave.
-bool overlap(const View &a, const View &b)
-{
-    const uint64_t p = (uint64_t)(uintptr_t)a.p, q = (uint64_t)(uintptr_t)b.p;
-    if (!a.bytes() || !b.bytes()) return false;
-    if (q >= p ? q - p >= a.bytes() : p - q >= b.bytes()) return false;
-    const uint64_t row = a.ld * a.size;
-    if (row != b.ld * b.size || a.cols * a.size > row || b.cols * b.size > row) return true;
-    const uint64_t off = q >= p ? (q - p) % row : (row - (p - q) % row) % row;
-    return off < a.cols * a.size || off + b.cols * b.size > row;
-}
-
-int check_input(const View &v, uint64_t align, const char *who)
-{
-    if (!v.p) return set_error(FIONA_ERR_ARG, "%s: null %s", who, v.name);
-    if ((uintptr_t)v.p % align) return set_error(FIONA_ERR_ARG, "%s: %s is not %llu-byte aligned", who, v.name, (unsigned long long)align);
-    const uint64_t reach = std::max<uint64_t>(std::max(v.ld, v.cols), 1);
-    if (v.ld >= (1ull << 40) || v.rows >= (1ull << 40) || v.rows > (1ull << 60) / reach)  // (no product that could wrap)
-        return set_error(FIONA_ERR_ARG, "%s: rows or row stride of %s out of range", who, v.name);
-    return FIONA_OK;
-}
-
-int check_output(const View &v, uint64_t align, const char *who)
-{
-    const int rc = check_input(v, align, who);
-    if (rc) return rc;
-    if (v.rows > 1 && v.ld < v.cols)
-        return set_error(FIONA_ERR_ARG, "%s: row stride of %s (%llu) below its width (%llu)", who, v.name,
-                         (unsigned long long)v.ld, (unsigned long long)v.cols);
-    return FIONA_OK;
-}
-
-// `in_place`: which of the others `out` may be, or -1
-int check_apart(const View &out, const View *others, int n, int in_place, const char *who)
-{
-    for (int i = 0; i < n; ++i) {
-        if (!others[i].p || (i == in_place && others[i].p == out.p && (others[i].ld == out.ld || out.rows == 1))) continue;
-        if (overlap(out, others[i])) return set_error(FIONA_ERR_ARG, "%s: %s overlaps %s", who, out.name, others[i].name);
-    }
-    return FIONA_OK;
-}
-
-int make_mask(const fiona_dropout_spec *d, uint64_t cols, dropout::Mask &m, const char *who)
-{
-    m = dropout::Mask();
-    m.groups = (cols + 3) / 4;
-    if (!d) return FIONA_OK;
-    if (!(d->p >= 0.0 && d->p <= 1.0)) return set_error(FIONA_ERR_ARG, "%s: dropout probability outside [0, 1]", who);
-    m.level = (uint32_t)std::nearbyint(d->p * 65536.0);
-    m.factor = m.level < 65536 ? (float)(65536.0 / (65536.0 - m.level)) : 0.f;
-    m.base = dropout::mix64(d->seed + (dropout::kStream + 1) * dropout::kGolden) + (d->offset + 1) * dropout::kGolden;
-    return FIONA_OK;
-}
 
 int check_layer(const fiona_adapter_batch *b, const fiona_adapter_layer *l, const char *who)
 {
@@ -114,15 +44,6 @@ uint64_t work_needed(const fiona_adapter_batch *b, uint32_t d_in, uint32_t d_out
 
 // rows that TMA can address
 bool tma_rows(const View &v) { return !v.p || (((uintptr_t)v.p | (v.ld * v.size)) % 16 == 0 && v.ld >= v.cols); }
-
-int check_work(uint64_t needed, const void *work, uint64_t bytes, const char *who)
-{
-    if (needed && (!work || ((uintptr_t)work & 15))) return set_error(FIONA_ERR_ARG, "%s: null or misaligned workspace", who);
-    if (bytes < needed)
-        return set_error(FIONA_ERR_ARG, "%s: workspace of %llu bytes, %llu needed", who, (unsigned long long)bytes,
-                         (unsigned long long)needed);
-    return FIONA_OK;
-}
 
 AdapterArgs common_args(const fiona_adapter_batch *b, const fiona_adapter_layer *l)
 {
@@ -359,8 +280,8 @@ extern "C" int fiona_adapter_forward(const fiona_adapter_batch *b, void *stream,
         (h && (rc = check_output(vh, 16, who))) || (rc = check_work(needed, work, work_bytes, who)))
         return rc;
     const View inputs[] = {vx, vbase, vA, vB, vh, vwork};
-    if ((rc = check_apart(vout, inputs, 6, 1, who)) || (h && (rc = check_apart(vh, inputs, 4, -1, who))) ||
-        (rc = check_apart(vwork, inputs, 5, -1, who)))
+    if ((rc = check_apart(vout, inputs, 6, 1u << 1, who)) || (h && (rc = check_apart(vh, inputs, 4, 0, who))) ||
+        (rc = check_apart(vwork, inputs, 5, 0, who)))
         return rc;
     if (b->ctx->device == FIONA_DEVICE_NONE) return set_error(FIONA_ERR_NODEVICE, "%s: validation-only context", who);
     DeviceGuard g(b->ctx->device);
@@ -418,8 +339,8 @@ extern "C" int fiona_adapter_backward(const fiona_adapter_batch *b, void *stream
         return rc;
     if (b->n_adapters && ((rc = check_output(vdA, 16, who)) || (rc = check_output(vdB, 16, who)))) return rc;
     const View inputs[] = {vx, vh, vdy, vbase, vA, vB, vwork, vdA, vdB};
-    if ((rc = check_apart(vdx, inputs, 9, 3, who)) || (rc = check_apart(vdA, inputs, 7, -1, who)) ||
-        (rc = check_apart(vdB, inputs, 8, -1, who)) || (rc = check_apart(vwork, inputs, 6, -1, who)))
+    if ((rc = check_apart(vdx, inputs, 9, 1u << 3, who)) || (rc = check_apart(vdA, inputs, 7, 0, who)) ||
+        (rc = check_apart(vdB, inputs, 8, 0, who)) || (rc = check_apart(vwork, inputs, 6, 0, who)))
         return rc;
     if (b->ctx->device == FIONA_DEVICE_NONE) return set_error(FIONA_ERR_NODEVICE, "%s: validation-only context", who);
     if (!T && !b->n_adapters) return FIONA_OK;
@@ -460,7 +381,7 @@ extern "C" int fiona_dropout(const fiona_ctx *ctx, void *stream, uint32_t dtype,
     const View vx{x, rows, cols, ldx, e, "x"}, vres{residual, rows, cols, ld_residual, e, "residual"};
     const View vout{out, rows, cols, ld_out, e, "out"};
     if ((rc = check_input(vx, e, who)) || (residual && (rc = check_input(vres, e, who))) || (rc = check_output(vout, e, who)) ||
-        (rc = check_apart(vout, &vx, 1, 0, who)) || (rc = check_apart(vout, &vres, 1, 0, who)))
+        (rc = check_apart(vout, &vx, 1, 1, who)) || (rc = check_apart(vout, &vres, 1, 1, who)))
         return rc;
     if (ctx->device == FIONA_DEVICE_NONE) return set_error(FIONA_ERR_NODEVICE, "%s: validation-only context", who);
     DeviceGuard g(ctx->device);

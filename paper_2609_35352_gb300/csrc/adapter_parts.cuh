@@ -5,21 +5,16 @@
 #include <stdint.h>
 
 #include "adapter_tiles.h"
+#include "launch.cuh"
 #include "real.cuh"
 
 namespace parts {
 
+using launches::launch;
+using launches::next_may_start;
+using launches::previous_done;
 using real::narrow;
 using real::widen;
-
-// Launches overlap: a kernel lets the next start at once (`next_may_start`), and the
-// next waits for it, as a whole (`previous_done`), before it touches anything that a
-// kernel before it writes.  The first kernel of a call waits for what came before
-// the call, before it reads anything, and only then lets the next start: so the later
-// ones may read the call's inputs without waiting.  Every kernel waits before it
-// ends, so that the last one's end is the end of all.
-__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void previous_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // Sums over column ranges of the partial h or dh: N pieces of four ranks at once,
 // piece i at element at[i] of a range (none where that is negative), all of
@@ -99,25 +94,6 @@ struct GradSum {
 int launch_any_grad_sum(const fiona_adapter_batch *b, cudaStream_t s, uint32_t dtype, const GradSum &A, const GradSum &B);
 
 constexpr uint64_t kMostBlocks = 0x7FFFFFFF;  // of a grid
-
-// a kernel that waits for the one before it by itself
-template <typename K>
-inline int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t s, void **args, const char *what)
-{
-    cudaLaunchConfig_t c{};
-    c.gridDim = grid;
-    c.blockDim = dim3(threads);
-    c.dynamicSmemBytes = smem;
-    c.stream = s;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = &attr;
-    c.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelExC(&c, (const void *)kernel, args);
-    if (e != cudaSuccess) return set_error(FIONA_ERR_CUDA, "%s launch: %s", what, cudaGetErrorString(e));
-    return FIONA_OK;
-}
 
 // the same for `blocks` in one dimension, which may be more than a grid holds
 template <typename K>
