@@ -1,0 +1,301 @@
+"""Layer norm with dropout and residual, and its gradient, against the formulas in 64
+bits (norm_util.py derives what rounding may do)."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+from paper_2609_35352_gb300 import adapters as AD  # noqa: E402
+from paper_2609_35352_gb300 import build as BUILD  # noqa: E402
+from paper_2609_35352_gb300 import fiona as F  # noqa: E402
+from paper_2609_35352_gb300 import layernorm as LN  # noqa: E402
+from paper_2609_35352_gb300 import workloads as W  # noqa: E402
+
+import norm_util as NU  # noqa: E402
+from adapter_util import keep_mask  # noqa: E402
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+SHAPES = [(1, 1, 0), (1, 768, 0), (3, 5, 0), (17, 64, 0), (300, 777, 0), (64, 1024, 0), (33, 256, 2), (33, 250, 8),
+          (5, 4099, 3), (2, 65536, 0), (1, 1 << 20, 0), (1000, 8, 0), (2047, 33, 0), (7, 16384, 0), (5, 16392, 0), (130, 2048, 0),
+          (40, 8192, 0), (9, 12288, 8), (11, 4096, 0), (10, 511, 1), (700, 264, 0), (3, 32768, 0), (4, 20000, 0)]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    BUILD.build()
+    return F.Context(1024, W.ntt_primes(1024, 50, 1), device=0)
+
+
+def make(rows, cols, dtype, pad=0, seed=0, scale=1.0, shift=0.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    t = (torch.randn(rows, cols + pad, generator=g, device="cuda") * scale + shift).to(DT[dtype])
+    return t[:, pad // 2:pad // 2 + cols]
+
+
+def vector(cols, dtype, seed, scale=1.0, shift=0.0):
+    return make(1, cols, dtype, 0, seed, scale, shift)[0].contiguous()
+
+
+def f64(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def run_forward(ctx, x, res, weight, bias, eps, drop, stream=None):
+    rows = x.shape[0]
+    r = {"out": torch.empty_strided(x.shape, (max(x.stride(0), x.shape[1]), 1), dtype=x.dtype, device="cuda"),
+         "sum": torch.empty(x.shape, dtype=x.dtype, device="cuda"), "mean": torch.empty(rows, device="cuda"),
+         "rstd": torch.empty(rows, device="cuda")}
+    LN.layer_norm(ctx, x, r["out"], weight=weight, bias=bias, eps=eps, residual=res, dropout=drop, sum=r["sum"], mean=r["mean"],
+                  rstd=r["rstd"], stream=stream)
+    return r
+
+
+def check_all(dtype, wtype, got, want):
+    for k, (value, bound) in want.items():
+        if got.get(k) is not None:
+            NU.check(k, "f32" if k in ("mean", "rstd") else wtype if k in ("dweight", "dbias") else dtype, f64(got[k]), value, bound)
+
+
+def spec(drop):
+    return None if drop is None else (drop.p, drop.seed, drop.offset)
+
+
+@pytest.mark.parametrize("dtype,wtype", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f32")])
+@pytest.mark.parametrize("rows,cols,pad", SHAPES)
+def test_forward(ctx, dtype, wtype, rows, cols, pad):
+    x, res = make(rows, cols, dtype, pad, 1), make(rows, cols, dtype, pad, 2, 2.0, 0.5)
+    weight, bias = vector(cols, wtype, 3, 0.2, 1.0), vector(cols, wtype, 4)
+    for drop, r, w, b in ((AD.Dropout(0.2, 2609 + cols, (1 << 50) + rows), res, weight, bias), (None, None, weight, None), (None, res, None, bias)):
+        got = run_forward(ctx, x, r, w, b, 1e-5, drop)
+        check_all(dtype, wtype, got, NU.forward(f64(x), f64(r), f64(w), f64(b), 1e-5, spec(drop)))
+        plain = torch.empty_like(x)
+        LN.layer_norm(ctx, x, plain, weight=w, bias=b, residual=r, dropout=drop)  # (nothing kept)
+        assert torch.equal(plain, got["out"])
+
+
+@pytest.mark.parametrize("dtype,wtype", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f32")])
+@pytest.mark.parametrize("rows,cols,pad", SHAPES)
+def test_backward(ctx, dtype, wtype, rows, cols, pad):
+    dy, s, dsum = make(rows, cols, dtype, pad, 1), make(rows, cols, dtype, pad, 2, 2.0, 0.5), make(rows, cols, dtype, pad, 3)
+    weight = vector(cols, wtype, 4, 0.2, 1.0)
+    mean, rstd = s.double().mean(1).float(), (s.double().var(1, unbiased=False) + 1e-5).rsqrt().float()
+    work = LN.workspace(ctx, rows, cols)
+    for drop, w, extra in ((AD.Dropout(0.2, 7, 1 << 40), weight, None), (None, weight, dsum), (None, None, None)):
+        got = {"dx": torch.empty_like(dy), "dresidual": torch.empty_strided(dy.shape, dy.stride(), dtype=dy.dtype, device="cuda"),
+               "dweight": torch.empty(cols, dtype=DT[wtype], device="cuda"), "dbias": torch.empty(cols, dtype=DT[wtype], device="cuda")}
+        LN.layer_norm_backward(ctx, dy, s, mean, rstd, weight=w, dsum=extra, dropout=drop, work=work, **got)
+        check_all(dtype, wtype, got, NU.backward(f64(dy), f64(s), f64(mean), f64(rstd), f64(w), f64(extra), spec(drop)))
+        if drop is None:
+            assert torch.equal(got["dx"], got["dresidual"])
+        # each output by itself is the same
+        for k in got:
+            one = torch.empty_like(got[k])
+            LN.layer_norm_backward(ctx, dy, s, mean, rstd, weight=w, dsum=extra, dropout=drop, work=work, **{k: one})
+            assert torch.equal(one, got[k]), k
+
+
+def test_random_sizes(ctx):
+    rng = np.random.default_rng(2609)
+    for i in range(60):
+        rows, cols = int(np.exp(rng.uniform(0, 7))), int(np.exp(rng.uniform(0, 9.3)))
+        dtype, pad = ["f32", "f16", "bf16"][i % 3], int(rng.integers(0, 9))
+        wtype = dtype if rng.random() < 0.5 else "f32"
+        drop = AD.Dropout(float(rng.choice([0.1, 0.5])), i, i << 33) if rng.random() < 0.5 else None
+        x, res = make(rows, cols, dtype, pad, i), make(rows, cols, dtype, 0, i + 1000, 3.0) if rng.random() < 0.5 else None
+        weight, bias = vector(cols, wtype, i + 1, 0.2, 1.0), vector(cols, wtype, i + 2)
+        got = run_forward(ctx, x, res, weight, bias, 1e-6, drop)
+        check_all(dtype, wtype, got, NU.forward(f64(x), f64(res), f64(weight), f64(bias), 1e-6, spec(drop)))
+        dy = make(rows, cols, dtype, pad, i + 3)
+        g = {"dx": torch.empty_like(dy), "dweight": torch.empty_like(weight), "dbias": torch.empty_like(weight), "dresidual": torch.empty_like(dy)}
+        LN.layer_norm_backward(ctx, dy, got["sum"], got["mean"], got["rstd"], weight=weight, dropout=drop, work=LN.workspace(ctx, rows, cols), **g)
+        check_all(dtype, wtype, g, NU.backward(f64(dy), f64(got["sum"]), f64(got["mean"]), f64(got["rstd"]), f64(weight), None, spec(drop)))
+
+
+@pytest.mark.parametrize("cols", [96, 700, 4096, 17000])
+def test_gradient_against_differences(ctx, cols):
+    """fp32: the loss sum(c out) by differences of the kernel's own formula in 64 bits."""
+    rows, h = 3, 1e-4
+    x, res, c = make(rows, cols, "f32", 0, 1), make(rows, cols, "f32", 0, 2), make(rows, cols, "f32", 0, 3)
+    weight, bias, drop = vector(cols, "f32", 4, 0.2, 1.0), vector(cols, "f32", 5), AD.Dropout(0.3, 11)
+    f = run_forward(ctx, x, res, weight, bias, 1e-5, drop)
+    g = {k: torch.empty_like(t) for k, t in (("dx", x), ("dresidual", x), ("dweight", weight), ("dbias", bias))}
+    LN.layer_norm_backward(ctx, c, f["sum"], f["mean"], f["rstd"], weight=weight, dropout=drop, work=LN.workspace(ctx, rows, cols), **g)
+
+    def loss(**change):
+        v = {"x": f64(x), "res": f64(res), "weight": f64(weight), "bias": f64(bias)}
+        for k, d in change.items():
+            v[k] = v[k] + d
+        return (f64(c) * NU.forward(v["x"], v["res"], v["weight"], v["bias"], 1e-5, spec(drop))["out"][0]).sum()
+
+    rng = np.random.default_rng(1)
+    for arg, grad in (("x", "dx"), ("res", "dresidual"), ("weight", "dweight"), ("bias", "dbias")):
+        d = rng.standard_normal(f64(g[grad]).shape)
+        slope = (loss(**{arg: h * d}) - loss(**{arg: -h * d})) / (2 * h)
+        # (the difference's own error is h^2 of third derivatives; the kernel's 32 bits)
+        assert abs(slope - (f64(g[grad]) * d).sum()) <= 1e-4 * np.abs(f64(g[grad]) * d).sum() ** 0.5 * max(1.0, abs(slope)) ** 0.5 + 1e-4
+
+
+def test_in_place_and_neighbours(ctx):
+    for dtype in DT:
+        for cols in (96, 100, 1024, 18000):
+            x, res = make(40, cols, dtype, 0, 1), make(40, cols, dtype, 0, 2)
+            weight, bias, drop = vector(cols, dtype, 3), vector(cols, dtype, 4), AD.Dropout(0.4, 5)
+            want = run_forward(ctx, x, res, weight, bias, 1e-5, drop)
+            for out_is, sum_is in (("x", "res"), ("res", "x"), (None, "res"), ("x", None)):
+                a = {"x": x.clone(), "res": res.clone()}
+                out, total = a.get(out_is, torch.empty_like(x)), a.get(sum_is, torch.empty_like(x))
+                LN.layer_norm(ctx, a["x"], out, weight=weight, bias=bias, residual=a["res"], dropout=drop, sum=total)
+                assert torch.equal(out, want["out"]) and torch.equal(total, want["sum"])
+            wide = torch.full((40, cols + 64), 3.0, dtype=DT[dtype], device="cuda")
+            LN.layer_norm(ctx, x, wide[:, 9:9 + cols], weight=weight, bias=bias, residual=res, dropout=drop)
+            assert torch.equal(wide[:, 9:9 + cols], want["out"])
+            assert (wide[:, :9] == 3).all() and (wide[:, 9 + cols:] == 3).all()
+            # the gradient: outputs in the place of inputs
+            dy, dsum, work = make(40, cols, dtype, 0, 6), make(40, cols, dtype, 0, 7), LN.workspace(ctx, 40, cols)
+            g = {k: torch.empty_like(t) for k, t in (("dx", dy), ("dresidual", dy), ("dweight", weight), ("dbias", weight))}
+            LN.layer_norm_backward(ctx, dy, want["sum"], want["mean"], want["rstd"], weight=weight, dsum=dsum, dropout=drop, work=work, **g)
+            for p, q in (("dy", "sum"), ("sum", "dsum"), ("dsum", "dy"), ("dy", None), (None, "dsum")):
+                a = {"dy": dy.clone(), "sum": want["sum"].clone(), "dsum": dsum.clone()}
+                dx, dres = a.get(p, torch.empty_like(dy)), a.get(q, torch.empty_like(dy))
+                dw, db = torch.empty_like(weight), torch.empty_like(weight)
+                LN.layer_norm_backward(ctx, a["dy"], a["sum"], want["mean"], want["rstd"], weight=weight, dsum=a["dsum"], dropout=drop,
+                                       dx=dx, dresidual=dres, dweight=dw, dbias=db, work=work)
+                assert torch.equal(dx, g["dx"]) and torch.equal(dres, g["dresidual"]) and torch.equal(dw, g["dweight"]) and torch.equal(db, g["dbias"])
+
+
+def test_is_dropout_then_norm(ctx):
+    """The sum is what `dropout` gives, bit for bit."""
+    for dtype in DT:
+        for cols in (64, 333, 4096):
+            x, res, drop = make(50, cols, dtype, 0, 1), make(50, cols, dtype, 0, 2), AD.Dropout(0.3, 9, 77)
+            want = torch.empty_like(x)
+            AD.dropout(ctx, x, want, drop, residual=res)
+            assert torch.equal(run_forward(ctx, x, res, None, None, 1e-5, drop)["sum"], want)
+
+
+def test_rows_by_themselves(ctx):
+    """A row's result does not depend on the others: rows one by one, with the mask's
+    offset moved on, and one row for all by a stride of 0."""
+    for dtype in DT:
+        for cols in (40, 1000, 5000):
+            x, res, drop = make(23, cols, dtype, 0, 1), make(23, cols, dtype, 0, 2), AD.Dropout(0.25, 5, 11)
+            weight, bias = vector(cols, dtype, 3), vector(cols, dtype, 4)
+            want = run_forward(ctx, x, res, weight, bias, 1e-5, drop)
+            for t in (0, 7, 22):
+                got = run_forward(ctx, x[t:t + 1], res[t:t + 1], weight, bias, 1e-5, drop.advance(t, cols))
+                assert all(torch.equal(got[k], want[k][t:t + 1]) for k in want)
+            same = run_forward(ctx, x[:1].expand(23, cols), None, weight, bias, 1e-5, None)
+            one = run_forward(ctx, x[:1], None, weight, bias, 1e-5, None)
+            assert all(torch.equal(same[k], one[k].expand_as(same[k])) for k in same)
+
+
+def test_infinities_and_nans_stay_in_their_rows(ctx):
+    for dtype in DT:
+        for cols in (64, 1000, 4096, 17000):
+            x = make(12, cols, dtype, 0, 1)
+            clean = run_forward(ctx, x, None, None, None, 1e-5, None)
+            x[3, cols // 2], x[5, 0], x[7, cols - 1] = float("inf"), float("nan"), float("-inf")
+            got = run_forward(ctx, x, None, None, None, 1e-5, None)
+            bad = [3, 5, 7]
+            good = [t for t in range(12) if t not in bad]
+            assert torch.isnan(got["out"][bad]).all() and torch.isnan(got["rstd"][bad]).all()
+            assert all(torch.equal(got[k][good], clean[k][good]) for k in got)
+            # what is dropped does not count, whatever it held
+            drop = AD.Dropout(0.5, 3)
+            keep = torch.from_numpy(keep_mask(12, cols, 0.5, 3, 0)).cuda()
+            y = torch.where(keep, make(12, cols, dtype, 0, 2), float("nan"))
+            z = torch.where(keep, y, 0.0)
+            a, b = run_forward(ctx, y, None, None, None, 1e-5, drop), run_forward(ctx, z, None, None, None, 1e-5, drop)
+            assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+def test_flat_rows_and_far_means(ctx):
+    """Rows of one value: out = bias, rstd = 1 / sqrt(eps).  A mean that is large beside the
+    spread: within what norm_util allows, far below the rounding of the mean in fp32."""
+    for cols in (1, 3, 256, 1000, 4096, 20000):
+        x = torch.full((5, cols), 1000.3, device="cuda")
+        bias = vector(cols, "f32", 1)
+        got = run_forward(ctx, x, None, None, bias, 1e-5, None)
+        check_all("f32", "f32", got, NU.forward(f64(x), None, None, f64(bias), 1e-5))
+        assert (got["rstd"] - 1e5 ** 0.5).abs().max() < 0.01
+        if cols > 3:
+            x = make(5, cols, "f32", 0, 2, 1.0, 3e4)
+            got = run_forward(ctx, x, None, None, None, 1e-5, None)
+            check_all("f32", "f32", got, NU.forward(f64(x), None, None, None, 1e-5))
+            assert (got["out"].double().mean(1).abs() < 2e-6 * cols ** 0.5 + 1e-5).all()
+
+
+def test_no_rows(ctx):
+    for dtype in DT:
+        x = make(0, 64, dtype)
+        weight = vector(64, dtype, 1)
+        got = run_forward(ctx, x, None, weight, None, 1e-5, None)
+        dw, db = torch.full_like(weight, 7), torch.full_like(weight, 7)
+        LN.layer_norm_backward(ctx, x, x, got["mean"], got["rstd"], weight=weight, dweight=dw, dbias=db)
+        assert (dw == 0).all() and (db == 0).all()
+
+
+def test_many_rows(ctx):
+    """Element offsets past 32 bits; a long sum over the rows."""
+    rows, cols = 4_500_000, 1000
+    row = make(1, cols, "f16", 0, 1)
+    x = row.expand(rows, cols)
+    out, mean, rstd = torch.empty(rows, cols, dtype=torch.float16, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    drop = AD.Dropout(0.5, 21)
+    LN.layer_norm(ctx, x, out, dropout=drop, mean=mean, rstd=rstd)
+    tail = run_forward(ctx, x[:50], None, None, None, 1e-5, drop.advance(rows - 50, cols))
+    assert torch.equal(out[-50:], tail["out"]) and torch.equal(mean[-50:], tail["mean"])
+    dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    LN.layer_norm_backward(ctx, out, x, mean, rstd, dx=out, dropout=drop, dweight=dw, dbias=db, work=LN.workspace(ctx, rows, cols))
+    back = {"dx": torch.empty(50, cols, dtype=torch.float16, device="cuda")}
+    LN.layer_norm_backward(ctx, tail["out"], x[:50], mean[-50:], rstd[-50:], dropout=drop.advance(rows - 50, cols),
+                           work=LN.workspace(ctx, 50, cols), **back)
+    assert torch.equal(out[-50:], back["dx"])
+    ones = torch.ones(1, cols, dtype=torch.float16, device="cuda").expand(rows, cols)
+    mean.zero_()
+    rstd.fill_(1.0)
+    LN.layer_norm_backward(ctx, ones, x, mean, rstd, dweight=dw, dbias=db, work=LN.workspace(ctx, rows, cols))
+    c = NU.column_chain_of(rows) * 2.0 ** -24
+    assert (db.double() / rows - 1).abs().max() <= c
+    assert (dw.double() / rows - row[0].double()).abs().max() <= (c + 2.0 ** -22) * float(row.abs().max())
+
+
+def test_streams_and_graphs(ctx):
+    """Calls on another stream; a captured forward and backward pass, replayed on new
+    inputs, beside the eager calls."""
+    x, res, dy = make(200, 768, "bf16", 0, 1), make(200, 768, "bf16", 0, 2), make(200, 768, "bf16", 0, 3)
+    weight, bias, drop = vector(768, "f32", 4, 0.2, 1.0), vector(768, "f32", 5), AD.Dropout(0.1, 3)
+    work = LN.workspace(ctx, 200, 768)
+
+    def call(stream, work):
+        f = run_forward(ctx, x, res, weight, bias, 1e-5, drop, stream=stream)
+        g = {"dx": torch.empty_like(dy), "dresidual": torch.empty_like(dy), "dweight": torch.empty_like(weight), "dbias": torch.empty_like(bias)}
+        LN.layer_norm_backward(ctx, dy, f["sum"], f["mean"], f["rstd"], weight=weight, dropout=drop, work=work, stream=stream, **g)
+        return list(f.values()) + list(g.values())
+
+    want = [t.clone() for t in call(None, work)]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = call(s, work)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call(torch.cuda.current_stream(), work)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, held))
+    x.copy_(make(200, 768, "bf16", 0, 9))
+    dy.copy_(make(200, 768, "bf16", 0, 10))
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    new = call(None, LN.workspace(ctx, 200, 768))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(new, held))
+    assert not torch.equal(new[0], want[0])
