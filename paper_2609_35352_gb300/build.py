@@ -36,7 +36,7 @@ LIBRARIES = {
                     "kernel_tiled.cu", "kernel_tiled_off.cu", "kernel_tiled_w12.cu", "kernel_ws.cu", "kernel_gemm.cu", "rescale.cu", "encode.cu",
                     "adapter_host.cpp", "adapter_any.cu", "adapter_rows.cpp", "adapter_rows_f32.cu", "adapter_rows_f16.cu",
                     "adapter_rows_bf16.cu", "adapter_tiles.cu", "adapter_pad.cu",
-                    "dropout.cu", "norm_host.cpp", "norm_any.cu", "optim_host.cpp", "optim.cu"],
+                    "dropout.cu", "norm_host.cpp", "norm_any.cu", "norm_rows_f32.cu", "norm_rows_f16.cu", "norm_rows_bf16.cu", "optim_host.cpp", "optim.cu"],
     "libfiona_workload.so": ["workload_fill.cu", "mul_roof.cu"],
 }
 

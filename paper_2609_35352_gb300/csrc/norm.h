@@ -30,6 +30,8 @@ struct NormGradArgs {
     dropout::Mask mask;
 };
 
+constexpr uint32_t kMostRun = 512;  // rows that one fp32 sum of a column takes before it is written down
+
 // norm_any.cu: any sizes, strides and alignment; the backward pass's workspace
 uint64_t norm_any_grad_work(const fiona_ctx *ctx, uint64_t rows, uint32_t cols);
 int launch_norm_any(const fiona_ctx *ctx, void *stream, uint32_t dtype, uint32_t wtype, const NormArgs &a);

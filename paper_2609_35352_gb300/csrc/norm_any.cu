@@ -15,7 +15,6 @@ namespace {
 using namespace layernorm;
 
 constexpr uint32_t kThreads = 512, kColThreads = 128, kColumns = 4;
-constexpr uint32_t kMostRun = 512;  // rows that one fp32 sum of a column takes before it is written down
 
 // sums over a block of kThreads, the same in every thread
 __device__ float2 block_sum(float2 v, float2 *part)

@@ -7,7 +7,7 @@
 
 #include "checks.h"
 #include "device_guard.h"
-#include "norm.h"
+#include "norm_rows.h"
 
 namespace {
 
@@ -24,6 +24,21 @@ int check_shape(const fiona_ctx *ctx, const Call *c, const char *who)
     if (cols < 1 || cols > FIONA_NORM_MAX_COLS || rows >= (1ull << 40))
         return set_error(FIONA_ERR_ARG, "%s: size out of range", who);
     return FIONA_OK;
+}
+
+// blocks of a backward pass by rows: as many as run at once, or more where a column's
+// sum in one would take more than kMostRun rows
+uint64_t grad_blocks(const fiona_ctx *ctx, uint64_t rows, uint32_t cols)
+{
+    const RowShape s = backward_shape(cols);
+    const uint64_t units = (rows + s.groups() - 1) / s.groups(), sms = ctx->sm_count ? ctx->sm_count : 152;
+    return std::min(units, std::max(sms * (s.lanes <= 256 ? 2 : 1), (units + kMostRun - 1) / kMostRun));
+}
+
+uint64_t grad_work(const fiona_ctx *ctx, uint64_t rows, uint32_t cols, bool sums)
+{
+    if (cols > kMostBackward) return norm_any_grad_work(ctx, rows, cols);
+    return sums ? grad_blocks(ctx, rows, cols) * 2 * cols * 4 : 0;
 }
 
 // a vector of the call (NULL: not there)
@@ -70,7 +85,10 @@ extern "C" int fiona_layer_norm(const fiona_ctx *ctx, void *stream, const fiona_
     a.ld_sum = c->ld_sum;
     a.mean = c->mean;
     a.rstd = c->rstd;
-    return launch_norm_any(ctx, stream, c->dtype, c->weight_dtype, a);
+    if (cols > kMostForward) return launch_norm_any(ctx, stream, c->dtype, c->weight_dtype, a);
+    const bool w16 = c->weight_dtype == c->dtype;
+    return c->dtype == FIONA_F32   ? launch_norm_rows_f32(ctx, stream, a, w16)
+           : c->dtype == FIONA_F16 ? launch_norm_rows_f16(ctx, stream, a, w16) : launch_norm_rows_bf16(ctx, stream, a, w16);
 }
 
 extern "C" int fiona_layer_norm_work_bytes(const fiona_ctx *ctx, uint64_t rows, uint64_t cols, uint64_t *bytes)
@@ -78,7 +96,7 @@ extern "C" int fiona_layer_norm_work_bytes(const fiona_ctx *ctx, uint64_t rows, 
     const char *who = "layer_norm_work_bytes";
     if (!ctx || !bytes) return set_error(FIONA_ERR_ARG, "%s: null argument", who);
     if (cols < 1 || cols > FIONA_NORM_MAX_COLS || rows >= (1ull << 40)) return set_error(FIONA_ERR_ARG, "%s: size out of range", who);
-    *bytes = norm_any_grad_work(ctx, rows, (uint32_t)cols);
+    *bytes = grad_work(ctx, rows, (uint32_t)cols, true);
     return FIONA_OK;
 }
 
@@ -103,7 +121,8 @@ extern "C" int fiona_layer_norm_backward(const fiona_ctx *ctx, void *stream, con
                  (c->dx && (rc = check_output(vdx, e, who))) || (c->dresidual && (rc = check_output(vdr, e, who)))))
         return rc;
     if ((rc = check_vector(vw, we, who)) || (rc = check_vector(vdw, we, who)) || (rc = check_vector(vdb, we, who))) return rc;
-    const uint64_t needed = norm_any_grad_work(ctx, rows, c->cols);
+    const bool sums = c->dweight || c->dbias;
+    const uint64_t needed = grad_work(ctx, rows, c->cols, sums);
     if (rows && (rc = check_work(needed, c->work, c->work_bytes, who))) return rc;
     const View others[] = {vdy, vsum, vds, vw, vm, vr, vwork, vdw, vdb, vdr};
     if ((c->dx && (rc = check_apart(vdx, others, 10, 7, who))) || (c->dresidual && (rc = check_apart(vdr, others, 9, 7, who))) ||
@@ -131,5 +150,14 @@ extern "C" int fiona_layer_norm_backward(const fiona_ctx *ctx, void *stream, con
     a.dweight = c->dweight;
     a.dbias = c->dbias;
     if (rows == 0) return launch_norm_grad_sum(stream, c->weight_dtype, nullptr, 0, c->cols, c->dweight, c->dbias);
-    return launch_norm_any_grad(ctx, stream, c->dtype, c->weight_dtype, a, c->work);
+    if (cols > kMostBackward) return launch_norm_any_grad(ctx, stream, c->dtype, c->weight_dtype, a, c->work);
+    const bool w16 = c->weight_dtype == c->dtype;
+    const uint64_t blocks = grad_blocks(ctx, rows, c->cols);
+    if (blocks > 0x7FFFFFFF) return set_error(FIONA_ERR_ARG, "%s: %llu rows", who, (unsigned long long)rows);
+    float *part = sums ? static_cast<float *>(c->work) : nullptr;
+    rc = c->dtype == FIONA_F32   ? launch_norm_rows_grad_f32(ctx, stream, a, w16, (uint32_t)blocks, part)
+         : c->dtype == FIONA_F16 ? launch_norm_rows_grad_f16(ctx, stream, a, w16, (uint32_t)blocks, part)
+                                 : launch_norm_rows_grad_bf16(ctx, stream, a, w16, (uint32_t)blocks, part);
+    if (rc || !sums) return rc;
+    return launch_norm_grad_sum(stream, c->weight_dtype, part, (uint32_t)blocks, c->cols, c->dweight, c->dbias);
 }

@@ -163,6 +163,7 @@ def test_accepted(ctx):
         assert Case(ctx, False).put(**{k: None}) == NODEVICE, k
     for k in ("weight", "dsum", "dx", "dresidual", "dweight", "dbias"):
         assert Case(ctx, True).put(**{k: None}) == NODEVICE, k
+    assert Case(ctx, True).put(dweight=None, dbias=None, work=None, work_bytes=0) == NODEVICE  # no sums: no workspace
     assert Case(ctx, False).put(ldx=0) == NODEVICE  # one row for all
     assert Case(ctx, False).put(rows=0, x=None, out=None) == F.FIONA_OK
     for dt in (0, 1, 2):
