@@ -15,16 +15,29 @@ using launches::previous_done;
 using real::narrow;
 using real::widen;
 
-// sums of two values over a warp, the same in every lane
-__device__ __forceinline__ float2 warp_sum(float2 v)
+// sums over a warp, the same in every lane
+__device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
-    for (uint32_t i = 16; i; i >>= 1) {
-        v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, i);
-        v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, i);
-    }
+    for (uint32_t i = 16; i; i >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, i);
     return v;
 }
+// (each half of the warp takes on one of the two: six exchanges, not ten)
+__device__ __forceinline__ float2 warp_sum(float2 v)
+{
+    const bool upper = threadIdx.x & 16;
+    float s = (upper ? v.y : v.x) + __shfl_xor_sync(0xFFFFFFFFu, upper ? v.x : v.y, 16);
+#pragma unroll
+    for (uint32_t i = 8; i; i >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, i);
+    const float t = __shfl_xor_sync(0xFFFFFFFFu, s, 16);
+    return upper ? make_float2(t, s) : make_float2(s, t);
+}
+
+__device__ __forceinline__ float plus(float a, float b) { return a + b; }
+__device__ __forceinline__ float2 plus(float2 a, float2 b) { return make_float2(a.x + b.x, a.y + b.y); }
+// the value of the lane whose number differs by `mask`
+__device__ __forceinline__ float other(float v, uint32_t mask) { return __shfl_xor_sync(0xFFFFFFFFu, v, mask); }
+__device__ __forceinline__ float2 other(float2 v, uint32_t mask) { return make_float2(other(v.x, mask), other(v.y, mask)); }
 
 // The formulas element by element, each operation said outright, so that every kernel
 // and every path through one rounds in the same places (a compiler may fuse a product
@@ -42,26 +55,50 @@ __device__ __forceinline__ float dropped(const dropout::Mask &m, float v, uint64
 }
 
 // A row's mean is `about + left`: the sum's share, and what its rounding left.
-__device__ __forceinline__ float centred(float s, float about, float left) { return __fsub_rn(__fsub_rn(s, about), left); }
+// Averages below are of d = s - about.
 
-// 1 / sqrt(var + eps) from the averages of d = s - about and of d^2; NaN where they are
+// 1 / sqrt(var + eps) from the averages of d and of d^2; NaN where they are.  (rsqrtf: two
+// units in the last place; the exact root and quotient are 30 instructions a row and thread.)
 __device__ __forceinline__ float rstd_of(float avg_d, float avg_dd, float eps)
 {
     const float var = __fmaf_rn(-avg_d, avg_d, avg_dd);
-    return __frcp_rn(__fsqrt_rn(__fadd_rn(var < 0.f ? 0.f : var, eps)));
+    return rsqrtf(__fadd_rn(var < 0.f ? 0.f : var, eps));
 }
 
-__device__ __forceinline__ float scaled(float centred, float rstd, float weight, float bias)
+// weight (d - left) rstd + bias
+__device__ __forceinline__ float shift_of(float left, float rstd) { return -__fmul_rn(left, rstd); }
+__device__ __forceinline__ float scaled(float d, float rstd, float shift, float weight, float bias)
 {
-    return __fmaf_rn(__fmul_rn(centred, rstd), weight, bias);
+    return __fmaf_rn(__fmaf_rn(d, rstd, shift), weight, bias);
 }
 
 __device__ __forceinline__ float xhat(float s, float mean, float rstd) { return __fmul_rn(__fsub_rn(s, mean), rstd); }
 
-// ds from g and xh, the row's averages of g and g xh, and dsum (0: none)
+// ds from g and xh, the row's averages of g and g xh, and dsum
+__device__ __forceinline__ float gradient(float g, float xh, float2 avg, float rstd)
+{
+    return __fmul_rn(rstd, __fmaf_rn(-xh, avg.y, __fsub_rn(g, avg.x)));
+}
 __device__ __forceinline__ float gradient(float g, float xh, float2 avg, float rstd, float dsum)
 {
     return __fmaf_rn(rstd, __fmaf_rn(-xh, avg.y, __fsub_rn(g, avg.x)), dsum);
+}
+
+// The same for two columns at once (one instruction for both, rounded as one by one).
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 dropped(const dropout::Mask &m, float2 v, bool keep_x, bool keep_y)
+{
+    const float2 k = __fmul2_rn(v, both(m.factor));
+    return make_float2(keep_x ? k.x : 0.f, keep_y ? k.y : 0.f);
+}
+__device__ __forceinline__ float2 scaled(float2 d, float2 rstd, float2 shift, float2 weight, float2 bias)
+{
+    return __ffma2_rn(__ffma2_rn(d, rstd, shift), weight, bias);
+}
+__device__ __forceinline__ float2 xhat(float2 s, float2 minus_mean, float2 rstd) { return __fmul2_rn(__fadd2_rn(s, minus_mean), rstd); }
+__device__ __forceinline__ float2 centred_gradient(float2 g, float2 xh, float2 minus_avg_g, float2 minus_avg_gxh)
+{
+    return __ffma2_rn(xh, minus_avg_gxh, __fadd2_rn(g, minus_avg_g));
 }
 
 }  // namespace layernorm

@@ -47,15 +47,15 @@ __global__ void __launch_bounds__(kThreads) k_norm_any(const NormArgs a)
         const float about = block_sum(s, part).x * per;
         s = make_float2(0.f, 0.f);
         for (uint32_t i = threadIdx.x; i < a.cols; i += kThreads) {
-            const float d = centred(at(i), about, 0.f);
+            const float d = __fsub_rn(at(i), about);
             s.x += d, s.y = __fmaf_rn(d, d, s.y);
         }
         s = block_sum(s, part);
-        const float left = s.x * per, rstd = rstd_of(left, s.y * per, a.eps);
+        const float left = s.x * per, rstd = rstd_of(left, s.y * per, a.eps), shift = shift_of(left, rstd);
         for (uint32_t i = threadIdx.x; i < a.cols; i += kThreads) {
             const float v = at(i), w = a.weight ? widen(((const W *)a.weight)[i]) : 1.f, b = a.bias ? widen(((const W *)a.bias)[i]) : 0.f;
             if (a.sum) ((T *)a.sum)[t * a.ld_sum + i] = narrow<T>(v);
-            ((T *)a.out)[t * a.ld_out + i] = narrow<T>(scaled(centred(v, about, left), rstd, w, b));
+            ((T *)a.out)[t * a.ld_out + i] = narrow<T>(scaled(__fsub_rn(v, about), rstd, shift, w, b));
         }
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[t] = about + left;
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kColThreads) k_columns(const NormGradArgs a, c
                 if (i >= a.cols) continue;
                 const float d = widen(dy[i]), xh = xhat(widen(x[i]), mean, rstd);
                 const float g = __fmul_rn(d, a.weight ? widen(((const W *)a.weight)[i]) : 1.f);
-                const float ds = gradient(g, xh, s, rstd, a.dsum ? widen(((const T *)a.dsum)[t * a.ld_dsum + i]) : 0.f);
+                const float ds = a.dsum ? gradient(g, xh, s, rstd, widen(((const T *)a.dsum)[t * a.ld_dsum + i])) : gradient(g, xh, s, rstd);
                 dw[k] = __fmaf_rn(d, xh, dw[k]), db[k] += d;
                 if (a.dres) ((T *)a.dres)[t * a.ld_dres + i] = narrow<T>(ds);
                 if (a.dx) ((T *)a.dx)[t * a.ld_dx + i] = narrow<T>(dropped(a.mask, ds, dropout::Mask::field(draw, k) >= a.mask.level));

@@ -30,9 +30,9 @@ int check_shape(const fiona_ctx *ctx, const Call *c, const char *who)
 // sum in one would take more than kMostRun rows
 uint64_t grad_blocks(const fiona_ctx *ctx, uint64_t rows, uint32_t cols)
 {
-    const RowShape s = backward_shape(cols);
-    const uint64_t units = (rows + s.groups() - 1) / s.groups(), sms = ctx->sm_count ? ctx->sm_count : 152;
-    return std::min(units, std::max(sms * (s.lanes <= 256 ? 2 : 1), (units + kMostRun - 1) / kMostRun));
+    const uint32_t lanes = backward_lanes(cols);
+    const uint64_t groups = backward_threads(lanes) / lanes, units = (rows + groups - 1) / groups, sms = ctx->sm_count ? ctx->sm_count : 152;
+    return std::min(units, std::max(sms * backward_blocks(cols), (units + kMostRun - 1) / kMostRun));
 }
 
 uint64_t grad_work(const fiona_ctx *ctx, uint64_t rows, uint32_t cols, bool sums)

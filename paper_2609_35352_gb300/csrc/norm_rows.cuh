@@ -1,7 +1,7 @@
 // norm_rows.cuh -- layer norm of rows that a warp or a block holds in registers.
 //
 // Bound by HBM: forward x, residual, out and sum once, backward dy, sum, dx and
-// dresidual (and dsum) once.  A row is spread over LANES threads, EIGHTS times eight
+// dresidual (and dsum) once.  A row is spread over LANES threads, 8 to 32
 // columns each; a block walks over rows a grid apart.  Rows ahead come by 16-byte
 // asynchronous copies into shared memory, each thread's columns into places of its own:
 // it alone reads them, so that nothing but the row's sums needs a barrier, and what is
@@ -20,215 +20,291 @@
 
 namespace layernorm {
 
-// rows in flight: 3 of up to 16 KB a block and buffer, fewer of longer ones (`tensors`
-// buffers at most in 192 KB of shared memory)
-constexpr uint32_t ahead(uint32_t row_bytes, uint32_t tensors) { return row_bytes * tensors * 3 <= 192 * 1024 ? 3 : row_bytes * tensors * 2 <= 192 * 1024 ? 2 : 1; }
+// rows in flight: as many as `room` bytes hold of `tensors` rows, 1 to `most`
+constexpr uint32_t ahead(uint32_t row_bytes, uint32_t tensors, uint32_t room, uint32_t most)
+{
+    return most == 1 || row_bytes * tensors * most <= room ? most : ahead(row_bytes, tensors, room, most - 1);
+}
 
-// eight elements as they lie: one or two vectors
+// K elements as they lie in 16 bytes.  A thread's share of a row is so many of them, LANES
+// apart: the threads of a warp read and write 512 bytes one after another (eight fp32 a
+// thread would be halves of 32-byte sectors, each of them written twice).
 template <typename T>
-struct Eight {
-    static constexpr uint32_t n = sizeof(T) / 2;
-    uint4 u[n];
-    __device__ __forceinline__ void load(const T *p)
+constexpr uint32_t K = 16 / sizeof(T);
+
+template <typename T>
+struct Vector {
+    uint4 u;
+    __device__ __forceinline__ const T *values() const { return reinterpret_cast<const T *>(&u); }
+    __device__ __forceinline__ T *values() { return reinterpret_cast<T *>(&u); }
+    __device__ __forceinline__ void widened(float2 (&v)[K<T> / 2]) const
     {
 #pragma unroll
-        for (uint32_t i = 0; i < n; ++i) u[i] = reinterpret_cast<const uint4 *>(p)[i];
+        for (uint32_t i = 0; i < K<T> / 2; ++i) v[i] = make_float2(widen(values()[2 * i]), widen(values()[2 * i + 1]));
     }
-    __device__ __forceinline__ void store(T *p) const
-    {
-#pragma unroll
-        for (uint32_t i = 0; i < n; ++i) __stcs(reinterpret_cast<uint4 *>(p) + i, u[i]);
-    }
-    __device__ __forceinline__ const T *values() const { return reinterpret_cast<const T *>(u); }
-    __device__ __forceinline__ T *values() { return reinterpret_cast<T *>(u); }
 };
 
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T *row, uint32_t col, uint32_t cols, float (&v)[8])
+__device__ __forceinline__ void load(const T *p, uint32_t left, float2 (&v)[K<T> / 2])  // left: columns from p on
 {
     if (VEC) {
-        Eight<T> e;
-        e.load(row + col);
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) v[i] = widen(e.values()[i]);
+        const Vector<T> x{*reinterpret_cast<const uint4 *>(p)};
+        x.widened(v);
     } else {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) v[i] = col + i < cols ? widen(row[col + i]) : 0.f;
+        for (uint32_t i = 0; i < K<T> / 2; ++i)
+            v[i] = make_float2(2 * i < left ? widen(p[2 * i]) : 0.f, 2 * i + 1 < left ? widen(p[2 * i + 1]) : 0.f);
     }
 }
 
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T *row, uint32_t col, uint32_t cols, const float (&v)[8])
+__device__ __forceinline__ void store(T *p, uint32_t left, const float2 (&v)[K<T> / 2])
 {
     if (VEC) {
-        Eight<T> e;
+        Vector<T> x;
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) e.values()[i] = narrow<T>(v[i]);
-        e.store(row + col);
+        for (uint32_t i = 0; i < K<T> / 2; ++i) x.values()[2 * i] = narrow<T>(v[i].x), x.values()[2 * i + 1] = narrow<T>(v[i].y);
+        __stcs(reinterpret_cast<uint4 *>(p), x.u);
     } else {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-            if (col + i < cols) row[col + i] = narrow<T>(v[i]);
+        for (uint32_t i = 0; i < K<T> / 2; ++i) {
+            if (2 * i < left) p[2 * i] = narrow<T>(v[i].x);
+            if (2 * i + 1 < left) p[2 * i + 1] = narrow<T>(v[i].y);
+        }
     }
 }
 
-// weights or biases of eight columns (null: `none`)
+// column i of a share
+template <uint32_t N>
+__device__ __forceinline__ float of(const float2 (&v)[N], uint32_t i) { return i % 2 ? v[i / 2].y : v[i / 2].x; }
+
+// weights or biases of the columns from `col` on (null: `none`), from global memory
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_weights(const void *p, bool w16, uint32_t col, uint32_t cols, float none, float (&v)[8])
+__device__ __forceinline__ void load_weights(const void *p, bool w16, uint32_t col, uint32_t left, float none, float2 (&v)[K<T> / 2])
 {
     if (!p) {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) v[i] = none;
+        for (uint32_t i = 0; i < K<T> / 2; ++i) v[i] = both(none);
     } else if (w16 || sizeof(T) == 4) {
-        load8<T, VEC>((const T *)p, col, cols, v);
+        load<T, VEC>((const T *)p + col, left, v);
+    } else if (VEC) {
+#pragma unroll
+        for (uint32_t i = 0; i < K<T>; i += 4) {
+            const float4 f = *reinterpret_cast<const float4 *>((const float *)p + col + i);
+            v[i / 2] = make_float2(f.x, f.y), v[i / 2 + 1] = make_float2(f.z, f.w);
+        }
     } else {
-        load8<float, VEC>((const float *)p, col, cols, v);
+#pragma unroll
+        for (uint32_t i = 0; i < K<T> / 2; ++i)
+            v[i] = make_float2(2 * i < left ? ((const float *)p)[col + 2 * i] : 0.f, 2 * i + 1 < left ? ((const float *)p)[col + 2 * i + 1] : 0.f);
     }
 }
 
-// which of eight columns from `col` of row t the mask keeps, a bit each
-__device__ __forceinline__ uint32_t kept(const dropout::Mask &m, uint64_t t, uint32_t col)
+// The mask of N pairs of columns, whose draws are z and those behind it, on their values.  Fields
+// in the places of a word's upper half are compared with the lower half behind them, which
+// decides nothing: upper >= level is word > (level << 16) - 1, for a level of 65536 too.
+template <uint32_t N>
+__device__ __forceinline__ void drop(const dropout::Mask &m, uint64_t z, float2 (&v)[N])
 {
-    const uint64_t a = m.draw(t, col / 4), b = m.draw(t, col / 4 + 1);
-    uint32_t k = 0;
+    const uint32_t limit = (m.level << 16) - 1;
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-        k |= (dropout::Mask::field(a, i) >= m.level) << i;
-        k |= (dropout::Mask::field(b, i) >= m.level) << (4 + i);
+    for (uint32_t d = 0; d < N; d += 2) {
+        const uint64_t draw = dropout::mix64(z + d / 2 * dropout::kGolden);
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) {
+            const uint32_t word = (uint32_t)(draw >> (32 * i));
+            v[d + i] = dropped(m, v[d + i], word << 16 > limit, word > limit);
+        }
     }
-    return k;
 }
 
-// A thread's places in the ring of rows ahead: [stages][tensors][EIGHTS][vectors][threads]
-template <typename T, uint32_t EIGHTS>
+constexpr uint32_t kGradAhead = 3;  // rows ahead in a backward pass
+
+// A thread's places for rows ahead, [stages][tensors][VECS][THREADS]: `now` those of the
+// row that is taken next.
+template <typename T, uint32_t VECS, uint32_t THREADS, uint32_t TENSORS, uint32_t MOST>
 struct Ring {
-    static constexpr uint32_t vectors = Eight<T>::n;
-    uint32_t tensors;
-    uint4 *at;
-    __device__ __forceinline__ uint4 *place(uint32_t stage, uint32_t tensor, uint32_t e) const
+    static constexpr uint32_t tensor = VECS * THREADS;
+    static constexpr uint32_t stages = ahead(tensor * 16, TENSORS, 192 * 1024, MOST);
+    uint4 *begin, *now, *end;
+    uint32_t stage;
+    __device__ __forceinline__ Ring(uint4 *smem, uint32_t tensors)
+        : begin(smem + threadIdx.x), now(begin), end(begin + stages * tensors * tensor), stage(tensors * tensor)
     {
-        return at + (((stage * tensors + tensor) * EIGHTS + e) * vectors) * blockDim.x + threadIdx.x;
     }
-    __device__ __forceinline__ void copy(uint32_t stage, uint32_t tensor, uint32_t e, const T *p) const
+    __device__ __forceinline__ void copy(uint4 *place, uint32_t t, uint32_t e, const T *p) const
     {
-        uint4 *to = place(stage, tensor, e);
-#pragma unroll
-        for (uint32_t i = 0; i < vectors; ++i)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(async::smem_addr(to + i * blockDim.x)), "l"(reinterpret_cast<const uint4 *>(p) + i) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(async::smem_addr(place + t * tensor + e * THREADS)), "l"(p) : "memory");
     }
-    __device__ __forceinline__ void read(uint32_t stage, uint32_t tensor, uint32_t e, float (&v)[8]) const
+    __device__ __forceinline__ void read(uint32_t t, uint32_t e, float2 (&v)[K<T> / 2]) const
     {
-        Eight<T> x;
-        const uint4 *from = place(stage, tensor, e);
-#pragma unroll
-        for (uint32_t i = 0; i < vectors; ++i) x.u[i] = from[i * blockDim.x];
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) v[i] = widen(x.values()[i]);
+        const Vector<T> x{now[t * tensor + e * THREADS]};
+        x.widened(v);
     }
-    static constexpr uint32_t bytes(uint32_t threads) { return EIGHTS * vectors * 16 * threads; }  // of a stage of a tensor
+    __device__ __forceinline__ void next()
+    {
+        now += stage;
+        if (now == end) now = begin;
+    }
 };
 
-// Sums of two values over a row's threads, the same in each of them; `slot`: two in
-// turn, so that one barrier a sum is enough.
-template <uint32_t LANES>
-__device__ __forceinline__ float2 row_sum(float2 v, float2 (*part)[32], uint32_t slot)
+// A thread's weights and biases in shared memory, as they lie: [2][VECS][vectors][THREADS].
+// For blocks of one row at a time: from global memory they would come out of L2 for every
+// row, since the rows ahead take L1's room (16384 x 4096 bf16, two rows in flight: 103 us
+// for 96).  They come by way of L1: copies past it of the same lines by every block go to
+// a few slices of L2 (2048 x 1024 fp32, each warp its own copy: 49 us for 6.5).
+constexpr bool held_weights(uint32_t lanes) { return lanes >= 128 && lanes <= 512; }  // (1024: no room beside the rows)
+
+template <typename T, uint32_t VECS, uint32_t THREADS>
+struct Held {
+    uint4 *at;
+    bool w16;
+    uint32_t parts;  // 16 bytes each of K weights
+    __device__ __forceinline__ Held(uint4 *place, bool w16) : at(place), w16(w16 || sizeof(T) == 4), parts(this->w16 ? 1 : 2) {}
+    static uint32_t bytes(bool w16) { return 2 * VECS * (w16 || sizeof(T) == 4 ? 1 : 2) * THREADS * 16; }
+    __device__ __forceinline__ void copy(uint32_t which, uint32_t e, const void *p, uint32_t col) const
+    {
+        const uint4 *from = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p) + (size_t)col * (w16 ? sizeof(T) : 4));
+        for (uint32_t i = 0; i < parts; ++i)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(async::smem_addr(at + ((which * VECS + e) * parts + i) * THREADS)), "l"(from + i) : "memory");
+    }
+    __device__ __forceinline__ void read(uint32_t which, uint32_t e, float2 (&v)[K<T> / 2]) const
+    {
+        if (w16) {
+            const Vector<T> x{at[(which * VECS + e) * THREADS]};
+            x.widened(v);
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < K<T> / 4; ++k) {
+                const Vector<float> x{at[((which * VECS + e) * 2 + k) * THREADS]};
+#pragma unroll
+                for (uint32_t i = 0; i < 2; ++i) v[2 * k + i] = make_float2(x.values()[2 * i], x.values()[2 * i + 1]);
+            }
+        }
+    }
+};
+
+// Sums over a row's threads, the same in each of them; `slot`: two in turn, so that one
+// barrier a sum is enough.
+template <uint32_t LANES, typename V>
+__device__ __forceinline__ V row_sum(V v, float2 (*part)[32], uint32_t slot)
 {
     v = warp_sum(v);
     if (LANES == 32) return v;
     constexpr uint32_t kWarps = LANES / 32;
     const uint32_t warp = threadIdx.x / 32, first = warp / kWarps * kWarps;
-    if ((threadIdx.x & 31) == 0) part[slot][warp] = v;
+    if ((threadIdx.x & 31) == 0) reinterpret_cast<V &>(part[slot][warp]) = v;
     async::named_barrier(1 + warp / kWarps, LANES);
-    float2 s = part[slot][first];
+    V p[4];
 #pragma unroll
-    for (uint32_t w = 1; w < kWarps; ++w) {
-        const float2 p = part[slot][first + w];
-        s.x += p.x, s.y += p.y;
-    }
-    return s;
+    for (uint32_t w = 0; w < 4; ++w)
+        if (w < kWarps) p[w] = reinterpret_cast<V &>(part[slot][first + w + (kWarps > 4 ? (threadIdx.x % (kWarps < 4 ? 1 : kWarps / 4)) * 4 : 0)]);
+    v = p[0];
+#pragma unroll
+    for (uint32_t w = 1; w < 4; ++w)
+        if (w < kWarps) v = plus(v, p[w]);
+#pragma unroll
+    for (uint32_t i = 1; i < (kWarps + 3) / 4; i *= 2) v = plus(v, other(v, i));
+    return v;
 }
 
-template <typename T, uint32_t LANES, uint32_t EIGHTS, bool VEC>
-__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) k_norm_rows(const NormArgs a, const bool w16)
+template <typename T, uint32_t LANES, uint32_t VECS, bool VEC>
+__global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const NormArgs a, const bool w16)
 {
-    constexpr uint32_t kThreads = LANES < 256 ? 256 : LANES, kGroups = kThreads / LANES;
-    constexpr uint32_t kAhead = ahead(Ring<T, EIGHTS>::bytes(kThreads), 2);
+    constexpr uint32_t kThreads = forward_threads(LANES), kGroups = kThreads / LANES;
     extern __shared__ uint4 smem[];
     __shared__ float2 part[2][32];
     previous_done();
     next_may_start();
-    const uint32_t lane = threadIdx.x % LANES;
+    const uint32_t lane = threadIdx.x % LANES, at = lane * K<T>;
     const uint64_t step = (uint64_t)gridDim.x * kGroups;
-    const Ring<T, EIGHTS> ring{a.res ? 2u : 1u, smem};
+    using Rows = Ring<T, VECS, kThreads, 2, LANES == 128 ? 2 : 1>;
+    Rows ring(smem, a.res ? 2 : 1);
+    constexpr uint32_t kAhead = Rows::stages;
+    constexpr bool kHeld = VEC && held_weights(LANES);
+    const Held<T, VECS, kThreads> held(ring.end, w16);
     const float per = 1.f / (float)a.cols;
-    auto fetch = [&](uint64_t t, uint32_t stage) {
-        if (t < a.rows)
+    // this thread's first column of the next row to fetch, and of the row taken
+    uint64_t t = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES, next_t = t;
+    const T *x = (const T *)a.x + t * a.ldx + at, *res = (const T *)a.res + t * a.ld_res + at;
+    T *out = (T *)a.out + t * a.ld_out + at, *total = (T *)a.sum + t * a.ld_sum + at;
+    const uint64_t step_x = step * a.ldx, step_res = step * a.ld_res, step_out = step * a.ld_out, step_sum = step * a.ld_sum;
+    const uint64_t step_z = step * a.mask.groups * dropout::kGolden;
+    uint64_t z = a.mask.base + (t * a.mask.groups + lane * (K<T> / 4)) * dropout::kGolden;  // its first draw
+    auto fetch = [&](uint4 *place) {
+        if (next_t < a.rows)
 #pragma unroll
-            for (uint32_t e = 0; e < EIGHTS; ++e) {
-                const uint32_t col = (e * LANES + lane) * 8;
-                if (col >= a.cols) continue;
-                ring.copy(stage, 0, e, (const T *)a.x + t * a.ldx + col);
-                if (a.res) ring.copy(stage, 1, e, (const T *)a.res + t * a.ld_res + col);
-            }
+            for (uint32_t e = 0; e < VECS; ++e)
+                if (e * LANES * K<T> + at < a.cols) {
+                    ring.copy(place, 0, e, x + e * LANES * K<T>);
+                    if (a.res) ring.copy(place, 1, e, res + e * LANES * K<T>);
+                }
         async::cp_async_commit();
+        next_t += step, x += step_x, res += step_res;
     };
-    uint64_t t = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES;
-    if (VEC)
-        for (uint32_t i = 0; i < kAhead; ++i) fetch(t + i * step, i);
-    for (uint32_t stage = 0; t < a.rows; t += step, stage = stage + 1 == kAhead ? 0 : stage + 1) {
-        float s[EIGHTS][8];
-        float2 sum = make_float2(0.f, 0.f);
+    if (VEC) {
+#pragma unroll
+        for (uint32_t e = 0; e < VECS; ++e)
+            if (kHeld && e * LANES * K<T> + at < a.cols) {
+                if (a.weight) held.copy(0, e, a.weight, e * LANES * K<T> + at);
+                if (a.bias) held.copy(1, e, a.bias, e * LANES * K<T> + at);
+            }
+        for (uint32_t i = 0; i < kAhead; ++i) fetch(ring.begin + i * ring.stage);  // (the weights with the first row)
+    }
+    for (; t < a.rows; t += step, out += step_out, total += step_sum, z += step_z) {
+        float2 s[VECS][K<T> / 2], sum = both(0.f);
         if (VEC) async::cp_async_wait<kAhead - 1>();
 #pragma unroll
-        for (uint32_t e = 0; e < EIGHTS; ++e) {
-            const uint32_t col = (e * LANES + lane) * 8;
+        for (uint32_t e = 0; e < VECS; ++e) {
+            const uint32_t col = e * LANES * K<T> + at;
             if (col < a.cols) {
-                float r[8];
-                if (VEC) ring.read(stage, 0, e, s[e]);
-                else load8<T, false>((const T *)a.x + t * a.ldx, col, a.cols, s[e]);
-                if (a.mask.level) {
-                    const uint32_t keep = kept(a.mask, t, col);
-#pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) s[e][i] = dropped(a.mask, s[e][i], keep >> i & 1);
-                }
+                if (VEC) ring.read(0, e, s[e]);
+                else load<T, false>(x + e * LANES * K<T>, a.cols - col, s[e]);
+                if (a.mask.level) drop(a.mask, z + (uint64_t)(e * LANES * (K<T> / 4)) * dropout::kGolden, s[e]);
                 if (a.res) {
-                    if (VEC) ring.read(stage, 1, e, r);
-                    else load8<T, false>((const T *)a.res + t * a.ld_res, col, a.cols, r);
+                    float2 r[K<T> / 2];
+                    if (VEC) ring.read(1, e, r);
+                    else load<T, false>(res + e * LANES * K<T>, a.cols - col, r);
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) s[e][i] = __fadd_rn(s[e][i], r[i]);
+                    for (uint32_t i = 0; i < K<T> / 2; ++i) s[e][i] = __fadd2_rn(s[e][i], r[i]);
                 }
 #pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) sum.x += s[e][i];  // (columns past the last are 0)
+                for (uint32_t i = 0; i < K<T> / 2; ++i) sum = __fadd2_rn(sum, s[e][i]);  // (columns past the last are 0)
+                if (a.sum) store<T, VEC>(total + e * LANES * K<T>, a.cols - col, s[e]);
             }
         }
-        const float about = row_sum<LANES>(sum, part, 0).x * per;
+        const float about = row_sum<LANES>(sum.x + sum.y, part, 0) * per;
         // (the sum has used all that was read: its places may be filled again)
-        if (VEC) fetch(t + kAhead * step, stage);
-        sum = make_float2(0.f, 0.f);
+        if (VEC) fetch(ring.now), ring.next();
+        else x += step_x, res += step_res;
+        const float2 minus_about = both(-about);
+        float2 s1 = both(0.f), s2 = both(0.f);
 #pragma unroll
-        for (uint32_t e = 0; e < EIGHTS; ++e) {
-            const uint32_t col = (e * LANES + lane) * 8;
+        for (uint32_t e = 0; e < VECS; ++e) {
+            const uint32_t col = e * LANES * K<T> + at;
             if (col < a.cols)
 #pragma unroll
-                for (uint32_t i = 0; i < 8; ++i)
-                    if (VEC || col + i < a.cols) {
-                        const float d = centred(s[e][i], about, 0.f);
-                        sum.x += d, sum.y = __fmaf_rn(d, d, sum.y);
-                    }
+                for (uint32_t i = 0; i < K<T> / 2; ++i) {
+                    s[e][i] = __fadd2_rn(s[e][i], minus_about);
+                    if (!VEC && col + 2 * i >= a.cols) s[e][i].x = 0.f;
+                    if (!VEC && col + 2 * i + 1 >= a.cols) s[e][i].y = 0.f;
+                    s1 = __fadd2_rn(s1, s[e][i]), s2 = __ffma2_rn(s[e][i], s[e][i], s2);
+                }
         }
-        sum = row_sum<LANES>(sum, part, 1);
-        const float left = sum.x * per, rstd = rstd_of(left, sum.y * per, a.eps);
+        const float2 sums = row_sum<LANES>(make_float2(s1.x + s1.y, s2.x + s2.y), part, 1);
+        const float left = sums.x * per, rstd = rstd_of(left, sums.y * per, a.eps), shift = shift_of(left, rstd);
 #pragma unroll
-        for (uint32_t e = 0; e < EIGHTS; ++e) {
-            const uint32_t col = (e * LANES + lane) * 8;
+        for (uint32_t e = 0; e < VECS; ++e) {
+            const uint32_t col = e * LANES * K<T> + at;
             if (col < a.cols) {
-                if (a.sum) store8<T, VEC>((T *)a.sum + t * a.ld_sum, col, a.cols, s[e]);
-                float w[8], b[8];
-                load_weights<T, VEC>(a.weight, w16, col, a.cols, 1.f, w);
-                load_weights<T, VEC>(a.bias, w16, col, a.cols, 0.f, b);
+                float2 w[K<T> / 2], b[K<T> / 2];
+                if (kHeld && a.weight) held.read(0, e, w);
+                else load_weights<T, VEC>(a.weight, w16, col, a.cols - col, 1.f, w);
+                if (kHeld && a.bias) held.read(1, e, b);
+                else load_weights<T, VEC>(a.bias, w16, col, a.cols - col, 0.f, b);
 #pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) s[e][i] = scaled(centred(s[e][i], about, left), rstd, w[i], b[i]);
-                store8<T, VEC>((T *)a.out + t * a.ld_out, col, a.cols, s[e]);
+                for (uint32_t i = 0; i < K<T> / 2; ++i) s[e][i] = scaled(s[e][i], both(rstd), both(shift), w[i], b[i]);
+                store<T, VEC>(out + e * LANES * K<T>, a.cols - col, s[e]);
             }
         }
         if (lane == 0) {
@@ -238,99 +314,109 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) k_norm_rows(const N
     }
 }
 
-// `part`: [gridDim.x][2][cols], null: dweight and dbias are not wanted
-template <typename T, uint32_t LANES, uint32_t EIGHTS, bool VEC>
-__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) k_norm_rows_grad(const NormGradArgs a, const bool w16, float *sums)
+// `sums`: [gridDim.x][2][cols], null: dweight and dbias are not wanted.  (Rows in twos, for
+// one barrier and two chains at once: no quicker, 133 us for 132 on 16384 x 4096 bf16 with
+// dropout, and slower below 2048 columns for want of registers.)
+template <typename T, uint32_t LANES, uint32_t VECS, bool VEC>
+__global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES * VECS * K<T>)) k_norm_rows_grad(const NormGradArgs a, const bool w16, float *sums)
 {
-    constexpr uint32_t kThreads = LANES < 256 ? 256 : LANES, kGroups = kThreads / LANES;
-    constexpr uint32_t kAhead = ahead(Ring<T, EIGHTS>::bytes(kThreads), 3);
+    constexpr uint32_t kThreads = backward_threads(LANES), kGroups = kThreads / LANES;
     extern __shared__ uint4 smem[];
     __shared__ float2 part[2][32];
     previous_done();
     next_may_start();
-    const uint32_t lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const uint32_t lane = threadIdx.x % LANES, group = threadIdx.x / LANES, at = lane * K<T>;
     const uint64_t step = (uint64_t)gridDim.x * kGroups;
-    const Ring<T, EIGHTS> ring{a.dsum ? 3u : 2u, smem};
+    using Rows = Ring<T, VECS, kThreads, 3, kGradAhead>;
+    Rows ring(smem, a.dsum ? 3 : 2);
+    constexpr uint32_t kAhead = Rows::stages;
     const float per = 1.f / (float)a.cols;
-    float w[EIGHTS][8], dw[EIGHTS][8] = {}, db[EIGHTS][8] = {};
+    float2 w[VECS][K<T> / 2], dw[VECS][K<T> / 2] = {}, db[VECS][K<T> / 2] = {};
 #pragma unroll
-    for (uint32_t e = 0; e < EIGHTS; ++e) {
-        const uint32_t col = (e * LANES + lane) * 8;
-        if (col < a.cols) load_weights<T, VEC>(a.weight, w16, col, a.cols, 1.f, w[e]);
+    for (uint32_t e = 0; e < VECS; ++e) {
+        const uint32_t col = e * LANES * K<T> + at;
+        if (col < a.cols) load_weights<T, VEC>(a.weight, w16, col, a.cols - col, 1.f, w[e]);
     }
-    auto fetch = [&](uint64_t t, uint32_t stage) {
-        if (t < a.rows)
+    // This thread's first column of the next row to fetch, and of the row taken, moved on
+    // from row to row.  (Made anew from the row's number: 144 us for 132 on 16384 x 4096 bf16.)
+    uint64_t t = (uint64_t)blockIdx.x * kGroups + group, next_t = t;
+    const T *dy = (const T *)a.dy + t * a.ld_dy + at, *x = (const T *)a.sum + t * a.ld_sum + at, *dsum = (const T *)a.dsum + t * a.ld_dsum + at;
+    T *dx = (T *)a.dx + t * a.ld_dx + at, *dres = (T *)a.dres + t * a.ld_dres + at;
+    const uint64_t step_dy = step * a.ld_dy, step_x = step * a.ld_sum, step_ds = step * a.ld_dsum, step_dx = step * a.ld_dx, step_dr = step * a.ld_dres;
+    const uint64_t step_z = step * a.mask.groups * dropout::kGolden;
+    uint64_t z = a.mask.base + (t * a.mask.groups + lane * (K<T> / 4)) * dropout::kGolden;  // its first draw
+    auto fetch = [&](uint4 *place) {
+        if (next_t < a.rows)
 #pragma unroll
-            for (uint32_t e = 0; e < EIGHTS; ++e) {
-                const uint32_t col = (e * LANES + lane) * 8;
-                if (col >= a.cols) continue;
-                ring.copy(stage, 0, e, (const T *)a.dy + t * a.ld_dy + col);
-                ring.copy(stage, 1, e, (const T *)a.sum + t * a.ld_sum + col);
-                if (a.dsum) ring.copy(stage, 2, e, (const T *)a.dsum + t * a.ld_dsum + col);
-            }
+            for (uint32_t e = 0; e < VECS; ++e)
+                if (e * LANES * K<T> + at < a.cols) {
+                    ring.copy(place, 0, e, dy + e * LANES * K<T>);
+                    ring.copy(place, 1, e, x + e * LANES * K<T>);
+                    if (a.dsum) ring.copy(place, 2, e, dsum + e * LANES * K<T>);
+                }
         async::cp_async_commit();
+        next_t += step, dy += step_dy, x += step_x, dsum += step_ds;
     };
-    uint64_t t = (uint64_t)blockIdx.x * kGroups + group;
     if (VEC)
-        for (uint32_t i = 0; i < kAhead; ++i) fetch(t + i * step, i);
+        for (uint32_t i = 0; i < kAhead; ++i) fetch(ring.begin + i * ring.stage);
     uint32_t slot = 0;
-    for (uint32_t stage = 0; t < a.rows; t += step, stage = stage + 1 == kAhead ? 0 : stage + 1, slot ^= 1) {
-        float g[EIGHTS][8], xh[EIGHTS][8];
-        float2 avg = make_float2(0.f, 0.f);
+    for (; t < a.rows; t += step, dx += step_dx, dres += step_dr, z += step_z, slot ^= 1) {
+        float2 g[VECS][K<T> / 2], xh[VECS][K<T> / 2], s1 = both(0.f), s2 = both(0.f);
         const float mean = a.mean[t], rstd = a.rstd[t];
         if (VEC) async::cp_async_wait<kAhead - 1>();
 #pragma unroll
-        for (uint32_t e = 0; e < EIGHTS; ++e) {
-            const uint32_t col = (e * LANES + lane) * 8;
+        for (uint32_t e = 0; e < VECS; ++e) {
+            const uint32_t col = e * LANES * K<T> + at;
             if (col < a.cols) {
-                if (VEC) ring.read(stage, 0, e, g[e]), ring.read(stage, 1, e, xh[e]);
-                else load8<T, false>((const T *)a.dy + t * a.ld_dy, col, a.cols, g[e]), load8<T, false>((const T *)a.sum + t * a.ld_sum, col, a.cols, xh[e]);
+                if (VEC) ring.read(0, e, g[e]), ring.read(1, e, xh[e]);
+                else load<T, false>(dy + e * LANES * K<T>, a.cols - col, g[e]), load<T, false>(x + e * LANES * K<T>, a.cols - col, xh[e]);
 #pragma unroll
-                for (uint32_t i = 0; i < 8; ++i)
-                    if (VEC || col + i < a.cols) {
-                        xh[e][i] = xhat(xh[e][i], mean, rstd);
-                        dw[e][i] = __fmaf_rn(g[e][i], xh[e][i], dw[e][i]), db[e][i] += g[e][i];
-                        g[e][i] = __fmul_rn(g[e][i], w[e][i]);
-                        avg.x += g[e][i], avg.y = __fmaf_rn(g[e][i], xh[e][i], avg.y);
-                    }
+                for (uint32_t i = 0; i < K<T> / 2; ++i) {  // (columns past the last: g is 0)
+                    xh[e][i] = xhat(xh[e][i], both(-mean), both(rstd));
+                    dw[e][i] = __ffma2_rn(g[e][i], xh[e][i], dw[e][i]), db[e][i] = __fadd2_rn(db[e][i], g[e][i]);
+                    g[e][i] = __fmul2_rn(g[e][i], w[e][i]);
+                    s1 = __fadd2_rn(s1, g[e][i]), s2 = __ffma2_rn(g[e][i], xh[e][i], s2);
+                }
             }
         }
-        avg = row_sum<LANES>(avg, part, slot);
-        avg.x *= per, avg.y *= per;
+        const float2 avg = row_sum<LANES>(make_float2(s1.x + s1.y, s2.x + s2.y), part, slot);
+        const float2 minus_g = both(avg.x * -per), minus_gxh = both(avg.y * -per);
 #pragma unroll
-        for (uint32_t e = 0; e < EIGHTS; ++e) {
-            const uint32_t col = (e * LANES + lane) * 8;
+        for (uint32_t e = 0; e < VECS; ++e) {
+            const uint32_t col = e * LANES * K<T> + at;
             if (col < a.cols) {
-                float d[8] = {};
+#pragma unroll
+                for (uint32_t i = 0; i < K<T> / 2; ++i) g[e][i] = centred_gradient(g[e][i], xh[e][i], minus_g, minus_gxh);
                 if (a.dsum) {
-                    if (VEC) ring.read(stage, 2, e, d);
-                    else load8<T, false>((const T *)a.dsum + t * a.ld_dsum, col, a.cols, d);
+                    float2 d[K<T> / 2];
+                    if (VEC) ring.read(2, e, d);
+                    else load<T, false>(dsum + e * LANES * K<T>, a.cols - col, d);
+#pragma unroll
+                    for (uint32_t i = 0; i < K<T> / 2; ++i) g[e][i] = __ffma2_rn(both(rstd), g[e][i], d[i]);
+                } else {
+#pragma unroll
+                    for (uint32_t i = 0; i < K<T> / 2; ++i) g[e][i] = __fmul2_rn(both(rstd), g[e][i]);
                 }
-#pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) g[e][i] = gradient(g[e][i], xh[e][i], avg, rstd, d[i]);
-                if (a.dres) store8<T, VEC>((T *)a.dres + t * a.ld_dres, col, a.cols, g[e]);
+                if (a.dres) store<T, VEC>(dres + e * LANES * K<T>, a.cols - col, g[e]);
                 if (a.dx) {
-                    if (a.mask.level) {
-                        const uint32_t keep = kept(a.mask, t, col);
-#pragma unroll
-                        for (uint32_t i = 0; i < 8; ++i) g[e][i] = dropped(a.mask, g[e][i], keep >> i & 1);
-                    }
-                    store8<T, VEC>((T *)a.dx + t * a.ld_dx, col, a.cols, g[e]);
+                    if (a.mask.level) drop(a.mask, z + (uint64_t)(e * LANES * (K<T> / 4)) * dropout::kGolden, g[e]);
+                    store<T, VEC>(dx + e * LANES * K<T>, a.cols - col, g[e]);
                 }
             }
         }
         // (all that was read has been used: its places may be filled again)
-        if (VEC) fetch(t + kAhead * step, stage);
+        if (VEC) fetch(ring.now), ring.next();
+        else dy += step_dy, x += step_x, dsum += step_ds;
     }
     if (!sums) return;
     float *out = sums + (uint64_t)blockIdx.x * 2 * a.cols;
     if (kGroups == 1) {
 #pragma unroll
-        for (uint32_t e = 0; e < EIGHTS; ++e) {
-            const uint32_t col = (e * LANES + lane) * 8;
+        for (uint32_t e = 0; e < VECS; ++e) {
+            const uint32_t col = (e * LANES + lane) * K<T>;
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i)
-                if (col + i < a.cols) out[col + i] = dw[e][i], out[a.cols + col + i] = db[e][i];
+            for (uint32_t i = 0; i < K<T>; ++i)
+                if (col + i < a.cols) out[col + i] = of(dw[e], i), out[a.cols + col + i] = of(db[e], i);
         }
     } else {
         // the groups' sums, added up in order
@@ -338,11 +424,11 @@ __global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) k_norm_rows_grad(co
         if (VEC) async::cp_async_wait<0>();
         __syncthreads();
 #pragma unroll
-        for (uint32_t e = 0; e < EIGHTS; ++e) {
-            const uint32_t col = (e * LANES + lane) * 8;
+        for (uint32_t e = 0; e < VECS; ++e) {
+            const uint32_t col = (e * LANES + lane) * K<T>;
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i)
-                if (col + i < a.cols) s[group * 2 * a.cols + col + i] = dw[e][i], s[(group * 2 + 1) * a.cols + col + i] = db[e][i];
+            for (uint32_t i = 0; i < K<T>; ++i)
+                if (col + i < a.cols) s[group * 2 * a.cols + col + i] = of(dw[e], i), s[(group * 2 + 1) * a.cols + col + i] = of(db[e], i);
         }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < 2 * a.cols; i += kThreads) {
@@ -368,31 +454,31 @@ struct Allowed {
     }
 };
 
-inline bool vectors(uint32_t cols, std::initializer_list<const void *> starts, std::initializer_list<uint64_t> bytes)
+inline bool vectors(uint32_t cols, uint32_t k, std::initializer_list<const void *> starts, std::initializer_list<uint64_t> bytes)
 {
     uint64_t all = 0;
     for (const void *p : starts) all |= (uint64_t)(uintptr_t)p;
     for (uint64_t b : bytes) all |= b;
-    return cols % 8 == 0 && all % 16 == 0;
+    return cols % k == 0 && all % 16 == 0;
 }
 
-template <typename T, uint32_t LANES, uint32_t EIGHTS>
+template <typename T, uint32_t LANES, uint32_t VECS>
 int forward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormArgs &a, bool w16)
 {
-    constexpr uint32_t kThreads = LANES < 256 ? 256 : LANES, kGroups = kThreads / LANES;
+    constexpr uint32_t kThreads = forward_threads(LANES), kGroups = kThreads / LANES;
+    using Rows = Ring<T, VECS, kThreads, 2, LANES == 128 ? 2 : 1>;
     const uint64_t z = sizeof(T);
     const bool one = a.rows == 1;  // (one row has no stride)
-    const bool vec = vectors(a.cols, {a.x, a.res, a.out, a.sum, a.weight, a.bias},
+    const bool vec = vectors(a.cols, K<T>, {a.x, a.res, a.out, a.sum, a.weight, a.bias},
                              {one ? 0 : a.ldx * z, one || !a.res ? 0 : a.ld_res * z, one ? 0 : a.ld_out * z, one || !a.sum ? 0 : a.ld_sum * z});
-    constexpr uint32_t kRow = Ring<T, EIGHTS>::bytes(kThreads);
-    const uint32_t bytes = vec ? (a.res ? 2 : 1) * kRow * ahead(kRow, 2) : 0;
+    const uint32_t bytes = vec ? (a.res ? 2 : 1) * Rows::tensor * 16 * Rows::stages + (held_weights(LANES) && (a.weight || a.bias) ? Held<T, VECS, kThreads>::bytes(w16) : 0) : 0;
     const uint64_t units = (a.rows + kGroups - 1) / kGroups;
     // as many blocks as run at once: 1024 threads an SM, if their rows have room
-    const uint32_t blocks = std::max(1u, std::min(1024 / kThreads, bytes ? 200 * 1024 / bytes : 32u));
+    const uint32_t blocks = std::max(1u, std::min(1024 / kThreads, bytes ? 220 * 1024 / (bytes + 1536) : 32u));
     const uint64_t fill = (uint64_t)ctx->sm_count * blocks;
     NormArgs b = a;
     void *args[] = {&b, &w16};
-    const void *k = vec ? (const void *)k_norm_rows<T, LANES, EIGHTS, true> : (const void *)k_norm_rows<T, LANES, EIGHTS, false>;
+    const void *k = vec ? (const void *)k_norm_rows<T, LANES, VECS, true> : (const void *)k_norm_rows<T, LANES, VECS, false>;
     static Allowed allowed;
     if (const int rc = allowed.set(k, ctx->device, bytes, "layer norm")) return rc;
     return launch(k, dim3((uint32_t)std::min(units, fill)), kThreads, bytes, s, args, "layer norm");
@@ -402,33 +488,34 @@ template <typename T>
 int forward_rows(const fiona_ctx *ctx, void *stream, const NormArgs &a, bool w16)
 {
     cudaStream_t s = (cudaStream_t)stream;
-    const RowShape r = forward_shape(a.cols);
-    switch (r.lanes * 8 + r.eights) {
-        case 32 * 8 + 1: return forward_rows<T, 32, 1>(ctx, s, a, w16);
-        case 32 * 8 + 2: return forward_rows<T, 32, 2>(ctx, s, a, w16);
-        case 32 * 8 + 4: return forward_rows<T, 32, 4>(ctx, s, a, w16);
-        case 128 * 8 + 2: return forward_rows<T, 128, 2>(ctx, s, a, w16);
-        case 256 * 8 + 2: return forward_rows<T, 256, 2>(ctx, s, a, w16);
-        case 512 * 8 + 2: return forward_rows<T, 512, 2>(ctx, s, a, w16);
-        default: return forward_rows<T, 1024, 2>(ctx, s, a, w16);
+    constexpr uint32_t one = 8 / K<T>, two = 2 * one, four = 4 * one;  // eights of columns in vectors
+    switch (forward_lanes(a.cols, sizeof(T))) {
+        case 32:
+            return a.cols <= 256   ? forward_rows<T, 32, one>(ctx, s, a, w16)
+                   : a.cols <= 512 ? forward_rows<T, 32, two>(ctx, s, a, w16) : forward_rows<T, 32, four>(ctx, s, a, w16);
+        case 64: return forward_rows<T, 64, two>(ctx, s, a, w16);
+        case 128: return forward_rows<T, 128, two>(ctx, s, a, w16);
+        case 256: return forward_rows<T, 256, two>(ctx, s, a, w16);
+        case 512: return forward_rows<T, 512, two>(ctx, s, a, w16);
+        default: return forward_rows<T, 1024, two>(ctx, s, a, w16);
     }
 }
 
-template <typename T, uint32_t LANES, uint32_t EIGHTS>
+template <typename T, uint32_t LANES, uint32_t VECS>
 int backward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormGradArgs &a, bool w16, uint32_t blocks, float *part)
 {
-    constexpr uint32_t kThreads = LANES < 256 ? 256 : LANES, kGroups = kThreads / LANES;
+    constexpr uint32_t kThreads = backward_threads(LANES), kGroups = kThreads / LANES;
+    using Rows = Ring<T, VECS, kThreads, 3, kGradAhead>;
     const uint64_t z = sizeof(T);
     const bool one = a.rows == 1;
-    const bool vec = vectors(a.cols, {a.dy, a.sum, a.dsum, a.dx, a.dres, a.weight},
+    const bool vec = vectors(a.cols, K<T>, {a.dy, a.sum, a.dsum, a.dx, a.dres, a.weight},
                              {one ? 0 : a.ld_dy * z, one ? 0 : a.ld_sum * z, one || !a.dsum ? 0 : a.ld_dsum * z, one || !a.dx ? 0 : a.ld_dx * z,
                               one || !a.dres ? 0 : a.ld_dres * z});
-    constexpr uint32_t kRow = Ring<T, EIGHTS>::bytes(kThreads);
-    uint32_t bytes = vec ? (a.dsum ? 3 : 2) * kRow * ahead(kRow, 3) : 0;
+    uint32_t bytes = vec ? (a.dsum ? 3 : 2) * Rows::tensor * 16 * Rows::stages : 0;
     if (part && kGroups > 1) bytes = std::max(bytes, kGroups * 2 * a.cols * 4);
     NormGradArgs b = a;
     void *args[] = {&b, &w16, &part};
-    const void *k = vec ? (const void *)k_norm_rows_grad<T, LANES, EIGHTS, true> : (const void *)k_norm_rows_grad<T, LANES, EIGHTS, false>;
+    const void *k = vec ? (const void *)k_norm_rows_grad<T, LANES, VECS, true> : (const void *)k_norm_rows_grad<T, LANES, VECS, false>;
     static Allowed allowed;
     if (const int rc = allowed.set(k, ctx->device, bytes, "layer norm gradient")) return rc;
     return launch(k, dim3(blocks), kThreads, bytes, s, args, "layer norm gradient");
@@ -438,14 +525,13 @@ template <typename T>
 int backward_rows(const fiona_ctx *ctx, void *stream, const NormGradArgs &a, bool w16, uint32_t blocks, float *part)
 {
     cudaStream_t s = (cudaStream_t)stream;
-    const RowShape r = backward_shape(a.cols);
-    switch (r.lanes * 8 + r.eights) {
-        case 32 * 8 + 1: return backward_rows<T, 32, 1>(ctx, s, a, w16, blocks, part);
-        case 32 * 8 + 2: return backward_rows<T, 32, 2>(ctx, s, a, w16, blocks, part);
-        case 64 * 8 + 2: return backward_rows<T, 64, 2>(ctx, s, a, w16, blocks, part);
-        case 128 * 8 + 2: return backward_rows<T, 128, 2>(ctx, s, a, w16, blocks, part);
-        case 256 * 8 + 2: return backward_rows<T, 256, 2>(ctx, s, a, w16, blocks, part);
-        default: return backward_rows<T, 512, 2>(ctx, s, a, w16, blocks, part);
+    constexpr uint32_t one = 8 / K<T>, two = 2 * one;  // eights of columns in vectors
+    switch (backward_lanes(a.cols)) {
+        case 32: return a.cols <= 256 ? backward_rows<T, 32, one>(ctx, s, a, w16, blocks, part) : backward_rows<T, 32, two>(ctx, s, a, w16, blocks, part);
+        case 64: return backward_rows<T, 64, two>(ctx, s, a, w16, blocks, part);
+        case 128: return backward_rows<T, 128, two>(ctx, s, a, w16, blocks, part);
+        case 256: return backward_rows<T, 256, two>(ctx, s, a, w16, blocks, part);
+        default: return backward_rows<T, 512, two>(ctx, s, a, w16, blocks, part);
     }
 }
 

@@ -2,24 +2,27 @@
 #pragma once
 #include "norm.h"
 
-// A row's threads and the eights of columns that each takes.
-struct RowShape {
-    uint32_t lanes, eights;
-    uint32_t groups() const { return lanes < 256 ? 256 / lanes : 1; }  // rows of a block
-};
-
 constexpr uint32_t kMostForward = 16384, kMostBackward = 8192;  // columns
 
-inline RowShape forward_shape(uint32_t cols)
+// A row's threads, by its width and type alone: a row comes out the same however many
+// others there are.  Each takes up to 16 columns; forward 32 where a row of 513 to 1024
+// 16-bit columns is a warp's.  (32 columns spread wider what a row costs each thread beside
+// them, but half the threads are too few to hide its chain of sums: 16384 x 4096 bf16 96 us,
+// with 16 columns 89.  87381 rows of 768: 32 threads a row 92 us, 64 115; in fp32 192 and
+// 161; one row of them 3.1 us and 2.5.)
+inline uint32_t forward_lanes(uint32_t cols, uint32_t size)
 {
-    return cols <= 256 ? RowShape{32, 1} : cols <= 512 ? RowShape{32, 2} : cols <= 1024 ? RowShape{32, 4} : cols <= 2048 ? RowShape{128, 2}
-           : cols <= 4096 ? RowShape{256, 2} : cols <= 8192 ? RowShape{512, 2} : RowShape{1024, 2};
+    return cols <= 512 ? 32 : cols <= 1024 ? (size == 4 ? 64 : 32) : cols <= 2048 ? 128 : cols <= 4096 ? 256 : cols <= 8192 ? 512 : 1024;
 }
-inline RowShape backward_shape(uint32_t cols)
+inline uint32_t backward_lanes(uint32_t cols)
 {
-    return cols <= 256 ? RowShape{32, 1} : cols <= 512 ? RowShape{32, 2} : cols <= 1024 ? RowShape{64, 2} : cols <= 2048 ? RowShape{128, 2}
-           : cols <= 4096 ? RowShape{256, 2} : RowShape{512, 2};
+    return cols <= 512 ? 32 : cols <= 1024 ? 64 : cols <= 2048 ? 128 : cols <= 4096 ? 256 : 512;
 }
+// blocks of a backward pass on an SM at a time, for rows of up to `cols`: what their sums
+// leave of the registers
+constexpr uint32_t backward_blocks(uint32_t cols) { return cols <= 256 ? 3 : cols <= 4096 ? 2 : 1; }
+constexpr uint32_t forward_threads(uint32_t lanes) { return lanes < 128 ? 128 : lanes; }   // of a block
+constexpr uint32_t backward_threads(uint32_t lanes) { return lanes < 256 ? 256 : lanes; }
 
 // norm_rows_*.cu, one element type each.  w16: weights of the rows' type, not fp32
 int launch_norm_rows_f32(const fiona_ctx *ctx, void *stream, const NormArgs &a, bool w16);
