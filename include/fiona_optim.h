@@ -15,8 +15,8 @@
  *   v = beta2 v + (1 - beta2) (k g)^2
  *   w = w - lr weight_decay w - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
  *
- * A group that sits out keeps its weights, moments and step count as they are, and
- * its gradients are not read.
+ * A group that sits out keeps its weights, moments and step count as they are,
+ * whatever its gradients hold.
  *
  * State, in buffers of the caller's (fiona_adamw_state).  Tensor i has its elements
  * from place at[i] on: at[0] = 0, at[i+1] = at[i] + count[i] rounded up to a multiple
@@ -35,9 +35,9 @@
  * master (optional): fp32 [places], the weights that 16-bit tensors are rounded from;
  * then their own tensors are written, but not read.  fp32 tensors do not use theirs.
  *
- * Arithmetic: fp32, from gradients in the weights' type; 1 - beta^t in fp64.  A weight
+ * Arithmetic: fp32, from gradients in the weights' type; beta^t from t log beta in fp64.  A weight
  * is rounded once (to nearest).  A norm is summed in fp32 by pieces of 1024 elements and
- * in fp64 from there; a piece whose sum of squares passes fp32's range (a norm above
+ * in fp64 from there; a sum of squares that passes fp32's range (a norm above
  * 1.8e19) counts as infinite.  Results do not depend on the order in which blocks run:
  * no atomics on values.
  *

@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "fiona_internal.h"
 
 namespace launches {
@@ -34,5 +36,18 @@ inline int launch(K kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream
     if (e != cudaSuccess) return set_error(FIONA_ERR_CUDA, "%s launch: %s", what, cudaGetErrorString(e));
     return FIONA_OK;
 }
+
+// Lets one kernel's launches on a device have their dynamic shared memory, asked for once.
+// (Up to 40 KB, 48 with what kernels have besides, every launch may have.)
+struct Allowed {
+    std::atomic<uint64_t> devices{0};
+    int set(const void *kernel, int device, uint64_t bytes, const char *what)
+    {
+        if (bytes <= 40 * 1024 || (devices.load(std::memory_order_relaxed) >> device & 1)) return FIONA_OK;
+        const int rc = allow_shared_memory(kernel, bytes, what);
+        if (rc == FIONA_OK) devices.fetch_or(1ull << device, std::memory_order_relaxed);
+        return rc;
+    }
+};
 
 }  // namespace launches

@@ -9,6 +9,7 @@
 
 namespace layernorm {
 
+using launches::Allowed;
 using launches::launch;
 using launches::next_may_start;
 using launches::previous_done;

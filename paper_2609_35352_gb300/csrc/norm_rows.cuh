@@ -11,7 +11,6 @@
 // k_grad_sum adds up the blocks' in order.
 #pragma once
 #include <algorithm>
-#include <atomic>
 #include <initializer_list>
 
 #include "async.cuh"
@@ -439,20 +438,6 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
         }
     }
 }
-
-// Lets a kernel's launches on a device have their shared memory, asked for once (of
-// the kernels that take vectors: the others stay
-// below what every launch may have, 48 KB with the row sums').
-struct Allowed {
-    std::atomic<uint64_t> devices{0};
-    int set(const void *k, int device, uint32_t bytes, const char *what)
-    {
-        if (bytes <= 40 * 1024 || (devices.load(std::memory_order_relaxed) >> device & 1)) return FIONA_OK;
-        const int rc = allow_shared_memory(k, bytes, what);
-        if (rc == FIONA_OK) devices.fetch_or(1ull << device, std::memory_order_relaxed);
-        return rc;
-    }
-};
 
 inline bool vectors(uint32_t cols, uint32_t k, std::initializer_list<const void *> starts, std::initializer_list<uint64_t> bytes)
 {

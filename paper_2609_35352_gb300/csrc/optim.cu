@@ -9,6 +9,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.cuh"
 #include "optim.h"
@@ -16,48 +17,84 @@
 
 namespace {
 
+using launches::Allowed;
 using launches::launch;
 using launches::next_may_start;
 using launches::previous_done;
 using real::narrow;
 using real::widen;
 
-constexpr uint32_t kThreads = 256, kWarps = kThreads / 32;
-constexpr uint32_t kLane = kBlock / 32;  // elements of a block that a lane takes
+constexpr uint32_t kThreads = 256, kWarps = kThreads / 32, kRateThreads = 1024;
+constexpr uint32_t kPairs = kBlock / 64;  // pairs of elements of a block that a lane takes
 constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: largest values below count as zero
 
-// the sum of squares of a piece's gradients
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// Four elements as they lie, and as two pairs.
 template <typename T>
-__device__ __forceinline__ float squares(const AdamPiece &p, uint32_t lane)
+struct Four {
+    using Bits = typename std::conditional<sizeof(T) == 4, uint4, uint2>::type;
+    Bits u;
+    __device__ __forceinline__ void pairs(float2 (&v)[2]) const
+    {
+        const T *x = reinterpret_cast<const T *>(&u);
+        v[0] = make_float2(widen(x[0]), widen(x[1])), v[1] = make_float2(widen(x[2]), widen(x[3]));
+    }
+    __device__ __forceinline__ void set(const float2 a, const float2 b)
+    {
+        T *x = reinterpret_cast<T *>(&u);
+        x[0] = narrow<T>(a.x), x[1] = narrow<T>(a.y), x[2] = narrow<T>(b.x), x[3] = narrow<T>(b.y);
+    }
+};
+
+// the sum of squares of a piece's gradients, added to eight sums
+template <typename T>
+__device__ __forceinline__ void squares(const AdamPiece &p, uint32_t lane, float2 (&s)[4])
 {
     const T *g = (const T *)p.grad;
-    float s = 0.f;
-    for (uint32_t i = lane; i < p.count; i += 32) {
-        const float v = widen(g[i]);
-        s = __fmaf_rn(v, v, s);
+    if (p.aligned && p.count % kBlock == 0) {
+        constexpr uint32_t k = 16 / sizeof(T);
+#pragma unroll 4
+        for (uint32_t i = lane; i < p.count / k; i += 32) {
+            const uint4 u = reinterpret_cast<const uint4 *>(g)[i];
+            const T *x = reinterpret_cast<const T *>(&u);
+#pragma unroll
+            for (uint32_t j = 0; j < k; j += 2) {
+                const float2 v = make_float2(widen(x[j]), widen(x[j + 1]));
+                s[j / 2 % 4] = __ffma2_rn(v, v, s[j / 2 % 4]);
+            }
+        }
+    } else {
+#pragma unroll 8
+        for (uint32_t i = lane; i < p.count; i += 32) {
+            const float v = widen(g[i]);
+            s[0].x = __fmaf_rn(v, v, s[0].x);
+        }
     }
-    return s;
 }
 
-__global__ void __launch_bounds__(kThreads) k_squares(const AdamPiece *pieces, uint32_t n, const uint8_t *active, float *out)
+__global__ void __launch_bounds__(kThreads) k_squares(const AdamPiece *pieces, const AdamRun *runs, uint32_t n, const uint8_t *active, float *out)
 {
     previous_done();
     next_may_start();
     const uint32_t at = blockIdx.x * kWarps + threadIdx.x / 32, lane = threadIdx.x & 31;
     if (at >= n) return;
-    const AdamPiece p = pieces[at];
-    float s = 0.f;
-    if (!active || active[p.group]) {
+    const AdamRun r = runs[at];
+    float2 s[4] = {};
+    for (uint32_t i = r.begin; i < r.end; ++i) {
+        const AdamPiece p = pieces[i];
+        if (active && !active[p.group]) break;  // (all of a run are of one group)
         if (p.dtype == FIONA_F32)
-            s = squares<float>(p, lane);
+            squares<float>(p, lane, s);
         else if (p.dtype == FIONA_F16)
-            s = squares<__half>(p, lane);
+            squares<__half>(p, lane, s);
         else
-            s = squares<__nv_bfloat16>(p, lane);
+            squares<__nv_bfloat16>(p, lane, s);
     }
+    float v = ((s[0].x + s[0].y) + (s[1].x + s[1].y)) + ((s[2].x + s[2].y) + (s[3].x + s[3].y));
 #pragma unroll
-    for (uint32_t i = 16; i; i >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, i);
-    if (lane == 0) out[at] = s;
+    for (uint32_t i = 16; i; i >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, i);
+    if (lane == 0) out[at] = v;
 }
 
 struct RateArgs {
@@ -78,18 +115,19 @@ __device__ __forceinline__ void set_rate(const RateArgs &a, uint32_t i, double s
     r.clip = 1.f;
     r.live = !a.active || a.active[i];
     if (a.squares) {
-        const double norm = sqrt(square);
-        a.norms[i] = (float)norm;
-        if (norm > g.max_norm) r.clip = (float)(g.max_norm / norm);
-        if (a.skip && !(norm <= 1.7e308)) r.live = 0;
+        const float norm = sqrtf((float)square);
+        a.norms[i] = norm;
+        if (norm > g.max_norm) r.clip = g.max_norm / norm;
+        if (a.skip && !(norm <= 3.402823466e38f)) r.live = 0;
     }
     if (r.live) {
         const int64_t t = a.steps[i] + 1;
         a.steps[i] = t;
-        // 1 - beta^t = -expm1(t log beta); beta = 0: log beta is -infinity
+        // 1 - beta^t = -expm1(t log beta), its argument in fp64; beta = 0: log beta is -infinity.
+        // (All of it in fp64 took 4 us, on a device that does little of it.)
         const float lr = a.lr[i];
-        r.rate = (float)((double)lr / -expm1((double)t * g.log_beta1));
-        r.root = (float)(1.0 / sqrt(-expm1((double)t * g.log_beta2)));
+        r.rate = lr / -expm1f((float)((double)t * g.log_beta1));
+        r.root = rsqrtf(-expm1f((float)((double)t * g.log_beta2)));
         r.decay = lr * g.weight_decay;
     }
     a.rates[i] = r;
@@ -104,33 +142,65 @@ __global__ void __launch_bounds__(kThreads) k_rates(const RateArgs a)
     if (i < a.n) set_rate(a, i, 0.0);
 }
 
-// with norms: a block a group, its pieces' sums added up in fp64
-__global__ void __launch_bounds__(kThreads) k_norm_rates(const RateArgs a)
+// With norms: a block a group, its runs' sums added up, eight at a time in fp32, in
+// fp64 from there (this device adds two numbers a cycle in fp64 on an SM).
+__global__ void __launch_bounds__(kRateThreads) k_norm_rates(const RateArgs a)
 {
-    __shared__ double part[kThreads];
+    __shared__ double part[kRateThreads];
     next_may_start();
     previous_done();
     const AdamGroup &g = a.groups[blockIdx.x];
     double s = 0.0;
-    for (uint32_t i = g.begin + threadIdx.x; i < g.end; i += kThreads) s += (double)a.squares[i];
-    part[threadIdx.x] = s;
+    for (uint32_t i = g.begin + threadIdx.x * 8; i < g.end; i += kRateThreads * 8) {
+        float v[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) v[k] = i + k < g.end ? a.squares[i + k] : 0.f;
+        s += (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+    }
+    // (only so many threads as have something)
+    uint32_t n = 32;
+    while (n < kRateThreads && n * 8 < g.end - g.begin) n *= 2;
+    if (threadIdx.x < n) part[threadIdx.x] = s;
     __syncthreads();
-    for (uint32_t n = kThreads / 2; n; n /= 2) {
+    for (n /= 2; n; n /= 2) {
         if (threadIdx.x < n) part[threadIdx.x] += part[threadIdx.x + n];
         __syncthreads();
     }
     if (threadIdx.x == 0) set_rate(a, blockIdx.x, part[0]);
 }
 
-// The formulas element by element, each operation said outright, so that every path
+// The formulas by pairs of elements, each operation said outright, so that every path
 // rounds in the same places.
-__device__ __forceinline__ float next_m(const AdamGroup &g, float m, float d) { return __fmaf_rn(g.beta1, m, __fmul_rn(g.rest1, d)); }
-__device__ __forceinline__ float next_v(const AdamGroup &g, float v, float d) { return __fmaf_rn(g.beta2, v, __fmul_rn(g.rest2, __fmul_rn(d, d))); }
-// (decay and step are added up before they are taken from w: w is rounded once)
-__device__ __forceinline__ float next_w(const AdamGroup &g, const AdamRate &r, float w, float m, float u)
+struct Settings {
+    float2 clip, beta1, rest1, beta2, rest2, root, eps, rate, decay;
+    __device__ __forceinline__ Settings(const AdamGroup &g, const AdamRate &r)
+        : clip(both(r.clip)), beta1(both(g.beta1)), rest1(both(g.rest1)), beta2(both(g.beta2)), rest2(both(g.rest2)), root(both(r.root)),
+          eps(both(g.eps)), rate(both(r.rate)), decay(both(r.decay))
+    {
+    }
+};
+
+// w less decay and step, which are added up first: w is rounded once
+__device__ __forceinline__ float2 minus(float2 w, float2 decay, float2 step) { return __ffma2_rn(__ffma2_rn(decay, w, step), both(-1.f), w); }
+
+__device__ __forceinline__ float root_approx(float v)  // below 2^-126: 0
 {
-    const float step = __fdiv_rn(__fmul_rn(r.rate, m), __fmaf_rn(u, r.root, g.eps));
-    return __fsub_rn(w, __fmaf_rn(r.decay, w, step));
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float reciprocal_approx(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// the larger of absolute values; NaN where one is
+__device__ __forceinline__ float largest(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
 struct StepArgs {
@@ -142,129 +212,345 @@ struct StepArgs {
     uint32_t n;
 };
 
-// values in 8 bits: the nearest of q^2 / TOP^2, their squares' middle at (q + 1/2)^2 + 1/4
-template <uint32_t TOP>
-__device__ __forceinline__ uint32_t encode(float share)
+// Codes in 8 bits, four to a word.  To fp32 by a byte in the mantissa of 2^23, from fp32
+// by adding 1.5 2^23 (to nearest): conversions run at an eighth of the additions' rate.
+__device__ __forceinline__ float2 bytes_to_float(uint32_t word, uint32_t k, float bias)  // bytes k and k + 1
 {
-    return (uint32_t)__float2int_rn(sqrtf(fmaxf(fmaf(share, (float)(TOP * TOP), -0.25f), 0.f)));
+    const uint32_t x = __byte_perm(word, 0x4B000000u, 0x7540 + k), y = __byte_perm(word, 0x4B000000u, 0x7541 + k);
+    return __fadd2_rn(make_float2(__uint_as_float(x), __uint_as_float(y)), both(-8388608.f - bias));
+}
+__device__ __forceinline__ float2 signed_codes(uint32_t word, uint32_t k) { return bytes_to_float(word ^ 0x80808080u, k, 128.f); }
+__device__ __forceinline__ float2 unsigned_codes(uint32_t word, uint32_t k) { return bytes_to_float(word, k, 0.f); }
+__device__ __forceinline__ uint32_t to_bytes(float2 a, float2 b)
+{
+    a = __fadd2_rn(a, both(12582912.f)), b = __fadd2_rn(b, both(12582912.f));
+    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
 }
 
-// the largest over a warp; not finite: NaN; below kTiny: 0
+// The largest over a warp; not finite: NaN; below kTiny: 0.  (Bits of absolute values are
+// in their order, NaN above all.)
 __device__ __forceinline__ float block_scale(float most)
 {
-    // (bits of values that are not negative are in their order, NaN above all)
     const uint32_t u = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most) & 0x7FFFFFFFu);
     return u >= 0x7F800000u ? __uint_as_float(0x7FFFFFFFu) : u < __float_as_uint(kTiny) ? 0.f : __uint_as_float(u);
 }
-
-// fmaxf, but NaN stays
-__device__ __forceinline__ float larger(float a, float b) { return __uint_as_float(max(__float_as_uint(a) & 0x7FFFFFFFu, __float_as_uint(b) & 0x7FFFFFFFu)); }
-
-__device__ __forceinline__ int32_t encode_m(float m, float scale)
+// what a value is multiplied by for its code's square, TOP^2 at the scale
+template <uint32_t TOP>
+__device__ __forceinline__ float per_scale(float scale)
 {
-    if (!(scale > 0.f)) return 0;
-    const int32_t q = (int32_t)encode<127>(fabsf(m) / scale);
-    return m < 0.f ? -q : q;
+    float r;  // (of the largest scales: below 2^-126)
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(scale));
+    return scale == 0.f ? 0.f : __fmul_rn((float)(TOP * TOP), r);
 }
 
-__device__ __forceinline__ uint32_t encode_v(float u, float scale)
+// The nearest of q^2, as q not rounded yet: two squares' middle is (q + 1/2)^2 + 1/4, so
+// that q is sqrt(x - 1/4) to nearest.  NaN gives 0.
+__device__ __forceinline__ float2 codes_m(float2 m, float per)
 {
-    if (!(scale > 0.f)) return 0;
-    const uint32_t q = encode<255>(u / scale);
-    return u > 0.f ? max(q, 1u) : 0u;
+    return make_float2(copysignf(root_approx(fmaxf(__fmaf_rn(fabsf(m.x), per, -0.25f), 0.f)), m.x),
+                       copysignf(root_approx(fmaxf(__fmaf_rn(fabsf(m.y), per, -0.25f), 0.f)), m.y));
+}
+// (u above zero: code 1 at least)
+__device__ __forceinline__ float2 codes_u(float2 u, float per)
+{
+    const float2 x = __ffma2_rn(u, both(per), both(-0.25f));
+    return make_float2(root_approx(fmaxf(x.x, u.x > 0.f ? 1.f : 0.f)), root_approx(fmaxf(x.y, u.y > 0.f ? 1.f : 0.f)));
 }
 
-__device__ __forceinline__ float decode_m(int8_t c, float scale)
-{
-    const float q = (float)c;
-    return q * fabsf(q) * (scale * (1.f / 16129.f));
-}
+__device__ __forceinline__ float2 value_m(float2 q, float unit) { return __fmul2_rn(make_float2(q.x * fabsf(q.x), q.y * fabsf(q.y)), both(unit)); }
+__device__ __forceinline__ float2 value_u(float2 q, float unit) { return __fmul2_rn(__fmul2_rn(q, q), both(unit)); }
+__device__ __forceinline__ float unit_m(float scale) { return __fmul_rn(scale, 1.f / 16129.f); }
+__device__ __forceinline__ float unit_u(float scale) { return __fmul_rn(scale, 1.f / 65025.f); }
 
-__device__ __forceinline__ float decode_v(uint8_t c, float scale)
-{
-    const float q = (float)c, u = q * q * (scale * (1.f / 65025.f));
-    return u * u;
-}
-
-// root of a second moment; what is below 2^-126 counts as zero in 8 bits
-__device__ __forceinline__ float root8(float v) { return v < 1.17549435e-38f ? 0.f : sqrtf(v); }
-
+// A lane's first four elements of a piece in each buffer.
 template <typename T, bool BITS8, bool MASTER>
-__device__ __forceinline__ void step_block(const StepArgs &a, const AdamPiece &p, const AdamGroup &g, const AdamRate &r, uint32_t first, uint32_t lane)
-{
-    T *w16 = (T *)p.param + first;
-    const T *grad = (const T *)p.grad + first;
-    const uint64_t place = p.place + first;
-    const uint32_t count = min(p.count - first, kBlock);
-    float m[kLane], v[kLane], u[kLane], w[kLane], d[kLane];
-    const float m_scale = BITS8 ? a.m_scale[place / kBlock] : 0.f, v_scale = BITS8 ? a.v_scale[place / kBlock] : 0.f;
-#pragma unroll
-    for (uint32_t k = 0; k < kLane; ++k) {
-        const uint32_t i = lane + 32 * k;
-        m[k] = v[k] = w[k] = d[k] = 0.f;
-        if (i >= count) continue;
-        d[k] = __fmul_rn(widen(grad[i]), r.clip);
-        m[k] = BITS8 ? decode_m(((const int8_t *)a.m)[place + i], m_scale) : ((const float *)a.m)[place + i];
-        v[k] = BITS8 ? decode_v(((const uint8_t *)a.v)[place + i], v_scale) : ((const float *)a.v)[place + i];
-        w[k] = MASTER ? a.master[place + i] : widen(w16[i]);
+struct Places {
+    using Moment = typename std::conditional<BITS8, uint8_t, float>::type;
+    const T *grad;
+    T *param;
+    Moment *m, *v;
+    float *master, *m_scale, *v_scale;
+    __device__ __forceinline__ Places(const StepArgs &a, const AdamPiece &p, uint32_t lane)
+        : grad((const T *)p.grad + lane * 4), param((T *)p.param + lane * 4), m((Moment *)a.m + p.place + lane * 4), v((Moment *)a.v + p.place + lane * 4),
+          master(MASTER ? a.master + p.place + lane * 4 : nullptr), m_scale(BITS8 ? a.m_scale + p.place / kBlock : nullptr),
+          v_scale(BITS8 ? a.v_scale + p.place / kBlock : nullptr)
+    {
     }
+};
+
+// A lane's eight elements of a block, as they lie, by fours: each load and store of a warp
+// is one stretch of memory in every type.  FAST: a whole block of an aligned tensor;
+// otherwise weights and gradients go one by one, and past the tensor's end (`left` elements
+// of the piece from this lane's first on) there are zeros.
+template <typename T, bool BITS8, bool MASTER, bool FAST>
+struct Raw {
+    Four<T> g[2], w[2];
+    uint32_t m8[2], v8[2];
+    Four<float> m[2], v[2], master[2];
+    float m_scale, v_scale;
+
+    __device__ __forceinline__ void load(const Places<T, BITS8, MASTER> &at, uint32_t block, int32_t left)
+    {
+        if (BITS8) m_scale = at.m_scale[block], v_scale = at.v_scale[block];
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+            const uint32_t i = block * kBlock + j * 128;
+            if (FAST) {
+                g[j].u = __ldcs(reinterpret_cast<const typename Four<T>::Bits *>(at.grad + i));
+                if (!MASTER) w[j].u = __ldcs(reinterpret_cast<const typename Four<T>::Bits *>(at.param + i));
+            }
+            // (the state has whole blocks)
+            if (MASTER) master[j].u = __ldcs(reinterpret_cast<const uint4 *>(at.master + i));
+            if (BITS8) {
+                m8[j] = __ldcs(reinterpret_cast<const uint32_t *>(at.m + i));
+                v8[j] = __ldcs(reinterpret_cast<const uint32_t *>(at.v + i));
+            } else {
+                m[j].u = __ldcs(reinterpret_cast<const uint4 *>(at.m + i));
+                v[j].u = __ldcs(reinterpret_cast<const uint4 *>(at.v + i));
+            }
+            if (!FAST) {
+                T *x = reinterpret_cast<T *>(&g[j].u), *y = reinterpret_cast<T *>(&w[j].u);
+                float *xm = reinterpret_cast<float *>(&m[j].u), *xv = reinterpret_cast<float *>(&v[j].u), *xw = reinterpret_cast<float *>(&master[j].u);
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    const bool inside = (int32_t)(i + k) < left;
+                    x[k] = inside ? at.grad[i + k] : narrow<T>(0.f);
+                    if (!MASTER) y[k] = inside ? at.param[i + k] : narrow<T>(0.f);
+                    if (inside) continue;
+                    if (MASTER) xw[k] = 0.f;
+                    if (BITS8) m8[j] &= ~(0xFFu << (8 * k)), v8[j] &= ~(0xFFu << (8 * k));
+                    else xm[k] = xv[k] = 0.f;
+                }
+            }
+        }
+    }
+};
+
+// The same by way of shared memory, for whole pieces with moments in 8 bits: all of a
+// piece's loads are under way at once and take no registers.  Each thread reads what it
+// copied itself.  [blocks][halves of a block][threads] of each buffer.
+template <typename T, bool MASTER>
+struct Staged {
+    static constexpr uint32_t kSlots = kPiece / kBlock * 2;
+    using W = typename std::conditional<MASTER, float, T>::type;
+    typename Four<T>::Bits g[kSlots][kThreads];
+    typename Four<W>::Bits w[kSlots][kThreads];
+    uint32_t m[kSlots][kThreads], v[kSlots][kThreads];
+
+    template <uint32_t BYTES>
+    static __device__ __forceinline__ void copy(void *to, const void *from)
+    {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "n"(BYTES) : "memory");
+    }
+    __device__ __forceinline__ void start(const Places<T, true, MASTER> &at)
+    {
+#pragma unroll
+        for (uint32_t k = 0; k < kSlots; ++k) {
+            copy<sizeof(T) * 4>(&g[k][threadIdx.x], at.grad + k * 128);
+            copy<sizeof(W) * 4>(&w[k][threadIdx.x], MASTER ? (const void *)(at.master + k * 128) : (const void *)(at.param + k * 128));
+            copy<4>(&m[k][threadIdx.x], at.m + k * 128);
+            copy<4>(&v[k][threadIdx.x], at.v + k * 128);
+            if (k % 2) asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    }
+    template <uint32_t LEFT>  // blocks behind this one
+    __device__ __forceinline__ void take(Raw<T, true, MASTER, true> &r, uint32_t block) const
+    {
+        asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+            const uint32_t k = block * 2 + j;
+            r.g[j].u = g[k][threadIdx.x];
+            if constexpr (MASTER) r.master[j].u = w[k][threadIdx.x];
+            else r.w[j].u = w[k][threadIdx.x];
+            r.m8[j] = m[k][threadIdx.x], r.v8[j] = v[k][threadIdx.x];
+        }
+    }
+};
+
+// the first `count` of four values
+template <typename T>
+__device__ __forceinline__ void put(T *to, const Four<T> &v, int32_t count)
+{
+    const T *x = reinterpret_cast<const T *>(&v.u);
+#pragma unroll
+    for (int32_t k = 0; k < 4; ++k)
+        if (k < count) to[k] = x[k];
+}
+__device__ __forceinline__ void put(uint8_t *to, uint32_t codes, int32_t count)
+{
+#pragma unroll
+    for (int32_t k = 0; k < 4; ++k)
+        if (k < count) to[k] = (uint8_t)(codes >> (8 * k));
+}
+// four values of the state: all of them, or the first `count`
+template <typename V>
+__device__ __forceinline__ void put(float *to, const V &v, bool all, int32_t count)
+{
+    if (all) __stcs(reinterpret_cast<uint4 *>(to), v.u);
+    else put(to, v, count);
+}
+__device__ __forceinline__ void put(uint8_t *to, uint32_t codes, bool all, int32_t count)
+{
+    if (all) __stcs(reinterpret_cast<uint32_t *>(to), codes);
+    else put(to, codes, count);
+}
+
+template <typename T, bool BITS8, bool MASTER, bool FAST>
+__device__ __forceinline__ void step_block(const Places<T, BITS8, MASTER> &at, const Settings &s, const Raw<T, BITS8, MASTER, FAST> &raw, uint32_t block,
+                                           int32_t left, bool whole, uint32_t lane)
+{
+    float2 m[kPairs], u[kPairs];
     float most_m = 0.f, most_u = 0.f;
+    const float m_unit = BITS8 ? unit_m(raw.m_scale) : 0.f, u_unit = BITS8 ? unit_u(raw.v_scale) : 0.f;
 #pragma unroll
-    for (uint32_t k = 0; k < kLane; ++k) {
-        m[k] = next_m(g, m[k], d[k]);
-        v[k] = next_v(g, v[k], d[k]);
-        u[k] = BITS8 ? root8(v[k]) : __fsqrt_rn(v[k]);
-        w[k] = next_w(g, r, w[k], m[k], u[k]);
-        if (BITS8) {
-            const bool inside = lane + 32 * k < count;
-            if (inside) most_m = larger(most_m, m[k]), most_u = larger(most_u, u[k]);
+    for (uint32_t j = 0; j < 2; ++j) {
+        float2 g[2], w[2], v[2];
+        raw.g[j].pairs(g);
+        if (MASTER) raw.master[j].pairs(w);
+        else raw.w[j].pairs(w);
+        if (!BITS8) {
+            float2 old[2];
+            raw.m[j].pairs(old);
+            raw.v[j].pairs(v);
+            m[2 * j] = old[0], m[2 * j + 1] = old[1];
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+            float2 &mk = m[2 * j + k], &uk = u[2 * j + k];
+            const float2 d = __fmul2_rn(g[k], s.clip), dd = __fmul2_rn(s.rest2, __fmul2_rn(d, d));
+            if (BITS8) {
+                mk = value_m(signed_codes(raw.m8[j], 2 * k), m_unit);
+                const float2 old = value_u(unsigned_codes(raw.v8[j], 2 * k), u_unit);
+                v[k] = __ffma2_rn(__fmul2_rn(s.beta2, old), old, dd);
+            } else {
+                v[k] = __ffma2_rn(s.beta2, v[k], dd);
+            }
+            mk = __ffma2_rn(s.beta1, mk, __fmul2_rn(s.rest1, d));
+            if (BITS8) {
+                // (roots and reciprocals of two units in the last place)
+                uk = make_float2(root_approx(v[k].x), root_approx(v[k].y));
+                const float2 den = __ffma2_rn(uk, s.root, s.eps);
+                w[k] = minus(w[k], s.decay, __fmul2_rn(__fmul2_rn(s.rate, mk), make_float2(reciprocal_approx(den.x), reciprocal_approx(den.y))));
+                most_m = largest(most_m, mk.x, mk.y), most_u = largest(most_u, uk.x, uk.y);
+            } else {
+                uk = make_float2(__fsqrt_rn(v[k].x), __fsqrt_rn(v[k].y));
+                const float2 den = __ffma2_rn(uk, s.root, s.eps), step = __fmul2_rn(s.rate, mk);
+                w[k] = minus(w[k], s.decay, make_float2(__fdiv_rn(step.x, den.x), __fdiv_rn(step.y, den.y)));
+            }
+        }
+        const uint32_t i = block * kBlock + j * 128;
+        const int32_t some = left - (int32_t)i;
+        Four<T> to;
+        to.set(w[0], w[1]);
+        if (FAST) __stcs(reinterpret_cast<typename Four<T>::Bits *>(at.param + i), to.u);
+        else put(at.param + i, to, some);
+        Four<float> wide;
+        if (MASTER) wide.set(w[0], w[1]), put(at.master + i, wide, whole, some);
+        if constexpr (!BITS8) {
+            wide.set(m[2 * j], m[2 * j + 1]), put(at.m + i, wide, whole, some);
+            wide.set(v[0], v[1]), put(at.v + i, wide, whole, some);
         }
     }
-    float new_m = 0.f, new_u = 0.f;
-    if (BITS8) {
-        new_m = block_scale(most_m);
-        new_u = block_scale(most_u);
-        if (new_m != new_m || new_u != new_u) new_m = new_u = __uint_as_float(0x7FFFFFFFu);
-        if (lane == 0) a.m_scale[place / kBlock] = new_m, a.v_scale[place / kBlock] = new_u;
-    }
+    if constexpr (BITS8) {
+        // (elements behind the tensor's end came from zeros: they are zeros)
+        float m_scale = block_scale(most_m), v_scale = block_scale(most_u);
+        if (m_scale + v_scale != m_scale + v_scale) m_scale = v_scale = __uint_as_float(0x7FFFFFFFu);
+        if (lane == 0) at.m_scale[block] = m_scale, at.v_scale[block] = v_scale;
+        const float m_per = per_scale<127>(m_scale), v_per = per_scale<255>(v_scale);
 #pragma unroll
-    for (uint32_t k = 0; k < kLane; ++k) {
-        const uint32_t i = lane + 32 * k;
-        if (i >= count) continue;
-        if (BITS8) {
-            ((int8_t *)a.m)[place + i] = (int8_t)encode_m(m[k], new_m);
-            ((uint8_t *)a.v)[place + i] = (uint8_t)encode_v(u[k], new_u);
-        } else {
-            ((float *)a.m)[place + i] = m[k];
-            ((float *)a.v)[place + i] = v[k];
+        for (uint32_t j = 0; j < 2; ++j) {
+            const uint32_t i = block * kBlock + j * 128;
+            put(at.m + i, to_bytes(codes_m(m[2 * j], m_per), codes_m(m[2 * j + 1], m_per)), whole, left - (int32_t)i);
+            put(at.v + i, to_bytes(codes_u(u[2 * j], v_per), codes_u(u[2 * j + 1], v_per)), whole, left - (int32_t)i);
         }
-        if (MASTER) a.master[place + i] = w[k];
-        w16[i] = narrow<T>(w[k]);
     }
 }
 
-template <typename T, bool BITS8, bool MASTER>
-__device__ __forceinline__ void step_piece(const StepArgs &a, const AdamPiece &p, const AdamGroup &g, const AdamRate &r, uint32_t lane)
+// Blocks of a piece; the first one's loads before the rates are there.  BLOCKS: how many,
+// where that is known (then every address is its first one's and a constant), or 0.
+template <typename T, bool BITS8, bool MASTER, bool FAST, uint32_t BLOCKS>
+__device__ __forceinline__ void step_blocks(const StepArgs &a, const AdamPiece &p, uint32_t lane)
 {
-    for (uint32_t first = 0; first < p.count; first += kBlock) step_block<T, BITS8, MASTER>(a, p, g, r, first, lane);
-}
-
-template <bool BITS8>
-__global__ void __launch_bounds__(kThreads) k_step(const StepArgs a)
-{
-    const uint32_t at = blockIdx.x * kWarps + threadIdx.x / 32, lane = threadIdx.x & 31;
+    const Places<T, BITS8, MASTER> at(a, p, lane);
+    const uint32_t blocks = BLOCKS ? BLOCKS : (p.count + kBlock - 1) / kBlock, whole = p.count / kBlock;
+    const int32_t left = (int32_t)p.count - (int32_t)lane * 4;
+    Raw<T, BITS8, MASTER, FAST> raw;
+    raw.load(at, 0, left);
     previous_done();
-    if (at >= a.n) return;
-    const AdamPiece p = a.pieces[at];
-    const AdamGroup &g = a.groups[p.group];
     const AdamRate r = a.rates[p.group];
     if (!r.live) return;
-    if (p.dtype == FIONA_F32)
-        step_piece<float, BITS8, false>(a, p, g, r, lane);
-    else if (p.dtype == FIONA_F16)
-        a.master ? step_piece<__half, BITS8, true>(a, p, g, r, lane) : step_piece<__half, BITS8, false>(a, p, g, r, lane);
+    const Settings s(a.groups[p.group], r);
+#pragma unroll(BLOCKS ? BLOCKS : 1)
+    for (uint32_t b = 0; b < blocks; ++b) {
+        step_block<T, BITS8, MASTER, FAST>(at, s, raw, b, left, FAST || b < whole, lane);
+        if (b + 1 < blocks) raw.load(at, b + 1, left);
+    }
+}
+
+template <typename T, bool MASTER, uint32_t BLOCK>
+__device__ __forceinline__ void staged_blocks(const Places<T, true, MASTER> &at, const Staged<T, MASTER> &stage, const Settings &s, const float (&scales)[2 * kPiece / kBlock],
+                                              uint32_t lane)
+{
+    constexpr uint32_t kBlocks = kPiece / kBlock;
+    if constexpr (BLOCK < kBlocks) {
+        Raw<T, true, MASTER, true> raw;
+        stage.template take<kBlocks - 1 - BLOCK>(raw, BLOCK);
+        raw.m_scale = scales[2 * BLOCK], raw.v_scale = scales[2 * BLOCK + 1];
+        step_block<T, true, MASTER, true>(at, s, raw, BLOCK, 0, true, lane);
+        staged_blocks<T, MASTER, BLOCK + 1>(at, stage, s, scales, lane);
+    }
+}
+
+template <typename T, bool MASTER>
+__device__ __forceinline__ void step_staged(const StepArgs &a, const AdamPiece &p, uint32_t lane, Staged<T, MASTER> &stage)
+{
+    const Places<T, true, MASTER> at(a, p, lane);
+    stage.start(at);
+    float scales[2 * kPiece / kBlock];
+#pragma unroll
+    for (uint32_t b = 0; b < kPiece / kBlock; ++b) scales[2 * b] = at.m_scale[b], scales[2 * b + 1] = at.v_scale[b];
+    previous_done();
+    const AdamRate r = a.rates[p.group];
+    if (r.live) {
+        const Settings s(a.groups[p.group], r);
+        staged_blocks<T, MASTER, 0>(at, stage, s, scales, lane);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+// `a.pieces`: of tensors of type T
+template <typename T, bool BITS8, bool MASTER>
+__global__ void __launch_bounds__(kThreads, 3) k_step(const StepArgs a)
+{
+    extern __shared__ uint4 smem[];
+    const uint32_t at = blockIdx.x * kWarps + threadIdx.x / 32, lane = threadIdx.x & 31;
+    if (at >= a.n) {
+        previous_done();
+        return;
+    }
+    const AdamPiece p = a.pieces[at];
+    if (p.aligned && p.count == kPiece) {
+        if constexpr (BITS8) step_staged<T, MASTER>(a, p, lane, *reinterpret_cast<Staged<T, MASTER> *>(smem));
+        else step_blocks<T, BITS8, MASTER, true, kPiece / kBlock>(a, p, lane);
+    } else if (p.aligned && p.count % kBlock == 0)
+        step_blocks<T, BITS8, MASTER, true, 0>(a, p, lane);
     else
-        a.master ? step_piece<__nv_bfloat16, BITS8, true>(a, p, g, r, lane) : step_piece<__nv_bfloat16, BITS8, false>(a, p, g, r, lane);
+        step_blocks<T, BITS8, MASTER, false, 0>(a, p, lane);
+}
+
+template <typename T>
+int launch_steps(const fiona_adamw *o, const StepArgs &args, cudaStream_t s)
+{
+    const bool bits8 = o->flags & FIONA_ADAMW_8BIT, master = sizeof(T) == 2 && o->state.master;
+    const void *k = bits8 ? (master ? (const void *)k_step<T, true, sizeof(T) == 2> : (const void *)k_step<T, true, false>)
+                          : (master ? (const void *)k_step<T, false, sizeof(T) == 2> : (const void *)k_step<T, false, false>);
+    const uint32_t bytes = !bits8 ? 0 : master ? (uint32_t)sizeof(Staged<T, sizeof(T) == 2>) : (uint32_t)sizeof(Staged<T, false>);
+    static Allowed allowed[2];
+    if (const int rc = allowed[master].set(k, o->ctx->device, bytes, "adamw step")) return rc;
+    StepArgs a = args;
+    void *p[] = {&a};
+    return launch(k, dim3((a.n + kWarps - 1) / kWarps), kThreads, bytes, s, p, "adamw step");
 }
 
 // masters from the weights
@@ -278,18 +564,64 @@ __global__ void __launch_bounds__(kThreads) k_masters(const AdamPiece *pieces, u
         master[p.place + i] = p.dtype == FIONA_F16 ? widen(((const __half *)p.param)[i]) : widen(((const __nv_bfloat16 *)p.param)[i]);
 }
 
-// moments as values, and back; a warp a block of 256 places
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_moments(const fiona_adamw_state s, bool bits8, uint64_t blocks, T *m, T *v)
+// Moments as values, and back.  A warp reads four blocks at once, and every store is a
+// stretch of 512 bytes of them.
+constexpr uint32_t kTogether = 4;
+
+template <typename T, bool BITS8>
+__global__ void __launch_bounds__(kThreads) k_moments(const fiona_adamw_state s, uint64_t blocks, T *m, T *v)
 {
-    const uint64_t b = (uint64_t)blockIdx.x * kWarps + threadIdx.x / 32;
-    if (b >= blocks) return;
-    const float m_scale = bits8 ? s.m_scale[b] : 0.f, v_scale = bits8 ? s.v_scale[b] : 0.f;
+    constexpr uint32_t k = 16 / sizeof(T), steps = kBlock / (32 * k);  // elements of a lane's store; of them to a block
+    using Codes = typename std::conditional<k == 8, uint2, uint32_t>::type;
+    const uint64_t first = ((uint64_t)blockIdx.x * kWarps + threadIdx.x / 32) * kTogether;
+    if (first >= blocks) return;
+    const uint32_t n = (uint32_t)min((uint64_t)kTogether, blocks - first), lane = threadIdx.x & 31;
 #pragma unroll
-    for (uint32_t k = 0; k < kLane; ++k) {
-        const uint64_t i = b * kBlock + (threadIdx.x & 31) + 32 * k;
-        if (m) m[i] = narrow<T>(bits8 ? decode_m(((const int8_t *)s.m)[i], m_scale) : ((const float *)s.m)[i]);
-        if (v) v[i] = narrow<T>(bits8 ? decode_v(((const uint8_t *)s.v)[i], v_scale) : ((const float *)s.v)[i]);
+    for (uint32_t which = 0; which < 2; ++which) {
+        T *to = which ? v : m;
+        if (!to) continue;
+        to += first * kBlock + lane * k;
+        const void *state = which ? s.v : s.m;
+        const float *scales = (which ? s.v_scale : s.m_scale) + first;
+        Codes q[kTogether * steps];
+        float4 f[BITS8 ? 1 : kTogether * steps][k / 4];
+        float scale[kTogether];
+#pragma unroll
+        for (uint32_t i = 0; i < kTogether * steps; ++i)
+            if (i / steps < n) {
+                const uint64_t at = first * kBlock + i * 32 * k + lane * k;
+                if (BITS8) {
+                    q[i] = __ldcs(reinterpret_cast<const Codes *>((const uint8_t *)state + at));
+                    scale[i / steps] = scales[i / steps];
+                } else {
+#pragma unroll
+                    for (uint32_t j = 0; j < k / 4; ++j) f[i][j] = __ldcs(reinterpret_cast<const float4 *>((const float *)state + at) + j);
+                }
+            }
+#pragma unroll
+        for (uint32_t i = 0; i < kTogether * steps; ++i)
+            if (i / steps < n) {
+                uint4 u;
+                T *x = reinterpret_cast<T *>(&u);
+#pragma unroll
+                for (uint32_t j = 0; j < k; j += 2) {
+                    float2 y;
+                    if (BITS8) {
+                        const uint32_t word = reinterpret_cast<const uint32_t *>(&q[i])[j / 4];
+                        if (which) {
+                            y = value_u(unsigned_codes(word, j % 4), unit_u(scale[i / steps]));
+                            y = __fmul2_rn(y, y);
+                        } else {
+                            y = value_m(signed_codes(word, j % 4), unit_m(scale[i / steps]));
+                        }
+                    } else {
+                        const float4 w = f[i][j / 4];
+                        y = j % 4 ? make_float2(w.z, w.w) : make_float2(w.x, w.y);
+                    }
+                    x[j] = narrow<T>(y.x), x[j + 1] = narrow<T>(y.y);
+                }
+                __stcs(reinterpret_cast<uint4 *>(to + i * 32 * k), u);
+            }
     }
 }
 
@@ -299,29 +631,44 @@ __global__ void __launch_bounds__(kThreads) k_load_moments(const fiona_adamw_sta
     const uint64_t b = (uint64_t)blockIdx.x * kWarps + threadIdx.x / 32;
     if (b >= blocks) return;
     const uint32_t lane = threadIdx.x & 31;
-    float x[kLane], u[kLane], most_m = 0.f, most_u = 0.f;
+    float2 x[kPairs] = {}, u[kPairs] = {};
+    float most_m = 0.f, most_u = 0.f;
 #pragma unroll
-    for (uint32_t k = 0; k < kLane; ++k) {
-        const uint64_t i = b * kBlock + lane + 32 * k;
-        x[k] = m ? widen(m[i]) : 0.f;
-        u[k] = v ? widen(v[i]) : 0.f;
-        if (bits8) {
-            u[k] = root8(u[k]);
-            most_m = larger(most_m, x[k]), most_u = larger(most_u, u[k]);
+    for (uint32_t j = 0; j < 2; ++j) {
+        const uint64_t i = b * kBlock + j * 128 + lane * 4;
+        float2 t[2];
+        if (m) {
+            Four<T>{__ldcs(reinterpret_cast<const typename Four<T>::Bits *>(m + i))}.pairs(t);
+            x[2 * j] = t[0], x[2 * j + 1] = t[1];
         }
+        if (v) {
+            Four<T>{__ldcs(reinterpret_cast<const typename Four<T>::Bits *>(v + i))}.pairs(t);
+            u[2 * j] = t[0], u[2 * j + 1] = t[1];
+        }
+#pragma unroll
+        for (uint32_t k = 2 * j; k < 2 * j + 2; ++k)
+            if (bits8) {
+                u[k] = make_float2(root_approx(u[k].x), root_approx(u[k].y));
+                most_m = largest(most_m, x[k].x, x[k].y), most_u = largest(most_u, u[k].x, u[k].y);
+            }
     }
     const float m_scale = block_scale(most_m), v_scale = block_scale(most_u);
+    const float m_per = per_scale<127>(m_scale), v_per = per_scale<255>(v_scale);
     if (bits8 && lane == 0) {
         if (m) s.m_scale[b] = m_scale;
         if (v) s.v_scale[b] = v_scale;
     }
 #pragma unroll
-    for (uint32_t k = 0; k < kLane; ++k) {
-        const uint64_t i = b * kBlock + lane + 32 * k;
-        if (m && bits8) ((int8_t *)s.m)[i] = (int8_t)encode_m(x[k], m_scale);
-        if (m && !bits8) ((float *)s.m)[i] = x[k];
-        if (v && bits8) ((uint8_t *)s.v)[i] = (uint8_t)encode_v(u[k], v_scale);
-        if (v && !bits8) ((float *)s.v)[i] = u[k];
+    for (uint32_t j = 0; j < 2; ++j) {
+        const uint64_t i = b * kBlock + j * 128 + lane * 4;
+        if (bits8) {
+            if (m) *reinterpret_cast<uint32_t *>((int8_t *)s.m + i) = to_bytes(codes_m(x[2 * j], m_per), codes_m(x[2 * j + 1], m_per));
+            if (v) *reinterpret_cast<uint32_t *>((uint8_t *)s.v + i) = to_bytes(codes_u(u[2 * j], v_per), codes_u(u[2 * j + 1], v_per));
+        } else {
+            Four<float> to;
+            if (m) to.set(x[2 * j], x[2 * j + 1]), *reinterpret_cast<uint4 *>((float *)s.m + i) = to.u;
+            if (v) to.set(u[2 * j], u[2 * j + 1]), *reinterpret_cast<uint4 *>((float *)s.v + i) = to.u;
+        }
     }
 }
 
@@ -337,7 +684,9 @@ template <typename T>
 void moments(const fiona_adamw *o, cudaStream_t s, void *m, void *v)
 {
     const uint64_t n = o->places / kBlock;
-    k_moments<T><<<blocks_of(n), kThreads, 0, s>>>(o->state, o->flags & FIONA_ADAMW_8BIT, n, (T *)m, (T *)v);
+    const uint32_t blocks = blocks_of((n + kTogether - 1) / kTogether);
+    if (o->flags & FIONA_ADAMW_8BIT) k_moments<T, true><<<blocks, kThreads, 0, s>>>(o->state, n, (T *)m, (T *)v);
+    else k_moments<T, false><<<blocks, kThreads, 0, s>>>(o->state, n, (T *)m, (T *)v);
 }
 
 template <typename T>
@@ -352,25 +701,29 @@ void load(const fiona_adamw *o, cudaStream_t s, const void *m, const void *v)
 int launch_adamw_step(const fiona_adamw *o, void *stream, const uint8_t *active)
 {
     cudaStream_t s = (cudaStream_t)stream;
-    uint32_t n = o->n_pieces;
     const bool norms = o->state.norms != nullptr;
-    if (norms && n) {
+    if (o->n_runs) {
         const AdamPiece *pieces = o->d_pieces;
+        const AdamRun *runs = o->d_runs;
+        uint32_t n_runs = o->n_runs;
         float *out = o->d_squares;
-        void *args[] = {&pieces, &n, &active, &out};
-        if (const int rc = launch(k_squares, dim3(blocks_of(n)), kThreads, 0, s, args, "adamw norms")) return rc;
+        void *args[] = {&pieces, &runs, &n_runs, &active, &out};
+        if (const int rc = launch(k_squares, dim3(blocks_of(n_runs)), kThreads, 0, s, args, "adamw norms")) return rc;
     }
     RateArgs r{o->d_groups, norms ? o->d_squares : nullptr, active, o->state.lr, o->state.steps, o->state.norms, o->d_rates, o->n_groups,
                o->flags & FIONA_ADAMW_SKIP_NONFINITE};
     void *rate_args[] = {&r};
-    if (const int rc = norms ? launch(k_norm_rates, dim3(o->n_groups), kThreads, 0, s, rate_args, "adamw rates")
+    if (const int rc = norms ? launch(k_norm_rates, dim3(o->n_groups), kRateThreads, 0, s, rate_args, "adamw rates")
                              : launch(k_rates, dim3((o->n_groups + kThreads - 1) / kThreads), kThreads, 0, s, rate_args, "adamw rates"))
         return rc;
-    if (!n) return FIONA_OK;
-    StepArgs a{o->d_pieces, o->d_groups, o->d_rates, o->state.m, o->state.v, o->state.m_scale, o->state.v_scale, o->state.master, n};
-    void *args[] = {&a};
-    return o->flags & FIONA_ADAMW_8BIT ? launch(k_step<true>, dim3(blocks_of(n)), kThreads, 0, s, args, "adamw step")
-                                       : launch(k_step<false>, dim3(blocks_of(n)), kThreads, 0, s, args, "adamw step");
+    StepArgs a{o->d_pieces, o->d_groups, o->d_rates, o->state.m, o->state.v, o->state.m_scale, o->state.v_scale, o->state.master, 0};
+    for (uint32_t t = 0; t < 3; ++t) {
+        a.pieces = o->d_pieces + o->type_begin[t];
+        a.n = o->type_begin[t + 1] - o->type_begin[t];
+        if (!a.n) continue;
+        if (const int rc = t == FIONA_F32 ? launch_steps<float>(o, a, s) : t == FIONA_F16 ? launch_steps<__half>(o, a, s) : launch_steps<__nv_bfloat16>(o, a, s)) return rc;
+    }
+    return FIONA_OK;
 }
 
 int launch_adamw_reset(const fiona_adamw *o, void *stream)

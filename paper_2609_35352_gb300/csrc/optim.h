@@ -7,20 +7,28 @@
 #include "fiona_optim.h"
 
 constexpr uint32_t kBlock = FIONA_ADAMW_BLOCK;
-constexpr uint32_t kPiece = 1024;  // elements of a tensor that a warp steps
+// Elements of a tensor that a warp steps: kPiece, or a block where that leaves the
+// device's schedulers short of warps (8 each).
+constexpr uint32_t kPiece = 1024;
+constexpr uint32_t kMostRun = 16;  // pieces that one fp32 sum of squares takes
 
 // A warp's work: up to kPiece elements of one tensor, from `place` of the state on.
 struct AdamPiece {
     void *param;
     const void *grad;
     uint64_t place;
-    uint32_t count, group, dtype, pad;
+    uint32_t count, group, dtype, aligned;  // aligned: param and grad to 16 bytes
 };
 
-// A group's settings, and its pieces [begin, end).
+// Pieces of one group whose squares are summed by a warp.
+struct AdamRun {
+    uint32_t begin, end;
+};
+
+// A group's settings, and its runs [begin, end).
 struct AdamGroup {
     double log_beta1, log_beta2;
-    double max_norm;
+    float max_norm;
     float beta1, rest1, beta2, rest2;  // rest: 1 - beta
     float eps, weight_decay;
     uint32_t begin, end;
@@ -37,14 +45,16 @@ struct AdamRate {
 
 struct fiona_adamw {
     const fiona_ctx *ctx = nullptr;
-    uint32_t n_groups = 0, n_pieces = 0, flags = 0;
+    uint32_t n_groups = 0, n_pieces = 0, n_runs = 0, flags = 0;
     uint64_t places = 0;
     fiona_adamw_state state{};
     void *blob = nullptr;  // everything below
-    const AdamPiece *d_pieces = nullptr;  // by group
+    const AdamPiece *d_pieces = nullptr;  // by type, and by group
+    uint32_t type_begin[4] = {};          // of fp32, fp16, bf16, and the end
+    const AdamRun *d_runs = nullptr;      // by group
     const AdamGroup *d_groups = nullptr;
     AdamRate *d_rates = nullptr;   // [n_groups], written by each step
-    float *d_squares = nullptr;    // [n_pieces], written by each step that takes norms
+    float *d_squares = nullptr;    // [n_runs], written by each step that takes norms
 };
 
 int launch_adamw_step(const fiona_adamw *o, void *stream, const uint8_t *active);

@@ -118,8 +118,10 @@ extern "C" int fiona_adamw_create(const fiona_ctx *ctx, uint32_t n, const fiona_
         if (std::isfinite(g.max_norm) && !s.norms) return set_error(FIONA_ERR_ARG, "%s: group %u is clipped, but norms is NULL", who, i);
     }
     if ((flags & FIONA_ADAMW_SKIP_NONFINITE) && !s.norms) return set_error(FIONA_ERR_ARG, "%s: SKIP_NONFINITE, but norms is NULL", who);
+    const uint32_t sms = ctx->sm_count ? ctx->sm_count : 152;
+    const uint32_t piece = places >= 32ull * sms * kPiece ? kPiece : kBlock;
     std::vector<Range> ranges;
-    std::vector<uint32_t> begin(n_groups + 1, 0);  // pieces by group
+    std::vector<uint32_t> begin(3ull * n_groups + 1, 0);  // pieces by type and group
     for (uint32_t i = 0; i < n; ++i) {
         const fiona_adamw_tensor &t = tensors[i];
         if (t.group >= n_groups) return set_error(FIONA_ERR_PLAN, "%s: tensor %u is of group %u of %u", who, i, t.group, n_groups);
@@ -128,7 +130,7 @@ extern "C" int fiona_adamw_create(const fiona_ctx *ctx, uint32_t n, const fiona_
         if (((uintptr_t)t.param | (uintptr_t)t.grad) % e) return set_error(FIONA_ERR_ARG, "%s: tensor %u is not aligned to its element", who, i);
         add(ranges, t.param, t.count * e, true);
         add(ranges, t.grad, t.count * e, false);
-        begin[t.group + 1] += (uint32_t)((t.count + kPiece - 1) / kPiece);
+        begin[(uint64_t)t.dtype * n_groups + t.group + 1] += (uint32_t)((t.count + piece - 1) / piece);
     }
     add(ranges, s.m, places * (bits8 ? 1 : 4), true);
     add(ranges, s.v, places * (bits8 ? 1 : 4), true);
@@ -139,7 +141,19 @@ extern "C" int fiona_adamw_create(const fiona_ctx *ctx, uint32_t n, const fiona_
     add(ranges, s.lr, n_groups * 4ull, false);
     add(ranges, s.norms, n_groups * 4ull, true);
     if (overlapping(ranges)) return set_error(FIONA_ERR_PLAN, "%s: a written range overlaps another", who);
-    for (uint32_t i = 0; i < n_groups; ++i) begin[i + 1] += begin[i];
+    for (uint64_t i = 0; i < 3ull * n_groups; ++i) begin[i + 1] += begin[i];
+    const uint32_t n_pieces = begin.back();
+
+    // runs of pieces: as long as leaves some for every scheduler of the device
+    const uint32_t run = std::min(std::max(n_pieces / (64 * sms), 1u), kMostRun);
+    std::vector<AdamRun> runs;
+    std::vector<uint32_t> run_begin(n_groups + 1, 0);
+    if (s.norms)
+        for (uint32_t i = 0; i < n_groups; ++i) {
+            for (uint64_t c = i; c < 3ull * n_groups; c += n_groups)
+                for (uint32_t k = begin[c]; k < begin[c + 1]; k += run) runs.push_back({k, std::min(k + run, begin[c + 1])});
+            run_begin[i + 1] = (uint32_t)runs.size();
+        }
 
     struct Hold {  // (an exception below frees what there is)
         fiona_adamw *o;
@@ -148,38 +162,44 @@ extern "C" int fiona_adamw_create(const fiona_ctx *ctx, uint32_t n, const fiona_
     fiona_adamw *o = hold.o;
     o->ctx = ctx;
     o->n_groups = n_groups;
-    o->n_pieces = begin[n_groups];
+    o->n_pieces = n_pieces;
+    for (uint32_t c = 0; c < 4; ++c) o->type_begin[c] = begin[(uint64_t)c * n_groups];
+    o->n_runs = (uint32_t)runs.size();
     o->flags = flags;
     o->places = places;
     o->state = s;
     if (ctx->device != FIONA_DEVICE_NONE) {
         DeviceGuard guard(ctx->device);
         if (!guard.ok) return set_error(FIONA_ERR_CUDA, "%s: cannot select device %d", who, ctx->device);
-        const size_t o_groups = align_up(o->n_pieces * sizeof(AdamPiece)), copied = o_groups + align_up(n_groups * sizeof(AdamGroup));
+        const size_t o_runs = align_up(o->n_pieces * sizeof(AdamPiece)), o_groups = o_runs + align_up(runs.size() * sizeof(AdamRun));
+        const size_t copied = o_groups + align_up(n_groups * sizeof(AdamGroup));
         std::vector<uint8_t> image(copied);
         AdamPiece *pieces = reinterpret_cast<AdamPiece *>(image.data());
+        if (!runs.empty()) memcpy(image.data() + o_runs, runs.data(), runs.size() * sizeof(AdamRun));
         AdamGroup *g = reinterpret_cast<AdamGroup *>(image.data() + o_groups);
         for (uint32_t i = 0; i < n_groups; ++i) {
             const fiona_adamw_group &x = groups[i];
-            g[i] = AdamGroup{std::log(x.beta1), std::log(x.beta2), x.max_norm, (float)x.beta1, (float)(1 - x.beta1),
-                             (float)x.beta2, (float)(1 - x.beta2), (float)x.eps, (float)x.weight_decay, begin[i], begin[i + 1]};
+            g[i] = AdamGroup{std::log(x.beta1), std::log(x.beta2), x.max_norm <= 3e38 ? (float)x.max_norm : INFINITY, (float)x.beta1, (float)(1 - x.beta1),
+                             (float)x.beta2, (float)(1 - x.beta2), (float)x.eps, (float)x.weight_decay, run_begin[i], run_begin[i + 1]};
         }
         std::vector<uint32_t> next(begin.begin(), begin.end() - 1);
         uint64_t place = 0;
         for (uint32_t i = 0; i < n; ++i) {
             const fiona_adamw_tensor &t = tensors[i];
             const uint64_t e = element(t.dtype);
-            for (uint64_t k = 0; k < t.count; k += kPiece)
-                pieces[next[t.group]++] = AdamPiece{(uint8_t *)t.param + k * e, (const uint8_t *)t.grad + k * e, place + k,
-                                                    (uint32_t)std::min<uint64_t>(t.count - k, kPiece), t.group, t.dtype, 0};
+            for (uint64_t k = 0; k < t.count; k += piece)
+                pieces[next[(uint64_t)t.dtype * n_groups + t.group]++] = AdamPiece{(uint8_t *)t.param + k * e, (const uint8_t *)t.grad + k * e, place + k,
+                                                    (uint32_t)std::min<uint64_t>(t.count - k, piece), t.group, t.dtype,
+                                                    (((uintptr_t)t.param | (uintptr_t)t.grad) & 15) == 0};
             place += (t.count + kBlock - 1) / kBlock * kBlock;
         }
         const size_t o_rates = copied, o_squares = o_rates + align_up(n_groups * sizeof(AdamRate));
-        cudaError_t e = cudaMalloc(&o->blob, o_squares + align_up(o->n_pieces * 4ull));
+        cudaError_t e = cudaMalloc(&o->blob, o_squares + align_up(o->n_runs * 4ull));
         if (e == cudaSuccess) e = upload(o->blob, image.data(), image.size());
         if (e != cudaSuccess) return cuda_fail(e, who);
         uint8_t *d = static_cast<uint8_t *>(o->blob);
         o->d_pieces = reinterpret_cast<const AdamPiece *>(d);
+        o->d_runs = reinterpret_cast<const AdamRun *>(d + o_runs);
         o->d_groups = reinterpret_cast<const AdamGroup *>(d + o_groups);
         o->d_rates = reinterpret_cast<AdamRate *>(d + o_rates);
         o->d_squares = reinterpret_cast<float *>(d + o_squares);
