@@ -28,17 +28,20 @@ int check_shape(const fiona_ctx *ctx, const Call *c, const char *who)
 
 // blocks of a backward pass by rows: as many as run at once, or more where a column's
 // sum in one would take more than kMostRun rows
-uint64_t grad_blocks(const fiona_ctx *ctx, uint64_t rows, uint32_t cols)
+uint64_t grad_blocks(const fiona_ctx *ctx, uint64_t rows, uint32_t cols, uint32_t size)
 {
-    const uint32_t lanes = backward_lanes(cols);
+    const uint32_t lanes = backward_lanes(cols, size);
     const uint64_t groups = backward_threads(lanes) / lanes, units = (rows + groups - 1) / groups, sms = ctx->sm_count ? ctx->sm_count : 152;
-    return std::min(units, std::max(sms * backward_blocks(cols), (units + kMostRun - 1) / kMostRun));
+    return std::min(units, std::max(sms * backward_blocks(cols, size), (units + kMostRun - 1) / kMostRun));
 }
+
+// whether the kernels that hold rows in registers take a call (they count rows in 32 bits)
+bool by_rows(uint64_t rows, uint64_t cols, uint32_t most) { return cols <= most && rows < (1ull << 31); }
 
 uint64_t grad_work(const fiona_ctx *ctx, uint64_t rows, uint32_t cols, bool sums)
 {
-    if (cols > kMostBackward) return norm_any_grad_work(ctx, rows, cols);
-    return sums ? grad_blocks(ctx, rows, cols) * 2 * cols * 4 : 0;
+    if (!by_rows(rows, cols, kMostBackward)) return norm_any_grad_work(ctx, rows, cols);
+    return sums ? grad_blocks(ctx, rows, cols, 2) * 2 * cols * 4 : 0;  // (as many in fp32, or fewer)
 }
 
 // a vector of the call (NULL: not there)
@@ -85,7 +88,7 @@ extern "C" int fiona_layer_norm(const fiona_ctx *ctx, void *stream, const fiona_
     a.ld_sum = c->ld_sum;
     a.mean = c->mean;
     a.rstd = c->rstd;
-    if (cols > kMostForward) return launch_norm_any(ctx, stream, c->dtype, c->weight_dtype, a);
+    if (!by_rows(rows, cols, kMostForward)) return launch_norm_any(ctx, stream, c->dtype, c->weight_dtype, a);
     const bool w16 = c->weight_dtype == c->dtype;
     return c->dtype == FIONA_F32   ? launch_norm_rows_f32(ctx, stream, a, w16)
            : c->dtype == FIONA_F16 ? launch_norm_rows_f16(ctx, stream, a, w16) : launch_norm_rows_bf16(ctx, stream, a, w16);
@@ -150,10 +153,9 @@ extern "C" int fiona_layer_norm_backward(const fiona_ctx *ctx, void *stream, con
     a.dweight = c->dweight;
     a.dbias = c->dbias;
     if (rows == 0) return launch_norm_grad_sum(stream, c->weight_dtype, nullptr, 0, c->cols, c->dweight, c->dbias);
-    if (cols > kMostBackward) return launch_norm_any_grad(ctx, stream, c->dtype, c->weight_dtype, a, c->work);
+    if (!by_rows(rows, cols, kMostBackward)) return launch_norm_any_grad(ctx, stream, c->dtype, c->weight_dtype, a, c->work);
     const bool w16 = c->weight_dtype == c->dtype;
-    const uint64_t blocks = grad_blocks(ctx, rows, c->cols);
-    if (blocks > 0x7FFFFFFF) return set_error(FIONA_ERR_ARG, "%s: %llu rows", who, (unsigned long long)rows);
+    const uint64_t blocks = grad_blocks(ctx, rows, c->cols, (uint32_t)e);
     float *part = sums ? static_cast<float *>(c->work) : nullptr;
     rc = c->dtype == FIONA_F32   ? launch_norm_rows_grad_f32(ctx, stream, a, w16, (uint32_t)blocks, part)
          : c->dtype == FIONA_F16 ? launch_norm_rows_grad_f16(ctx, stream, a, w16, (uint32_t)blocks, part)

@@ -56,21 +56,13 @@ __device__ __forceinline__ void load(const T *p, uint32_t left, float2 (&v)[K<T>
     }
 }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void store(T *p, uint32_t left, const float2 (&v)[K<T> / 2])
+template <typename T>
+__device__ __forceinline__ uint4 narrowed(const float2 (&v)[K<T> / 2])
 {
-    if (VEC) {
-        Vector<T> x;
+    Vector<T> x;
 #pragma unroll
-        for (uint32_t i = 0; i < K<T> / 2; ++i) x.values()[2 * i] = narrow<T>(v[i].x), x.values()[2 * i + 1] = narrow<T>(v[i].y);
-        __stcs(reinterpret_cast<uint4 *>(p), x.u);
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < K<T> / 2; ++i) {
-            if (2 * i < left) p[2 * i] = narrow<T>(v[i].x);
-            if (2 * i + 1 < left) p[2 * i + 1] = narrow<T>(v[i].y);
-        }
-    }
+    for (uint32_t i = 0; i < K<T> / 2; ++i) x.values()[2 * i] = narrow<T>(v[i].x), x.values()[2 * i + 1] = narrow<T>(v[i].y);
+    return x.u;
 }
 
 // column i of a share
@@ -117,20 +109,25 @@ __device__ __forceinline__ void drop(const dropout::Mask &m, uint64_t z, float2 
     }
 }
 
-constexpr uint32_t kGradAhead = 3;  // rows ahead in a backward pass
+// Rows ahead in a backward pass (one: 16384 x 4096 bf16 130 us for 112), their room beside
+// the weights, for rows of up to `cols`, and whether the weights have room beside them.
+constexpr uint32_t kGradAhead = 2;
+constexpr uint32_t grad_room(uint32_t cols, uint32_t size) { return backward_blocks(cols, size) > 1 ? 96 * 1024 : cols <= 8192 ? 192 * 1024 : 128 * 1024; }
+constexpr bool held_grad_weights(uint32_t cols, uint32_t size) { return size == 2 || cols <= 8192; }
 
 // A thread's places for rows ahead, [stages][tensors][VECS][THREADS]: `now` those of the
 // row that is taken next.
-template <typename T, uint32_t VECS, uint32_t THREADS, uint32_t TENSORS, uint32_t MOST>
+template <typename T, uint32_t VECS, uint32_t THREADS, uint32_t TENSORS, uint32_t ROOM, uint32_t MOST>
 struct Ring {
     static constexpr uint32_t tensor = VECS * THREADS;
-    static constexpr uint32_t stages = ahead(tensor * 16, TENSORS, 192 * 1024, MOST);
+    static constexpr uint32_t stages = ahead(tensor * 16, TENSORS, ROOM, MOST);
     uint4 *begin, *now, *end;
     uint32_t stage;
     __device__ __forceinline__ Ring(uint4 *smem, uint32_t tensors)
         : begin(smem + threadIdx.x), now(begin), end(begin + stages * tensors * tensor), stage(tensors * tensor)
     {
     }
+    __device__ __forceinline__ uint4 *behind() const { return end - threadIdx.x; }  // of all threads' places
     __device__ __forceinline__ void copy(uint4 *place, uint32_t t, uint32_t e, const T *p) const
     {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(async::smem_addr(place + t * tensor + e * THREADS)), "l"(p) : "memory");
@@ -140,6 +137,30 @@ struct Ring {
         const Vector<T> x{now[t * tensor + e * THREADS]};
         x.widened(v);
     }
+    __device__ __forceinline__ void put(uint32_t t, uint32_t e, uint4 u) const { now[t * tensor + e * THREADS] = u; }
+
+    // Rows that vectors cannot address pass through the same places, but one element after
+    // another along the row: LANES threads take what lies side by side.  (Each thread its
+    // own columns one by one: every access of a warp touches 16 sectors for 32 elements.)
+    template <uint32_t LANES>
+    __device__ __forceinline__ T *element(uint32_t t, uint32_t j) const
+    {
+        T *row = reinterpret_cast<T *>(now - threadIdx.x % LANES + t * tensor);
+        return row + j / (LANES * K<T>) * (THREADS * K<T>) + j % (LANES * K<T>);
+    }
+    template <uint32_t LANES>
+    __device__ __forceinline__ void fill(uint32_t t, const T *row, uint32_t cols) const  // (zeros up to a whole vector)
+    {
+        const uint32_t end = (cols + K<T> - 1) / K<T> * K<T>;
+#pragma unroll 8
+        for (uint32_t j = threadIdx.x % LANES; j < end; j += LANES) *element<LANES>(t, j) = j < cols ? row[j] : narrow<T>(0.f);
+    }
+    template <uint32_t LANES>
+    __device__ __forceinline__ void drain(uint32_t t, T *row, uint32_t cols) const
+    {
+#pragma unroll 8
+        for (uint32_t j = threadIdx.x % LANES; j < cols; j += LANES) row[j] = *element<LANES>(t, j);
+    }
     __device__ __forceinline__ void next()
     {
         now += stage;
@@ -147,41 +168,49 @@ struct Ring {
     }
 };
 
-// A thread's weights and biases in shared memory, as they lie: [2][VECS][vectors][THREADS].
-// For blocks of one row at a time: from global memory they would come out of L2 for every
-// row, since the rows ahead take L1's room (16384 x 4096 bf16, two rows in flight: 103 us
-// for 96).  They come by way of L1: copies past it of the same lines by every block go to
-// a few slices of L2 (2048 x 1024 fp32, each warp its own copy: 49 us for 6.5).
-constexpr bool held_weights(uint32_t lanes) { return lanes >= 128 && lanes <= 512; }  // (1024: no room beside the rows)
+// A row's weights (and biases) in shared memory, as they lie: [2][VECS][parts][LANES].
+// For rows of several warps: from global memory they would come out of L2 for every row,
+// since the rows ahead take L1's room (16384 x 4096 bf16, two rows in flight: 103 us for
+// 96).  They come by way of L1: copies past it of the same lines by every block go to a
+// few slices of L2 (2048 x 1024 fp32, each warp its own copy: 49 us for 6.5).
+constexpr bool held_weights(uint32_t lanes) { return lanes >= 128 && lanes <= 512; }  // (forward; 1024: no room beside the rows)
 
-template <typename T, uint32_t VECS, uint32_t THREADS>
+template <typename T, uint32_t VECS, uint32_t LANES>
 struct Held {
     uint4 *at;
     bool w16;
     uint32_t parts;  // 16 bytes each of K weights
-    __device__ __forceinline__ Held(uint4 *place, bool w16) : at(place), w16(w16 || sizeof(T) == 4), parts(this->w16 ? 1 : 2) {}
-    static uint32_t bytes(bool w16) { return 2 * VECS * (w16 || sizeof(T) == 4 ? 1 : 2) * THREADS * 16; }
+    __device__ __forceinline__ Held(uint4 *place, bool w16) : at(place + threadIdx.x % LANES), w16(w16 || sizeof(T) == 4), parts(this->w16 ? 1 : 2) {}
+    static uint32_t bytes(bool w16) { return VECS * (w16 || sizeof(T) == 4 ? 1 : 2) * LANES * 16; }  // of weights or biases
     __device__ __forceinline__ void copy(uint32_t which, uint32_t e, const void *p, uint32_t col) const
     {
         const uint4 *from = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p) + (size_t)col * (w16 ? sizeof(T) : 4));
         for (uint32_t i = 0; i < parts; ++i)
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(async::smem_addr(at + ((which * VECS + e) * parts + i) * THREADS)), "l"(from + i) : "memory");
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(async::smem_addr(at + ((which * VECS + e) * parts + i) * LANES)), "l"(from + i) : "memory");
     }
     __device__ __forceinline__ void read(uint32_t which, uint32_t e, float2 (&v)[K<T> / 2]) const
     {
         if (w16) {
-            const Vector<T> x{at[(which * VECS + e) * THREADS]};
+            const Vector<T> x{at[(which * VECS + e) * LANES]};
             x.widened(v);
         } else {
 #pragma unroll
             for (uint32_t k = 0; k < K<T> / 4; ++k) {
-                const Vector<float> x{at[((which * VECS + e) * 2 + k) * THREADS]};
+                const Vector<float> x{at[((which * VECS + e) * 2 + k) * LANES]};
 #pragma unroll
                 for (uint32_t i = 0; i < 2; ++i) v[2 * k + i] = make_float2(x.values()[2 * i], x.values()[2 * i + 1]);
             }
         }
     }
 };
+
+// a barrier of a row's threads
+template <uint32_t LANES>
+__device__ __forceinline__ void row_barrier()
+{
+    if (LANES == 32) __syncwarp();
+    else async::named_barrier(1 + threadIdx.x / LANES, LANES);
+}
 
 // Sums over a row's threads, the same in each of them; `slot`: two in turn, so that one
 // barrier a sum is enough.
@@ -193,7 +222,7 @@ __device__ __forceinline__ V row_sum(V v, float2 (*part)[32], uint32_t slot)
     constexpr uint32_t kWarps = LANES / 32;
     const uint32_t warp = threadIdx.x / 32, first = warp / kWarps * kWarps;
     if ((threadIdx.x & 31) == 0) reinterpret_cast<V &>(part[slot][warp]) = v;
-    async::named_barrier(1 + warp / kWarps, LANES);
+    row_barrier<LANES>();
     V p[4];
 #pragma unroll
     for (uint32_t w = 0; w < 4; ++w)
@@ -216,22 +245,22 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
     previous_done();
     next_may_start();
     const uint32_t lane = threadIdx.x % LANES, at = lane * K<T>;
-    const uint64_t step = (uint64_t)gridDim.x * kGroups;
-    using Rows = Ring<T, VECS, kThreads, 2, LANES == 128 ? 2 : 1>;
-    Rows ring(smem, a.res ? 2 : 1);
+    const uint32_t step = gridDim.x * kGroups, rows = (uint32_t)a.rows;  // (fewer than 2^31 here)
+    using Rows = Ring<T, VECS, kThreads, 2, 192 * 1024, LANES == 128 ? 2 : 1>;
+    Rows ring(smem, a.res || !VEC ? 2 : 1);
     constexpr uint32_t kAhead = Rows::stages;
     constexpr bool kHeld = VEC && held_weights(LANES);
-    const Held<T, VECS, kThreads> held(ring.end, w16);
+    const Held<T, VECS, LANES> held(ring.behind(), w16);
     const float per = 1.f / (float)a.cols;
     // this thread's first column of the next row to fetch, and of the row taken
-    uint64_t t = (uint64_t)blockIdx.x * kGroups + threadIdx.x / LANES, next_t = t;
+    uint32_t t = blockIdx.x * kGroups + threadIdx.x / LANES, next_t = t;
     const T *x = (const T *)a.x + t * a.ldx + at, *res = (const T *)a.res + t * a.ld_res + at;
     T *out = (T *)a.out + t * a.ld_out + at, *total = (T *)a.sum + t * a.ld_sum + at;
     const uint64_t step_x = step * a.ldx, step_res = step * a.ld_res, step_out = step * a.ld_out, step_sum = step * a.ld_sum;
     const uint64_t step_z = step * a.mask.groups * dropout::kGolden;
     uint64_t z = a.mask.base + (t * a.mask.groups + lane * (K<T> / 4)) * dropout::kGolden;  // its first draw
     auto fetch = [&](uint4 *place) {
-        if (next_t < a.rows)
+        if (next_t < rows)
 #pragma unroll
             for (uint32_t e = 0; e < VECS; ++e)
                 if (e * LANES * K<T> + at < a.cols) {
@@ -250,26 +279,31 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
             }
         for (uint32_t i = 0; i < kAhead; ++i) fetch(ring.begin + i * ring.stage);  // (the weights with the first row)
     }
-    for (; t < a.rows; t += step, out += step_out, total += step_sum, z += step_z) {
+    for (; t < rows; t += step, out += step_out, total += step_sum, z += step_z) {
         float2 s[VECS][K<T> / 2], sum = both(0.f);
-        if (VEC) async::cp_async_wait<kAhead - 1>();
+        if (VEC) {
+            async::cp_async_wait<kAhead - 1>();
+        } else {
+            ring.template fill<LANES>(0, x - at, a.cols);
+            if (a.res) ring.template fill<LANES>(1, res - at, a.cols);
+            row_barrier<LANES>();
+        }
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e) {
             const uint32_t col = e * LANES * K<T> + at;
             if (col < a.cols) {
-                if (VEC) ring.read(0, e, s[e]);
-                else load<T, false>(x + e * LANES * K<T>, a.cols - col, s[e]);
+                ring.read(0, e, s[e]);
                 if (a.mask.level) drop(a.mask, z + (uint64_t)(e * LANES * (K<T> / 4)) * dropout::kGolden, s[e]);
                 if (a.res) {
                     float2 r[K<T> / 2];
-                    if (VEC) ring.read(1, e, r);
-                    else load<T, false>(res + e * LANES * K<T>, a.cols - col, r);
+                    ring.read(1, e, r);
 #pragma unroll
                     for (uint32_t i = 0; i < K<T> / 2; ++i) s[e][i] = __fadd2_rn(s[e][i], r[i]);
                 }
 #pragma unroll
                 for (uint32_t i = 0; i < K<T> / 2; ++i) sum = __fadd2_rn(sum, s[e][i]);  // (columns past the last are 0)
-                if (a.sum) store<T, VEC>(total + e * LANES * K<T>, a.cols - col, s[e]);
+                if (VEC && a.sum) __stcs(reinterpret_cast<uint4 *>(total + e * LANES * K<T>), narrowed<T>(s[e]));
+                if (!VEC && a.sum) ring.put(1, e, narrowed<T>(s[e]));
             }
         }
         const float about = row_sum<LANES>(sum.x + sum.y, part, 0) * per;
@@ -303,8 +337,15 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
                 else load_weights<T, VEC>(a.bias, w16, col, a.cols - col, 0.f, b);
 #pragma unroll
                 for (uint32_t i = 0; i < K<T> / 2; ++i) s[e][i] = scaled(s[e][i], both(rstd), both(shift), w[i], b[i]);
-                store<T, VEC>(out + e * LANES * K<T>, a.cols - col, s[e]);
+                if (VEC) __stcs(reinterpret_cast<uint4 *>(out + e * LANES * K<T>), narrowed<T>(s[e]));
+                else ring.put(0, e, narrowed<T>(s[e]));
             }
+        }
+        if (!VEC) {
+            row_barrier<LANES>();
+            ring.template drain<LANES>(0, out - at, a.cols);
+            if (a.sum) ring.template drain<LANES>(1, total - at, a.cols);
+            row_barrier<LANES>();  // (before the next row comes)
         }
         if (lane == 0) {
             if (a.mean) a.mean[t] = about + left;
@@ -313,11 +354,13 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
     }
 }
 
-// `sums`: [gridDim.x][2][cols], null: dweight and dbias are not wanted.  (Rows in twos, for
-// one barrier and two chains at once: no quicker, 133 us for 132 on 16384 x 4096 bf16 with
-// dropout, and slower below 2048 columns for want of registers.)
-template <typename T, uint32_t LANES, uint32_t VECS, bool VEC>
-__global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES * VECS * K<T>)) k_norm_rows_grad(const NormGradArgs a, const bool w16, float *sums)
+// A thread keeps the sums of its up to 32 columns in registers, and nothing else of a row:
+// once the row's averages are there, it takes the row out of its places in shared memory
+// again.  (With g and xh in registers from one to the other and 16 columns a thread, half as
+// many rows are under way on an SM: 16384 x 4096 bf16 with dropout 131 us.)  `sums`:
+// [gridDim.x][2][cols], null: dweight and dbias are not wanted.
+template <typename T, uint32_t LANES, uint32_t VECS, bool VEC, bool DSUM>
+__global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES * VECS * K<T>, sizeof(T))) k_norm_rows_grad(const NormGradArgs a, const bool w16, float *sums)
 {
     constexpr uint32_t kThreads = backward_threads(LANES), kGroups = kThreads / LANES;
     extern __shared__ uint4 smem[];
@@ -325,83 +368,111 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
     previous_done();
     next_may_start();
     const uint32_t lane = threadIdx.x % LANES, group = threadIdx.x / LANES, at = lane * K<T>;
-    const uint64_t step = (uint64_t)gridDim.x * kGroups;
-    using Rows = Ring<T, VECS, kThreads, 3, kGradAhead>;
-    Rows ring(smem, a.dsum ? 3 : 2);
+    const uint32_t step = gridDim.x * kGroups, rows = (uint32_t)a.rows;  // (fewer than 2^31 here)
+    constexpr uint32_t kTensors = DSUM ? 3 : 2;
+    using Rows = Ring<T, VECS, kThreads, kTensors, grad_room(LANES * VECS * K<T>, sizeof(T)), kGradAhead>;
+    Rows ring(smem, kTensors);
     constexpr uint32_t kAhead = Rows::stages;
+    constexpr bool kHeld = VEC && held_grad_weights(LANES * VECS * K<T>, sizeof(T));
+    const Held<T, VECS, LANES> held(ring.behind(), w16);
     const float per = 1.f / (float)a.cols;
-    float2 w[VECS][K<T> / 2], dw[VECS][K<T> / 2] = {}, db[VECS][K<T> / 2] = {};
-#pragma unroll
-    for (uint32_t e = 0; e < VECS; ++e) {
-        const uint32_t col = e * LANES * K<T> + at;
-        if (col < a.cols) load_weights<T, VEC>(a.weight, w16, col, a.cols - col, 1.f, w[e]);
-    }
+    float2 dw[VECS][K<T> / 2] = {}, db[VECS][K<T> / 2] = {};
     // This thread's first column of the next row to fetch, and of the row taken, moved on
-    // from row to row.  (Made anew from the row's number: 144 us for 132 on 16384 x 4096 bf16.)
-    uint64_t t = (uint64_t)blockIdx.x * kGroups + group, next_t = t;
+    // from row to row.  (Made anew from the row's number: 144 us for 132.)
+    uint32_t t = blockIdx.x * kGroups + group, next_t = t;
     const T *dy = (const T *)a.dy + t * a.ld_dy + at, *x = (const T *)a.sum + t * a.ld_sum + at, *dsum = (const T *)a.dsum + t * a.ld_dsum + at;
     T *dx = (T *)a.dx + t * a.ld_dx + at, *dres = (T *)a.dres + t * a.ld_dres + at;
     const uint64_t step_dy = step * a.ld_dy, step_x = step * a.ld_sum, step_ds = step * a.ld_dsum, step_dx = step * a.ld_dx, step_dr = step * a.ld_dres;
     const uint64_t step_z = step * a.mask.groups * dropout::kGolden;
     uint64_t z = a.mask.base + (t * a.mask.groups + lane * (K<T> / 4)) * dropout::kGolden;  // its first draw
     auto fetch = [&](uint4 *place) {
-        if (next_t < a.rows)
+        if (next_t < rows)
 #pragma unroll
             for (uint32_t e = 0; e < VECS; ++e)
                 if (e * LANES * K<T> + at < a.cols) {
                     ring.copy(place, 0, e, dy + e * LANES * K<T>);
                     ring.copy(place, 1, e, x + e * LANES * K<T>);
-                    if (a.dsum) ring.copy(place, 2, e, dsum + e * LANES * K<T>);
+                    if (DSUM) ring.copy(place, 2, e, dsum + e * LANES * K<T>);
                 }
         async::cp_async_commit();
         next_t += step, dy += step_dy, x += step_x, dsum += step_ds;
     };
-    if (VEC)
+    if (VEC) {
+        if (kHeld && a.weight && group == 0)
+#pragma unroll
+            for (uint32_t e = 0; e < VECS; ++e)
+                if (e * LANES * K<T> + at < a.cols) held.copy(0, e, a.weight, e * LANES * K<T> + at);
+        async::cp_async_commit();
         for (uint32_t i = 0; i < kAhead; ++i) fetch(ring.begin + i * ring.stage);
+        if (kHeld && a.weight) {  // (the weights are the whole block's)
+            async::cp_async_wait<kAhead>();
+            __syncthreads();
+        }
+    }
+    // dy, xh and g of vector e of the row taken (columns past the last: dy is 0)
+    auto take = [&](uint32_t e, float mean, float rstd, float2 (&d)[K<T> / 2], float2 (&xh)[K<T> / 2], float2 (&g)[K<T> / 2]) {
+        const uint32_t col = e * LANES * K<T> + at;
+        ring.read(0, e, d), ring.read(1, e, xh);
+        if (kHeld && a.weight) held.read(0, e, g);
+        else load_weights<T, VEC>(a.weight, w16, col, a.cols - col, 1.f, g);
+#pragma unroll
+        for (uint32_t i = 0; i < K<T> / 2; ++i) xh[i] = xhat(xh[i], both(-mean), both(rstd)), g[i] = __fmul2_rn(d[i], g[i]);
+    };
     uint32_t slot = 0;
-    for (; t < a.rows; t += step, dx += step_dx, dres += step_dr, z += step_z, slot ^= 1) {
-        float2 g[VECS][K<T> / 2], xh[VECS][K<T> / 2], s1 = both(0.f), s2 = both(0.f);
+    for (; t < rows; t += step, dx += step_dx, dres += step_dr, z += step_z, slot ^= 1) {
+        float2 s1 = both(0.f), s2 = both(0.f);
         const float mean = a.mean[t], rstd = a.rstd[t];
-        if (VEC) async::cp_async_wait<kAhead - 1>();
+        if (VEC) {
+            async::cp_async_wait<kAhead - 1>();
+        } else {
+            ring.template fill<LANES>(0, dy - at, a.cols);
+            ring.template fill<LANES>(1, x - at, a.cols);
+            if (DSUM) ring.template fill<LANES>(2, dsum - at, a.cols);
+            row_barrier<LANES>();
+        }
 #pragma unroll
-        for (uint32_t e = 0; e < VECS; ++e) {
-            const uint32_t col = e * LANES * K<T> + at;
-            if (col < a.cols) {
-                if (VEC) ring.read(0, e, g[e]), ring.read(1, e, xh[e]);
-                else load<T, false>(dy + e * LANES * K<T>, a.cols - col, g[e]), load<T, false>(x + e * LANES * K<T>, a.cols - col, xh[e]);
+        for (uint32_t e = 0; e < VECS; ++e)
+            if (e * LANES * K<T> + at < a.cols) {
+                float2 d[K<T> / 2], xh[K<T> / 2], g[K<T> / 2];
+                take(e, mean, rstd, d, xh, g);
 #pragma unroll
-                for (uint32_t i = 0; i < K<T> / 2; ++i) {  // (columns past the last: g is 0)
-                    xh[e][i] = xhat(xh[e][i], both(-mean), both(rstd));
-                    dw[e][i] = __ffma2_rn(g[e][i], xh[e][i], dw[e][i]), db[e][i] = __fadd2_rn(db[e][i], g[e][i]);
-                    g[e][i] = __fmul2_rn(g[e][i], w[e][i]);
-                    s1 = __fadd2_rn(s1, g[e][i]), s2 = __ffma2_rn(g[e][i], xh[e][i], s2);
+                for (uint32_t i = 0; i < K<T> / 2; ++i) {
+                    dw[e][i] = __ffma2_rn(d[i], xh[i], dw[e][i]), db[e][i] = __fadd2_rn(db[e][i], d[i]);
+                    s1 = __fadd2_rn(s1, g[i]), s2 = __ffma2_rn(g[i], xh[i], s2);
                 }
             }
-        }
         const float2 avg = row_sum<LANES>(make_float2(s1.x + s1.y, s2.x + s2.y), part, slot);
         const float2 minus_g = both(avg.x * -per), minus_gxh = both(avg.y * -per);
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e) {
             const uint32_t col = e * LANES * K<T> + at;
             if (col < a.cols) {
+                float2 d[K<T> / 2], xh[K<T> / 2], g[K<T> / 2];
+                take(e, mean, rstd, d, xh, g);
 #pragma unroll
-                for (uint32_t i = 0; i < K<T> / 2; ++i) g[e][i] = centred_gradient(g[e][i], xh[e][i], minus_g, minus_gxh);
-                if (a.dsum) {
-                    float2 d[K<T> / 2];
-                    if (VEC) ring.read(2, e, d);
-                    else load<T, false>(dsum + e * LANES * K<T>, a.cols - col, d);
+                for (uint32_t i = 0; i < K<T> / 2; ++i) g[i] = centred_gradient(g[i], xh[i], minus_g, minus_gxh);
+                if (DSUM) {
+                    ring.read(2, e, d);
 #pragma unroll
-                    for (uint32_t i = 0; i < K<T> / 2; ++i) g[e][i] = __ffma2_rn(both(rstd), g[e][i], d[i]);
+                    for (uint32_t i = 0; i < K<T> / 2; ++i) g[i] = __ffma2_rn(both(rstd), g[i], d[i]);
                 } else {
 #pragma unroll
-                    for (uint32_t i = 0; i < K<T> / 2; ++i) g[e][i] = __fmul2_rn(both(rstd), g[e][i]);
+                    for (uint32_t i = 0; i < K<T> / 2; ++i) g[i] = __fmul2_rn(both(rstd), g[i]);
                 }
-                if (a.dres) store<T, VEC>(dres + e * LANES * K<T>, a.cols - col, g[e]);
+                if (VEC && a.dres) __stcs(reinterpret_cast<uint4 *>(dres + e * LANES * K<T>), narrowed<T>(g));
+                if (!VEC) ring.put(0, e, narrowed<T>(g));
                 if (a.dx) {
-                    if (a.mask.level) drop(a.mask, z + (uint64_t)(e * LANES * (K<T> / 4)) * dropout::kGolden, g[e]);
-                    store<T, VEC>(dx + e * LANES * K<T>, a.cols - col, g[e]);
+                    if (a.mask.level) drop(a.mask, z + (uint64_t)(e * LANES * (K<T> / 4)) * dropout::kGolden, g);
+                    if (VEC) __stcs(reinterpret_cast<uint4 *>(dx + e * LANES * K<T>), narrowed<T>(g));
+                    else ring.put(1, e, narrowed<T>(g));
                 }
             }
+        }
+        if (!VEC) {
+            row_barrier<LANES>();
+            if (a.dres) ring.template drain<LANES>(0, dres - at, a.cols);
+            if (a.dx) ring.template drain<LANES>(1, dx - at, a.cols);
+            row_barrier<LANES>();  // (before the next row comes)
         }
         // (all that was read has been used: its places may be filled again)
         if (VEC) fetch(ring.now), ring.next();
@@ -451,12 +522,12 @@ template <typename T, uint32_t LANES, uint32_t VECS>
 int forward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormArgs &a, bool w16)
 {
     constexpr uint32_t kThreads = forward_threads(LANES), kGroups = kThreads / LANES;
-    using Rows = Ring<T, VECS, kThreads, 2, LANES == 128 ? 2 : 1>;
+    using Rows = Ring<T, VECS, kThreads, 2, 192 * 1024, LANES == 128 ? 2 : 1>;
     const uint64_t z = sizeof(T);
     const bool one = a.rows == 1;  // (one row has no stride)
     const bool vec = vectors(a.cols, K<T>, {a.x, a.res, a.out, a.sum, a.weight, a.bias},
                              {one ? 0 : a.ldx * z, one || !a.res ? 0 : a.ld_res * z, one ? 0 : a.ld_out * z, one || !a.sum ? 0 : a.ld_sum * z});
-    const uint32_t bytes = vec ? (a.res ? 2 : 1) * Rows::tensor * 16 * Rows::stages + (held_weights(LANES) && (a.weight || a.bias) ? Held<T, VECS, kThreads>::bytes(w16) : 0) : 0;
+    const uint32_t bytes = (vec ? (a.res ? 2 : 1) * Rows::stages : 2) * Rows::tensor * 16 + (vec && held_weights(LANES) && (a.weight || a.bias) ? 2 * Held<T, VECS, LANES>::bytes(w16) : 0);
     const uint64_t units = (a.rows + kGroups - 1) / kGroups;
     // as many blocks as run at once: 1024 threads an SM, if their rows have room
     const uint32_t blocks = std::max(1u, std::min(1024 / kThreads, bytes ? 220 * 1024 / (bytes + 1536) : 32u));
@@ -464,8 +535,8 @@ int forward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormArgs &a, bool w
     NormArgs b = a;
     void *args[] = {&b, &w16};
     const void *k = vec ? (const void *)k_norm_rows<T, LANES, VECS, true> : (const void *)k_norm_rows<T, LANES, VECS, false>;
-    static Allowed allowed;
-    if (const int rc = allowed.set(k, ctx->device, bytes, "layer norm")) return rc;
+    static Allowed allowed[2];
+    if (const int rc = allowed[vec].set(k, ctx->device, bytes, "layer norm")) return rc;
     return launch(k, dim3((uint32_t)std::min(units, fill)), kThreads, bytes, s, args, "layer norm");
 }
 
@@ -486,37 +557,50 @@ int forward_rows(const fiona_ctx *ctx, void *stream, const NormArgs &a, bool w16
     }
 }
 
-template <typename T, uint32_t LANES, uint32_t VECS>
+template <typename T, uint32_t LANES, uint32_t VECS, bool DSUM>
 int backward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormGradArgs &a, bool w16, uint32_t blocks, float *part)
 {
     constexpr uint32_t kThreads = backward_threads(LANES), kGroups = kThreads / LANES;
-    using Rows = Ring<T, VECS, kThreads, 3, kGradAhead>;
+    constexpr uint32_t kTensors = DSUM ? 3 : 2;
+    using Rows = Ring<T, VECS, kThreads, kTensors, grad_room(LANES * VECS * K<T>, sizeof(T)), kGradAhead>;
+    constexpr bool kHeld = held_grad_weights(LANES * VECS * K<T>, sizeof(T));
     const uint64_t z = sizeof(T);
     const bool one = a.rows == 1;
     const bool vec = vectors(a.cols, K<T>, {a.dy, a.sum, a.dsum, a.dx, a.dres, a.weight},
                              {one ? 0 : a.ld_dy * z, one ? 0 : a.ld_sum * z, one || !a.dsum ? 0 : a.ld_dsum * z, one || !a.dx ? 0 : a.ld_dx * z,
                               one || !a.dres ? 0 : a.ld_dres * z});
-    uint32_t bytes = vec ? (a.dsum ? 3 : 2) * Rows::tensor * 16 * Rows::stages : 0;
+    uint32_t bytes = kTensors * Rows::tensor * 16 * (vec ? Rows::stages : 1) + (vec && kHeld && a.weight ? Held<T, VECS, LANES>::bytes(w16) : 0);
     if (part && kGroups > 1) bytes = std::max(bytes, kGroups * 2 * a.cols * 4);
     NormGradArgs b = a;
     void *args[] = {&b, &w16, &part};
-    const void *k = vec ? (const void *)k_norm_rows_grad<T, LANES, VECS, true> : (const void *)k_norm_rows_grad<T, LANES, VECS, false>;
-    static Allowed allowed;
-    if (const int rc = allowed.set(k, ctx->device, bytes, "layer norm gradient")) return rc;
+    const void *k = vec ? (const void *)k_norm_rows_grad<T, LANES, VECS, true, DSUM> : (const void *)k_norm_rows_grad<T, LANES, VECS, false, DSUM>;
+    static Allowed allowed[2];
+    if (const int rc = allowed[vec].set(k, ctx->device, bytes, "layer norm gradient")) return rc;
     return launch(k, dim3(blocks), kThreads, bytes, s, args, "layer norm gradient");
+}
+
+template <typename T, uint32_t LANES, uint32_t VECS>
+int backward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormGradArgs &a, bool w16, uint32_t blocks, float *part)
+{
+    return a.dsum ? backward_rows<T, LANES, VECS, true>(ctx, s, a, w16, blocks, part) : backward_rows<T, LANES, VECS, false>(ctx, s, a, w16, blocks, part);
 }
 
 template <typename T>
 int backward_rows(const fiona_ctx *ctx, void *stream, const NormGradArgs &a, bool w16, uint32_t blocks, float *part)
 {
     cudaStream_t s = (cudaStream_t)stream;
-    constexpr uint32_t one = 8 / K<T>, two = 2 * one;  // eights of columns in vectors
-    switch (backward_lanes(a.cols)) {
-        case 32: return a.cols <= 256 ? backward_rows<T, 32, one>(ctx, s, a, w16, blocks, part) : backward_rows<T, 32, two>(ctx, s, a, w16, blocks, part);
-        case 64: return backward_rows<T, 64, two>(ctx, s, a, w16, blocks, part);
-        case 128: return backward_rows<T, 128, two>(ctx, s, a, w16, blocks, part);
-        case 256: return backward_rows<T, 256, two>(ctx, s, a, w16, blocks, part);
-        default: return backward_rows<T, 512, two>(ctx, s, a, w16, blocks, part);
+    constexpr uint32_t one = 8 / K<T>, two = 2 * one, four = 4 * one;  // eights of columns in vectors
+    switch (backward_lanes(a.cols, sizeof(T))) {
+        case 32:
+            return a.cols <= 256   ? backward_rows<T, 32, one>(ctx, s, a, w16, blocks, part)
+                   : a.cols <= 512 ? backward_rows<T, 32, two>(ctx, s, a, w16, blocks, part) : backward_rows<T, 32, four>(ctx, s, a, w16, blocks, part);
+        case 64: return backward_rows<T, 64, four>(ctx, s, a, w16, blocks, part);
+        case 128: return backward_rows<T, 128, four>(ctx, s, a, w16, blocks, part);
+        case 256: return backward_rows<T, 256, four>(ctx, s, a, w16, blocks, part);
+        default:
+            if constexpr (sizeof(T) == 4)
+                if (a.cols <= 8192) return backward_rows<T, 512, two>(ctx, s, a, w16, blocks, part);
+            return backward_rows<T, 512, four>(ctx, s, a, w16, blocks, part);
     }
 }
 

@@ -2,7 +2,7 @@
 #pragma once
 #include "norm.h"
 
-constexpr uint32_t kMostForward = 16384, kMostBackward = 8192;  // columns
+constexpr uint32_t kMostForward = 16384, kMostBackward = 16384;  // columns
 
 // A row's threads, by its width and type alone: a row comes out the same however many
 // others there are.  Each takes up to 16 columns; forward 32 where a row of 513 to 1024
@@ -14,13 +14,15 @@ inline uint32_t forward_lanes(uint32_t cols, uint32_t size)
 {
     return cols <= 512 ? 32 : cols <= 1024 ? (size == 4 ? 64 : 32) : cols <= 2048 ? 128 : cols <= 4096 ? 256 : cols <= 8192 ? 512 : 1024;
 }
-inline uint32_t backward_lanes(uint32_t cols)
+// (backward 8 to 32 columns: 16 of 4097 to 8192 in fp32, whose rows ahead leave room for
+// one block an SM)
+inline uint32_t backward_lanes(uint32_t cols, uint32_t size)
 {
-    return cols <= 512 ? 32 : cols <= 1024 ? 64 : cols <= 2048 ? 128 : cols <= 4096 ? 256 : 512;
+    return cols <= 1024 ? 32 : cols <= 2048 ? 64 : cols <= 4096 ? 128 : cols <= 8192 && size == 2 ? 256 : 512;
 }
 // blocks of a backward pass on an SM at a time, for rows of up to `cols`: what their sums
-// leave of the registers
-constexpr uint32_t backward_blocks(uint32_t cols) { return cols <= 256 ? 3 : cols <= 4096 ? 2 : 1; }
+// leave of the registers, and their rows of shared memory
+constexpr uint32_t backward_blocks(uint32_t cols, uint32_t size) { return cols <= 256 ? 3 : cols <= 4096 || (cols <= 8192 && size == 2) ? 2 : 1; }
 constexpr uint32_t forward_threads(uint32_t lanes) { return lanes < 128 ? 128 : lanes; }   // of a block
 constexpr uint32_t backward_threads(uint32_t lanes) { return lanes < 256 ? 256 : lanes; }
 
