@@ -479,35 +479,28 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
         else dy += step_dy, x += step_x, dsum += step_ds;
     }
     if (!sums) return;
-    float *out = sums + (uint64_t)blockIdx.x * 2 * a.cols;
-    if (kGroups == 1) {
+    // The groups' sums, added up in order, by way of shared memory: a thread's eight or four
+    // columns would go to as many stretches of memory.
+    float *out = sums + (uint64_t)blockIdx.x * 2 * a.cols, *s = reinterpret_cast<float *>(smem);
+    constexpr uint32_t kLine = LANES + 32 / K<T>, kTable = VECS * K<T> * kLine;  // (no two banks meet)
+    if (VEC) async::cp_async_wait<0>();
+    __syncthreads();
 #pragma unroll
-        for (uint32_t e = 0; e < VECS; ++e) {
-            const uint32_t col = (e * LANES + lane) * K<T>;
+    for (uint32_t e = 0; e < VECS; ++e)
 #pragma unroll
-            for (uint32_t i = 0; i < K<T>; ++i)
-                if (col + i < a.cols) out[col + i] = of(dw[e], i), out[a.cols + col + i] = of(db[e], i);
+        for (uint32_t i = 0; i < K<T>; ++i) {
+            s[2 * group * kTable + (e * K<T> + i) * kLine + lane] = of(dw[e], i);
+            s[(2 * group + 1) * kTable + (e * K<T> + i) * kLine + lane] = of(db[e], i);
         }
-    } else {
-        // the groups' sums, added up in order
-        float *s = reinterpret_cast<float *>(smem);
-        if (VEC) async::cp_async_wait<0>();
-        __syncthreads();
+    __syncthreads();
+    for (uint32_t which = 0; which < 2; ++which)
+        for (uint32_t j = threadIdx.x; j < a.cols; j += kThreads) {
+            const uint32_t at = which * kTable + (j / (LANES * K<T>) * K<T> + j % K<T>) * kLine + j % (LANES * K<T>) / K<T>;
+            float v = s[at];
 #pragma unroll
-        for (uint32_t e = 0; e < VECS; ++e) {
-            const uint32_t col = (e * LANES + lane) * K<T>;
-#pragma unroll
-            for (uint32_t i = 0; i < K<T>; ++i)
-                if (col + i < a.cols) s[group * 2 * a.cols + col + i] = of(dw[e], i), s[(group * 2 + 1) * a.cols + col + i] = of(db[e], i);
+            for (uint32_t k = 1; k < kGroups; ++k) v += s[2 * k * kTable + at];
+            out[which * a.cols + j] = v;
         }
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < 2 * a.cols; i += kThreads) {
-            float v = s[i];
-#pragma unroll
-            for (uint32_t k = 1; k < kGroups; ++k) v += s[k * 2 * a.cols + i];
-            out[i] = v;
-        }
-    }
 }
 
 inline bool vectors(uint32_t cols, uint32_t k, std::initializer_list<const void *> starts, std::initializer_list<uint64_t> bytes)
@@ -570,7 +563,7 @@ int backward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormGradArgs &a, b
                              {one ? 0 : a.ld_dy * z, one ? 0 : a.ld_sum * z, one || !a.dsum ? 0 : a.ld_dsum * z, one || !a.dx ? 0 : a.ld_dx * z,
                               one || !a.dres ? 0 : a.ld_dres * z});
     uint32_t bytes = kTensors * Rows::tensor * 16 * (vec ? Rows::stages : 1) + (vec && kHeld && a.weight ? Held<T, VECS, LANES>::bytes(w16) : 0);
-    if (part && kGroups > 1) bytes = std::max(bytes, kGroups * 2 * a.cols * 4);
+    if (part) bytes = std::max<uint32_t>(bytes, kGroups * 2 * VECS * K<T> * (LANES + 32 / K<T>) * 4);
     NormGradArgs b = a;
     void *args[] = {&b, &w16, &part};
     const void *k = vec ? (const void *)k_norm_rows_grad<T, LANES, VECS, true, DSUM> : (const void *)k_norm_rows_grad<T, LANES, VECS, false, DSUM>;
