@@ -8,9 +8,11 @@ client's own, the client's low-rank adapter and its training data:
     1. activations are packed by columns (ciphertext i: feature i of every token),
        encoded on the GPU and encrypted; the server evaluates y = W x;
     2. the adapters of all clients are trained at once on the decrypted
-       activations: forward with dropout, a loss, backward, a step;
-    3. serving: one new token of each client, through projection and adapter, its
-       output through the block's dropout into the residual stream (p = 0: as it is).
+       activations: forward with dropout, the block's dropout, residual and layer
+       norm in one call, a loss, backward through both, and an AdamW step in which
+       each client is a model of its own (the norm's weights, shared, another); a
+       client without data sits out;
+    3. serving: one new token of each client, through projection, adapter and norm.
 
 Run: python examples/private_adapters.py
 """
@@ -28,6 +30,8 @@ import oracle  # noqa: E402
 from paper_2609_35352_gb300 import adapters as AD  # noqa: E402
 from paper_2609_35352_gb300 import build as BUILD  # noqa: E402
 from paper_2609_35352_gb300 import fiona as F  # noqa: E402
+from paper_2609_35352_gb300 import layernorm as LN  # noqa: E402
+from paper_2609_35352_gb300 import optim as O  # noqa: E402
 from paper_2609_35352_gb300 import workloads as W  # noqa: E402
 
 N, LIMBS, DELTA = 1024, 3, 2.0 ** 40
@@ -100,6 +104,11 @@ def shared_projection(ctx, rng):
     return F.Plan(ctx, F.compile_plan(WIDTH, WIDTH, WIDTH, routes)), signs * gamma[:, None], gamma
 
 
+def normed(v):
+    """What the clients want comes out of a norm too (weights one and zero)."""
+    return torch.nn.functional.layer_norm(v, (WIDTH,))
+
+
 def main(steps=300, verbose=True):
     say = print if verbose else (lambda *a: None)
     BUILD.build()
@@ -130,10 +139,11 @@ def main(steps=300, verbose=True):
     error = float((base.double() - x.double() @ torch.from_numpy(weights.T).cuda()).abs().max())
     say("encrypted projection: %d tokens, off by at most %.1e" % (starts[-1], error))
     shift = torch.randn(CLIENTS, WIDTH, 4, device="cuda") @ torch.randn(CLIENTS, 4, WIDTH, device="cuda") * 0.25
-    target = base.clone()
+    target = x + base
     for c in range(CLIENTS):
         rows = slice(starts[c], starts[c + 1])
         target[rows] += x[rows] @ shift[c].T
+    target = normed(target)
 
     # train all clients' adapters at once
     A = torch.randn(CLIENTS, r_max, WIDTH, device="cuda") * WIDTH ** -0.5
@@ -142,17 +152,33 @@ def main(steps=300, verbose=True):
     work = batch.workspace(WIDTH, WIDTH, x.dtype)
     out, dx, h = torch.empty_like(base), torch.empty_like(x), torch.empty(starts[-1], r_max, device="cuda")
     dA, dB = torch.empty_like(A), torch.empty_like(B)
-    drop = AD.Dropout(0.02, seed=7)
+    # the block's norm: residual + dropout(out), and what its gradient needs
+    weight, bias = torch.ones(WIDTH, device="cuda"), torch.zeros(WIDTH, device="cuda")
+    dweight, dbias = torch.empty_like(weight), torch.empty_like(bias)
+    y, total, dy = torch.empty_like(base), torch.empty_like(base), torch.empty_like(base)
+    mean, rstd = torch.empty(starts[-1], device="cuda"), torch.empty(starts[-1], device="cuda")
+    norm_work = LN.workspace(ctx, *x.shape)
+    # each client a group of its own, the norm's weights one more
+    clients = list(range(CLIENTS))
+    opt = O.AdamW(ctx, [A, B, weight, bias], [dA, dB, dweight, dbias], groups=[clients, clients, CLIENTS, CLIENTS],
+                  lr=[2e-2] * CLIENTS + [2e-3], weight_decay=0.0, max_norm=1.0)
+    active = torch.tensor([n > 0 for n in counts] + [True], device="cuda")
+    idle = A[counts.index(0)].clone()
+    drop, block_drop = AD.Dropout(0.02, seed=7), AD.Dropout(0.01, seed=8)
     stream, losses = torch.cuda.current_stream(), []
     for step in range(steps):
         batch.forward(x, A, B, out, base=base, h=h, dropout=drop, work=work, stream=stream)
-        diff = out - target
+        LN.layer_norm(ctx, out, y, weight=weight, bias=bias, residual=x, dropout=block_drop, sum=total, mean=mean, rstd=rstd, stream=stream)
+        diff = y - target
         losses.append(float((diff * diff).mean()))
-        dy = diff * 0.01
+        LN.layer_norm_backward(ctx, diff * (2.0 / diff.numel()), total, mean, rstd, weight=weight, dropout=block_drop, dx=dy, dweight=dweight,
+                               dbias=dbias, work=norm_work, stream=stream)
         batch.backward(x, h, dy, A, B, dx, dA, dB, dropout=drop, work=work, stream=stream)
-        A -= 0.05 * dA
-        B -= 0.05 * dB
-        drop = drop.advance(*x.shape)
+        opt.lr.mul_(0.99)
+        opt.step(active=active, stream=stream)
+        drop, block_drop = drop.advance(*x.shape), block_drop.advance(*x.shape)
+    if not torch.equal(A[counts.index(0)], idle):
+        raise AssertionError("a client without data has another adapter than before")
     say("training: loss %.4f -> %.4f in %d steps" % (losses[0], losses[-1], steps))
 
     # serve one new token of each client
@@ -161,11 +187,11 @@ def main(steps=300, verbose=True):
     served, stream_out = torch.empty(CLIENTS, WIDTH, device="cuda"), torch.empty(CLIENTS, WIDTH, device="cuda")
     token_base = project(token)
     single.forward(token, A, B, served, base=token_base, work=single.workspace(WIDTH, WIDTH, token.dtype), stream=stream)
-    AD.dropout(ctx, served, stream_out, AD.Dropout(0.0, 0), residual=token, stream=stream)
+    LN.layer_norm(ctx, served, stream_out, weight=weight, bias=bias, residual=token, stream=stream)
     trained = [c for c in range(CLIENTS) if counts[c]]
-    wanted = token_base + torch.stack([token[c] @ shift[c].T for c in range(CLIENTS)])
-    before = float((token_base - wanted)[trained].pow(2).mean())
-    after = float((stream_out - token - wanted)[trained].pow(2).mean())
+    wanted = normed(token + token_base + torch.stack([token[c] @ shift[c].T for c in range(CLIENTS)]))
+    before = float((normed(token + token_base) - wanted)[trained].pow(2).mean())
+    after = float((stream_out - wanted)[trained].pow(2).mean())
     say("serving: squared error on new tokens %.4f without adapters, %.4f with" % (before, after))
     return {"projection_error": error, "losses": losses, "before": before, "after": after}
 

@@ -30,8 +30,9 @@
  * mean's own rounding left is taken out again.  out and sum are each rounded once,
  * from the same fp32 s: out is the norm of s, not of the rounded sum.  The gradient
  * goes by the sum, mean and rstd that it is given.  Results do not depend on the
- * order in which blocks run: no atomics on values.  A row with an infinity or a
- * NaN that is not dropped comes out as NaN, and no other row does.
+ * order in which blocks run: no atomics on values; a row's do not depend on the rows
+ * beside it.  A row with an infinity or a NaN that is not dropped comes out as NaN, and
+ * no other row does; one whose squares pass fp32's range has rstd 0.
  *
  * Errors, ownership, streams and devices as in fiona.h.
  */
@@ -79,7 +80,7 @@ int fiona_layer_norm(const fiona_ctx *ctx, void *cuda_stream, const fiona_layer_
 /* The gradient, from the sum, mean, rstd and drop of the forward pass.  NULL:
  * weight one, dsum zero; dx, dresidual, dweight, dbias not wanted.  dweight and
  * dbias are overwritten (with zero if there are no rows).  work: NULL will do where
- * neither dweight nor dbias is wanted and cols is at most 8192. */
+ * neither dweight nor dbias is wanted and cols is at most 16384. */
 typedef struct fiona_layer_norm_grad_call {
     uint64_t rows;
     uint32_t cols;
