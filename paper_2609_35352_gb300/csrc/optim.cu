@@ -262,7 +262,7 @@ __device__ __forceinline__ float2 value_u(float2 q, float unit) { return __fmul2
 __device__ __forceinline__ float unit_m(float scale) { return __fmul_rn(scale, 1.f / 16129.f); }
 __device__ __forceinline__ float unit_u(float scale) { return __fmul_rn(scale, 1.f / 65025.f); }
 
-// A lane's first four elements of a piece in each buffer.
+// A lane's first elements of a piece in each buffer: its fours, or its eights.
 template <typename T, bool BITS8, bool MASTER>
 struct Places {
     using Moment = typename std::conditional<BITS8, uint8_t, float>::type;
@@ -270,9 +270,9 @@ struct Places {
     T *param;
     Moment *m, *v;
     float *master, *m_scale, *v_scale;
-    __device__ __forceinline__ Places(const StepArgs &a, const AdamPiece &p, uint32_t lane)
-        : grad((const T *)p.grad + lane * 4), param((T *)p.param + lane * 4), m((Moment *)a.m + p.place + lane * 4), v((Moment *)a.v + p.place + lane * 4),
-          master(MASTER ? a.master + p.place + lane * 4 : nullptr), m_scale(BITS8 ? a.m_scale + p.place / kBlock : nullptr),
+    __device__ __forceinline__ Places(const StepArgs &a, const AdamPiece &p, uint32_t first)
+        : grad((const T *)p.grad + first), param((T *)p.param + first), m((Moment *)a.m + p.place + first), v((Moment *)a.v + p.place + first),
+          master(MASTER ? a.master + p.place + first : nullptr), m_scale(BITS8 ? a.m_scale + p.place / kBlock : nullptr),
           v_scale(BITS8 ? a.v_scale + p.place / kBlock : nullptr)
     {
     }
@@ -328,42 +328,61 @@ struct Raw {
 
 // The same by way of shared memory, for whole pieces with moments in 8 bits: all of a
 // piece's loads are under way at once and take no registers.  Each thread reads what it
-// copied itself.  [blocks][halves of a block][threads] of each buffer.
+// copied itself.  [blocks][threads] of each buffer: a lane's eight elements side by side
+// where nothing of them is wider than 16 bits (half as many copies and stores), else its
+// two fours, [blocks][2][threads].
 template <typename T, bool MASTER>
 struct Staged {
-    static constexpr uint32_t kSlots = kPiece / kBlock * 2;
+    static constexpr bool kEights = sizeof(T) == 2 && !MASTER;
+    static constexpr uint32_t kBlocks = kPiece / kBlock, kEach = kEights ? 1 : 2, kCount = kEights ? 8 : 4;  // elements of a copy
     using W = typename std::conditional<MASTER, float, T>::type;
-    typename Four<T>::Bits g[kSlots][kThreads];
-    typename Four<W>::Bits w[kSlots][kThreads];
-    uint32_t m[kSlots][kThreads], v[kSlots][kThreads];
+    using G4 = typename Four<T>::Bits;
+    using W4 = typename Four<W>::Bits;
+    using G = typename std::conditional<kEights, uint4, G4>::type;
+    using V = typename std::conditional<kEights, uint4, W4>::type;
+    using Codes = typename std::conditional<kEights, uint2, uint32_t>::type;
+    G g[kBlocks * kEach][kThreads];
+    V w[kBlocks * kEach][kThreads];
+    Codes m[kBlocks * kEach][kThreads], v[kBlocks * kEach][kThreads];
 
-    template <uint32_t BYTES>
-    static __device__ __forceinline__ void copy(void *to, const void *from)
+    template <typename X>
+    static __device__ __forceinline__ void copy(X *to, const void *from)
     {
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "n"(BYTES) : "memory");
+        const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+        if (sizeof(X) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(sizeof(X)) : "memory");
     }
     __device__ __forceinline__ void start(const Places<T, true, MASTER> &at)
     {
 #pragma unroll
-        for (uint32_t k = 0; k < kSlots; ++k) {
-            copy<sizeof(T) * 4>(&g[k][threadIdx.x], at.grad + k * 128);
-            copy<sizeof(W) * 4>(&w[k][threadIdx.x], MASTER ? (const void *)(at.master + k * 128) : (const void *)(at.param + k * 128));
-            copy<4>(&m[k][threadIdx.x], at.m + k * 128);
-            copy<4>(&v[k][threadIdx.x], at.v + k * 128);
-            if (k % 2) asm volatile("cp.async.commit_group;" ::: "memory");
+        for (uint32_t k = 0; k < kBlocks * kEach; ++k) {
+            const uint32_t i = k * 32 * kCount;
+            copy(&g[k][threadIdx.x], at.grad + i);
+            copy(&w[k][threadIdx.x], MASTER ? (const void *)(at.master + i) : (const void *)(at.param + i));
+            copy(&m[k][threadIdx.x], at.m + i);
+            copy(&v[k][threadIdx.x], at.v + i);
+            if (kEights || k % 2) asm volatile("cp.async.commit_group;" ::: "memory");
         }
     }
     template <uint32_t LEFT>  // blocks behind this one
     __device__ __forceinline__ void take(Raw<T, true, MASTER, true> &r, uint32_t block) const
     {
         asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+        if constexpr (kEights) {
+            const uint4 x = g[block][threadIdx.x], y = w[block][threadIdx.x];
+            r.g[0].u = make_uint2(x.x, x.y), r.g[1].u = make_uint2(x.z, x.w);
+            r.w[0].u = make_uint2(y.x, y.y), r.w[1].u = make_uint2(y.z, y.w);
+            const uint2 a = m[block][threadIdx.x], b = v[block][threadIdx.x];
+            r.m8[0] = a.x, r.m8[1] = a.y, r.v8[0] = b.x, r.v8[1] = b.y;
+        } else {
 #pragma unroll
-        for (uint32_t j = 0; j < 2; ++j) {
-            const uint32_t k = block * 2 + j;
-            r.g[j].u = g[k][threadIdx.x];
-            if constexpr (MASTER) r.master[j].u = w[k][threadIdx.x];
-            else r.w[j].u = w[k][threadIdx.x];
-            r.m8[j] = m[k][threadIdx.x], r.v8[j] = v[k][threadIdx.x];
+            for (uint32_t j = 0; j < 2; ++j) {
+                const uint32_t k = block * 2 + j;
+                r.g[j].u = g[k][threadIdx.x];
+                if constexpr (MASTER) r.master[j].u = w[k][threadIdx.x];
+                else r.w[j].u = w[k][threadIdx.x];
+                r.m8[j] = m[k][threadIdx.x], r.v8[j] = v[k][threadIdx.x];
+            }
         }
     }
 };
@@ -396,11 +415,12 @@ __device__ __forceinline__ void put(uint8_t *to, uint32_t codes, bool all, int32
     else put(to, codes, count);
 }
 
-template <typename T, bool BITS8, bool MASTER, bool FAST>
+template <typename T, bool BITS8, bool MASTER, bool FAST, bool EIGHTS = false>
 __device__ __forceinline__ void step_block(const Places<T, BITS8, MASTER> &at, const Settings &s, const Raw<T, BITS8, MASTER, FAST> &raw, uint32_t block,
                                            int32_t left, bool whole, uint32_t lane)
 {
     float2 m[kPairs], u[kPairs];
+    Four<T> to[2];
     float most_m = 0.f, most_u = 0.f;
     const float m_unit = BITS8 ? unit_m(raw.m_scale) : 0.f, u_unit = BITS8 ? unit_u(raw.v_scale) : 0.f;
 #pragma unroll
@@ -441,10 +461,9 @@ __device__ __forceinline__ void step_block(const Places<T, BITS8, MASTER> &at, c
         }
         const uint32_t i = block * kBlock + j * 128;
         const int32_t some = left - (int32_t)i;
-        Four<T> to;
-        to.set(w[0], w[1]);
-        if (FAST) __stcs(reinterpret_cast<typename Four<T>::Bits *>(at.param + i), to.u);
-        else put(at.param + i, to, some);
+        to[j].set(w[0], w[1]);
+        if (FAST && !EIGHTS) __stcs(reinterpret_cast<typename Four<T>::Bits *>(at.param + i), to[j].u);
+        if (!FAST) put(at.param + i, to[j], some);
         Four<float> wide;
         if (MASTER) wide.set(w[0], w[1]), put(at.master + i, wide, whole, some);
         if constexpr (!BITS8) {
@@ -452,17 +471,24 @@ __device__ __forceinline__ void step_block(const Places<T, BITS8, MASTER> &at, c
             wide.set(v[0], v[1]), put(at.v + i, wide, whole, some);
         }
     }
+    if constexpr (EIGHTS) __stcs(reinterpret_cast<uint4 *>(at.param + block * kBlock), make_uint4(to[0].u.x, to[0].u.y, to[1].u.x, to[1].u.y));
     if constexpr (BITS8) {
         // (elements behind the tensor's end came from zeros: they are zeros)
         float m_scale = block_scale(most_m), v_scale = block_scale(most_u);
         if (m_scale + v_scale != m_scale + v_scale) m_scale = v_scale = __uint_as_float(0x7FFFFFFFu);
         if (lane == 0) at.m_scale[block] = m_scale, at.v_scale[block] = v_scale;
         const float m_per = per_scale<127>(m_scale), v_per = per_scale<255>(v_scale);
+        uint32_t m8[2], v8[2];
 #pragma unroll
         for (uint32_t j = 0; j < 2; ++j) {
+            m8[j] = to_bytes(codes_m(m[2 * j], m_per), codes_m(m[2 * j + 1], m_per));
+            v8[j] = to_bytes(codes_u(u[2 * j], v_per), codes_u(u[2 * j + 1], v_per));
             const uint32_t i = block * kBlock + j * 128;
-            put(at.m + i, to_bytes(codes_m(m[2 * j], m_per), codes_m(m[2 * j + 1], m_per)), whole, left - (int32_t)i);
-            put(at.v + i, to_bytes(codes_u(u[2 * j], v_per), codes_u(u[2 * j + 1], v_per)), whole, left - (int32_t)i);
+            if (!EIGHTS) put(at.m + i, m8[j], whole, left - (int32_t)i), put(at.v + i, v8[j], whole, left - (int32_t)i);
+        }
+        if (EIGHTS) {
+            __stcs(reinterpret_cast<uint2 *>(at.m + block * kBlock), make_uint2(m8[0], m8[1]));
+            __stcs(reinterpret_cast<uint2 *>(at.v + block * kBlock), make_uint2(v8[0], v8[1]));
         }
     }
 }
@@ -472,7 +498,7 @@ __device__ __forceinline__ void step_block(const Places<T, BITS8, MASTER> &at, c
 template <typename T, bool BITS8, bool MASTER, bool FAST, uint32_t BLOCKS>
 __device__ __forceinline__ void step_blocks(const StepArgs &a, const AdamPiece &p, uint32_t lane)
 {
-    const Places<T, BITS8, MASTER> at(a, p, lane);
+    const Places<T, BITS8, MASTER> at(a, p, lane * 4);
     const uint32_t blocks = BLOCKS ? BLOCKS : (p.count + kBlock - 1) / kBlock, whole = p.count / kBlock;
     const int32_t left = (int32_t)p.count - (int32_t)lane * 4;
     Raw<T, BITS8, MASTER, FAST> raw;
@@ -497,7 +523,7 @@ __device__ __forceinline__ void staged_blocks(const Places<T, true, MASTER> &at,
         Raw<T, true, MASTER, true> raw;
         stage.template take<kBlocks - 1 - BLOCK>(raw, BLOCK);
         raw.m_scale = scales[2 * BLOCK], raw.v_scale = scales[2 * BLOCK + 1];
-        step_block<T, true, MASTER, true>(at, s, raw, BLOCK, 0, true, lane);
+        step_block<T, true, MASTER, true, Staged<T, MASTER>::kEights>(at, s, raw, BLOCK, 0, true, lane);
         staged_blocks<T, MASTER, BLOCK + 1>(at, stage, s, scales, lane);
     }
 }
@@ -505,7 +531,7 @@ __device__ __forceinline__ void staged_blocks(const Places<T, true, MASTER> &at,
 template <typename T, bool MASTER>
 __device__ __forceinline__ void step_staged(const StepArgs &a, const AdamPiece &p, uint32_t lane, Staged<T, MASTER> &stage)
 {
-    const Places<T, true, MASTER> at(a, p, lane);
+    const Places<T, true, MASTER> at(a, p, lane * Staged<T, MASTER>::kCount);
     stage.start(at);
     float scales[2 * kPiece / kBlock];
 #pragma unroll
