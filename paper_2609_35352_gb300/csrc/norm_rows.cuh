@@ -236,10 +236,16 @@ __device__ __forceinline__ V row_sum(V v, float2 (*part)[32], uint32_t slot)
     return v;
 }
 
-template <typename T, uint32_t LANES, uint32_t VECS, bool VEC>
+// How a row lies: by elements; in whole vectors; in as many as its threads have, LANES times
+// VECS (then nothing asks whether a vector is there: 16384 x 4096 bf16 82 us for 84 and,
+// backward, 103 for 106).
+enum class Reach { elements, vectors, whole };
+
+template <typename T, uint32_t LANES, uint32_t VECS, Reach REACH>
 __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const NormArgs a, const bool w16)
 {
     constexpr uint32_t kThreads = forward_threads(LANES), kGroups = kThreads / LANES;
+    constexpr bool VEC = REACH != Reach::elements;
     extern __shared__ uint4 smem[];
     __shared__ float2 part[2][32];
     previous_done();
@@ -252,6 +258,8 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
     constexpr bool kHeld = VEC && held_weights(LANES);
     const Held<T, VECS, LANES> held(ring.behind(), w16);
     const float per = 1.f / (float)a.cols;
+    // whether the row reaches to this thread's vector from column `col` on
+    auto inside = [&](uint32_t col) { return REACH == Reach::whole || col < a.cols; };
     // this thread's first column of the next row to fetch, and of the row taken
     uint32_t t = blockIdx.x * kGroups + threadIdx.x / LANES, next_t = t;
     const T *x = (const T *)a.x + t * a.ldx + at, *res = (const T *)a.res + t * a.ld_res + at;
@@ -263,7 +271,7 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
         if (next_t < rows)
 #pragma unroll
             for (uint32_t e = 0; e < VECS; ++e)
-                if (e * LANES * K<T> + at < a.cols) {
+                if (inside(e * LANES * K<T> + at)) {
                     ring.copy(place, 0, e, x + e * LANES * K<T>);
                     if (a.res) ring.copy(place, 1, e, res + e * LANES * K<T>);
                 }
@@ -273,7 +281,7 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
     if (VEC) {
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e)
-            if (kHeld && e * LANES * K<T> + at < a.cols) {
+            if (kHeld && inside(e * LANES * K<T> + at)) {
                 if (a.weight) held.copy(0, e, a.weight, e * LANES * K<T> + at);
                 if (a.bias) held.copy(1, e, a.bias, e * LANES * K<T> + at);
             }
@@ -291,7 +299,7 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e) {
             const uint32_t col = e * LANES * K<T> + at;
-            if (col < a.cols) {
+            if (inside(col)) {
                 ring.read(0, e, s[e]);
                 if (a.mask.level) drop(a.mask, z + (uint64_t)(e * LANES * (K<T> / 4)) * dropout::kGolden, s[e]);
                 if (a.res) {
@@ -315,7 +323,7 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e) {
             const uint32_t col = e * LANES * K<T> + at;
-            if (col < a.cols)
+            if (inside(col))
 #pragma unroll
                 for (uint32_t i = 0; i < K<T> / 2; ++i) {
                     s[e][i] = __fadd2_rn(s[e][i], minus_about);
@@ -329,7 +337,7 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e) {
             const uint32_t col = e * LANES * K<T> + at;
-            if (col < a.cols) {
+            if (inside(col)) {
                 float2 w[K<T> / 2], b[K<T> / 2];
                 if (kHeld && a.weight) held.read(0, e, w);
                 else load_weights<T, VEC>(a.weight, w16, col, a.cols - col, 1.f, w);
@@ -359,10 +367,11 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
 // again.  (With g and xh in registers from one to the other and 16 columns a thread, half as
 // many rows are under way on an SM: 16384 x 4096 bf16 with dropout 131 us.)  `sums`:
 // [gridDim.x][2][cols], null: dweight and dbias are not wanted.
-template <typename T, uint32_t LANES, uint32_t VECS, bool VEC, bool DSUM>
+template <typename T, uint32_t LANES, uint32_t VECS, Reach REACH, bool DSUM>
 __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES * VECS * K<T>, sizeof(T))) k_norm_rows_grad(const NormGradArgs a, const bool w16, float *sums)
 {
     constexpr uint32_t kThreads = backward_threads(LANES), kGroups = kThreads / LANES;
+    constexpr bool VEC = REACH != Reach::elements;
     extern __shared__ uint4 smem[];
     __shared__ float2 part[2][32];
     previous_done();
@@ -376,6 +385,8 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
     constexpr bool kHeld = VEC && held_grad_weights(LANES * VECS * K<T>, sizeof(T));
     const Held<T, VECS, LANES> held(ring.behind(), w16);
     const float per = 1.f / (float)a.cols;
+    // whether the row reaches to this thread's vector from column `col` on
+    auto inside = [&](uint32_t col) { return REACH == Reach::whole || col < a.cols; };
     float2 dw[VECS][K<T> / 2] = {}, db[VECS][K<T> / 2] = {};
     // This thread's first column of the next row to fetch, and of the row taken, moved on
     // from row to row.  (Made anew from the row's number: 144 us for 132.)
@@ -389,7 +400,7 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
         if (next_t < rows)
 #pragma unroll
             for (uint32_t e = 0; e < VECS; ++e)
-                if (e * LANES * K<T> + at < a.cols) {
+                if (inside(e * LANES * K<T> + at)) {
                     ring.copy(place, 0, e, dy + e * LANES * K<T>);
                     ring.copy(place, 1, e, x + e * LANES * K<T>);
                     if (DSUM) ring.copy(place, 2, e, dsum + e * LANES * K<T>);
@@ -401,7 +412,7 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
         if (kHeld && a.weight && group == 0)
 #pragma unroll
             for (uint32_t e = 0; e < VECS; ++e)
-                if (e * LANES * K<T> + at < a.cols) held.copy(0, e, a.weight, e * LANES * K<T> + at);
+                if (inside(e * LANES * K<T> + at)) held.copy(0, e, a.weight, e * LANES * K<T> + at);
         async::cp_async_commit();
         for (uint32_t i = 0; i < kAhead; ++i) fetch(ring.begin + i * ring.stage);
         if (kHeld && a.weight) {  // (the weights are the whole block's)
@@ -432,7 +443,7 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
         }
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e)
-            if (e * LANES * K<T> + at < a.cols) {
+            if (inside(e * LANES * K<T> + at)) {
                 float2 d[K<T> / 2], xh[K<T> / 2], g[K<T> / 2];
                 take(e, mean, rstd, d, xh, g);
 #pragma unroll
@@ -446,7 +457,7 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e) {
             const uint32_t col = e * LANES * K<T> + at;
-            if (col < a.cols) {
+            if (inside(col)) {
                 float2 d[K<T> / 2], xh[K<T> / 2], g[K<T> / 2];
                 take(e, mean, rstd, d, xh, g);
 #pragma unroll
@@ -527,9 +538,12 @@ int forward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormArgs &a, bool w
     const uint64_t fill = (uint64_t)ctx->sm_count * blocks;
     NormArgs b = a;
     void *args[] = {&b, &w16};
-    const void *k = vec ? (const void *)k_norm_rows<T, LANES, VECS, true> : (const void *)k_norm_rows<T, LANES, VECS, false>;
-    static Allowed allowed[2];
-    if (const int rc = allowed[vec].set(k, ctx->device, bytes, "layer norm")) return rc;
+    const void *k = !vec                                ? (const void *)k_norm_rows<T, LANES, VECS, Reach::elements>
+                    : a.cols == LANES * VECS * K<T> ? (const void *)k_norm_rows<T, LANES, VECS, Reach::whole>
+                                                    : (const void *)k_norm_rows<T, LANES, VECS, Reach::vectors>;
+    const uint32_t which = !vec ? 0 : a.cols == LANES * VECS * K<T> ? 2 : 1;
+    static Allowed allowed[3];
+    if (const int rc = allowed[which].set(k, ctx->device, bytes, "layer norm")) return rc;
     return launch(k, dim3((uint32_t)std::min(units, fill)), kThreads, bytes, s, args, "layer norm");
 }
 
@@ -566,9 +580,14 @@ int backward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormGradArgs &a, b
     if (part) bytes = std::max<uint32_t>(bytes, kGroups * 2 * VECS * K<T> * (LANES + 32 / K<T>) * 4);
     NormGradArgs b = a;
     void *args[] = {&b, &w16, &part};
-    const void *k = vec ? (const void *)k_norm_rows_grad<T, LANES, VECS, true, DSUM> : (const void *)k_norm_rows_grad<T, LANES, VECS, false, DSUM>;
-    static Allowed allowed[2];
-    if (const int rc = allowed[vec].set(k, ctx->device, bytes, "layer norm gradient")) return rc;
+    // (a warp's rows are not asked for as a whole: its registers would not hold what is then loaded ahead)
+    constexpr Reach kWhole = LANES > 32 ? Reach::whole : Reach::vectors;
+    const uint32_t which = !vec ? 0 : a.cols == LANES * VECS * K<T> ? 2 : 1;
+    const void *k = which == 0   ? (const void *)k_norm_rows_grad<T, LANES, VECS, Reach::elements, DSUM>
+                    : which == 1 ? (const void *)k_norm_rows_grad<T, LANES, VECS, Reach::vectors, DSUM>
+                                 : (const void *)k_norm_rows_grad<T, LANES, VECS, kWhole, DSUM>;
+    static Allowed allowed[3];
+    if (const int rc = allowed[which].set(k, ctx->device, bytes, "layer norm gradient")) return rc;
     return launch(k, dim3(blocks), kThreads, bytes, s, args, "layer norm gradient");
 }
 
