@@ -56,27 +56,37 @@ def workspace(ctx: F.Context, rows: int, cols: int):
     return torch.empty(max(work_bytes(ctx, rows, cols), 16), dtype=torch.uint8, device="cuda:%d" % ctx.device)
 
 
-def _weights(shape: tuple, dt: Any, dev: Any, *named: tuple) -> tuple:
-    """The element type of weight, bias or their gradients (that of the rows, or
-    fp32, the same for all that are given) and their addresses."""
-    wt, at = dt, []
-    for t, _ in named:
-        if t is not None:
-            wt = t.dtype
-            break
-    if wt != dt and wt != torch.float32:
-        raise ValueError("weights of %s: %s or float32 expected" % (wt, dt))
-    for t, name in named:
-        at.append(0 if t is None else AD._whole(t, shape, wt, dev, name))
-    return AD._dtype(wt), at
+def _weight_type(dt: Any, first: Any) -> Any:
+    """The element type of weight, bias and their gradients: that of the rows, or fp32."""
+    if first is None or first.dtype is dt:
+        return dt
+    if first.dtype is not torch.float32:
+        raise ValueError("weights of %s: %s or float32 expected" % (first.dtype, dt))
+    return torch.float32
+
+
+def _vector(t: Any, shape: tuple, dt: Any, dev: Any, name: str) -> int:
+    return 0 if t is None else AD._whole(t, shape, dt, dev, name)
+
+
+def _rows(t: Any, shape: tuple, dt: Any, dev: Any, name: str) -> tuple:
+    """Address and row stride of a matrix (or of none)."""
+    if t is None:
+        return 0, 0
+    if t.dtype is dt and t.shape == shape and t.device == dev:
+        row, col = t.stride()
+        if col == 1 or shape[1] == 1:
+            return t.data_ptr(), row if shape[0] > 1 else shape[1]
+    AD._refuse(t, shape, dt, dev, name)
 
 
 def _shape(x: Any, name: str) -> tuple:
     if x.dim() != 2:
         raise ValueError("%s [rows][cols] expected" % name)
-    if not 1 <= x.shape[1] <= MAX_COLS:
+    shape = x.shape
+    if not 1 <= shape[1] <= MAX_COLS:
         raise ValueError("%s: 1 to %d columns expected" % (name, MAX_COLS))
-    return x.shape
+    return shape
 
 
 def layer_norm(ctx: F.Context, x, out, weight=None, bias=None, eps: float = 1e-5, residual=None,
@@ -87,16 +97,15 @@ def layer_norm(ctx: F.Context, x, out, weight=None, bias=None, eps: float = 1e-5
     shape = _shape(x, "x")
     dt, dev, f32 = x.dtype, AD._device(ctx), torch.float32
     rows, cols = shape
-    wt, (pw, pb) = _weights((cols,), dt, dev, (weight, "weight"), (bias, "bias"))
-    call = _call(rows, cols, AD._dtype(dt), wt, 0, eps, pw, pb,
-                 x.data_ptr(), AD._matrix(x, shape, dt, dev, "x"),
-                 *((0, 0) if residual is None else (residual.data_ptr(), AD._matrix(residual, shape, dt, dev, "residual"))),
-                 out.data_ptr(), AD._matrix(out, shape, dt, dev, "out"),
-                 *((0, 0) if sum is None else (sum.data_ptr(), AD._matrix(sum, shape, dt, dev, "sum"))),
-                 0 if mean is None else AD._whole(mean, (rows,), f32, dev, "mean"),
-                 0 if rstd is None else AD._whole(rstd, (rows,), f32, dev, "rstd")) \
-        + (_no_dropout if dropout is None else dropout._spec)
-    rc = lib().fiona_layer_norm(ctx.handle, AD._handle(stream), call)
+    wt, per_col, per_row = _weight_type(dt, bias if weight is None else weight), (cols,), (rows,)
+    px, ldx = _rows(x, shape, dt, dev, "x")
+    pr, ldr = _rows(residual, shape, dt, dev, "residual")
+    po, ldo = _rows(out, shape, dt, dev, "out")
+    ps, lds = _rows(sum, shape, dt, dev, "sum")
+    call = _call(rows, cols, AD._dtype(dt), AD._dtype(wt), 0, eps, _vector(weight, per_col, wt, dev, "weight"),
+                 _vector(bias, per_col, wt, dev, "bias"), px, ldx, pr, ldr, po, ldo, ps, lds, _vector(mean, per_row, f32, dev, "mean"),
+                 _vector(rstd, per_row, f32, dev, "rstd")) + (_no_dropout if dropout is None else dropout._spec)
+    rc = (_lib or lib()).fiona_layer_norm(ctx.handle, AD._handle(stream), call)
     if rc:
         F._check(rc, "fiona_layer_norm")
 
@@ -111,16 +120,17 @@ def layer_norm_backward(ctx: F.Context, dy, sum, mean, rstd, dx=None, weight=Non
     shape = _shape(dy, "dy")
     dt, dev, f32 = dy.dtype, AD._device(ctx), torch.float32
     rows, cols = shape
-    wt, (pw, pdw, pdb) = _weights((cols,), dt, dev, (weight, "weight"), (dweight, "dweight"), (dbias, "dbias"))
-
-    def matrix(t, name):
-        return (0, 0) if t is None else (t.data_ptr(), AD._matrix(t, shape, dt, dev, name))
-
-    pwork, nwork = (0, 0) if work is None else (AD._workspace(work, dev), work.nbytes)
-    call = _grad_call(rows, cols, AD._dtype(dt), wt, 0, pw, *matrix(dy, "dy"), *matrix(sum, "sum"),
-                      AD._whole(mean, (rows,), f32, dev, "mean"), AD._whole(rstd, (rows,), f32, dev, "rstd"),
-                      *matrix(dsum, "dsum"), *matrix(dx, "dx"), *matrix(dresidual, "dresidual"), pdw, pdb, pwork, nwork) \
+    wt, per_col, per_row = _weight_type(dt, next((t for t in (weight, dweight, dbias) if t is not None), None)), (cols,), (rows,)
+    pw, nw = (0, 0) if work is None else (AD._workspace(work, dev), work.nbytes)
+    py, ldy = _rows(dy, shape, dt, dev, "dy")
+    ps, lds = _rows(sum, shape, dt, dev, "sum")
+    pd, ldd = _rows(dsum, shape, dt, dev, "dsum")
+    px, ldx = _rows(dx, shape, dt, dev, "dx")
+    pr, ldr = _rows(dresidual, shape, dt, dev, "dresidual")
+    call = _grad_call(rows, cols, AD._dtype(dt), AD._dtype(wt), 0, _vector(weight, per_col, wt, dev, "weight"), py, ldy, ps, lds,
+                      AD._whole(mean, per_row, f32, dev, "mean"), AD._whole(rstd, per_row, f32, dev, "rstd"), pd, ldd, px, ldx, pr, ldr,
+                      _vector(dweight, per_col, wt, dev, "dweight"), _vector(dbias, per_col, wt, dev, "dbias"), pw, nw) \
         + (_no_dropout if dropout is None else dropout._spec)
-    rc = lib().fiona_layer_norm_backward(ctx.handle, AD._handle(stream), call)
+    rc = (_lib or lib()).fiona_layer_norm_backward(ctx.handle, AD._handle(stream), call)
     if rc:
         F._check(rc, "fiona_layer_norm_backward")
