@@ -139,6 +139,55 @@ def test_gradient_against_differences(ctx, cols):
         assert abs(slope - (f64(g[grad]) * d).sum()) <= 1e-4 * np.abs(f64(g[grad]) * d).sum() ** 0.5 * max(1.0, abs(slope)) ** 0.5 + 1e-4
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("p", [0.0, 2.0 ** -18, 0.5, 0.999, 1.0])
+def test_probabilities(ctx, dtype, p):
+    """Masks that keep everything, little and nothing, on rows with and without whole vectors."""
+    for cols in (100, 1024, 777, 17000):
+        x, res, dy = make(9, cols, dtype, 0, 1), make(9, cols, dtype, 0, 2), make(9, cols, dtype, 0, 3)
+        drop = AD.Dropout(p, 5, 1 << 33)
+        got = run_forward(ctx, x, res, None, None, 1e-5, drop)
+        check_all(dtype, dtype, got, NU.forward(f64(x), f64(res), None, None, 1e-5, spec(drop)))
+        g = {"dx": torch.empty_like(x), "dresidual": torch.empty_like(x)}
+        LN.layer_norm_backward(ctx, dy, got["sum"], got["mean"], got["rstd"], dropout=drop, work=LN.workspace(ctx, 9, cols), **g)
+        check_all(dtype, dtype, g, NU.backward(f64(dy), f64(got["sum"]), f64(got["mean"]), f64(got["rstd"]), None, None, spec(drop)))
+        if p == 1.0:
+            assert (g["dx"] == 0).all() and torch.equal(got["sum"], res)
+        if p < 2.0 ** -17:
+            assert torch.equal(g["dx"], g["dresidual"])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("cols", [256, 768, 2048, 4096, 8192, 16384])
+def test_strides_and_alignment_change_nothing(ctx, dtype, cols):
+    """Rows apart, rows and weights off 16 bytes: the same results, to the last bit, as whole
+    vectors side by side."""
+    rows = 21
+    src = [make(rows, cols, dtype, 0, i) for i in range(4)]
+    weight, bias, drop = vector(cols, "f32", 5, 0.2, 1.0), vector(cols, "f32", 6), AD.Dropout(0.3, 2)
+    work, results = LN.workspace(ctx, rows, cols), []
+    for off, extra, weights_off in ((0, 0, 0), (16, 64, 0), (3, 6, 0), (0, 0, 1), (5, 7, 3)):
+        def place(t):
+            wide = torch.zeros(rows, cols + extra, dtype=t.dtype, device="cuda")
+            wide[:, off:off + cols] = t
+            return wide[:, off:off + cols]
+
+        def shifted(t):
+            flat = torch.zeros(cols + weights_off, device="cuda")
+            flat[weights_off:] = t
+            return flat[weights_off:]
+
+        x, res, dy, dsum = (place(t) for t in src)
+        w, b = shifted(weight), shifted(bias)
+        f = {"out": place(src[0]), "sum": place(src[0]), "mean": torch.empty(rows, device="cuda"), "rstd": torch.empty(rows, device="cuda")}
+        LN.layer_norm(ctx, x, f["out"], weight=w, bias=b, residual=res, dropout=drop, sum=f["sum"], mean=f["mean"], rstd=f["rstd"])
+        g = {"dx": place(src[0]), "dresidual": place(src[0]), "dweight": torch.empty(cols, device="cuda"), "dbias": torch.empty(cols, device="cuda")}
+        LN.layer_norm_backward(ctx, dy, f["sum"], f["mean"], f["rstd"], weight=w, dsum=dsum, dropout=drop, work=work, **g)
+        results.append({**f, **g})
+    for r in results[1:]:
+        assert all(torch.equal(r[k], results[0][k]) for k in r)
+
+
 def test_in_place_and_neighbours(ctx):
     for dtype in DT:
         for cols in (96, 100, 1024, 18000):
@@ -299,3 +348,45 @@ def test_streams_and_graphs(ctx):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(new, held))
     assert not torch.equal(new[0], want[0])
+
+
+FIRST_CALLS = """
+import sys
+sys.path[:0] = [%r]
+import torch
+from paper_2609_35352_gb300 import adapters as AD, fiona as F, layernorm as LN, optim as O, workloads as W
+ctx = F.Context(1024, W.ntt_primes(1024, 50, 1), device=0)
+x, w = torch.randn(300, 4096, device="cuda").bfloat16(), torch.ones(4096, device="cuda")
+out, total, dx, dw = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x), torch.empty_like(w)
+mean, rstd, work = torch.empty(300, device="cuda"), torch.empty(300, device="cuda"), LN.workspace(ctx, 300, 4096)
+p, g = torch.randn(2000000, device="cuda").bfloat16(), torch.randn(2000000, device="cuda").bfloat16()
+opts = [O.AdamW(ctx, [p.clone()], [g], state_bits=b, max_norm=1.0) for b in (8, 32)]
+torch.cuda.synchronize()
+def calls():
+    s = torch.cuda.current_stream()
+    LN.layer_norm(ctx, x, out, weight=w, dropout=AD.Dropout(0.1, 1), sum=total, mean=mean, rstd=rstd, stream=s)
+    LN.layer_norm_backward(ctx, x, total, mean, rstd, weight=w, dx=dx, dweight=dw, work=work, stream=s)
+    for o in opts:
+        o.step(stream=s)
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    calls()
+graph.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (out, dx, dw)]
+assert [o.steps.tolist() for o in opts] == [[1], [1]]
+calls()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (out, dx, dw)))
+print("well")
+"""
+
+
+def test_first_calls_in_a_capture(ctx):
+    """A program whose very first calls are captured ones."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS % root], capture_output=True, text=True, timeout=300, cwd=root)
+    assert r.returncode == 0 and "well" in r.stdout, r.stderr[-2000:]
