@@ -168,37 +168,46 @@ struct Ring {
     }
 };
 
-// A row's weights (and biases) in shared memory, as they lie: [2][VECS][parts][LANES].
+// A row's weights (and biases) in shared memory, [2][VECS][parts][LANES].
 // For rows of several warps: from global memory they would come out of L2 for every row,
 // since the rows ahead take L1's room (16384 x 4096 bf16, two rows in flight: 103 us for
 // 96).  They come by way of L1: copies past it of the same lines by every block go to a
 // few slices of L2 (2048 x 1024 fp32, each warp its own copy: 49 us for 6.5).
+constexpr bool wide_weights(uint32_t cols, uint32_t size) { return size == 4 || cols <= 4096; }  // (backward; more: no room beside the rows)
 constexpr bool held_weights(uint32_t lanes) { return lanes >= 128 && lanes <= 512; }  // (forward; 1024: no room beside the rows)
 
-template <typename T, uint32_t VECS, uint32_t LANES>
+// WIDE: in fp32 whatever they are, so that no row widens them again (backward, which takes
+// them twice: 97 us for 103 on 16384 x 4096 bf16; forward they would take a block's room
+// on an SM up to 2048 columns, 99 us for 84).
+template <typename T, uint32_t VECS, uint32_t LANES, bool WIDE>
 struct Held {
     uint4 *at;
-    bool w16;
-    uint32_t parts;  // 16 bytes each of K weights
-    __device__ __forceinline__ Held(uint4 *place, bool w16) : at(place + threadIdx.x % LANES), w16(w16 || sizeof(T) == 4), parts(this->w16 ? 1 : 2) {}
-    static uint32_t bytes(bool w16) { return VECS * (w16 || sizeof(T) == 4 ? 1 : 2) * LANES * 16; }  // of weights or biases
-    __device__ __forceinline__ void copy(uint32_t which, uint32_t e, const void *p, uint32_t col) const
+    bool raw;  // as they lie, 16 bits each
+    __device__ __forceinline__ Held(uint4 *place, bool w16) : at(place + threadIdx.x % LANES), raw(!WIDE && w16 && sizeof(T) == 2) {}
+    static constexpr uint32_t kParts = K<T> / 4;  // 16 bytes each of K weights in fp32
+    static uint32_t bytes(bool w16) { return VECS * (!WIDE && w16 && sizeof(T) == 2 ? 1 : kParts) * LANES * 16; }  // of weights or biases
+    __device__ __forceinline__ void put(uint32_t which, uint32_t e, const void *p, bool w16, uint32_t col) const
     {
-        const uint4 *from = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p) + (size_t)col * (w16 ? sizeof(T) : 4));
-        for (uint32_t i = 0; i < parts; ++i)
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(async::smem_addr(at + ((which * VECS + e) * parts + i) * LANES)), "l"(from + i) : "memory");
+        if (raw) {
+            at[(which * VECS + e) * LANES] = *reinterpret_cast<const uint4 *>((const T *)p + col);
+        } else {
+            float2 v[K<T> / 2];
+            load_weights<T, true>(p, w16, col, K<T>, 0.f, v);
+#pragma unroll
+            for (uint32_t k = 0; k < kParts; ++k)
+                reinterpret_cast<float4 *>(at)[((which * VECS + e) * kParts + k) * LANES] = make_float4(v[2 * k].x, v[2 * k].y, v[2 * k + 1].x, v[2 * k + 1].y);
+        }
     }
     __device__ __forceinline__ void read(uint32_t which, uint32_t e, float2 (&v)[K<T> / 2]) const
     {
-        if (w16) {
+        if (raw) {
             const Vector<T> x{at[(which * VECS + e) * LANES]};
             x.widened(v);
         } else {
 #pragma unroll
-            for (uint32_t k = 0; k < K<T> / 4; ++k) {
-                const Vector<float> x{at[((which * VECS + e) * 2 + k) * LANES]};
-#pragma unroll
-                for (uint32_t i = 0; i < 2; ++i) v[2 * k + i] = make_float2(x.values()[2 * i], x.values()[2 * i + 1]);
+            for (uint32_t k = 0; k < kParts; ++k) {
+                const float4 f = reinterpret_cast<const float4 *>(at)[((which * VECS + e) * kParts + k) * LANES];
+                v[2 * k] = make_float2(f.x, f.y), v[2 * k + 1] = make_float2(f.z, f.w);
             }
         }
     }
@@ -256,7 +265,7 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
     Rows ring(smem, a.res || !VEC ? 2 : 1);
     constexpr uint32_t kAhead = Rows::stages;
     constexpr bool kHeld = VEC && held_weights(LANES);
-    const Held<T, VECS, LANES> held(ring.behind(), w16);
+    const Held<T, VECS, LANES, false> held(ring.behind(), w16);
     const float per = 1.f / (float)a.cols;
     // whether the row reaches to this thread's vector from column `col` on
     auto inside = [&](uint32_t col) { return REACH == Reach::whole || col < a.cols; };
@@ -279,13 +288,14 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
         next_t += step, x += step_x, res += step_res;
     };
     if (VEC) {
+        for (uint32_t i = 0; i < kAhead; ++i) fetch(ring.begin + i * ring.stage);
+        // (each thread its own columns')
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e)
             if (kHeld && inside(e * LANES * K<T> + at)) {
-                if (a.weight) held.copy(0, e, a.weight, e * LANES * K<T> + at);
-                if (a.bias) held.copy(1, e, a.bias, e * LANES * K<T> + at);
+                if (a.weight) held.put(0, e, a.weight, w16, e * LANES * K<T> + at);
+                if (a.bias) held.put(1, e, a.bias, w16, e * LANES * K<T> + at);
             }
-        for (uint32_t i = 0; i < kAhead; ++i) fetch(ring.begin + i * ring.stage);  // (the weights with the first row)
     }
     for (; t < rows; t += step, out += step_out, total += step_sum, z += step_z) {
         float2 s[VECS][K<T> / 2], sum = both(0.f);
@@ -383,7 +393,7 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
     Rows ring(smem, kTensors);
     constexpr uint32_t kAhead = Rows::stages;
     constexpr bool kHeld = VEC && held_grad_weights(LANES * VECS * K<T>, sizeof(T));
-    const Held<T, VECS, LANES> held(ring.behind(), w16);
+    const Held<T, VECS, LANES, wide_weights(LANES * VECS * K<T>, sizeof(T))> held(ring.behind(), w16);
     const float per = 1.f / (float)a.cols;
     // whether the row reaches to this thread's vector from column `col` on
     auto inside = [&](uint32_t col) { return REACH == Reach::whole || col < a.cols; };
@@ -409,14 +419,12 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
         next_t += step, dy += step_dy, x += step_x, dsum += step_ds;
     };
     if (VEC) {
-        if (kHeld && a.weight && group == 0)
-#pragma unroll
-            for (uint32_t e = 0; e < VECS; ++e)
-                if (inside(e * LANES * K<T> + at)) held.copy(0, e, a.weight, e * LANES * K<T> + at);
-        async::cp_async_commit();
         for (uint32_t i = 0; i < kAhead; ++i) fetch(ring.begin + i * ring.stage);
-        if (kHeld && a.weight) {  // (the weights are the whole block's)
-            async::cp_async_wait<kAhead>();
+        if (kHeld && a.weight) {
+            if (group == 0)
+#pragma unroll
+                for (uint32_t e = 0; e < VECS; ++e)
+                    if (inside(e * LANES * K<T> + at)) held.put(0, e, a.weight, w16, e * LANES * K<T> + at);
             __syncthreads();
         }
     }
@@ -531,7 +539,7 @@ int forward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormArgs &a, bool w
     const bool one = a.rows == 1;  // (one row has no stride)
     const bool vec = vectors(a.cols, K<T>, {a.x, a.res, a.out, a.sum, a.weight, a.bias},
                              {one ? 0 : a.ldx * z, one || !a.res ? 0 : a.ld_res * z, one ? 0 : a.ld_out * z, one || !a.sum ? 0 : a.ld_sum * z});
-    const uint32_t bytes = (vec ? (a.res ? 2 : 1) * Rows::stages : 2) * Rows::tensor * 16 + (vec && held_weights(LANES) && (a.weight || a.bias) ? 2 * Held<T, VECS, LANES>::bytes(w16) : 0);
+    const uint32_t bytes = (vec ? (a.res ? 2 : 1) * Rows::stages : 2) * Rows::tensor * 16 + (vec && held_weights(LANES) && (a.weight || a.bias) ? 2 * Held<T, VECS, LANES, false>::bytes(w16) : 0);
     const uint64_t units = (a.rows + kGroups - 1) / kGroups;
     // as many blocks as run at once: 1024 threads an SM, if their rows have room
     const uint32_t blocks = std::max(1u, std::min(1024 / kThreads, bytes ? 220 * 1024 / (bytes + 1536) : 32u));
@@ -576,7 +584,7 @@ int backward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormGradArgs &a, b
     const bool vec = vectors(a.cols, K<T>, {a.dy, a.sum, a.dsum, a.dx, a.dres, a.weight},
                              {one ? 0 : a.ld_dy * z, one ? 0 : a.ld_sum * z, one || !a.dsum ? 0 : a.ld_dsum * z, one || !a.dx ? 0 : a.ld_dx * z,
                               one || !a.dres ? 0 : a.ld_dres * z});
-    uint32_t bytes = kTensors * Rows::tensor * 16 * (vec ? Rows::stages : 1) + (vec && kHeld && a.weight ? Held<T, VECS, LANES>::bytes(w16) : 0);
+    uint32_t bytes = kTensors * Rows::tensor * 16 * (vec ? Rows::stages : 1) + (vec && kHeld && a.weight ? Held<T, VECS, LANES, wide_weights(LANES * VECS * K<T>, sizeof(T))>::bytes(w16) : 0);
     if (part) bytes = std::max<uint32_t>(bytes, kGroups * 2 * VECS * K<T> * (LANES + 32 / K<T>) * 4);
     NormGradArgs b = a;
     void *args[] = {&b, &w16, &part};
