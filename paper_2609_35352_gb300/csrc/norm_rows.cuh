@@ -168,13 +168,16 @@ struct Ring {
     }
 };
 
-// A row's weights (and biases) in shared memory, [2][VECS][parts][LANES].
-// For rows of several warps: from global memory they would come out of L2 for every row,
-// since the rows ahead take L1's room (16384 x 4096 bf16, two rows in flight: 103 us for
-// 96).  They come by way of L1: copies past it of the same lines by every block go to a
-// few slices of L2 (2048 x 1024 fp32, each warp its own copy: 49 us for 6.5).
+// A row's weights (and biases) in shared memory, [2][VECS][parts][LANES].  From global
+// memory they would come out of L2 for every row, since the rows ahead take L1's room
+// (16384 x 4096 bf16, two rows in flight: 103 us for 96).  They come by way of L1: copies
+// past it of the same lines by every block go to a few slices of L2 (2048 x 1024 fp32, each
+// warp its own copy: 49 us for 6.5).  WIDE: in fp32 whatever they are, so that no row
+// widens them again: backward, which takes them twice (97 us for 103 on 16384 x 4096
+// bf16), and forward for rows of a warp or two (65536 x 1024 bf16 with dropout 90 us for
+// 101); above they would take a block's room on an SM (2048 columns 99 us for 84).
 constexpr bool wide_weights(uint32_t cols, uint32_t size) { return size == 4 || cols <= 4096; }  // (backward; more: no room beside the rows)
-constexpr bool held_weights(uint32_t lanes) { return lanes >= 128 && lanes <= 512; }  // (forward; 1024: no room beside the rows)
+constexpr bool held_weights(uint32_t lanes) { return lanes <= 512; }  // (forward; 1024: no room beside the rows)
 
 // WIDE: in fp32 whatever they are, so that no row widens them again (backward, which takes
 // them twice: 97 us for 103 on 16384 x 4096 bf16; forward they would take a block's room
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
     Rows ring(smem, a.res || !VEC ? 2 : 1);
     constexpr uint32_t kAhead = Rows::stages;
     constexpr bool kHeld = VEC && held_weights(LANES);
-    const Held<T, VECS, LANES, false> held(ring.behind(), w16);
+    const Held<T, VECS, LANES, (LANES < 128)> held(ring.behind(), w16);
     const float per = 1.f / (float)a.cols;
     // whether the row reaches to this thread's vector from column `col` on
     auto inside = [&](uint32_t col) { return REACH == Reach::whole || col < a.cols; };
@@ -289,13 +292,14 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
     };
     if (VEC) {
         for (uint32_t i = 0; i < kAhead; ++i) fetch(ring.begin + i * ring.stage);
-        // (each thread its own columns')
+        if (kHeld && (kGroups == 1 || threadIdx.x < LANES))
 #pragma unroll
-        for (uint32_t e = 0; e < VECS; ++e)
-            if (kHeld && inside(e * LANES * K<T> + at)) {
-                if (a.weight) held.put(0, e, a.weight, w16, e * LANES * K<T> + at);
-                if (a.bias) held.put(1, e, a.bias, w16, e * LANES * K<T> + at);
-            }
+            for (uint32_t e = 0; e < VECS; ++e)
+                if (inside(e * LANES * K<T> + at)) {
+                    if (a.weight) held.put(0, e, a.weight, w16, e * LANES * K<T> + at);
+                    if (a.bias) held.put(1, e, a.bias, w16, e * LANES * K<T> + at);
+                }
+        if (kHeld && kGroups > 1) __syncthreads();  // (else each thread has its own columns')
     }
     for (; t < rows; t += step, out += step_out, total += step_sum, z += step_z) {
         float2 s[VECS][K<T> / 2], sum = both(0.f);
@@ -539,7 +543,7 @@ int forward_rows(const fiona_ctx *ctx, cudaStream_t s, const NormArgs &a, bool w
     const bool one = a.rows == 1;  // (one row has no stride)
     const bool vec = vectors(a.cols, K<T>, {a.x, a.res, a.out, a.sum, a.weight, a.bias},
                              {one ? 0 : a.ldx * z, one || !a.res ? 0 : a.ld_res * z, one ? 0 : a.ld_out * z, one || !a.sum ? 0 : a.ld_sum * z});
-    const uint32_t bytes = (vec ? (a.res ? 2 : 1) * Rows::stages : 2) * Rows::tensor * 16 + (vec && held_weights(LANES) && (a.weight || a.bias) ? 2 * Held<T, VECS, LANES, false>::bytes(w16) : 0);
+    const uint32_t bytes = (vec ? (a.res ? 2 : 1) * Rows::stages : 2) * Rows::tensor * 16 + (vec && held_weights(LANES) && (a.weight || a.bias) ? 2 * Held<T, VECS, LANES, (LANES < 128)>::bytes(w16) : 0);
     const uint64_t units = (a.rows + kGroups - 1) / kGroups;
     // as many blocks as run at once: 1024 threads an SM, if their rows have room
     const uint32_t blocks = std::max(1u, std::min(1024 / kThreads, bytes ? 220 * 1024 / (bytes + 1536) : 32u));
