@@ -35,11 +35,16 @@
  * master (optional): fp32 [places], the weights that 16-bit tensors are rounded from;
  * then their own tensors are written, but not read.  fp32 tensors do not use theirs.
  *
- * Arithmetic: fp32, from gradients in the weights' type; beta^t from t log beta in fp64.  A weight
- * is rounded once (to nearest).  A norm is summed in fp32 by pieces of 1024 elements and
- * in fp64 from there; a sum of squares that passes fp32's range (a norm above
- * 1.8e19) counts as infinite.  Results do not depend on the order in which blocks run:
- * no atomics on values.
+ * Arithmetic: fp32, from gradients in the weights' type; beta^t from t log beta in fp64.
+ * A weight is rounded once (to nearest).  A norm is summed in two fp32 parts, as good as
+ * from fp64; where squares or their sums pass fp32's range (a norm above 1.8e19) it counts
+ * as infinite.  Codes are those of the formulas step by step, each product, sum, quotient
+ * and root rounded to nearest by itself:
+ *   m = beta1 m + (1 - beta1) (k g),  v = beta2 v + (1 - beta2) ((k g) (k g)),  u = sqrt(v),
+ *   q = rint(sqrt(top^2 (|m| / scale) - 1/4)) with top 127, or u in the place of |m| with
+ *   255, and back (q |q|) (scale (1 / 127^2)),
+ * so that a value on the border of two codes comes out on one side everywhere.  Results do
+ * not depend on the order in which blocks run: no atomics on values.
  *
  * Errors, ownership, streams and devices as in fiona.h.  Calls on one optimizer have
  * to follow one another (one stream, or streams that wait): it owns scratch of its own,

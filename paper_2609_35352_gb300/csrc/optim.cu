@@ -29,6 +29,9 @@ constexpr uint32_t kPairs = kBlock / 64;  // pairs of elements of a block that a
 constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: largest values below count as zero
 
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+// A sum whose terms may be products just rounded: one by one, as sums of pairs are fused with
+// products of pairs (compilers do it to the intrinsics, whatever their names say).
+__device__ __forceinline__ float2 sum_apart(float2 a, float2 b) { return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)); }
 
 // Four elements as they lie, and as two pairs.
 template <typename T>
@@ -47,9 +50,48 @@ struct Four {
     }
 };
 
-// the sum of squares of a piece's gradients, added to eight sums
+// Sums of squares go in two parts, the second what the additions to the first have lost
+// (Kahan 1965 along a thread, Knuth's sum of two between threads), so that a norm and the
+// factor by which it clips are as good as from fp64, and codes in 8 bits do not go by the
+// order of a sum.  (fp64 itself does two additions a cycle on an SM here.)
+struct Pair {
+    float hi, lo;
+};
+__device__ __forceinline__ Pair sum_of(Pair a, Pair b)
+{
+    const float s = __fadd_rn(a.hi, b.hi), bb = __fsub_rn(s, a.hi);
+    if (s - s != 0.f) return {s, 0.f};  // (infinite, or NaN)
+    const float e = __fadd_rn(__fadd_rn(__fsub_rn(a.hi, __fsub_rn(s, bb)), __fsub_rn(b.hi, bb)), __fadd_rn(a.lo, b.lo));
+    const float hi = __fadd_rn(s, e);
+    return {hi, __fsub_rn(e, __fsub_rn(hi, s))};
+}
+__device__ __forceinline__ Pair warp_sum(Pair v)
+{
+#pragma unroll
+    for (uint32_t i = 16; i; i >>= 1) v = sum_of(v, Pair{__shfl_xor_sync(0xFFFFFFFFu, v.hi, i), __shfl_xor_sync(0xFFFFFFFFu, v.lo, i)});
+    return v;
+}
+// sums += x, the losses kept apart (negated)
+__device__ __forceinline__ void add_square(float2 &sum, float2 &lost, float2 v)
+{
+    const float2 x = __fadd2_rn(__fmul2_rn(v, v), make_float2(-lost.x, -lost.y)), s = __fadd2_rn(sum, x);
+    lost = __fadd2_rn(__fadd2_rn(s, make_float2(-sum.x, -sum.y)), make_float2(-x.x, -x.y));
+    sum = s;
+}
+
+// the same in one part
 template <typename T>
-__device__ __forceinline__ void squares(const AdamPiece &p, uint32_t lane, float2 (&s)[4])
+__device__ __forceinline__ float plain_squares(const AdamPiece &p, uint32_t lane)
+{
+    const T *g = (const T *)p.grad;
+    float s = 0.f;
+    for (uint32_t i = lane; i < p.count; i += 32) s = __fmaf_rn(widen(g[i]), widen(g[i]), s);
+    return s;
+}
+
+// the sum of squares of a piece's gradients, added to a thread's four sums
+template <typename T>
+__device__ __forceinline__ void squares(const AdamPiece &p, uint32_t lane, float2 (&s)[2], float2 (&lost)[2])
 {
     const T *g = (const T *)p.grad;
     if (p.aligned && p.count % kBlock == 0) {
@@ -60,46 +102,48 @@ __device__ __forceinline__ void squares(const AdamPiece &p, uint32_t lane, float
             const T *x = reinterpret_cast<const T *>(&u);
 #pragma unroll
             for (uint32_t j = 0; j < k; j += 2) {
-                const float2 v = make_float2(widen(x[j]), widen(x[j + 1]));
-                s[j / 2 % 4] = __ffma2_rn(v, v, s[j / 2 % 4]);
+                add_square(s[j / 2 % 2], lost[j / 2 % 2], make_float2(widen(x[j]), widen(x[j + 1])));
             }
         }
     } else {
-#pragma unroll 8
-        for (uint32_t i = lane; i < p.count; i += 32) {
-            const float v = widen(g[i]);
-            s[0].x = __fmaf_rn(v, v, s[0].x);
-        }
+#pragma unroll 4
+        for (uint32_t i = lane; i < p.count; i += 64)
+            add_square(s[0], lost[0], make_float2(widen(g[i]), i + 32 < p.count ? widen(g[i + 32]) : 0.f));
     }
 }
 
-__global__ void __launch_bounds__(kThreads) k_squares(const AdamPiece *pieces, const AdamRun *runs, uint32_t n, const uint8_t *active, float *out)
+__global__ void __launch_bounds__(kThreads) k_squares(const AdamPiece *pieces, const AdamRun *runs, uint32_t n, const uint8_t *active, Pair *out)
 {
     previous_done();
     next_may_start();
     const uint32_t at = blockIdx.x * kWarps + threadIdx.x / 32, lane = threadIdx.x & 31;
     if (at >= n) return;
     const AdamRun r = runs[at];
-    float2 s[4] = {};
+    float2 s[2] = {}, lost[2] = {};
     for (uint32_t i = r.begin; i < r.end; ++i) {
         const AdamPiece p = pieces[i];
         if (active && !active[p.group]) break;  // (all of a run are of one group)
         if (p.dtype == FIONA_F32)
-            squares<float>(p, lane, s);
+            squares<float>(p, lane, s, lost);
         else if (p.dtype == FIONA_F16)
-            squares<__half>(p, lane, s);
+            squares<__half>(p, lane, s, lost);
         else
-            squares<__nv_bfloat16>(p, lane, s);
+            squares<__nv_bfloat16>(p, lane, s, lost);
     }
-    float v = ((s[0].x + s[0].y) + (s[1].x + s[1].y)) + ((s[2].x + s[2].y) + (s[3].x + s[3].y));
-#pragma unroll
-    for (uint32_t i = 16; i; i >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, i);
+    Pair v = sum_of(sum_of(Pair{s[0].x, -lost[0].x}, Pair{s[0].y, -lost[0].y}), sum_of(Pair{s[1].x, -lost[1].x}, Pair{s[1].y, -lost[1].y}));
+    if (__any_sync(0xFFFFFFFFu, v.hi - v.hi != 0.f)) {  // (what an infinite sum has lost is NaN: which of the two is it?)
+        v = Pair{0.f, 0.f};
+        for (uint32_t i = r.begin; i < r.end; ++i)
+            v.hi += pieces[i].dtype == FIONA_F32   ? plain_squares<float>(pieces[i], lane)
+                    : pieces[i].dtype == FIONA_F16 ? plain_squares<__half>(pieces[i], lane) : plain_squares<__nv_bfloat16>(pieces[i], lane);
+    }
+    v = warp_sum(v);
     if (lane == 0) out[at] = v;
 }
 
 struct RateArgs {
     const AdamGroup *groups;
-    const float *squares;  // null: no norms
+    const Pair *squares;  // null: no norms
     const uint8_t *active;
     const float *lr;
     int64_t *steps;
@@ -108,16 +152,23 @@ struct RateArgs {
     uint32_t n, skip;
 };
 
-__device__ __forceinline__ void set_rate(const RateArgs &a, uint32_t i, double square)
+__device__ __forceinline__ void set_rate(const RateArgs &a, uint32_t i, Pair square)
 {
     const AdamGroup g = a.groups[i];
     AdamRate r{};
     r.clip = 1.f;
     r.live = !a.active || a.active[i];
     if (a.squares) {
-        const float norm = sqrtf((float)square);
+        // the root, and the quotient by it, with what their first parts leave over
+        const float root = __fsqrt_rn(square.hi);
+        const bool plain = !(root > 0.f && root <= 3.402823466e38f);
+        const float rest = plain ? 0.f : __fdiv_rn(__fadd_rn(__fmaf_rn(-root, root, square.hi), square.lo), 2.f * root);
+        const float norm = __fadd_rn(root, rest);
         a.norms[i] = norm;
-        if (norm > g.max_norm) r.clip = g.max_norm / norm;
+        if (norm > g.max_norm) {
+            const float q = __fdiv_rn(g.max_norm, root);
+            r.clip = plain ? q : __fadd_rn(q, __fdiv_rn(__fadd_rn(__fmaf_rn(-q, root, g.max_norm), __fmaf_rn(-q, rest, g.max_norm_rest)), root));
+        }
         if (a.skip && !(norm <= 3.402823466e38f)) r.live = 0;
     }
     if (r.live) {
@@ -139,34 +190,25 @@ __global__ void __launch_bounds__(kThreads) k_rates(const RateArgs a)
     previous_done();
     next_may_start();
     const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-    if (i < a.n) set_rate(a, i, 0.0);
+    if (i < a.n) set_rate(a, i, Pair{0.f, 0.f});
 }
 
-// With norms: a block a group, its runs' sums added up, eight at a time in fp32, in
-// fp64 from there (this device adds two numbers a cycle in fp64 on an SM).
+// with norms: a block a group, its runs' sums added up
 __global__ void __launch_bounds__(kRateThreads) k_norm_rates(const RateArgs a)
 {
-    __shared__ double part[kRateThreads];
+    __shared__ Pair part[kRateThreads / 32];
     next_may_start();
     previous_done();
     const AdamGroup &g = a.groups[blockIdx.x];
-    double s = 0.0;
-    for (uint32_t i = g.begin + threadIdx.x * 8; i < g.end; i += kRateThreads * 8) {
-        float v[8];
-#pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) v[k] = i + k < g.end ? a.squares[i + k] : 0.f;
-        s += (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
-    }
-    // (only so many threads as have something)
-    uint32_t n = 32;
-    while (n < kRateThreads && n * 8 < g.end - g.begin) n *= 2;
-    if (threadIdx.x < n) part[threadIdx.x] = s;
+    Pair s{0.f, 0.f};
+    for (uint32_t i = g.begin + threadIdx.x; i < g.end; i += kRateThreads) s = sum_of(s, a.squares[i]);
+    const uint32_t lane = threadIdx.x & 31;
+    s = warp_sum(s);
+    if (lane == 0) part[threadIdx.x / 32] = s;
     __syncthreads();
-    for (n /= 2; n; n /= 2) {
-        if (threadIdx.x < n) part[threadIdx.x] += part[threadIdx.x + n];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) set_rate(a, blockIdx.x, part[0]);
+    if (threadIdx.x >= 32) return;
+    s = warp_sum(part[lane]);
+    if (lane == 0) set_rate(a, blockIdx.x, s);
 }
 
 // The formulas by pairs of elements, each operation said outright, so that every path
@@ -213,7 +255,7 @@ struct StepArgs {
 };
 
 // Codes in 8 bits, four to a word.  To fp32 by a byte in the mantissa of 2^23, from fp32
-// by adding 1.5 2^23 (to nearest): conversions run at an eighth of the additions' rate.
+// by adding 1.5 2^23: conversions run at an eighth of the additions' rate.
 __device__ __forceinline__ float2 bytes_to_float(uint32_t word, uint32_t k, float bias)  // bytes k and k + 1
 {
     const uint32_t x = __byte_perm(word, 0x4B000000u, 0x7540 + k), y = __byte_perm(word, 0x4B000000u, 0x7541 + k);
@@ -221,11 +263,6 @@ __device__ __forceinline__ float2 bytes_to_float(uint32_t word, uint32_t k, floa
 }
 __device__ __forceinline__ float2 signed_codes(uint32_t word, uint32_t k) { return bytes_to_float(word ^ 0x80808080u, k, 128.f); }
 __device__ __forceinline__ float2 unsigned_codes(uint32_t word, uint32_t k) { return bytes_to_float(word, k, 0.f); }
-__device__ __forceinline__ uint32_t to_bytes(float2 a, float2 b)
-{
-    a = __fadd2_rn(a, both(12582912.f)), b = __fadd2_rn(b, both(12582912.f));
-    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
-}
 
 // The largest over a warp; not finite: NaN; below kTiny: 0.  (Bits of absolute values are
 // in their order, NaN above all.)
@@ -234,27 +271,83 @@ __device__ __forceinline__ float block_scale(float most)
     const uint32_t u = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most) & 0x7FFFFFFFu);
     return u >= 0x7F800000u ? __uint_as_float(0x7FFFFFFFu) : u < __float_as_uint(kTiny) ? 0.f : __uint_as_float(u);
 }
-// what a value is multiplied by for its code's square, TOP^2 at the scale
-template <uint32_t TOP>
-__device__ __forceinline__ float per_scale(float scale)
+// A root to nearest: one step of Newton's on the reciprocal root, its residual exact by an
+// fma (Markstein, IBM J. Res. Dev. 34, 1990).  What is below 2^-126 counts as zero.
+__device__ __forceinline__ float2 roots(float2 v)
 {
-    float r;  // (of the largest scales: below 2^-126)
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(scale));
-    return scale == 0.f ? 0.f : __fmul_rn((float)(TOP * TOP), r);
+    float2 s, r, y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, 1.17549435e-38f)));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(v.y, 1.17549435e-38f)));
+    asm("mul.rn.ftz.f32 %0, %1, %2;" : "=f"(s.x) : "f"(v.x), "f"(y.x));
+    asm("mul.rn.ftz.f32 %0, %1, %2;" : "=f"(s.y) : "f"(v.y), "f"(y.y));
+    asm("fma.rn.ftz.f32 %0, %1, %2, %3;" : "=f"(r.x) : "f"(-s.x), "f"(s.x), "f"(v.x));
+    asm("fma.rn.ftz.f32 %0, %1, %2, %3;" : "=f"(r.y) : "f"(-s.y), "f"(s.y), "f"(v.y));
+    return __ffma2_rn(r, __fmul2_rn(y, both(0.5f)), s);
 }
 
-// The nearest of q^2, as q not rounded yet: two squares' middle is (q + 1/2)^2 + 1/4, so
-// that q is sqrt(x - 1/4) to nearest.  NaN gives 0.
-__device__ __forceinline__ float2 codes_m(float2 m, float per)
+// Codes are what the formulas give step by step, each operation rounded to nearest: the
+// share of the block's largest, times TOP^2, less 1/4 (two squares' middle is (q + 1/2)^2 +
+// 1/4), its root, and that to nearest.  A value on the border of two codes so comes out on
+// one side, whichever kernel or program makes the code.  The quotient by the scale: its
+// reciprocal, rounded once a block, and the remainder by an fma (Markstein).
+struct Scale {
+    float2 reciprocal, minus;
+    __device__ __forceinline__ explicit Scale(float s)
+    {
+        reciprocal = both(s == 0.f ? 0.f : __frcp_rn(s));
+        minus = both(-s);
+    }
+};
+template <uint32_t TOP>
+__device__ __forceinline__ float2 squared_codes(float2 magnitude, const Scale &s)
 {
-    return make_float2(copysignf(root_approx(fmaxf(__fmaf_rn(fabsf(m.x), per, -0.25f), 0.f)), m.x),
-                       copysignf(root_approx(fmaxf(__fmaf_rn(fabsf(m.y), per, -0.25f), 0.f)), m.y));
+    const float2 x = __fmul2_rn(magnitude, s.reciprocal);
+    const float2 share = __ffma2_rn(__ffma2_rn(x, s.minus, magnitude), s.reciprocal, x);
+    return sum_apart(__fmul2_rn(share, both((float)(TOP * TOP))), both(-0.25f));
 }
-// (u above zero: code 1 at least)
-__device__ __forceinline__ float2 codes_u(float2 u, float per)
+__device__ __forceinline__ float2 squared_codes_m(float2 m, const Scale &s)
 {
-    const float2 x = __ffma2_rn(u, both(per), both(-0.25f));
-    return make_float2(root_approx(fmaxf(x.x, u.x > 0.f ? 1.f : 0.f)), root_approx(fmaxf(x.y, u.y > 0.f ? 1.f : 0.f)));
+    const float2 y = squared_codes<127>(make_float2(fabsf(m.x), fabsf(m.y)), s);
+    return make_float2(fmaxf(y.x, 0.f), fmaxf(y.y, 0.f));  // (NaN: 0)
+}
+__device__ __forceinline__ float2 squared_codes_u(float2 u, const Scale &s)  // (u above zero: code 1 at least)
+{
+    const float2 y = squared_codes<255>(u, s);
+    return make_float2(fmaxf(y.x, u.x > 0.f ? 1.f : 0.f), fmaxf(y.y, u.y > 0.f ? 1.f : 0.f));
+}
+__device__ __forceinline__ float2 with_signs(float2 q, float2 m) { return make_float2(copysignf(q.x, m.x), copysignf(q.y, m.y)); }
+
+constexpr float kToInteger = 12582912.f;  // 1.5 2^23: what is added comes out to nearest, in the low bits
+
+// Four codes, from approximate roots.  `close`: one of them is so near the middle of two
+// codes that the root's error (some 1e-4 at most) could tell.
+__device__ __forceinline__ uint32_t to_bytes(float2 a, float2 b, bool &close)
+{
+    const float2 ia = __fadd2_rn(a, both(kToInteger)), ib = __fadd2_rn(b, both(kToInteger));
+    const float2 da = __fadd2_rn(__fadd2_rn(ia, both(-kToInteger)), make_float2(-a.x, -a.y)), db = __fadd2_rn(__fadd2_rn(ib, both(-kToInteger)), make_float2(-b.x, -b.y));
+    close = close || fabsf(da.x) > 0.4998f || fabsf(da.y) > 0.4998f || fabsf(db.x) > 0.4998f || fabsf(db.y) > 0.4998f;
+    return __byte_perm(__byte_perm(__float_as_uint(ia.x), __float_as_uint(ia.y), 0x0040), __byte_perm(__float_as_uint(ib.x), __float_as_uint(ib.y), 0x0040), 0x5410);
+}
+__device__ __forceinline__ float2 roots_approx(float2 y) { return make_float2(root_approx(y.x), root_approx(y.y)); }
+__device__ __forceinline__ float2 roots_exact(float2 y) { return make_float2(__fsqrt_rn(y.x), __fsqrt_rn(y.y)); }
+
+// the codes of a lane's eight values
+__device__ __forceinline__ void codes_of(const float2 (&m)[kPairs], const float2 (&u)[kPairs], const Scale &ms, const Scale &us, uint32_t (&m8)[2], uint32_t (&v8)[2])
+{
+    bool close = false, none = false;
+#pragma unroll
+    for (uint32_t j = 0; j < 2; ++j) {
+        m8[j] = to_bytes(with_signs(roots_approx(squared_codes_m(m[2 * j], ms)), m[2 * j]),
+                         with_signs(roots_approx(squared_codes_m(m[2 * j + 1], ms)), m[2 * j + 1]), close);
+        v8[j] = to_bytes(roots_approx(squared_codes_u(u[2 * j], us)), roots_approx(squared_codes_u(u[2 * j + 1], us)), close);
+    }
+    if (!close) return;
+#pragma unroll
+    for (uint32_t j = 0; j < 2; ++j) {
+        m8[j] = to_bytes(with_signs(roots_exact(squared_codes_m(m[2 * j], ms)), m[2 * j]),
+                         with_signs(roots_exact(squared_codes_m(m[2 * j + 1], ms)), m[2 * j + 1]), none);
+        v8[j] = to_bytes(roots_exact(squared_codes_u(u[2 * j], us)), roots_exact(squared_codes_u(u[2 * j + 1], us)), none);
+    }
 }
 
 __device__ __forceinline__ float2 value_m(float2 q, float unit) { return __fmul2_rn(make_float2(q.x * fabsf(q.x), q.y * fabsf(q.y)), both(unit)); }
@@ -440,20 +533,19 @@ __device__ __forceinline__ void step_block(const Places<T, BITS8, MASTER> &at, c
             float2 &mk = m[2 * j + k], &uk = u[2 * j + k];
             const float2 d = __fmul2_rn(g[k], s.clip), dd = __fmul2_rn(s.rest2, __fmul2_rn(d, d));
             if (BITS8) {
+                // (products and sums apart, as codes go by each rounding)
                 mk = value_m(signed_codes(raw.m8[j], 2 * k), m_unit);
                 const float2 old = value_u(unsigned_codes(raw.v8[j], 2 * k), u_unit);
-                v[k] = __ffma2_rn(__fmul2_rn(s.beta2, old), old, dd);
-            } else {
-                v[k] = __ffma2_rn(s.beta2, v[k], dd);
-            }
-            mk = __ffma2_rn(s.beta1, mk, __fmul2_rn(s.rest1, d));
-            if (BITS8) {
-                // (roots and reciprocals of two units in the last place)
-                uk = make_float2(root_approx(v[k].x), root_approx(v[k].y));
+                mk = sum_apart(__fmul2_rn(s.beta1, mk), __fmul2_rn(s.rest1, d));
+                v[k] = sum_apart(__fmul2_rn(s.beta2, __fmul2_rn(old, old)), dd);
+                uk = roots(v[k]);
+                // (reciprocals of two units in the last place)
                 const float2 den = __ffma2_rn(uk, s.root, s.eps);
                 w[k] = minus(w[k], s.decay, __fmul2_rn(__fmul2_rn(s.rate, mk), make_float2(reciprocal_approx(den.x), reciprocal_approx(den.y))));
                 most_m = largest(most_m, mk.x, mk.y), most_u = largest(most_u, uk.x, uk.y);
             } else {
+                mk = __ffma2_rn(s.beta1, mk, __fmul2_rn(s.rest1, d));
+                v[k] = __ffma2_rn(s.beta2, v[k], dd);
                 uk = make_float2(__fsqrt_rn(v[k].x), __fsqrt_rn(v[k].y));
                 const float2 den = __ffma2_rn(uk, s.root, s.eps), step = __fmul2_rn(s.rate, mk);
                 w[k] = minus(w[k], s.decay, make_float2(__fdiv_rn(step.x, den.x), __fdiv_rn(step.y, den.y)));
@@ -477,12 +569,10 @@ __device__ __forceinline__ void step_block(const Places<T, BITS8, MASTER> &at, c
         float m_scale = block_scale(most_m), v_scale = block_scale(most_u);
         if (m_scale + v_scale != m_scale + v_scale) m_scale = v_scale = __uint_as_float(0x7FFFFFFFu);
         if (lane == 0) at.m_scale[block] = m_scale, at.v_scale[block] = v_scale;
-        const float m_per = per_scale<127>(m_scale), v_per = per_scale<255>(v_scale);
         uint32_t m8[2], v8[2];
+        codes_of(m, u, Scale(m_scale), Scale(v_scale), m8, v8);
 #pragma unroll
         for (uint32_t j = 0; j < 2; ++j) {
-            m8[j] = to_bytes(codes_m(m[2 * j], m_per), codes_m(m[2 * j + 1], m_per));
-            v8[j] = to_bytes(codes_u(u[2 * j], v_per), codes_u(u[2 * j + 1], v_per));
             const uint32_t i = block * kBlock + j * 128;
             if (!EIGHTS) put(at.m + i, m8[j], whole, left - (int32_t)i), put(at.v + i, v8[j], whole, left - (int32_t)i);
         }
@@ -674,12 +764,13 @@ __global__ void __launch_bounds__(kThreads) k_load_moments(const fiona_adamw_sta
 #pragma unroll
         for (uint32_t k = 2 * j; k < 2 * j + 2; ++k)
             if (bits8) {
-                u[k] = make_float2(root_approx(u[k].x), root_approx(u[k].y));
+                u[k] = roots(u[k]);
                 most_m = largest(most_m, x[k].x, x[k].y), most_u = largest(most_u, u[k].x, u[k].y);
             }
     }
     const float m_scale = block_scale(most_m), v_scale = block_scale(most_u);
-    const float m_per = per_scale<127>(m_scale), v_per = per_scale<255>(v_scale);
+    uint32_t m8[2], v8[2];
+    codes_of(x, u, Scale(m_scale), Scale(v_scale), m8, v8);
     if (bits8 && lane == 0) {
         if (m) s.m_scale[b] = m_scale;
         if (v) s.v_scale[b] = v_scale;
@@ -688,8 +779,8 @@ __global__ void __launch_bounds__(kThreads) k_load_moments(const fiona_adamw_sta
     for (uint32_t j = 0; j < 2; ++j) {
         const uint64_t i = b * kBlock + j * 128 + lane * 4;
         if (bits8) {
-            if (m) *reinterpret_cast<uint32_t *>((int8_t *)s.m + i) = to_bytes(codes_m(x[2 * j], m_per), codes_m(x[2 * j + 1], m_per));
-            if (v) *reinterpret_cast<uint32_t *>((uint8_t *)s.v + i) = to_bytes(codes_u(u[2 * j], v_per), codes_u(u[2 * j + 1], v_per));
+            if (m) *reinterpret_cast<uint32_t *>((int8_t *)s.m + i) = m8[j];
+            if (v) *reinterpret_cast<uint32_t *>((uint8_t *)s.v + i) = v8[j];
         } else {
             Four<float> to;
             if (m) to.set(x[2 * j], x[2 * j + 1]), *reinterpret_cast<uint4 *>((float *)s.m + i) = to.u;
@@ -732,11 +823,11 @@ int launch_adamw_step(const fiona_adamw *o, void *stream, const uint8_t *active)
         const AdamPiece *pieces = o->d_pieces;
         const AdamRun *runs = o->d_runs;
         uint32_t n_runs = o->n_runs;
-        float *out = o->d_squares;
+        Pair *out = (Pair *)o->d_squares;
         void *args[] = {&pieces, &runs, &n_runs, &active, &out};
         if (const int rc = launch(k_squares, dim3(blocks_of(n_runs)), kThreads, 0, s, args, "adamw norms")) return rc;
     }
-    RateArgs r{o->d_groups, norms ? o->d_squares : nullptr, active, o->state.lr, o->state.steps, o->state.norms, o->d_rates, o->n_groups,
+    RateArgs r{o->d_groups, norms ? (const Pair *)o->d_squares : nullptr, active, o->state.lr, o->state.steps, o->state.norms, o->d_rates, o->n_groups,
                o->flags & FIONA_ADAMW_SKIP_NONFINITE};
     void *rate_args[] = {&r};
     if (const int rc = norms ? launch(k_norm_rates, dim3(o->n_groups), kRateThreads, 0, s, rate_args, "adamw rates")

@@ -28,7 +28,7 @@ struct AdamRun {
 // A group's settings, and its runs [begin, end).
 struct AdamGroup {
     double log_beta1, log_beta2;
-    float max_norm;
+    float max_norm, max_norm_rest;  // and what it lost when it was rounded
     float beta1, rest1, beta2, rest2;  // rest: 1 - beta
     float eps, weight_decay;
     uint32_t begin, end;
@@ -54,7 +54,7 @@ struct fiona_adamw {
     const AdamRun *d_runs = nullptr;      // by group
     const AdamGroup *d_groups = nullptr;
     AdamRate *d_rates = nullptr;   // [n_groups], written by each step
-    float *d_squares = nullptr;    // [n_runs], written by each step that takes norms
+    float *d_squares = nullptr;    // [n_runs][2], written by each step that takes norms
 };
 
 int launch_adamw_step(const fiona_adamw *o, void *stream, const uint8_t *active);

@@ -179,7 +179,8 @@ extern "C" int fiona_adamw_create(const fiona_ctx *ctx, uint32_t n, const fiona_
         AdamGroup *g = reinterpret_cast<AdamGroup *>(image.data() + o_groups);
         for (uint32_t i = 0; i < n_groups; ++i) {
             const fiona_adamw_group &x = groups[i];
-            g[i] = AdamGroup{std::log(x.beta1), std::log(x.beta2), x.max_norm <= 3e38 ? (float)x.max_norm : INFINITY, (float)x.beta1, (float)(1 - x.beta1),
+            const float most = x.max_norm <= 3e38 ? (float)x.max_norm : INFINITY;
+            g[i] = AdamGroup{std::log(x.beta1), std::log(x.beta2), most, std::isfinite(most) ? (float)(x.max_norm - most) : 0.f, (float)x.beta1, (float)(1 - x.beta1),
                              (float)x.beta2, (float)(1 - x.beta2), (float)x.eps, (float)x.weight_decay, run_begin[i], run_begin[i + 1]};
         }
         std::vector<uint32_t> next(begin.begin(), begin.end() - 1);
@@ -194,7 +195,7 @@ extern "C" int fiona_adamw_create(const fiona_ctx *ctx, uint32_t n, const fiona_
             place += (t.count + kBlock - 1) / kBlock * kBlock;
         }
         const size_t o_rates = copied, o_squares = o_rates + align_up(n_groups * sizeof(AdamRate));
-        cudaError_t e = cudaMalloc(&o->blob, o_squares + align_up(o->n_runs * 4ull));
+        cudaError_t e = cudaMalloc(&o->blob, o_squares + align_up(o->n_runs * 8ull));
         if (e == cudaSuccess) e = upload(o->blob, image.data(), image.size());
         if (e != cudaSuccess) return cuda_fail(e, who);
         uint8_t *d = static_cast<uint8_t *>(o->blob);
