@@ -298,55 +298,61 @@ struct Scale {
         minus = both(-s);
     }
 };
-template <uint32_t TOP>
-__device__ __forceinline__ float2 squared_codes(float2 magnitude, const Scale &s)
+__device__ __forceinline__ float2 share_of(float2 v, const Scale &s)
 {
-    const float2 x = __fmul2_rn(magnitude, s.reciprocal);
-    const float2 share = __ffma2_rn(__ffma2_rn(x, s.minus, magnitude), s.reciprocal, x);
-    return sum_apart(__fmul2_rn(share, both((float)(TOP * TOP))), both(-0.25f));
+    const float2 x = __fmul2_rn(v, s.reciprocal);
+    return __ffma2_rn(__ffma2_rn(x, s.minus, v), s.reciprocal, x);
+}
+__device__ __forceinline__ float squared_code_m(float share) { return fmaxf(__fadd_rn(__fmul_rn(fabsf(share), 16129.f), -0.25f), 0.f); }  // (NaN: 0)
+// (u above zero: code 1 at least, by u 2^127 cut to [0, 1])
+__device__ __forceinline__ float squared_code_u(float share, float u)
+{
+    float one;
+    asm("mul.sat.f32 %0, %1, %2;" : "=f"(one) : "f"(u), "f"(1.7014118e38f));
+    return fmaxf(__fadd_rn(__fmul_rn(share, 65025.f), -0.25f), one);
 }
 __device__ __forceinline__ float2 squared_codes_m(float2 m, const Scale &s)
 {
-    const float2 y = squared_codes<127>(make_float2(fabsf(m.x), fabsf(m.y)), s);
-    return make_float2(fmaxf(y.x, 0.f), fmaxf(y.y, 0.f));  // (NaN: 0)
+    const float2 x = share_of(m, s);
+    return make_float2(squared_code_m(x.x), squared_code_m(x.y));
 }
-__device__ __forceinline__ float2 squared_codes_u(float2 u, const Scale &s)  // (u above zero: code 1 at least)
+__device__ __forceinline__ float2 squared_codes_u(float2 u, const Scale &s)
 {
-    const float2 y = squared_codes<255>(u, s);
-    return make_float2(fmaxf(y.x, u.x > 0.f ? 1.f : 0.f), fmaxf(y.y, u.y > 0.f ? 1.f : 0.f));
+    const float2 x = share_of(u, s);
+    return make_float2(squared_code_u(x.x, u.x), squared_code_u(x.y, u.y));
 }
 __device__ __forceinline__ float2 with_signs(float2 q, float2 m) { return make_float2(copysignf(q.x, m.x), copysignf(q.y, m.y)); }
 
 constexpr float kToInteger = 12582912.f;  // 1.5 2^23: what is added comes out to nearest, in the low bits
 
-// Four codes, from approximate roots.  `close`: one of them is so near the middle of two
-// codes that the root's error (some 1e-4 at most) could tell.
-__device__ __forceinline__ uint32_t to_bytes(float2 a, float2 b, bool &close)
+// Four codes from their roots; `far`: the furthest that one of them lies from its code.
+__device__ __forceinline__ uint32_t to_bytes(float2 a, float2 b, float &far)
 {
     const float2 ia = __fadd2_rn(a, both(kToInteger)), ib = __fadd2_rn(b, both(kToInteger));
-    const float2 da = __fadd2_rn(__fadd2_rn(ia, both(-kToInteger)), make_float2(-a.x, -a.y)), db = __fadd2_rn(__fadd2_rn(ib, both(-kToInteger)), make_float2(-b.x, -b.y));
-    close = close || fabsf(da.x) > 0.4998f || fabsf(da.y) > 0.4998f || fabsf(db.x) > 0.4998f || fabsf(db.y) > 0.4998f;
+    const float2 da = __ffma2_rn(a, both(-1.f), __fadd2_rn(ia, both(-kToInteger))), db = __ffma2_rn(b, both(-1.f), __fadd2_rn(ib, both(-kToInteger)));
+    far = largest(largest(far, da.x, da.y), db.x, db.y);
     return __byte_perm(__byte_perm(__float_as_uint(ia.x), __float_as_uint(ia.y), 0x0040), __byte_perm(__float_as_uint(ib.x), __float_as_uint(ib.y), 0x0040), 0x5410);
 }
 __device__ __forceinline__ float2 roots_approx(float2 y) { return make_float2(root_approx(y.x), root_approx(y.y)); }
 __device__ __forceinline__ float2 roots_exact(float2 y) { return make_float2(__fsqrt_rn(y.x), __fsqrt_rn(y.y)); }
 
-// the codes of a lane's eight values
+// The codes of a lane's eight values: from approximate roots, unless one of them lies so
+// near the middle of two codes that the root's error (2^-23 of 255 at most) could tell.
 __device__ __forceinline__ void codes_of(const float2 (&m)[kPairs], const float2 (&u)[kPairs], const Scale &ms, const Scale &us, uint32_t (&m8)[2], uint32_t (&v8)[2])
 {
-    bool close = false, none = false;
+    float far = 0.f, any = 0.f;
 #pragma unroll
     for (uint32_t j = 0; j < 2; ++j) {
         m8[j] = to_bytes(with_signs(roots_approx(squared_codes_m(m[2 * j], ms)), m[2 * j]),
-                         with_signs(roots_approx(squared_codes_m(m[2 * j + 1], ms)), m[2 * j + 1]), close);
-        v8[j] = to_bytes(roots_approx(squared_codes_u(u[2 * j], us)), roots_approx(squared_codes_u(u[2 * j + 1], us)), close);
+                         with_signs(roots_approx(squared_codes_m(m[2 * j + 1], ms)), m[2 * j + 1]), far);
+        v8[j] = to_bytes(roots_approx(squared_codes_u(u[2 * j], us)), roots_approx(squared_codes_u(u[2 * j + 1], us)), far);
     }
-    if (!close) return;
+    if (far < 0.49996f) return;
 #pragma unroll
     for (uint32_t j = 0; j < 2; ++j) {
         m8[j] = to_bytes(with_signs(roots_exact(squared_codes_m(m[2 * j], ms)), m[2 * j]),
-                         with_signs(roots_exact(squared_codes_m(m[2 * j + 1], ms)), m[2 * j + 1]), none);
-        v8[j] = to_bytes(roots_exact(squared_codes_u(u[2 * j], us)), roots_exact(squared_codes_u(u[2 * j + 1], us)), none);
+                         with_signs(roots_exact(squared_codes_m(m[2 * j + 1], ms)), m[2 * j + 1]), any);
+        v8[j] = to_bytes(roots_exact(squared_codes_u(u[2 * j], us)), roots_exact(squared_codes_u(u[2 * j + 1], us)), any);
     }
 }
 
