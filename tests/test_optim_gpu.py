@@ -234,6 +234,73 @@ def test_tensors_do_not_depend_on_their_company(ctx, bits):
         assert torch.equal(together.m, moved.m) and torch.equal(together.v, moved.v)
 
 
+class Stepwise:
+    """Moments in 8 bits by the formulas step by step in fp32 (numpy: each operation rounded
+    to nearest by itself), blocks [n][256]."""
+    f = np.float32
+
+    @classmethod
+    def decode(cls, m8, v8, ms, vs):
+        q, r = m8.astype(cls.f), v8.astype(cls.f)
+        u = (r * r) * (vs * (cls.f(1) / cls.f(65025)))
+        return (q * np.abs(q)) * (ms * (cls.f(1) / cls.f(16129))), u * u
+
+    @classmethod
+    def encode(cls, value, top):
+        scale = np.abs(value).max(1, keepdims=True)
+        y = (np.abs(value) / np.maximum(scale, cls.f(1e-30))) * cls.f(top * top) - cls.f(0.25)
+        q = np.rint(np.sqrt(np.maximum(y, cls.f(0))))
+        q = np.where(value > 0, np.maximum(q, 1), 0) if top == 255 else np.copysign(q, value)
+        return q.astype(np.int8 if top == 127 else np.uint8), scale
+
+    @classmethod
+    def step(cls, m8, v8, ms, vs, g, beta1, beta2):
+        m, v = cls.decode(m8, v8, ms, vs)
+        m = cls.f(beta1) * m + cls.f(1 - beta1) * g
+        v = cls.f(beta2) * v + cls.f(1 - beta2) * (g * g)
+        return cls.encode(m, 127) + cls.encode(np.sqrt(v), 255)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("max_norm", [None, 0.5])
+@pytest.mark.parametrize("rows", [200, 9000])
+def test_codes_step_by_step(ctx, dtype, max_norm, rows):
+    """Every code and scale of three steps is that of the formulas evaluated operation by
+    operation, none a border further (a clipped gradient's factor goes by a norm that is as
+    good as from fp64)."""
+    n = rows * 256
+    p, g = normal((n,), DT[dtype], 1, 0.02), normal((n,), DT[dtype], 2, 1e-3)
+    o = O.AdamW(ctx, [p], [g], state_bits=8, max_norm=max_norm)
+    s = torch.cuda.current_stream()
+    o.load_moments(normal((n,), torch.float32, 3, 3e-4), (normal((n,), torch.float32, 4, 1e-3)).square(), stream=s)
+    state = [t.cpu().numpy() for t in (o.m.view(-1, 256), o.v.view(-1, 256), o.m_scale.view(-1, 1), o.v_scale.view(-1, 1))]
+    for k in range(3):
+        grad = g.float().cpu().numpy().reshape(-1, 256)
+        if max_norm is not None:
+            norm = np.sqrt((grad.astype(np.float64) ** 2).sum())
+            grad = grad * np.float32(min(1.0, max_norm / norm))
+            assert (norm > max_norm) == (rows == 9000)
+        m8, ms, v8, vs = Stepwise.step(*state, grad, 0.9, 0.999)
+        o.step(stream=s)
+        torch.cuda.synchronize()
+        got = [t.cpu().numpy() for t in (o.m.view(-1, 256), o.v.view(-1, 256), o.m_scale.view(-1, 1), o.v_scale.view(-1, 1))]
+        assert np.array_equal(got[2], ms) and np.array_equal(got[3], vs)
+        assert np.array_equal(got[0], m8) and np.array_equal(got[1], v8)
+        state = got
+        g.copy_(normal((n,), DT[dtype], 10 + k, 1e-3))
+    # what is loaded is rounded the same way, and read out as it stands
+    values = [torch.empty(n, device="cuda") for _ in range(2)]
+    o.moments(*values, stream=s)
+    torch.cuda.synchronize()
+    want = Stepwise.decode(*got)
+    assert np.array_equal(values[0].cpu().numpy(), want[0].reshape(-1)) and np.array_equal(values[1].cpu().numpy(), want[1].reshape(-1))
+    fresh = normal((n,), torch.float32, 20), normal((n,), torch.float32, 21).square()
+    o.load_moments(*fresh, stream=s)
+    for x, codes, scale, top in ((fresh[0], o.m, o.m_scale, 127), (fresh[1].sqrt(), o.v, o.v_scale, 255)):
+        q, want = Stepwise.encode(x.cpu().numpy().reshape(-1, 256), top)
+        assert np.array_equal(scale.cpu().numpy(), want.reshape(-1)) and np.array_equal(codes.cpu().numpy().reshape(-1, 256), q)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_not_finite(ctx, bits):
     """A gradient that is not finite: with skip_nonfinite its group sits the step out; without,
