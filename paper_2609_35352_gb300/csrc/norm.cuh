@@ -85,7 +85,8 @@ __device__ __forceinline__ float gradient(float g, float xh, float2 avg, float r
     return __fmaf_rn(rstd, __fmaf_rn(-xh, avg.y, __fsub_rn(g, avg.x)), dsum);
 }
 
-// The same for two columns at once (one instruction for both, rounded as one by one).
+// The same for two columns at once, by one instruction for both.  (No sum follows a product
+// of pairs here but in an fma: a compiler may fuse the two, whatever their names say.)
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 __device__ __forceinline__ float2 dropped(const dropout::Mask &m, float2 v, bool keep_x, bool keep_y)
 {
@@ -97,9 +98,9 @@ __device__ __forceinline__ float2 scaled(float2 d, float2 rstd, float2 shift, fl
     return __ffma2_rn(__ffma2_rn(d, rstd, shift), weight, bias);
 }
 __device__ __forceinline__ float2 xhat(float2 s, float2 minus_mean, float2 rstd) { return __fmul2_rn(__fadd2_rn(s, minus_mean), rstd); }
-__device__ __forceinline__ float2 centred_gradient(float2 g, float2 xh, float2 minus_avg_g, float2 minus_avg_gxh)
+__device__ __forceinline__ float2 centred_gradient(float2 dy, float2 weight, float2 xh, float2 minus_avg_g, float2 minus_avg_gxh)
 {
-    return __ffma2_rn(xh, minus_avg_gxh, __fadd2_rn(g, minus_avg_g));
+    return __ffma2_rn(xh, minus_avg_gxh, __ffma2_rn(dy, weight, minus_avg_g));
 }
 
 }  // namespace layernorm

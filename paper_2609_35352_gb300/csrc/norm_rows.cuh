@@ -432,14 +432,14 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
             __syncthreads();
         }
     }
-    // dy, xh and g of vector e of the row taken (columns past the last: dy is 0)
-    auto take = [&](uint32_t e, float mean, float rstd, float2 (&d)[K<T> / 2], float2 (&xh)[K<T> / 2], float2 (&g)[K<T> / 2]) {
+    // dy, xh and weights of vector e of the row taken (columns past the last: dy is 0)
+    auto take = [&](uint32_t e, float mean, float rstd, float2 (&d)[K<T> / 2], float2 (&xh)[K<T> / 2], float2 (&w)[K<T> / 2]) {
         const uint32_t col = e * LANES * K<T> + at;
         ring.read(0, e, d), ring.read(1, e, xh);
-        if (kHeld && a.weight) held.read(0, e, g);
-        else load_weights<T, VEC>(a.weight, w16, col, a.cols - col, 1.f, g);
+        if (kHeld && a.weight) held.read(0, e, w);
+        else load_weights<T, VEC>(a.weight, w16, col, a.cols - col, 1.f, w);
 #pragma unroll
-        for (uint32_t i = 0; i < K<T> / 2; ++i) xh[i] = xhat(xh[i], both(-mean), both(rstd)), g[i] = __fmul2_rn(d[i], g[i]);
+        for (uint32_t i = 0; i < K<T> / 2; ++i) xh[i] = xhat(xh[i], both(-mean), both(rstd));
     };
     uint32_t slot = 0;
     for (; t < rows; t += step, dx += step_dx, dres += step_dr, z += step_z, slot ^= 1) {
@@ -456,12 +456,13 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e)
             if (inside(e * LANES * K<T> + at)) {
-                float2 d[K<T> / 2], xh[K<T> / 2], g[K<T> / 2];
-                take(e, mean, rstd, d, xh, g);
+                float2 d[K<T> / 2], xh[K<T> / 2], w[K<T> / 2];
+                take(e, mean, rstd, d, xh, w);
 #pragma unroll
                 for (uint32_t i = 0; i < K<T> / 2; ++i) {
+                    const float2 dxh = __fmul2_rn(d[i], xh[i]);
                     dw[e][i] = __ffma2_rn(d[i], xh[i], dw[e][i]), db[e][i] = __fadd2_rn(db[e][i], d[i]);
-                    s1 = __fadd2_rn(s1, g[i]), s2 = __ffma2_rn(g[i], xh[i], s2);
+                    s1 = __ffma2_rn(d[i], w[i], s1), s2 = __ffma2_rn(dxh, w[i], s2);
                 }
             }
         const float2 avg = row_sum<LANES>(make_float2(s1.x + s1.y, s2.x + s2.y), part, slot);
@@ -473,7 +474,7 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
                 float2 d[K<T> / 2], xh[K<T> / 2], g[K<T> / 2];
                 take(e, mean, rstd, d, xh, g);
 #pragma unroll
-                for (uint32_t i = 0; i < K<T> / 2; ++i) g[i] = centred_gradient(g[i], xh[i], minus_g, minus_gxh);
+                for (uint32_t i = 0; i < K<T> / 2; ++i) g[i] = centred_gradient(d[i], g[i], xh[i], minus_g, minus_gxh);
                 if (DSUM) {
                     ring.read(2, e, d);
 #pragma unroll
