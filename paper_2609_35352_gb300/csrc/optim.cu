@@ -71,11 +71,11 @@ __device__ __forceinline__ Pair warp_sum(Pair v)
     for (uint32_t i = 16; i; i >>= 1) v = sum_of(v, Pair{__shfl_xor_sync(0xFFFFFFFFu, v.hi, i), __shfl_xor_sync(0xFFFFFFFFu, v.lo, i)});
     return v;
 }
-// sums += x, the losses kept apart (negated)
-__device__ __forceinline__ void add_square(float2 &sum, float2 &lost, float2 v)
+// sum += v^2, with `rest`, what the sum has not taken of it so far
+__device__ __forceinline__ void add_square(float2 &sum, float2 &rest, float2 v)
 {
-    const float2 x = __fadd2_rn(__fmul2_rn(v, v), make_float2(-lost.x, -lost.y)), s = __fadd2_rn(sum, x);
-    lost = __fadd2_rn(__fadd2_rn(s, make_float2(-sum.x, -sum.y)), make_float2(-x.x, -x.y));
+    const float2 x = __ffma2_rn(v, v, rest), s = __fadd2_rn(sum, x);
+    rest = __ffma2_rn(__ffma2_rn(sum, both(-1.f), s), both(-1.f), x);
     sum = s;
 }
 
@@ -91,7 +91,7 @@ __device__ __forceinline__ float plain_squares(const AdamPiece &p, uint32_t lane
 
 // the sum of squares of a piece's gradients, added to a thread's four sums
 template <typename T>
-__device__ __forceinline__ void squares(const AdamPiece &p, uint32_t lane, float2 (&s)[2], float2 (&lost)[2])
+__device__ __forceinline__ void squares(const AdamPiece &p, uint32_t lane, float2 (&s)[2], float2 (&rest)[2])
 {
     const T *g = (const T *)p.grad;
     if (p.aligned && p.count % kBlock == 0) {
@@ -102,13 +102,13 @@ __device__ __forceinline__ void squares(const AdamPiece &p, uint32_t lane, float
             const T *x = reinterpret_cast<const T *>(&u);
 #pragma unroll
             for (uint32_t j = 0; j < k; j += 2) {
-                add_square(s[j / 2 % 2], lost[j / 2 % 2], make_float2(widen(x[j]), widen(x[j + 1])));
+                add_square(s[j / 2 % 2], rest[j / 2 % 2], make_float2(widen(x[j]), widen(x[j + 1])));
             }
         }
     } else {
 #pragma unroll 4
         for (uint32_t i = lane; i < p.count; i += 64)
-            add_square(s[0], lost[0], make_float2(widen(g[i]), i + 32 < p.count ? widen(g[i + 32]) : 0.f));
+            add_square(s[0], rest[0], make_float2(widen(g[i]), i + 32 < p.count ? widen(g[i + 32]) : 0.f));
     }
 }
 
@@ -119,19 +119,21 @@ __global__ void __launch_bounds__(kThreads) k_squares(const AdamPiece *pieces, c
     const uint32_t at = blockIdx.x * kWarps + threadIdx.x / 32, lane = threadIdx.x & 31;
     if (at >= n) return;
     const AdamRun r = runs[at];
-    float2 s[2] = {}, lost[2] = {};
+    float2 s[2] = {}, rest[2] = {};
+    AdamPiece next = pieces[r.begin];
     for (uint32_t i = r.begin; i < r.end; ++i) {
-        const AdamPiece p = pieces[i];
+        const AdamPiece p = next;
+        if (i + 1 < r.end) next = pieces[i + 1];
         if (active && !active[p.group]) break;  // (all of a run are of one group)
         if (p.dtype == FIONA_F32)
-            squares<float>(p, lane, s, lost);
+            squares<float>(p, lane, s, rest);
         else if (p.dtype == FIONA_F16)
-            squares<__half>(p, lane, s, lost);
+            squares<__half>(p, lane, s, rest);
         else
-            squares<__nv_bfloat16>(p, lane, s, lost);
+            squares<__nv_bfloat16>(p, lane, s, rest);
     }
-    Pair v = sum_of(sum_of(Pair{s[0].x, -lost[0].x}, Pair{s[0].y, -lost[0].y}), sum_of(Pair{s[1].x, -lost[1].x}, Pair{s[1].y, -lost[1].y}));
-    if (__any_sync(0xFFFFFFFFu, v.hi - v.hi != 0.f)) {  // (what an infinite sum has lost is NaN: which of the two is it?)
+    Pair v = sum_of(sum_of(Pair{s[0].x, rest[0].x}, Pair{s[0].y, rest[0].y}), sum_of(Pair{s[1].x, rest[1].x}, Pair{s[1].y, rest[1].y}));
+    if (__any_sync(0xFFFFFFFFu, v.hi - v.hi != 0.f)) {  // (the rest of an infinite sum is NaN: which of the two is it?)
         v = Pair{0.f, 0.f};
         for (uint32_t i = r.begin; i < r.end; ++i)
             v.hi += pieces[i].dtype == FIONA_F32   ? plain_squares<float>(pieces[i], lane)
@@ -201,6 +203,7 @@ __global__ void __launch_bounds__(kRateThreads) k_norm_rates(const RateArgs a)
     previous_done();
     const AdamGroup &g = a.groups[blockIdx.x];
     Pair s{0.f, 0.f};
+#pragma unroll 4
     for (uint32_t i = g.begin + threadIdx.x; i < g.end; i += kRateThreads) s = sum_of(s, a.squares[i]);
     const uint32_t lane = threadIdx.x & 31;
     s = warp_sum(s);

@@ -144,8 +144,9 @@ extern "C" int fiona_adamw_create(const fiona_ctx *ctx, uint32_t n, const fiona_
     for (uint64_t i = 0; i < 3ull * n_groups; ++i) begin[i + 1] += begin[i];
     const uint32_t n_pieces = begin.back();
 
-    // runs of pieces: as long as leaves some for every scheduler of the device
-    const uint32_t run = std::min(std::max(n_pieces / (64 * sms), 1u), kMostRun);
+    // runs of pieces: as long as leaves four for every warp that the device holds at a time
+    // (in two or three waves of them the last one stands half empty)
+    const uint32_t run = std::min(std::max(n_pieces / (4 * 64 * sms), 1u), kMostRun);
     std::vector<AdamRun> runs;
     std::vector<uint32_t> run_begin(n_groups + 1, 0);
     if (s.norms)
