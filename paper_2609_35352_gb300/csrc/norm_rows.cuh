@@ -1,7 +1,13 @@
 // norm_rows.cuh -- layer norm of rows that a warp or a block holds in registers.
 //
 // Bound by HBM: forward x, residual, out and sum once, backward dy, sum, dx and
-// dresidual (and dsum) once.  A row is spread over LANES threads, 8 to 32
+// dresidual (and dsum) once.  16384 x 4096 bf16 with dropout, 537 MB either way: forward
+// 82 us (6.5 TB/s, of 6.8 that a copy reaches), backward with dweight and dbias 97 us (5.5;
+// warps issue 58% of the time, 10 of 36 instructions an element for the mask, and 16 warps
+// an SM hide no more of a row's chain of sums); 4096 x 8192 fp32 backward 95 us (5.6: its
+// rows ahead leave room for one block an SM).
+//
+// A row is spread over LANES threads, 8 to 32
 // columns each; a block walks over rows a grid apart.  Rows ahead come by 16-byte
 // asynchronous copies into shared memory, each thread's columns into places of its own:
 // it alone reads them, so that nothing but the row's sums needs a barrier, and what is
@@ -109,7 +115,7 @@ __device__ __forceinline__ void drop(const dropout::Mask &m, uint64_t z, float2 
     }
 }
 
-// Rows ahead in a backward pass (one: 16384 x 4096 bf16 130 us for 112), their room beside
+// Rows ahead in a backward pass (16384 x 4096 bf16 97 us; one 115, three 99), their room beside
 // the weights, for rows of up to `cols`, and whether the weights have room beside them.
 constexpr uint32_t kGradAhead = 2;
 constexpr uint32_t grad_room(uint32_t cols, uint32_t size) { return backward_blocks(cols, size) > 1 ? 96 * 1024 : cols <= 8192 ? 192 * 1024 : 128 * 1024; }
@@ -170,18 +176,15 @@ struct Ring {
 
 // A row's weights (and biases) in shared memory, [2][VECS][parts][LANES].  From global
 // memory they would come out of L2 for every row, since the rows ahead take L1's room
-// (16384 x 4096 bf16, two rows in flight: 103 us for 96).  They come by way of L1: copies
+// (16384 x 4096 bf16, forward: 110 us for 82).  They come by way of L1: copies
 // past it of the same lines by every block go to a few slices of L2 (2048 x 1024 fp32, each
 // warp its own copy: 49 us for 6.5).  WIDE: in fp32 whatever they are, so that no row
-// widens them again: backward, which takes them twice (97 us for 103 on 16384 x 4096
+// widens them again: backward, which takes them twice (97 us for 104 on 16384 x 4096
 // bf16), and forward for rows of a warp or two (65536 x 1024 bf16 with dropout 90 us for
 // 101); above they would take a block's room on an SM (2048 columns 99 us for 84).
 constexpr bool wide_weights(uint32_t cols, uint32_t size) { return size == 4 || cols <= 4096; }  // (backward; more: no room beside the rows)
 constexpr bool held_weights(uint32_t lanes) { return lanes <= 512; }  // (forward; 1024: no room beside the rows)
 
-// WIDE: in fp32 whatever they are, so that no row widens them again (backward, which takes
-// them twice: 97 us for 103 on 16384 x 4096 bf16; forward they would take a block's room
-// on an SM up to 2048 columns, 99 us for 84).
 template <typename T, uint32_t VECS, uint32_t LANES, bool WIDE>
 struct Held {
     uint4 *at;
@@ -249,8 +252,8 @@ __device__ __forceinline__ V row_sum(V v, float2 (*part)[32], uint32_t slot)
 }
 
 // How a row lies: by elements; in whole vectors; in as many as its threads have, LANES times
-// VECS (then nothing asks whether a vector is there: 16384 x 4096 bf16 82 us for 84 and,
-// backward, 103 for 106).
+// VECS (then nothing asks whether a vector is there: 16384 x 4096 bf16 82 us for 86 and,
+// backward, 97 for 101).
 enum class Reach { elements, vectors, whole };
 
 template <typename T, uint32_t LANES, uint32_t VECS, Reach REACH>
@@ -378,8 +381,8 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
 
 // A thread keeps the sums of its up to 32 columns in registers, and nothing else of a row:
 // once the row's averages are there, it takes the row out of its places in shared memory
-// again.  (With g and xh in registers from one to the other and 16 columns a thread, half as
-// many rows are under way on an SM: 16384 x 4096 bf16 with dropout 131 us.)  `sums`:
+// again.  (16 columns a thread: 16384 x 4096 bf16 with dropout 123 us for 97, half as many
+// rows under way on an SM; three blocks of them an SM 109, and their registers spill.)  `sums`:
 // [gridDim.x][2][cols], null: dweight and dbias are not wanted.
 template <typename T, uint32_t LANES, uint32_t VECS, Reach REACH, bool DSUM>
 __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES * VECS * K<T>, sizeof(T))) k_norm_rows_grad(const NormGradArgs a, const bool w16, float *sums)
@@ -403,7 +406,7 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
     auto inside = [&](uint32_t col) { return REACH == Reach::whole || col < a.cols; };
     float2 dw[VECS][K<T> / 2] = {}, db[VECS][K<T> / 2] = {};
     // This thread's first column of the next row to fetch, and of the row taken, moved on
-    // from row to row.  (Made anew from the row's number: 144 us for 132.)
+    // from row to row.  (Made anew from the row's number it cost a tenth.)
     uint32_t t = blockIdx.x * kGroups + group, next_t = t;
     const T *dy = (const T *)a.dy + t * a.ld_dy + at, *x = (const T *)a.sum + t * a.ld_sum + at, *dsum = (const T *)a.dsum + t * a.ld_dsum + at;
     T *dx = (T *)a.dx + t * a.ld_dx + at, *dres = (T *)a.dres + t * a.ld_dres + at;
@@ -566,9 +569,12 @@ int forward_rows(const fiona_ctx *ctx, void *stream, const NormArgs &a, bool w16
     cudaStream_t s = (cudaStream_t)stream;
     constexpr uint32_t one = 8 / K<T>, two = 2 * one, four = 4 * one;  // eights of columns in vectors
     switch (forward_lanes(a.cols, sizeof(T))) {
+        // (three: 87381 x 768 bf16 94 us for 103 by four, a vector of them empty; backward it gains
+        // 2% in 16 bits and costs 5% in fp32)
         case 32:
             return a.cols <= 256   ? forward_rows<T, 32, one>(ctx, s, a, w16)
-                   : a.cols <= 512 ? forward_rows<T, 32, two>(ctx, s, a, w16) : forward_rows<T, 32, four>(ctx, s, a, w16);
+                   : a.cols <= 512 ? forward_rows<T, 32, two>(ctx, s, a, w16)
+                   : a.cols <= 768 ? forward_rows<T, 32, 3 * one>(ctx, s, a, w16) : forward_rows<T, 32, four>(ctx, s, a, w16);
         case 64: return forward_rows<T, 64, two>(ctx, s, a, w16);
         case 128: return forward_rows<T, 128, two>(ctx, s, a, w16);
         case 256: return forward_rows<T, 256, two>(ctx, s, a, w16);

@@ -7,9 +7,9 @@ constexpr uint32_t kMostForward = 16384, kMostBackward = 16384;  // columns
 // A row's threads, by its width and type alone: a row comes out the same however many
 // others there are.  Each takes up to 16 columns; forward 32 where a row of 513 to 1024
 // 16-bit columns is a warp's.  (32 columns spread wider what a row costs each thread beside
-// them, but half the threads are too few to hide its chain of sums: 16384 x 4096 bf16 96 us,
-// with 16 columns 89.  87381 rows of 768: 32 threads a row 92 us, 64 115; in fp32 192 and
-// 161; one row of them 3.1 us and 2.5.)
+// them, but half the threads are too few to hide its chain of sums: 16384 x 4096 bf16 99 us,
+// with 16 columns 82.  87381 rows of 768 with dropout: 32 threads a row 96 us, 64 112; in
+// fp32 175 and 161.)
 inline uint32_t forward_lanes(uint32_t cols, uint32_t size)
 {
     return cols <= 512 ? 32 : cols <= 1024 ? (size == 4 ? 64 : 32) : cols <= 2048 ? 128 : cols <= 4096 ? 256 : cols <= 8192 ? 512 : 1024;

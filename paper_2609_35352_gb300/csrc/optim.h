@@ -10,7 +10,7 @@ constexpr uint32_t kBlock = FIONA_ADAMW_BLOCK;
 // Elements of a tensor that a warp steps: kPiece, or a block where that leaves the
 // device's schedulers short of warps (8 each).
 constexpr uint32_t kPiece = 1024;
-constexpr uint32_t kMostRun = 16;  // pieces that one fp32 sum of squares takes
+constexpr uint32_t kMostRun = 16;  // pieces that a warp takes the squares of, at most
 
 // A warp's work: up to kPiece elements of one tensor, from `place` of the state on.
 struct AdamPiece {
