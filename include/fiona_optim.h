@@ -79,7 +79,7 @@ typedef struct fiona_adamw_tensor {
 
 typedef struct fiona_adamw_group {
     double beta1, beta2;  /* [0, 1) */
-    double eps;           /* not negative */
+    double eps;           /* 0, or from 2^-126 on; finite */
     double weight_decay;  /* finite */
     double max_norm;      /* above 0; infinity: no clipping */
 } fiona_adamw_group;
@@ -120,8 +120,9 @@ int fiona_adamw_reset(const fiona_adamw *opt, void *cuda_stream);
 int fiona_adamw_step(const fiona_adamw *opt, void *cuda_stream, const uint8_t *active);
 
 /* The moments as values of the type given, [places] each (either may be NULL), and
- * back: what is read is rounded to the state's form as a step rounds it.  For programs
- * that save, inspect or convert a state.  16-byte aligned buffers. */
+ * back: what is read (v not negative) is rounded to the state's form as a step rounds it.
+ * For programs that save, inspect or convert a state.  16-byte aligned buffers, which may
+ * not overlap each other or the state. */
 int fiona_adamw_moments(const fiona_adamw *opt, void *cuda_stream, uint32_t dtype, void *m, void *v);
 int fiona_adamw_load_moments(const fiona_adamw *opt, void *cuda_stream, uint32_t dtype, const void *m, const void *v);
 

@@ -22,6 +22,10 @@ inline uint64_t element(uint32_t dtype) { return dtype == FIONA_F32 ? 4 : 2; }
 
 inline uint64_t align_up(uint64_t n) { return (n + 255) & ~255ull; }
 
+// whether an eps is none, or one that fp32 holds (a smaller one would be zero in a kernel, and
+// divide zeros by zeros where the formula does not)
+inline bool normal(double eps) { return eps == 0.0 || (eps >= 0x1p-126 && std::isfinite(eps)); }
+
 // A strided matrix of one call.
 struct View {
     const void *p;

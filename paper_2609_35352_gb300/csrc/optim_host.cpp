@@ -73,6 +73,10 @@ int check_moments(const fiona_adamw *o, uint32_t dtype, const void *m, const voi
     std::vector<Range> r;
     add(r, m, o->places * element(dtype), true);
     add(r, v, o->places * element(dtype), true);
+    add(r, s.master, o->places * 4, true);
+    add(r, s.steps, o->n_groups * 8ull, true);
+    add(r, s.lr, o->n_groups * 4ull, true);
+    add(r, s.norms, o->n_groups * 4ull, true);
     add(r, s.m, o->places * (bits8 ? 1 : 4), true);
     add(r, s.v, o->places * (bits8 ? 1 : 4), true);
     add(r, s.m_scale, o->places / kBlock * 4, true);
@@ -112,7 +116,7 @@ extern "C" int fiona_adamw_create(const fiona_ctx *ctx, uint32_t n, const fiona_
     if ((uintptr_t)s.steps & 7 || ((uintptr_t)s.lr | (uintptr_t)s.norms) & 3) return set_error(FIONA_ERR_ARG, "%s: misaligned steps, lr or norms", who);
     for (uint32_t i = 0; i < n_groups; ++i) {
         const fiona_adamw_group &g = groups[i];
-        if (!(g.beta1 >= 0 && g.beta1 < 1 && g.beta2 >= 0 && g.beta2 < 1 && g.eps >= 0 && std::isfinite(g.eps)) ||
+        if (!(g.beta1 >= 0 && g.beta1 < 1 && g.beta2 >= 0 && g.beta2 < 1 && normal(g.eps)) ||
             !std::isfinite(g.weight_decay) || !(g.max_norm > 0))
             return set_error(FIONA_ERR_ARG, "%s: group %u: beta outside [0, 1), eps negative, or eps, weight decay or max_norm out of range", who, i);
         if (std::isfinite(g.max_norm) && !s.norms) return set_error(FIONA_ERR_ARG, "%s: group %u is clipped, but norms is NULL", who, i);

@@ -133,8 +133,10 @@ def test_refused(ctx, backward):
         assert Case(ctx, backward).put(work=c.c.work + 8) == ARG
         assert Case(ctx, backward).put(dx=None, dresidual=None, dweight=None, dbias=None) == ARG
     else:
-        for eps in (-1e-9, float("nan"), float("inf")):
+        for eps in (-1e-9, 1e-39, 5e-324, float("nan"), float("inf")):
             assert Case(ctx, backward).put(eps=eps) == ARG
+        for eps in (0.0, 2.0 ** -126):
+            assert Case(ctx, backward).put(eps=eps) == NODEVICE
     assert (LN.lib().fiona_layer_norm_backward if backward else LN.lib().fiona_layer_norm)(ctx.handle, None, None) == ARG
 
 

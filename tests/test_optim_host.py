@@ -129,7 +129,7 @@ def test_refused(ctx, bits8):
         c = Case(ctx)
         c.s.m_scale = c.room(64)
         assert c() == ARG
-    for k, bad in (("beta1", (-0.1, 1.0, float("nan"))), ("beta2", (-0.1, 1.0, float("nan"))), ("eps", (-1.0, float("nan"), float("inf"))),
+    for k, bad in (("beta1", (-0.1, 1.0, float("nan"))), ("beta2", (-0.1, 1.0, float("nan"))), ("eps", (-1.0, 1e-39, float("nan"), float("inf"))),
                    ("weight_decay", (float("nan"), float("inf"))), ("max_norm", (0.0, -1.0, float("nan")))):
         for v in bad:
             c = Case(ctx, bits8)
@@ -214,6 +214,12 @@ def test_binding(ctx):
             o.moments(m, v)
         with pytest.raises(ValueError):
             o.load_moments(m, v)
+    values = torch.zeros(1280)
+    for call in (o.moments, o.load_moments):
+        for m, v, status in ((values, None, NODEVICE), (o.master, None, ARG), (None, o.master, ARG), (values, values, ARG), (o.norms.new_zeros(0), None, None)):
+            with pytest.raises(ValueError if status is None else F.FionaError) as e:
+                call(m, v)
+            assert status is None or e.value.status == status
     o = make()
     assert o.norms is None and o.master is None and o.n_groups == 1 and o.m.dtype == torch.float32
     assert make(n_groups=5).steps.shape == (5,)
