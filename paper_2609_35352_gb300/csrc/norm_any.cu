@@ -122,7 +122,11 @@ __global__ void __launch_bounds__(kColThreads) k_columns(const NormGradArgs a, c
     }
 }
 
-// dweight (blockIdx.y = 0) and dbias (1): 32 columns a block
+// dweight (blockIdx.y = 0) and dbias (1): 32 columns a block.  A thread's sums are taken
+// kMostParts at a time, and what is lost where those are added up goes into the next (Kahan):
+// 2^30 rows have 2048 parts along a thread, 3e-5 of a sum whose roundings go one way.  (For
+// every part: 2.7 us more of 304 parts of 4096 columns.)
+constexpr uint32_t kMostParts = 64;
 template <typename W>
 __global__ void __launch_bounds__(1024) k_grad_sum(const float *part, uint32_t parts, uint32_t cols, W *dweight, W *dbias)
 {
@@ -130,12 +134,22 @@ __global__ void __launch_bounds__(1024) k_grad_sum(const float *part, uint32_t p
     previous_done();
     const uint32_t x = threadIdx.x & 31, y = threadIdx.x / 32, i = blockIdx.x * 32 + x;
     W *out = blockIdx.y ? dbias : dweight;
-    float v[4] = {};
+    float v[4] = {}, rest[4] = {};
     if (i < cols && out)
-        for (uint32_t k = y; k < parts; k += 128)
+        for (uint32_t begin = 0; begin < parts; begin += 128 * kMostParts) {
+            float w[4] = {};
+#pragma unroll 2
+            for (uint32_t k = begin + y, end = min(parts, begin + 128 * kMostParts); k < end; k += 128)
 #pragma unroll
-            for (uint32_t q = 0; q < 4; ++q)
-                if (k + 32 * q < parts) v[q] += part[(2ull * (k + 32 * q) + blockIdx.y) * cols + i];
+                for (uint32_t q = 0; q < 4; ++q)
+                    if (k + 32 * q < end) w[q] += part[(2ull * (k + 32 * q) + blockIdx.y) * cols + i];
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                const float p = __fadd_rn(w[q], rest[q]), sum = __fadd_rn(v[q], p);
+                rest[q] = sum - sum == 0.f ? __fsub_rn(p, __fsub_rn(sum, v[q])) : 0.f;  // (none of an infinity's)
+                v[q] = sum;
+            }
+        }
     s[y][x] = (v[0] + v[1]) + (v[2] + v[3]);
     __syncthreads();
     if (y == 0 && i < cols && out) {

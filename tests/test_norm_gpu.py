@@ -313,6 +313,17 @@ def test_many_rows(ctx):
     assert (dw.double() / rows - row[0].double()).abs().max() <= (c + 2.0 ** -22) * float(row.abs().max())
 
 
+def test_sums_of_a_billion_rows(ctx):
+    """A thread's sums of 512 rows of 1 + 2^-14, and those of a block, are exact; how many blocks'
+    sums are added up after that does not show: 40 additions at most are rounded at their own size."""
+    rows = 1 << 30
+    dy = torch.full((1, 1), 1 + 2.0 ** -14, device="cuda").expand(rows, 1)
+    zero, one = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    dw, db = torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    LN.layer_norm_backward(ctx, dy, dy, zero, one, dweight=dw, dbias=db, work=LN.workspace(ctx, rows, 1))
+    assert abs(float(db) / rows / (1 + 2.0 ** -14) - 1) <= 40 * 2.0 ** -24
+
+
 def test_streams_and_graphs(ctx):
     """Calls on another stream; a captured forward and backward pass, replayed on new
     inputs, beside the eager calls."""
