@@ -324,6 +324,17 @@ def test_sums_of_a_billion_rows(ctx):
     assert abs(float(db) / rows / (1 + 2.0 ** -14) - 1) <= 40 * 2.0 ** -24
 
 
+def test_squares_of_a_million_columns(ctx):
+    """Equal squares, whose additions all round one way: at most 64 + 32 + 21 one after another
+    (a rounding of the sum is half of one of rstd), and eight roundings of rstd itself."""
+    cols, v = 1 << 20, 1.984375
+    x = torch.full((2, cols), v, device="cuda")
+    x[:, ::2] = -v
+    out, rstd = torch.empty_like(x), torch.empty(2, device="cuda")
+    LN.layer_norm(ctx, x, out, rstd=rstd)
+    assert (rstd.double() * (v * v + 1e-5) ** 0.5 - 1).abs().max() <= (117 / 2 + 8) * 2.0 ** -24
+
+
 def test_streams_and_graphs(ctx):
     """Calls on another stream; a captured forward and backward pass, replayed on new
     inputs, beside the eager calls."""
