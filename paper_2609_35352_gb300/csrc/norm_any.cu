@@ -3,9 +3,13 @@
 // Forward: a block a row, which it reads three times (the mean; squares about the
 // mean, with what is left of the mean; the outputs): from HBM once, from L2 or L1
 // after that.  Backward: a block a row for the two averages of the row (k_averages),
-// then blocks of columns (k_columns), a thread four columns of a run of rows, which
+// then blocks of columns (k_columns), a thread a vector of columns of a run of rows, which
 // make dx and dresidual and keep the sums of dweight and dbias in registers; the
 // runs' sums are added up in order (k_grad_sum).  dy and sum are read twice.
+//
+// 134 M elements in rows of 32768, bf16: forward with the sum 160 us (5.0 TB/s), backward
+// 314 us (4.3 TB/s with the second reading; element by element, not in vectors, 272 and 575).
+// Rows of 2^20, of which these are 128, leave SMs idle: 438 and 882 us.
 #include <algorithm>
 
 #include "norm.cuh"
@@ -14,7 +18,7 @@ namespace {
 
 using namespace layernorm;
 
-constexpr uint32_t kThreads = 512, kColThreads = 128, kColumns = 4;
+constexpr uint32_t kThreads = 512, kColThreads = 128;
 
 // sums over a block of kThreads, the same in every thread
 __device__ float2 block_sum(float2 v, float2 *part)
@@ -29,45 +33,89 @@ __device__ float2 block_sum(float2 v, float2 *part)
     return s;
 }
 
-// The sums over a row of what `add(i, s)` adds to s for column i, the same in every thread.
-// A thread adds up to 64 columns, then those sums (in one sum 2048 of 2^20 columns: 3e-5 of
-// squares whose roundings go one way).
-template <typename Add>
+// The sums over a row of what `add(i, s)` adds for a vector of columns from i on, each pair's
+// two, the same in every thread.  A thread adds up to 64 columns, then those sums (in one sum
+// 2048 of 2^20 columns: 3e-5 of squares whose roundings go one way).
+struct Two {
+    float2 a, b;
+};
+template <typename T, typename Add>
 __device__ __forceinline__ float2 row_sums(uint32_t cols, float2 *part, const Add &add)
 {
     constexpr uint32_t kStretch = 64 * kThreads;
-    float2 s = make_float2(0.f, 0.f);
+    Two s{};
     for (uint32_t begin = 0; begin < cols; begin += kStretch) {
-        float2 w = make_float2(0.f, 0.f);
-        for (uint32_t i = begin + threadIdx.x, end = min(cols, begin + kStretch); i < end; i += kThreads) add(i, w);
-        s.x += w.x, s.y += w.y;
+        Two w{};
+#pragma unroll 2
+        for (uint32_t i = begin + threadIdx.x * K<T>, end = min(cols, begin + kStretch); i < end; i += kThreads * K<T>) add(i, w);
+        s.a = __fadd2_rn(s.a, w.a), s.b = __fadd2_rn(s.b, w.b);
     }
-    return block_sum(s, part);
+    return block_sum(make_float2(s.a.x + s.a.y, s.b.x + s.b.y), part);
 }
 
-template <typename T, typename W>
-__global__ void __launch_bounds__(kThreads) k_norm_any(const NormArgs a)
+template <typename T, bool VEC>
+__device__ __forceinline__ void store(T *p, uint32_t left, const float2 (&v)[K<T> / 2])
 {
+    const Vector<T> x{narrowed<T>(v)};
+    if (VEC) {
+        *reinterpret_cast<uint4 *>(p) = x.u;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < K<T>; ++i)
+            if (i < left) p[i] = x.values()[i];
+    }
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_norm_any(const NormArgs a, const bool w16)
+{
+    constexpr uint32_t kPairs = K<T> / 2;
     __shared__ float2 part[kThreads / 32];
     previous_done();
     next_may_start();
     const float per = 1.f / (float)a.cols;
     for (uint64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
         const T *x = (const T *)a.x + t * a.ldx, *res = (const T *)a.res + t * a.ld_res;
-        auto at = [&](uint32_t i) {
-            const float v = dropped(a.mask, widen(x[i]), t, i);
-            return a.res ? __fadd_rn(v, widen(res[i])) : v;
+        const uint64_t z = a.mask.base + t * a.mask.groups * dropout::kGolden;  // the row's first draw
+        // (columns past the last are 0)
+        auto take = [&](uint32_t i, float2 (&v)[kPairs]) {
+            load<T, VEC>(x + i, a.cols - i, v);
+            if (a.mask.level) drop(a.mask, z + (uint64_t)(i / 4) * dropout::kGolden, v);
+            if (a.res) {
+                float2 r[kPairs];
+                load<T, VEC>(res + i, a.cols - i, r);
+#pragma unroll
+                for (uint32_t k = 0; k < kPairs; ++k) v[k] = __fadd2_rn(v[k], r[k]);
+            }
         };
-        const float about = row_sums(a.cols, part, [&](uint32_t i, float2 &w) { w.x += at(i); }).x * per;
-        const float2 s = row_sums(a.cols, part, [&](uint32_t i, float2 &w) {
-            const float d = __fsub_rn(at(i), about);
-            w.x += d, w.y = __fmaf_rn(d, d, w.y);
+        const float about = row_sums<T>(a.cols, part, [&](uint32_t i, Two &w) {
+            float2 v[kPairs];
+            take(i, v);
+#pragma unroll
+            for (uint32_t k = 0; k < kPairs; ++k) w.a = __fadd2_rn(w.a, v[k]);
+        }).x * per;
+        const float2 s = row_sums<T>(a.cols, part, [&](uint32_t i, Two &w) {
+            float2 v[kPairs];
+            take(i, v);
+#pragma unroll
+            for (uint32_t k = 0; k < kPairs; ++k) {
+                float2 d = __fadd2_rn(v[k], both(-about));
+                if (!VEC && i + 2 * k >= a.cols) d.x = 0.f;
+                if (!VEC && i + 2 * k + 1 >= a.cols) d.y = 0.f;
+                w.a = __fadd2_rn(w.a, d), w.b = __ffma2_rn(d, d, w.b);
+            }
         });
         const float left = s.x * per, rstd = rstd_of(left, s.y * per, a.eps), shift = shift_of(left, rstd);
-        for (uint32_t i = threadIdx.x; i < a.cols; i += kThreads) {
-            const float v = at(i), w = a.weight ? widen(((const W *)a.weight)[i]) : 1.f, b = a.bias ? widen(((const W *)a.bias)[i]) : 0.f;
-            if (a.sum) ((T *)a.sum)[t * a.ld_sum + i] = narrow<T>(v);
-            ((T *)a.out)[t * a.ld_out + i] = narrow<T>(scaled(__fsub_rn(v, about), rstd, shift, w, b));
+#pragma unroll 2
+        for (uint32_t i = threadIdx.x * K<T>; i < a.cols; i += kThreads * K<T>) {
+            float2 v[kPairs], w[kPairs], b[kPairs];
+            take(i, v);
+            load_weights<T, VEC>(a.weight, w16, i, a.cols - i, 1.f, w);
+            load_weights<T, VEC>(a.bias, w16, i, a.cols - i, 0.f, b);
+            if (a.sum) store<T, VEC>((T *)a.sum + t * a.ld_sum + i, a.cols - i, v);
+#pragma unroll
+            for (uint32_t k = 0; k < kPairs; ++k) v[k] = scaled(__fadd2_rn(v[k], both(-about)), both(rstd), both(shift), w[k], b[k]);
+            store<T, VEC>((T *)a.out + t * a.ld_out + i, a.cols - i, v);
         }
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[t] = about + left;
@@ -76,10 +124,11 @@ __global__ void __launch_bounds__(kThreads) k_norm_any(const NormArgs a)
     }
 }
 
-// avg g and avg (g xh) of each row
-template <typename T, typename W>
-__global__ void __launch_bounds__(kThreads) k_averages(const NormGradArgs a, float2 *avg)
+// avg g and avg (g xh) of each row, negated
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_averages(const NormGradArgs a, const bool w16, float2 *avg)
 {
+    constexpr uint32_t kPairs = K<T> / 2;
     __shared__ float2 part[kThreads / 32];
     previous_done();
     next_may_start();
@@ -87,48 +136,76 @@ __global__ void __launch_bounds__(kThreads) k_averages(const NormGradArgs a, flo
     for (uint64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
         const T *dy = (const T *)a.dy + t * a.ld_dy, *x = (const T *)a.sum + t * a.ld_sum;
         const float mean = a.mean[t], rstd = a.rstd[t];
-        const float2 s = row_sums(a.cols, part, [&](uint32_t i, float2 &w) {
-            const float g = __fmul_rn(widen(dy[i]), a.weight ? widen(((const W *)a.weight)[i]) : 1.f);
-            w.x += g, w.y = __fmaf_rn(g, xhat(widen(x[i]), mean, rstd), w.y);
+        const float2 s = row_sums<T>(a.cols, part, [&](uint32_t i, Two &sum) {
+            float2 d[kPairs], xh[kPairs], w[kPairs];
+            load<T, VEC>(dy + i, a.cols - i, d);
+            load<T, VEC>(x + i, a.cols - i, xh);
+            load_weights<T, VEC>(a.weight, w16, i, a.cols - i, 1.f, w);
+#pragma unroll
+            for (uint32_t k = 0; k < kPairs; ++k) {  // (columns past the last: d is 0, and w)
+                const float2 dxh = __fmul2_rn(d[k], xhat(xh[k], both(-mean), both(rstd)));
+                sum.a = __ffma2_rn(d[k], w[k], sum.a), sum.b = __ffma2_rn(dxh, w[k], sum.b);
+            }
         });
-        if (threadIdx.x == 0) avg[t] = make_float2(s.x * per, s.y * per);
+        if (threadIdx.x == 0) avg[t] = make_float2(s.x * -per, s.y * -per);
     }
 }
 
-// block (x, y): columns from x * kColThreads * kColumns, rows from y * run
-template <typename T, typename W>
-__global__ void __launch_bounds__(kColThreads) k_columns(const NormGradArgs a, const float2 *avg, float *sums, uint32_t run)
+// block (x, y): columns from x * kColThreads * K on, rows from y * run on
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kColThreads) k_columns(const NormGradArgs a, const bool w16, const float2 *avg, float *sums, uint32_t run)
 {
+    constexpr uint32_t kPairs = K<T> / 2;
     previous_done();
     next_may_start();
-    const uint32_t col0 = blockIdx.x * kColThreads * kColumns + threadIdx.x * kColumns;
+    const uint32_t col = (blockIdx.x * kColThreads + threadIdx.x) * K<T>;
+    if (col >= a.cols) return;
+    const uint32_t left = a.cols - col;
+    float2 w[kPairs];
+    load_weights<T, VEC>(a.weight, w16, col, left, 1.f, w);
     for (uint64_t y = blockIdx.y; y * run < a.rows; y += gridDim.y) {
-        float dw[kColumns] = {}, db[kColumns] = {};
+        float2 dw[kPairs] = {}, db[kPairs] = {};
         const uint64_t end = min(a.rows, (y + 1) * run);
+        float2 d[kPairs], x[kPairs], next_d[kPairs] = {}, next_x[kPairs] = {};
+        auto fetch = [&](uint64_t t, float2 (&to_d)[kPairs], float2 (&to_x)[kPairs]) {
+            load<T, VEC>((const T *)a.dy + t * a.ld_dy + col, left, to_d);
+            load<T, VEC>((const T *)a.sum + t * a.ld_sum + col, left, to_x);
+        };
+        fetch(y * run, d, x);
         for (uint64_t t = y * run; t < end; ++t) {
-            const T *dy = (const T *)a.dy + t * a.ld_dy, *x = (const T *)a.sum + t * a.ld_sum;
             const float mean = a.mean[t], rstd = a.rstd[t];
             const float2 s = avg[t];
-            const uint64_t draw = a.mask.level && col0 < a.cols ? a.mask.draw(t, col0 / 4) : 0;
+            float2 g[kPairs];
+            if (t + 1 < end) fetch(t + 1, next_d, next_x);  // (before this row's outputs, which may lie there)
 #pragma unroll
-            for (uint32_t k = 0; k < kColumns; ++k) {
-                const uint32_t i = col0 + k;
-                if (i >= a.cols) continue;
-                const float d = widen(dy[i]), xh = xhat(widen(x[i]), mean, rstd);
-                const float g = __fmul_rn(d, a.weight ? widen(((const W *)a.weight)[i]) : 1.f);
-                const float ds = a.dsum ? gradient(g, xh, s, rstd, widen(((const T *)a.dsum)[t * a.ld_dsum + i])) : gradient(g, xh, s, rstd);
-                dw[k] = __fmaf_rn(d, xh, dw[k]), db[k] += d;
-                if (a.dres) ((T *)a.dres)[t * a.ld_dres + i] = narrow<T>(ds);
-                if (a.dx) ((T *)a.dx)[t * a.ld_dx + i] = narrow<T>(dropped(a.mask, ds, dropout::Mask::field(draw, k) >= a.mask.level));
+            for (uint32_t k = 0; k < kPairs; ++k) {
+                const float2 xh = xhat(x[k], both(-mean), both(rstd));
+                dw[k] = __ffma2_rn(d[k], xh, dw[k]), db[k] = __fadd2_rn(db[k], d[k]);
+                g[k] = centred_gradient(d[k], w[k], xh, both(s.x), both(s.y));
             }
-        }
-        if (sums)
+            if (a.dsum) {
+                float2 ds[kPairs];
+                load<T, VEC>((const T *)a.dsum + t * a.ld_dsum + col, left, ds);
 #pragma unroll
-            for (uint32_t k = 0; k < kColumns; ++k)
-                if (col0 + k < a.cols) {
-                    float *p = sums + 2 * y * a.cols + col0 + k;
-                    p[0] = dw[k], p[a.cols] = db[k];
-                }
+                for (uint32_t k = 0; k < kPairs; ++k) g[k] = __ffma2_rn(both(rstd), g[k], ds[k]);
+            } else {
+#pragma unroll
+                for (uint32_t k = 0; k < kPairs; ++k) g[k] = __fmul2_rn(both(rstd), g[k]);
+            }
+            if (a.dres) store<T, VEC>((T *)a.dres + t * a.ld_dres + col, left, g);
+            if (a.dx) {
+                if (a.mask.level) drop(a.mask, a.mask.base + (t * a.mask.groups + col / 4) * dropout::kGolden, g);
+                store<T, VEC>((T *)a.dx + t * a.ld_dx + col, left, g);
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < kPairs; ++k) d[k] = next_d[k], x[k] = next_x[k];
+        }
+        if (sums) {
+            float *p = sums + 2 * y * a.cols + col;
+#pragma unroll
+            for (uint32_t k = 0; k < K<T>; ++k)
+                if (k < left) p[k] = of(dw, k), p[(uint64_t)a.cols + k] = of(db, k);
+        }
     }
 }
 
@@ -172,11 +249,11 @@ __global__ void __launch_bounds__(1024) k_grad_sum(const float *part, uint32_t p
 
 uint64_t align_up(uint64_t n) { return (n + 255) & ~255ull; }
 
-// into how many runs of rows a column's sum is cut: some blocks an SM
+// into how many runs of rows a column's sum is cut: some blocks an SM, whatever the type
 uint64_t runs_of(const fiona_ctx *ctx, uint32_t cols)
 {
     const uint64_t sms = ctx->sm_count ? ctx->sm_count : 152;
-    const uint64_t ranges = (cols + kColThreads * kColumns - 1) / (kColThreads * kColumns);
+    const uint64_t ranges = (cols + 8 * kColThreads - 1) / (8 * kColThreads);
     return std::max<uint64_t>((8 * sms + ranges - 1) / ranges, 1);
 }
 // their length
@@ -186,27 +263,31 @@ uint32_t run_of(const fiona_ctx *ctx, uint64_t rows, uint32_t cols)
     return (uint32_t)std::max<uint64_t>(std::min<uint64_t>((rows + runs - 1) / runs, kMostRun), 1);
 }
 
-template <typename T, typename W>
-int forward(const NormArgs &a, cudaStream_t s)
+template <typename T>
+int forward(const NormArgs &a, bool w16, cudaStream_t s)
 {
     NormArgs b = a;
-    void *args[] = {&b};
-    return launch(k_norm_any<T, W>, dim3((uint32_t)std::min<uint64_t>(a.rows, 1u << 30)), kThreads, 0, s, args, "layer norm");
+    void *args[] = {&b, &w16};
+    const uint64_t z = sizeof(T);
+    const bool vec = vectors(a.cols, K<T>, {a.x, a.res, a.out, a.sum, a.weight, a.bias}, {a.ldx * z, a.res ? a.ld_res * z : 0, a.ld_out * z, a.sum ? a.ld_sum * z : 0});
+    return launch(vec ? k_norm_any<T, true> : k_norm_any<T, false>, dim3((uint32_t)std::min<uint64_t>(a.rows, 1u << 30)), kThreads, 0, s, args, "layer norm");
 }
 
-template <typename T, typename W>
-int backward(const fiona_ctx *ctx, const NormGradArgs &a, void *work, uint32_t wtype, cudaStream_t s)
+template <typename T>
+int backward(const fiona_ctx *ctx, const NormGradArgs &a, void *work, uint32_t wtype, bool w16, cudaStream_t s)
 {
     NormGradArgs b = a;
     float2 *avg = static_cast<float2 *>(work);
     float *sums = a.dweight || a.dbias ? reinterpret_cast<float *>(static_cast<uint8_t *>(work) + align_up(a.rows * sizeof(float2))) : nullptr;
     uint32_t run = run_of(ctx, a.rows, a.cols);
-    const uint64_t parts = (a.rows + run - 1) / run;
-    void *args[] = {&b, &avg}, *column_args[] = {&b, &avg, &sums, &run};
-    int rc = launch(k_averages<T, W>, dim3((uint32_t)std::min<uint64_t>(a.rows, 1u << 30)), kThreads, 0, s, args, "layer norm averages");
-    const uint32_t ranges = (a.cols + kColThreads * kColumns - 1) / (kColThreads * kColumns);
+    const uint64_t parts = (a.rows + run - 1) / run, z = sizeof(T);
+    const bool vec = vectors(a.cols, K<T>, {a.dy, a.sum, a.dsum, a.dx, a.dres, a.weight},
+                             {a.ld_dy * z, a.ld_sum * z, a.dsum ? a.ld_dsum * z : 0, a.dx ? a.ld_dx * z : 0, a.dres ? a.ld_dres * z : 0});
+    void *args[] = {&b, &w16, &avg}, *column_args[] = {&b, &w16, &avg, &sums, &run};
+    int rc = launch(vec ? k_averages<T, true> : k_averages<T, false>, dim3((uint32_t)std::min<uint64_t>(a.rows, 1u << 30)), kThreads, 0, s, args, "layer norm averages");
+    const uint32_t ranges = (a.cols + kColThreads * K<T> - 1) / (kColThreads * K<T>);
     if (rc == FIONA_OK)
-        rc = launch(k_columns<T, W>, dim3(ranges, (uint32_t)std::min<uint64_t>(parts, 65535)), kColThreads, 0, s, column_args, "layer norm columns");
+        rc = launch(vec ? k_columns<T, true> : k_columns<T, false>, dim3(ranges, (uint32_t)std::min<uint64_t>(parts, 65535)), kColThreads, 0, s, column_args, "layer norm columns");
     if (rc == FIONA_OK && sums) rc = launch_norm_grad_sum(s, wtype, sums, (uint32_t)parts, a.cols, a.dweight, a.dbias);
     return rc;
 }
@@ -223,23 +304,16 @@ uint64_t norm_any_grad_work(const fiona_ctx *ctx, uint64_t rows, uint32_t cols)
 int launch_norm_any(const fiona_ctx *, void *stream, uint32_t dtype, uint32_t wtype, const NormArgs &a)
 {
     cudaStream_t s = (cudaStream_t)stream;
-    switch (dtype) {
-        case FIONA_F32: return forward<float, float>(a, s);
-        case FIONA_F16: return wtype == FIONA_F32 ? forward<__half, float>(a, s) : forward<__half, __half>(a, s);
-        default: return wtype == FIONA_F32 ? forward<__nv_bfloat16, float>(a, s) : forward<__nv_bfloat16, __nv_bfloat16>(a, s);
-    }
+    const bool w16 = wtype == dtype;
+    return dtype == FIONA_F32 ? forward<float>(a, w16, s) : dtype == FIONA_F16 ? forward<__half>(a, w16, s) : forward<__nv_bfloat16>(a, w16, s);
 }
 
 int launch_norm_any_grad(const fiona_ctx *ctx, void *stream, uint32_t dtype, uint32_t wtype, const NormGradArgs &a, void *work)
 {
     cudaStream_t s = (cudaStream_t)stream;
-    switch (dtype) {
-        case FIONA_F32: return backward<float, float>(ctx, a, work, wtype, s);
-        case FIONA_F16: return wtype == FIONA_F32 ? backward<__half, float>(ctx, a, work, wtype, s) : backward<__half, __half>(ctx, a, work, wtype, s);
-        default:
-            return wtype == FIONA_F32 ? backward<__nv_bfloat16, float>(ctx, a, work, wtype, s)
-                                      : backward<__nv_bfloat16, __nv_bfloat16>(ctx, a, work, wtype, s);
-    }
+    const bool w16 = wtype == dtype;
+    return dtype == FIONA_F32   ? backward<float>(ctx, a, work, wtype, w16, s)
+           : dtype == FIONA_F16 ? backward<__half>(ctx, a, work, wtype, w16, s) : backward<__nv_bfloat16>(ctx, a, work, wtype, w16, s);
 }
 
 int launch_norm_grad_sum(void *stream, uint32_t wtype, const float *part, uint32_t parts, uint32_t cols, void *dweight, void *dbias)

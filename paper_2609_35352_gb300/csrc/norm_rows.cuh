@@ -17,7 +17,6 @@
 // k_grad_sum adds up the blocks' in order.
 #pragma once
 #include <algorithm>
-#include <initializer_list>
 
 #include "async.cuh"
 #include "norm.cuh"
@@ -29,90 +28,6 @@ namespace layernorm {
 constexpr uint32_t ahead(uint32_t row_bytes, uint32_t tensors, uint32_t room, uint32_t most)
 {
     return most == 1 || row_bytes * tensors * most <= room ? most : ahead(row_bytes, tensors, room, most - 1);
-}
-
-// K elements as they lie in 16 bytes.  A thread's share of a row is so many of them, LANES
-// apart: the threads of a warp read and write 512 bytes one after another (eight fp32 a
-// thread would be halves of 32-byte sectors, each of them written twice).
-template <typename T>
-constexpr uint32_t K = 16 / sizeof(T);
-
-template <typename T>
-struct Vector {
-    uint4 u;
-    __device__ __forceinline__ const T *values() const { return reinterpret_cast<const T *>(&u); }
-    __device__ __forceinline__ T *values() { return reinterpret_cast<T *>(&u); }
-    __device__ __forceinline__ void widened(float2 (&v)[K<T> / 2]) const
-    {
-#pragma unroll
-        for (uint32_t i = 0; i < K<T> / 2; ++i) v[i] = make_float2(widen(values()[2 * i]), widen(values()[2 * i + 1]));
-    }
-};
-
-template <typename T, bool VEC>
-__device__ __forceinline__ void load(const T *p, uint32_t left, float2 (&v)[K<T> / 2])  // left: columns from p on
-{
-    if (VEC) {
-        const Vector<T> x{*reinterpret_cast<const uint4 *>(p)};
-        x.widened(v);
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < K<T> / 2; ++i)
-            v[i] = make_float2(2 * i < left ? widen(p[2 * i]) : 0.f, 2 * i + 1 < left ? widen(p[2 * i + 1]) : 0.f);
-    }
-}
-
-template <typename T>
-__device__ __forceinline__ uint4 narrowed(const float2 (&v)[K<T> / 2])
-{
-    Vector<T> x;
-#pragma unroll
-    for (uint32_t i = 0; i < K<T> / 2; ++i) x.values()[2 * i] = narrow<T>(v[i].x), x.values()[2 * i + 1] = narrow<T>(v[i].y);
-    return x.u;
-}
-
-// column i of a share
-template <uint32_t N>
-__device__ __forceinline__ float of(const float2 (&v)[N], uint32_t i) { return i % 2 ? v[i / 2].y : v[i / 2].x; }
-
-// weights or biases of the columns from `col` on (null: `none`), from global memory
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_weights(const void *p, bool w16, uint32_t col, uint32_t left, float none, float2 (&v)[K<T> / 2])
-{
-    if (!p) {
-#pragma unroll
-        for (uint32_t i = 0; i < K<T> / 2; ++i) v[i] = both(none);
-    } else if (w16 || sizeof(T) == 4) {
-        load<T, VEC>((const T *)p + col, left, v);
-    } else if (VEC) {
-#pragma unroll
-        for (uint32_t i = 0; i < K<T>; i += 4) {
-            const float4 f = *reinterpret_cast<const float4 *>((const float *)p + col + i);
-            v[i / 2] = make_float2(f.x, f.y), v[i / 2 + 1] = make_float2(f.z, f.w);
-        }
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < K<T> / 2; ++i)
-            v[i] = make_float2(2 * i < left ? ((const float *)p)[col + 2 * i] : 0.f, 2 * i + 1 < left ? ((const float *)p)[col + 2 * i + 1] : 0.f);
-    }
-}
-
-// The mask of N pairs of columns, whose draws are z and those behind it, on their values.  Fields
-// in the places of a word's upper half are compared with the lower half behind them, which
-// decides nothing: upper >= level is word > (level << 16) - 1, for a level of 65536 too.
-template <uint32_t N>
-__device__ __forceinline__ void drop(const dropout::Mask &m, uint64_t z, float2 (&v)[N])
-{
-    const uint32_t limit = (m.level << 16) - 1;
-#pragma unroll
-    for (uint32_t d = 0; d < N; d += 2) {
-        const uint64_t draw = dropout::mix64(z + d / 2 * dropout::kGolden);
-#pragma unroll
-        for (uint32_t i = 0; i < 2; ++i) {
-            const uint32_t word = (uint32_t)(draw >> (32 * i));
-            v[d + i] = dropped(m, v[d + i], word << 16 > limit, word > limit);
-        }
-    }
 }
 
 // Rows ahead in a backward pass (16384 x 4096 bf16 97 us; one 115, three 99), their room beside
@@ -528,14 +443,6 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
             for (uint32_t k = 1; k < kGroups; ++k) v += s[2 * k * kTable + at];
             out[which * a.cols + j] = v;
         }
-}
-
-inline bool vectors(uint32_t cols, uint32_t k, std::initializer_list<const void *> starts, std::initializer_list<uint64_t> bytes)
-{
-    uint64_t all = 0;
-    for (const void *p : starts) all |= (uint64_t)(uintptr_t)p;
-    for (uint64_t b : bytes) all |= b;
-    return cols % k == 0 && all % 16 == 0;
 }
 
 template <typename T, uint32_t LANES, uint32_t VECS>

@@ -19,7 +19,7 @@ from adapter_util import keep_mask  # noqa: E402
 DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 SHAPES = [(1, 1, 0), (1, 768, 0), (3, 5, 0), (17, 64, 0), (300, 777, 0), (64, 1024, 0), (33, 256, 2), (33, 250, 8),
           (5, 4099, 3), (2, 65536, 0), (1, 1 << 20, 0), (1000, 8, 0), (2047, 33, 0), (7, 16384, 0), (5, 16392, 0), (130, 2048, 0),
-          (40, 8192, 0), (37, 640, 0), (9, 765, 3), (9, 12288, 8), (11, 4096, 0), (10, 511, 1), (700, 264, 0), (3, 32768, 0), (4, 20000, 0)]
+          (40, 8192, 0), (37, 640, 0), (9, 765, 3), (9, 12288, 8), (11, 4096, 0), (10, 511, 1), (700, 264, 0), (3, 32768, 0), (4, 20000, 0), (3, 20001, 0), (300, 16411, 2)]
 
 
 @pytest.fixture(scope="module")
@@ -158,7 +158,7 @@ def test_probabilities(ctx, dtype, p):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("cols", [256, 768, 2048, 4096, 8192, 16384])
+@pytest.mark.parametrize("cols", [256, 768, 2048, 4096, 8192, 16384, 20000])
 def test_strides_and_alignment_change_nothing(ctx, dtype, cols):
     """Rows apart, rows and weights off 16 bytes: the same results, to the last bit, as whole
     vectors side by side."""
