@@ -420,7 +420,7 @@ def test_reset_and_checkpoints(ctx):
             p.copy_(t)
         o.reset(stream=s)
         assert o.steps.tolist() == [0] and (o.m == 0).all() and (o.v == 0).all()
-        assert torch.equal(o.master[:3000], first[0].view(-1).float()) and (o.master[3000:3072] == 0).all()
+        assert torch.equal(o.master[:3000], first[0].view(-1).float()) and (o.master[3000:int(o.places[1])] == 0).all()
         for _ in range(5):
             o.step(stream=s)
         assert same(want, state_of(o, params))
