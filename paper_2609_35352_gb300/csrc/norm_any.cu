@@ -211,25 +211,27 @@ __global__ void __launch_bounds__(kColThreads) k_columns(const NormGradArgs a, c
 
 // dweight (blockIdx.y = 0) and dbias (1): 32 columns a block.  A thread's sums are taken
 // kMostParts at a time, and what is lost where those are added up goes into the next (Kahan):
-// 2^30 rows have 2048 parts along a thread, 3e-5 of a sum whose roundings go one way.  (For
-// every part: 2.7 us more of 304 parts of 4096 columns.)
-constexpr uint32_t kMostParts = 64;
+// of 2^30 rows a thread has thousands, and 2048 in one sum whose roundings go one way were 3e-5
+// off.  (For every part: 2.7 us more of 304 parts of 4096 columns.)  kSumRows: 32 would leave
+// one block an SM (4096 x 8192 fp32, all of it: 95 us for 93), 8 too few parts under way
+// (1531 x 777 fp16: 13.3 us for 12.2).
+constexpr uint32_t kMostParts = 64, kSumRows = 16;
 template <typename W>
-__global__ void __launch_bounds__(1024) k_grad_sum(const float *part, uint32_t parts, uint32_t cols, W *dweight, W *dbias)
+__global__ void __launch_bounds__(32 * kSumRows) k_grad_sum(const float *part, uint32_t parts, uint32_t cols, W *dweight, W *dbias)
 {
-    __shared__ float s[32][33];
+    __shared__ float s[kSumRows][33];
     previous_done();
     const uint32_t x = threadIdx.x & 31, y = threadIdx.x / 32, i = blockIdx.x * 32 + x;
     W *out = blockIdx.y ? dbias : dweight;
     float v[4] = {}, rest[4] = {};
     if (i < cols && out)
-        for (uint32_t begin = 0; begin < parts; begin += 128 * kMostParts) {
+        for (uint32_t begin = 0; begin < parts; begin += 4 * kSumRows * kMostParts) {
             float w[4] = {};
 #pragma unroll 2
-            for (uint32_t k = begin + y, end = min(parts, begin + 128 * kMostParts); k < end; k += 128)
+            for (uint32_t k = begin + y, end = min(parts, begin + 4 * kSumRows * kMostParts); k < end; k += 4 * kSumRows)
 #pragma unroll
                 for (uint32_t q = 0; q < 4; ++q)
-                    if (k + 32 * q < end) w[q] += part[(2ull * (k + 32 * q) + blockIdx.y) * cols + i];
+                    if (k + kSumRows * q < end) w[q] += part[(2ull * (k + kSumRows * q) + blockIdx.y) * cols + i];
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q) {
                 const float p = __fadd_rn(w[q], rest[q]), sum = __fadd_rn(v[q], p);
@@ -242,7 +244,7 @@ __global__ void __launch_bounds__(1024) k_grad_sum(const float *part, uint32_t p
     if (y == 0 && i < cols && out) {
         float r = 0.f;
 #pragma unroll
-        for (uint32_t k = 0; k < 32; ++k) r += s[k][x];
+        for (uint32_t k = 0; k < kSumRows; ++k) r += s[k][x];
         out[i] = narrow<W>(r);
     }
 }
@@ -321,5 +323,5 @@ int launch_norm_grad_sum(void *stream, uint32_t wtype, const float *part, uint32
     void *args[] = {&part, &parts, &cols, &dweight, &dbias};
     const void *k = wtype == FIONA_F32 ? (const void *)k_grad_sum<float>
                     : wtype == FIONA_F16 ? (const void *)k_grad_sum<__half> : (const void *)k_grad_sum<__nv_bfloat16>;
-    return launch(k, dim3((cols + 31) / 32, 2), 1024, 0, (cudaStream_t)stream, args, "layer norm sums");
+    return launch(k, dim3((cols + 31) / 32, 2), 32 * kSumRows, 0, (cudaStream_t)stream, args, "layer norm sums");
 }

@@ -4,7 +4,7 @@
 // dresidual (and dsum) once.  16384 x 4096 bf16 with dropout, 537 MB either way: forward
 // 82 us (6.5 TB/s, of 6.8 that a copy reaches), backward with dweight and dbias 97 us (5.5;
 // warps issue 58% of the time, 10 of 36 instructions an element for the mask, and 16 warps
-// an SM hide no more of a row's chain of sums); 4096 x 8192 fp32 backward 95 us (5.6: its
+// an SM hide no more of a row's chain of sums); 4096 x 8192 fp32 backward 94 us (5.7: its
 // rows ahead leave room for one block an SM).
 //
 // A row is spread over LANES threads, 8 to 32
