@@ -100,6 +100,9 @@ __device__ __forceinline__ float2 scaled(float2 d, float2 rstd, float2 shift, fl
     return __ffma2_rn(__ffma2_rn(d, rstd, shift), weight, bias);
 }
 __device__ __forceinline__ float2 xhat(float2 s, float2 minus_mean, float2 rstd) { return __fmul2_rn(__fadd2_rn(s, minus_mean), rstd); }
+// 0 in the place of columns past the last: (0 - mean) rstd may be infinite there, of a row of equal
+// values far from zero, whose own xh are 0
+__device__ __forceinline__ float2 inside_only(float2 xh, uint32_t col, uint32_t cols) { return make_float2(col < cols ? xh.x : 0.f, col + 1 < cols ? xh.y : 0.f); }
 __device__ __forceinline__ float2 centred_gradient(float2 dy, float2 weight, float2 xh, float2 minus_avg_g, float2 minus_avg_gxh)
 {
     return __ffma2_rn(xh, minus_avg_gxh, __ffma2_rn(dy, weight, minus_avg_g));

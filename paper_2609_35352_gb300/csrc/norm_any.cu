@@ -142,8 +142,10 @@ __global__ void __launch_bounds__(kThreads) k_averages(const NormGradArgs a, con
             load<T, VEC>(x + i, a.cols - i, xh);
             load_weights<T, VEC>(a.weight, w16, i, a.cols - i, 1.f, w);
 #pragma unroll
-            for (uint32_t k = 0; k < kPairs; ++k) {  // (columns past the last: d is 0, and w)
-                const float2 dxh = __fmul2_rn(d[k], xhat(xh[k], both(-mean), both(rstd)));
+            for (uint32_t k = 0; k < kPairs; ++k) {  // (columns past the last: d, xh and w are 0)
+                xh[k] = xhat(xh[k], both(-mean), both(rstd));
+                if (!VEC) xh[k] = inside_only(xh[k], i + 2 * k, a.cols);
+                const float2 dxh = __fmul2_rn(d[k], xh[k]);
                 sum.a = __ffma2_rn(d[k], w[k], sum.a), sum.b = __ffma2_rn(dxh, w[k], sum.b);
             }
         });

@@ -350,14 +350,17 @@ __global__ void __launch_bounds__(backward_threads(LANES), backward_blocks(LANES
             __syncthreads();
         }
     }
-    // dy, xh and weights of vector e of the row taken (columns past the last: dy is 0)
+    // dy, xh and weights of vector e of the row taken (columns past the last: dy and xh are 0)
     auto take = [&](uint32_t e, float mean, float rstd, float2 (&d)[K<T> / 2], float2 (&xh)[K<T> / 2], float2 (&w)[K<T> / 2]) {
         const uint32_t col = e * LANES * K<T> + at;
         ring.read(0, e, d), ring.read(1, e, xh);
         if (kHeld && a.weight) held.read(0, e, w);
         else load_weights<T, VEC>(a.weight, w16, col, a.cols - col, 1.f, w);
 #pragma unroll
-        for (uint32_t i = 0; i < K<T> / 2; ++i) xh[i] = xhat(xh[i], both(-mean), both(rstd));
+        for (uint32_t i = 0; i < K<T> / 2; ++i) {
+            xh[i] = xhat(xh[i], both(-mean), both(rstd));
+            if (!VEC) xh[i] = inside_only(xh[i], col + 2 * i, a.cols);
+        }
     };
     uint32_t slot = 0;
     for (; t < rows; t += step, dx += step_dx, dres += step_dr, z += step_z, slot ^= 1) {

@@ -412,3 +412,28 @@ def test_first_calls_in_a_capture(ctx):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST_CALLS % root], capture_output=True, text=True, timeout=300, cwd=root)
     assert r.returncode == 0 and "well" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [1, 3, 8, 776, 777, 5003, 20000, 20001])
+def test_gradient_of_flat_rows_far_from_zero(ctx, dtype, cols):
+    """Rows of one value: xh is 0 at every column, whatever (0 - mean) rstd would be behind the last."""
+    dy, s, dsum = make(9, cols, dtype, 0, 1), make(9, cols, dtype, 0, 2, 2.0, 0.5), make(9, cols, dtype, 0, 3)
+    mean, rstd = s.double().mean(1).float(), (s.double().var(1, unbiased=False) + 1e-5).rsqrt().float()
+    weight, work = vector(cols, dtype, 4, 0.2, 1.0), LN.workspace(ctx, 9, cols)
+
+    def call(extra):
+        g = {"dx": torch.empty_like(dy), "dresidual": torch.empty_like(dy), "dweight": torch.empty_like(weight), "dbias": torch.empty_like(weight)}
+        LN.layer_norm_backward(ctx, dy, s, mean, rstd, weight=weight, dsum=extra, work=work, **g)
+        return g
+
+    clean = [call(extra) for extra in (None, dsum)]
+    flat = {2: 2e36, 5: torch.finfo(DT[dtype]).min, 7: 1e33}
+    for t, value in flat.items():
+        s[t] = value
+        mean[t], rstd[t] = s[t, 0].float(), 1e-5 ** -0.5 if t != 7 else 1e-12 ** -0.5
+    good = [t for t in range(9) if t not in flat]
+    for extra, before in zip((None, dsum), clean):
+        got = call(extra)
+        check_all(dtype, dtype, got, NU.backward(f64(dy), f64(s), f64(mean), f64(rstd), f64(weight), f64(extra)))
+        assert all(torch.equal(got[k][good], before[k][good]) for k in ("dx", "dresidual"))
