@@ -31,15 +31,18 @@
  *            but v > 0 to no less than code 1 (a v of zero beside an m that is not would
  *            take a step of m / eps).  A step uses m and v before they are rounded.
  *            Largest |m| or u below 2^-100 count as zero (u is taken from v at or above
- *            2^-126).  A block with an m or v that is not finite gets a scale of NaN.
+ *            2^-126).  A block with an m or v that is not finite gets scales of NaN: what
+ *            this step does to its weights is still the formula's, after the next step
+ *            all of them are NaN.
  * master (optional): fp32 [places], the weights that 16-bit tensors are rounded from;
  * then their own tensors are written, but not read.  fp32 tensors do not use theirs.
  *
  * Arithmetic: fp32, from gradients in the weights' type; beta^t from t log beta in fp64.
- * A weight is rounded once (to nearest).  A norm is summed in two fp32 parts, as good as
- * from fp64; where squares or their sums pass fp32's range (a norm above 1.8e19) it counts
- * as infinite.  Codes are those of the formulas step by step, each product, sum, quotient
- * and root rounded to nearest by itself:
+ * A weight is rounded once (to nearest).  Where the square of k g passes fp32's range (k g
+ * above 1.8e19) v is infinite, and the step of that weight none.  A norm is summed in two
+ * fp32 parts, as good as from fp64; where squares or their sums pass fp32's range (a norm
+ * above 1.8e19) it counts as infinite.  Codes are those of the formulas step by step, each
+ * product, sum, quotient and root rounded to nearest by itself:
  *   m = beta1 m + (1 - beta1) (k g),  v = beta2 v + (1 - beta2) ((k g) (k g)),  u = sqrt(v),
  *   q = rint(sqrt(top^2 (|m| / scale) - 1/4)) with top 127, or u in the place of |m| with
  *   255, and back (q |q|) (scale (1 / 127^2)),

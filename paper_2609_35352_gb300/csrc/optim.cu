@@ -283,17 +283,17 @@ __device__ __forceinline__ float block_scale(float most)
     return u >= 0x7F800000u ? __uint_as_float(0x7FFFFFFFu) : u < __float_as_uint(kTiny) ? 0.f : __uint_as_float(u);
 }
 // A root to nearest: one step of Newton's on the reciprocal root, its residual exact by an
-// fma (Markstein, IBM J. Res. Dev. 34, 1990).  What is below 2^-126 counts as zero.
+// fma (Markstein, IBM J. Res. Dev. 34, 1990).  What is below 2^-126 counts as zero.  Of zero
+// and of infinity the steps give NaN; v 2^-64, which is no more than any other root, is the
+// root itself there, and the larger of the two is the root in each case (NaN where v is).
 __device__ __forceinline__ float2 roots(float2 v)
 {
-    float2 s, r, y;
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, 1.17549435e-38f)));
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(v.y, 1.17549435e-38f)));
-    asm("mul.rn.ftz.f32 %0, %1, %2;" : "=f"(s.x) : "f"(v.x), "f"(y.x));
-    asm("mul.rn.ftz.f32 %0, %1, %2;" : "=f"(s.y) : "f"(v.y), "f"(y.y));
-    asm("fma.rn.ftz.f32 %0, %1, %2, %3;" : "=f"(r.x) : "f"(-s.x), "f"(s.x), "f"(v.x));
-    asm("fma.rn.ftz.f32 %0, %1, %2, %3;" : "=f"(r.y) : "f"(-s.y), "f"(s.y), "f"(v.y));
-    return __ffma2_rn(r, __fmul2_rn(y, both(0.5f)), s);
+    float2 y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(v.x));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(v.y));
+    const float2 s = __fmul2_rn(v, y), r = __ffma2_rn(make_float2(-s.x, -s.y), s, v);
+    const float2 u = __ffma2_rn(r, __fmul2_rn(y, both(0.5f)), s), least = __fmul2_rn(v, both(5.4210109e-20f));
+    return make_float2(fmaxf(u.x, least.x), fmaxf(u.y, least.y));
 }
 
 // Codes are what the formulas give step by step, each operation rounded to nearest: the

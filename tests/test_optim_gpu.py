@@ -482,3 +482,37 @@ def test_many_elements(ctx):
     tail = o.m[(n + 255) // 256 * 256 - (k + 255) // 256 * 256:][:k]
     assert (tail.int() - alone.m[:k].int()).abs().max() <= 1
     assert (o.m[:1 << 20] == 0).all() and (p[:1 << 20] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bits,master", [(32, False), (8, False), (8, True)])
+@pytest.mark.parametrize("n", [300, 5000, 6_000_000])
+def test_squares_past_fp32(ctx, dtype, bits, master, n):
+    """A finite gradient whose square is infinite: v is, so the step is none and decay alone moves
+    its weight, in either width of the moments; other weights are as without it."""
+    p, g = normal((n,), DT[dtype], 1), normal((n,), DT[dtype], 2, 1e-2)
+    q, h = p.clone(), g.clone()
+    at = [0, 17, 256 + 3, n - 1]
+    for i in at[:-1]:
+        g[i] = 2e19
+    g[at[-1]] = -3e38
+    s = torch.cuda.current_stream()
+    opts = [O.AdamW(ctx, [w], [d], lr=0.1, state_bits=bits, master=master) for w, d in ((p, g), (q, h))]
+    old = p.clone()
+    for o in opts:
+        o.step(stream=s)
+    w = f64(old)[at]
+    # (lr and weight decay are rounded, then their product and the weight)
+    OU.check("weights", dtype, f64(p)[at], w - 0.1 * 0.01 * w, 4 * OU.U * 0.001 * np.abs(w) + OU.U * np.abs(w))
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[at] = False
+    assert torch.equal(p[keep], q[keep])
+    if bits == 8:
+        blocks = sorted({i // 256 for i in at})
+        for o in opts[:1]:
+            scales = torch.stack([o.m_scale, o.v_scale])
+            assert torch.isnan(scales[:, blocks]).all()
+            others = [b for b in range(scales.shape[1]) if b not in blocks]
+            assert torch.equal(scales[:, others], torch.stack([opts[1].m_scale, opts[1].v_scale])[:, others])
+    else:
+        assert torch.isinf(opts[0].v[at]).all() and torch.isfinite(opts[0].m).all()
