@@ -40,9 +40,11 @@
  * Arithmetic: fp32, from gradients in the weights' type; beta^t from t log beta in fp64.
  * A weight is rounded once (to nearest).  Where the square of k g passes fp32's range (k g
  * above 1.8e19) v is infinite, and the step of that weight none.  A norm is summed in two
- * fp32 parts, as good as from fp64; where squares or their sums pass fp32's range (a norm
- * above 1.8e19) it counts as infinite.  Codes are those of the formulas step by step, each
- * product, sum, quotient and root rounded to nearest by itself:
+ * fp32 parts, as good as from fp64, for gradients from 1e-15 on (below, what squares lose
+ * leaves fp32's range, and below 1e-19 digits of the squares themselves; below 2.6e-23 they
+ * count as zero); where squares or their sums pass that range (a norm above 1.8e19) it
+ * counts as infinite.  Codes are those of the formulas step by step, each product, sum,
+ * quotient and root rounded to nearest by itself:
  *   m = beta1 m + (1 - beta1) (k g),  v = beta2 v + (1 - beta2) ((k g) (k g)),  u = sqrt(v),
  *   q = rint(sqrt(top^2 (|m| / scale) - 1/4)) with top 127, or u in the place of |m| with
  *   255, and back (q |q|) (scale (1 / 127^2)),

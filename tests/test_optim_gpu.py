@@ -1,5 +1,7 @@
 """AdamW over many tensors against the formulas in 64 bits (optim_util.py derives what
 rounding may do)."""
+import math
+
 import numpy as np
 import pytest
 
@@ -516,3 +518,35 @@ def test_squares_past_fp32(ctx, dtype, bits, master, n):
             assert torch.equal(scales[:, others], torch.stack([opts[1].m_scale, opts[1].v_scale])[:, others])
     else:
         assert torch.isinf(opts[0].v[at]).all() and torch.isfinite(opts[0].m).all()
+
+
+@pytest.mark.parametrize("groups,offset", [(300, 0), (300, 1), (1600, 0), (1600, 1)])
+def test_norms_of_equal_gradients(ctx, groups, offset):
+    """4096 equal fp32 gradients c a group, whose squares lose the same in every product: the norm is
+    64 c to the last bit, and the factor of clipping the nearest to max_norm / (64 c).  (What the sums
+    in two parts leave is some 2^-40 of the norm: of 1900 factors none lies that near a border.)"""
+    flat = torch.zeros(groups * 4096 + offset, device="cuda")
+    g = flat[offset:].view(groups, 4096)
+    c = normal((groups, 1), torch.float32, 7).abs() + 0.01
+    g.copy_(c.expand(groups, 4096))
+    p = torch.zeros(groups * 4096 + offset, device="cuda")[offset:].view(groups, 4096)
+    o = O.AdamW(ctx, [p], [g], groups=[list(range(groups))], betas=(0.0, 0.999), max_norm=0.1)
+    o.step(stream=torch.cuda.current_stream())
+    c = c[:, 0].cpu().numpy()
+    assert np.array_equal(o.norms.cpu().numpy(), c * np.float32(64))
+    k = np.minimum(0.1 / (64 * c.astype(np.float64)), 1.0).astype(np.float32)
+    assert np.array_equal(o.m.view(groups, 4096).cpu().numpy(), np.broadcast_to((k * c)[:, None], (groups, 4096)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_norms_to_the_last_bit(ctx, dtype):
+    """Norms of gradients of all sizes, some far larger than others, are those of 64 bits, rounded."""
+    sizes = [1, 2, 33, 256, 1000, 4096, 70001, 1 << 20] * 20
+    grads = [(normal((n,), torch.float32, 40 + i) * torch.exp(normal((n,), torch.float32, 400 + i, 4.0))).clamp(-6e4, 6e4).to(DT[dtype])
+             for i, n in enumerate(sizes)]
+    params = [torch.zeros_like(g) for g in grads]
+    o = O.AdamW(ctx, params, grads, groups=list(range(len(sizes))), max_norm=1.0)
+    o.step(stream=torch.cuda.current_stream())
+    # (squares are exact in 64 bits, and math.fsum has no error of its own)
+    want = [math.sqrt(math.fsum((f64(g) ** 2).tolist())) for g in grads]
+    assert np.array_equal(o.norms.cpu().numpy(), np.array(want, dtype=np.float32))
