@@ -32,7 +32,10 @@
  * goes by the sum, mean and rstd that it is given.  Results do not depend on the
  * order in which blocks run: no atomics on values; a row's do not depend on the rows
  * beside it.  A row with an infinity or a NaN that is not dropped comes out as NaN, and
- * no other row does; one whose squares pass fp32's range has rstd 0.
+ * no other row does (but one of equal values with an eps of 0): where the sum or the
+ * squares of finite s pass fp32's range the row is taken again in units of 2^80, and its
+ * rstd may be below fp32's normal numbers.  A row of the gradient is finite as far as the
+ * differences, products and sums of the formulas above are, in fp32.
  *
  * Errors, ownership, streams and devices as in fiona.h.
  */

@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <initializer_list>
+#include <type_traits>
 
 #include "launch.cuh"
 #include "norm.h"
@@ -66,6 +67,24 @@ __device__ __forceinline__ float rstd_of(float avg_d, float avg_dd, float eps)
 {
     const float var = __fmaf_rn(-avg_d, avg_d, avg_dd);
     return rsqrtf(__fadd_rn(var < 0.f ? 0.f : var, eps));
+}
+
+// Far rows, whose sum of squares is not finite, are taken again in units of 2^80: 2^20 columns'
+// squares add up to 2^116 at most there.  Where the mean is 2^100 or more, or its sum not finite,
+// `about` is 0, so that every finite row has finite d.  An eps that is not zero is no less than
+// 2^-126 in these units: so little beside a variance that is not zero itself (2^-52 or more)
+// that it does not show, and equal values come out as 0 times a finite rstd.
+constexpr float kUnit = 0x1p80f, kPerUnit = 0x1p-80f;
+template <typename T>  // (fp16's values and a residual, by whatever factor of the dropout, stay far below)
+constexpr bool kFarRows = !std::is_same<T, __half>::value;
+template <typename T>
+__device__ __forceinline__ float about_of(float mean) { return !kFarRows<T> || fabsf(mean) < 0x1p100f ? mean : 0.f; }
+__device__ __forceinline__ bool infinite(float sum) { return !(sum <= 3.402823466e38f); }
+__device__ __forceinline__ float far_eps(float eps) { return eps == 0.f ? 0.f : fmaxf(__fmul_rn(__fmul_rn(eps, kPerUnit), kPerUnit), 1.17549435e-38f); }
+// rstd of s itself
+__device__ __forceinline__ float far_rstd(float rstd, float2 avg, float eps)
+{
+    return __fmaf_rn(-avg.x, avg.x, avg.y) <= 0.f ? rsqrtf(eps) : __fmul_rn(rstd, kPerUnit);
 }
 
 // weight (d - left) rstd + bias

@@ -66,37 +66,58 @@ __device__ __forceinline__ void store(T *p, uint32_t left, const float2 (&v)[K<T
     }
 }
 
+// A row of a forward call.  FAR: s is taken in units of 2^80.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_norm_any(const NormArgs a, const bool w16)
-{
-    constexpr uint32_t kPairs = K<T> / 2;
-    __shared__ float2 part[kThreads / 32];
-    previous_done();
-    next_may_start();
-    const float per = 1.f / (float)a.cols;
-    for (uint64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
-        const T *x = (const T *)a.x + t * a.ldx, *res = (const T *)a.res + t * a.ld_res;
-        const uint64_t z = a.mask.base + t * a.mask.groups * dropout::kGolden;  // the row's first draw
-        // (columns past the last are 0)
-        auto take = [&](uint32_t i, float2 (&v)[kPairs]) {
-            load<T, VEC>(x + i, a.cols - i, v);
-            if (a.mask.level) drop(a.mask, z + (uint64_t)(i / 4) * dropout::kGolden, v);
-            if (a.res) {
-                float2 r[kPairs];
-                load<T, VEC>(res + i, a.cols - i, r);
+struct Row {
+    static constexpr uint32_t kPairs = K<T> / 2;
+    const NormArgs &a;
+    const T *x, *res;
+    uint64_t t, z;  // z: the row's first draw
+    bool w16;
+    float2 *part;
+    __device__ __forceinline__ Row(const NormArgs &a, uint64_t t, bool w16, float2 *part)
+        : a(a), x((const T *)a.x + t * a.ldx), res((const T *)a.res + t * a.ld_res), t(t), z(a.mask.base + t * a.mask.groups * dropout::kGolden), w16(w16), part(part)
+    {
+    }
+
+    template <bool FAR>
+    __device__ __forceinline__ void shrink(float2 (&v)[kPairs]) const
+    {
+        if (FAR)
 #pragma unroll
-                for (uint32_t k = 0; k < kPairs; ++k) v[k] = __fadd2_rn(v[k], r[k]);
-            }
-        };
-        const float about = row_sums<T>(a.cols, part, [&](uint32_t i, Two &w) {
+            for (uint32_t k = 0; k < kPairs; ++k) v[k] = __fmul2_rn(v[k], both(kPerUnit));
+    }
+    // s of a vector of columns (past the last: 0)
+    __device__ __forceinline__ void take(uint32_t i, float2 (&v)[kPairs]) const
+    {
+        load<T, VEC>(x + i, a.cols - i, v);
+        if (a.mask.level) drop(a.mask, z + (uint64_t)(i / 4) * dropout::kGolden, v);
+        if (a.res) {
+            float2 r[kPairs];
+            load<T, VEC>(res + i, a.cols - i, r);
+#pragma unroll
+            for (uint32_t k = 0; k < kPairs; ++k) v[k] = __fadd2_rn(v[k], r[k]);
+        }
+    }
+    template <bool FAR>
+    __device__ __forceinline__ float sum() const
+    {
+        return row_sums<T>(a.cols, part, [&](uint32_t i, Two &w) {
             float2 v[kPairs];
             take(i, v);
+            shrink<FAR>(v);
 #pragma unroll
             for (uint32_t k = 0; k < kPairs; ++k) w.a = __fadd2_rn(w.a, v[k]);
-        }).x * per;
-        const float2 s = row_sums<T>(a.cols, part, [&](uint32_t i, Two &w) {
+        }).x;
+    }
+    // of d = s - about and of d^2
+    template <bool FAR>
+    __device__ __forceinline__ float2 squares(float about) const
+    {
+        return row_sums<T>(a.cols, part, [&](uint32_t i, Two &w) {
             float2 v[kPairs];
             take(i, v);
+            shrink<FAR>(v);
 #pragma unroll
             for (uint32_t k = 0; k < kPairs; ++k) {
                 float2 d = __fadd2_rn(v[k], both(-about));
@@ -105,7 +126,11 @@ __global__ void __launch_bounds__(kThreads) k_norm_any(const NormArgs a, const b
                 w.a = __fadd2_rn(w.a, d), w.b = __ffma2_rn(d, d, w.b);
             }
         });
-        const float left = s.x * per, rstd = rstd_of(left, s.y * per, a.eps), shift = shift_of(left, rstd);
+    }
+    template <bool FAR>
+    __device__ __forceinline__ void finish(float about, float2 avg) const
+    {
+        const float rstd = rstd_of(avg.x, avg.y, FAR ? far_eps(a.eps) : a.eps), shift = shift_of(avg.x, rstd);
 #pragma unroll 2
         for (uint32_t i = threadIdx.x * K<T>; i < a.cols; i += kThreads * K<T>) {
             float2 v[kPairs], w[kPairs], b[kPairs];
@@ -113,14 +138,43 @@ __global__ void __launch_bounds__(kThreads) k_norm_any(const NormArgs a, const b
             load_weights<T, VEC>(a.weight, w16, i, a.cols - i, 1.f, w);
             load_weights<T, VEC>(a.bias, w16, i, a.cols - i, 0.f, b);
             if (a.sum) store<T, VEC>((T *)a.sum + t * a.ld_sum + i, a.cols - i, v);
+            shrink<FAR>(v);
 #pragma unroll
             for (uint32_t k = 0; k < kPairs; ++k) v[k] = scaled(__fadd2_rn(v[k], both(-about)), both(rstd), both(shift), w[k], b[k]);
             store<T, VEC>((T *)a.out + t * a.ld_out + i, a.cols - i, v);
         }
         if (threadIdx.x == 0) {
-            if (a.mean) a.mean[t] = about + left;
-            if (a.rstd) a.rstd[t] = rstd;
+            if (a.mean) a.mean[t] = FAR ? __fmul_rn(about + avg.x, kUnit) : about + avg.x;
+            if (a.rstd) a.rstd[t] = FAR ? far_rstd(rstd, avg, a.eps) : rstd;
         }
+    }
+};
+
+// (a function of its own: in line it took registers from the rows that never come here)
+template <typename T, bool VEC>
+__device__ __noinline__ void far_row(const NormArgs &a, uint64_t t, bool w16, float2 *part, float per)
+{
+    const Row<T, VEC> row(a, t, w16, part);
+    const float about = row.template sum<true>() * per;
+    const float2 s = row.template squares<true>(about);
+    row.template finish<true>(about, make_float2(s.x * per, s.y * per));
+}
+
+// (three blocks an SM in fp32: 134 M elements in rows of 20000 306 us with two, 277 with three)
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 3 : 2) k_norm_any(const __grid_constant__ NormArgs a, const bool w16)
+{
+    __shared__ float2 part[kThreads / 32];
+    previous_done();
+    next_may_start();
+    const float per = 1.f / (float)a.cols;
+    for (uint64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
+        const Row<T, VEC> row(a, t, w16, part);
+        const float about = row.template sum<false>() * per;
+        const float2 s = row.template squares<false>(about);
+        // (for all threads; the vote tells the compiler that a warp stays together)
+        if (kFarRows<T> && __builtin_expect(__any_sync(0xFFFFFFFFu, infinite(s.y)), 0)) far_row<T, VEC>(a, t, w16, part, per);
+        else row.template finish<false>(about, make_float2(s.x * per, s.y * per));
     }
 }
 

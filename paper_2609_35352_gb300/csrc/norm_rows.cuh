@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
                 if (!VEC && a.sum) ring.put(1, e, narrowed<T>(s[e]));
             }
         }
-        const float about = row_sum<LANES>(sum.x + sum.y, part, 0) * per;
+        const float about = about_of<T>(row_sum<LANES>(sum.x + sum.y, part, 0) * per);
         // (the sum has used all that was read: its places may be filled again)
         if (VEC) fetch(ring.now), ring.next();
         else x += step_x, res += step_res;
@@ -265,7 +265,30 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
                 }
         }
         const float2 sums = row_sum<LANES>(make_float2(s1.x + s1.y, s2.x + s2.y), part, 1);
-        const float left = sums.x * per, rstd = rstd_of(left, sums.y * per, a.eps), shift = shift_of(left, rstd);
+        float left = sums.x * per, rstd = rstd_of(left, sums.y * per, a.eps), mean = about + left, rstd_out = rstd;
+        // (for all threads of the row; the vote tells the compiler that a warp stays together)
+        if (kFarRows<T> && __builtin_expect(__any_sync(0xFFFFFFFFu, infinite(sums.y)), 0)) {
+            auto each = [&](auto f) {
+#pragma unroll
+                for (uint32_t e = 0; e < VECS; ++e)
+                    if (inside(e * LANES * K<T> + at))
+#pragma unroll
+                        for (uint32_t i = 0; i < K<T> / 2; ++i) f(s[e][i], e * LANES * K<T> + at + 2 * i);
+            };
+            sum = s1 = s2 = both(0.f);
+            each([&](float2 &d, uint32_t) { d = __fmul2_rn(d, both(kPerUnit)), sum = __fadd2_rn(sum, d); });
+            row_barrier<LANES>();  // (before the slots of sums are written again)
+            const float more = row_sum<LANES>(sum.x + sum.y, part, 0) * per;
+            each([&](float2 &d, uint32_t col) {
+                d = __fadd2_rn(d, both(-more));
+                if (!VEC) d = inside_only(d, col, a.cols);
+                s1 = __fadd2_rn(s1, d), s2 = __ffma2_rn(d, d, s2);
+            });
+            const float2 again = row_sum<LANES>(make_float2(s1.x + s1.y, s2.x + s2.y), part, 1), avg = make_float2(again.x * per, again.y * per);
+            left = avg.x, rstd = rstd_of(avg.x, avg.y, far_eps(a.eps));
+            mean = __fmul_rn(__fadd_rn(__fmul_rn(about, kPerUnit), more) + left, kUnit), rstd_out = far_rstd(rstd, avg, a.eps);
+        }
+        const float shift = shift_of(left, rstd);
 #pragma unroll
         for (uint32_t e = 0; e < VECS; ++e) {
             const uint32_t col = e * LANES * K<T> + at;
@@ -288,8 +311,8 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
             row_barrier<LANES>();  // (before the next row comes)
         }
         if (lane == 0) {
-            if (a.mean) a.mean[t] = about + left;
-            if (a.rstd) a.rstd[t] = rstd;
+            if (a.mean) a.mean[t] = mean;
+            if (a.rstd) a.rstd[t] = rstd_out;
         }
     }
 }

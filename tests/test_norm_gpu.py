@@ -437,3 +437,40 @@ def test_gradient_of_flat_rows_far_from_zero(ctx, dtype, cols):
         got = call(extra)
         check_all(dtype, dtype, got, NU.backward(f64(dy), f64(s), f64(mean), f64(rstd), f64(weight), f64(extra)))
         assert all(torch.equal(got[k][good], before[k][good]) for k in ("dx", "dresidual"))
+
+
+@pytest.mark.parametrize("dtype,wtype", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("cols", [1, 3, 8, 100, 512, 777, 1024, 2048, 4096, 5000, 8192, 16384, 17000, 20001])
+def test_finite_rows_past_the_range_of_sums(ctx, dtype, wtype, cols):
+    """Rows of finite values whose sum, squares or distances from the mean pass fp32's range come
+    out by the formula (the bound of its rounding is that of any row), others as without them."""
+    weight, bias = vector(cols, wtype, 3, 0.2, 1.0), vector(cols, wtype, 4)
+    for drop, res, scale in ((None, None, 1.0), (AD.Dropout(0.5, 9), make(12, cols, dtype, 0, 2), 0.25)):
+        x = make(12, cols, dtype, 0, 1)
+        clean = run_forward(ctx, x, res, weight, bias, 1e-5, drop)
+        signs = torch.where(torch.arange(cols, device="cuda") % 2 == 0, 1.0, -1.0)
+        first = torch.where(torch.arange(cols, device="cuda") == 0, -1.0, 1.0)
+        noise = make(1, cols, "f32", 0, 5)[0]
+        far = {1: torch.full((cols,), 1e38, device="cuda"), 2: noise * 3e37, 4: signs * 3.3e38, 5: first * 3.3e38, 6: noise * 1e25,
+               8: noise * 1e18, 9: torch.full((cols,), torch.finfo(DT[dtype]).min, device="cuda"), 11: noise * 1e37 - 1e38}
+        for t, row in far.items():
+            x[t] = (row * scale).to(DT[dtype])
+        assert torch.isfinite(x).all()
+        got = run_forward(ctx, x, res, weight, bias, 1e-5, drop)
+        check_all(dtype, wtype, got, NU.forward(f64(x), f64(res), f64(weight), f64(bias), 1e-5, spec(drop)))
+        good = [t for t in range(12) if t not in far]
+        assert all(torch.equal(got[k][good], clean[k][good]) for k in got)
+        plain = torch.empty_like(x)
+        LN.layer_norm(ctx, x, plain, weight=weight, bias=bias, residual=res, dropout=drop)
+        assert torch.equal(plain, got["out"])
+        # alone, and with rows of an infinity or a NaN beside them
+        for t in (2, 4, 6):
+            d = None if drop is None else drop.advance(t, cols)
+            one = run_forward(ctx, x[t:t + 1], None if res is None else res[t:t + 1], weight, bias, 1e-5, d)
+            assert all(torch.equal(one[k], got[k][t:t + 1]) for k in got)
+        if drop is None:
+            x[0, cols - 1], x[3, 0] = float("inf"), float("nan")
+            bad = run_forward(ctx, x, None, weight, bias, 1e-5, None)
+            assert torch.isnan(bad["out"][[0, 3]]).all() and torch.isnan(bad["rstd"][[0, 3]]).all()
+            rest = [t for t in range(12) if t not in (0, 3)]
+            assert all(torch.equal(bad[k][rest], got[k][rest]) for k in got)
