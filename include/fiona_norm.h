@@ -60,7 +60,7 @@ typedef struct fiona_layer_norm_call {
     uint32_t cols; /* 1 .. 2^20 */
     uint32_t dtype, weight_dtype;
     uint32_t reserved; /* must be 0 */
-    double eps;        /* 0, or from 2^-126 on; finite */
+    double eps;        /* 0, or from 2^-126 to fp32's largest */
     const void *weight, *bias;
     const void *x;
     uint64_t ldx;

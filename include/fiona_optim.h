@@ -84,8 +84,8 @@ typedef struct fiona_adamw_tensor {
 
 typedef struct fiona_adamw_group {
     double beta1, beta2;  /* [0, 1) */
-    double eps;           /* 0, or from 2^-126 on; finite */
-    double weight_decay;  /* finite */
+    double eps;           /* 0, or from 2^-126 to fp32's largest */
+    double weight_decay;  /* finite in fp32 */
     double max_norm;      /* above 0; infinity: no clipping */
 } fiona_adamw_group;
 

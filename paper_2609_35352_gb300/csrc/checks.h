@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "dropout.cuh"
 #include "fiona_adapter.h"
@@ -22,9 +23,12 @@ inline uint64_t element(uint32_t dtype) { return dtype == FIONA_F32 ? 4 : 2; }
 
 inline uint64_t align_up(uint64_t n) { return (n + 255) & ~255ull; }
 
+// whether fp32 holds a setting, rather than taking it for infinite
+inline bool held(double v) { return std::fabs(v) <= std::numeric_limits<float>::max(); }
+
 // whether an eps is none, or one that fp32 holds (a smaller one would be zero in a kernel, and
 // divide zeros by zeros where the formula does not)
-inline bool normal(double eps) { return eps == 0.0 || (eps >= 0x1p-126 && std::isfinite(eps)); }
+inline bool normal(double eps) { return eps == 0.0 || (eps >= 0x1p-126 && held(eps)); }
 
 // A strided matrix of one call.
 struct View {

@@ -54,7 +54,7 @@ extern "C" int fiona_layer_norm(const fiona_ctx *ctx, void *stream, const fiona_
     const char *who = "layer_norm";
     int rc = check_shape(ctx, c, who);
     if (rc) return rc;
-    if (!normal(c->eps)) return set_error(FIONA_ERR_ARG, "%s: eps is negative, not finite, or below 2^-126 and not 0", who);
+    if (!normal(c->eps)) return set_error(FIONA_ERR_ARG, "%s: eps is negative, past fp32, or below 2^-126 and not 0", who);
     NormArgs a{};
     if ((rc = make_mask(&c->drop, c->cols, a.mask, who)) || c->rows == 0) return rc;
     const uint64_t e = element(c->dtype), we = element(c->weight_dtype), rows = c->rows, cols = c->cols;

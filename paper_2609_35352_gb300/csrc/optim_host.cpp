@@ -117,7 +117,7 @@ extern "C" int fiona_adamw_create(const fiona_ctx *ctx, uint32_t n, const fiona_
     for (uint32_t i = 0; i < n_groups; ++i) {
         const fiona_adamw_group &g = groups[i];
         if (!(g.beta1 >= 0 && g.beta1 < 1 && g.beta2 >= 0 && g.beta2 < 1 && normal(g.eps)) ||
-            !std::isfinite(g.weight_decay) || !(g.max_norm > 0))
+            !held(g.weight_decay) || !(g.max_norm > 0))
             return set_error(FIONA_ERR_ARG, "%s: group %u: beta outside [0, 1), eps negative, or eps, weight decay or max_norm out of range", who, i);
         if (std::isfinite(g.max_norm) && !s.norms) return set_error(FIONA_ERR_ARG, "%s: group %u is clipped, but norms is NULL", who, i);
     }

@@ -222,3 +222,12 @@ def test_binding(ctx, monkeypatch):
                 dict(work=work, dsum=aligned(6, 40, dtype=torch.float16))):
         with pytest.raises((ValueError, F.FionaError)):
             LN.layer_norm_backward(ctx, x, out, f, f, **{"dweight": aligned(40), **bad})
+
+
+def test_eps_of_fp32(ctx):
+    """An eps that fp32 holds, and none that it would take for infinite."""
+    most = float(np.finfo(np.float32).max)
+    for eps in (1.0, 1e30, most, 2.0 ** -126):
+        assert Case(ctx, False).put(eps=eps) == NODEVICE, eps
+    for eps in (2.0 ** 128, 1e39, 1e300):
+        assert Case(ctx, False).put(eps=eps) == ARG, eps

@@ -240,3 +240,15 @@ def test_binding(ctx):
     with pytest.raises(F.FionaError) as e:  # the same tensor twice
         make(params=[one, one], grads=[torch.zeros(4, 100)] * 2)
     assert e.value.status == PLAN
+
+
+def test_settings_of_fp32(ctx):
+    """An eps and a weight decay that fp32 holds, and none that it would take for infinite."""
+    most = float(np.finfo(np.float32).max)
+    for k, fine, bad in (("eps", (2.0 ** -126, 1.0, most), (2.0 ** 128, 1e39, 1e300)),
+                         ("weight_decay", (most, -most, 1e-300), (2.0 ** 128, -1e39, 1e300))):
+        for values, rc in ((fine, F.FIONA_OK), (bad, ARG)):
+            for v in values:
+                c = Case(ctx, False)
+                setattr(c.g[1], k, v)
+                assert c() == rc, (k, v)
