@@ -83,7 +83,7 @@ int fiona_layer_norm(const fiona_ctx *ctx, void *cuda_stream, const fiona_layer_
 /* The gradient, from the sum, mean, rstd and drop of the forward pass.  NULL:
  * weight one, dsum zero; dx, dresidual, dweight, dbias not wanted.  dweight and
  * dbias are overwritten (with zero if there are no rows).  work: NULL will do where
- * neither dweight nor dbias is wanted and cols is at most 16384. */
+ * neither dweight nor dbias is wanted, cols is at most 16384, and rows fewer than 2^31. */
 typedef struct fiona_layer_norm_grad_call {
     uint64_t rows;
     uint32_t cols;

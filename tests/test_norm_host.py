@@ -231,3 +231,19 @@ def test_eps_of_fp32(ctx):
         assert Case(ctx, False).put(eps=eps) == NODEVICE, eps
     for eps in (2.0 ** 128, 1e39, 1e300):
         assert Case(ctx, False).put(eps=eps) == ARG, eps
+
+
+def test_workspace_of_very_many_rows(ctx):
+    """dx alone needs no workspace for fewer than 2^31 rows of up to 16384 columns; from there on
+    it needs what work_bytes says.  (Addresses are made up: they are checked, and nothing runs.)"""
+    for rows, cols, none in (((1 << 31) - 1, 8, True), (1 << 31, 8, False), (1 << 32, 1, False), (3, 16384, True), (3, 16385, False)):
+        c = Case(ctx, True)
+        c.put(rows=rows, cols=cols, dweight=None, dbias=None, dresidual=None, dsum=None, work=None, work_bytes=0)
+        for i, k in enumerate(("weight", "dy", "sum", "mean", "rstd", "dx")):
+            setattr(c.c, k, (i + 1) << 44)
+        for k in ("dy", "sum", "dx"):
+            setattr(c.c, "ldx" if k == "x" else "ld_" + k, cols)
+        assert c() == (NODEVICE if none else ARG), (rows, cols)
+        if not none:
+            assert "workspace" in F.last_error()
+            assert c.put(work=7 << 44, work_bytes=LN.work_bytes(ctx, rows, cols)) == NODEVICE
