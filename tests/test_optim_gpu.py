@@ -550,3 +550,27 @@ def test_norms_to_the_last_bit(ctx, dtype):
     # (squares are exact in 64 bits, and math.fsum has no error of its own)
     want = [math.sqrt(math.fsum((f64(g) ** 2).tolist())) for g in grads]
     assert np.array_equal(o.norms.cpu().numpy(), np.array(want, dtype=np.float32))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_last_of_many_elements(ctx, bits):
+    """Places past 32 bits, bit for bit: the last of 4.4e9 weights move as they would alone."""
+    n, k = (1 << 32) + 70000, 5000
+    if torch.cuda.mem_get_info()[0] < (90 << 30):
+        pytest.skip("90 GB of device memory")
+    p, g = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    first = (n - k) // 256 * 256
+    p[first:], g[first:] = normal((n - first,), torch.bfloat16, 1), normal((n - first,), torch.bfloat16, 2)
+    q, h = p[first:].clone(), g[first:].clone()
+    old = q.clone()
+    s = torch.cuda.current_stream()
+    o, alone = (O.AdamW(ctx, [w], [d], lr=0.1, state_bits=bits) for w, d in ((p, g), (q, h)))
+    for _ in range(2):
+        o.step(stream=s)
+        alone.step(stream=s)
+    assert float((q != old).float().mean()) > 0.99
+    assert torch.equal(p[first:], q)
+    for name in ("m", "v") + (("m_scale", "v_scale") if bits == 8 else ()):
+        end = getattr(alone, name)
+        assert torch.equal(getattr(o, name)[-end.numel():], end) and (end != 0).any(), name
+    assert (p[:1 << 20] == 0).all() and (o.m[:1 << 20] == 0).all()
