@@ -43,20 +43,10 @@ __device__ __forceinline__ float2 plus(float2 a, float2 b) { return make_float2(
 __device__ __forceinline__ float other(float v, uint32_t mask) { return __shfl_xor_sync(0xFFFFFFFFu, v, mask); }
 __device__ __forceinline__ float2 other(float2 v, uint32_t mask) { return make_float2(other(v.x, mask), other(v.y, mask)); }
 
-// The formulas element by element, each operation said outright, so that every kernel
-// and every path through one rounds in the same places (a compiler may fuse a product
-// and a sum here and not there).
-
-// what x becomes by the dropout (keep: by the mask) and the residual
-__device__ __forceinline__ float dropped(const dropout::Mask &m, float v, bool keep)
-{
-    return m.level == 0 ? v : keep ? __fmul_rn(v, m.factor) : 0.f;
-}
-// the same for element (t, i), read one at a time
-__device__ __forceinline__ float dropped(const dropout::Mask &m, float v, uint64_t t, uint32_t i)
-{
-    return dropped(m, v, m.level == 0 || m.keep(t, i));
-}
+// The formulas, each operation said outright, so that every kernel and every path through one
+// rounds in the same places (a compiler may fuse a product and a sum here and not there).  Most
+// are of two columns at once, by one instruction for both.  (No sum follows a product of pairs
+// but in an fma: a compiler may fuse the two, whatever their names say.)
 
 // A row's mean is `about + left`: the sum's share, and what its rounding left.
 // Averages below are of d = s - about.
@@ -87,33 +77,15 @@ __device__ __forceinline__ float far_rstd(float rstd, float2 avg, float eps)
     return __fmaf_rn(-avg.x, avg.x, avg.y) <= 0.f ? rsqrtf(eps) : __fmul_rn(rstd, kPerUnit);
 }
 
-// weight (d - left) rstd + bias
-__device__ __forceinline__ float shift_of(float left, float rstd) { return -__fmul_rn(left, rstd); }
-__device__ __forceinline__ float scaled(float d, float rstd, float shift, float weight, float bias)
-{
-    return __fmaf_rn(__fmaf_rn(d, rstd, shift), weight, bias);
-}
-
-__device__ __forceinline__ float xhat(float s, float mean, float rstd) { return __fmul_rn(__fsub_rn(s, mean), rstd); }
-
-// ds from g and xh, the row's averages of g and g xh, and dsum
-__device__ __forceinline__ float gradient(float g, float xh, float2 avg, float rstd)
-{
-    return __fmul_rn(rstd, __fmaf_rn(-xh, avg.y, __fsub_rn(g, avg.x)));
-}
-__device__ __forceinline__ float gradient(float g, float xh, float2 avg, float rstd, float dsum)
-{
-    return __fmaf_rn(rstd, __fmaf_rn(-xh, avg.y, __fsub_rn(g, avg.x)), dsum);
-}
-
-// The same for two columns at once, by one instruction for both.  (No sum follows a product
-// of pairs here but in an fma: a compiler may fuse the two, whatever their names say.)
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+// what x becomes by the dropout (keep: by the mask)
 __device__ __forceinline__ float2 dropped(const dropout::Mask &m, float2 v, bool keep_x, bool keep_y)
 {
     const float2 k = __fmul2_rn(v, both(m.factor));
     return make_float2(keep_x ? k.x : 0.f, keep_y ? k.y : 0.f);
 }
+// weight (d - left) rstd + bias
+__device__ __forceinline__ float shift_of(float left, float rstd) { return -__fmul_rn(left, rstd); }
 __device__ __forceinline__ float2 scaled(float2 d, float2 rstd, float2 shift, float2 weight, float2 bias)
 {
     return __ffma2_rn(__ffma2_rn(d, rstd, shift), weight, bias);
@@ -122,6 +94,7 @@ __device__ __forceinline__ float2 xhat(float2 s, float2 minus_mean, float2 rstd)
 // 0 in the place of columns past the last: (0 - mean) rstd may be infinite there, of a row of equal
 // values far from zero, whose own xh are 0
 __device__ __forceinline__ float2 inside_only(float2 xh, uint32_t col, uint32_t cols) { return make_float2(col < cols ? xh.x : 0.f, col + 1 < cols ? xh.y : 0.f); }
+// g - avg g - xh avg (g xh): ds is rstd times that, and dsum
 __device__ __forceinline__ float2 centred_gradient(float2 dy, float2 weight, float2 xh, float2 minus_avg_g, float2 minus_avg_gxh)
 {
     return __ffma2_rn(xh, minus_avg_gxh, __ffma2_rn(dy, weight, minus_avg_g));

@@ -501,14 +501,16 @@ int forward_rows(const fiona_ctx *ctx, void *stream, const NormArgs &a, bool w16
 {
     cudaStream_t s = (cudaStream_t)stream;
     constexpr uint32_t one = 8 / K<T>, two = 2 * one, four = 4 * one;  // eights of columns in vectors
-    switch (forward_lanes(a.cols, sizeof(T))) {
+    const uint32_t lanes = forward_lanes(a.cols, sizeof(T));
+    if constexpr (sizeof(T) == 2) {
         // (three: 87381 x 768 bf16 94 us for 103 by four, a vector of them empty; backward it gains
         // 2% in 16 bits and costs 5% in fp32)
-        case 32:
-            return a.cols <= 256   ? forward_rows<T, 32, one>(ctx, s, a, w16)
-                   : a.cols <= 512 ? forward_rows<T, 32, two>(ctx, s, a, w16)
-                   : a.cols <= 768 ? forward_rows<T, 32, 3 * one>(ctx, s, a, w16) : forward_rows<T, 32, four>(ctx, s, a, w16);
-        case 64: return forward_rows<T, 64, two>(ctx, s, a, w16);
+        if (lanes == 32 && a.cols > 512) return a.cols <= 768 ? forward_rows<T, 32, 3 * one>(ctx, s, a, w16) : forward_rows<T, 32, four>(ctx, s, a, w16);
+    } else {
+        if (lanes == 64) return forward_rows<T, 64, two>(ctx, s, a, w16);
+    }
+    switch (lanes) {
+        case 32: return a.cols <= 256 ? forward_rows<T, 32, one>(ctx, s, a, w16) : forward_rows<T, 32, two>(ctx, s, a, w16);
         case 128: return forward_rows<T, 128, two>(ctx, s, a, w16);
         case 256: return forward_rows<T, 256, two>(ctx, s, a, w16);
         case 512: return forward_rows<T, 512, two>(ctx, s, a, w16);
@@ -554,17 +556,19 @@ int backward_rows(const fiona_ctx *ctx, void *stream, const NormGradArgs &a, boo
 {
     cudaStream_t s = (cudaStream_t)stream;
     constexpr uint32_t one = 8 / K<T>, two = 2 * one, four = 4 * one;  // eights of columns in vectors
-    switch (backward_lanes(a.cols, sizeof(T))) {
+    const uint32_t lanes = backward_lanes(a.cols, sizeof(T));
+    if constexpr (sizeof(T) == 2) {
+        if (lanes == 256) return backward_rows<T, 256, four>(ctx, s, a, w16, blocks, part);
+    } else {
+        if (lanes == 512 && a.cols <= 8192) return backward_rows<T, 512, two>(ctx, s, a, w16, blocks, part);
+    }
+    switch (lanes) {
         case 32:
             return a.cols <= 256   ? backward_rows<T, 32, one>(ctx, s, a, w16, blocks, part)
                    : a.cols <= 512 ? backward_rows<T, 32, two>(ctx, s, a, w16, blocks, part) : backward_rows<T, 32, four>(ctx, s, a, w16, blocks, part);
         case 64: return backward_rows<T, 64, four>(ctx, s, a, w16, blocks, part);
         case 128: return backward_rows<T, 128, four>(ctx, s, a, w16, blocks, part);
-        case 256: return backward_rows<T, 256, four>(ctx, s, a, w16, blocks, part);
-        default:
-            if constexpr (sizeof(T) == 4)
-                if (a.cols <= 8192) return backward_rows<T, 512, two>(ctx, s, a, w16, blocks, part);
-            return backward_rows<T, 512, four>(ctx, s, a, w16, blocks, part);
+        default: return backward_rows<T, 512, four>(ctx, s, a, w16, blocks, part);
     }
 }
 
