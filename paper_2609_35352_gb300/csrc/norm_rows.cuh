@@ -171,8 +171,56 @@ __device__ __forceinline__ V row_sum(V v, float2 (*part)[32], uint32_t slot)
 // backward, 97 for 101).
 enum class Reach { elements, vectors, whole };
 
+// A far row that vectors cannot address, from memory, by the same steps as the kernel's other far
+// rows.  (With the row in registers it took them from the rows that never come here: 67108 x 250
+// fp32 with dropout 255 us for 146.)
+template <typename T, uint32_t LANES, uint32_t VECS>
+__device__ __forceinline__ void far_row(const NormArgs &a, uint64_t t, float about, bool w16, float2 (*part)[32])
+{
+    const uint32_t lane = threadIdx.x % LANES;
+    const float per = 1.f / (float)a.cols;
+    float more = 0.f, left = 0.f, rstd = 0.f;
+    auto s_of = [&](uint32_t col) {  // (0 behind the last column)
+        if (col >= a.cols) return 0.f;
+        float v = widen(((const T *)a.x)[t * a.ldx + col]);
+        if (a.mask.level) v = a.mask.keep(t, col) ? __fmul_rn(v, a.mask.factor) : 0.f;
+        return a.res ? __fadd_rn(v, widen(((const T *)a.res)[t * a.ld_res + col])) : v;
+    };
+    auto weight_of = [&](const void *p, uint32_t col, float none) { return !p ? none : w16 ? widen(((const T *)p)[col]) : ((const float *)p)[col]; };
+    auto finish = [&](uint32_t col, float s, float d) {
+        if (col >= a.cols) return;
+        if (a.sum) ((T *)a.sum)[t * a.ld_sum + col] = narrow<T>(s);
+        const float y = __fmaf_rn(__fmaf_rn(d, rstd, shift_of(left, rstd)), weight_of(a.weight, col, 1.f), weight_of(a.bias, col, 0.f));
+        ((T *)a.out)[t * a.ld_out + col] = narrow<T>(y);
+    };
+    row_barrier<LANES>();  // (before the slots of sums are written again)
+#pragma unroll 1
+    for (uint32_t round = 0; round < 3; ++round) {  // the mean; squares about it; the outputs
+        float2 s1 = both(0.f), s2 = both(0.f);
+#pragma unroll 1
+        for (uint32_t i = 0; i < VECS * (K<T> / 2); ++i) {
+            const uint32_t col = (i / (K<T> / 2) * LANES + lane) * K<T> + i % (K<T> / 2) * 2;
+            const float2 s = make_float2(s_of(col), s_of(col + 1));
+            float2 d = __fmul2_rn(__fadd2_rn(s, both(-about)), both(kPerUnit));
+            if (round) d = __fadd2_rn(d, both(-more));
+            d = inside_only(d, col, a.cols);
+            s1 = __fadd2_rn(s1, d), s2 = __ffma2_rn(d, d, s2);
+            if (round == 2) finish(col, s.x, d.x), finish(col + 1, s.y, d.y);
+        }
+        if (round == 0) more = row_sum<LANES>(s1.x + s1.y, part, 0) * per;
+        if (round == 1) {
+            const float2 sums = row_sum<LANES>(make_float2(s1.x + s1.y, s2.x + s2.y), part, 1), avg = make_float2(sums.x * per, sums.y * per);
+            left = avg.x, rstd = rstd_of(avg.x, avg.y, far_eps(a.eps));
+            if (lane == 0 && a.mean) a.mean[t] = __fmul_rn(__fadd_rn(__fmul_rn(about, kPerUnit), more) + left, kUnit);
+            if (lane == 0 && a.rstd) a.rstd[t] = far_rstd(rstd, avg, a.eps);
+        }
+    }
+}
+
+// (Rows by elements, up to 16 columns a thread: 64 registers, with which the 1024 threads an SM that
+// the grid counts on run at once.  4097 x 4095 fp32 with dropout: 77 us, with 119 registers 105.)
 template <typename T, uint32_t LANES, uint32_t VECS, Reach REACH>
-__global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const NormArgs a, const bool w16)
+__global__ void __launch_bounds__(forward_threads(LANES), REACH == Reach::elements && VECS * K<T> <= 16 ? 1024 / forward_threads(LANES) : 0) k_norm_rows(const __grid_constant__ NormArgs a, const bool w16)
 {
     constexpr uint32_t kThreads = forward_threads(LANES), kGroups = kThreads / LANES;
     constexpr bool VEC = REACH != Reach::elements;
@@ -268,20 +316,23 @@ __global__ void __launch_bounds__(forward_threads(LANES)) k_norm_rows(const Norm
         float left = sums.x * per, rstd = rstd_of(left, sums.y * per, a.eps), mean = about + left, rstd_out = rstd;
         // (for all threads of the row; the vote tells the compiler that a warp stays together)
         if (kFarRows<T> && __builtin_expect(__any_sync(0xFFFFFFFFu, infinite(sums.y)), 0)) {
+            if constexpr (!VEC) {
+                far_row<T, LANES, VECS>(a, t, about, w16, part);  // (nothing of the row has been written so far)
+                continue;
+            }
             auto each = [&](auto f) {
 #pragma unroll
                 for (uint32_t e = 0; e < VECS; ++e)
                     if (inside(e * LANES * K<T> + at))
 #pragma unroll
-                        for (uint32_t i = 0; i < K<T> / 2; ++i) f(s[e][i], e * LANES * K<T> + at + 2 * i);
+                        for (uint32_t i = 0; i < K<T> / 2; ++i) f(s[e][i]);
             };
             sum = s1 = s2 = both(0.f);
-            each([&](float2 &d, uint32_t) { d = __fmul2_rn(d, both(kPerUnit)), sum = __fadd2_rn(sum, d); });
+            each([&](float2 &d) { d = __fmul2_rn(d, both(kPerUnit)), sum = __fadd2_rn(sum, d); });
             row_barrier<LANES>();  // (before the slots of sums are written again)
             const float more = row_sum<LANES>(sum.x + sum.y, part, 0) * per;
-            each([&](float2 &d, uint32_t col) {
+            each([&](float2 &d) {
                 d = __fadd2_rn(d, both(-more));
-                if (!VEC) d = inside_only(d, col, a.cols);
                 s1 = __fadd2_rn(s1, d), s2 = __ffma2_rn(d, d, s2);
             });
             const float2 again = row_sum<LANES>(make_float2(s1.x + s1.y, s2.x + s2.y), part, 1), avg = make_float2(again.x * per, again.y * per);

@@ -474,3 +474,30 @@ def test_finite_rows_past_the_range_of_sums(ctx, dtype, wtype, cols):
             assert torch.isnan(bad["out"][[0, 3]]).all() and torch.isnan(bad["rstd"][[0, 3]]).all()
             rest = [t for t in range(12) if t not in (0, 3)]
             assert all(torch.equal(bad[k][rest], got[k][rest]) for k in got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [64, 256, 512, 768, 1024, 2048, 4096, 8192, 16384, 20000])
+def test_far_rows_by_any_path(ctx, dtype, cols):
+    """Rows past the range of sums: to the last bit the same off 16 bytes and in place of the inputs."""
+    src, res = make(7, cols, dtype, 0, 1), make(7, cols, dtype, 0, 2)
+    src[1], src[2], src[4] = (src[1].float() * 3e37).to(DT[dtype]), (src[2].float() * 1e25).to(DT[dtype]), 1e38
+    src[5, 1::2] = -3e38
+    weight, bias, drop = vector(cols, "f32", 3, 0.2, 1.0), vector(cols, "f32", 4), AD.Dropout(0.25, 3)
+    results = []
+    for off in (0, 1, 8):
+        def place(t):
+            wide = torch.zeros(7, cols + 2 * off, dtype=t.dtype, device="cuda")
+            wide[:, off:off + cols] = t
+            return wide[:, off:off + cols]
+
+        for in_place in (False, True):
+            x, r = place(src), place(res)
+            out, total = (r, x) if in_place else (place(src), place(src))
+            mean, rstd = torch.empty(7, device="cuda"), torch.empty(7, device="cuda")
+            LN.layer_norm(ctx, x, out, weight=weight, bias=bias, residual=r, dropout=drop, sum=total, mean=mean, rstd=rstd)
+            results.append((out, total, mean, rstd))
+    finite = torch.isfinite(results[0][1]).all(1)  # (what is kept grows by the dropout's factor)
+    assert finite.sum() >= 6 and torch.isfinite(results[0][0][finite]).all() and torch.isfinite(results[0][3][finite]).all()
+    for r in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip((t[finite] for t in r), (t[finite] for t in results[0])))
