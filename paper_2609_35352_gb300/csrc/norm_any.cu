@@ -7,9 +7,9 @@
 // make dx and dresidual and keep the sums of dweight and dbias in registers; the
 // runs' sums are added up in order (k_grad_sum).  dy and sum are read twice.
 //
-// 134 M elements in rows of 32768, bf16: forward with the sum 160 us (5.0 TB/s), backward
-// 314 us (4.3 TB/s with the second reading; element by element, not in vectors, 272 and 575).
-// Rows of 2^20, of which these are 128, leave SMs idle: 438 and 882 us.
+// 134 M elements in rows of 32768, bf16: forward with the sum 162 us (5.0 TB/s), backward
+// 301 us (4.5 TB/s with the second reading; element by element, not in vectors, 272 and 575).
+// Rows of 2^20, of which these are 128, leave SMs idle: 440 and 505 us.
 #include <algorithm>
 
 #include "norm.cuh"

@@ -2,10 +2,14 @@
 //
 // Bound by HBM: forward x, residual, out and sum once, backward dy, sum, dx and
 // dresidual (and dsum) once.  16384 x 4096 bf16 with dropout, 537 MB either way: forward
-// 82 us (6.5 TB/s, of 6.8 that a copy reaches), backward with dweight and dbias 97 us (5.5;
+// 84 us (6.4 TB/s, of 6.8 that a copy reaches), backward with dweight and dbias 98 us (5.5;
 // warps issue 58% of the time, 10 of 36 instructions an element for the mask, and 16 warps
 // an SM hide no more of a row's chain of sums); 4096 x 8192 fp32 backward 94 us (5.7: its
 // rows ahead leave room for one block an SM).
+//
+// The same by columns of 4095, which vectors cannot address: bf16 229 and 297 us, fp32 280 and 373
+// with a floor of 159 (a load, a store and two passes through shared memory an element, and no
+// row ahead).  Comparisons below are older than the test for far rows (1 us of the 84).
 //
 // A row is spread over LANES threads, 8 to 32
 // columns each; a block walks over rows a grid apart.  Rows ahead come by 16-byte
@@ -30,8 +34,10 @@ constexpr uint32_t ahead(uint32_t row_bytes, uint32_t tensors, uint32_t room, ui
     return most == 1 || row_bytes * tensors * most <= room ? most : ahead(row_bytes, tensors, room, most - 1);
 }
 
-// Rows ahead in a backward pass (16384 x 4096 bf16 97 us; one 115, three 99), their room beside
-// the weights, for rows of up to `cols`, and whether the weights have room beside them.
+// Rows ahead in a backward pass at most (16384 x 4096 bf16 97 us; one 115, three 99), their room
+// beside the weights, for rows of up to `cols`, and whether the weights have room beside them.
+// fp32 rows of 513 to 4096 columns have room for one: 32 columns a thread are twice the bytes there
+// (16384 x 4096 with dropout 173 us, 87381 x 768 169, with a floor of 159).
 constexpr uint32_t kGradAhead = 2;
 constexpr uint32_t grad_room(uint32_t cols, uint32_t size) { return backward_blocks(cols, size) > 1 ? 96 * 1024 : cols <= 8192 ? 192 * 1024 : 128 * 1024; }
 constexpr bool held_grad_weights(uint32_t cols, uint32_t size) { return size == 2 || cols <= 8192; }

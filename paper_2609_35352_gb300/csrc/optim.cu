@@ -8,10 +8,11 @@
 // 1024 elements of one tensor, in blocks of 256, so that tensors of any size share a grid
 // and a block of 8-bit moments finds its largest value within a warp.
 //
-// 403 M weights in bf16 with masters and norms: 1785 us, 6.8 TB/s of the 12.1 GB with the
-// gradients' second reading.  201 M in 8 bits without masters and norms: a step 391 us
-// (5.1 TB/s of 2.0 GB; its instructions keep the schedulers 70% busy), the moments read and
-// written out as bf16 163 us.  One launch for a step in place of two or three, each warp making its own
+// 403 M weights in bf16 with masters and norms: 1789 us, 6.8 TB/s of the 12.1 GB with the
+// gradients' second reading.  201 M in 8 bits without masters and norms: a step 378 us
+// (5.3 TB/s of 2.0 GB; its instructions keep the schedulers 71% busy), the moments read and
+// written out as bf16 175 us, and made of fp32 values 344 us (a warp a block of 256, m and v one
+// after another; HBM would take 297).  One launch for a step in place of two or three, each warp making its own
 // rates and the last block counting the step, took 4.4 us for 3.3 on one small model and 15%
 // more in 8 bits: what a call's first kernel may read ahead of its wait is nothing.
 #include <cuda_runtime.h>
