@@ -201,20 +201,20 @@ __device__ __forceinline__ void far_row(const NormArgs &a, uint64_t t, float abo
     };
     row_barrier<LANES>();  // (before the slots of sums are written again)
 #pragma unroll 1
-    for (uint32_t round = 0; round < 3; ++round) {  // the mean; squares about it; the outputs
+    for (uint32_t pass = 0; pass < 3; ++pass) {  // the mean; squares about it; the outputs
         float2 s1 = both(0.f), s2 = both(0.f);
 #pragma unroll 1
         for (uint32_t i = 0; i < VECS * (K<T> / 2); ++i) {
             const uint32_t col = (i / (K<T> / 2) * LANES + lane) * K<T> + i % (K<T> / 2) * 2;
             const float2 s = make_float2(s_of(col), s_of(col + 1));
             float2 d = __fmul2_rn(__fadd2_rn(s, both(-about)), both(kPerUnit));
-            if (round) d = __fadd2_rn(d, both(-more));
+            if (pass) d = __fadd2_rn(d, both(-more));
             d = inside_only(d, col, a.cols);
             s1 = __fadd2_rn(s1, d), s2 = __ffma2_rn(d, d, s2);
-            if (round == 2) finish(col, s.x, d.x), finish(col + 1, s.y, d.y);
+            if (pass == 2) finish(col, s.x, d.x), finish(col + 1, s.y, d.y);
         }
-        if (round == 0) more = row_sum<LANES>(s1.x + s1.y, part, 0) * per;
-        if (round == 1) {
+        if (pass == 0) more = row_sum<LANES>(s1.x + s1.y, part, 0) * per;
+        if (pass == 1) {
             const float2 sums = row_sum<LANES>(make_float2(s1.x + s1.y, s2.x + s2.y), part, 1), avg = make_float2(sums.x * per, sums.y * per);
             left = avg.x, rstd = rstd_of(avg.x, avg.y, far_eps(a.eps));
             if (lane == 0 && a.mean) a.mean[t] = __fmul_rn(__fadd_rn(__fmul_rn(about, kPerUnit), more) + left, kUnit);
